@@ -655,6 +655,202 @@ const char* kv_status_string(kvx_status status);
 
 int kv_abi_version(void);
 
+/*
+ * ---------------------------------------------------------------- operators
+ *
+ * What a replica runs on its pages and state slots between a restore and the
+ * next store (Sec. 2.2: the K/V pages of the attention layers and the recurrent
+ * state of the others).  All take a context, are enqueued on `stream` and
+ * allocate nothing, so they may be captured into CUDA graphs; lengths, tables
+ * and slots are read on the device, so a replayed graph follows them.  Argument
+ * errors return before anything is enqueued.  Sums, softmax statistics and
+ * states are held in 32 bits.  Tensors are device memory of ctx's GPU, 16-byte
+ * aligned unless an entry says otherwise, with a contiguous innermost dimension
+ * and the other strides given in elements (strides that 16-byte vectors cannot
+ * follow are KVX_EALIGN).  Inputs and outputs of a call must not overlap unless
+ * the call says so.
+ */
+typedef enum {
+  KVX_TYPE_BF16 = 0,
+  KVX_TYPE_FP16 = 1,
+  KVX_TYPE_E4M3 = 2 /* 8-bit float, a cache's only: value = stored * scale */
+} kvx_type;
+
+/* The sequences of one step and where their tokens lie in a pool. */
+typedef struct {
+  const int32_t* block_tables; /* device [num_seqs][table_stride]: entry i names
+                                  the pages of tokens [i*P*B, (i+1)*P*B)         */
+  int64_t table_stride;
+  int64_t table_len;           /* entries of a row (<= table_stride unless there
+                                  is one row)                                    */
+  const int32_t* lengths;      /* device [num_seqs]: tokens each cache holds, the
+                                  ones of this step included; 0: an idle place    */
+  int32_t num_seqs;
+  int64_t max_length;          /* no length is above this; 0: table_len * P * B.
+                                  A longer (or negative) one counts as this (or
+                                  0) and is reported as block table_len by
+                                  kv_get_device_error                            */
+} kvx_batch;
+
+/* New tokens' keys and values: rows [tokens][heads][head_dim]. */
+typedef struct {
+  int32_t type;         /* KVX_TYPE_BF16 or _FP16                               */
+  int32_t cache_type;   /* the same, or KVX_TYPE_E4M3                           */
+  int64_t tokens;       /* rows                                                 */
+  int32_t new_tokens;   /* starts NULL: rows of every sequence                  */
+  const int32_t* starts;/* device [num_seqs + 1]: rows [starts[s], starts[s+1])
+                           are sequence s's, or NULL                            */
+  int64_t key_token_stride, key_head_stride, value_token_stride, value_head_stride;
+  float k_scale, v_scale; /* KVX_TYPE_E4M3: stored = x / scale rounded to nearest
+                             even and clamped to +-448; 0 means 1                */
+} kvx_new_rows;
+
+/*
+ * Put the K/V of the newest tokens of every sequence into layer `layer`'s pages:
+ * a sequence with n new rows gets them at positions lengths[s]-n .. lengths[s]-1
+ * (rows before position 0 are dropped).  A token whose table entry is out of
+ * range is not written and is reported by kv_get_device_error.
+ */
+kvx_status kv_append(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch,
+                     const kvx_new_rows* rows, const void* key, const void* value, kvx_stream_t stream);
+
+/*
+ * Attention of each sequence's last new_tokens positions over its pages.  With
+ * q head i reading KV head i / (q_heads / num_heads), for the query at position p:
+ *   s_j = scale * (q . k_j);  s_j = softcap * tanh(s_j / softcap) if softcap > 0;
+ *   s_j += slopes[i] * (j - p) if slopes;   j <= p, and j > p - window if window > 0
+ *   out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j).
+ * A query that sees no key (a position before 0, an idle place) gets out = 0 and
+ * lse = -inf.  A key whose table entry is out of range is left out and reported.
+ * Positions count the cache's tokens: after an eviction they are its slots.
+ */
+typedef struct {
+  int32_t type;         /* of q and out: KVX_TYPE_BF16 or _FP16                 */
+  int32_t cache_type;   /* the same, or KVX_TYPE_E4M3                           */
+  int32_t q_heads;      /* a multiple of the pool's heads                       */
+  int32_t new_tokens;   /* 1 .. 64                                              */
+  float scale;          /* 0: 1 / sqrt(head_dim)                                */
+  float softcap;        /* 0: none                                              */
+  float k_scale, v_scale; /* of an e4m3 cache; 0 means 1                        */
+  int32_t window;       /* 0: none                                              */
+  const float* slopes;  /* device [q_heads], or NULL                            */
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+                        /* rows: token s * new_tokens + i is the i-th of sequence s */
+  float* lse;           /* device [num_seqs * new_tokens][q_heads], or NULL     */
+  float* weights;       /* device [num_seqs][num_heads][>= longest length], or
+                           NULL: weights[s][h][j] += the attention probability of
+                           key j, summed over the heads and tokens that read it */
+  int64_t weights_seq_stride, weights_head_stride;
+} kvx_attention;
+#define KVX_ATTEND_MAX_NEW_TOKENS 64
+
+/* Bytes of device workspace that kv_attend needs for these shapes (more with
+   attention->weights, whose scores are kept until the softmax sums are known).
+   It must be zero before its first use; every call leaves it fit for the next.
+   One call uses it at a time: calls that may overlap need one each.            */
+kvx_status kv_attend_workspace(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch,
+                               const kvx_attention* attention, int64_t* bytes);
+kvx_status kv_attend(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch,
+                     const kvx_attention* attention, const void* q, void* out, void* workspace,
+                     int64_t workspace_bytes, kvx_stream_t stream);
+
+/*
+ * Shrink caches to `budget` tokens: in every layer of the pool, for every
+ * sequence and KV head, keep the first `sinks` tokens, the last `recent` and, of
+ * the others, those with the largest weights (what kv_attend accumulated; equal
+ * ones: the lowest position; NaN counts as -inf).  Their K and V are copied in
+ * their order to the pages that new_tables names; the old pages are not changed
+ * (other sequences may share them) and are the caller's to free.  A sequence of
+ * at most `budget` tokens keeps all.  The pages of new_tables must not be among
+ * those of the block tables.
+ */
+typedef struct {
+  int32_t budget;          /* >= 1, sinks + recent <= budget                     */
+  int32_t sinks, recent;
+  const float* weights;    /* device [num_layers][num_seqs][num_heads][>= longest]
+                              4-byte aligned                                     */
+  int64_t weights_layer_stride, weights_seq_stride, weights_head_stride;
+  const int32_t* new_tables; /* device [num_seqs][new_table_stride]              */
+  int64_t new_table_stride, new_table_len;
+  int32_t* kept;           /* device [num_layers][num_seqs][num_heads][budget]: the
+                              kept positions, ascending, -1 behind the last      */
+  int32_t* new_lengths;    /* device [num_seqs]: min(length, budget)             */
+  float* new_weights;      /* device, the kept tokens' weights, or NULL (what lies
+                              behind the last is not written)                    */
+  int64_t new_weights_layer_stride, new_weights_seq_stride, new_weights_head_stride;
+} kvx_eviction;
+kvx_status kv_evict(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch, const kvx_eviction* eviction,
+                    kvx_stream_t stream);
+
+/*
+ * One recurrent layer's state slots, as kv_state_store / kv_state_load move them:
+ * slot i is slot_bytes at base + i * slot_bytes and holds, at recurrent_offset,
+ * fp32 [heads][head_dim][state_dim] and, at conv_offset, the convolution's past
+ * inputs [width - 1][channels], oldest first.
+ */
+typedef struct {
+  void* base;
+  int64_t num_slots, slot_bytes, recurrent_offset, conv_offset; /* bytes, multiples of 16 */
+} kvx_state;
+
+/* The sequences of one step over a state layer.  A sequence whose slot is out of
+   range gets zeros and leaves no state; kv_get_device_error then tells the lowest
+   such sequence. */
+typedef struct {
+  int32_t num_seqs;
+  const int32_t* slots_in;  /* device [num_seqs]: the slot each state is read from */
+  const int32_t* slots_out; /* device [num_seqs]: and written to (may be the same
+                               slot; another sequence's is a caller error)        */
+  const int32_t* fresh;     /* device [num_seqs], nonzero: begin from zeros; or NULL */
+  const int32_t* starts;    /* device [num_seqs + 1]: rows [starts[s], starts[s+1])
+                               are sequence s's, or NULL: row s                   */
+  int64_t tokens;           /* rows; num_seqs without starts                     */
+} kvx_state_batch;
+
+/*
+ * Short causal convolution of every channel over the last `width` inputs:
+ *   y_t = bias + sum_j weight[c][j] * x[t - width + 1 + j],  out = y * sigmoid(y) if silu.
+ * The inputs before a sequence's first row come from its slot (zeros if fresh),
+ * which keeps the last width - 1 inputs.
+ */
+typedef struct {
+  int32_t type;       /* KVX_TYPE_BF16 or _FP16: x, weight, bias, out, window     */
+  int32_t channels;   /* a multiple of 8                                        */
+  int32_t width;      /* 2 .. 4                                                 */
+  int32_t silu;
+  const void* weight; /* device [channels][width]                               */
+  const void* bias;   /* device [channels], or NULL                             */
+  int64_t x_stride, out_stride;
+} kvx_conv;
+kvx_status kv_state_conv(kvx_ctx* ctx, const kvx_state* state, const kvx_state_batch* batch, const kvx_conv* conv,
+                         const void* x, void* out, kvx_stream_t stream);
+
+/*
+ * Selective state space scan, one decay per head and token.  With
+ * d_t = dt_t + dt_bias (softplus of it if softplus is set), B and C of group
+ * h / (heads / groups):
+ *   h_t = exp(d_t A) h_{t-1} + d_t x_t B_t^T   (head_dim x state_dim, fp32)
+ *   out_t = h_t C_t + D x_t
+ */
+typedef struct {
+  int32_t type;       /* KVX_TYPE_BF16 or _FP16: x, dt, B, C, out                 */
+  int32_t heads;
+  int32_t head_dim;   /* a multiple of 8, at most 256                           */
+  int32_t state_dim;  /* 16, 32, 64, 128 or 256                                 */
+  int32_t groups;     /* of B and C; divides heads                              */
+  int32_t softplus;
+  const float* A;       /* device [heads]                                       */
+  const float* D;       /* device [heads], or NULL                              */
+  const float* dt_bias; /* device [heads], or NULL                              */
+  int64_t x_token_stride, x_head_stride, dt_token_stride, b_token_stride, b_group_stride, c_token_stride,
+      c_group_stride, out_token_stride, out_head_stride;
+} kvx_scan;
+/* Device workspace of kv_state_scan (0 for one token of every sequence).       */
+kvx_status kv_state_scan_workspace(kvx_ctx* ctx, const kvx_state_batch* batch, const kvx_scan* scan, int64_t* bytes);
+kvx_status kv_state_scan(kvx_ctx* ctx, const kvx_state* state, const kvx_state_batch* batch, const kvx_scan* scan,
+                         const void* x, const void* dt, const void* B, const void* C, void* out, void* workspace,
+                         int64_t workspace_bytes, kvx_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -182,6 +182,40 @@ void touch_before_transfer(void* const* chunks, const std::vector<int32_t>& toke
 
 // Records the last CUDA error seen by this thread (kv_last_cuda_error).
 void set_last_cuda_error(int e);
+void record_cuda_error(int e, const char* call, int line);
+
+// What the operators' translation unit (operators.cu) uses of a context.
+struct CtxView {
+  int device, num_sms;
+  long long* err;  // device error word: lowest bad logical block (or sequence)
+};
+CtxView view_of(const kvx_ctx* ctx);
+void count_launches(kvx_ctx* ctx, int n);
+kvx_status check_shape(const kvx_pool* P, Geometry* g);
+kvx_status check_stream(cudaStream_t s, int device);
+// Device memory of `device` at [p, p + bytes), by one driver query for each
+// plain allocation: a call's buffers share few, so the last ones are kept for
+// the length of the call.
+class DeviceMemory {
+ public:
+  explicit DeviceMemory(int device) : device_(device) {}
+  kvx_status check(const void* p, int64_t bytes);
+
+ private:
+  static constexpr int kKept = 6;
+  int device_, next_ = 0;
+  const uint8_t *begin_[kKept] = {}, *end_[kKept] = {};
+};
+// Makes `device` current for a scope and the caller's device again after it.
+class CurrentDevice {
+ public:
+  explicit CurrentDevice(int device);
+  ~CurrentDevice();
+  bool ok = false;
+
+ private:
+  int prev_ = -1;
+};
 
 // Host-side fault injection (kv_fault_inject): true if the armed point fails now.
 bool fault_point(const char* point);

@@ -781,6 +781,42 @@ void push_job(MoveParams* p, uint8_t* chunk_side, int64_t first_page, int32_t to
 
 int64_t chunk_bytes(const kvx_pool* P, const Geometry& g, int64_t tokens) { return chunk_bytes_of(P, g, tokens); }
 
+CtxView view_of(const kvx_ctx* ctx) { return {ctx->device, ctx->num_sms, ctx->d_err}; }
+
+void count_launches(kvx_ctx* ctx, int n) {
+  std::lock_guard<std::mutex> lock(ctx->mu);
+  ctx->launches += n;
+}
+
+kvx_status check_shape(const kvx_pool* P, Geometry* g) { return check_pool_shape(P, g); }
+kvx_status check_stream(cudaStream_t s, int device) { return check_stream_device(s, device); }
+
+kvx_status DeviceMemory::check(const void* p, int64_t bytes) {
+  if (!p) return KVX_EINVAL;
+  const uint8_t* b = (const uint8_t*)p;
+  for (int i = 0; i < kKept; ++i)
+    if (b >= begin_[i] && b < end_[i] && bytes <= end_[i] - b) return KVX_OK;
+  const uint8_t *begin = nullptr, *end = nullptr;
+  if (!plain_allocation(device_, b, &begin, &end) || bytes > end - b) return check_device_range(device_, b, bytes);
+  begin_[next_] = begin;
+  end_[next_] = end;
+  next_ = (next_ + 1) % kKept;
+  return KVX_OK;
+}
+
+CurrentDevice::CurrentDevice(int device) {
+  if (cudaGetDevice(&prev_) != cudaSuccess) {
+    cudaGetLastError();
+    prev_ = -1;
+  }
+  ok = prev_ == device || cudaSetDevice(device) == cudaSuccess;
+  if (!ok) cudaGetLastError();
+  if (prev_ == device) prev_ = -1;  // nothing to restore
+}
+CurrentDevice::~CurrentDevice() {
+  if (prev_ >= 0) cudaSetDevice(prev_);
+}
+
 }  // namespace kvx
 
 namespace {

@@ -1,0 +1,171 @@
+// operators.cuh -- what the operators' kernels share: a batch's view of one
+// layer's pages, element types, and the launchers operators.cu calls.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "kvx_internal.h"
+
+namespace kvx {
+
+// One layer's pages as a batch's block tables name them.
+struct PagesView {
+  uint8_t* base;
+  const int32_t* tables;
+  const int32_t* lengths;
+  long long* err;
+  int64_t table_stride, page_bytes;
+  int64_t half_bytes;               // K half of a page; the V half follows
+  int64_t token_bytes, head_bytes;  // from a token / head of a page half to the next
+  FastDiv by_block, by_pack;        // tokens per page, pages per logical block
+  uint32_t entries;                 // valid table entries are below this
+  uint32_t table_len;
+  int32_t heads, head_dim, num_seqs;
+  int32_t max_length;               // longer sequences count as this
+};
+
+struct AppendParams {
+  PagesView pages;
+  const uint8_t *key, *value;
+  const int32_t* starts;
+  int64_t tokens;
+  int64_t key_token, key_head, value_token, value_head;  // strides in bytes
+  int32_t new_tokens, num_seqs;
+  float k_scale, v_scale;
+};
+
+struct AttendParams {
+  PagesView pages;
+  const uint8_t* q;
+  uint8_t* out;
+  float *lse, *weights;
+  const float* slopes;
+  int64_t q_token, q_head, out_token, out_head;  // strides in bytes
+  int64_t weights_seq, weights_head;             // strides in elements
+  int32_t q_heads, group, new_tokens, window;
+  float scale, softcap, k_scale, v_scale;
+};
+
+struct EvictParams {
+  PagesView pages;                // base is not used
+  uint8_t* layer_base[KVX_MAX_LAYERS];
+  const float* weights;
+  const int32_t* new_tables;
+  int32_t *kept, *new_lengths;
+  float* new_weights;
+  int64_t weights_layer, weights_seq, weights_head;              // strides in elements
+  int64_t new_weights_layer, new_weights_seq, new_weights_head;
+  int64_t new_table_stride;
+  uint32_t new_table_len;
+  int32_t budget, sinks, recent, num_layers;
+};
+static_assert(sizeof(EvictParams) <= 4096, "kernel parameters");
+
+struct StateView {
+  uint8_t* base;
+  const int32_t *slots_in, *slots_out, *fresh, *starts;
+  long long* err;
+  int64_t num_slots, slot_bytes, offset;  // offset: of the part the kernel works on
+  int64_t tokens;
+  int32_t num_seqs;
+};
+
+struct ConvParams {
+  StateView state;
+  const uint8_t *x, *weight, *bias;
+  uint8_t* out;
+  int64_t x_stride, out_stride;  // in elements
+  int32_t channels, width, silu;
+};
+
+struct ScanParams {
+  StateView state;
+  const uint8_t *x, *dt, *b, *c;
+  uint8_t* out;
+  const float *A, *D, *dt_bias;
+  int64_t x_token, x_head, dt_token, b_token, b_group, c_token, c_group, out_token, out_head;  // in elements
+  int32_t heads, head_dim, state_dim, heads_per_group, softplus;
+};
+
+cudaError_t launch_append(const AppendParams& p, int type, int cache_type, cudaStream_t s);
+cudaError_t launch_attend(const AttendParams& p, int type, int cache_type, cudaStream_t s);
+cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
+cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s);
+cudaError_t launch_scan(const ScanParams& p, int type, cudaStream_t s);
+
+#ifdef __CUDACC__
+namespace {
+
+struct Bf16 {
+  using T = __nv_bfloat16;
+  static __device__ __forceinline__ float up(T v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ T down(float v) { return __float2bfloat16_rn(v); }
+};
+struct Fp16 {
+  using T = __half;
+  static __device__ __forceinline__ float up(T v) { return __half2float(v); }
+  static __device__ __forceinline__ T down(float v) { return __float2half_rn(v); }
+};
+struct E4m3 {
+  using T = __nv_fp8_e4m3;
+  static __device__ __forceinline__ float up(T v) { return (float)v; }
+};
+
+__device__ __forceinline__ uint32_t fdiv(const FastDiv& f, uint32_t n) {
+  return f.d > 1 ? (uint32_t)__umul64hi(f.m, n) : n;
+}
+
+// Tokens that sequence `s` holds, between 0 and max_length.
+__device__ __forceinline__ int32_t length_of(const PagesView& v, int32_t s) {
+  return min(max(v.lengths[s], 0), v.max_length);
+}
+
+// Byte offset from the layer's base of head 0 of the K row at `pos`, or -1 for a
+// table entry that names no page (reported as its logical block).
+__device__ __forceinline__ int64_t row_offset(const PagesView& v, const int32_t* table, uint32_t table_len,
+                                              uint32_t pos) {
+  const uint32_t page = fdiv(v.by_block, pos), slot = pos - page * v.by_block.d;
+  const uint32_t block = fdiv(v.by_pack, page), sub = page - block * v.by_pack.d;
+  const uint32_t entry = block < table_len ? (uint32_t)__ldg(table + block) : UINT32_MAX;
+  if (entry >= v.entries) {
+    atomicMin(v.err, (long long)block);
+    return -1;
+  }
+  return ((int64_t)entry * v.by_pack.d + sub) * v.page_bytes + slot * v.token_bytes;
+}
+
+// Reports a length outside [0, max_length] (one thread of a launch calls it per sequence).
+__device__ __forceinline__ void check_length(const PagesView& v, int32_t s) {
+  const int32_t n = v.lengths[s];
+  if (n < 0 || n > v.max_length) atomicMin(v.err, (long long)v.table_len);
+}
+
+// The slot `slots[s]`, or null (and reported) where it is out of range.
+__device__ __forceinline__ uint8_t* slot_of(const StateView& v, const int32_t* slots, int32_t s) {
+  const int32_t i = slots[s];
+  if (i < 0 || i >= v.num_slots) {
+    atomicMin(v.err, (long long)s);
+    return nullptr;
+  }
+  return v.base + (int64_t)i * v.slot_bytes + v.offset;
+}
+
+// Rows of sequence s, cut to the rows there are.
+__device__ __forceinline__ void rows_of(const StateView& v, int32_t s, int64_t* first, int64_t* last) {
+  if (!v.starts) {
+    *first = s;
+    *last = s + 1;
+    return;
+  }
+  *first = min((int64_t)max(v.starts[s], 0), v.tokens);
+  *last = max(*first, min((int64_t)v.starts[s + 1], v.tokens));
+}
+
+}  // namespace
+#endif
+
+}  // namespace kvx

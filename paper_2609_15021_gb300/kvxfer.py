@@ -42,7 +42,11 @@ EXPORTED = (
     "kv_tier_acquire", "kv_tier_release", "kv_tier_acquire_many", "kv_tier_release_many", "kv_tier_prefix_hits", "kv_tier_stats", "kv_fault_inject",
     "kv_tier_open_shared", "kv_tier_poll", "kv_tier_reclaim", "kv_host_alloc_numa", "kv_host_alloc_ex",
     "kv_host_pool_info", "kv_host_touch", "kv_tier_wait",
+    "kv_append", "kv_attend", "kv_attend_workspace", "kv_evict", "kv_state_conv", "kv_state_scan",
+    "kv_state_scan_workspace",
 )
+KVX_TYPE_BF16, KVX_TYPE_FP16, KVX_TYPE_E4M3 = 0, 1, 2
+KVX_ATTEND_MAX_NEW_TOKENS = 64
 KVX_ENOENT, KVX_EBUSY = -8, -9
 KVX_TIER_CREATE, KVX_TIER_NO_PIN = 0x1, 0x2
 KVX_NO_STREAM = -1  # the handle value of KVX_NO_STREAM
@@ -84,6 +88,67 @@ class kvx_stats(ctypes.Structure):
     _fields_ = [("kernel_launches", ctypes.c_int64), ("memcpy_calls", ctypes.c_int64),
                 ("timed_launches", ctypes.c_int64 * 2), ("kernel_ms", ctypes.c_double * 2),
                 ("kernel_bytes", ctypes.c_int64 * 2)]
+
+
+class kvx_batch(ctypes.Structure):
+    _fields_ = [("block_tables", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("table_len", ctypes.c_int64),
+                ("lengths", ctypes.c_void_p), ("num_seqs", ctypes.c_int32), ("max_length", ctypes.c_int64)]
+
+
+class kvx_new_rows(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("cache_type", ctypes.c_int32), ("tokens", ctypes.c_int64),
+                ("new_tokens", ctypes.c_int32), ("starts", ctypes.c_void_p),
+                ("key_token_stride", ctypes.c_int64), ("key_head_stride", ctypes.c_int64),
+                ("value_token_stride", ctypes.c_int64), ("value_head_stride", ctypes.c_int64),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float)]
+
+
+class kvx_attention(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("cache_type", ctypes.c_int32), ("q_heads", ctypes.c_int32),
+                ("new_tokens", ctypes.c_int32), ("scale", ctypes.c_float), ("softcap", ctypes.c_float),
+                ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("window", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("lse", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("weights_seq_stride", ctypes.c_int64), ("weights_head_stride", ctypes.c_int64)]
+
+
+class kvx_eviction(ctypes.Structure):
+    _fields_ = [("budget", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("weights", ctypes.c_void_p), ("weights_layer_stride", ctypes.c_int64),
+                ("weights_seq_stride", ctypes.c_int64), ("weights_head_stride", ctypes.c_int64),
+                ("new_tables", ctypes.c_void_p), ("new_table_stride", ctypes.c_int64),
+                ("new_table_len", ctypes.c_int64), ("kept", ctypes.c_void_p), ("new_lengths", ctypes.c_void_p),
+                ("new_weights", ctypes.c_void_p), ("new_weights_layer_stride", ctypes.c_int64),
+                ("new_weights_seq_stride", ctypes.c_int64), ("new_weights_head_stride", ctypes.c_int64)]
+
+
+class kvx_state(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("num_slots", ctypes.c_int64), ("slot_bytes", ctypes.c_int64),
+                ("recurrent_offset", ctypes.c_int64), ("conv_offset", ctypes.c_int64)]
+
+
+class kvx_state_batch(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("slots_in", ctypes.c_void_p), ("slots_out", ctypes.c_void_p),
+                ("fresh", ctypes.c_void_p), ("starts", ctypes.c_void_p), ("tokens", ctypes.c_int64)]
+
+
+class kvx_conv(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("channels", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("silu", ctypes.c_int32), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
+class kvx_scan(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("state_dim", ctypes.c_int32), ("groups", ctypes.c_int32), ("softplus", ctypes.c_int32),
+                ("A", ctypes.c_void_p), ("D", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p),
+                ("x_token_stride", ctypes.c_int64), ("x_head_stride", ctypes.c_int64),
+                ("dt_token_stride", ctypes.c_int64),
+                ("b_token_stride", ctypes.c_int64), ("b_group_stride", ctypes.c_int64),
+                ("c_token_stride", ctypes.c_int64), ("c_group_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
 
 
 class kvx_tier_stats(ctypes.Structure):
@@ -139,6 +204,13 @@ def _declare(lib):
         "kv_tier_stats": (st, [vp, P(kvx_tier_stats)]),
         "kv_fault_inject": (st, [ctypes.c_char_p, i32]),
         "kv_host_touch": (st, [P(vp), P(i64), i64]),
+        "kv_append": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_new_rows), vp, vp, vp]),
+        "kv_attend_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_attention), P(i64)]),
+        "kv_attend": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_attention), vp, vp, vp, i64, vp]),
+        "kv_evict": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_eviction), vp]),
+        "kv_state_conv": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_conv), vp, vp, vp]),
+        "kv_state_scan_workspace": (st, [vp, P(kvx_state_batch), P(kvx_scan), P(i64)]),
+        "kv_state_scan": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_scan), vp, vp, vp, vp, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -620,6 +692,264 @@ def kv_abi_version() -> int:
 
 def kv_status_string(status: int) -> str:
     return _lib.kv_status_string(status).decode()
+
+
+# ---------------------------------------------------------------- operators
+
+
+_types: dict = {}
+
+
+def _type_of(dtype) -> int:
+    """KVX_TYPE_* of a torch dtype."""
+    if not _types:
+        import torch
+        _types.update({torch.bfloat16: KVX_TYPE_BF16, torch.float16: KVX_TYPE_FP16,
+                       torch.float8_e4m3fn: KVX_TYPE_E4M3})
+    try:
+        return _types[dtype]
+    except KeyError:
+        raise TypeError(f"{dtype} is none of bfloat16, float16 and float8_e4m3fn") from None
+
+
+def _cache_type(pool: KvPool, given) -> int:
+    """Type of a pool's elements: that of its tensors, or, where they are plain bytes, as given."""
+    return _type_of(pool.layers[0].dtype if given is None else given)
+
+
+def _need(x, what: str, dtype, shape=None) -> None:
+    """A tensor of `dtype` (and shape) whose innermost dimension is contiguous."""
+    if str(x.dtype) != "torch." + dtype:
+        raise TypeError(f"{what} must be {dtype}, not {x.dtype}")
+    if shape is not None and x.shape != shape:
+        raise ValueError(f"{what} is {tuple(x.shape)}, not {tuple(shape)}")
+    if x.dim() and x.shape[-1] > 1 and x.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+
+
+def _need_rows(x, what: str, dtype, shape) -> None:
+    if x.dtype != dtype:
+        raise TypeError(f"{what} must be {dtype}, not {x.dtype}")
+    if x.shape != shape:
+        raise ValueError(f"{what} is {tuple(x.shape)}, not {tuple(shape)}")
+    if x.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+
+
+class KvBatch:
+    """The sequences of a step: their block tables [sequences][entries] and lengths (device int32
+    tensors, read when the kernels run), with the description marshalled once.  max_length: no
+    length is above it (0: as many tokens as the tables hold)."""
+
+    def __init__(self, block_tables, lengths, max_length: int = 0):
+        if block_tables.dim() != 2:
+            raise ValueError("block_tables must be [sequences][entries]")
+        _need(block_tables, "block_tables", "int32")
+        _need(lengths, "lengths", "int32", (block_tables.shape[0],))
+        self.block_tables, self.lengths, self.num_seqs = block_tables, lengths, block_tables.shape[0]
+        self.max_length = max_length
+        self._c = kvx_batch(block_tables.data_ptr(), block_tables.stride(0), block_tables.shape[1],
+                            lengths.data_ptr(), self.num_seqs, max_length)
+
+    def _longest(self, pool: KvPool) -> int:
+        return self.max_length or self.block_tables.shape[1] * pool.block_tokens * max(1, pool.pages_per_block)
+
+
+def kv_append(ctx, pool: KvPool, layer: int, batch: KvBatch, key, value, new_tokens: int = 1, starts=None,
+              k_scale: float = 1.0, v_scale: float = 1.0, cache_dtype=None, stream=None) -> None:
+    """Put new tokens' key and value rows [tokens][heads][head_dim] into a layer's pages, as the last
+    tokens of their sequences: new_tokens of each, or (starts, a device int32 tensor) rows
+    starts[s] .. starts[s+1] of sequence s."""
+    shape = (key.shape[0] if starts is not None else batch.num_seqs * new_tokens, pool.num_heads, pool.head_dim)
+    _need_rows(key, "key", key.dtype, shape)
+    _need_rows(value, "value", key.dtype, shape)
+    if starts is not None:
+        _need(starts, "starts", "int32", (batch.num_seqs + 1,))
+    ks, vs = key.stride(), value.stride()
+    rows = kvx_new_rows(_type_of(key.dtype), _cache_type(pool, cache_dtype), shape[0], new_tokens,
+                        None if starts is None else starts.data_ptr(), ks[0], ks[1], vs[0], vs[1], k_scale, v_scale)
+    _check(_lib.kv_append(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(rows),
+                          key.data_ptr(), value.data_ptr(), _stream_handle(stream)), "kv_append")
+
+
+class KvAttention:
+    """What an attention computes, marshalled once: query heads, tokens of each sequence that attend,
+    scale (None: 1/sqrt(head_dim)), softcap, window, slopes (device float32 [q_heads]; a bias of
+    slope * distance) and the scales of an e4m3 cache."""
+
+    def __init__(self, q_heads: int, new_tokens: int = 1, scale: float | None = None, softcap: float = 0.0,
+                 window: int = 0, slopes=None, k_scale: float = 1.0, v_scale: float = 1.0, cache_dtype=None):
+        if slopes is not None:
+            _need(slopes, "slopes", "float32", (q_heads,))
+        self.q_heads, self.new_tokens, self.slopes, self.cache_dtype = q_heads, new_tokens, slopes, cache_dtype
+        self._c = kvx_attention(q_heads=q_heads, new_tokens=new_tokens, scale=scale or 0.0, softcap=softcap,
+                                window=window, slopes=None if slopes is None else slopes.data_ptr(),
+                                k_scale=k_scale, v_scale=v_scale)
+
+
+def kv_attend_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttention, weights: bool = False,
+                        dtype=None):
+    """A zeroed workspace tensor for kv_attend calls of these shapes (weights: that accumulate the
+    attention weights; dtype: the queries', where the cache's does not tell).  One call uses it at a time."""
+    import torch
+    c = kvx_attention.from_buffer_copy(attention._c)
+    c.cache_type = _cache_type(pool, attention.cache_dtype)
+    c.type = _type_of(dtype) if dtype is not None else KVX_TYPE_BF16 if c.cache_type == KVX_TYPE_E4M3 else c.cache_type
+    c.weights = 16 if weights else None  # only whether there are any matters here
+    out = ctypes.c_int64()
+    _check(_lib.kv_attend_workspace(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(c),
+                                    ctypes.byref(out)), "kv_attend_workspace")
+    return torch.zeros(max(16, out.value), dtype=torch.uint8, device=batch.lengths.device)
+
+
+def kv_attend(ctx, pool: KvPool, layer: int, batch: KvBatch, attention: KvAttention, query, out, workspace,
+              lse=None, weights=None, stream=None) -> None:
+    """Attention of every sequence's last new_tokens tokens over a layer's pages: query and out are
+    [sequences * new_tokens][q_heads][head_dim]; lse (float32 [sequences * new_tokens][q_heads])
+    gets the logarithms of the softmax sums; weights (float32 [sequences][heads][longest]) is added
+    the attention weight that every cached token got."""
+    shape = (batch.num_seqs * attention.new_tokens, attention.q_heads, pool.head_dim)
+    _need_rows(query, "query", query.dtype, shape)
+    _need_rows(out, "out", query.dtype, shape)
+    c = kvx_attention.from_buffer_copy(attention._c)
+    c.type = _type_of(query.dtype)
+    c.cache_type = _cache_type(pool, attention.cache_dtype)
+    c.q_token_stride, c.q_head_stride, _ = query.stride()
+    c.out_token_stride, c.out_head_stride, _ = out.stride()
+    if lse is not None:
+        _need(lse, "lse", "float32", shape[:2])
+        _check_tensor(lse, "lse")
+        c.lse = lse.data_ptr()
+    if weights is not None:
+        longest = batch._longest(pool)
+        if weights.dim() != 3 or weights.shape[-1] < longest:
+            raise ValueError(f"weights must be [sequences][heads][{longest} or more]")
+        _need(weights, "weights", "float32", (batch.num_seqs, pool.num_heads, weights.shape[-1]))
+        c.weights = weights.data_ptr()
+        c.weights_seq_stride, c.weights_head_stride, _ = weights.stride()
+    _check(_lib.kv_attend(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(c),
+                          query.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                          _stream_handle(stream)), "kv_attend")
+
+
+def kv_evict(ctx, pool: KvPool, batch: KvBatch, weights, budget: int, new_tables, kept, new_lengths,
+             new_weights=None, sinks: int = 0, recent: int = 0, stream=None) -> None:
+    """Keep `budget` tokens of every sequence in every layer and head of the pool: the first `sinks`,
+    the last `recent` and those of the largest weights (float32 [layers][sequences][heads][longest]),
+    copied in order into the pages of new_tables.  kept (int32 [layers][sequences][heads][budget]) gets
+    their positions, new_lengths (int32) the sequences' lengths, new_weights (float32, as kept) theirs."""
+    layers, s, h = len(pool.layers), batch.num_seqs, pool.num_heads
+    longest = batch._longest(pool)
+    if weights.dim() != 4 or weights.shape[-1] < longest:
+        raise ValueError(f"weights must be [layers][sequences][heads][{longest} or more]")
+    _need(weights, "weights", "float32", (layers, s, h, weights.shape[-1]))
+    if new_tables.dim() != 2:
+        raise ValueError("new_tables must be [sequences][entries]")
+    _need(new_tables, "new_tables", "int32", (s, new_tables.shape[1]))
+    _need(kept, "kept", "int32", (layers, s, h, budget))
+    _check_tensor(kept, "kept")
+    _need(new_lengths, "new_lengths", "int32", (s,))
+    e = kvx_eviction(budget, sinks, recent, weights.data_ptr(), *weights.stride()[:3], new_tables.data_ptr(),
+                     new_tables.stride(0), new_tables.shape[1], kept.data_ptr(), new_lengths.data_ptr())
+    if new_weights is not None:
+        _need(new_weights, "new_weights", "float32", (layers, s, h, budget))
+        e.new_weights = new_weights.data_ptr()
+        e.new_weights_layer_stride, e.new_weights_seq_stride, e.new_weights_head_stride, _ = new_weights.stride()
+    _check(_lib.kv_evict(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(e),
+                         _stream_handle(stream)), "kv_evict")
+
+
+class StateSlots:
+    """One recurrent layer's state slots (the buffer kv_state_store / kv_state_load move slots of),
+    and where a slot keeps the recurrent state and the convolution's window."""
+
+    def __init__(self, tensor, num_slots: int, slot_bytes: int, recurrent_offset: int = 0, conv_offset: int = 0):
+        _check_tensor(tensor, "state slots", num_slots * slot_bytes)
+        self.tensor = tensor
+        self._c = kvx_state(tensor.data_ptr(), num_slots, slot_bytes, recurrent_offset, conv_offset)
+
+
+class StateBatch:
+    """The sequences of a step over recurrent layers: the slots (device int32) their states are read
+    from and written to (None: the same), the rows of each (starts, device int32 [sequences + 1], of
+    `tokens` in all; None: one each) and which begin from zeros (fresh, device int32)."""
+
+    def __init__(self, slots_in, slots_out=None, starts=None, tokens: int | None = None, fresh=None):
+        n = slots_in.shape[0]
+        slots_out = slots_in if slots_out is None else slots_out
+        _need(slots_in, "slots_in", "int32", (n,))
+        _need(slots_out, "slots_out", "int32", (n,))
+        if starts is not None:
+            _need(starts, "starts", "int32", (n + 1,))
+            if tokens is None:
+                raise ValueError("tokens (the rows of all sequences) must be given with starts")
+        elif tokens not in (None, n):
+            raise ValueError("without starts every sequence has one row")
+        if fresh is not None:
+            _need(fresh, "fresh", "int32", (n,))
+        self.num_seqs, self.tokens = n, n if starts is None else tokens
+        self._tensors = slots_in, slots_out, starts, fresh  # kept while their addresses are
+        self._c = kvx_state_batch(n, slots_in.data_ptr(), slots_out.data_ptr(),
+                                  None if fresh is None else fresh.data_ptr(),
+                                  None if starts is None else starts.data_ptr(), self.tokens)
+
+
+def kv_state_conv(ctx, state: StateSlots, batch: StateBatch, x, weight, out, bias=None, silu: bool = True,
+                  stream=None) -> None:
+    """Causal convolution of x [tokens][channels] with weight [channels][width], the inputs before a
+    sequence's first row taken from its slot, which keeps the last width - 1 inputs."""
+    channels, width = weight.shape
+    _need_rows(x, "x", weight.dtype, (batch.tokens, channels))
+    _need_rows(out, "out", weight.dtype, (batch.tokens, channels))
+    _check_tensor(weight, "weight")
+    if bias is not None:
+        _need_rows(bias, "bias", weight.dtype, (channels,))
+    c = kvx_conv(_type_of(weight.dtype), channels, width, silu, weight.data_ptr(),
+                 None if bias is None else bias.data_ptr(), x.stride(0), out.stride(0))
+    _check(_lib.kv_state_conv(ctx, ctypes.byref(state._c), ctypes.byref(batch._c), ctypes.byref(c), x.data_ptr(),
+                              out.data_ptr(), _stream_handle(stream)), "kv_state_conv")
+
+
+def kv_state_scan_workspace(ctx, batch: StateBatch, heads: int, head_dim: int, state_dim: int):
+    """A workspace tensor for kv_state_scan calls of these shapes; one call uses it at a time."""
+    import torch
+    c = kvx_scan(heads=heads, head_dim=head_dim, state_dim=state_dim, groups=1)
+    out = ctypes.c_int64()
+    _check(_lib.kv_state_scan_workspace(ctx, ctypes.byref(batch._c), ctypes.byref(c), ctypes.byref(out)),
+           "kv_state_scan_workspace")
+    return torch.empty(max(16, out.value), dtype=torch.uint8, device=batch._tensors[0].device)
+
+
+def kv_state_scan(ctx, state: StateSlots, batch: StateBatch, x, dt, A, B, C, out, D=None, dt_bias=None,
+                  softplus: bool = True, workspace=None, stream=None) -> None:
+    """Selective scan of x [tokens][heads][head_dim] with dt [tokens][heads], B and C
+    [tokens][groups][state_dim], A, D and dt_bias [heads] (float32), on the state in each sequence's
+    slot.  workspace: from kv_state_scan_workspace (None: none is needed for one token of each sequence)."""
+    t, heads, head_dim = x.shape
+    groups, state_dim = B.shape[1:]
+    _need_rows(x, "x", x.dtype, (batch.tokens, heads, head_dim))
+    _need_rows(out, "out", x.dtype, x.shape)
+    _need_rows(B, "B", x.dtype, (t, groups, state_dim))
+    _need_rows(C, "C", x.dtype, B.shape)
+    _need_rows(dt, "dt", x.dtype, (t, heads))
+    c = kvx_scan(_type_of(x.dtype), heads, head_dim, state_dim, groups, softplus, A.data_ptr())
+    _need(A, "A", "float32", (heads,))
+    if D is not None:
+        _need(D, "D", "float32", (heads,))
+        c.D = D.data_ptr()
+    if dt_bias is not None:
+        _need(dt_bias, "dt_bias", "float32", (heads,))
+        c.dt_bias = dt_bias.data_ptr()
+    c.x_token_stride, c.x_head_stride, _ = x.stride()
+    c.dt_token_stride = dt.stride(0)
+    c.b_token_stride, c.b_group_stride, _ = B.stride()
+    c.c_token_stride, c.c_group_stride, _ = C.stride()
+    c.out_token_stride, c.out_head_stride, _ = out.stride()
+    _check(_lib.kv_state_scan(ctx, ctypes.byref(state._c), ctypes.byref(batch._c), ctypes.byref(c), x.data_ptr(),
+                              dt.data_ptr(), B.data_ptr(), C.data_ptr(), out.data_ptr(),
+                              None if workspace is None else workspace.data_ptr(),
+                              0 if workspace is None else workspace.numel(), _stream_handle(stream)),
+           "kv_state_scan")
 
 
 # ---------------------------------------------------------------- convenience

@@ -1,0 +1,357 @@
+"""kv_state_conv and kv_state_scan against token-by-token 64-bit recurrences."""
+import math
+
+import pytest
+import torch
+
+import operator_refs as refs
+from gpu_util import kvx
+
+pytestmark = pytest.mark.gpu
+
+BF16, FP16 = torch.bfloat16, torch.float16
+
+
+def normal(shape, dtype, seed, scale=1.0):
+    return (torch.randn(shape, generator=torch.Generator().manual_seed(seed)) * scale).to(dtype)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    k = kvx()
+    c = k.kv_ctx_create(0)
+    yield c
+    k.kv_ctx_destroy(c)
+
+
+class Slots:
+    """Slots of a recurrent state and a window each, all of random numbers, on the CPU and the GPU."""
+
+    def __init__(self, n, heads=1, p=8, state=16, width=4, channels=8, dtype=BF16, seed=1):
+        k = kvx()
+        self.rec, self.win = heads * p * state * 4, (width - 1) * channels * 2
+        self.bytes = -(-(self.rec + self.win) // 256) * 256 + 256
+        self.n, self.dtype = n, dtype
+        self.cpu = torch.zeros((n, self.bytes), dtype=torch.uint8)
+        self.state = self.cpu[:, :self.rec].view(torch.float32).view(n, heads, p, state)
+        self.window = self.cpu[:, self.rec:self.rec + self.win].view(dtype).view(n, width - 1, channels)
+        self.state.copy_(normal(self.state.shape, torch.float32, seed))
+        self.window.copy_(normal(self.window.shape, dtype, seed + 1))
+        self.cpu[:, self.rec + self.win:] = 0xA5  # padding that nothing may touch
+        self.dev = self.cpu.cuda()
+        self.slots = k.StateSlots(self.dev, n, self.bytes, recurrent_offset=0, conv_offset=self.rec)
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def batch_of(lens, slots_in, slots_out=None, fresh=None, single=False):
+    k = kvx()
+    starts = [sum(lens[:i]) for i in range(len(lens) + 1)]
+    return k.StateBatch(ints(slots_in), None if slots_out is None else ints(slots_out),
+                        starts=None if single else ints(starts), tokens=starts[-1],
+                        fresh=None if fresh is None else ints(fresh)), starts
+
+
+def check_conv(ctx, lens, channels, width, dtype, bias=True, silu=True, single=False, in_place=False, fresh=None, stream=None):
+    k = kvx()
+    s = len(lens)
+    st = Slots(2 * s + 1, width=width, channels=channels, dtype=dtype)
+    ins = [(3 * i + 1) % (2 * s + 1) for i in range(s)] if in_place else list(range(s, 0, -1))
+    outs = ins if in_place else [s + 1 + i for i in range(s)]
+    if in_place and len(set(ins)) < s:
+        ins = outs = list(range(s))
+    batch, starts = batch_of(lens, ins, None if in_place else outs, fresh, single)
+    t = starts[-1]
+    wide = normal((t, channels + 24), dtype, 3)
+    x, w = wide[:, 8:8 + channels], normal((channels, width), dtype, 4, 0.6)
+    b = normal((channels,), dtype, 5) if bias else None
+    out = torch.full((t, channels + 8), 7.0, dtype=dtype, device="cuda")
+    dev = wide.cuda()
+    w_dev, b_dev = w.cuda(), None if b is None else b.cuda()
+    torch.cuda.synchronize()
+    k.kv_state_conv(ctx, st.slots, batch, dev[:, 8:8 + channels], w_dev, out[:, :channels], bias=b_dev, silu=silu, stream=stream)
+    torch.cuda.synchronize()
+    unit = refs.UNIT[dtype]
+    want = st.cpu.clone()
+    windows = want[:, st.rec:st.rec + st.win].view(dtype).view(st.n, width - 1, channels)
+    for i in range(s):
+        first = torch.zeros_like(st.window[0]).double() if fresh and fresh[i] else st.window[ins[i]].double()
+        rows = x[starts[i]:starts[i + 1]].double()
+        y, window = refs.conv(rows, w.double(), None if b is None else b.double(), first, silu)
+        size, _ = refs.conv(rows.abs(), w.double().abs(), None if b is None else b.double().abs(), first.abs(), False)
+        # a sum of width products and a bias in 32 bits, and y * sigmoid(y), whose slope is below 1.1; then one rounding
+        bound = unit * y.abs() + 2.0 ** -20 * size + 1e-7
+        got = out[starts[i]:starts[i + 1], :channels].cpu().double()
+        assert bool(((got - y).abs() <= bound).all()), i
+        windows[outs[i]] = window.to(dtype)
+    assert bool((out[:, channels:] == 7.0).all())
+    assert torch.equal(st.dev.cpu(), want)
+    assert k.kv_get_device_error(ctx) == -1
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("width", [2, 3, 4])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_conv_prompts(ctx, dtype, width, in_place):
+    check_conv(ctx, [0, 1, 2, 3, 70, 129, 600], 72, width, dtype, in_place=in_place)
+
+
+@pytest.mark.parametrize("channels", [8, 264, 2048, 8192])
+@pytest.mark.parametrize("seqs", [1, 5])
+def test_conv_single_tokens(ctx, channels, seqs):
+    check_conv(ctx, [1] * seqs, channels, 4, BF16, single=True)
+    check_conv(ctx, [1] * seqs, channels, 3, FP16, single=True, in_place=True, bias=False)
+
+
+@pytest.mark.parametrize("silu,bias", [(True, False), (False, True), (False, False)])
+def test_conv_options_and_fresh_sequences(ctx, silu, bias):
+    check_conv(ctx, [2, 5, 1, 40], 40, 4, BF16, silu=silu, bias=bias, fresh=[0, 1, 1, 0], stream=torch.cuda.Stream())
+
+
+def scan_inputs(t, heads, p, n, groups, dtype, seed=3, fast=False):
+    """fast: decays from none at all to one that forgets within a token."""
+    wide = normal((t, heads * p + 2 * groups * n + 8), dtype, seed)
+    x = wide[:, :heads * p].view(t, heads, p)
+    b = wide[:, heads * p:heads * p + groups * n].view(t, groups, n)
+    c = wide[:, heads * p + groups * n:heads * p + 2 * groups * n].view(t, groups, n)
+    g = torch.Generator().manual_seed(seed + 1)
+    dt = normal((t, heads), dtype, seed + 2, 3.0 if fast else 1.0)
+    A = -torch.exp(torch.rand(heads, generator=g) * (8.0 if fast else 2.5) - (5.0 if fast else 0.0))
+    return wide, x, b, c, dt, A, torch.randn(heads, generator=g), torch.randn(heads, generator=g) - 4.0
+
+
+def check_scan(ctx, lens, heads, p, n, groups, dtype, single=False, in_place=False, fresh=None, softplus=True, skip=True,
+               bias=True, fast=False, stream=None):
+    k = kvx()
+    s = len(lens)
+    st = Slots(2 * s + 1, heads, p, n, dtype=dtype)
+    ins = list(range(s)) if in_place else list(range(s, 0, -1))
+    outs = ins if in_place else [s + 1 + i for i in range(s)]
+    batch, starts = batch_of(lens, ins, None if in_place else outs, fresh, single)
+    t = starts[-1]
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, groups, dtype, fast=fast)
+    if not softplus:
+        dt = (dt.abs() * 0.02).to(dtype)
+    dev = wide.cuda()
+    dx = dev[:, :heads * p].view(t, heads, p)
+    db = dev[:, heads * p:heads * p + groups * n].view(t, groups, n)
+    dc = dev[:, heads * p + groups * n:heads * p + 2 * groups * n].view(t, groups, n)
+    out = torch.full((t, heads * p + 8), 7.0, dtype=dtype, device="cuda")
+    use_bias = bias and softplus
+    ws = k.kv_state_scan_workspace(ctx, batch, heads, p, n)
+    ws.fill_(0xFF)  # NaN: nothing of it may be read before it is written
+    args = dt.cuda(), A.cuda(), D.cuda() if skip else None, dt_bias.cuda() if use_bias else None
+    torch.cuda.synchronize()
+    k.kv_state_scan(ctx, st.slots, batch, dx, args[0], args[1], db, dc, out[:, :heads * p].view(t, heads, p), D=args[2],
+                    dt_bias=args[3], softplus=softplus, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+    unit = refs.UNIT[dtype]
+    got_state = st.dev.cpu()[:, :st.rec].view(torch.float32).view(st.state.shape)
+    untouched = st.cpu.clone()
+    for i in range(s):
+        rows = slice(starts[i], starts[i + 1])
+        first = torch.zeros_like(st.state[0]).double() if fresh and fresh[i] else st.state[ins[i]].double()
+        y, state, size, big = refs.scan(x[rows].double(), dt[rows].double(), A.double(), b[rows].double(), c[rows].double(),
+                                        D.double() if skip else None, dt_bias.double() if use_bias else None, softplus, first)
+        # Products of matrices round up to three factors of a term to the inputs' type (a pair's decayed product, a
+        # decayed input, a carried state); the rest is in 32 bits, with decays from exponents of up to some hundreds.
+        got = out[rows, :heads * p].view(-1, heads, p).cpu().double()
+        bound = unit * y.abs() + (3 * unit + 2.0 ** -13) * size + 1e-7
+        assert bool(((got - y).abs() <= bound).all()), (i, float(((got - y).abs() / bound).max()))
+        off = (got_state[outs[i]].double() - state).abs()
+        assert bool((off <= 2.0 ** -14 * big + 1e-9).all()), (i, float((off / (big + 1e-9)).max()))
+        untouched[outs[i], :st.rec] = st.dev.cpu()[outs[i], :st.rec]
+    assert bool((out[:, heads * p:] == 7.0).all())
+    assert torch.equal(st.dev.cpu(), untouched)
+    assert k.kv_get_device_error(ctx) == -1
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("p", [8, 64, 120, 128, 256])
+@pytest.mark.parametrize("n", [16, 32, 64, 128, 256])
+def test_scan_single_tokens(ctx, dtype, p, n):
+    check_scan(ctx, [1, 1, 1], 4, p, n, 2, dtype, single=True, in_place=n == 64)
+
+
+# lengths around the 64 and 128 tokens of a chunk, of one token and of none
+LENS = [0, 1, 2, 63, 64, 65, 127, 128, 129, 300]
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("p,n,heads,groups", [(64, 64, 2, 1), (64, 128, 4, 2), (128, 64, 3, 3), (128, 128, 2, 1)])
+def test_scan_prompts(ctx, dtype, p, n, heads, groups):
+    check_scan(ctx, LENS, heads, p, n, groups, dtype)
+    check_scan(ctx, [200, 5], heads, p, n, groups, dtype, in_place=True, fresh=[1, 0])
+
+
+@pytest.mark.parametrize("p,n", [(8, 16), (40, 32), (256, 64), (64, 256), (72, 128), (16, 16)])
+def test_scan_prompts_of_other_sizes(ctx, p, n):
+    check_scan(ctx, [0, 1, 40, 150], 2, p, n, 1, BF16)
+
+
+def test_scan_long_prompt(ctx):
+    check_scan(ctx, [1500, 700], 2, 128, 128, 1, BF16)
+
+
+@pytest.mark.parametrize("softplus,skip,bias", [(False, True, False), (True, False, True), (True, True, False), (False, False, False)])
+def test_scan_options(ctx, softplus, skip, bias):
+    check_scan(ctx, [150, 1, 30], 2, 64, 128, 1, BF16, softplus=softplus, skip=skip, bias=bias, stream=torch.cuda.Stream())
+
+
+def test_scan_of_fast_and_slow_decays(ctx):
+    """Heads that forget within a token beside heads that forget nothing: exponents of thousands over a chunk."""
+    check_scan(ctx, [260, 70], 8, 64, 64, 1, BF16, fast=True, bias=False)
+
+
+def test_fresh_sequences_do_not_read_their_slots(ctx):
+    """A fresh sequence's slot may hold anything, NaN too."""
+    k = kvx()
+    for lens, single in (([1, 1], True), ([130, 3], False)):
+        st = Slots(2, 2, 64, 64)
+        st.dev.fill_(0xFF)
+        batch, starts = batch_of(lens, [1, 0], fresh=[1, 1], single=single)
+        t = starts[-1]
+        wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, 2, 64, 64, 1, BF16)
+        out = torch.empty((t, 2, 64), dtype=BF16, device="cuda")
+        k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out,
+                        workspace=k.kv_state_scan_workspace(ctx, batch, 2, 64, 64))
+        cv = torch.empty((t, 8), dtype=BF16, device="cuda")
+        k.kv_state_conv(ctx, st.slots, batch, normal((t, 8), BF16, 8).cuda(), normal((8, 4), BF16, 9).cuda(), cv)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(cv).all())
+        assert bool(torch.isfinite(st.dev[:, :st.rec].view(torch.float32)).all())
+
+
+def test_token_by_token_is_the_prompt(ctx):
+    """A prompt in one call and its tokens one by one leave the same state within the bounds of both."""
+    k = kvx()
+    t, heads, p, n = 90, 2, 64, 64
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, BF16)
+    dev = [v.cuda() for v in (x, dt, A, b, c)]
+    st, one = Slots(1, heads, p, n), Slots(1, heads, p, n)
+    out, outs = torch.empty((t, heads, p), dtype=BF16, device="cuda"), torch.empty((t, heads, p), dtype=BF16, device="cuda")
+    batch, _ = batch_of([t], [0])
+    k.kv_state_scan(ctx, st.slots, batch, dev[0], dev[1], dev[2], dev[3], dev[4], out,
+                    workspace=k.kv_state_scan_workspace(ctx, batch, heads, p, n))
+    single = k.StateBatch(ints([0]))
+    for i in range(t):
+        r = slice(i, i + 1)
+        k.kv_state_scan(ctx, one.slots, single, dev[0][r], dev[1][r], dev[2], dev[3][r], dev[4][r], outs[r])
+    torch.cuda.synchronize()
+    _, _, size, big = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, True, st.state[0].double())
+    a = st.dev.cpu()[:, :st.rec].view(torch.float32).double().view(heads, p, n)
+    z = one.dev.cpu()[:, :st.rec].view(torch.float32).double().view(heads, p, n)
+    assert bool(((a - z).abs() <= 2.0 ** -13 * big + 1e-9).all())
+    assert bool(((out.cpu().double() - outs.cpu().double()).abs() <= 5 * refs.UNIT[BF16] * size + 1e-6).all())
+
+
+def test_bad_slots_give_zeros_and_are_reported(ctx):
+    k = kvx()
+    for lens, single in (([1, 1, 1], True), ([100, 70, 3], False)):
+        st = Slots(3, 2, 64, 64)
+        batch, starts = batch_of(lens, [0, 5, 1], [0, 1, -1], single=single)
+        t = starts[-1]
+        wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, 2, 64, 64, 1, BF16)
+        out = torch.full((t, 2, 64), math.nan, dtype=BF16, device="cuda")
+        k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out, D=D.cuda(),
+                        workspace=k.kv_state_scan_workspace(ctx, batch, 2, 64, 64))
+        cv = torch.full((t, 8), 7.0, dtype=BF16, device="cuda")
+        k.kv_state_conv(ctx, st.slots, batch, normal((t, 8), BF16, 8).cuda(), normal((8, 4), BF16, 9).cuda(), cv)
+        torch.cuda.synchronize()
+        assert bool((out[starts[1]:] == 0).all()) and bool((cv[starts[1]:] == 0).all())
+        assert bool(torch.isfinite(out[:starts[1]]).all())
+        assert torch.equal(st.dev.cpu()[1:], st.cpu[1:])
+        assert k.kv_get_device_error(ctx) == 1
+
+
+def test_captured_step(ctx):
+    """A captured convolution and scan of single tokens, replayed: the state moves on in its slot."""
+    k = kvx()
+    heads, p, n = 2, 64, 64
+    st = Slots(2, heads, p, n, channels=64)
+    batch = k.StateBatch(ints([1]))
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(3, heads, p, n, 1, BF16)
+    bufs = [v[:1].cuda() for v in (x, dt, b, c)]
+    cx, w = normal((3, 64), BF16, 8), normal((64, 4), BF16, 9)
+    cbuf, wd, Ad, out, cout = cx[:1].cuda(), w.cuda(), A.cuda(), torch.empty((1, heads, p), dtype=BF16, device="cuda"), torch.empty((1, 64), dtype=BF16, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        k.kv_state_conv(ctx, st.slots, batch, cbuf, wd, cout)
+        k.kv_state_scan(ctx, st.slots, batch, bufs[0], bufs[1], Ad, bufs[2], bufs[3], out)
+    y, state, size, big = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, True, st.state[1].double())
+    cy, window = refs.conv(cx.double(), w.double(), None, st.window[1].double(), True)
+    for i in range(3):
+        for buf, v in zip(bufs + [cbuf], (x, dt, b, c, cx)):
+            buf.copy_(v[i:i + 1])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bool(((out[0].cpu().double() - y[i]).abs() <= refs.UNIT[BF16] * y[i].abs() + 2.0 ** -13 * size[i] + 1e-7).all())
+        assert bool(((cout[0].cpu().double() - cy[i]).abs() <= refs.UNIT[BF16] * cy[i].abs() + 1e-5).all())
+    assert bool(((st.dev.cpu()[1, :st.rec].view(torch.float32).view(heads, p, n).double() - state).abs() <= 2.0 ** -14 * big).all())
+    assert torch.equal(st.dev.cpu()[1, st.rec:st.rec + st.win].view(BF16).view(3, 64).double(), window)
+    assert torch.equal(st.dev.cpu()[0], st.cpu[0])
+
+
+def test_slots_past_four_gib(ctx):
+    k = kvx()
+    slot = 64 << 10
+    n = (5 << 30) // slot
+    buf = torch.zeros(n * slot, dtype=torch.uint8, device="cuda")
+    slots = k.StateSlots(buf, n, slot, 0, 32 << 10)
+    batch = k.StateBatch(ints([n - 1]))
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(1, 2, 64, 64, 1, BF16)
+    out = torch.empty((1, 2, 64), dtype=BF16, device="cuda")
+    k.kv_state_scan(ctx, slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out)
+    torch.cuda.synchronize()
+    _, state, _, big = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, True,
+                                 torch.zeros((2, 64, 64), dtype=torch.float64))
+    got = buf.view(n, slot)[n - 1, :32 << 10].view(torch.float32).view(2, 64, 64).cpu().double()
+    assert bool(((got - state).abs() <= 2.0 ** -14 * big + 1e-9).all())
+    assert int(buf.view(n, slot)[:n - 1].max()) == 0
+
+
+def test_refusals(ctx):
+    k = kvx()
+    st = Slots(2, 2, 64, 64, channels=64)
+    batch = k.StateBatch(ints([0, 1]))
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(2, 2, 64, 64, 1, BF16)
+    x, b, c, dt, A = (v.cuda() for v in (x, b, c, dt, A))
+    out = torch.full((2, 2, 64), 7.0, dtype=BF16, device="cuda")
+
+    def scan(status, slots=st.slots, batch=batch, x=x, dt=dt, b=b, c=c, out=out, A=A, **kw):
+        with pytest.raises(k.KvxError) as e:
+            k.kv_state_scan(ctx, slots, batch, x, dt, A, b, c, out, **kw)
+        assert e.value.status == status, e.value
+
+    scan(k.KVX_EINVAL, b=b[..., :48], c=c[..., :48])
+    scan(k.KVX_EALIGN, x=x[..., :60], out=out[..., :60])
+    scan(k.KVX_ERANGE, slots=k.StateSlots(st.dev, 2, st.bytes, st.bytes - 16, 0))
+    scan(k.KVX_EALIGN, slots=k.StateSlots(st.dev, 2, st.bytes, 8, 0))
+    scan(k.KVX_EINVAL, slots=k.StateSlots(st.dev, 0, st.bytes, 0, 0))
+    scan(k.KVX_EDEVICE, x=x.cpu())
+    scan(k.KVX_EDEVICE, A=A.cpu())
+    scan(k.KVX_EINVAL, out=out[:1].expand(2, 2, 64))
+    w, xc = normal((64, 4), BF16, 9).cuda(), normal((2, 64), BF16, 8).cuda()
+    co = torch.full((2, 64), 7.0, dtype=BF16, device="cuda")
+
+    def conv(status, slots=st.slots, x=xc, w=w, out=co, **kw):
+        with pytest.raises(k.KvxError) as e:
+            k.kv_state_conv(ctx, slots, batch, x, w, out, **kw)
+        assert e.value.status == status, e.value
+
+    conv(k.KVX_EINVAL, w=torch.zeros((64, 5), dtype=BF16, device="cuda"))
+    conv(k.KVX_EALIGN, w=w[:60], x=xc[:, :60], out=co[:, :60])
+    conv(k.KVX_ERANGE, slots=k.StateSlots(st.dev, 2, st.bytes, 0, st.bytes - 16))
+    conv(k.KVX_EDEVICE, out=co.cpu())
+    assert bool((out == 7.0).all()) and bool((co == 7.0).all())
+    assert torch.equal(st.dev.cpu(), st.cpu)
+    with pytest.raises(ValueError):
+        k.StateBatch(ints([0]), starts=ints([0, 4]))
+    with pytest.raises(TypeError):
+        k.StateBatch(ints([0]).long())
+    with pytest.raises(ValueError):
+        k.kv_state_scan(ctx, st.slots, batch, x[:1], dt, A, b, c, out)
