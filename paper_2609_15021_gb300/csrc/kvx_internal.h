@@ -144,6 +144,8 @@ cudaError_t launch_move_tma(int dir, int layout, const MoveParams& p, int grid, 
 // Sets the TMA kernels' shared-memory limit for the current device (once per
 // context creation; never on the launch path).
 cudaError_t prepare_tma_kernels();
+// Shared-memory limits of the attention kernels (attend_kernels.cu), likewise.
+cudaError_t prepare_attend_kernels();
 // Tensor-map variant for HND pools: one TMA box per full page half.
 constexpr int kTensorMapBytes = 128;
 // Encodes one tensor map per layer of P (kTensorMapBytes each) into `out`;

@@ -154,6 +154,29 @@ kvx_status view_state(const CtxView& ctx, const kvx_state* s, const kvx_state_ba
   return KVX_OK;
 }
 
+// kv_attend's workspace.  The most CTAs a launch has are two an SM.
+struct AttendSpace {
+  int64_t counters, parts, row_lse2, scores, bytes;  // offsets, and all of it
+  int64_t score_stride;
+};
+AttendSpace attend_space(const CtxView& ctx, const PagesView& v, const kvx_attention* a) {
+  auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
+  const int64_t rows = (int64_t)a->q_heads / v.heads * a->new_tokens, block = rows <= 16 ? 16 : 32;
+  const int64_t items = (int64_t)v.num_seqs * v.heads * ((rows + block - 1) / block);
+  AttendSpace w;
+  w.counters = 0;
+  w.parts = up(items * 4);
+  w.row_lse2 = w.parts + up((int64_t)ctx.num_sms * 2 * 2 * block * (attend_pad(v.head_dim) + 2) * 4);
+  w.scores = w.row_lse2;
+  w.bytes = w.row_lse2;
+  w.score_stride = ((int64_t)v.max_length + 15) / 16 * 16;
+  if (a->weights) {
+    w.scores += up((int64_t)v.num_seqs * v.heads * rows * 4);
+    w.bytes = w.scores + up((int64_t)v.num_seqs * v.heads * rows * w.score_stride * 4);
+  }
+  return w;
+}
+
 // Checks of an attention that need no device.
 kvx_status check_attention(const kvx_pool* pool, const kvx_attention* a) {
   if (!check_types(a->type, a->cache_type, pool->elem_bytes)) return refuse(KVX_EINVAL, "type, cache_type or elem_bytes");
@@ -222,7 +245,7 @@ kvx_status kv_attend_workspace(kvx_ctx* c, const kvx_pool* pool, const kvx_batch
     kvx_status st = view_pages(view_of(c), pool, batch, &g, &v);
     if (st == KVX_OK) st = check_attention(pool, a);
     if (st != KVX_OK) return st;
-    *bytes = a->weights ? (int64_t)batch->num_seqs * a->new_tokens * a->q_heads * 4 : 0;
+    *bytes = attend_space(view_of(c), v, a).bytes;
     return KVX_OK;
   });
 }
@@ -258,16 +281,19 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
         return refuse(KVX_EINVAL, "strides of weights");
       if ((st = check_words(mem, a->weights, bytes / 4, "weights")) != KVX_OK) return st;
     }
-    int64_t need = 0;
-    if ((st = kv_attend_workspace(c, pool, batch, a, &need)) != KVX_OK) return st;
-    if (need > 0) {
-      if (workspace_bytes < need) return refuse(KVX_ERANGE, "workspace is smaller than kv_attend_workspace says");
-      if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
-      if ((st = mem.check(workspace, need)) != KVX_OK) return refuse(st, "workspace");
-    }
+    const AttendSpace space = attend_space(ctx, p.pages, a);
+    if (workspace_bytes < space.bytes) return refuse(KVX_ERANGE, "workspace is smaller than kv_attend_workspace says");
+    if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
+    if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
+    uint8_t* ws = (uint8_t*)workspace;
+    p.counters = (int32_t*)(ws + space.counters);
+    p.parts = (float*)(ws + space.parts);
+    p.row_lse2 = (float*)(ws + space.row_lse2);
+    p.scores = (float*)(ws + space.scores);
+    p.score_stride = space.score_stride;
     p.q = (const uint8_t*)q;
     p.out = (uint8_t*)out;
-    p.lse = a->lse ? a->lse : (float*)(need ? workspace : nullptr);
+    p.lse = a->lse;
     p.weights = a->weights;
     p.slopes = a->slopes;
     p.q_token = 2 * a->q_token_stride;
@@ -285,7 +311,11 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     const bool e4m3 = a->cache_type == KVX_TYPE_E4M3;
     p.k_scale = e4m3 && a->k_scale ? a->k_scale : 1.f;
     p.v_scale = e4m3 && a->v_scale ? a->v_scale : 1.f;
-    return KVX_LAUNCHED(c, launch_attend(p, a->type, a->cache_type, stream), a->weights ? 2 : 1);
+    p.type = a->type;
+    const int64_t blocks = ((int64_t)p.group * p.new_tokens + 16 * attend_tiles(p) - 1) / (16 * attend_tiles(p));
+    p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * (space.score_stride / 16);
+    p.min_steps = 4;
+    return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), a->weights ? 2 : 1);
   });
 }
 

@@ -46,9 +46,20 @@ struct AttendParams {
   const float* slopes;
   int64_t q_token, q_head, out_token, out_head;  // strides in bytes
   int64_t weights_seq, weights_head;             // strides in elements
-  int32_t q_heads, group, new_tokens, window;
+  int32_t type, q_heads, group, new_tokens, window;
   float scale, softcap, k_scale, v_scale;
+  int64_t most_steps;     // of 16 keys that the batch may have, over all items
+  int32_t min_steps;      // the least a CTA is started for
+  // workspace
+  int32_t* counters;      // [item]: CTAs that have left their part of it, 0 between calls
+  float* parts;           // [CTA][2][rows of a block][head_dim and 2]: sums of pieces of items
+  float *row_lse2;        // [sequence][head][row], with weights only
+  float* scores;          // [sequence][head][row][score_stride], with weights only
+  int64_t score_stride;
 };
+// Elements of a row in shared memory, and warps that share a step's keys.
+inline int attend_pad(int32_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
+inline int attend_tiles(const AttendParams& p) { return p.group * p.new_tokens <= 16 ? 1 : 2; }
 
 struct EvictParams {
   PagesView pages;                // base is not used
@@ -92,7 +103,13 @@ struct ScanParams {
 };
 
 cudaError_t launch_append(const AppendParams& p, int type, int cache_type, cudaStream_t s);
-cudaError_t launch_attend(const AttendParams& p, int type, int cache_type, cudaStream_t s);
+cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cudaStream_t s);
+cudaError_t launch_attend_bf16(const AttendParams& p, int num_sms, cudaStream_t s);
+cudaError_t launch_attend_fp16(const AttendParams& p, int num_sms, cudaStream_t s);
+cudaError_t launch_attend_e4m3(const AttendParams& p, int num_sms, cudaStream_t s);
+cudaError_t prepare_attend_bf16();
+cudaError_t prepare_attend_fp16();
+cudaError_t prepare_attend_e4m3();
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
 cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s);
 cudaError_t launch_scan(const ScanParams& p, int type, cudaStream_t s);
