@@ -39,11 +39,11 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
   if (rest == 0 && half == 0) check_length(v, s);
   const int64_t pos = length_of(v, s) - back;
   if (pos < 0) return;
-  const int64_t at = row_offset(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)pos);
-  if (at < 0) return;
+  const uint32_t at = row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)pos);
+  if (at == kNoRow) return;
   const uint8_t* src = half ? p.value + token * p.value_token + head * p.value_head
                             : p.key + token * p.key_token + head * p.key_head;
-  uint8_t* dst = v.base + at + half * v.half_bytes + head * v.head_bytes;
+  uint8_t* dst = v.base + at * v.row_bytes + half * v.half_bytes + head * v.head_bytes;
   const uint4 raw = *reinterpret_cast<const uint4*>(src + col * 2);
   if constexpr (!kFp8) {
     *reinterpret_cast<uint4*>(dst + col * 2) = raw;
@@ -69,14 +69,16 @@ __global__ void __launch_bounds__(256) weights_kernel(const __grid_constant__ At
   const int32_t length = length_of(v, s);
   const int32_t from = p.window > 0 ? max(0, length - p.new_tokens + 1 - p.window) : 0;
   const int64_t item = (int64_t)s * v.heads + h;
-  const float* scores = p.scores + item * rows * p.score_stride;
+  const float* scores = p.scores + item * p.score_rows * p.score_stride;
   const float* lse2 = p.row_lse2 + item * rows;
   float* weights = p.weights + s * p.weights_seq + h * p.weights_head;
   for (int32_t j = from + blockIdx.x * 256 + threadIdx.x; j < length; j += gridDim.x * 256) {
     float sum = 0.f;
-    for (int32_t r = 0; r < rows; ++r) {
-      const float x = scores[r * p.score_stride + j];
-      if (x != -INFINITY) sum += exp2f(x - lse2[r]);
+    const float2* row = reinterpret_cast<const float2*>(scores + (int64_t)j * p.score_rows);
+    for (int32_t r = 0; r < rows; r += 2) {
+      const float2 x = row[r / 2];
+      if (x.x != -INFINITY) sum += exp2f(x.x - lse2[r]);
+      if (r + 1 < rows && x.y != -INFINITY) sum += exp2f(x.y - lse2[r + 1]);
     }
     weights[j] += sum;
   }

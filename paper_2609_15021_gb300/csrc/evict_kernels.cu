@@ -110,14 +110,14 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Evi
   if (pos < 0) return;
   const int32_t h = (int32_t)(at % v.heads), s = (int32_t)(at / v.heads % v.num_seqs);
   uint8_t* base = p.layer_base[at / v.heads / v.num_seqs];
-  const int64_t old_row = row_offset(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)pos);
-  const int64_t new_row = row_offset(v, p.new_tables + s * p.new_table_stride, p.new_table_len, (uint32_t)to);
-  if (new_row < 0) return;
-  const int32_t vecs = (int32_t)(min(v.token_bytes, v.head_bytes) / 16);
+  const uint32_t old_row = row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)pos);
+  const uint32_t new_row = row_index(v, p.new_tables + s * p.new_table_stride, p.new_table_len, (uint32_t)to);
+  if (new_row == kNoRow) return;
+  const int32_t vecs = (int32_t)(v.row_bytes / 16);
   for (int32_t k = lane; k < 2 * vecs; k += 32) {
     const int64_t off = (k >= vecs ? v.half_bytes + (k - vecs) * 16 : k * 16) + h * v.head_bytes;
-    const uint4 x = old_row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(base + old_row + off);
-    *reinterpret_cast<uint4*>(base + new_row + off) = x;
+    const uint4 x = old_row == kNoRow ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(base + old_row * v.row_bytes + off);
+    *reinterpret_cast<uint4*>(base + new_row * v.row_bytes + off) = x;
   }
 }
 

@@ -91,13 +91,16 @@ kvx_status view_pages(const CtxView& ctx, const kvx_pool* pool, const kvx_batch*
   v->lengths = b->lengths;
   v->err = ctx.err;
   v->table_stride = b->table_stride;
-  v->page_bytes = g->page_bytes;
   v->half_bytes = g->page_bytes / 2;
   const bool hnd = pool->layout == KVX_LAYOUT_HND;
-  v->token_bytes = hnd ? g->row : g->row * pool->num_heads;
+  // rows are counted in 32 bits (of which the last number means none)
+  if (g->layer_bytes / g->row >= (1ll << 32) - 1) return refuse(KVX_ERANGE, "a layer of 2^32 rows or more");
+  v->row_bytes = g->row;
+  v->page_rows = (uint32_t)(g->page_bytes / g->row);
+  v->token_rows = hnd ? 1 : (uint32_t)pool->num_heads;
   v->head_bytes = hnd ? g->row * pool->block_tokens : g->row;
-  v->by_block = fast_div((uint32_t)pool->block_tokens);
-  v->by_pack = fast_div((uint32_t)pack);
+  v->by_block = div31((uint32_t)pool->block_tokens);
+  v->by_pack = div31((uint32_t)pack);
   v->entries = (uint32_t)std::min<int64_t>(pool->num_blocks / pack, INT32_MAX);
   v->table_len = (uint32_t)b->table_len;
   v->heads = pool->num_heads;
@@ -158,10 +161,12 @@ kvx_status view_state(const CtxView& ctx, const kvx_state* s, const kvx_state_ba
 struct AttendSpace {
   int64_t counters, parts, row_lse2, scores, bytes;  // offsets, and all of it
   int64_t score_stride;
+  int32_t score_rows;
 };
 AttendSpace attend_space(const CtxView& ctx, const PagesView& v, const kvx_attention* a) {
   auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
-  const int64_t rows = (int64_t)a->q_heads / v.heads * a->new_tokens, block = rows <= 16 ? 16 : 32;
+  const int64_t rows = (int64_t)a->q_heads / v.heads * a->new_tokens;
+  const int64_t block = 8 * attend_tiles(v.head_dim, (int32_t)rows);
   const int64_t items = (int64_t)v.num_seqs * v.heads * ((rows + block - 1) / block);
   AttendSpace w;
   w.counters = 0;
@@ -170,9 +175,10 @@ AttendSpace attend_space(const CtxView& ctx, const PagesView& v, const kvx_atten
   w.scores = w.row_lse2;
   w.bytes = w.row_lse2;
   w.score_stride = ((int64_t)v.max_length + 15) / 16 * 16;
+  w.score_rows = (int32_t)((rows + 1) / 2 * 2);
   if (a->weights) {
     w.scores += up((int64_t)v.num_seqs * v.heads * rows * 4);
-    w.bytes = w.scores + up((int64_t)v.num_seqs * v.heads * rows * w.score_stride * 4);
+    w.bytes = w.scores + up((int64_t)v.num_seqs * v.heads * w.score_rows * w.score_stride * 4);
   }
   return w;
 }
@@ -291,6 +297,7 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     p.row_lse2 = (float*)(ws + space.row_lse2);
     p.scores = (float*)(ws + space.scores);
     p.score_stride = space.score_stride;
+    p.score_rows = space.score_rows;
     p.q = (const uint8_t*)q;
     p.out = (uint8_t*)out;
     p.lse = a->lse;
@@ -312,7 +319,8 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     p.k_scale = e4m3 && a->k_scale ? a->k_scale : 1.f;
     p.v_scale = e4m3 && a->v_scale ? a->v_scale : 1.f;
     p.type = a->type;
-    const int64_t blocks = ((int64_t)p.group * p.new_tokens + 16 * attend_tiles(p) - 1) / (16 * attend_tiles(p));
+    const int32_t rows = p.group * p.new_tokens, block = 8 * attend_tiles(p.pages.head_dim, rows);
+    const int64_t blocks = (rows + block - 1) / block;
     p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * (space.score_stride / 16);
     p.min_steps = 4;
     return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), a->weights ? 2 : 1);

@@ -12,16 +12,31 @@
 
 namespace kvx {
 
+// Division of numbers n < 2^31 by d >= 1: with 2^(l-1) < d <= 2^l and m = ceil(2^(31+l) / d), n / d is
+// floor(n m / 2^(31+l)), as m is too large by less than 1 and n < 2^31 (Granlund, Montgomery, "Division by
+// invariant integers using multiplication", 1994).
+struct Div31 {
+  uint32_t d, m, shift;  // shift: l - 1, the high word's
+};
+inline Div31 div31(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return {d, d > 1 ? (uint32_t)(((1ull << (31 + l)) + d - 1) / d) : 0, l ? l - 1 : 0};
+}
+
 // One layer's pages as a batch's block tables name them.
 struct PagesView {
   uint8_t* base;
   const int32_t* tables;
   const int32_t* lengths;
   long long* err;
-  int64_t table_stride, page_bytes;
+  int64_t table_stride;
   int64_t half_bytes;               // K half of a page; the V half follows
-  int64_t token_bytes, head_bytes;  // from a token / head of a page half to the next
-  FastDiv by_block, by_pack;        // tokens per page, pages per logical block
+  int64_t head_bytes;               // from a head of a page half to the next
+  int64_t row_bytes;
+  // A K row's number in its layer's rows is (page * page_rows + slot * token_rows + head * head_rows).
+  uint32_t page_rows, token_rows;
+  Div31 by_block, by_pack;          // tokens per page, pages per logical block
   uint32_t entries;                 // valid table entries are below this
   uint32_t table_len;
   int32_t heads, head_dim, num_seqs;
@@ -54,12 +69,18 @@ struct AttendParams {
   int32_t* counters;      // [item]: CTAs that have left their part of it, 0 between calls
   float* parts;           // [CTA][2][rows of a block][head_dim and 2]: sums of pieces of items
   float *row_lse2;        // [sequence][head][row], with weights only
-  float* scores;          // [sequence][head][row][score_stride], with weights only
+  float* scores;          // [sequence][head][score_stride keys][score_rows], with weights only
   int64_t score_stride;
+  int32_t score_rows;     // query rows of a head, made even
 };
-// Elements of a row in shared memory, and warps that share a step's keys.
+// Elements of a row in shared memory, and tiles of 8 query rows that a warp takes at once: what its
+// registers hold of sums (at most 4, 3 for rows of 256); more rows are blocks of their own.
 inline int attend_pad(int32_t head_dim) { return head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256; }
-inline int attend_tiles(const AttendParams& p) { return p.group * p.new_tokens <= 16 ? 1 : 2; }
+inline int attend_tiles(int32_t head_dim, int32_t rows) {
+  const int most = head_dim > 128 ? 3 : 4, tiles = (rows + 7) / 8, blocks = (tiles + most - 1) / most;
+  const int each = (tiles + blocks - 1) / blocks;
+  return each == 3 && most == 4 ? 4 : each;
+}
 
 struct EvictParams {
   PagesView pages;                // base is not used
@@ -132,8 +153,8 @@ struct E4m3 {
   static __device__ __forceinline__ float up(T v) { return (float)v; }
 };
 
-__device__ __forceinline__ uint32_t fdiv(const FastDiv& f, uint32_t n) {
-  return f.d > 1 ? (uint32_t)__umul64hi(f.m, n) : n;
+__device__ __forceinline__ uint32_t quotient(const Div31& f, uint32_t n) {
+  return f.d > 1 ? __umulhi(f.m, n) >> f.shift : n;
 }
 
 // Tokens that sequence `s` holds, between 0 and max_length.
@@ -141,18 +162,18 @@ __device__ __forceinline__ int32_t length_of(const PagesView& v, int32_t s) {
   return min(max(v.lengths[s], 0), v.max_length);
 }
 
-// Byte offset from the layer's base of head 0 of the K row at `pos`, or -1 for a
-// table entry that names no page (reported as its logical block).
-__device__ __forceinline__ int64_t row_offset(const PagesView& v, const int32_t* table, uint32_t table_len,
-                                              uint32_t pos) {
-  const uint32_t page = fdiv(v.by_block, pos), slot = pos - page * v.by_block.d;
-  const uint32_t block = fdiv(v.by_pack, page), sub = page - block * v.by_pack.d;
+constexpr uint32_t kNoRow = UINT32_MAX;
+// Number in the layer's rows of head 0's K row at `pos`, or kNoRow for a table entry that
+// names no page (reported as its logical block).
+__device__ __forceinline__ uint32_t row_index(const PagesView& v, const int32_t* table, uint32_t table_len, uint32_t pos) {
+  const uint32_t page = quotient(v.by_block, pos), slot = pos - page * v.by_block.d;
+  const uint32_t block = quotient(v.by_pack, page), sub = page - block * v.by_pack.d;
   const uint32_t entry = block < table_len ? (uint32_t)__ldg(table + block) : UINT32_MAX;
   if (entry >= v.entries) {
     atomicMin(v.err, (long long)block);
-    return -1;
+    return kNoRow;
   }
-  return ((int64_t)entry * v.by_pack.d + sub) * v.page_bytes + slot * v.token_bytes;
+  return (entry * v.by_pack.d + sub) * v.page_rows + slot * v.token_rows;
 }
 
 // Reports a length outside [0, max_length] (one thread of a launch calls it per sequence).
