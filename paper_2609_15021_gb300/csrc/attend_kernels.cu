@@ -2,7 +2,7 @@
 
 #include <algorithm>
 
-#include "operators.cuh"
+#include "attend_common.cuh"
 
 namespace kvx {
 namespace {
@@ -59,28 +59,108 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
   }
 }
 
-// ---------------------------------------------------------------- attention weights
+// ---------------------------------------------------------------- the end of an attention
 
-// weights[s][h][j] += sum over the head's query rows of exp2(score - lse2), from the
-// scores that the attention left: a thread per key, so the sums have one order.
-__global__ void __launch_bounds__(256) weights_kernel(const __grid_constant__ AttendParams p) {
+constexpr int kFinishThreads = 256;
+
+__device__ __forceinline__ const float* part_of(const AttendParams& p, int2 item, int32_t c) {
+  const int64_t slot = c ? (item.x / 2 + c) * 2 : item.x;
+  return p.parts + slot * (p.part_rows * (p.part_dim + 2));
+}
+
+// A row's logarithm of the sum, from its item's parts (a warp).
+__device__ __forceinline__ float joined_lse2(const AttendParams& p, int2 item, int32_t row) {
+  const int lane = threadIdx.x & 31;
+  float top = -INFINITY, sum = 0.f;
+  for (int32_t c = lane; c < item.y; c += 32) {
+    const float2 ml = *reinterpret_cast<const float2*>(part_of(p, item, c) + p.part_rows * p.part_dim + 2 * row);
+    const float now = fmaxf(top, ml.x);
+    sum = sum * factor(top, now) + ml.y * factor(ml.x, now);
+    top = now;
+  }
+  float all = top;
+  for (int d = 16; d; d >>= 1) all = fmaxf(all, __shfl_xor_sync(~0u, all, d));
+  sum *= factor(top, all);
+  for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
+  return sum == 0.f ? -INFINITY : all + log2f(sum);
+}
+
+// CTAs below `join` join the parts of one query row each: threads by (part, four columns), parts in order
+// within a thread and threads in order after that.  The others add a stretch of keys' attention
+// weights, a thread per key, so that every sum has one order:
+//   weights[s][h][j] += sum over the head's rows of 2^(score - lse2), scores as the attention left them.
+__global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ AttendParams p) {
+  wait_for_previous();
   const PagesView& v = p.pages;
-  const int32_t h = blockIdx.y, s = blockIdx.z, rows = p.group * p.new_tokens;
-  const int32_t length = length_of(v, s);
-  const int32_t from = p.window > 0 ? max(0, length - p.new_tokens + 1 - p.window) : 0;
-  const int64_t item = (int64_t)s * v.heads + h;
-  const float* scores = p.scores + item * p.score_rows * p.score_stride;
-  const float* lse2 = p.row_lse2 + item * rows;
-  float* weights = p.weights + s * p.weights_seq + h * p.weights_head;
-  for (int32_t j = from + blockIdx.x * 256 + threadIdx.x; j < length; j += gridDim.x * 256) {
-    float sum = 0.f;
-    const float2* row = reinterpret_cast<const float2*>(scores + (int64_t)j * p.score_rows);
-    for (int32_t r = 0; r < rows; r += 2) {
-      const float2 x = row[r / 2];
-      if (x.x != -INFINITY) sum += exp2f(x.x - lse2[r]);
-      if (r + 1 < rows && x.y != -INFINITY) sum += exp2f(x.y - lse2[r + 1]);
+  const int32_t rows = p.group * p.new_tokens, blocks = (rows + p.part_rows - 1) / p.part_rows;
+  const int32_t heads_all = v.heads * v.num_seqs;
+  const int64_t join = (int64_t)heads_all * rows;
+  __shared__ float4 o_s[kFinishThreads];
+  __shared__ float m_s[kFinishThreads], l_s[kFinishThreads];
+  if (blockIdx.x < join) {
+    const int32_t sh = blockIdx.x / rows, r = blockIdx.x - sh * rows, in = r % p.part_rows;
+    const int2 item = p.items[(int64_t)sh * blocks + r / p.part_rows];
+    if (item.y == 0) return;
+    const int32_t cols = p.part_dim / 4, col = threadIdx.x % cols, groups = kFinishThreads / cols;
+    float top = -INFINITY, sum = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int32_t c = threadIdx.x / cols; c < item.y; c += groups) {
+      const float* part = part_of(p, item, c);
+      const float2 ml = *reinterpret_cast<const float2*>(part + p.part_rows * p.part_dim + 2 * in);
+      const float4 x = *reinterpret_cast<const float4*>(part + in * p.part_dim + 4 * col);
+      const float now = fmaxf(top, ml.x), f0 = factor(top, now), f1 = factor(ml.x, now);
+      sum = sum * f0 + ml.y * f1;
+      o.x = o.x * f0 + x.x * f1, o.y = o.y * f0 + x.y * f1, o.z = o.z * f0 + x.z * f1, o.w = o.w * f0 + x.w * f1;
+      top = now;
     }
-    weights[j] += sum;
+    o_s[threadIdx.x] = o, m_s[threadIdx.x] = top, l_s[threadIdx.x] = sum;
+    __syncthreads();
+    if (threadIdx.x >= cols) return;
+    for (int32_t g = 1; g < groups; ++g) {
+      const int32_t i = g * cols + col;
+      const float now = fmaxf(top, m_s[i]), f0 = factor(top, now), f1 = factor(m_s[i], now);
+      const float4 x = o_s[i];
+      sum = sum * f0 + l_s[i] * f1;
+      o.x = o.x * f0 + x.x * f1, o.y = o.y * f0 + x.y * f1, o.z = o.z * f0 + x.z * f1, o.w = o.w * f0 + x.w * f1;
+      top = now;
+    }
+    const float by = sum == 0.f ? 0.f : p.v_scale / sum;
+    if (sum == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (4 * col < v.head_dim)
+      write_out(p, sh / v.heads, sh % v.heads, r, 4 * col, make_float4(o.x * by, o.y * by, o.z * by, o.w * by));
+    if (col == 0 && p.lse) {
+      const int32_t head = sh % v.heads * p.group + r % p.group;
+      p.lse[((int64_t)(sh / v.heads) * p.new_tokens + r / p.group) * p.q_heads + head] =
+          (sum == 0.f ? -INFINITY : top + log2f(sum)) * kLn2;
+    }
+    return;
+  }
+  const int32_t chunks = (int32_t)((gridDim.x - join) / heads_all);
+  const int32_t rest = (int32_t)(blockIdx.x - join), sh = rest / chunks, chunk = rest - sh * chunks;
+  const int32_t s = sh / v.heads, h = sh - s * v.heads, length = length_of(v, s);
+  const int32_t from = p.window > 0 ? max(0, length - p.new_tokens + 1 - p.window) : 0;
+  const float* scores = p.scores + (int64_t)sh * p.score_rows * p.score_stride;
+  float* weights = p.weights + s * p.weights_seq + h * p.weights_head;
+  for (int32_t r0 = 0; r0 < rows; r0 += kFinishThreads) {  // rows whose sums are kept at once
+    const int32_t n = min(rows - r0, kFinishThreads);
+    __syncthreads();
+    for (int32_t r = threadIdx.x >> 5; r < n; r += kFinishThreads / 32) {
+      const int2 item = p.items[(int64_t)sh * blocks + (r0 + r) / p.part_rows];
+      const float lse2 = item.y == 0 ? p.row_lse2[(int64_t)sh * rows + r0 + r] : joined_lse2(p, item, (r0 + r) % p.part_rows);
+      if ((threadIdx.x & 31) == 0) l_s[r] = lse2;
+    }
+    __syncthreads();
+    for (int32_t j = from + chunk * kFinishThreads + threadIdx.x; j < length; j += chunks * kFinishThreads) {
+      const float2* row = reinterpret_cast<const float2*>(scores + (int64_t)j * p.score_rows + r0);
+      float sum = 0.f;
+      for (int32_t r = 0; r < n; r += 2) {
+        const float2 x = row[r / 2];
+        if (x.x != -INFINITY) sum += ex2(x.x - l_s[r]);
+        if (r + 1 < n && x.y != -INFINITY) sum += ex2(x.y - l_s[r + 1]);
+      }
+      weights[j] += sum;
+    }
   }
 }
 
@@ -102,12 +182,14 @@ cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cu
   const cudaError_t e = cache_type == KVX_TYPE_E4M3   ? launch_attend_e4m3(p, num_sms, s)
                         : cache_type == KVX_TYPE_BF16 ? launch_attend_bf16(p, num_sms, s)
                                                       : launch_attend_fp16(p, num_sms, s);
-  if (e != cudaSuccess || !p.weights) return e;
-  const int32_t items = p.pages.heads * p.pages.num_seqs;
-  const int32_t most = (p.pages.max_length + 255) / 256;
-  const int32_t chunks = std::max(1, std::min(most, 16 * num_sms / items));
-  weights_kernel<<<dim3(chunks, p.pages.heads, p.pages.num_seqs), 256, 0, s>>>(p);
-  return cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  const int64_t heads_all = (int64_t)p.pages.heads * p.pages.num_seqs;
+  int64_t grid = heads_all * p.group * p.new_tokens;
+  if (p.weights) {
+    const int64_t most = (p.pages.max_length + kFinishThreads - 1) / kFinishThreads;
+    grid += heads_all * std::max<int64_t>(1, std::min(most, 8 * num_sms / heads_all));
+  }
+  return launch_after(finish_kernel, dim3((unsigned)grid), kFinishThreads, 0, s, p);
 }
 
 cudaError_t prepare_attend_kernels() {

@@ -12,9 +12,12 @@
 //
 //   * The work is cut into steps of 16 keys of one item (sequence, KV head, block
 //     of query rows).  The grid's CTAs take equal runs of the steps of all items,
-//     whatever the lengths, which are read on the device.  A run that covers only a
-//     part of an item leaves its unnormalised sums in the workspace, and the CTA that
-//     comes last to an item joins the parts, in their order.
+//     whatever the lengths, which are read on the device (an item counts for kItemSteps
+//     more than it has, what beginning and ending one takes).  A run that covers only
+//     a part of an item leaves its unnormalised sums in the workspace, and a second kernel
+//     joins the parts in their order, a CTA per row.  (Joined by the CTA that came last to
+//     an item, the same took 11 us instead of 3 at 38 parts: few CTAs, in code that is in no
+//     instruction cache.)
 //   * In a CTA, four warps take the steps in turn.  A warp has a ring of its own in shared
 //     memory and shares nothing with the others until a piece ends, so there is no
 //     barrier in the loop.
@@ -36,7 +39,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "operators.cuh"
+#include "attend_common.cuh"
 
 namespace kvx {
 namespace {
@@ -44,7 +47,7 @@ namespace {
 constexpr int kStep = 16;  // keys of a step
 constexpr int kAttendThreads = 128, kWarps = kAttendThreads / 32;
 constexpr int kMaxCtas = 320;  // of a launch
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kItemSteps = 6;
 // Exponents are relative to 2^10 below the largest score so far (fp16 probabilities stay
 // normal down to 2^-24 of it), and it is raised when a score passes it by more than 2^5.
 constexpr float kBelow = 10.f, kSlack = 15.f;
@@ -71,10 +74,7 @@ struct AttendShape {
   // the ring serves to join the warps' sums too: [warp][row][dim], then [warp][row] maxima and sums
   static constexpr int kSumPitch = kDim + 4;
   static constexpr int kJoin = kWarps * kRows * (kSumPitch + 2) * 4;
-  // and at last the maxima and sums, then factors, of an item's parts
-  static constexpr int kFactors = kRows * (2 * kMaxCtas + 1) * 4;
-  static constexpr int kUse = kRing > kJoin ? kRing : kJoin;
-  static constexpr int kQueryAt = kUse > kFactors ? kUse : kFactors;
+  static constexpr int kQueryAt = kRing > kJoin ? kRing : kJoin;
   static constexpr int kSmem = kQueryAt + kQueryBytes;
   static constexpr int kPart = kRows * (kDim + 2);  // floats of a part: sums, then maxima and sums
   static_assert(kStages >= 2, "a ring");
@@ -89,17 +89,6 @@ __device__ __forceinline__ void commit_async() { asm volatile("cp.async.commit_g
 template <int kLeft>
 __device__ __forceinline__ void wait_async() {
   asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
-}
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float rcp(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
@@ -128,17 +117,6 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Two numbers in the type of the products (a: low half).
-template <class C>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  if constexpr (std::is_same<C, Bf16>::value) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  } else {
-    const __half2 v = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-}
 // Four e4m3 values as two pairs of fp16.
 __device__ __forceinline__ void widen4(uint32_t v, uint32_t& lo, uint32_t& hi) {
   asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}"
@@ -164,6 +142,9 @@ __device__ __forceinline__ int32_t steps_of(const AttendParams& p, int32_t lengt
   *first = lo & ~(kStep - 1);
   return (length - *first + kStep - 1) / kStep;
 }
+
+// What a sequence's item counts for in a run.
+__device__ __forceinline__ int32_t run_steps(int32_t steps) { return steps > 0 ? steps + kItemSteps : 0; }
 
 // Sum over the CTA of one value a thread, to all.
 __device__ __forceinline__ long long cta_sum(long long v, long long* buf) {
@@ -193,32 +174,6 @@ struct Runs {
   }
 };
 
-template <class Q>
-__device__ __forceinline__ void write_out4(const AttendParams& p, int32_t s, int32_t h, int32_t r, int32_t col, float4 v) {
-  const int32_t t = r / p.group, head = h * p.group + r % p.group;
-  const int64_t token = (int64_t)s * p.new_tokens + t;
-  uint2 o = make_uint2(pack2<Q>(v.x, v.y), pack2<Q>(v.z, v.w));
-  *reinterpret_cast<uint2*>(p.out + token * p.out_token + head * p.out_head + col * 2) = o;
-}
-// Four neighbouring elements of a row's output.
-__device__ __forceinline__ void write_out(const AttendParams& p, int32_t s, int32_t h, int32_t r, int32_t col, float4 v) {
-  if (p.type == KVX_TYPE_BF16)
-    write_out4<Bf16>(p, s, h, r, col, v);
-  else
-    write_out4<Fp16>(p, s, h, r, col, v);
-}
-
-// A row's logarithm of its sum l, which is relative to 2^m.
-__device__ __forceinline__ void write_lse(const AttendParams& p, int32_t s, int32_t h, int32_t r, float m, float l) {
-  const int32_t t = r / p.group, head = h * p.group + r % p.group;
-  const float lse2 = l == 0.f ? -INFINITY : m + log2f(l);
-  if (p.lse) p.lse[((int64_t)s * p.new_tokens + t) * p.q_heads + head] = lse2 * kLn2;
-  if (p.weights) p.row_lse2[((int64_t)s * p.pages.heads + h) * (p.group * p.new_tokens) + r] = lse2;
-}
-__device__ __forceinline__ float factor(float m, float top) {  // 2^(m - top), 0 for a part without a key
-  return m == -INFINITY ? 0.f : ex2(m - top);
-}
-
 template <class C, int kDim, int kTiles>
 __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::kCtas)
     attend_kernel(const __grid_constant__ AttendParams p) {
@@ -230,7 +185,8 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
   __shared__ uint32_t masks[kWarps][S::kStages];
   __shared__ int32_t row_pos[kRows];
   __shared__ float row_slope[kRows], row_scale[kRows];
-  __shared__ int32_t found, last_s;
+  __shared__ int32_t found;
+  wait_for_previous();
   const PagesView& v = p.pages;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int quad = lane >> 2, sub = lane & 3;
@@ -243,7 +199,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
   for (int32_t s = threadIdx.x; s < v.num_seqs; s += kAttendThreads) {
     int32_t first;
     if (blockIdx.x == 0) check_length(v, s);
-    total += steps_of(p, length_of(v, s), &first);
+    total += run_steps(steps_of(p, length_of(v, s), &first));
   }
   total = cta_sum(total, buf) * per_seq;
   for (int32_t s = blockIdx.x; s < v.num_seqs; s += gridDim.x) {  // sequences without a key
@@ -253,6 +209,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
       write_out(p, s, hr / rows, hr % rows, col, make_float4(0.f, 0.f, 0.f, 0.f));
       if (col == 0) write_lse(p, s, hr / rows, hr % rows, 0.f, 0.f);
     }
+    for (int32_t i = threadIdx.x; i < per_seq; i += kAttendThreads) p.items[(int64_t)s * per_seq + i] = make_int2(0, 0);
   }
   const int32_t ctas = (int32_t)min((long long)gridDim.x, max(1ll, quotient(total + p.min_steps - 1, p.min_steps)));
   if (blockIdx.x >= ctas || total == 0) return;
@@ -265,7 +222,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
   for (int32_t base = 0; base < v.num_seqs && v.num_seqs > 1; base += kAttendThreads) {
     int32_t first;
     const int32_t s = base + threadIdx.x;
-    const long long mine = s < v.num_seqs ? (long long)steps_of(p, length_of(v, s), &first) * per_seq : 0;
+    const long long mine = s < v.num_seqs ? (long long)run_steps(steps_of(p, length_of(v, s), &first)) * per_seq : 0;
     long long before = mine;  // inclusive scan over the warp
     for (int d = 1; d < 32; d <<= 1) {
       const long long y = __shfl_up_sync(~0u, before, d);
@@ -315,13 +272,14 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
     for (;;) {
       length = length_of(v, seq);
       steps = steps_of(p, length, &first_key);
-      if (at < seq_begin + (long long)steps * per_seq) break;
-      seq_begin += (long long)steps * per_seq;
+      if (at < seq_begin + (long long)run_steps(steps) * per_seq) break;
+      seq_begin += (long long)run_steps(steps) * per_seq;
       if (++seq >= v.num_seqs) return;  // lengths that changed under the kernel
     }
-    const int32_t item = (int32_t)quotient(at - seq_begin, steps);
-    const long long item_begin = seq_begin + (long long)item * steps;
-    const int32_t i0 = (int32_t)(at - item_begin), i1 = (int32_t)min((long long)steps, end - item_begin);
+    const int32_t item = (int32_t)quotient(at - seq_begin, run_steps(steps));
+    const long long item_begin = seq_begin + (long long)item * run_steps(steps) + kItemSteps;  // its first step's place
+    const int32_t i0 = (int32_t)max(0ll, at - item_begin), i1 = (int32_t)min((long long)steps, end - item_begin);
+    if (i1 <= i0) break;  // the run ends before the item's first step
     const int32_t h = item / blocks, row0 = (item % blocks) * kRows;
     const int32_t here = min(rows - row0, kRows);  // rows of this block
     const int32_t* table = v.tables + seq * v.table_stride;
@@ -704,6 +662,10 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
       }
     __syncthreads();
     const bool whole_item = i0 == 0 && i1 == steps;
+    if (i0 == 0 && threadIdx.x == 0) {  // where the item's parts are, and how many
+      const int32_t parts = whole_item ? 0 : runs.cta_of(item_begin + steps - 1) - (int32_t)blockIdx.x + 1;
+      p.items[(int64_t)seq * per_seq + item] = make_int2(blockIdx.x * 2 + (begin < item_begin), parts);
+    }
     float* part = p.parts + ((long long)blockIdx.x * 2 + (begin < item_begin)) * S::kPart;
     for (int idx = threadIdx.x; idx < here * (kDim / 4); idx += kAttendThreads) {
       const int r = idx / (kDim / 4), col = idx % (kDim / 4) * 4;
@@ -726,74 +688,6 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
       } else {
         __stcg(reinterpret_cast<float4*>(part + r * kDim + col), o);
         if (col == 0) __stcg(reinterpret_cast<float2*>(part + kRows * kDim + 2 * r), make_float2(top, sum));
-      }
-    }
-    if (!whole_item) {
-      // The CTAs that this item's steps fall to, in order; the one that comes last joins their parts.
-      __threadfence();
-      __syncthreads();
-      const int32_t c0 = runs.cta_of(item_begin), parts = runs.cta_of(item_begin + steps - 1) - c0 + 1;
-      if (threadIdx.x == 0) {
-        int32_t* counter = p.counters + (long long)seq * per_seq + item;
-        last_s = atomicAdd(counter, 1) == parts - 1;
-        if (last_s) {
-          __stcg(counter, 0);  // as the next call wants it
-          __threadfence();
-        }
-      }
-      __syncthreads();
-      if (last_s) {
-        // All maxima and sums first, then the factors, a warp per row, then the parts, whose loads do not wait
-        // for one another.
-        const float* first_part = p.parts + (2ll * c0 + (runs.begin(c0) < item_begin)) * S::kPart;
-        const float* next_part = p.parts + 2ll * (c0 + 1) * S::kPart;
-        float2* ml = reinterpret_cast<float2*>(smem);  // [row][part]; then .x: the part's factor
-        float* whole = reinterpret_cast<float*>(ml + kRows * parts);
-        for (int idx = threadIdx.x; idx < here * parts; idx += kAttendThreads) {
-          const int r = idx / parts, c = idx % parts;
-          ml[idx] = __ldcg(reinterpret_cast<const float2*>((c ? next_part + 2ll * (c - 1) * S::kPart : first_part) +
-                                                          kRows * kDim + 2 * r));
-        }
-        __syncthreads();
-        for (int r = warp; r < here; r += kWarps) {
-          float top = -INFINITY, sum = 0.f;
-          for (int c = lane; c < parts; c += 32) top = fmaxf(top, ml[r * parts + c].x);
-          for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
-          for (int c = lane; c < parts; c += 32) {
-            const float f = factor(ml[r * parts + c].x, top);
-            sum += f * ml[r * parts + c].y;
-            ml[r * parts + c].x = f;
-          }
-          for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(~0u, sum, d);
-          if (lane == 0) {
-            whole[r] = sum;
-            write_lse(p, seq, h, row0 + r, top, sum);
-          }
-        }
-        __syncthreads();
-        for (int idx = threadIdx.x; idx < here * (kDim / 4); idx += kAttendThreads) {
-          const int r = idx / (kDim / 4), col = idx % (kDim / 4) * 4;
-          if (col >= v.head_dim) continue;
-          const float2* fr = ml + r * parts;
-          const float* from = next_part + r * kDim + col;
-          float4 o = __ldcg(reinterpret_cast<const float4*>(first_part + r * kDim + col));
-          o.x *= fr[0].x, o.y *= fr[0].x, o.z *= fr[0].x, o.w *= fr[0].x;
-          for (int c = 1; c < parts; c += 16) {
-            float4 x[16];
-#pragma unroll
-            for (int u = 0; u < 16; ++u)
-              x[u] = c + u < parts ? __ldcg(reinterpret_cast<const float4*>(from + 2ll * (c + u - 1) * S::kPart))
-                                   : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int u = 0; u < 16; ++u) {
-              const float f = c + u < parts ? fr[c + u].x : 0.f;
-              o.x += x[u].x * f, o.y += x[u].y * f, o.z += x[u].z * f, o.w += x[u].w * f;
-            }
-          }
-          const float sum = whole[r], by = sum == 0.f ? 0.f : p.v_scale / sum;
-          if (sum == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
-          write_out(p, seq, h, row0 + r, col, make_float4(o.x * by, o.y * by, o.z * by, o.w * by));
-        }
       }
     }
     __syncthreads();
@@ -832,8 +726,7 @@ template <class C, int kDim, int kTiles>
 cudaError_t attend(const AttendParams& p, int num_sms, cudaStream_t s) {
   using S = AttendShape<C, kDim, kTiles>;
   const int grid = (int)std::min<int64_t>(std::min(num_sms * S::kCtas, kMaxCtas), std::max<int64_t>(1, p.most_steps / p.min_steps));
-  attend_kernel<C, kDim, kTiles><<<grid, kAttendThreads, S::kSmem, s>>>(p);
-  return cudaGetLastError();
+  return launch_after(attend_kernel<C, kDim, kTiles>, dim3(grid), kAttendThreads, S::kSmem, s, p);
 }
 
 template <class C>

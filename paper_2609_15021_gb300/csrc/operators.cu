@@ -159,7 +159,7 @@ kvx_status view_state(const CtxView& ctx, const kvx_state* s, const kvx_state_ba
 
 // kv_attend's workspace.  The most CTAs a launch has are two an SM.
 struct AttendSpace {
-  int64_t counters, parts, row_lse2, scores, bytes;  // offsets, and all of it
+  int64_t items, parts, row_lse2, scores, bytes;  // offsets, and all of it
   int64_t score_stride;
   int32_t score_rows;
 };
@@ -169,8 +169,8 @@ AttendSpace attend_space(const CtxView& ctx, const PagesView& v, const kvx_atten
   const int64_t block = 8 * attend_tiles(v.head_dim, (int32_t)rows);
   const int64_t items = (int64_t)v.num_seqs * v.heads * ((rows + block - 1) / block);
   AttendSpace w;
-  w.counters = 0;
-  w.parts = up(items * 4);
+  w.items = 0;
+  w.parts = up(items * 8);
   w.row_lse2 = w.parts + up((int64_t)ctx.num_sms * 2 * 2 * block * (attend_pad(v.head_dim) + 2) * 4);
   w.scores = w.row_lse2;
   w.bytes = w.row_lse2;
@@ -292,7 +292,7 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
     if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
     uint8_t* ws = (uint8_t*)workspace;
-    p.counters = (int32_t*)(ws + space.counters);
+    p.items = (int2*)(ws + space.items);
     p.parts = (float*)(ws + space.parts);
     p.row_lse2 = (float*)(ws + space.row_lse2);
     p.scores = (float*)(ws + space.scores);
@@ -321,9 +321,11 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     p.type = a->type;
     const int32_t rows = p.group * p.new_tokens, block = 8 * attend_tiles(p.pages.head_dim, rows);
     const int64_t blocks = (rows + block - 1) / block;
+    p.part_rows = block;
+    p.part_dim = attend_pad(p.pages.head_dim);
     p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * (space.score_stride / 16);
-    p.min_steps = 4;
-    return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), a->weights ? 2 : 1);
+    p.min_steps = 4 + 6;  // of four warps, and what an item counts for besides
+    return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), 2);
   });
 }
 

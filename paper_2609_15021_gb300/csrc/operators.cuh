@@ -66,8 +66,9 @@ struct AttendParams {
   int64_t most_steps;     // of 16 keys that the batch may have, over all items
   int32_t min_steps;      // the least a CTA is started for
   // workspace
-  int32_t* counters;      // [item]: CTAs that have left their part of it, 0 between calls
+  int2* items;            // [item]: its first part and their number, 0 where there are none
   float* parts;           // [CTA][2][rows of a block][head_dim and 2]: sums of pieces of items
+  int32_t part_rows, part_dim;
   float *row_lse2;        // [sequence][head][row], with weights only
   float* scores;          // [sequence][head][score_stride keys][score_rows], with weights only
   int64_t score_stride;
@@ -137,6 +138,24 @@ cudaError_t launch_scan(const ScanParams& p, int type, cudaStream_t s);
 
 #ifdef __CUDACC__
 namespace {
+
+// A kernel that is launched while the one before it in the stream still runs, and waits for it
+// (wait_for_previous) before it touches memory: only the launch itself overlaps.
+template <class P>
+cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t s, const P& p) {
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = grid;
+  c.blockDim = dim3(threads);
+  c.dynamicSmemBytes = smem;
+  c.stream = s;
+  c.attrs = &attr;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, p);
+}
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 struct Bf16 {
   using T = __nv_bfloat16;
