@@ -1,37 +1,11 @@
 // attend_common.cuh -- what the attention kernel and the kernel that finishes its work share.
 #pragma once
 
-#include <type_traits>
-
-#include "operators.cuh"
+#include "mma.cuh"
 
 namespace kvx {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float rcp(float x) {
-  float y;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// Two numbers in the type of the products (a: low half).
-template <class C>
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  if constexpr (std::is_same<C, Bf16>::value) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  } else {
-    const __half2 v = __floats2half2_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-}
 template <class Q>
 __device__ __forceinline__ void write_out4(const AttendParams& p, int32_t s, int32_t h, int32_t r, int32_t col, float4 v) {
   const int32_t t = r / p.group, head = h * p.group + r % p.group;

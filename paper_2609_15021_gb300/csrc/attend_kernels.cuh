@@ -80,43 +80,6 @@ struct AttendShape {
   static_assert(kStages >= 2, "a ring");
 };
 
-__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void commit_async() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft>
-__device__ __forceinline__ void wait_async() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
-}
-
-__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void load_matrices_t(uint32_t (&r)[4], uint32_t at) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ uint32_t transpose(uint32_t v) {
-  uint32_t r;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
-  return r;
-}
-
-template <class C>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (std::is_same<C, Bf16>::value)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
 // Four e4m3 values as two pairs of fp16.
 __device__ __forceinline__ void widen4(uint32_t v, uint32_t& lo, uint32_t& hi) {
   asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}"
@@ -347,11 +310,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
     // 2 sub, 2 sub + 1 and those 8 further on (4 sub .. 4 sub + 3 where the cache is widened).
     uint32_t qf[S::kQueryInRegs ? kKs : 1][S::kQueryInRegs ? kTiles : 1][2];
     {
-      auto wide = [&](uint32_t raw) -> float2 {
-        if (p.type == KVX_TYPE_BF16)
-          return make_float2(__uint_as_float(raw << 16), __uint_as_float(raw & 0xFFFF0000u));
-        return __half22float2(*reinterpret_cast<const __half2*>(&raw));
-      };
+      auto wide = [&](uint32_t raw) { return p.type == KVX_TYPE_BF16 ? unpack2<Bf16>(raw) : unpack2<Fp16>(raw); };
 #pragma unroll
       for (int tile = 0; tile < kTiles; ++tile) {
         if (!S::kQueryInRegs && tile % kWarps != warp) continue;
@@ -564,8 +523,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
             if constexpr (kWide) {
               for (int b = 0; b < 32; b += 8) odd |= (w[q] >> b & 0x7F) == 0x7F;
             } else {
-              constexpr uint32_t kInf = std::is_same<C, Bf16>::value ? 0x7F80u : 0x7C00u;
-              odd |= (w[q] & kInf) == kInf || (w[q] >> 16 & kInf) == kInf;
+              odd |= odd2<C>(w[q]);
             }
           }
         }

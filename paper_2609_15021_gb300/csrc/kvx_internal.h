@@ -146,6 +146,7 @@ cudaError_t launch_move_tma(int dir, int layout, const MoveParams& p, int grid, 
 cudaError_t prepare_tma_kernels();
 // Shared-memory limits of the attention kernels (attend_kernels.cu), likewise.
 cudaError_t prepare_attend_kernels();
+cudaError_t prepare_state_kernels();  // and the scan's (state_kernels.cu)
 // Tensor-map variant for HND pools: one TMA box per full page half.
 constexpr int kTensorMapBytes = 128;
 // Encodes one tensor map per layer of P (kTensorMapBytes each) into `out`;

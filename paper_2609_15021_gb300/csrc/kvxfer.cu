@@ -1127,6 +1127,7 @@ kvx_status kv_ctx_create(int device, const kvx_opts* opts, kvx_ctx** out) {
     ctx->seg_occ = segment_ctas_per_sm();
     if ((e = prepare_tma_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_attend_kernels()) != cudaSuccess) return fail(e);
+    if ((e = prepare_state_kernels()) != cudaSuccess) return fail(e);
     // the host-page touch threads, once per process, at set-up rather than
     // inside a transfer call
     if (!(o.flags & KVX_FLAG_NO_HOST_TOUCH)) start_touch_threads();

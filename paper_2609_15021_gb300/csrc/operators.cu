@@ -449,6 +449,26 @@ kvx_status check_scan(const kvx_state_batch* b, const kvx_scan* s) {
   return KVX_OK;
 }
 
+// kv_state_scan's workspace: the segments' states and exponents, where sequences are cut.
+struct ScanSpace {
+  int32_t segment;
+  int64_t exponents, bytes;
+};
+ScanSpace scan_space(const CtxView& ctx, const kvx_state_batch* b, const kvx_scan* a) {
+  StateView v = {};
+  v.starts = b->starts;
+  v.tokens = b->tokens;
+  v.num_seqs = b->num_seqs;
+  bool cut;
+  ScanSpace w = {scan_segment(v, a->heads, a->head_dim, a->state_dim, ctx.num_sms, &cut), 0, 0};
+  if (cut) {
+    const int64_t pieces = b->tokens / w.segment + b->num_seqs;
+    w.exponents = pieces * a->heads * a->head_dim * a->state_dim * 4;
+    w.bytes = w.exponents + pieces * a->heads * 4;
+  }
+  return w;
+}
+
 }  // namespace
 
 kvx_status kv_state_scan_workspace(kvx_ctx* c, const kvx_state_batch* batch, const kvx_scan* scan, int64_t* bytes) {
@@ -456,7 +476,7 @@ kvx_status kv_state_scan_workspace(kvx_ctx* c, const kvx_state_batch* batch, con
     if (!c || !batch || !scan || !bytes) return KVX_EINVAL;
     const kvx_status st = check_scan(batch, scan);
     if (st != KVX_OK) return st;
-    *bytes = 0;
+    *bytes = scan_space(view_of(c), batch, scan).bytes;
     return KVX_OK;
   });
 }
@@ -491,13 +511,15 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
     if ((st = check_words(mem, a->A, h, "A")) != KVX_OK) return st;
     if (a->D && (st = check_words(mem, a->D, h, "D")) != KVX_OK) return st;
     if (a->dt_bias && (st = check_words(mem, a->dt_bias, h, "dt_bias")) != KVX_OK) return st;
-    int64_t need = 0;
-    if ((st = kv_state_scan_workspace(c, batch, a, &need)) != KVX_OK) return st;
-    if (need > 0) {
-      if (workspace_bytes < need) return refuse(KVX_ERANGE, "workspace is smaller than kv_state_scan_workspace says");
+    const ScanSpace space = scan_space(ctx, batch, a);
+    if (space.bytes > 0) {
+      if (workspace_bytes < space.bytes) return refuse(KVX_ERANGE, "workspace is smaller than kv_state_scan_workspace says");
       if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
-      if ((st = mem.check(workspace, need)) != KVX_OK) return refuse(st, "workspace");
+      if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
     }
+    p.segment = space.segment;
+    p.segment_states = space.bytes > 0 ? (float*)workspace : nullptr;
+    p.segment_exponents = space.bytes > 0 ? (float*)((uint8_t*)workspace + space.exponents) : nullptr;
     p.x = (const uint8_t*)x;
     p.dt = (const uint8_t*)dt;
     p.b = (const uint8_t*)B;
@@ -520,6 +542,6 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
     p.state_dim = a->state_dim;
     p.heads_per_group = a->heads / a->groups;
     p.softplus = a->softplus;
-    return KVX_LAUNCHED(c, launch_scan(p, a->type, stream), 1);
+    return KVX_LAUNCHED(c, launch_scan(p, a->type, ctx.num_sms, stream), space.bytes > 0 ? 3 : 1);
   });
 }

@@ -122,7 +122,12 @@ struct ScanParams {
   const float *A, *D, *dt_bias;
   int64_t x_token, x_head, dt_token, b_token, b_group, c_token, c_group, out_token, out_head;  // in elements
   int32_t heads, head_dim, state_dim, heads_per_group, softplus;
+  int32_t segment;           // tokens of a segment in the matrix form; 0: token by token
+  float* segment_states;     // [piece][head][head_dim][state_dim], where sequences are cut into segments
+  float* segment_exponents;  // [piece][head]
 };
+// The segment of the matrix form for a batch, 0 where it is not used; *cut: whether a sequence may have several.
+int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut);
 
 cudaError_t launch_append(const AppendParams& p, int type, int cache_type, cudaStream_t s);
 cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cudaStream_t s);
@@ -134,7 +139,7 @@ cudaError_t prepare_attend_fp16();
 cudaError_t prepare_attend_e4m3();
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
 cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s);
-cudaError_t launch_scan(const ScanParams& p, int type, cudaStream_t s);
+cudaError_t launch_scan(const ScanParams& p, int type, int num_sms, cudaStream_t s);
 
 #ifdef __CUDACC__
 namespace {
