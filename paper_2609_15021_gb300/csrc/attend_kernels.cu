@@ -9,25 +9,42 @@ namespace {
 
 // ---------------------------------------------------------------- append
 
-// Eight elements of one row a thread.  Bound by its bytes (a row in, a row out).
-template <class In, bool kFp8>
-__global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ AppendParams p) {
+constexpr int kAppendThreads = 128;
+
+// x / scale to the nearest: a product with the rounded reciprocal, corrected by its residual (Markstein, "Computation
+// of elementary functions on the IBM RISC System/6000 processor", 1990).  Quotients that the 8 bits clamp are left as
+// they are, as their residual may not be finite.
+__device__ __forceinline__ float divided(float x, float scale, float inverse) {
+  const float q = x * inverse;
+  const float r = fmaf(fmaf(-q, scale, x), inverse, q);
+  return fabsf(q) < 512.f ? r : q;
+}
+__device__ __forceinline__ uint32_t to_e4m3(float2 x, float scale, float inverse) {
+  return __nv_cvt_float2_to_fp8x2(make_float2(divided(x.x, scale, inverse), divided(x.y, scale, inverse)), __NV_SATFINITE,
+                                  __NV_E4M3);
+}
+
+// A warp finds one token's sequence and place and moves its rows, or a quarter of them (kParts): bound by
+// the rows' bytes, in and out.  A lane has four vectors in flight; a vector is 16 bytes of the cache's row,
+// twice as much of an input that is narrowed.
+template <class In, bool kFp8, int kParts>
+__global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendParams p) {
+  wait_for_previous();
   const PagesView& v = p.pages;
-  const int32_t row_vecs = v.head_dim / 8, vecs = 2 * v.heads * row_vecs;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t token = i / vecs;
+  const int lane = threadIdx.x & 31;
+  const int64_t unit = (int64_t)blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5), token = unit / kParts;
   if (token >= p.tokens) return;
-  int32_t rest = (int32_t)(i - token * vecs);
-  const int32_t half = rest / (v.heads * row_vecs);
-  rest -= half * v.heads * row_vecs;
-  const int32_t head = rest / row_vecs, col = (rest - head * row_vecs) * 8;
+  const int part = (int)(unit - token * kParts);
   int32_t s;
   int64_t back;  // rows of this sequence from this one to its last
   if (p.starts) {
-    int32_t lo = 0, hi = p.num_seqs;  // the last s with starts[s] <= token
+    int32_t lo = 0, hi = p.num_seqs;  // the last s with starts[s] <= token lies in [lo, hi)
     while (hi - lo > 1) {
-      const int32_t mid = (lo + hi) / 2;
-      if (p.starts[mid] <= token) lo = mid; else hi = mid;
+      const int32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const uint32_t below = __ballot_sync(~0u, at < hi && p.starts[at] <= token);
+      const int32_t n = 31 - __clz(below | 1);
+      hi = min(hi, lo + (n + 1) * step);
+      lo += n * step;
     }
     s = lo;
     back = p.starts[s + 1] - token;
@@ -36,27 +53,59 @@ __global__ void __launch_bounds__(256) append_kernel(const __grid_constant__ App
     s = (int32_t)(token / p.new_tokens);
     back = (int64_t)(s + 1) * p.new_tokens - token;
   }
-  if (rest == 0 && half == 0) check_length(v, s);
+  if (lane == 0 && part == 0) check_length(v, s);
   const int64_t pos = length_of(v, s) - back;
   if (pos < 0) return;
-  const uint32_t at = row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)pos);
-  if (at == kNoRow) return;
-  const uint8_t* src = half ? p.value + token * p.value_token + head * p.value_head
-                            : p.key + token * p.key_token + head * p.key_head;
-  uint8_t* dst = v.base + at * v.row_bytes + half * v.half_bytes + head * v.head_bytes;
-  const uint4 raw = *reinterpret_cast<const uint4*>(src + col * 2);
-  if constexpr (!kFp8) {
-    *reinterpret_cast<uint4*>(dst + col * 2) = raw;
-  } else {
-    const typename In::T* e = reinterpret_cast<const typename In::T*>(&raw);
-    const float scale = half ? p.v_scale : p.k_scale;
-    uint2 packed;
-    uint8_t* o = reinterpret_cast<uint8_t*>(&packed);
+  const uint32_t row = row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)pos);
+  if (row == kNoRow) return;
+  uint8_t* to = v.base + row * v.row_bytes;
+  const uint8_t* from[2] = {p.key + token * p.key_token, p.value + token * p.value_token};
+  const int64_t head_step[2] = {p.key_head, p.value_head};
+  const uint32_t half_vecs = v.heads * p.row_vecs.d;  // of K, and of V
+  const float inverse[2] = {1.f / p.k_scale, 1.f / p.v_scale};
+  for (uint32_t i0 = part * 32 + lane; i0 < 2 * half_vecs; i0 += 4 * 32 * kParts) {
+    uint4 raw[4][kFp8 ? 2 : 1];
+    uint8_t* dst[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      o[j] = (uint8_t)__nv_cvt_float_to_fp8(__fdiv_rn(In::up(e[j]), scale), __NV_SATFINITE, __NV_E4M3);
-    *reinterpret_cast<uint2*>(dst + col) = packed;
+    for (int u = 0; u < 4; ++u) {
+      const uint32_t i = i0 + u * 32 * kParts;
+      dst[u] = nullptr;
+      if (i < 2 * half_vecs) {
+        const uint32_t half = i >= half_vecs, in = i - (half ? half_vecs : 0), head = quotient(p.row_vecs, in);
+        const uint32_t col = (in - head * p.row_vecs.d) * 16;  // bytes of the cache's row
+        const uint8_t* src = (half ? from[1] : from[0]) + head * (half ? head_step[1] : head_step[0]) + col * (kFp8 ? 2 : 1);
+        raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(src));
+        if constexpr (kFp8) raw[u][1] = __ldcs(reinterpret_cast<const uint4*>(src) + 1);
+        dst[u] = to + (half ? v.half_bytes : 0) + head * v.head_bytes + col;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (!dst[u]) continue;
+      if constexpr (!kFp8) {
+        *reinterpret_cast<uint4*>(dst[u]) = raw[u][0];
+      } else {
+        const bool half = i0 + u * 32 * kParts >= half_vecs;
+        const float scale = half ? p.v_scale : p.k_scale, by = half ? inverse[1] : inverse[0];
+        const uint32_t w[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w,
+                               raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
+        uint32_t o[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          o[k] = to_e4m3(unpack2<In>(w[2 * k]), scale, by) | to_e4m3(unpack2<In>(w[2 * k + 1]), scale, by) << 16;
+        *reinterpret_cast<uint4*>(dst[u]) = make_uint4(o[0], o[1], o[2], o[3]);
+      }
+    }
   }
+}
+
+template <class In, bool kFp8>
+cudaError_t append(const AppendParams& p, int num_sms, cudaStream_t s) {
+  constexpr int kWarps = kAppendThreads / 32;
+  // a warp per token where that fills the GPU, four where it does not
+  if (p.tokens >= 16 * num_sms)
+    return launch_after(append_kernel<In, kFp8, 1>, dim3((unsigned)((p.tokens + kWarps - 1) / kWarps)), kAppendThreads, 0, s, p);
+  return launch_after(append_kernel<In, kFp8, 4>, dim3((unsigned)((p.tokens * 4 + kWarps - 1) / kWarps)), kAppendThreads, 0, s, p);
 }
 
 // ---------------------------------------------------------------- the end of an attention
@@ -166,16 +215,9 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
 
 }  // namespace
 
-cudaError_t launch_append(const AppendParams& p, int type, int cache_type, cudaStream_t s) {
-  const int64_t n = p.tokens * 2 * p.pages.heads * (p.pages.head_dim / 8);
-  const unsigned grid = (unsigned)((n + 255) / 256);
-  if (cache_type != KVX_TYPE_E4M3)
-    append_kernel<Bf16, false><<<grid, 256, 0, s>>>(p);
-  else if (type == KVX_TYPE_BF16)
-    append_kernel<Bf16, true><<<grid, 256, 0, s>>>(p);
-  else
-    append_kernel<Fp16, true><<<grid, 256, 0, s>>>(p);
-  return cudaGetLastError();
+cudaError_t launch_append(const AppendParams& p, int type, int cache_type, int num_sms, cudaStream_t s) {
+  if (cache_type != KVX_TYPE_E4M3) return append<Bf16, false>(p, num_sms, s);  // bytes
+  return type == KVX_TYPE_BF16 ? append<Bf16, true>(p, num_sms, s) : append<Fp16, true>(p, num_sms, s);
 }
 
 cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cudaStream_t s) {

@@ -236,9 +236,10 @@ kvx_status kv_append(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     p.value_head = 2 * rows->value_head_stride;
     p.new_tokens = rows->new_tokens;
     p.num_seqs = batch->num_seqs;
+    p.row_vecs = div31((uint32_t)(g.row / 16));
     p.k_scale = rows->k_scale ? rows->k_scale : 1.f;
     p.v_scale = rows->v_scale ? rows->v_scale : 1.f;
-    return KVX_LAUNCHED(c, launch_append(p, rows->type, rows->cache_type, stream), 1);
+    return KVX_LAUNCHED(c, launch_append(p, rows->type, rows->cache_type, ctx.num_sms, stream), 1);
   });
 }
 
@@ -392,6 +393,8 @@ kvx_status kv_evict(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, co
     p.sinks = e->sinks;
     p.recent = e->recent;
     p.num_layers = (int32_t)layers;
+    p.row_vecs = div31((uint32_t)(g.row / 16));
+    p.units = (int32_t)((most + 31) / 32);
     return KVX_LAUNCHED(c, launch_evict(p, stream), 2);
   });
 }

@@ -50,6 +50,7 @@ struct AppendParams {
   int64_t tokens;
   int64_t key_token, key_head, value_token, value_head;  // strides in bytes
   int32_t new_tokens, num_seqs;
+  Div31 row_vecs;  // 16-byte vectors of a cached row
   float k_scale, v_scale;
 };
 
@@ -95,6 +96,8 @@ struct EvictParams {
   int64_t new_table_stride;
   uint32_t new_table_len;
   int32_t budget, sinks, recent, num_layers;
+  Div31 row_vecs;  // 16-byte vectors of a row
+  int32_t units;   // of 32 kept tokens, of a row of weights
 };
 static_assert(sizeof(EvictParams) <= 4096, "kernel parameters");
 
@@ -129,7 +132,7 @@ struct ScanParams {
 // The segment of the matrix form for a batch, 0 where it is not used; *cut: whether a sequence may have several.
 int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut);
 
-cudaError_t launch_append(const AppendParams& p, int type, int cache_type, cudaStream_t s);
+cudaError_t launch_append(const AppendParams& p, int type, int cache_type, int num_sms, cudaStream_t s);
 cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cudaStream_t s);
 cudaError_t launch_attend_bf16(const AttendParams& p, int num_sms, cudaStream_t s);
 cudaError_t launch_attend_fp16(const AttendParams& p, int num_sms, cudaStream_t s);

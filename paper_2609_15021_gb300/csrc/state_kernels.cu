@@ -76,7 +76,7 @@ __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
 }
 
 // A thread keeps 8 neighbouring channels' window of kWidth inputs in registers and walks up to 32 rows of
-// one sequence, four rows' loads in flight.  Bound by its bytes: a row in and a row out, the window's rows
+// one sequence, the next four rows' loads in flight behind the four it computes.  Bound by its bytes: a row in and a row out, the window's rows
 // read again at the head of a piece (3 of 32, from L2).  The piece at a sequence's head, which alone reads the slot,
 // also writes it, so a slot may be updated in place.
 template <class E, int kWidth>
@@ -123,11 +123,16 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
       old[j] = *reinterpret_cast<const uint4*>(in + ((int64_t)j * p.channels + c) * 2);
     unpack8<E>(old[j], x[j + 1]);
   }
-  for (int64_t t = begin; t < end; t += 4) {
-    uint4 raw[4];
+  uint4 raw[4], next[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (t + u < end) raw[u] = in_row(t + u);
+  for (int u = 0; u < 4; ++u)
+    if (begin + u < end) next[u] = in_row(begin + u);
+  for (int64_t t = begin; t < end; t += 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      raw[u] = next[u];
+      if (t + 4 + u < end) next[u] = in_row(t + 4 + u);
+    }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       if (t + u >= end) break;
