@@ -9,24 +9,27 @@ namespace kvx {
 namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWarps = kSelectThreads / 32;
-constexpr int kDigitBits = 8, kBins = 1 << kDigitBits;
+constexpr int kBins = 2048;  // digits of 11, 11 and 10 bits
 
-// Whole numbers in the order of the weights: NaN as -inf, -0 as +0.
+// Whole numbers in the order of the weights: NaN as -inf, -0 as +0.  None is kNone or kAlways.
+constexpr uint32_t kNone = 0, kAlways = UINT32_MAX;
 __device__ __forceinline__ uint32_t rank_of(float w) {
   if (isnan(w)) w = -INFINITY;
   const uint32_t u = __float_as_uint(w + 0.f);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One CTA per row of weights (head, sequence, layer).  The smallest kept weight is found as the m-th largest
-// rank, eight bits at a time, by counting the ranks that share the bits found so far; of the tokens that have just
+// One CTA per row of weights (head, sequence, layer).  Tokens that are kept whatever their weight have the largest
+// rank of all.  The smallest kept weight is found as the m-th largest
+// rank, 11 bits at a time, by counting the ranks that share the bits found so far (the first 11 hold the exponent and
+// two bits more, which spreads weights over enough counters that a warp's seldom meet); of the tokens that have just
 // that rank the first ones are kept.  A token's place among the kept ones is then
 //   #(greater before it) + min(#(equal before it), how many equal ones are kept),
 // which one scan of pairs of counts gives.  Up to 1024 * kEach weights are read once and stay in registers; longer
 // rows are read again, tile by tile, for every count.  Bound by the weights' bytes, and where rows are few by the
 // counts' barriers.
 template <int kEach>
-__global__ void __launch_bounds__(kSelectThreads, kEach > 16 ? 1 : 2) select_kernel(const __grid_constant__ EvictParams p) {
+__global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_constant__ EvictParams p) {
   const PagesView& v = p.pages;
   constexpr int kTile = kSelectThreads * kEach;
   __shared__ int32_t hist[kBins];
@@ -54,10 +57,9 @@ __global__ void __launch_bounds__(kSelectThreads, kEach > 16 ? 1 : 2) select_ker
     }
     return;
   }
-  // the middle: tokens that only their weight keeps
-  const int32_t first = p.sinks, last = n - p.recent;
-  int32_t want = keep - p.sinks - p.recent;    // of the middle
-  uint32_t prefix = want > 0 ? 0 : UINT32_MAX;  // no weight's rank is above UINT32_MAX
+  const int32_t last = n - p.recent;
+  int32_t want = keep;
+  uint32_t prefix = 0;
 
   uint32_t rank[kEach];  // of tokens base + k * 1024 + threadIdx.x
   auto load = [&](int32_t base) {
@@ -65,51 +67,51 @@ __global__ void __launch_bounds__(kSelectThreads, kEach > 16 ? 1 : 2) select_ker
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       const int32_t i = base + k * kSelectThreads + threadIdx.x;
-      x[k] = i >= first && i < last ? w[i] : 0.f;
+      x[k] = i < n ? w[i] : 0.f;
     }
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) rank[k] = rank_of(x[k]);
+    for (int k = 0; k < kEach; ++k) {
+      const int32_t i = base + k * kSelectThreads + threadIdx.x;
+      rank[k] = i >= n ? kNone : i < p.sinks || i >= last ? kAlways : rank_of(x[k]);
+    }
   };
   load(0);
-  if (want > 0) {
+  {
 #pragma unroll 1
-    for (int shift = 32 - kDigitBits; shift >= 0; shift -= kDigitBits) {
-      if (threadIdx.x < kBins) hist[threadIdx.x] = 0;
+    for (int shift = 21, width = 11; shift >= 0; width = shift < 11 ? shift : 11, shift -= width) {
+      hist[threadIdx.x] = hist[threadIdx.x + kSelectThreads] = 0;
       __syncthreads();
 #pragma unroll 1
       for (int32_t base = 0; base < n; base += kTile) {
         if (n > kTile) load(base);
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-          const int32_t i = base + k * kSelectThreads + threadIdx.x;
           // the bits above the digit, shifted in two steps as the first digit has none
-          if (i >= first && i < last && (rank[k] ^ prefix) >> shift >> kDigitBits == 0)
-            atomicAdd(&hist[rank[k] >> shift & (kBins - 1)], 1);
+          if ((rank[k] ^ prefix) >> shift >> width == 0)
+            atomicAdd(&hist[rank[k] >> shift & ((1 << width) - 1)], 1);
         }
       }
       __syncthreads();
-      if (warp == 0) {  // the digit of the want'th largest: sums from the top, eight bins a lane
-        int32_t mine = 0, bins[kBins / 32];
-#pragma unroll
-        for (int k = 0; k < kBins / 32; ++k) mine += bins[k] = hist[kBins - 1 - (lane * (kBins / 32) + k)];
-        int32_t upto = mine;
-        for (int d = 1; d < 32; d <<= 1) {
-          const int32_t y = __shfl_up_sync(~0u, upto, d);
-          if (lane >= d) upto += y;
-        }
-        int32_t left = want - (upto - mine);
-        if (left > 0 && left <= mine) {  // one lane's
-          int k = 0;
-#pragma unroll
-          for (int j = 0; j < kBins / 32 - 1; ++j)
-            if (k == j && left > bins[j]) left -= bins[j], ++k;
-          prefix_s = prefix | (uint32_t)(kBins - 1 - (lane * (kBins / 32) + k)) << shift;
-          want_s = left;
-        }
+      // the digit of the want'th largest: sums from the top, two bins a thread
+      const int32_t top_bin = kBins - 1 - 2 * threadIdx.x, b0 = hist[top_bin], b1 = hist[top_bin - 1];
+      int32_t upto = b0 + b1;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int32_t y = __shfl_up_sync(~0u, upto, d);
+        if (lane >= d) upto += y;
+      }
+      if (lane == 31) warp_above[warp] = upto;
+      __syncthreads();
+      int32_t before = upto - b0 - b1;
+      for (int i = 0; i < warp; ++i) before += warp_above[i];
+      const int32_t left = want - before;
+      if (left > 0 && left <= b0 + b1) {  // one thread's
+        prefix_s = prefix | (uint32_t)(left > b0 ? top_bin - 1 : top_bin) << shift;
+        want_s = left > b0 ? left - b0 : left;
       }
       __syncthreads();
       prefix = prefix_s;
       want = want_s;
+      if (shift == 0) break;
     }
   }
   // want: how many tokens of rank `prefix` itself are kept
@@ -120,10 +122,7 @@ __global__ void __launch_bounds__(kSelectThreads, kEach > 16 ? 1 : 2) select_ker
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-      const int32_t i = base + k * kSelectThreads + threadIdx.x;
-      const bool middle = i >= first && i < last;
-      const uint32_t gt = __ballot_sync(~0u, i < n && (!middle || rank[k] > prefix));
-      const uint32_t eq = __ballot_sync(~0u, middle && rank[k] == prefix);
+      const uint32_t gt = __ballot_sync(~0u, rank[k] > prefix), eq = __ballot_sync(~0u, rank[k] == prefix);
       if (lane == 0) above[k * kSelectWarps + warp] = __popc(gt), equal[k * kSelectWarps + warp] = __popc(eq);
     }
     __syncthreads();
@@ -149,10 +148,10 @@ __global__ void __launch_bounds__(kSelectThreads, kEach > 16 ? 1 : 2) select_ker
     }
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-      const int32_t i = base + k * kSelectThreads + threadIdx.x;
-      const bool middle = i >= first && i < last;
-      const bool is_gt = i < n && (!middle || rank[k] > prefix), is_eq = middle && rank[k] == prefix;
+      const bool is_gt = rank[k] > prefix, is_eq = rank[k] == prefix;
       const uint32_t gt = __ballot_sync(~0u, is_gt), eq = __ballot_sync(~0u, is_eq), under = (1u << lane) - 1;
+      if ((gt | eq) == 0) continue;
+      const int32_t i = base + k * kSelectThreads + threadIdx.x;
       const int32_t e = equal[k * kSelectWarps + warp] + __popc(eq & under);
       if (is_gt || (is_eq && e < want)) {
         const int32_t at = above[k * kSelectWarps + warp] + __popc(gt & under) + min(e, want);

@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
     for (int64_t t = begin; t < end; ++t) *out_row(t) = make_uint4(0, 0, 0, 0);
     return;
   }
-  float w[kWidth][8], bias[8] = {}, x[kWidth][8];
+  float w[kWidth][8], bias[8] = {}, x[kPast + 4][8];  // the inputs before four rows, and theirs
   {
     float flat[8 * kWidth];
 #pragma unroll
@@ -121,36 +121,54 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
       old[j] = make_uint4(0, 0, 0, 0);
     else
       old[j] = *reinterpret_cast<const uint4*>(in + ((int64_t)j * p.channels + c) * 2);
-    unpack8<E>(old[j], x[j + 1]);
+    unpack8<E>(old[j], x[j]);
   }
-  uint4 raw[4], next[4];
+  auto row = [&](int u, uint4* to) {  // of the four
+    float y[8];
 #pragma unroll
-  for (int u = 0; u < 4; ++u)
-    if (begin + u < end) next[u] = in_row(begin + u);
-  for (int64_t t = begin; t < end; t += 4) {
+    for (int k = 0; k < 8; ++k) {
+      y[k] = bias[k];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      raw[u] = next[u];
-      if (t + 4 + u < end) next[u] = in_row(t + 4 + u);
+      for (int j = 0; j < kWidth; ++j) y[k] += w[j][k] * x[u + j][k];
+    }
+    if (p.silu) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) y[k] *= rcp(1.f + ex2(-kLog2e * y[k]));
+    }
+    *to = make_uint4(pack2<E>(y[0], y[1]), pack2<E>(y[2], y[3]), pack2<E>(y[4], y[5]), pack2<E>(y[6], y[7]));
+  };
+  const uint8_t* from = p.x + (begin * p.x_stride + c) * 2;
+  uint8_t* to = p.out + (begin * p.out_stride + c) * 2;
+  const int64_t from_step = p.x_stride * 2, to_step = p.out_stride * 2;
+  int32_t left = (int32_t)(end - begin);
+  uint4 next[4];
+  if (left >= 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) next[u] = __ldcs(reinterpret_cast<const uint4*>(from + u * from_step));
+  }
+  for (; left >= 4; left -= 4) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) unpack8<E>(next[u], x[kPast + u]);
+    from += 4 * from_step;
+    if (left >= 8) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) next[u] = __ldcs(reinterpret_cast<const uint4*>(from + u * from_step));
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (t + u >= end) break;
+    for (int u = 0; u < 4; ++u) row(u, reinterpret_cast<uint4*>(to + u * to_step));
+    to += 4 * to_step;
 #pragma unroll
-      for (int j = 0; j < kPast; ++j)
+    for (int j = 0; j < kPast; ++j)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[j][k] = x[j + 1][k];
-      unpack8<E>(raw[u], x[kPast]);
-      float y[8];
+      for (int k = 0; k < 8; ++k) x[j][k] = x[j + 4][k];
+  }
+  for (; left > 0; --left, from += from_step, to += to_step) {
+    unpack8<E>(*reinterpret_cast<const uint4*>(from), x[kPast]);
+    row(0, reinterpret_cast<uint4*>(to));
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        y[k] = bias[k];
+    for (int j = 0; j < kPast; ++j)
 #pragma unroll
-        for (int j = 0; j < kWidth; ++j) y[k] += w[j][k] * x[j][k];
-        if (p.silu) y[k] *= rcp(1.f + ex2(-kLog2e * y[k]));
-      }
-      *out_row(t + u) = make_uint4(pack2<E>(y[0], y[1]), pack2<E>(y[2], y[3]), pack2<E>(y[4], y[5]), pack2<E>(y[6], y[7]));
-    }
+      for (int k = 0; k < 8; ++k) x[j][k] = x[j + 1][k];
   }
   if (piece == 0) {
 #pragma unroll
