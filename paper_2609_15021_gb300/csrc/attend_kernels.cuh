@@ -10,7 +10,7 @@
 // instruction, so that a group of up to 8 heads wastes nothing.  mma.sync does them at a few
 // per cent of its rate; what the kernel is built for is bytes in flight:
 //
-//   * The work is cut into steps of 16 keys of one item (sequence, KV head, block
+//   * The work is cut into steps of 16 or 32 keys of one item (sequence, KV head, block
 //     of query rows).  The grid's CTAs take equal runs of the steps of all items,
 //     whatever the lengths, which are read on the device (an item counts for kItemSteps
 //     more than it has, what beginning and ending one takes).  A run that covers only
@@ -18,7 +18,7 @@
 //     joins the parts in their order, a CTA per row.  (Joined by the CTA that came last to
 //     an item, the same took 11 us instead of 3 at 38 parts: few CTAs, in code that is in no
 //     instruction cache.)
-//   * In a CTA, four warps take the steps in turn.  A warp has a ring of its own in shared
+//   * In a CTA, three or four warps take the steps in turn.  A warp has a ring of its own in shared
 //     memory and shares nothing with the others until a piece ends, so there is no
 //     barrier in the loop.
 //   * The ring is filled by 16-byte asynchronous copies, row by row, wherever the pages
@@ -44,8 +44,6 @@
 namespace kvx {
 namespace {
 
-constexpr int kStep = 16;  // keys of a step
-constexpr int kAttendThreads = 128, kWarps = kAttendThreads / 32;
 constexpr int kMaxCtas = 320;  // of a launch
 constexpr int kItemSteps = 6;
 // Exponents are relative to 2^10 below the largest score so far (fp16 probabilities stay
@@ -57,10 +55,12 @@ struct AttendShape {
   static constexpr int kElem = (int)sizeof(typename C::T);
   static constexpr int kRowBytes = kDim * kElem;
   static constexpr int kPitch = kRowBytes + 16;  // an odd number of vectors
+  static constexpr int kBlocks = attend_blocks(kDim, kElem, kTiles), kStep = 16 * kBlocks;  // keys of a step
   static constexpr int kHalfBytes = kStep * kPitch;
   static constexpr int kStageBytes = 2 * kHalfBytes;  // K rows, then V rows
+  static constexpr int kWarps = kStageBytes > 16 * 1024 && kBlocks == 2 ? 3 : 4, kThreads = 32 * kWarps;
   static constexpr int kVecs = kRowBytes / 16;
-  static constexpr int kRowsPerLoad = 32 / kVecs > kStep ? kStep : 32 / kVecs;
+  static constexpr int kRowsPerLoad = 32 / kVecs;
   static constexpr int kLoads = kStep / kRowsPerLoad;  // of K, and of V, by a lane
   static constexpr int kRows = 8 * kTiles;
   // the queries as the products' right factor: [16 dims][tile] x 8 bytes a lane, kept in registers where they fit
@@ -98,11 +98,11 @@ __device__ __forceinline__ float column_sum(float v) {
   return v + __shfl_xor_sync(~0u, v, 16);
 }
 
-// 16-key steps of a sequence, from the step that holds the first key any of its
-// queries sees; *first: that step's first key.
+// Steps of a sequence, from a multiple of 16 keys (*first) that the first key any of its queries sees is not before.
+template <int kStep>
 __device__ __forceinline__ int32_t steps_of(const AttendParams& p, int32_t length, int32_t* first) {
   const int32_t lo = p.window > 0 ? max(0, length - p.new_tokens + 1 - p.window) : 0;
-  *first = lo & ~(kStep - 1);
+  *first = lo & ~15;
   return (length - *first + kStep - 1) / kStep;
 }
 
@@ -110,6 +110,7 @@ __device__ __forceinline__ int32_t steps_of(const AttendParams& p, int32_t lengt
 __device__ __forceinline__ int32_t run_steps(int32_t steps) { return steps > 0 ? steps + kItemSteps : 0; }
 
 // Sum over the CTA of one value a thread, to all.
+template <int kWarps>
 __device__ __forceinline__ long long cta_sum(long long v, long long* buf) {
   for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
   if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
@@ -138,11 +139,13 @@ struct Runs {
 };
 
 template <class C, int kDim, int kTiles>
-__global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::kCtas)
+__global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, AttendShape<C, kDim, kTiles>::kCtas)
     attend_kernel(const __grid_constant__ AttendParams p) {
   using S = AttendShape<C, kDim, kTiles>;
   constexpr bool kWide = S::kElem == 1;  // cache to be widened
-  constexpr int kKs = kDim / 16, kRows = S::kRows;
+  constexpr int kKs = kDim / 16, kRows = S::kRows, kBlocks = S::kBlocks, kStep = S::kStep;
+  constexpr int kWarps = S::kWarps, kAttendThreads = S::kThreads;
+  constexpr uint32_t kAllKeys = kStep == 32 ? ~0u : 0xFFFFu;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ long long buf[kWarps + 1];
   __shared__ uint32_t masks[kWarps][S::kStages];
@@ -162,9 +165,9 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
   for (int32_t s = threadIdx.x; s < v.num_seqs; s += kAttendThreads) {
     int32_t first;
     if (blockIdx.x == 0) check_length(v, s);
-    total += run_steps(steps_of(p, length_of(v, s), &first));
+    total += run_steps(steps_of<kStep>(p, length_of(v, s), &first));
   }
-  total = cta_sum(total, buf) * per_seq;
+  total = cta_sum<kWarps>(total, buf) * per_seq;
   for (int32_t s = blockIdx.x; s < v.num_seqs; s += gridDim.x) {  // sequences without a key
     if (length_of(v, s) > 0) continue;
     for (int32_t i = threadIdx.x; i < v.heads * rows * (v.head_dim / 4); i += kAttendThreads) {
@@ -185,7 +188,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
   for (int32_t base = 0; base < v.num_seqs && v.num_seqs > 1; base += kAttendThreads) {
     int32_t first;
     const int32_t s = base + threadIdx.x;
-    const long long mine = s < v.num_seqs ? (long long)run_steps(steps_of(p, length_of(v, s), &first)) * per_seq : 0;
+    const long long mine = s < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, length_of(v, s), &first)) * per_seq : 0;
     long long before = mine;  // inclusive scan over the warp
     for (int d = 1; d < 32; d <<= 1) {
       const long long y = __shfl_up_sync(~0u, before, d);
@@ -217,24 +220,22 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
   uint8_t* ring = smem + warp * S::kStages * S::kStageBytes;
   const uint32_t ring_at = smem_at(ring);
   uint8_t* query_smem = smem + S::kQueryAt;
-  const int ks_used = (v.head_dim + 15) / 16;
   // where a lane's matrices begin in a stage (K: keys 0-7 and 8-15 of 16 dims, or of 2 x 16 to widen; V the same,
   // transposed), and its vectors of a row
   const uint32_t at_lane_k = ((lane & 7) + (((lane >> 3) & 1) << 3)) * S::kPitch + (lane >> 4) * 16;
   const uint32_t at_lane_v = S::kHalfBytes + (kWide ? ((lane & 7) + (((lane >> 3) & 1) << 3)) * S::kPitch + (lane >> 4) * 16
                                                     : ((lane & 7) + ((lane >> 4) << 3)) * S::kPitch + ((lane >> 3) & 1) * 16);
   const int vec = lane % S::kVecs, vec_row = lane / S::kVecs;
-  const bool vec_used = vec * 16 < v.head_dim * S::kElem && vec_row < S::kRowsPerLoad;
+  const bool vec_used = vec * 16 < v.head_dim * S::kElem;
   const uint32_t at_lane_copy = vec_row * S::kPitch + vec * 16;
   const uint32_t row_bytes = (uint32_t)v.head_dim * S::kElem;
-  const bool padded = row_bytes % 32 != 0;  // the products take 32 bytes of a row at a time
 
   for (long long at = begin; at < end;) {
     // The piece: steps [i0, i1) of one item.
     int32_t first_key, length, steps;
     for (;;) {
       length = length_of(v, seq);
-      steps = steps_of(p, length, &first_key);
+      steps = steps_of<kStep>(p, length, &first_key);
       if (at < seq_begin + (long long)run_steps(steps) * per_seq) break;
       seq_begin += (long long)run_steps(steps) * per_seq;
       if (++seq >= v.num_seqs) return;  // lengths that changed under the kernel
@@ -247,10 +248,10 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
     const int32_t here = min(rows - row0, kRows);  // rows of this block
     const int32_t* table = v.tables + seq * v.table_stride;
 
-    // Lane r (and r + 16) finds key r of a step, in two parts, so that nothing waits for the table: its entry
+    // Lane r (and, of 16 keys, r + 16) finds key r of a step, in two parts, so that nothing waits for the table: its entry
     // and the place in the block first, the row when it is used.
     auto look = [&](int32_t i) -> uint2 {
-      const uint32_t key = first_key + i * kStep + (lane & 15);
+      const uint32_t key = first_key + i * kStep + lane % kStep;
       const bool there = i < i1 && (int32_t)key < length;
       const uint32_t page = quotient(v.by_block, key), slot = key - page * v.by_block.d;
       const uint32_t block = quotient(v.by_pack, page), in = page - block * v.by_pack.d;
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
     auto row_of = [&](uint2 l, int32_t i) -> uint32_t {
       if (l.x < v.entries && l.y != kNoRow) return l.x * (v.by_pack.d * v.page_rows) + l.y;
       if (l.y != kNoRow) {
-        const uint32_t key = first_key + i * kStep + (lane & 15);
+        const uint32_t key = first_key + i * kStep + lane % kStep;
         atomicMin(v.err, (long long)quotient(v.by_pack, quotient(v.by_block, key)));
       }
       return kNoRow;
@@ -270,10 +271,10 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
     auto issue = [&](int32_t i, uint2 l, uint32_t to) {
       if (i < i1) {
         const uint32_t row = row_of(l, i);
-        const uint32_t mask = __ballot_sync(~0u, row != kNoRow) & 0xFFFFu;
+        const uint32_t mask = __ballot_sync(~0u, row != kNoRow) & kAllKeys;
         if (lane == 0) masks[warp][to] = mask;
         const uint32_t dst = ring_at + to * S::kStageBytes + at_lane_copy;
-        if (mask == 0xFFFFu) {
+        if (mask == kAllKeys) {
 #pragma unroll
           for (int k = 0; k < S::kLoads; ++k) {
             const uint32_t r = __shfl_sync(~0u, row, k * S::kRowsPerLoad + vec_row);
@@ -362,7 +363,7 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
         }
       }
     }
-    if (padded) {  // columns that no row has are read by the products
+    if (row_bytes < S::kRowBytes) {  // columns that no row has are read by the products
       constexpr int kPerRow = S::kPitch / 16;
       for (int k = threadIdx.x; k < kWarps * S::kStages * 2 * kStep * kPerRow; k += kAttendThreads)
         if (k % kPerRow * 16 >= (int)row_bytes)
@@ -403,112 +404,129 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
       const uint32_t mask = masks[warp][stage];
       const int32_t key0 = first_key + i * kStep;
 
-      float sc[kTiles][4];
+      float sc[kBlocks][kTiles][4];
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+      for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[t][e] = 0.f;
-      auto score = [&](int ks, const uint32_t (&a)[4]) {
+        for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[n][t][e] = 0.f;
+      auto score = [&](int n, int ks, const uint32_t (&a)[4]) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
           if constexpr (S::kQueryInRegs) {
-            mma<C>(sc[t], a, qf[ks][t][0], qf[ks][t][1]);
+            mma<C>(sc[n][t], a, qf[ks][t][0], qf[ks][t][1]);
           } else {
             const uint2 b = *reinterpret_cast<const uint2*>(query_smem + ((ks * kTiles + t) * 32 + lane) * 8);
-            mma<C>(sc[t], a, b.x, b.y);
+            mma<C>(sc[n][t], a, b.x, b.y);
           }
         }
       };
 #pragma unroll
       for (int ks = 0; ks < kKs; ks += kWide ? 2 : 1) {
-        if (ks * 16 < v.head_dim) {
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) {
           uint32_t b[4];
           if constexpr (!kWide) {
-            load_matrices(b, at_k + ks * 32);
-            score(ks, b);
+            load_matrices(b, at_k + n * 16 * S::kPitch + ks * 32);
+            score(n, ks, b);
           } else {
-            load_matrices(b, at_k + ks * 16);
+            load_matrices(b, at_k + n * 16 * S::kPitch + ks * 16);
             uint32_t a[4];
             widen4(b[0], a[0], a[2]);
             widen4(b[1], a[1], a[3]);
-            score(ks, a);
+            score(n, ks, a);
             widen4(b[2], a[0], a[2]);
             widen4(b[3], a[1], a[3]);
-            score(ks + 1, a);
+            score(n, ks + 1, a);
           }
         }
       }
 
-      // Scores in powers of two; element e of tile t: key quad + 8 (e / 2), row 8 t + 2 sub + e % 2.
-      const bool whole = mask == 0xFFFFu && key0 + kStep <= all_to && key0 >= all_from;
-      uint32_t unseen = 0;  // a bit for every element of every tile
+      // Scores in powers of two; element e of block n, tile t: key 16 n + quad + 8 (e / 2), row 8 t + 2 sub + e % 2.
+      const bool whole = mask == kAllKeys && key0 + kStep <= all_to && key0 >= all_from;
+      uint32_t unseen[kBlocks] = {};  // a bit for every element of every tile
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = sc[t][e] * scale2[t][e & 1];
-          if (!plain_scores) {
-            const int r = t * 8 + 2 * sub + (e & 1);
-            // tanh y = 1 - 2 / (1 + e^2y): an absolute error of some 2^-22, which is what counts in an exponent
-            if (p.softcap > 0.f) x = cap2 - 2.f * cap2 * rcp(1.f + ex2(x * to_cap));
-            x += row_slope[r] * (key0 + quad + 8 * (e >> 1) - row_pos[r]);
-          }
-          sc[t][e] = x;
-        }
-      if (!whole) {
+      for (int n = 0; n < kBlocks; ++n)
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int k = quad + 8 * (e >> 1), pos = row_pos[t * 8 + 2 * sub + (e & 1)];
-            if (!(mask >> k & 1) || key0 + k > pos || (p.window > 0 && key0 + k <= pos - p.window)) {
-              sc[t][e] = -INFINITY;
-              unseen |= 1u << (4 * t + e);
+            float x = sc[n][t][e] * scale2[t][e & 1];
+            if (!plain_scores) {
+              const int r = t * 8 + 2 * sub + (e & 1);
+              // tanh y = 1 - 2 / (1 + e^2y): an absolute error of some 2^-22, which is what counts in an exponent
+              if (p.softcap > 0.f) x = cap2 - 2.f * cap2 * rcp(1.f + ex2(x * to_cap));
+              if (p.slopes) x += row_slope[r] * (key0 + n * 16 + quad + 8 * (e >> 1) - row_pos[r]);
             }
+            sc[n][t][e] = x;
           }
+      if (!whole) {
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int k = n * 16 + quad + 8 * (e >> 1), pos = row_pos[t * 8 + 2 * sub + (e & 1)];
+              if (!(mask >> k & 1) || key0 + k > pos || (p.window > 0 && key0 + k <= pos - p.window)) {
+                sc[n][t][e] = -INFINITY;
+                unseen[n] |= 1u << (4 * t + e);
+              }
+            }
       }
       if (scores) {
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          const int32_t r = row0 + t * 8 + 2 * sub;
-          if (r < p.score_rows) {
-            float* to = scores + (int64_t)(key0 + quad) * p.score_rows + r;
-            *reinterpret_cast<float2*>(to) = make_float2(sc[t][0], sc[t][1]);
-            *reinterpret_cast<float2*>(to + 8 * p.score_rows) = make_float2(sc[t][2], sc[t][3]);
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            const int32_t r = row0 + t * 8 + 2 * sub;
+            if (r < p.score_rows) {
+              float* to = scores + (int64_t)(key0 + n * 16 + quad) * p.score_rows + r;
+              *reinterpret_cast<float2*>(to) = make_float2(sc[n][t][0], sc[n][t][1]);
+              *reinterpret_cast<float2*>(to + 8 * p.score_rows) = make_float2(sc[n][t][2], sc[n][t][3]);
+            }
           }
-        }
       }
 
+      auto lane_max = [&](int t, int j) {
+        float top = fmaxf(sc[0][t][j], sc[0][t][2 + j]);
+#pragma unroll
+        for (int n = 1; n < kBlocks; ++n) top = fmaxf(top, fmaxf(sc[n][t][j], sc[n][t][2 + j]));
+        return top;
+      };
       bool raise = false;
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) raise |= fmaxf(sc[t][j], sc[t][2 + j]) > m[t][j] + kSlack;
+        for (int j = 0; j < 2; ++j) raise |= lane_max(t, j) > m[t][j] + kSlack;
       if (__any_sync(~0u, raise)) {
 #pragma unroll
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const float top = column_max(fmaxf(sc[t][j], sc[t][2 + j])) - kBelow;
-            if (top > m[t][j]) {
-              const float keep = factor(m[t][j], top);
-              m[t][j] = top;
-              l[t][j] *= keep;
+            const float top = fmaxf(m[t][j], column_max(lane_max(t, j)) - kBelow);
+            const float keep = factor(m[t][j], top);
+            m[t][j] = top;
+            l[t][j] *= keep;
 #pragma unroll
-              for (int c = 0; c < kKs; ++c) acc[c][t][j] *= keep, acc[c][t][2 + j] *= keep;
-            }
+            for (int c = 0; c < kKs; ++c) acc[c][t][j] *= keep, acc[c][t][2 + j] *= keep;
           }
       }
-      uint32_t pf[kTiles][2];
+      uint32_t pf[kBlocks][kTiles][2];
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
+        const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sc[t][e] = ex2(sc[t][e] - (m[t][e & 1] == -INFINITY ? 0.f : m[t][e & 1]));
-          l[t][e & 1] += sc[t][e];
+        for (int n = 0; n < kBlocks; ++n) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            sc[n][t][e] = ex2(sc[n][t][e] - ref[e & 1]);
+            l[t][e & 1] += sc[n][t][e];
+          }
+          pf[n][t][0] = transpose(pack2<C>(sc[n][t][0], sc[n][t][1]));
+          pf[n][t][1] = transpose(pack2<C>(sc[n][t][2], sc[n][t][3]));
         }
-        pf[t][0] = transpose(pack2<C>(sc[t][0], sc[t][1]));
-        pf[t][1] = transpose(pack2<C>(sc[t][2], sc[t][3]));
       }
 
       // A value that is not finite must not reach the rows that do not see it (0 x inf): where a
@@ -532,58 +550,62 @@ __global__ void __launch_bounds__(kAttendThreads, AttendShape<C, kDim, kTiles>::
       if (!odd) {
 #pragma unroll
         for (int c = 0; c < kKs; c += kWide ? 2 : 1) {
-          if (c * 16 < v.head_dim) {
+#pragma unroll
+          for (int n = 0; n < kBlocks; ++n) {
             uint32_t b[4];
             if constexpr (!kWide) {
-              load_matrices_t(b, at_v + c * 32);
+              load_matrices_t(b, at_v + n * 16 * S::kPitch + c * 32);
 #pragma unroll
-              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c][t], b, pf[t][0], pf[t][1]);
+              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c][t], b, pf[n][t][0], pf[n][t][1]);
             } else {
               // a transposed pair of bytes is two neighbouring dims of a key: the even ones are the product's
               // first eight rows, the odd ones the others
-              load_matrices_t(b, at_v + c * 16);
+              load_matrices_t(b, at_v + n * 16 * S::kPitch + c * 16);
 #pragma unroll
               for (int q = 0; q < 4; ++q) b[q] = __byte_perm(b[q], 0, 0x3120);
               uint32_t a[4];
               widen4(b[0], a[0], a[1]);
               widen4(b[1], a[2], a[3]);
 #pragma unroll
-              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c][t], a, pf[t][0], pf[t][1]);
+              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c][t], a, pf[n][t][0], pf[n][t][1]);
               widen4(b[2], a[0], a[1]);
               widen4(b[3], a[2], a[3]);
 #pragma unroll
-              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c + 1][t], a, pf[t][0], pf[t][1]);
+              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c + 1][t], a, pf[n][t][0], pf[n][t][1]);
             }
           }
         }
       } else {
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
 #pragma unroll 1
-        for (int k = 0; k < kStep; ++k) {
-          float pk[kTiles][2];
-          bool see[kTiles][2];
+          for (int k = 0; k < 16; ++k) {
+            float pk[kTiles][2];
+            bool see[kTiles][2];
 #pragma unroll
-          for (int t = 0; t < kTiles; ++t)
+            for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const int from = (k & 7) * 4 + sub;
-              pk[t][j] = __shfl_sync(~0u, k < 8 ? sc[t][j] : sc[t][2 + j], from);
-              see[t][j] = !(__shfl_sync(~0u, unseen, from) >> (4 * t + (k < 8 ? 0 : 2) + j) & 1);
-            }
+              for (int j = 0; j < 2; ++j) {
+                const int from = (k & 7) * 4 + sub;
+                pk[t][j] = __shfl_sync(~0u, k < 8 ? sc[n][t][j] : sc[n][t][2 + j], from);
+                see[t][j] = !(__shfl_sync(~0u, unseen[n], from) >> (4 * t + (k < 8 ? 0 : 2) + j) & 1);
+              }
 #pragma unroll
-          for (int c = 0; c < kKs; ++c)
+            for (int c = 0; c < kKs; ++c)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int col = c * 16 + (kWide ? quad * 2 + u : quad + 8 * u);
-              if (col >= v.head_dim) continue;
-              const uint8_t* at_e = ring + stage * S::kStageBytes + S::kHalfBytes + k * S::kPitch + col * S::kElem;
-              const float x = C::up(*reinterpret_cast<const typename C::T*>(at_e));
+              for (int u = 0; u < 2; ++u) {
+                const int col = c * 16 + (kWide ? quad * 2 + u : quad + 8 * u);
+                if (col >= v.head_dim) continue;
+                const uint8_t* at_e =
+                    ring + stage * S::kStageBytes + S::kHalfBytes + (n * 16 + k) * S::kPitch + col * S::kElem;
+                const float x = C::up(*reinterpret_cast<const typename C::T*>(at_e));
 #pragma unroll
-              for (int t = 0; t < kTiles; ++t)
+                for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
-                  if (see[t][j]) acc[c][t][2 * u + j] += pk[t][j] * x;
-            }
-        }
+                  for (int j = 0; j < 2; ++j)
+                    if (see[t][j]) acc[c][t][2 * u + j] += pk[t][j] * x;
+              }
+          }
       }
       __syncwarp();
       issue(i + S::kStages * kWarps, next, stage);
@@ -684,7 +706,7 @@ template <class C, int kDim, int kTiles>
 cudaError_t attend(const AttendParams& p, int num_sms, cudaStream_t s) {
   using S = AttendShape<C, kDim, kTiles>;
   const int grid = (int)std::min<int64_t>(std::min(num_sms * S::kCtas, kMaxCtas), std::max<int64_t>(1, p.most_steps / p.min_steps));
-  return launch_after(attend_kernel<C, kDim, kTiles>, dim3(grid), kAttendThreads, S::kSmem, s, p);
+  return launch_after(attend_kernel<C, kDim, kTiles>, dim3(grid), S::kThreads, S::kSmem, s, p);
 }
 
 template <class C>

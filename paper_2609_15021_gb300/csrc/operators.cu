@@ -174,7 +174,7 @@ AttendSpace attend_space(const CtxView& ctx, const PagesView& v, const kvx_atten
   w.row_lse2 = w.parts + up((int64_t)ctx.num_sms * 2 * 2 * block * (attend_pad(v.head_dim) + 2) * 4);
   w.scores = w.row_lse2;
   w.bytes = w.row_lse2;
-  w.score_stride = ((int64_t)v.max_length + 15) / 16 * 16;
+  w.score_stride = ((int64_t)v.max_length + 47) / 16 * 16;  // steps of 32 keys may begin at any multiple of 16
   w.score_rows = (int32_t)((rows + 1) / 2 * 2);
   if (a->weights) {
     w.scores += up((int64_t)v.num_seqs * v.heads * rows * 4);
@@ -324,7 +324,8 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     const int64_t blocks = (rows + block - 1) / block;
     p.part_rows = block;
     p.part_dim = attend_pad(p.pages.head_dim);
-    p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * (space.score_stride / 16);
+    const int32_t step = 16 * attend_blocks(p.part_dim, pool->elem_bytes, block / 8);
+    p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * ((p.pages.max_length + 15) / step + 1 + 6);
     p.min_steps = 4 + 6;  // of four warps, and what an item counts for besides
     return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), 2);
   });

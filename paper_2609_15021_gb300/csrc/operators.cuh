@@ -64,7 +64,7 @@ struct AttendParams {
   int64_t weights_seq, weights_head;             // strides in elements
   int32_t type, q_heads, group, new_tokens, window;
   float scale, softcap, k_scale, v_scale;
-  int64_t most_steps;     // of 16 keys that the batch may have, over all items
+  int64_t most_steps;     // that the batch may have, over all items
   int32_t min_steps;      // the least a CTA is started for
   // workspace
   int2* items;            // [item]: its first part and their number, 0 where there are none
@@ -83,6 +83,10 @@ inline int attend_tiles(int32_t head_dim, int32_t rows) {
   const int each = (tiles + blocks - 1) / blocks;
   return each == 3 && most == 4 ? 4 : each;
 }
+
+// 16-key blocks that a step of the attention takes: two where a warp's sums leave the registers for them and a step's
+// rows half of a warp's shared memory.
+constexpr int attend_blocks(int pad, int elem, int tiles) { return tiles == 1 && pad * elem <= 256 ? 2 : 1; }
 
 struct EvictParams {
   PagesView pages;                // base is not used
