@@ -227,6 +227,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
                                                     : ((lane & 7) + ((lane >> 4) << 3)) * S::kPitch + ((lane >> 3) & 1) * 16);
   const int vec = lane % S::kVecs, vec_row = lane / S::kVecs;
   const bool vec_used = vec * 16 < v.head_dim * S::kElem;
+  const int vec_bytes = vec_used ? 16 : 0;  // of vectors that no row has, none are copied and zeros written
   const uint32_t at_lane_copy = vec_row * S::kPitch + vec * 16;
   const uint32_t row_bytes = (uint32_t)v.head_dim * S::kElem;
 
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
       }
       return kNoRow;
     };
-    const uint8_t* lane_k = v.base + h * v.head_bytes + vec * 16;
+    const uint8_t* lane_k = v.base + h * v.head_bytes + (vec_used ? vec * 16 : 0);
     const uint8_t* lane_v = lane_k + v.half_bytes;
     auto issue = [&](int32_t i, uint2 l, uint32_t to) {
       if (i < i1) {
@@ -278,25 +279,16 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
 #pragma unroll
           for (int k = 0; k < S::kLoads; ++k) {
             const uint32_t r = __shfl_sync(~0u, row, k * S::kRowsPerLoad + vec_row);
-            if (vec_used) {
-              copy_async(dst + k * S::kRowsPerLoad * S::kPitch, lane_k + (uint64_t)r * row_bytes);
-              copy_async(dst + k * S::kRowsPerLoad * S::kPitch + S::kHalfBytes, lane_v + (uint64_t)r * row_bytes);
-            }
+            copy_async(dst + k * S::kRowsPerLoad * S::kPitch, lane_k + (uint64_t)r * row_bytes, vec_bytes);
+            copy_async(dst + k * S::kRowsPerLoad * S::kPitch + S::kHalfBytes, lane_v + (uint64_t)r * row_bytes, vec_bytes);
           }
         } else {  // rows that there are not: zeros, as V of no key meets a probability of 0
 #pragma unroll 1
           for (int k = 0; k < S::kLoads; ++k) {
             const uint32_t r = __shfl_sync(~0u, row, k * S::kRowsPerLoad + vec_row);
-            const uint32_t at_row = dst + k * S::kRowsPerLoad * S::kPitch;
-            if (!vec_used) continue;
-            if (r != kNoRow) {
-              copy_async(at_row, lane_k + (uint64_t)r * row_bytes);
-              copy_async(at_row + S::kHalfBytes, lane_v + (uint64_t)r * row_bytes);
-            } else {
-              uint8_t* z = smem + (at_row - smem_at(smem));
-              *reinterpret_cast<uint4*>(z) = make_uint4(0, 0, 0, 0);
-              *reinterpret_cast<uint4*>(z + S::kHalfBytes) = make_uint4(0, 0, 0, 0);
-            }
+            const uint64_t off = r != kNoRow ? (uint64_t)r * row_bytes : 0;
+            copy_async(dst + k * S::kRowsPerLoad * S::kPitch, lane_k + off, r != kNoRow ? vec_bytes : 0);
+            copy_async(dst + k * S::kRowsPerLoad * S::kPitch + S::kHalfBytes, lane_v + off, r != kNoRow ? vec_bytes : 0);
           }
         }
       }
@@ -362,12 +354,6 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
           }
         }
       }
-    }
-    if (row_bytes < S::kRowBytes) {  // columns that no row has are read by the products
-      constexpr int kPerRow = S::kPitch / 16;
-      for (int k = threadIdx.x; k < kWarps * S::kStages * 2 * kStep * kPerRow; k += kAttendThreads)
-        if (k % kPerRow * 16 >= (int)row_bytes)
-          *reinterpret_cast<uint4*>(smem + k / kPerRow * S::kPitch + k % kPerRow * 16) = make_uint4(0, 0, 0, 0);
     }
     __syncthreads();
 #pragma unroll

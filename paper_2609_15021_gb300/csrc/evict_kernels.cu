@@ -30,6 +30,7 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
 // counts' barriers.
 template <int kEach>
 __global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_constant__ EvictParams p) {
+  wait_for_previous();
   const PagesView& v = p.pages;
   constexpr int kTile = kSelectThreads * kEach;
   __shared__ int32_t hist[kBins];
@@ -206,15 +207,12 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s) {
   const PagesView& v = p.pages;
   const dim3 rows(v.heads, v.num_seqs, p.num_layers);
-  if (v.max_length <= 4 * kSelectThreads)
-    select_kernel<4><<<rows, kSelectThreads, 0, s>>>(p);
-  else if (v.max_length <= 12 * kSelectThreads)
-    select_kernel<12><<<rows, kSelectThreads, 0, s>>>(p);
-  else
-    select_kernel<32><<<rows, kSelectThreads, 0, s>>>(p);
+  auto select = v.max_length <= 4 * kSelectThreads    ? select_kernel<4>
+                : v.max_length <= 12 * kSelectThreads ? select_kernel<12>
+                                                      : select_kernel<32>;
+  const cudaError_t e = launch_after(select, rows, kSelectThreads, 0, s, p);
   const int64_t warps = (int64_t)p.num_layers * v.num_seqs * v.heads * p.units;
   const unsigned grid = (unsigned)((warps + kGatherThreads / 32 - 1) / (kGatherThreads / 32));
-  const cudaError_t e = cudaGetLastError();
   return e != cudaSuccess ? e : launch_after(gather_kernel, dim3(grid), kGatherThreads, 0, s, p);
 }
 

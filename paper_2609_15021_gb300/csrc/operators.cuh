@@ -151,8 +151,8 @@ cudaError_t launch_scan(const ScanParams& p, int type, int num_sms, cudaStream_t
 #ifdef __CUDACC__
 namespace {
 
-// A kernel that is launched while the one before it in the stream still runs, and waits for it
-// (wait_for_previous) before it touches memory: only the launch itself overlaps.
+// A kernel that is launched while the one before it in the stream still runs, and waits for its end
+// (wait_for_previous, its first statement) before it touches memory: only the launch itself overlaps.
 template <class P>
 cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t s, const P& p) {
   cudaLaunchAttribute attr;
@@ -167,7 +167,9 @@ cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem,
   c.numAttrs = 1;
   return cudaLaunchKernelEx(&c, kernel, p);
 }
-__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() {
+  asm volatile("griddepcontrol.launch_dependents;\n griddepcontrol.wait;" ::: "memory");
+}
 
 struct Bf16 {
   using T = __nv_bfloat16;

@@ -375,10 +375,8 @@ __global__ void __launch_bounds__(kScanThreads, 2) chunk_kernel(const __grid_con
       for (int i = threadIdx.x; i < kChunk * vecs; i += kScanThreads) {
         const int r = i / vecs, k = i % vecs;
         const uint32_t dst = at + r * pitch + k * 16;
-        if (t0 + r < end)
-          copy_async(dst, src + (t0 + r) * stride + k * 8);
-        else
-          *reinterpret_cast<uint4*>(smem + (dst - base)) = make_uint4(0, 0, 0, 0);
+        const bool there = t0 + r < end;
+        copy_async(dst, src + (there ? t0 + r : t0) * stride + k * 8, there ? 16 : 0);
       }
     };
     rows(b_at, p.b_token, N / 8, to, S::kBPitch);
