@@ -17,7 +17,7 @@ LIB = os.path.join(PKG, "_lib", "libkvxfer.so")
 PROBE_LIB = os.path.join(PKG, "_lib", "libkvxfer_probe.so")
 
 SOURCES = ["pack_kernels.cu", "segment_kernels.cu", "tma_kernels.cu", "kvxfer.cu", "no_alloc.cu", "operators.cu",
-           "attend_kernels.cu", "attend_bf16.cu", "attend_fp16.cu", "attend_e4m3.cu", "evict_kernels.cu", "state_kernels.cu", "tier.cpp",
+           "attend_kernels.cu", "attend_bf16.cu", "attend_fp16.cu", "attend_e4m3.cu", "evict_kernels.cu", "state_kernels.cu", "scan_kernels.cu", "tier.cpp",
            "tier_kernels.cu", "host_alloc.cpp", "host_touch.cpp"]
 PROBE_SOURCES = ["probe.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

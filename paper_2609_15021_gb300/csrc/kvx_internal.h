@@ -146,7 +146,7 @@ cudaError_t launch_move_tma(int dir, int layout, const MoveParams& p, int grid, 
 cudaError_t prepare_tma_kernels();
 // Shared-memory limits of the attention kernels (attend_kernels.cu), likewise.
 cudaError_t prepare_attend_kernels();
-cudaError_t prepare_state_kernels();  // and the scan's (state_kernels.cu)
+cudaError_t prepare_state_kernels();  // and the scan's (scan_kernels.cu)
 // Tensor-map variant for HND pools: one TMA box per full page half.
 constexpr int kTensorMapBytes = 128;
 // Encodes one tensor map per layer of P (kTensorMapBytes each) into `out`;
@@ -190,7 +190,9 @@ void record_cuda_error(int e, const char* call, int line);
 // What the operators' translation unit (operators.cu) uses of a context.
 struct CtxView {
   int device, num_sms;
-  long long* err;  // device error word: lowest bad logical block (or sequence)
+  long long* err;         // device error word: lowest bad logical block (or sequence)
+  int* timeout;           // device flag: a bounded wait inside a kernel ran out
+  long long wait_cycles;  // and its limit
 };
 CtxView view_of(const kvx_ctx* ctx);
 void count_launches(kvx_ctx* ctx, int n);

@@ -781,7 +781,10 @@ void push_job(MoveParams* p, uint8_t* chunk_side, int64_t first_page, int32_t to
 
 int64_t chunk_bytes(const kvx_pool* P, const Geometry& g, int64_t tokens) { return chunk_bytes_of(P, g, tokens); }
 
-CtxView view_of(const kvx_ctx* ctx) { return {ctx->device, ctx->num_sms, ctx->d_err}; }
+CtxView view_of(const kvx_ctx* ctx) {
+  return {ctx->device, ctx->num_sms, ctx->d_err, ctx->d_timeout,
+          ctx->opts.wait_cycles ? ctx->opts.wait_cycles : kDefaultWaitCycles};
+}
 
 void count_launches(kvx_ctx* ctx, int n) {
   std::lock_guard<std::mutex> lock(ctx->mu);

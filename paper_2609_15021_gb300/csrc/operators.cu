@@ -546,6 +546,8 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
     p.state_dim = a->state_dim;
     p.heads_per_group = a->heads / a->groups;
     p.softplus = a->softplus;
+    p.wait_cycles = ctx.wait_cycles;
+    p.timeout = ctx.timeout;
     return KVX_LAUNCHED(c, launch_scan(p, a->type, ctx.num_sms, stream), space.bytes > 0 ? 3 : 1);
   });
 }

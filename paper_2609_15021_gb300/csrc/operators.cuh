@@ -132,6 +132,8 @@ struct ScanParams {
   int32_t segment;           // tokens of a segment in the matrix form; 0: token by token
   float* segment_states;     // [piece][head][head_dim][state_dim], where sequences are cut into segments
   float* segment_exponents;  // [piece][head]
+  long long wait_cycles;     // limit of a wait for the tensor cores
+  int* timeout;              // set when one ran out
 };
 // The segment of the matrix form for a batch, 0 where it is not used; *cut: whether a sequence may have several.
 int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut);
@@ -147,6 +149,7 @@ cudaError_t prepare_attend_e4m3();
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
 cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s);
 cudaError_t launch_scan(const ScanParams& p, int type, int num_sms, cudaStream_t s);
+cudaError_t launch_scan_chunks(const ScanParams& p, int type, cudaStream_t s);
 
 #ifdef __CUDACC__
 namespace {

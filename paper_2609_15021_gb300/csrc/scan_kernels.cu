@@ -1,0 +1,530 @@
+// scan_kernels.cu -- the selective scan of prompts, in matrix form on the tensor cores.
+//
+// With a_t = A d_t and c_t the sum of a up to t within a chunk of 128 tokens,
+//   y_t = sum_{s <= t} (C_t . B_s) e^{c_t - c_s} d_s x_s + e^{c_t} C_t h_in
+//   h_out = e^{c_127} h_in + sum_s e^{c_127 - c_s} d_s x_s B_s^T
+// so a chunk is four products of 128 x 128 matrices:
+//   G = C B^T,  Y2 = C h_in^T,  Y1 = M X with M = G decayed and masked,  S = B^T W with W = x weighted.
+// A CTA has a slice of one head's state (64 or 128 of head_dim) in its threads' registers, as H[state_dim][head_dim] in
+// fp32 laid out as S is in tensor memory, and walks the chunks of a segment.  G, Y1, Y2 and S are all of tensor
+// memory; M takes the place of G as the product's left factor, so it never passes through shared memory.  The products take a quarter of the time that
+// the threads take for the elements between them (an exponential each for G, the splits of W, the rounding of H), so
+// there is one CTA an SM with eight warps, two for every 32 lanes of tensor memory, and the next chunk's
+// rows are fetched as soon as a product has done with the last one's.
+//
+// Rounding: M and the carried state are rounded to the inputs' type for the product that makes y, one rounding
+// a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into two numbers of that
+// type, whose sum is the weighted x to 16 bits or more, and both are multiplied with B.  In fp16 the state and W are
+// scaled by powers of two into its range; M is not.
+//
+// A long sequence is cut into segments, so that every SM has some: a first pass makes each segment's state from
+// nothing (from its last chunk to its first, so that weights need no later decay), a second one carries the states
+// through the segments, and the last one starts every segment with its own.
+
+#include <algorithm>
+
+#include "state_common.cuh"
+#include "tcgen05.cuh"
+
+namespace kvx {
+namespace {
+
+constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;
+
+template <int kP>
+struct ScanShape {
+  static constexpr int kRows = 2 * kPanel;            // B or C: 128 tokens of up to 128 elements
+  static constexpr int kSlice = kP / 64 * kPanel;     // x, its two weighted parts, the rounded state
+  static constexpr int kB = 0, kC = kRows, kX = 2 * kRows, kHi = kX + kSlice, kLo = kHi + kSlice, kH = kLo + kSlice;
+  static constexpr int kSmem = kH + kSlice + 1024;    // and what aligns it to the swizzle's 1024 bytes
+};
+// Columns of tensor memory.
+constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
+
+// What a chunk's tokens weigh.
+struct Weights {
+  float sum[kChunk];     // exponents up to a token
+  float weight[kChunk];  // d times the decay behind it
+  float d[kChunk];
+  float exponent;        // of the whole chunk
+  float shift;           // fp16: the power of two that makes the largest weight less than 1
+};
+
+// The largest value over the CTA.
+__device__ __forceinline__ float cta_max(float v, float* buf) {
+  for (int m = 16; m; m >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, m));
+  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = buf[0];
+  for (int i = 1; i < kWarps; ++i) v = fmaxf(v, buf[i]);
+  return v;
+}
+// A power of two that takes values up to `top` below 2^11.
+__device__ __forceinline__ int range_of(float top) {
+  return top > 0.f && top < INFINITY ? max(-100, min(100, 10 - ilogbf(top))) : 0;
+}
+
+template <class E, int N, int kP, bool kStateOnly>
+__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constant__ ScanParams p) {
+  using S = ScanShape<kP>;
+  using T = typename E::T;
+  constexpr bool kHalf = std::is_same<E, Fp16>::value;
+  constexpr int kCols = kP / 2;  // columns of x, Y and H that a thread has
+  constexpr bool kAdds = kStateOnly && !kHalf;  // S adds up over the chunks in tensor memory
+  wait_for_previous();
+  extern __shared__ __align__(16) uint8_t raw_smem[];
+  __shared__ int32_t buf[kWarps + 3];
+  __shared__ float max_s[2][kWarps];
+  __shared__ Weights weights_s[2];
+  __shared__ __align__(8) uint64_t bars[2];
+  __shared__ uint32_t tmem_s;
+  uint8_t* smem = raw_smem + (-smem_at(raw_smem) & 1023);
+  const StateView& v = p.state;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int line = (warp & 3) * 32 + lane;  // of tensor memory: a token of G and Y, an element of state_dim of H
+  const int side = warp >> 2;               // which half of the columns
+  const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
+  const int32_t h = blockIdx.y, group = h / p.heads_per_group;
+  int32_t s, seg, segs;
+  if (!find_piece<kThreads>(v, piece, p.segment, buf, &s, &seg, &segs)) return;
+  if (kStateOnly && seg + 1 == segs) return;  // the last segment's state is nobody's start
+  int64_t first, last;
+  rows_of(v, s, &first, &last);
+  const int64_t begin = first + (int64_t)seg * p.segment, end = min(last, begin + p.segment);
+  const uint8_t* in = slot_of(v, v.slots_in, s);
+  uint8_t* keep = slot_of(v, v.slots_out, s);
+  if (!in || !keep) {
+    if (!kStateOnly)
+      for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kThreads)
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.out) + (begin + i / (kP / 2)) * p.out_token + h * p.out_head + p0 +
+                                     i % (kP / 2) * 2) = 0;
+    return;
+  }
+  const T* b_at = reinterpret_cast<const T*>(p.b) + group * p.b_group;
+  const T* c_at = reinterpret_cast<const T*>(p.c) + group * p.c_group;
+  const T* x_at = reinterpret_cast<const T*>(p.x) + h * p.x_head + p0;
+  const T* dt_at = reinterpret_cast<const T*>(p.dt) + h;
+  const uint32_t base = smem_at(smem), bar0 = smem_at(&bars[0]), bar1 = smem_at(&bars[1]);
+
+  // Rows of a chunk, swizzled; those behind the last are zeros.
+  auto fetch = [&](const T* src, int64_t stride, int64_t t0, uint32_t to, int vecs) {
+    for (int i = threadIdx.x; i < kChunk * vecs; i += kThreads) {
+      const int r = i / vecs, c = i % vecs;
+      const bool there = t0 + r < end;
+      copy_async(base + to + panel_at(r, c), src + (there ? t0 + r : begin) * stride + c * 8, there ? 16 : 0);
+    }
+  };
+  // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
+  // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
+  const float A2 = p.A[h] * kLog2e, D = p.D ? p.D[h] : 0.f;
+  auto weigh = [&](int64_t t0, float after, Weights* w) {
+    float d[4], a[4], upto = 0.f, behind = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t t = t0 + 4 * lane + k;
+      d[k] = t < end ? step_of(p, E::up(dt_at[t * p.dt_token]), h) : 0.f;
+      a[k] = d[k] * A2;
+    }
+    upto = behind = (a[0] + a[1]) + (a[2] + a[3]);
+    for (int m = 1; m < 32; m <<= 1) {
+      const float y = __shfl_up_sync(~0u, upto, m), z = __shfl_down_sync(~0u, behind, m);
+      if (lane >= m) upto += y;
+      if (lane + m < 32) behind += z;
+    }
+    float below = __shfl_up_sync(~0u, upto, 1), above = __shfl_down_sync(~0u, behind, 1);
+    if (lane == 0) below = 0.f;
+    if (lane == 31) above = 0.f, w->exponent = upto;
+    above += after;
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      w->d[4 * lane + k] = d[k];
+      w->sum[4 * lane + k] = below += a[k];
+    }
+#pragma unroll
+    for (int k = 3; k >= 0; --k) {
+      const float weight = d[k] * ex2(above);
+      w->weight[4 * lane + k] = weight;
+      above += a[k];
+      top = fmaxf(top, fabsf(weight));
+    }
+    if (kHalf) {
+      for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
+      if (lane == 0) w->shift = top > 0.f && top < INFINITY ? ldexpf(1.f, max(-100, min(100, -1 - ilogbf(top)))) : 1.f;
+    }
+  };
+
+  // ---- set-up: barriers, tensor memory, the first chunk's rows and weights
+  const int64_t chunks = (end - begin + kChunk - 1) / kChunk;
+  const int64_t step = kStateOnly ? -kChunk : kChunk;
+  int64_t t0 = kStateOnly ? begin + (chunks - 1) * kChunk : begin;
+  if (chunks > 0) {
+    fetch(b_at, p.b_token, t0, S::kB, N / 8);
+    fetch(x_at, p.x_token, t0, S::kX, kP / 8);
+    if (!kStateOnly) fetch(c_at, p.c_token, t0, S::kC, N / 8);
+  }
+  commit_async();
+  if (threadIdx.x == 0) {
+    bar_init(bar0);
+    bar_init(bar1);
+    fence_operands();
+  }
+  if (warp == 0) tmem_alloc(smem_at(&tmem_s), kColumns);
+  if (warp == 1 && chunks > 0) weigh(t0, 0.f, &weights_s[0]);
+  if (N == 64)  // H's lanes beyond state_dim: their rows of B^T are zeros
+    for (int i = threadIdx.x; i < kPanel / 16; i += kThreads)
+      *reinterpret_cast<uint4*>(smem + S::kB + kPanel + i * 16) = make_uint4(0, 0, 0, 0);
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  const uint32_t tmem = tmem_s, my_lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  bool dead = false;  // a wait ran out
+
+  // The state a segment starts from, and the one after every chunk, rounded to shared memory as Y2's right factor.
+  float state_scale = 1.f;  // fp16: what undoes the rounded state's scaling
+  auto round_state = [&](const float (&state)[kCols]) {
+    float scale = 1.f;
+    if constexpr (kHalf) {
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) top = fmaxf(top, fabsf(state[k]));
+      const int e = range_of(cta_max(top, max_s[0]));
+      scale = ldexpf(1.f, e), state_scale = ldexpf(1.f, -e);
+    }
+    if (line < N) {
+#pragma unroll
+      for (int k = 0; k < kCols; k += 8)
+        *reinterpret_cast<uint4*>(smem + S::kH + panel_at(line, (side * kCols + k) / 8)) =
+            make_uint4(pack2<E>(state[k] * scale, state[k + 1] * scale), pack2<E>(state[k + 2] * scale, state[k + 3] * scale),
+                       pack2<E>(state[k + 4] * scale, state[k + 5] * scale), pack2<E>(state[k + 6] * scale, state[k + 7] * scale));
+    }
+    fence_operands();
+  };
+  const int64_t all = (int64_t)p.heads * p.head_dim * N;
+  const int64_t state_at = ((int64_t)h * p.head_dim + p0 + side * kCols) * N + line;  // + column * N
+  float state[kCols];
+#pragma unroll
+  for (int k = 0; k < kCols; ++k) state[k] = 0.f;
+  if (!kStateOnly) {
+    const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
+    if (line < N && (p.segment_states || !(v.fresh && v.fresh[s]))) {
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
+    }
+    if (chunks > 0) round_state(state);
+  }
+
+  float exponent = 0.f;  // of the decay over the segment's chunks so far
+  for (int64_t n = 0; n < chunks; ++n, t0 += step) {
+    const Weights& w = weights_s[n & 1];
+    const uint32_t parity = n & 1;
+    wait_async<0>();
+    fence_operands();
+    tmem_before_sync();
+    if (__syncthreads_or(dead)) break;  // the chunk's rows, its weights and the rounded state are there
+    tmem_after_sync();
+    if (!kStateOnly && threadIdx.x == 0) {
+#pragma unroll
+      for (int k = 0; k < N / 16; ++k)
+        matrix_product(tmem + kG, operand_k(base + S::kC, k), operand_k(base + S::kB, k), instruction<E>(false, false, 128), k > 0);
+#pragma unroll
+      for (int k = 0; k < N / 16; ++k)
+        matrix_product(tmem + kY2, operand_k(base + S::kC, k), operand_rows(base + S::kH, k), instruction<E>(false, true, kP), k > 0);
+      products_done(bar0);
+    }
+    exponent += w.exponent;
+    if (warp == kWarps - 1 && n + 1 < chunks) weigh(t0 + step, kStateOnly ? exponent : 0.f, &weights_s[(n + 1) & 1]);
+
+    // x weighted, in two parts, vector by vector where it lies
+    bool odd = false;
+    float back = 1.f;  // fp16: what undoes the scaling of W
+    {
+      constexpr int kVecs = kChunk * kP / 8 / kThreads;
+      float scale = 1.f;
+      if constexpr (kHalf) {
+        float top = 0.f;
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+          const uint4 x = *reinterpret_cast<const uint4*>(smem + S::kX + (k * kThreads + threadIdx.x) * 16);
+          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = unpack2<E>(u[j]);
+            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        }
+        const int e = range_of(cta_max(top, max_s[1]));
+        scale = w.shift * ldexpf(1.f, e), back = ldexpf(1.f, -e) / w.shift;
+      }
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int i = k * kThreads + threadIdx.x, row = i / 8 % kChunk;
+        const uint4 x = *reinterpret_cast<const uint4*>(smem + S::kX + i * 16);
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+        const float weight = w.weight[row] * scale;
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float2 f = unpack2<E>(u[j]);
+          odd |= odd2<E>(u[j]);
+          f.x *= weight, f.y *= weight;
+          hi[j] = pack2<E>(f.x, f.y);
+          const float2 r = unpack2<E>(hi[j]);
+          lo[j] = odd2<E>(hi[j]) ? 0 : pack2<E>(f.x - r.x, f.y - r.y);
+        }
+        *reinterpret_cast<uint4*>(smem + S::kHi + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(smem + S::kLo + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      }
+    }
+    fence_operands();
+
+    const int64_t token = t0 + line;
+    float y[kCols];
+    if constexpr (!kStateOnly) {
+      // G decayed and masked, in 16 columns of every 32 a side: read by all before M takes its place
+      dead |= !bar_wait(bar0, parity, p.wait_cycles);
+      tmem_after_sync();
+      float g[4][16];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) tmem_load16(g[q], my_lanes + kG + q * 32 + side * 16);
+      tmem_wait_loads();
+      tmem_before_sync();
+      odd = __syncthreads_or(odd);
+      tmem_after_sync();
+      if (n + 1 < chunks) fetch(c_at, p.c_token, t0 + step, S::kC, N / 8);
+      const float sum_t = w.sum[line];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c0 = q * 32 + side * 16;
+        uint32_t m[8];
+        if (c0 <= (warp & 3) * 32 + 31) {  // some of the warp's tokens see some of these
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int u = c0 + 2 * j;
+            const float2 su = *reinterpret_cast<const float2*>(&w.sum[u]), du = *reinterpret_cast<const float2*>(&w.d[u]);
+            const float a = u <= line ? g[q][2 * j] * (ex2(sum_t - su.x) * du.x) : 0.f;
+            const float b = u + 1 <= line ? g[q][2 * j + 1] * (ex2(sum_t - su.y) * du.y) : 0.f;
+            m[j] = pack2<E>(a, b);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) m[j] = 0;
+        }
+        tmem_store8(my_lanes + kG + c0 / 2, m);
+      }
+      tmem_wait_stores();
+      // Y2 decayed, and the tokens' own x
+      const float by = ex2(sum_t) * state_scale;
+#pragma unroll
+      for (int k = 0; k < kCols; k += 16) {
+        float r[16];
+        tmem_load16(r, my_lanes + kY2 + side * kCols + k);
+        tmem_wait_loads();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[k + j] = r[j] * by;
+      }
+      if (p.D) {
+#pragma unroll
+        for (int k = 0; k < kCols; k += 8) {
+          const uint4 x = *reinterpret_cast<const uint4*>(smem + S::kX + panel_at(line, (side * kCols + k) / 8));
+          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 f = unpack2<E>(u[j]);
+            y[k + 2 * j] += D * f.x, y[k + 2 * j + 1] += D * f.y;
+          }
+        }
+      }
+      if (odd) {  // a token's x that is not finite must not reach the tokens before it (0 x inf): added below
+        __syncthreads();
+        for (int i = threadIdx.x; i < S::kSlice / 4; i += kThreads) {
+          uint32_t* at = reinterpret_cast<uint32_t*>(smem + S::kX) + i;
+          if (odd2<E>(*at & 0xFFFFu)) *at &= 0xFFFF0000u;
+          if (odd2<E>(*at & 0xFFFF0000u)) *at &= 0xFFFFu;
+        }
+        fence_operands();
+      }
+    }
+    tmem_before_sync();
+    __syncthreads();  // M, W, and x as the product takes it
+    tmem_after_sync();
+    if (threadIdx.x == 0) {
+      if (!kStateOnly) {
+#pragma unroll
+        for (int k = 0; k < kChunk / 16; ++k)
+          matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + S::kX, k), instruction<E>(false, true, kP), k > 0);
+      }
+#pragma unroll
+      for (int k = 0; k < kChunk / 16; ++k) {
+        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kLo, k),
+                       instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
+        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kHi, k),
+                       instruction<E>(true, true, kP), true);
+      }
+      products_done(bar1);
+    }
+    dead |= !bar_wait(bar1, parity, p.wait_cycles);
+    tmem_after_sync();
+    if (n + 1 < chunks) {
+      fetch(b_at, p.b_token, t0 + step, S::kB, N / 8);
+      fetch(x_at, p.x_token, t0 + step, S::kX, kP / 8);
+    }
+    commit_async();
+    if constexpr (!kStateOnly) {
+#pragma unroll
+      for (int k = 0; k < kCols; k += 16) {
+        float r[16];
+        tmem_load16(r, my_lanes + kY1 + side * kCols + k);
+        tmem_wait_loads();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[k + j] += r[j];
+      }
+      if (odd) {
+        for (int u = 0; u < kChunk && t0 + u < end; ++u) {
+          uint32_t m;
+          tmem_load1(m, my_lanes + kG + u / 2);
+          tmem_wait_loads();
+          const float2 mu = unpack2<E>(m);
+          const T* xu = x_at + (t0 + u) * p.x_token + side * kCols;
+#pragma unroll
+          for (int k = 0; k < kCols; ++k) {
+            const float x = E::up(xu[k]);
+            if (u <= line && !isfinite(x)) y[k] += (u & 1 ? mu.y : mu.x) * x;
+          }
+        }
+      }
+      if (token < end) {
+        T* to = reinterpret_cast<T*>(p.out) + token * p.out_token + h * p.out_head + p0 + side * kCols;
+#pragma unroll
+        for (int k = 0; k < kCols; k += 8)
+          *reinterpret_cast<uint4*>(to + k) = make_uint4(pack2<E>(y[k], y[k + 1]), pack2<E>(y[k + 2], y[k + 3]),
+                                                         pack2<E>(y[k + 4], y[k + 5]), pack2<E>(y[k + 6], y[k + 7]));
+      }
+    }
+    // The state after the chunk.
+    if (!kAdds || n + 1 == chunks) {
+      const float decay = kStateOnly ? 1.f : ex2(w.exponent);
+#pragma unroll
+      for (int k = 0; k < kCols; k += 16) {
+        float r[16];
+        tmem_load16(r, my_lanes + kState + side * kCols + k);
+        tmem_wait_loads();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) state[k + j] = state[k + j] * decay + r[j] * back;
+      }
+      if (!kStateOnly && n + 1 < chunks) round_state(state);
+    }
+  }
+  if (kStateOnly || seg + 1 == segs) {
+    float* to = kStateOnly ? p.segment_states + piece * all : reinterpret_cast<float*>(keep);
+    if (line < N) {
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) to[state_at + k * N] = state[k];
+    }
+    if (kStateOnly && p0 == 0 && threadIdx.x == 0) p.segment_exponents[(int64_t)piece * p.heads + h] = exponent;
+  }
+  if (dead) *p.timeout = 1;
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  if (warp == 0) tmem_free(tmem, kColumns);
+}
+
+// Carries the states through a sequence's segments, four elements a thread: where the first pass left what a
+// segment makes, the state it starts from takes its place.
+__global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ ScanParams p) {
+  wait_for_previous();
+  __shared__ int32_t first_s;
+  const StateView& v = p.state;
+  const int32_t s = blockIdx.z, h = blockIdx.y;
+  if (threadIdx.x == 0) first_s = 0;
+  __syncthreads();
+  int32_t mine = 0;  // pieces of the sequences before
+  for (int32_t i = threadIdx.x; i < s; i += 256) {
+    int64_t a, b;
+    rows_of(v, i, &a, &b);
+    mine += max(1, (int32_t)((b - a + p.segment - 1) / p.segment));
+  }
+  for (int m = 16; m; m >>= 1) mine += __shfl_xor_sync(~0u, mine, m);
+  if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&first_s, mine);
+  __syncthreads();
+  const uint8_t* in = slot_of(v, v.slots_in, s);
+  if (!in || !slot_of(v, v.slots_out, s)) return;
+  int64_t a, b;
+  rows_of(v, s, &a, &b);
+  const int32_t segs = max(1, (int32_t)((b - a + p.segment - 1) / p.segment));
+  const int32_t i = blockIdx.x * 256 + threadIdx.x, vecs = p.head_dim * p.state_dim / 4;
+  if (i >= vecs) return;
+  float4 state = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (!(v.fresh && v.fresh[s])) state = reinterpret_cast<const float4*>(in)[(int64_t)h * vecs + i];
+  for (int32_t g = 0; g < segs; ++g) {
+    const int64_t piece = first_s + g;
+    float4* at = reinterpret_cast<float4*>(p.segment_states) + (piece * p.heads + h) * vecs + i;
+    const float4 made = g + 1 < segs ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
+    *at = state;
+    if (g + 1 < segs) {
+      const float decay = ex2(p.segment_exponents[piece * p.heads + h]);
+      state.x = state.x * decay + made.x, state.y = state.y * decay + made.y;
+      state.z = state.z * decay + made.z, state.w = state.w * decay + made.w;
+    }
+  }
+}
+
+
+template <class E, int N, int kP>
+cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
+  const int64_t pieces = p.state.tokens / p.segment + p.state.num_seqs;
+  const dim3 grid((unsigned)(pieces * (p.head_dim / kP)), p.heads);
+  constexpr int kSmem = ScanShape<kP>::kSmem;
+  if (p.segment_states) {
+    cudaError_t e = launch_after(chunk_kernel<E, N, kP, true>, grid, kThreads, kSmem, s, p);
+    if (e != cudaSuccess) return e;
+    const dim3 all((p.head_dim * N / 4 + 255) / 256, p.heads, p.state.num_seqs);
+    if ((e = launch_after(carry_kernel, all, 256, 0, s, p)) != cudaSuccess) return e;
+  }
+  return launch_after(chunk_kernel<E, N, kP, false>, grid, kThreads, kSmem, s, p);
+}
+
+template <class E>
+cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
+  if (p.head_dim % 128 == 0) return p.state_dim == 64 ? chunks<E, 64, 128>(p, s) : chunks<E, 128, 128>(p, s);
+  return p.state_dim == 64 ? chunks<E, 64, 64>(p, s) : chunks<E, 128, 64>(p, s);
+}
+
+template <class E, int N, int kP>
+cudaError_t prepare() {
+  const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<E, N, kP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             ScanShape<kP>::kSmem);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(chunk_kernel<E, N, kP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, ScanShape<kP>::kSmem);
+}
+template <class E>
+cudaError_t prepare() {
+  cudaError_t e;
+  if ((e = prepare<E, 64, 64>()) != cudaSuccess || (e = prepare<E, 64, 128>()) != cudaSuccess) return e;
+  if ((e = prepare<E, 128, 64>()) != cudaSuccess) return e;
+  return prepare<E, 128, 128>();
+}
+
+}  // namespace
+
+int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut) {
+  *cut = false;
+  if (!v.starts || head_dim % 64 || (state_dim != 64 && state_dim != 128)) return 0;
+  if (v.tokens < 16ll * v.num_seqs) return 0;  // mostly short ones: a chunk would be mostly empty
+  const int64_t all = (v.tokens + kChunk - 1) / kChunk * heads * (head_dim / (head_dim % 128 ? 64 : 128));
+  const int64_t each = std::max<int64_t>(1, (all + num_sms - 1) / num_sms);
+  *cut = v.tokens > each * kChunk;
+  return (int32_t)(each * kChunk);
+}
+
+cudaError_t launch_scan_chunks(const ScanParams& p, int type, cudaStream_t s) {
+  return type == KVX_TYPE_BF16 ? chunks<Bf16>(p, s) : chunks<Fp16>(p, s);
+}
+
+cudaError_t prepare_state_kernels() {
+  const cudaError_t e = prepare<Bf16>();
+  return e == cudaSuccess ? prepare<Fp16>() : e;
+}
+
+}  // namespace kvx
