@@ -80,6 +80,12 @@ __device__ __forceinline__ float2 unpack2(uint32_t v) {
   else
     return __half22float2(*reinterpret_cast<const __half2*>(&v));
 }
+// Whether one of some pairs of numbers is not finite: their carries or-ed together, then tested.
+template <class C>
+__device__ __forceinline__ uint32_t odd_carry(uint32_t v) {
+  return (v & 0x7FFF7FFFu) + (std::is_same<C, Bf16>::value ? 0x00800080u : 0x04000400u);
+}
+__device__ __forceinline__ bool odd_carried(uint32_t carries) { return carries & 0x80008000u; }
 // Whether one of two numbers is not finite.
 template <class C>
 __device__ __forceinline__ bool odd2(uint32_t v) {

@@ -9,8 +9,9 @@
 // fp32 laid out as S is in tensor memory, and walks the chunks of a segment.  G, Y1, Y2 and S are all of tensor
 // memory; M takes the place of G as the product's left factor, so it never passes through shared memory.  The products take a quarter of the time that
 // the threads take for the elements between them (an exponential each for G, the splits of W, the rounding of H), so
-// there is one CTA an SM with eight warps, two for every 32 lanes of tensor memory, and the next chunk's
-// rows are fetched as soon as a product has done with the last one's.
+// there is one CTA an SM with eight warps, two for every 32 lanes of tensor memory; S is made while the threads
+// are at M and read while Y1 is made, and the next chunk's rows are fetched as soon as a product has done
+// with the last one's.
 //
 // Rounding: M and the carried state are rounded to the inputs' type for the product that makes y, one rounding
 // a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into two numbers of that
@@ -76,7 +77,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   __shared__ int32_t buf[kWarps + 3];
   __shared__ float max_s[2][kWarps];
   __shared__ Weights weights_s[2];
-  __shared__ __align__(8) uint64_t bars[2];
+  __shared__ __align__(8) uint64_t bars[3];
   __shared__ uint32_t tmem_s;
   uint8_t* smem = raw_smem + (-smem_at(raw_smem) & 1023);
   const StateView& v = p.state;
@@ -104,16 +105,24 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const T* c_at = reinterpret_cast<const T*>(p.c) + group * p.c_group;
   const T* x_at = reinterpret_cast<const T*>(p.x) + h * p.x_head + p0;
   const T* dt_at = reinterpret_cast<const T*>(p.dt) + h;
-  const uint32_t base = smem_at(smem), bar0 = smem_at(&bars[0]), bar1 = smem_at(&bars[1]);
+  const uint32_t base = smem_at(smem), bar_g = smem_at(&bars[0]), bar_y = smem_at(&bars[1]), bar_s = smem_at(&bars[2]);
 
-  // Rows of a chunk, swizzled; those behind the last are zeros.
-  auto fetch = [&](const T* src, int64_t stride, int64_t t0, uint32_t to, int vecs) {
-    for (int i = threadIdx.x; i < kChunk * vecs; i += kThreads) {
-      const int r = i / vecs, c = i % vecs;
-      const bool there = t0 + r < end;
-      copy_async(base + to + panel_at(r, c), src + (there ? t0 + r : begin) * stride + c * 8, there ? 16 : 0);
+  // Rows of a chunk, swizzled; those behind the last are zeros.  A thread has one column of vectors of rows that are a
+  // multiple of 8 apart, so its place within a row stays.
+  auto fetch = [&](const T* src, int64_t stride, int64_t t0, uint32_t to, auto vecs) {
+    constexpr int kVecs = decltype(vecs)::value, kApart = kThreads / kVecs;
+    const int r0 = threadIdx.x / kVecs, c = threadIdx.x % kVecs;
+    const int left = (int)min((int64_t)kChunk, end - t0) - r0;
+    const T* from = src + (t0 + r0) * stride + c * 8;
+    const uint32_t dst = base + to + panel_at(r0, c);
+#pragma unroll
+    for (int k = 0; k < kChunk / kApart; ++k, from += kApart * stride) {
+      const bool there = k * kApart < left;
+      copy_async(dst + k * kApart * 128, there ? from : src + begin * stride, there ? 16 : 0);
     }
   };
+  const std::integral_constant<int, N / 8> state_vecs;
+  const std::integral_constant<int, kP / 8> slice_vecs;
   // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
   // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
   const float A2 = p.A[h] * kLog2e, D = p.D ? p.D[h] : 0.f;
@@ -159,14 +168,27 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int64_t step = kStateOnly ? -kChunk : kChunk;
   int64_t t0 = kStateOnly ? begin + (chunks - 1) * kChunk : begin;
   if (chunks > 0) {
-    fetch(b_at, p.b_token, t0, S::kB, N / 8);
-    fetch(x_at, p.x_token, t0, S::kX, kP / 8);
-    if (!kStateOnly) fetch(c_at, p.c_token, t0, S::kC, N / 8);
+    fetch(b_at, p.b_token, t0, S::kB, state_vecs);
+    fetch(x_at, p.x_token, t0, S::kX, slice_vecs);
+    if (!kStateOnly) fetch(c_at, p.c_token, t0, S::kC, state_vecs);
   }
   commit_async();
+  const int64_t all = (int64_t)p.heads * p.head_dim * N;
+  const int64_t state_at = ((int64_t)h * p.head_dim + p0 + side * kCols) * N + line;  // + column * N
+  float state[kCols];
+#pragma unroll
+  for (int k = 0; k < kCols; ++k) state[k] = 0.f;
+  if (!kStateOnly) {
+    const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
+    if (line < N && (p.segment_states || !(v.fresh && v.fresh[s]))) {
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
+    }
+  }
   if (threadIdx.x == 0) {
-    bar_init(bar0);
-    bar_init(bar1);
+    bar_init(bar_g);
+    bar_init(bar_y);
+    bar_init(bar_s);
     fence_operands();
   }
   if (warp == 0) tmem_alloc(smem_at(&tmem_s), kColumns);
@@ -200,19 +222,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
     fence_operands();
   };
-  const int64_t all = (int64_t)p.heads * p.head_dim * N;
-  const int64_t state_at = ((int64_t)h * p.head_dim + p0 + side * kCols) * N + line;  // + column * N
-  float state[kCols];
-#pragma unroll
-  for (int k = 0; k < kCols; ++k) state[k] = 0.f;
-  if (!kStateOnly) {
-    const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
-    if (line < N && (p.segment_states || !(v.fresh && v.fresh[s]))) {
-#pragma unroll
-      for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
-    }
-    if (chunks > 0) round_state(state);
-  }
+  if (!kStateOnly && chunks > 0) round_state(state);
 
   float exponent = 0.f;  // of the decay over the segment's chunks so far
   for (int64_t n = 0; n < chunks; ++n, t0 += step) {
@@ -230,47 +240,55 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 #pragma unroll
       for (int k = 0; k < N / 16; ++k)
         matrix_product(tmem + kY2, operand_k(base + S::kC, k), operand_rows(base + S::kH, k), instruction<E>(false, true, kP), k > 0);
-      products_done(bar0);
+      products_done(bar_g);
     }
     exponent += w.exponent;
     if (warp == kWarps - 1 && n + 1 < chunks) weigh(t0 + step, kStateOnly ? exponent : 0.f, &weights_s[(n + 1) & 1]);
 
     // x weighted, in two parts, vector by vector where it lies
-    bool odd = false;
+    bool odd;
     float back = 1.f;  // fp16: what undoes the scaling of W
     {
       constexpr int kVecs = kChunk * kP / 8 / kThreads;
-      float scale = 1.f;
-      if constexpr (kHalf) {
-        float top = 0.f;
+      uint4 x[kVecs];
+      uint32_t carries = 0;
+      float scale = 1.f, top = 0.f;
 #pragma unroll
-        for (int k = 0; k < kVecs; ++k) {
-          const uint4 x = *reinterpret_cast<const uint4*>(smem + S::kX + (k * kThreads + threadIdx.x) * 16);
-          const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+      for (int k = 0; k < kVecs; ++k) {
+        x[k] = *reinterpret_cast<const uint4*>(smem + S::kX + (k * kThreads + threadIdx.x) * 16);
+        carries |= odd_carry<E>(x[k].x) | odd_carry<E>(x[k].y) | odd_carry<E>(x[k].z) | odd_carry<E>(x[k].w);
+        if constexpr (kHalf) {
+          const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 f = unpack2<E>(u[j]);
-            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+            const float2 f = unpack2<E>(u[j] & 0x7FFF7FFFu);
+            top = fmaxf(top, fmaxf(f.x, f.y));
           }
         }
+      }
+      odd = odd_carried(carries);
+      if constexpr (kHalf) {
         const int e = range_of(cta_max(top, max_s[1]));
         scale = w.shift * ldexpf(1.f, e), back = ldexpf(1.f, -e) / w.shift;
       }
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
         const int i = k * kThreads + threadIdx.x, row = i / 8 % kChunk;
-        const uint4 x = *reinterpret_cast<const uint4*>(smem + S::kX + i * 16);
-        const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+        const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
         const float weight = w.weight[row] * scale;
         uint32_t hi[4], lo[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float2 f = unpack2<E>(u[j]);
-          odd |= odd2<E>(u[j]);
           f.x *= weight, f.y *= weight;
           hi[j] = pack2<E>(f.x, f.y);
           const float2 r = unpack2<E>(hi[j]);
-          lo[j] = odd2<E>(hi[j]) ? 0 : pack2<E>(f.x - r.x, f.y - r.y);
+          lo[j] = pack2<E>(f.x - r.x, f.y - r.y);
+        }
+        if (odd) {  // inf - inf: an infinite x has no second part
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            lo[j] &= (odd2<E>(hi[j] & 0xFFFFu) ? 0 : 0xFFFFu) | (odd2<E>(hi[j] & 0xFFFF0000u) ? 0 : 0xFFFF0000u);
         }
         *reinterpret_cast<uint4*>(smem + S::kHi + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(smem + S::kLo + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -280,18 +298,30 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 
     const int64_t token = t0 + line;
     float y[kCols];
+    // G's columns, 16 of every 32 a side: read by all before M takes their place
+    float g[4][16];
     if constexpr (!kStateOnly) {
-      // G decayed and masked, in 16 columns of every 32 a side: read by all before M takes its place
-      dead |= !bar_wait(bar0, parity, p.wait_cycles);
+      dead |= !bar_wait(bar_g, parity, p.wait_cycles);
       tmem_after_sync();
-      float g[4][16];
 #pragma unroll
       for (int q = 0; q < 4; ++q) tmem_load16(g[q], my_lanes + kG + q * 32 + side * 16);
       tmem_wait_loads();
       tmem_before_sync();
-      odd = __syncthreads_or(odd);
-      tmem_after_sync();
-      if (n + 1 < chunks) fetch(c_at, p.c_token, t0 + step, S::kC, N / 8);
+    }
+    odd = __syncthreads_or(odd);  // W is there, and G read
+    tmem_after_sync();
+    if (threadIdx.x == 0) {
+#pragma unroll
+      for (int k = 0; k < kChunk / 16; ++k) {
+        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kLo, k),
+                       instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
+        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kHi, k),
+                       instruction<E>(true, true, kP), true);
+      }
+      products_done(bar_s);
+    }
+    if constexpr (!kStateOnly) {
+      if (n + 1 < chunks) fetch(c_at, p.c_token, t0 + step, S::kC, state_vecs);
       const float sum_t = w.sum[line];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -313,6 +343,23 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
         tmem_store8(my_lanes + kG + c0 / 2, m);
       }
       tmem_wait_stores();
+      if (odd) {  // a token's x that is not finite must not reach the tokens before it (0 x inf): added below
+        for (int i = threadIdx.x; i < S::kSlice / 4; i += kThreads) {
+          uint32_t* at = reinterpret_cast<uint32_t*>(smem + S::kX) + i;
+          if (odd2<E>(*at & 0xFFFFu)) *at &= 0xFFFF0000u;
+          if (odd2<E>(*at & 0xFFFF0000u)) *at &= 0xFFFFu;
+        }
+        fence_operands();
+      }
+      tmem_before_sync();
+      __syncthreads();  // M, and x as the product takes it
+      tmem_after_sync();
+      if (threadIdx.x == 0) {
+#pragma unroll
+        for (int k = 0; k < kChunk / 16; ++k)
+          matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + S::kX, k), instruction<E>(false, true, kP), k > 0);
+        products_done(bar_y);
+      }
       // Y2 decayed, and the tokens' own x
       const float by = ex2(sum_t) * state_scale;
 #pragma unroll
@@ -335,41 +382,28 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
           }
         }
       }
-      if (odd) {  // a token's x that is not finite must not reach the tokens before it (0 x inf): added below
-        __syncthreads();
-        for (int i = threadIdx.x; i < S::kSlice / 4; i += kThreads) {
-          uint32_t* at = reinterpret_cast<uint32_t*>(smem + S::kX) + i;
-          if (odd2<E>(*at & 0xFFFFu)) *at &= 0xFFFF0000u;
-          if (odd2<E>(*at & 0xFFFF0000u)) *at &= 0xFFFFu;
-        }
-        fence_operands();
-      }
     }
-    tmem_before_sync();
-    __syncthreads();  // M, W, and x as the product takes it
+    // The state after the chunk.
+    dead |= !bar_wait(bar_s, parity, p.wait_cycles);
     tmem_after_sync();
-    if (threadIdx.x == 0) {
-      if (!kStateOnly) {
+    if (n + 1 < chunks) fetch(b_at, p.b_token, t0 + step, S::kB, state_vecs);
+    if (!kAdds || n + 1 == chunks) {
+      const float decay = kStateOnly ? 1.f : ex2(w.exponent);
 #pragma unroll
-        for (int k = 0; k < kChunk / 16; ++k)
-          matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + S::kX, k), instruction<E>(false, true, kP), k > 0);
-      }
+      for (int k = 0; k < kCols; k += 16) {
+        float r[16];
+        tmem_load16(r, my_lanes + kState + side * kCols + k);
+        tmem_wait_loads();
 #pragma unroll
-      for (int k = 0; k < kChunk / 16; ++k) {
-        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kLo, k),
-                       instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
-        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kHi, k),
-                       instruction<E>(true, true, kP), true);
+        for (int j = 0; j < 16; ++j) state[k + j] = state[k + j] * decay + r[j] * back;
       }
-      products_done(bar1);
+      if (!kStateOnly && n + 1 < chunks) round_state(state);
     }
-    dead |= !bar_wait(bar1, parity, p.wait_cycles);
-    tmem_after_sync();
-    if (n + 1 < chunks) {
-      fetch(b_at, p.b_token, t0 + step, S::kB, N / 8);
-      fetch(x_at, p.x_token, t0 + step, S::kX, kP / 8);
+    if constexpr (!kStateOnly) {
+      dead |= !bar_wait(bar_y, parity, p.wait_cycles);
+      tmem_after_sync();
     }
-    commit_async();
+    if (n + 1 < chunks && (kStateOnly || !p.D)) fetch(x_at, p.x_token, t0 + step, S::kX, slice_vecs);
     if constexpr (!kStateOnly) {
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
@@ -390,30 +424,26 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
           for (int k = 0; k < kCols; ++k) {
             const float x = E::up(xu[k]);
             if (u <= line && !isfinite(x)) y[k] += (u & 1 ? mu.y : mu.x) * x;
+            if (p.D && u == line && !isfinite(x)) y[k] += D * x;
           }
         }
       }
-      if (token < end) {
-        T* to = reinterpret_cast<T*>(p.out) + token * p.out_token + h * p.out_head + p0 + side * kCols;
+      // y through W's place, so that whole rows are written
 #pragma unroll
-        for (int k = 0; k < kCols; k += 8)
-          *reinterpret_cast<uint4*>(to + k) = make_uint4(pack2<E>(y[k], y[k + 1]), pack2<E>(y[k + 2], y[k + 3]),
-                                                         pack2<E>(y[k + 4], y[k + 5]), pack2<E>(y[k + 6], y[k + 7]));
-      }
+      for (int k = 0; k < kCols; k += 8)
+        *reinterpret_cast<uint4*>(smem + S::kHi + panel_at(line, (side * kCols + k) / 8)) =
+            make_uint4(pack2<E>(y[k], y[k + 1]), pack2<E>(y[k + 2], y[k + 3]), pack2<E>(y[k + 4], y[k + 5]), pack2<E>(y[k + 6], y[k + 7]));
+      __syncthreads();
+      if (n + 1 < chunks && p.D) fetch(x_at, p.x_token, t0 + step, S::kX, slice_vecs);
+      constexpr int kVecs = kP / 8, kApart = kThreads / kVecs;
+      const int r0 = threadIdx.x / kVecs, c = threadIdx.x % kVecs;
+      T* to = reinterpret_cast<T*>(p.out) + (t0 + r0) * p.out_token + h * p.out_head + p0 + c * 8;
+#pragma unroll
+      for (int k = 0; k < kChunk / kApart; ++k, to += kApart * p.out_token)
+        if (t0 + r0 + k * kApart < end)
+          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(smem + S::kHi + panel_at(r0, c) + k * kApart * 128);
     }
-    // The state after the chunk.
-    if (!kAdds || n + 1 == chunks) {
-      const float decay = kStateOnly ? 1.f : ex2(w.exponent);
-#pragma unroll
-      for (int k = 0; k < kCols; k += 16) {
-        float r[16];
-        tmem_load16(r, my_lanes + kState + side * kCols + k);
-        tmem_wait_loads();
-#pragma unroll
-        for (int j = 0; j < 16; ++j) state[k + j] = state[k + j] * decay + r[j] * back;
-      }
-      if (!kStateOnly && n + 1 < chunks) round_state(state);
-    }
+    commit_async();
   }
   if (kStateOnly || seg + 1 == segs) {
     float* to = kStateOnly ? p.segment_states + piece * all : reinterpret_cast<float*>(keep);

@@ -16,6 +16,12 @@ __device__ __forceinline__ bool find_piece(const StateView& v, int32_t piece, in
     *seq = piece, *at = 0, *of = 1;
     return piece < v.num_seqs;
   }
+  if (v.num_seqs == 1) {
+    int64_t first, last;
+    rows_of(v, 0, &first, &last);
+    *seq = 0, *at = piece, *of = max(1, (int32_t)((last - first + length - 1) / length));
+    return piece < *of;
+  }
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   constexpr int kWarps = kThreads / 32;
   int32_t before_all = 0;

@@ -224,6 +224,33 @@ def test_fresh_sequences_do_not_read_their_slots(ctx):
         assert bool(torch.isfinite(st.dev[:, :st.rec].view(torch.float32)).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("p,skip", [(64, True), (128, False), (8, True)])
+def test_scan_of_infinities_and_nan(ctx, dtype, p, skip):
+    """An input that is not finite reaches its own row of the state from its token on, and nothing before it."""
+    k = kvx()
+    t, heads, n = 300, 2, 64
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, dtype)
+    x[70, 0, 3], x[150, 1, 5], x[151, 1, 6], x[299, 0, 7] = math.inf, math.nan, -math.inf, math.nan
+    st = Slots(1, heads, p, n, dtype=dtype)
+    batch, _ = batch_of([t], [0])
+    out = torch.empty((t, heads, p), dtype=dtype, device="cuda")
+    k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out, D=D.cuda() if skip else None,
+                    workspace=k.kv_state_scan_workspace(ctx, batch, heads, p, n))
+    torch.cuda.synchronize()
+    y, state, size, big = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), D.double() if skip else None,
+                                    None, True, st.state[0].double())
+    got = out.cpu().double()
+    fine = torch.isfinite(y)
+    assert torch.equal(torch.isfinite(got), fine)
+    unit = refs.UNIT[dtype]
+    assert bool(((got - y).abs()[fine] <= (unit * y.abs() + (3 * unit + 2.0 ** -13) * size + 1e-7)[fine]).all())
+    after = st.dev.cpu()[0, :st.rec].view(torch.float32).view(state.shape).double()
+    fine = torch.isfinite(state)
+    assert torch.equal(torch.isfinite(after), fine)
+    assert bool(((after - state).abs()[fine] <= (2.0 ** -14 * big + 1e-9)[fine]).all())
+
+
 def test_token_by_token_is_the_prompt(ctx):
     """A prompt in one call and its tokens one by one leave the same state within the bounds of both."""
     k = kvx()
