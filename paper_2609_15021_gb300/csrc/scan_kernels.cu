@@ -36,8 +36,8 @@ template <int kP>
 struct ScanShape {
   static constexpr int kRows = 2 * kPanel;            // B or C: 128 tokens of up to 128 elements
   static constexpr int kSlice = kP / 64 * kPanel;     // x, its two weighted parts, the rounded state
-  static constexpr int kB = 0, kC = kRows, kX = 2 * kRows, kHi = kX + kSlice, kLo = kHi + kSlice, kH = kLo + kSlice;
-  static constexpr int kSmem = kH + kSlice + 1024;    // and what aligns it to the swizzle's 1024 bytes
+  static constexpr int kB = 0, kC = kRows, kX = 2 * kRows, kH = kX + 3 * kSlice;  // x and its parts take turns
+  static constexpr int kSmem = kH + kSlice + 1024;               // and what aligns it to the swizzle's 1024 bytes
 };
 // Columns of tensor memory.
 constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
@@ -81,19 +81,18 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   __shared__ uint32_t tmem_s;
   uint8_t* smem = raw_smem + (-smem_at(raw_smem) & 1023);
   const StateView& v = p.state;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
   const int line = (warp & 3) * 32 + lane;  // of tensor memory: a token of G and Y, an element of state_dim of H
   const int side = warp >> 2;               // which half of the columns
   const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
   const int32_t h = blockIdx.y, group = h / p.heads_per_group;
-  int32_t s, seg, segs;
-  if (!find_piece<kThreads>(v, piece, p.segment, buf, &s, &seg, &segs)) return;
+  Piece found;
+  if (!find_piece<kThreads>(v, piece, p.segment, buf, &found)) return;
+  const int32_t seg = found.at, segs = found.of;
   if (kStateOnly && seg + 1 == segs) return;  // the last segment's state is nobody's start
-  int64_t first, last;
-  rows_of(v, s, &first, &last);
-  const int64_t begin = first + (int64_t)seg * p.segment, end = min(last, begin + p.segment);
-  const uint8_t* in = slot_of(v, v.slots_in, s);
-  uint8_t* keep = slot_of(v, v.slots_out, s);
+  const int64_t begin = found.first + (int64_t)seg * p.segment, end = min(found.last, begin + p.segment);
+  const uint8_t* in = found.in;
+  uint8_t* keep = found.keep;
   if (!in || !keep) {
     if (!kStateOnly)
       for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kThreads)
@@ -167,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int64_t chunks = (end - begin + kChunk - 1) / kChunk;
   const int64_t step = kStateOnly ? -kChunk : kChunk;
   int64_t t0 = kStateOnly ? begin + (chunks - 1) * kChunk : begin;
+  if (warp == 1 && chunks > 0) weigh(t0, 0.f, &weights_s[0]);
   if (chunks > 0) {
     fetch(b_at, p.b_token, t0, S::kB, state_vecs);
     fetch(x_at, p.x_token, t0, S::kX, slice_vecs);
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   for (int k = 0; k < kCols; ++k) state[k] = 0.f;
   if (!kStateOnly) {
     const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
-    if (line < N && (p.segment_states || !(v.fresh && v.fresh[s]))) {
+    if (line < N && (p.segment_states || !found.fresh)) {
 #pragma unroll
       for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
     }
@@ -192,7 +192,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     fence_operands();
   }
   if (warp == 0) tmem_alloc(smem_at(&tmem_s), kColumns);
-  if (warp == 1 && chunks > 0) weigh(t0, 0.f, &weights_s[0]);
   if (N == 64)  // H's lanes beyond state_dim: their rows of B^T are zeros
     for (int i = threadIdx.x; i < kPanel / 16; i += kThreads)
       *reinterpret_cast<uint4*>(smem + S::kB + kPanel + i * 16) = make_uint4(0, 0, 0, 0);
@@ -225,6 +224,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   if (!kStateOnly && chunks > 0) round_state(state);
 
   float exponent = 0.f;  // of the decay over the segment's chunks so far
+  uint32_t x_to = S::kX, hi_to = S::kX + S::kSlice, lo_to = S::kX + 2 * S::kSlice;
   for (int64_t n = 0; n < chunks; ++n, t0 += step) {
     const Weights& w = weights_s[n & 1];
     const uint32_t parity = n & 1;
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     tmem_before_sync();
     if (__syncthreads_or(dead)) break;  // the chunk's rows, its weights and the rounded state are there
     tmem_after_sync();
-    if (!kStateOnly && threadIdx.x == 0) {
+    if (!kStateOnly && warp == 0 && elected()) {
 #pragma unroll
       for (int k = 0; k < N / 16; ++k)
         matrix_product(tmem + kG, operand_k(base + S::kC, k), operand_k(base + S::kB, k), instruction<E>(false, false, 128), k > 0);
@@ -243,7 +243,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       products_done(bar_g);
     }
     exponent += w.exponent;
-    if (warp == kWarps - 1 && n + 1 < chunks) weigh(t0 + step, kStateOnly ? exponent : 0.f, &weights_s[(n + 1) & 1]);
 
     // x weighted, in two parts, vector by vector where it lies
     bool odd;
@@ -252,23 +251,21 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       constexpr int kVecs = kChunk * kP / 8 / kThreads;
       uint4 x[kVecs];
       uint32_t carries = 0;
-      float scale = 1.f, top = 0.f;
+      float scale = 1.f;
+      __half2 top = __floats2half2_rn(0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
-        x[k] = *reinterpret_cast<const uint4*>(smem + S::kX + (k * kThreads + threadIdx.x) * 16);
-        carries |= odd_carry<E>(x[k].x) | odd_carry<E>(x[k].y) | odd_carry<E>(x[k].z) | odd_carry<E>(x[k].w);
-        if constexpr (kHalf) {
-          const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+        x[k] = *reinterpret_cast<const uint4*>(smem + x_to + (k * kThreads + threadIdx.x) * 16);
+        const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 f = unpack2<E>(u[j] & 0x7FFF7FFFu);
-            top = fmaxf(top, fmaxf(f.x, f.y));
-          }
+        for (int j = 0; j < 4; ++j) {
+          carries |= odd_carry<E>(u[j]);
+          if constexpr (kHalf) top = __hmax2(top, __habs2(*reinterpret_cast<const __half2*>(&u[j])));
         }
       }
       odd = odd_carried(carries);
       if constexpr (kHalf) {
-        const int e = range_of(cta_max(top, max_s[1]));
+        const int e = range_of(cta_max(fmaxf(__low2float(top), __high2float(top)), max_s[1]));
         scale = w.shift * ldexpf(1.f, e), back = ldexpf(1.f, -e) / w.shift;
       }
 #pragma unroll
@@ -290,8 +287,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
           for (int j = 0; j < 4; ++j)
             lo[j] &= (odd2<E>(hi[j] & 0xFFFFu) ? 0 : 0xFFFFu) | (odd2<E>(hi[j] & 0xFFFF0000u) ? 0 : 0xFFFF0000u);
         }
-        *reinterpret_cast<uint4*>(smem + S::kHi + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(smem + S::kLo + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<uint4*>(smem + hi_to + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(smem + lo_to + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
     }
     fence_operands();
@@ -310,12 +307,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
     odd = __syncthreads_or(odd);  // W is there, and G read
     tmem_after_sync();
-    if (threadIdx.x == 0) {
+    if (warp == 0 && elected()) {
 #pragma unroll
       for (int k = 0; k < kChunk / 16; ++k) {
-        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kLo, k),
+        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + lo_to, k),
                        instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
-        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + S::kHi, k),
+        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + hi_to, k),
                        instruction<E>(true, true, kP), true);
       }
       products_done(bar_s);
@@ -345,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       tmem_wait_stores();
       if (odd) {  // a token's x that is not finite must not reach the tokens before it (0 x inf): added below
         for (int i = threadIdx.x; i < S::kSlice / 4; i += kThreads) {
-          uint32_t* at = reinterpret_cast<uint32_t*>(smem + S::kX) + i;
+          uint32_t* at = reinterpret_cast<uint32_t*>(smem + x_to) + i;
           if (odd2<E>(*at & 0xFFFFu)) *at &= 0xFFFF0000u;
           if (odd2<E>(*at & 0xFFFF0000u)) *at &= 0xFFFFu;
         }
@@ -354,10 +351,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       tmem_before_sync();
       __syncthreads();  // M, and x as the product takes it
       tmem_after_sync();
-      if (threadIdx.x == 0) {
+      if (warp == 0 && elected()) {
 #pragma unroll
         for (int k = 0; k < kChunk / 16; ++k)
-          matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + S::kX, k), instruction<E>(false, true, kP), k > 0);
+          matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + x_to, k), instruction<E>(false, true, kP), k > 0);
         products_done(bar_y);
       }
       // Y2 decayed, and the tokens' own x
@@ -373,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       if (p.D) {
 #pragma unroll
         for (int k = 0; k < kCols; k += 8) {
-          const uint4 x = *reinterpret_cast<const uint4*>(smem + S::kX + panel_at(line, (side * kCols + k) / 8));
+          const uint4 x = *reinterpret_cast<const uint4*>(smem + x_to + panel_at(line, (side * kCols + k) / 8));
           const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -386,7 +383,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     // The state after the chunk.
     dead |= !bar_wait(bar_s, parity, p.wait_cycles);
     tmem_after_sync();
-    if (n + 1 < chunks) fetch(b_at, p.b_token, t0 + step, S::kB, state_vecs);
+    if (n + 1 < chunks) {
+      fetch(b_at, p.b_token, t0 + step, S::kB, state_vecs);
+      fetch(x_at, p.x_token, t0 + step, lo_to, slice_vecs);
+    }
+    commit_async();
     if (!kAdds || n + 1 == chunks) {
       const float decay = kStateOnly ? 1.f : ex2(w.exponent);
 #pragma unroll
@@ -403,7 +404,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       dead |= !bar_wait(bar_y, parity, p.wait_cycles);
       tmem_after_sync();
     }
-    if (n + 1 < chunks && (kStateOnly || !p.D)) fetch(x_at, p.x_token, t0 + step, S::kX, slice_vecs);
     if constexpr (!kStateOnly) {
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
@@ -431,19 +431,20 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       // y through W's place, so that whole rows are written
 #pragma unroll
       for (int k = 0; k < kCols; k += 8)
-        *reinterpret_cast<uint4*>(smem + S::kHi + panel_at(line, (side * kCols + k) / 8)) =
+        *reinterpret_cast<uint4*>(smem + hi_to + panel_at(line, (side * kCols + k) / 8)) =
             make_uint4(pack2<E>(y[k], y[k + 1]), pack2<E>(y[k + 2], y[k + 3]), pack2<E>(y[k + 4], y[k + 5]), pack2<E>(y[k + 6], y[k + 7]));
       __syncthreads();
-      if (n + 1 < chunks && p.D) fetch(x_at, p.x_token, t0 + step, S::kX, slice_vecs);
       constexpr int kVecs = kP / 8, kApart = kThreads / kVecs;
       const int r0 = threadIdx.x / kVecs, c = threadIdx.x % kVecs;
       T* to = reinterpret_cast<T*>(p.out) + (t0 + r0) * p.out_token + h * p.out_head + p0 + c * 8;
 #pragma unroll
       for (int k = 0; k < kChunk / kApart; ++k, to += kApart * p.out_token)
         if (t0 + r0 + k * kApart < end)
-          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(smem + S::kHi + panel_at(r0, c) + k * kApart * 128);
+          *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(smem + hi_to + panel_at(r0, c) + k * kApart * 128);
     }
-    commit_async();
+    if (warp == kWarps - 1 && n + 1 < chunks) weigh(t0 + step, kStateOnly ? exponent : 0.f, &weights_s[(n + 1) & 1]);
+    const uint32_t was = x_to;
+    x_to = lo_to, lo_to = hi_to, hi_to = was;
   }
   if (kStateOnly || seg + 1 == segs) {
     float* to = kStateOnly ? p.segment_states + piece * all : reinterpret_cast<float*>(keep);

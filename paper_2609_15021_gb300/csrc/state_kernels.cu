@@ -32,17 +32,17 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
   constexpr int kPast = kWidth - 1;
   __shared__ int32_t buf[kConvThreads / 32 + 3];
   const StateView& v = p.state;
-  int32_t s, piece, pieces;
-  if (!find_piece<kConvThreads>(v, blockIdx.x, kConvRows, buf, &s, &piece, &pieces)) return;
+  Piece found;
+  if (!find_piece<kConvThreads>(v, blockIdx.x, kConvRows, buf, &found)) return;
   const int32_t c = (blockIdx.y * kConvThreads + threadIdx.x) * 8;
   if (c >= p.channels) return;
-  int64_t first, last;
-  rows_of(v, s, &first, &last);
+  const int32_t piece = found.at;
+  const int64_t first = found.first, last = found.last;
   const int64_t begin = first + (int64_t)piece * kConvRows, end = min(last, begin + kConvRows);
   auto in_row = [&](int64_t t) { return *reinterpret_cast<const uint4*>(p.x + (t * p.x_stride + c) * 2); };
   auto out_row = [&](int64_t t) { return reinterpret_cast<uint4*>(p.out + (t * p.out_stride + c) * 2); };
-  const uint8_t* in = slot_of(v, v.slots_in, s);
-  uint8_t* keep = slot_of(v, v.slots_out, s);
+  const uint8_t* in = found.in;
+  uint8_t* keep = found.keep;
   if (!in || !keep) {
     for (int64_t t = begin; t < end; ++t) *out_row(t) = make_uint4(0, 0, 0, 0);
     return;
@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
   for (int j = 0; j < kPast; ++j) {
     if (piece > 0)
       old[j] = in_row(begin - kPast + j);
-    else if (v.fresh && v.fresh[s])
+    else if (found.fresh)
       old[j] = make_uint4(0, 0, 0, 0);
     else
       old[j] = *reinterpret_cast<const uint4*>(in + ((int64_t)j * p.channels + c) * 2);

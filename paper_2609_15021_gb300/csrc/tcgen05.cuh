@@ -97,6 +97,13 @@ __device__ __forceinline__ void matrix_product_t(uint32_t d, uint32_t a, uint64_
   asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
                "r"(a), "l"(b), "r"(what), "r"((uint32_t)add) : "memory");
 }
+// One lane of a converged warp: in a branch on it the compiler keeps what the warp shares in uniform registers, which
+// is where matrix instructions want their operands (issued by a thread picked by its number, one took 60 cycles).
+__device__ __forceinline__ bool elected() {
+  uint32_t one;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+  return one != 0;
+}
 // The barrier's phase ends when the instructions issued so far are done.
 __device__ __forceinline__ void products_done(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
