@@ -9,9 +9,10 @@
 // fp32 laid out as S is in tensor memory, and walks the chunks of a segment.  G, Y1, Y2 and S are all of tensor
 // memory; M takes the place of G as the product's left factor, so it never passes through shared memory.  The products take a quarter of the time that
 // the threads take for the elements between them (an exponential each for G, the splits of W, the rounding of H), so
-// there is one CTA an SM with eight warps, two for every 32 lanes of tensor memory; S is made while the threads
-// are at M and read while Y1 is made, and the next chunk's rows are fetched as soon as a product has done
-// with the last one's.
+// there is one CTA an SM with eight warps, two for every 32 lanes of tensor memory; Y2 and S are made while the
+// threads are at M, and S is read while Y1 is made.  A product with both factors in shared memory is bound by reading
+// them (64 cycles for 16 of k).  The next chunk's rows (96 KB an SM, some 2000 cycles) come in from the chunk's
+// beginning on, into one buffer more and those that a product has done with.
 //
 // Rounding: M and the carried state are rounded to the inputs' type for the product that makes y, one rounding
 // a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into two numbers of that
@@ -32,13 +33,6 @@ namespace {
 
 constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;
 
-template <int kP>
-struct ScanShape {
-  static constexpr int kRows = 2 * kPanel;            // B or C: 128 tokens of up to 128 elements
-  static constexpr int kSlice = kP / 64 * kPanel;     // x, its two weighted parts, the rounded state
-  static constexpr int kB = 0, kC = kRows, kX = 2 * kRows, kH = kX + 3 * kSlice;  // x and its parts take turns
-  static constexpr int kSmem = kH + kSlice + 1024;               // and what aligns it to the swizzle's 1024 bytes
-};
 // Columns of tensor memory.
 constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
 
@@ -49,6 +43,25 @@ struct Weights {
   float d[kChunk];
   float exponent;        // of the whole chunk
   float shift;           // fp16: the power of two that makes the largest weight less than 1
+};
+
+struct Shared {
+  Weights weights;
+  float largest[2][kWarps];
+  int32_t buf[kWarps + 3];
+  uint32_t tmem;
+  uint64_t bars[4];
+};
+
+template <int kP>
+struct ScanShape {
+  static constexpr int kRows = 2 * kPanel;         // B or C: 128 tokens of up to 128 elements
+  static constexpr int kSlice = kP / 64 * kPanel;  // x, its two weighted parts, the rounded state
+  // three buffers for B and C of this chunk and the next, three for x and its parts, the state's (the first pass: two
+  // for B, four for x and its parts)
+  static constexpr int kB = 0, kX = 3 * kRows, kShared = kX + 4 * kSlice;
+  static constexpr int kSmem = kShared + 2048 + 1024;  // 1024: what aligns the panels to their swizzle
+  static_assert(sizeof(Shared) <= 2048 && kSmem <= 232448, "shared memory of an SM");
 };
 
 // The largest value over the CTA.
@@ -74,12 +87,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   constexpr bool kAdds = kStateOnly && !kHalf;  // S adds up over the chunks in tensor memory
   wait_for_previous();
   extern __shared__ __align__(16) uint8_t raw_smem[];
-  __shared__ int32_t buf[kWarps + 3];
-  __shared__ float max_s[2][kWarps];
-  __shared__ Weights weights_s[2];
-  __shared__ __align__(8) uint64_t bars[3];
-  __shared__ uint32_t tmem_s;
   uint8_t* smem = raw_smem + (-smem_at(raw_smem) & 1023);
+  Shared& sh = *reinterpret_cast<Shared*>(smem + S::kShared);
+  Weights& w = sh.weights;
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
   const int line = (warp & 3) * 32 + lane;  // of tensor memory: a token of G and Y, an element of state_dim of H
@@ -87,7 +97,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
   const int32_t h = blockIdx.y, group = h / p.heads_per_group;
   Piece found;
-  if (!find_piece<kThreads>(v, piece, p.segment, buf, &found)) return;
+  if (!find_piece<kThreads>(v, piece, p.segment, sh.buf, &found)) return;
   const int32_t seg = found.at, segs = found.of;
   if (kStateOnly && seg + 1 == segs) return;  // the last segment's state is nobody's start
   const int64_t begin = found.first + (int64_t)seg * p.segment, end = min(found.last, begin + p.segment);
@@ -104,7 +114,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const T* c_at = reinterpret_cast<const T*>(p.c) + group * p.c_group;
   const T* x_at = reinterpret_cast<const T*>(p.x) + h * p.x_head + p0;
   const T* dt_at = reinterpret_cast<const T*>(p.dt) + h;
-  const uint32_t base = smem_at(smem), bar_g = smem_at(&bars[0]), bar_y = smem_at(&bars[1]), bar_s = smem_at(&bars[2]);
+  const uint32_t base = smem_at(smem), bar_g = smem_at(&sh.bars[0]), bar_y2 = smem_at(&sh.bars[1]),
+                 bar_s = smem_at(&sh.bars[2]), bar_y1 = smem_at(&sh.bars[3]);
+  constexpr uint32_t kLast = S::kX + 3 * S::kSlice;  // the rounded state's, or, in the first pass, x's fourth buffer
+  uint32_t b_to = S::kB, c_to = S::kB + S::kRows, spare_to = S::kB + 2 * S::kRows;
+  uint32_t x_to = S::kX, hi_to = S::kX + S::kSlice, lo_to = S::kX + 2 * S::kSlice, next_to = kLast;
 
   // Rows of a chunk, swizzled; those behind the last are zeros.  A thread has one column of vectors of rows that are a
   // multiple of 8 apart, so its place within a row stays.
@@ -125,7 +139,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
   // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
   const float A2 = p.A[h] * kLog2e, D = p.D ? p.D[h] : 0.f;
-  auto weigh = [&](int64_t t0, float after, Weights* w) {
+  auto weigh = [&](int64_t t0, float after) {
     float d[4], a[4], upto = 0.f, behind = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -141,24 +155,24 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
     float below = __shfl_up_sync(~0u, upto, 1), above = __shfl_down_sync(~0u, behind, 1);
     if (lane == 0) below = 0.f;
-    if (lane == 31) above = 0.f, w->exponent = upto;
+    if (lane == 31) above = 0.f, w.exponent = upto;
     above += after;
     float top = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      w->d[4 * lane + k] = d[k];
-      w->sum[4 * lane + k] = below += a[k];
+      w.d[4 * lane + k] = d[k];
+      w.sum[4 * lane + k] = below += a[k];
     }
 #pragma unroll
     for (int k = 3; k >= 0; --k) {
       const float weight = d[k] * ex2(above);
-      w->weight[4 * lane + k] = weight;
+      w.weight[4 * lane + k] = weight;
       above += a[k];
       top = fmaxf(top, fabsf(weight));
     }
     if (kHalf) {
       for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-      if (lane == 0) w->shift = top > 0.f && top < INFINITY ? ldexpf(1.f, max(-100, min(100, -1 - ilogbf(top)))) : 1.f;
+      if (lane == 0) w.shift = top > 0.f && top < INFINITY ? ldexpf(1.f, max(-100, min(100, -1 - ilogbf(top)))) : 1.f;
     }
   };
 
@@ -166,11 +180,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int64_t chunks = (end - begin + kChunk - 1) / kChunk;
   const int64_t step = kStateOnly ? -kChunk : kChunk;
   int64_t t0 = kStateOnly ? begin + (chunks - 1) * kChunk : begin;
-  if (warp == 1 && chunks > 0) weigh(t0, 0.f, &weights_s[0]);
+  if (warp == 1 && chunks > 0) weigh(t0, 0.f);
   if (chunks > 0) {
-    fetch(b_at, p.b_token, t0, S::kB, state_vecs);
-    fetch(x_at, p.x_token, t0, S::kX, slice_vecs);
-    if (!kStateOnly) fetch(c_at, p.c_token, t0, S::kC, state_vecs);
+    fetch(b_at, p.b_token, t0, b_to, state_vecs);
+    fetch(x_at, p.x_token, t0, x_to, slice_vecs);
+    if (!kStateOnly) fetch(c_at, p.c_token, t0, c_to, state_vecs);
   }
   commit_async();
   const int64_t all = (int64_t)p.heads * p.head_dim * N;
@@ -186,19 +200,18 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
   }
   if (threadIdx.x == 0) {
-    bar_init(bar_g);
-    bar_init(bar_y);
-    bar_init(bar_s);
+    for (uint64_t& bar : sh.bars) bar_init(smem_at(&bar));
     fence_operands();
   }
-  if (warp == 0) tmem_alloc(smem_at(&tmem_s), kColumns);
+  if (warp == 0) tmem_alloc(smem_at(&sh.tmem), kColumns);
   if (N == 64)  // H's lanes beyond state_dim: their rows of B^T are zeros
-    for (int i = threadIdx.x; i < kPanel / 16; i += kThreads)
-      *reinterpret_cast<uint4*>(smem + S::kB + kPanel + i * 16) = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < 3 * kPanel / 16; i += kThreads)
+      *reinterpret_cast<uint4*>(smem + S::kB + (i / (kPanel / 16) * 2 + 1) * kPanel + i % (kPanel / 16) * 16) =
+          make_uint4(0, 0, 0, 0);
   tmem_before_sync();
   __syncthreads();
   tmem_after_sync();
-  const uint32_t tmem = tmem_s, my_lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  const uint32_t tmem = sh.tmem, my_lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
   bool dead = false;  // a wait ran out
 
   // The state a segment starts from, and the one after every chunk, rounded to shared memory as Y2's right factor.
@@ -209,13 +222,13 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       float top = 0.f;
 #pragma unroll
       for (int k = 0; k < kCols; ++k) top = fmaxf(top, fabsf(state[k]));
-      const int e = range_of(cta_max(top, max_s[0]));
+      const int e = range_of(cta_max(top, sh.largest[0]));
       scale = ldexpf(1.f, e), state_scale = ldexpf(1.f, -e);
     }
     if (line < N) {
 #pragma unroll
       for (int k = 0; k < kCols; k += 8)
-        *reinterpret_cast<uint4*>(smem + S::kH + panel_at(line, (side * kCols + k) / 8)) =
+        *reinterpret_cast<uint4*>(smem + kLast + panel_at(line, (side * kCols + k) / 8)) =
             make_uint4(pack2<E>(state[k] * scale, state[k + 1] * scale), pack2<E>(state[k + 2] * scale, state[k + 3] * scale),
                        pack2<E>(state[k + 4] * scale, state[k + 5] * scale), pack2<E>(state[k + 6] * scale, state[k + 7] * scale));
     }
@@ -224,9 +237,8 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   if (!kStateOnly && chunks > 0) round_state(state);
 
   float exponent = 0.f;  // of the decay over the segment's chunks so far
-  uint32_t x_to = S::kX, hi_to = S::kX + S::kSlice, lo_to = S::kX + 2 * S::kSlice;
   for (int64_t n = 0; n < chunks; ++n, t0 += step) {
-    const Weights& w = weights_s[n & 1];
+    const bool more = n + 1 < chunks;
     const uint32_t parity = n & 1;
     wait_async<0>();
     fence_operands();
@@ -236,11 +248,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     if (!kStateOnly && warp == 0 && elected()) {
 #pragma unroll
       for (int k = 0; k < N / 16; ++k)
-        matrix_product(tmem + kG, operand_k(base + S::kC, k), operand_k(base + S::kB, k), instruction<E>(false, false, 128), k > 0);
-#pragma unroll
-      for (int k = 0; k < N / 16; ++k)
-        matrix_product(tmem + kY2, operand_k(base + S::kC, k), operand_rows(base + S::kH, k), instruction<E>(false, true, kP), k > 0);
+        matrix_product(tmem + kG, operand_k(base + c_to, k), operand_k(base + b_to, k), instruction<E>(false, false, 128), k > 0);
       products_done(bar_g);
+    }
+    if (more) {
+      fetch(kStateOnly ? b_at : c_at, kStateOnly ? p.b_token : p.c_token, t0 + step, spare_to, state_vecs);
+      if (kStateOnly) fetch(x_at, p.x_token, t0 + step, next_to, slice_vecs);
     }
     exponent += w.exponent;
 
@@ -265,7 +278,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       }
       odd = odd_carried(carries);
       if constexpr (kHalf) {
-        const int e = range_of(cta_max(fmaxf(__low2float(top), __high2float(top)), max_s[1]));
+        const int e = range_of(cta_max(fmaxf(__low2float(top), __high2float(top)), sh.largest[1]));
         scale = w.shift * ldexpf(1.f, e), back = ldexpf(1.f, -e) / w.shift;
       }
 #pragma unroll
@@ -308,17 +321,22 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     odd = __syncthreads_or(odd);  // W is there, and G read
     tmem_after_sync();
     if (warp == 0 && elected()) {
+      if (!kStateOnly) {
+#pragma unroll
+        for (int k = 0; k < N / 16; ++k)
+          matrix_product(tmem + kY2, operand_k(base + c_to, k), operand_rows(base + kLast, k), instruction<E>(false, true, kP), k > 0);
+        products_done(bar_y2);
+      }
 #pragma unroll
       for (int k = 0; k < kChunk / 16; ++k) {
-        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + lo_to, k),
+        matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + lo_to, k),
                        instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
-        matrix_product(tmem + kState, operand_rows(base + S::kB, k), operand_rows(base + hi_to, k),
+        matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + hi_to, k),
                        instruction<E>(true, true, kP), true);
       }
       products_done(bar_s);
     }
     if constexpr (!kStateOnly) {
-      if (n + 1 < chunks) fetch(c_at, p.c_token, t0 + step, S::kC, state_vecs);
       const float sum_t = w.sum[line];
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -355,9 +373,12 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 #pragma unroll
         for (int k = 0; k < kChunk / 16; ++k)
           matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + x_to, k), instruction<E>(false, true, kP), k > 0);
-        products_done(bar_y);
+        products_done(bar_y1);
       }
       // Y2 decayed, and the tokens' own x
+      dead |= !bar_wait(bar_y2, parity, p.wait_cycles);
+      tmem_after_sync();
+      if (more) fetch(b_at, p.b_token, t0 + step, c_to, state_vecs);
       const float by = ex2(sum_t) * state_scale;
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
@@ -383,12 +404,9 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     // The state after the chunk.
     dead |= !bar_wait(bar_s, parity, p.wait_cycles);
     tmem_after_sync();
-    if (n + 1 < chunks) {
-      fetch(b_at, p.b_token, t0 + step, S::kB, state_vecs);
-      fetch(x_at, p.x_token, t0 + step, lo_to, slice_vecs);
-    }
+    if (!kStateOnly && more) fetch(x_at, p.x_token, t0 + step, lo_to, slice_vecs);
     commit_async();
-    if (!kAdds || n + 1 == chunks) {
+    if (!kAdds || !more) {
       const float decay = kStateOnly ? 1.f : ex2(w.exponent);
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
@@ -398,10 +416,10 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
 #pragma unroll
         for (int j = 0; j < 16; ++j) state[k + j] = state[k + j] * decay + r[j] * back;
       }
-      if (!kStateOnly && n + 1 < chunks) round_state(state);
+      if (!kStateOnly && more) round_state(state);
     }
     if constexpr (!kStateOnly) {
-      dead |= !bar_wait(bar_y, parity, p.wait_cycles);
+      dead |= !bar_wait(bar_y1, parity, p.wait_cycles);
       tmem_after_sync();
     }
     if constexpr (!kStateOnly) {
@@ -442,9 +460,15 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
         if (t0 + r0 + k * kApart < end)
           *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(smem + hi_to + panel_at(r0, c) + k * kApart * 128);
     }
-    if (warp == kWarps - 1 && n + 1 < chunks) weigh(t0 + step, kStateOnly ? exponent : 0.f, &weights_s[(n + 1) & 1]);
-    const uint32_t was = x_to;
-    x_to = lo_to, lo_to = hi_to, hi_to = was;
+    if (warp == kWarps - 1 && more) weigh(t0 + step, kStateOnly ? exponent : 0.f);
+    if (kStateOnly) {
+      const uint32_t b_was = b_to, x_was = x_to;
+      b_to = spare_to, spare_to = b_was, x_to = next_to, next_to = x_was;
+    } else {
+      const uint32_t b_was = b_to, x_was = x_to;
+      b_to = c_to, c_to = spare_to, spare_to = b_was;
+      x_to = lo_to, lo_to = hi_to, hi_to = x_was;
+    }
   }
   if (kStateOnly || seg + 1 == segs) {
     float* to = kStateOnly ? p.segment_states + piece * all : reinterpret_cast<float*>(keep);
