@@ -9,8 +9,9 @@
 // fp32 laid out as S is in tensor memory, and walks the chunks of a segment.  G, Y1, Y2 and S are all of tensor
 // memory; M takes the place of G as the product's left factor, so it never passes through shared memory.  The products take a quarter of the time that
 // the threads take for the elements between them (an exponential each for G, the splits of W, the rounding of H), so
-// there is one CTA an SM with eight warps, two for every 32 lanes of tensor memory; Y2 and S are made while the
-// threads are at M, and S is read while Y1 is made.  A product with both factors in shared memory is bound by reading
+// there is one CTA an SM with eight warps for them, two for every 32 lanes of tensor memory, and a ninth that issues the
+// products and makes the next chunk's weights; Y2 and S are made while the threads are at M, and S is read while Y1
+// is made.  A product with both factors in shared memory is bound by reading
 // them (64 cycles for 16 of k).  The next chunk's rows (96 KB an SM, some 2000 cycles) come in from the chunk's
 // beginning on, into one buffer more and those that a product has done with.
 //
@@ -31,7 +32,7 @@
 namespace kvx {
 namespace {
 
-constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;
+constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;  // and a warp more
 
 // Columns of tensor memory.
 constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
@@ -48,7 +49,7 @@ struct Weights {
 struct Shared {
   Weights weights;
   float largest[2][kWarps];
-  int32_t buf[kWarps + 3];
+  int32_t buf[kWarps + 4];
   uint32_t tmem;
   uint64_t bars[4];
 };
@@ -64,11 +65,13 @@ struct ScanShape {
   static_assert(sizeof(Shared) <= 2048 && kSmem <= 232448, "shared memory of an SM");
 };
 
-// The largest value over the CTA.
+// A barrier of the eight warps.
+__device__ __forceinline__ void sync_eight() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// The largest value over their threads.
 __device__ __forceinline__ float cta_max(float v, float* buf) {
   for (int m = 16; m; m >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, m));
   if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
+  sync_eight();
   v = buf[0];
   for (int i = 1; i < kWarps; ++i) v = fmaxf(v, buf[i]);
   return v;
@@ -79,7 +82,7 @@ __device__ __forceinline__ int range_of(float top) {
 }
 
 template <class E, int N, int kP, bool kStateOnly>
-__global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_constant__ ScanParams p) {
   using S = ScanShape<kP>;
   using T = typename E::T;
   constexpr bool kHalf = std::is_same<E, Fp16>::value;
@@ -94,10 +97,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
   const int line = (warp & 3) * 32 + lane;  // of tensor memory: a token of G and Y, an element of state_dim of H
   const int side = warp >> 2;               // which half of the columns
+  const bool issuer = warp == kWarps;
   const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
   const int32_t h = blockIdx.y, group = h / p.heads_per_group;
   Piece found;
-  if (!find_piece<kThreads>(v, piece, p.segment, sh.buf, &found)) return;
+  if (!find_piece<kThreads + 32>(v, piece, p.segment, sh.buf, &found)) return;
   const int32_t seg = found.at, segs = found.of;
   if (kStateOnly && seg + 1 == segs) return;  // the last segment's state is nobody's start
   const int64_t begin = found.first + (int64_t)seg * p.segment, end = min(found.last, begin + p.segment);
@@ -105,7 +109,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   uint8_t* keep = found.keep;
   if (!in || !keep) {
     if (!kStateOnly)
-      for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kThreads)
+      for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kThreads + 32)
         *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.out) + (begin + i / (kP / 2)) * p.out_token + h * p.out_head + p0 +
                                      i % (kP / 2) * 2) = 0;
     return;
@@ -180,34 +184,37 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   const int64_t chunks = (end - begin + kChunk - 1) / kChunk;
   const int64_t step = kStateOnly ? -kChunk : kChunk;
   int64_t t0 = kStateOnly ? begin + (chunks - 1) * kChunk : begin;
-  if (warp == 1 && chunks > 0) weigh(t0, 0.f);
-  if (chunks > 0) {
-    fetch(b_at, p.b_token, t0, b_to, state_vecs);
-    fetch(x_at, p.x_token, t0, x_to, slice_vecs);
-    if (!kStateOnly) fetch(c_at, p.c_token, t0, c_to, state_vecs);
-  }
-  commit_async();
   const int64_t all = (int64_t)p.heads * p.head_dim * N;
   const int64_t state_at = ((int64_t)h * p.head_dim + p0 + side * kCols) * N + line;  // + column * N
   float state[kCols];
 #pragma unroll
   for (int k = 0; k < kCols; ++k) state[k] = 0.f;
-  if (!kStateOnly) {
-    const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
-    if (line < N && (p.segment_states || !found.fresh)) {
-#pragma unroll
-      for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
+  if (issuer) {
+    tmem_alloc(smem_at(&sh.tmem), kColumns);
+    if (lane == 0) {
+      for (uint64_t& bar : sh.bars) bar_init(smem_at(&bar));
+      fence_operands();
     }
+    if (chunks > 0) weigh(t0, 0.f);
+  } else {
+    if (chunks > 0) {
+      fetch(b_at, p.b_token, t0, b_to, state_vecs);
+      fetch(x_at, p.x_token, t0, x_to, slice_vecs);
+      if (!kStateOnly) fetch(c_at, p.c_token, t0, c_to, state_vecs);
+    }
+    commit_async();
+    if (!kStateOnly) {
+      const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
+      if (line < N && (p.segment_states || !found.fresh)) {
+#pragma unroll
+        for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
+      }
+    }
+    if (N == 64)  // S's lanes beyond state_dim: their rows of B^T are zeros
+      for (int i = threadIdx.x; i < 3 * kPanel / 16; i += kThreads)
+        *reinterpret_cast<uint4*>(smem + S::kB + (i / (kPanel / 16) * 2 + 1) * kPanel + i % (kPanel / 16) * 16) =
+            make_uint4(0, 0, 0, 0);
   }
-  if (threadIdx.x == 0) {
-    for (uint64_t& bar : sh.bars) bar_init(smem_at(&bar));
-    fence_operands();
-  }
-  if (warp == 0) tmem_alloc(smem_at(&sh.tmem), kColumns);
-  if (N == 64)  // H's lanes beyond state_dim: their rows of B^T are zeros
-    for (int i = threadIdx.x; i < 3 * kPanel / 16; i += kThreads)
-      *reinterpret_cast<uint4*>(smem + S::kB + (i / (kPanel / 16) * 2 + 1) * kPanel + i % (kPanel / 16) * 16) =
-          make_uint4(0, 0, 0, 0);
   tmem_before_sync();
   __syncthreads();
   tmem_after_sync();
@@ -234,9 +241,18 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
     fence_operands();
   };
-  if (!kStateOnly && chunks > 0) round_state(state);
+  if (!kStateOnly && !issuer && chunks > 0) round_state(state);
 
   float exponent = 0.f;  // of the decay over the segment's chunks so far
+  auto turn = [&]() {    // the buffers' roles in the next chunk
+    const uint32_t b_was = b_to, x_was = x_to;
+    if (kStateOnly) {
+      b_to = spare_to, spare_to = b_was, x_to = next_to, next_to = x_was;
+    } else {
+      b_to = c_to, c_to = spare_to, spare_to = b_was;
+      x_to = lo_to, lo_to = hi_to, hi_to = x_was;
+    }
+  };
   for (int64_t n = 0; n < chunks; ++n, t0 += step) {
     const bool more = n + 1 < chunks;
     const uint32_t parity = n & 1;
@@ -245,17 +261,52 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     tmem_before_sync();
     if (__syncthreads_or(dead)) break;  // the chunk's rows, its weights and the rounded state are there
     tmem_after_sync();
-    if (!kStateOnly && warp == 0 && elected()) {
+    const float chunk_exponent = w.exponent;
+    exponent += chunk_exponent;
+    if (issuer) {
+      if (!kStateOnly && elected()) {
 #pragma unroll
-      for (int k = 0; k < N / 16; ++k)
-        matrix_product(tmem + kG, operand_k(base + c_to, k), operand_k(base + b_to, k), instruction<E>(false, false, 128), k > 0);
-      products_done(bar_g);
+        for (int k = 0; k < N / 16; ++k)
+          matrix_product(tmem + kG, operand_k(base + c_to, k), operand_k(base + b_to, k), instruction<E>(false, false, 128), k > 0);
+        products_done(bar_g);
+      }
+      __syncthreads_or(0);  // W is there, and G read
+      tmem_after_sync();
+      if (elected()) {
+        if (!kStateOnly) {
+#pragma unroll
+          for (int k = 0; k < N / 16; ++k)
+            matrix_product(tmem + kY2, operand_k(base + c_to, k), operand_rows(base + kLast, k), instruction<E>(false, true, kP), k > 0);
+          products_done(bar_y2);
+        }
+#pragma unroll
+        for (int k = 0; k < kChunk / 16; ++k) {
+          matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + lo_to, k),
+                         instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
+          matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + hi_to, k),
+                         instruction<E>(true, true, kP), true);
+        }
+        products_done(bar_s);
+      }
+      if (!kStateOnly) {
+        __syncthreads();  // M, and x as the product takes it
+        tmem_after_sync();
+        if (elected()) {
+#pragma unroll
+          for (int k = 0; k < kChunk / 16; ++k)
+            matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + x_to, k), instruction<E>(false, true, kP), k > 0);
+          products_done(bar_y1);
+        }
+      }
+      __syncwarp();
+      if (more) weigh(t0 + step, kStateOnly ? exponent : 0.f);  // the others have read this chunk's
+      turn();
+      continue;
     }
     if (more) {
       fetch(kStateOnly ? b_at : c_at, kStateOnly ? p.b_token : p.c_token, t0 + step, spare_to, state_vecs);
       if (kStateOnly) fetch(x_at, p.x_token, t0 + step, next_to, slice_vecs);
     }
-    exponent += w.exponent;
 
     // x weighted, in two parts, vector by vector where it lies
     bool odd;
@@ -320,22 +371,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     }
     odd = __syncthreads_or(odd);  // W is there, and G read
     tmem_after_sync();
-    if (warp == 0 && elected()) {
-      if (!kStateOnly) {
-#pragma unroll
-        for (int k = 0; k < N / 16; ++k)
-          matrix_product(tmem + kY2, operand_k(base + c_to, k), operand_rows(base + kLast, k), instruction<E>(false, true, kP), k > 0);
-        products_done(bar_y2);
-      }
-#pragma unroll
-      for (int k = 0; k < kChunk / 16; ++k) {
-        matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + lo_to, k),
-                       instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
-        matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + hi_to, k),
-                       instruction<E>(true, true, kP), true);
-      }
-      products_done(bar_s);
-    }
     if constexpr (!kStateOnly) {
       const float sum_t = w.sum[line];
 #pragma unroll
@@ -369,12 +404,6 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       tmem_before_sync();
       __syncthreads();  // M, and x as the product takes it
       tmem_after_sync();
-      if (warp == 0 && elected()) {
-#pragma unroll
-        for (int k = 0; k < kChunk / 16; ++k)
-          matrix_product_t(tmem + kY1, tmem + kG + k * 8, operand_rows(base + x_to, k), instruction<E>(false, true, kP), k > 0);
-        products_done(bar_y1);
-      }
       // Y2 decayed, and the tokens' own x
       dead |= !bar_wait(bar_y2, parity, p.wait_cycles);
       tmem_after_sync();
@@ -407,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
     if (!kStateOnly && more) fetch(x_at, p.x_token, t0 + step, lo_to, slice_vecs);
     commit_async();
     if (!kAdds || !more) {
-      const float decay = kStateOnly ? 1.f : ex2(w.exponent);
+      const float decay = kStateOnly ? 1.f : ex2(chunk_exponent);
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
         float r[16];
@@ -451,7 +480,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
       for (int k = 0; k < kCols; k += 8)
         *reinterpret_cast<uint4*>(smem + hi_to + panel_at(line, (side * kCols + k) / 8)) =
             make_uint4(pack2<E>(y[k], y[k + 1]), pack2<E>(y[k + 2], y[k + 3]), pack2<E>(y[k + 4], y[k + 5]), pack2<E>(y[k + 6], y[k + 7]));
-      __syncthreads();
+      sync_eight();
       constexpr int kVecs = kP / 8, kApart = kThreads / kVecs;
       const int r0 = threadIdx.x / kVecs, c = threadIdx.x % kVecs;
       T* to = reinterpret_cast<T*>(p.out) + (t0 + r0) * p.out_token + h * p.out_head + p0 + c * 8;
@@ -460,19 +489,11 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
         if (t0 + r0 + k * kApart < end)
           *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(smem + hi_to + panel_at(r0, c) + k * kApart * 128);
     }
-    if (warp == kWarps - 1 && more) weigh(t0 + step, kStateOnly ? exponent : 0.f);
-    if (kStateOnly) {
-      const uint32_t b_was = b_to, x_was = x_to;
-      b_to = spare_to, spare_to = b_was, x_to = next_to, next_to = x_was;
-    } else {
-      const uint32_t b_was = b_to, x_was = x_to;
-      b_to = c_to, c_to = spare_to, spare_to = b_was;
-      x_to = lo_to, lo_to = hi_to, hi_to = x_was;
-    }
+    turn();
   }
   if (kStateOnly || seg + 1 == segs) {
     float* to = kStateOnly ? p.segment_states + piece * all : reinterpret_cast<float*>(keep);
-    if (line < N) {
+    if (!issuer && line < N) {
 #pragma unroll
       for (int k = 0; k < kCols; ++k) to[state_at + k * N] = state[k];
     }
@@ -482,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1) chunk_kernel(const __grid_constan
   tmem_before_sync();
   __syncthreads();
   tmem_after_sync();
-  if (warp == 0) tmem_free(tmem, kColumns);
+  if (issuer) tmem_free(tmem, kColumns);
 }
 
 // Carries the states through a sequence's segments, four elements a thread: where the first pass left what a
@@ -532,12 +553,12 @@ cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
   const dim3 grid((unsigned)(pieces * (p.head_dim / kP)), p.heads);
   constexpr int kSmem = ScanShape<kP>::kSmem;
   if (p.segment_states) {
-    cudaError_t e = launch_after(chunk_kernel<E, N, kP, true>, grid, kThreads, kSmem, s, p);
+    cudaError_t e = launch_after(chunk_kernel<E, N, kP, true>, grid, kThreads + 32, kSmem, s, p);
     if (e != cudaSuccess) return e;
     const dim3 all((p.head_dim * N / 4 + 255) / 256, p.heads, p.state.num_seqs);
     if ((e = launch_after(carry_kernel, all, 256, 0, s, p)) != cudaSuccess) return e;
   }
-  return launch_after(chunk_kernel<E, N, kP, false>, grid, kThreads, kSmem, s, p);
+  return launch_after(chunk_kernel<E, N, kP, false>, grid, kThreads + 32, kSmem, s, p);
 }
 
 template <class E>
