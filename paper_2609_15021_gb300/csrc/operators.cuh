@@ -155,7 +155,9 @@ cudaError_t launch_scan_chunks(const ScanParams& p, int type, cudaStream_t s);
 namespace {
 
 // A kernel that is launched while the one before it in the stream still runs, and waits for its end
-// (wait_for_previous, its first statement) before it touches memory: only the launch itself overlaps.
+// (wait_for_previous, its first statement) before it touches memory: only the launch itself overlaps.  It lets its own
+// successor start after that wait, so a kernel of a call may read before its own wait what was there before the call's
+// kernel in front of it began.
 template <class P>
 cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem, cudaStream_t s, const P& p) {
   cudaLaunchAttribute attr;
@@ -171,7 +173,7 @@ cudaError_t launch_after(void (*kernel)(P), dim3 grid, int threads, size_t smem,
   return cudaLaunchKernelEx(&c, kernel, p);
 }
 __device__ __forceinline__ void wait_for_previous() {
-  asm volatile("griddepcontrol.launch_dependents;\n griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.wait;\n griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 struct Bf16 {

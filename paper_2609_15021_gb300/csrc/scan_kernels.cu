@@ -88,7 +88,9 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   constexpr bool kHalf = std::is_same<E, Fp16>::value;
   constexpr int kCols = kP / 2;  // columns of x, Y and H that a thread has
   constexpr bool kAdds = kStateOnly && !kHalf;  // S adds up over the chunks in tensor memory
-  wait_for_previous();
+  // The last pass's predecessor is the carrying of the states: it waits for that before it reads them.
+  const bool carried = !kStateOnly && p.segment_states;
+  if (!carried) wait_for_previous();
   extern __shared__ __align__(16) uint8_t raw_smem[];
   uint8_t* smem = raw_smem + (-smem_at(raw_smem) & 1023);
   Shared& sh = *reinterpret_cast<Shared*>(smem + S::kShared);
@@ -101,13 +103,17 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
   const int32_t h = blockIdx.y, group = h / p.heads_per_group;
   Piece found;
-  if (!find_piece<kThreads + 32>(v, piece, p.segment, sh.buf, &found)) return;
+  if (!find_piece<kThreads + 32>(v, piece, p.segment, sh.buf, &found)) {
+    if (carried) wait_for_previous();  // no kernel may end before the one before it
+    return;
+  }
   const int32_t seg = found.at, segs = found.of;
   if (kStateOnly && seg + 1 == segs) return;  // the last segment's state is nobody's start
   const int64_t begin = found.first + (int64_t)seg * p.segment, end = min(found.last, begin + p.segment);
   const uint8_t* in = found.in;
   uint8_t* keep = found.keep;
   if (!in || !keep) {
+    if (carried) wait_for_previous();
     if (!kStateOnly)
       for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kThreads + 32)
         *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.out) + (begin + i / (kP / 2)) * p.out_token + h * p.out_head + p0 +
@@ -143,14 +149,18 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
   // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
   const float A2 = p.A[h] * kLog2e, D = p.D ? p.D[h] : 0.f;
-  auto weigh = [&](int64_t t0, float after) {
-    float d[4], a[4], upto = 0.f, behind = 0.f;
+  float d[4];
+  auto load_steps = [&](int64_t t0) {
+    T raw[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int64_t t = t0 + 4 * lane + k;
-      d[k] = t < end ? step_of(p, E::up(dt_at[t * p.dt_token]), h) : 0.f;
-      a[k] = d[k] * A2;
-    }
+    for (int k = 0; k < 4; ++k) raw[k] = t0 + 4 * lane + k < end ? dt_at[(t0 + 4 * lane + k) * p.dt_token] : E::down(0.f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) d[k] = t0 + 4 * lane + k < end ? step_of(p, E::up(raw[k]), h) : 0.f;
+  };
+  auto weigh = [&](float after) {
+    float a[4], upto = 0.f, behind = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a[k] = d[k] * A2;
     upto = behind = (a[0] + a[1]) + (a[2] + a[3]);
     for (int m = 1; m < 32; m <<= 1) {
       const float y = __shfl_up_sync(~0u, upto, m), z = __shfl_down_sync(~0u, behind, m);
@@ -190,12 +200,13 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
 #pragma unroll
   for (int k = 0; k < kCols; ++k) state[k] = 0.f;
   if (issuer) {
+    if (chunks > 0) load_steps(t0);
     tmem_alloc(smem_at(&sh.tmem), kColumns);
     if (lane == 0) {
       for (uint64_t& bar : sh.bars) bar_init(smem_at(&bar));
       fence_operands();
     }
-    if (chunks > 0) weigh(t0, 0.f);
+    if (chunks > 0) weigh(0.f);
   } else {
     if (chunks > 0) {
       fetch(b_at, p.b_token, t0, b_to, state_vecs);
@@ -204,6 +215,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
     }
     commit_async();
     if (!kStateOnly) {
+      if (carried) wait_for_previous();
       const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
       if (line < N && (p.segment_states || !found.fresh)) {
 #pragma unroll
@@ -270,6 +282,8 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
           matrix_product(tmem + kG, operand_k(base + c_to, k), operand_k(base + b_to, k), instruction<E>(false, false, 128), k > 0);
         products_done(bar_g);
       }
+      __syncwarp();
+      if (more) load_steps(t0 + step);
       __syncthreads_or(0);  // W is there, and G read
       tmem_after_sync();
       if (elected()) {
@@ -299,7 +313,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         }
       }
       __syncwarp();
-      if (more) weigh(t0 + step, kStateOnly ? exponent : 0.f);  // the others have read this chunk's
+      if (more) weigh(kStateOnly ? exponent : 0.f);  // the others have read this chunk's
       turn();
       continue;
     }
@@ -533,19 +547,27 @@ __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ Scan
   if (i >= vecs) return;
   float4 state = make_float4(0.f, 0.f, 0.f, 0.f);
   if (!(v.fresh && v.fresh[s])) state = reinterpret_cast<const float4*>(in)[(int64_t)h * vecs + i];
-  for (int32_t g = 0; g < segs; ++g) {
-    const int64_t piece = first_s + g;
-    float4* at = reinterpret_cast<float4*>(p.segment_states) + (piece * p.heads + h) * vecs + i;
-    const float4 made = g + 1 < segs ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
-    *at = state;
-    if (g + 1 < segs) {
-      const float decay = ex2(p.segment_exponents[piece * p.heads + h]);
-      state.x = state.x * decay + made.x, state.y = state.y * decay + made.y;
-      state.z = state.z * decay + made.z, state.w = state.w * decay + made.w;
+  for (int32_t g0 = 0; g0 < segs; g0 += 8) {  // eight segments' loads at once
+    float4 made[8];
+    float decay[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int64_t at = (int64_t)(first_s + g0 + k) * p.heads + h;
+      made[k] = make_float4(0.f, 0.f, 0.f, 0.f), decay[k] = 0.f;
+      if (g0 + k + 1 < segs) {
+        made[k] = reinterpret_cast<const float4*>(p.segment_states)[at * vecs + i];
+        decay[k] = ex2(p.segment_exponents[at]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (g0 + k >= segs) break;
+      reinterpret_cast<float4*>(p.segment_states)[((int64_t)(first_s + g0 + k) * p.heads + h) * vecs + i] = state;
+      state.x = state.x * decay[k] + made[k].x, state.y = state.y * decay[k] + made[k].y;
+      state.z = state.z * decay[k] + made[k].z, state.w = state.w * decay[k] + made[k].w;
     }
   }
 }
-
 
 template <class E, int N, int kP>
 cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
