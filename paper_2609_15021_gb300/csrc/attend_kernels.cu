@@ -193,6 +193,19 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
   float* weights = p.weights + s * p.weights_seq + h * p.weights_head;
   for (int32_t r0 = 0; r0 < rows; r0 += kFinishThreads) {  // rows whose sums are kept at once
     const int32_t n = min(rows - r0, kFinishThreads);
+    // the first key's scores and weight do not wait for the sums
+    int32_t j = from + chunk * kFinishThreads + threadIdx.x;
+    float2 ahead[4];
+    float before = 0.f;
+    auto load = [&]() {
+      if (j >= length) return;
+      const float2* row = reinterpret_cast<const float2*>(scores + (int64_t)j * p.score_rows + r0);
+      before = weights[j];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (2 * k < n) ahead[k] = row[k];
+    };
+    load();
     __syncthreads();
     for (int32_t r = threadIdx.x >> 5; r < n; r += kFinishThreads / 32) {
       const int2 item = p.items[(int64_t)sh * blocks + (r0 + r) / p.part_rows];
@@ -200,15 +213,18 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
       if ((threadIdx.x & 31) == 0) l_s[r] = lse2;
     }
     __syncthreads();
-    for (int32_t j = from + chunk * kFinishThreads + threadIdx.x; j < length; j += chunks * kFinishThreads) {
+    for (; j < length; j += chunks * kFinishThreads, load()) {
       const float2* row = reinterpret_cast<const float2*>(scores + (int64_t)j * p.score_rows + r0);
       float sum = 0.f;
-      for (int32_t r = 0; r < n; r += 2) {
-        const float2 x = row[r / 2];
+      auto add = [&](float2 x, int32_t r) {
         if (x.x != -INFINITY) sum += ex2(x.x - l_s[r]);
         if (r + 1 < n && x.y != -INFINITY) sum += ex2(x.y - l_s[r + 1]);
-      }
-      weights[j] += sum;
+      };
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (2 * k < n) add(ahead[k], 2 * k);
+      for (int32_t r = 8; r < n; r += 2) add(row[r / 2], r);
+      weights[j] = before + sum;
     }
   }
 }
@@ -229,7 +245,7 @@ cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cu
   int64_t grid = heads_all * p.group * p.new_tokens;
   if (p.weights) {
     const int64_t most = (p.pages.max_length + kFinishThreads - 1) / kFinishThreads;
-    grid += heads_all * std::max<int64_t>(1, std::min(most, 8 * num_sms / heads_all));
+    grid += heads_all * std::max<int64_t>(1, std::min(most, 12 * num_sms / heads_all));
   }
   return launch_after(finish_kernel, dim3((unsigned)grid), kFinishThreads, 0, s, p);
 }

@@ -160,14 +160,26 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
   const int32_t blocks = (rows + kRows - 1) / kRows;  // of query rows
   const int32_t per_seq = v.heads * blocks;           // items
 
-  // All steps, and this CTA's run of them.
-  long long total = 0;
-  for (int32_t s = threadIdx.x; s < v.num_seqs; s += kAttendThreads) {
+  // All steps, and this CTA's run of them.  Up to 32 sequences are added up by every warp for itself.
+  const bool few = v.num_seqs <= 32;
+  long long total = 0, upto = 0;  // few: steps of this lane's sequence and those before
+  if (few) {
     int32_t first;
-    if (blockIdx.x == 0) check_length(v, s);
-    total += run_steps(steps_of<kStep>(p, length_of(v, s), &first));
+    if (blockIdx.x == 0 && threadIdx.x < v.num_seqs) check_length(v, threadIdx.x);
+    upto = lane < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, length_of(v, lane), &first)) * per_seq : 0;
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long y = __shfl_up_sync(~0u, upto, d);
+      if (lane >= d) upto += y;
+    }
+    total = __shfl_sync(~0u, upto, 31);
+  } else {
+    for (int32_t s = threadIdx.x; s < v.num_seqs; s += kAttendThreads) {
+      int32_t first;
+      if (blockIdx.x == 0) check_length(v, s);
+      total += run_steps(steps_of<kStep>(p, length_of(v, s), &first));
+    }
+    total = cta_sum<kWarps>(total, buf) * per_seq;
   }
-  total = cta_sum<kWarps>(total, buf) * per_seq;
   for (int32_t s = blockIdx.x; s < v.num_seqs; s += gridDim.x) {  // sequences without a key
     if (length_of(v, s) > 0) continue;
     for (int32_t i = threadIdx.x; i < v.heads * rows * (v.head_dim / 4); i += kAttendThreads) {
@@ -185,7 +197,11 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
   // The sequence that `begin` lies in: every thread takes a sequence's steps, 128 at a time.
   int32_t seq = 0;
   long long seq_begin = 0;  // first step of `seq`'s items
-  for (int32_t base = 0; base < v.num_seqs && v.num_seqs > 1; base += kAttendThreads) {
+  if (few) {
+    seq = __ffs(__ballot_sync(~0u, begin < upto)) - 1;
+    seq_begin = seq > 0 ? __shfl_sync(~0u, upto, seq - 1) : 0;
+  }
+  for (int32_t base = 0; base < v.num_seqs && !few; base += kAttendThreads) {
     int32_t first;
     const int32_t s = base + threadIdx.x;
     const long long mine = s < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, length_of(v, s), &first)) * per_seq : 0;
@@ -314,38 +330,39 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         auto load2 = [&](int col) -> uint32_t {  // two raw neighbouring elements
           return there && col < v.head_dim ? *reinterpret_cast<const uint32_t*>(qrow + col * 2) : 0u;
         };
-        float shift = 1.f;
+        uint32_t raw[kKs][2];
+#pragma unroll
+        for (int ks = 0; ks < kKs; ++ks)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) raw[ks][e] = load2(kWide ? ks * 16 + sub * 4 + e * 2 : ks * 16 + sub * 2 + e * 8);
+        int shift = 0;
         if constexpr (kWide) {
           float top = 0.f;
 #pragma unroll
           for (int ks = 0; ks < kKs; ++ks)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float2 f = wide(load2(ks * 16 + sub * 4 + e * 2));
+              const float2 f = wide(raw[ks][e]);
               top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
             }
           top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
           top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
           // the largest to [2^10, 2^11): exponents only
-          const int e = top > 0.f && top < INFINITY ? 10 - ilogbf(top) : 0;
-          shift = ldexpf(1.f, max(-100, min(100, e)));
+          if (top > 0.f && top < INFINITY) shift = max(-100, min(100, 10 - ilogbf(top)));
         }
+        const float up = power_of_two(shift);
         if (sub == 0 && (!S::kQueryInRegs || warp == 0)) {
           row_pos[tile * 8 + quad] = there ? length - p.new_tokens + t : -1;
           row_slope[tile * 8 + quad] = there && p.slopes ? p.slopes[head] * kLog2e : 0.f;
-          row_scale[tile * 8 + quad] = p.scale * p.k_scale * kLog2e / shift;
+          row_scale[tile * 8 + quad] = p.scale * p.k_scale * kLog2e * power_of_two(-shift);
         }
 #pragma unroll
         for (int ks = 0; ks < kKs; ++ks) {
           uint32_t f[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            if constexpr (kWide) {
-              const float2 x = wide(load2(ks * 16 + sub * 4 + e * 2));
-              f[e] = pack2<Fp16>(x.x * shift, x.y * shift);
-            } else {
-              f[e] = load2(ks * 16 + sub * 2 + e * 8);
-            }
+            const float2 x = wide(raw[ks][e]);
+            f[e] = kWide ? pack2<Fp16>(x.x * up, x.y * up) : raw[ks][e];
           }
           if constexpr (S::kQueryInRegs) {
             qf[ks][tile][0] = f[0], qf[ks][tile][1] = f[1];

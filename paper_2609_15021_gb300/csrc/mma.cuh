@@ -33,6 +33,8 @@ __device__ __forceinline__ float rcp(float x) {
   return y;
 }
 
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((127 + e) << 23); }  // -126 <= e <= 127
+
 // Four 8 x 8 matrices of 16-bit elements, a row's address from each lane: lane i gets elements
 // 2 (i % 4) and the next of row i / 4 of each, or, transposed, rows 2 (i % 4) and the next of column i / 4.
 __device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t at) {

@@ -43,7 +43,7 @@ struct Weights {
   float weight[kChunk];  // d times the decay behind it
   float d[kChunk];
   float exponent;        // of the whole chunk
-  float shift;           // fp16: the power of two that makes the largest weight less than 1
+  int shift;             // fp16: the power of two that makes the largest weight less than 1
 };
 
 struct Shared {
@@ -78,7 +78,7 @@ __device__ __forceinline__ float cta_max(float v, float* buf) {
 }
 // A power of two that takes values up to `top` below 2^11.
 __device__ __forceinline__ int range_of(float top) {
-  return top > 0.f && top < INFINITY ? max(-100, min(100, 10 - ilogbf(top))) : 0;
+  return top > 0.f && top < INFINITY ? max(-60, min(60, 10 - ilogbf(top))) : 0;
 }
 
 template <class E, int N, int kP, bool kStateOnly>
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
     }
     if (kHalf) {
       for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-      if (lane == 0) w.shift = top > 0.f && top < INFINITY ? ldexpf(1.f, max(-100, min(100, -1 - ilogbf(top)))) : 1.f;
+      if (lane == 0) w.shift = top > 0.f && top < INFINITY ? max(-60, min(60, -1 - ilogbf(top))) : 0;
     }
   };
 
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
 #pragma unroll
       for (int k = 0; k < kCols; ++k) top = fmaxf(top, fabsf(state[k]));
       const int e = range_of(cta_max(top, sh.largest[0]));
-      scale = ldexpf(1.f, e), state_scale = ldexpf(1.f, -e);
+      scale = power_of_two(e), state_scale = power_of_two(-e);
     }
     if (line < N) {
 #pragma unroll
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       odd = odd_carried(carries);
       if constexpr (kHalf) {
         const int e = range_of(cta_max(fmaxf(__low2float(top), __high2float(top)), sh.largest[1]));
-        scale = w.shift * ldexpf(1.f, e), back = ldexpf(1.f, -e) / w.shift;
+        scale = power_of_two(e + w.shift), back = power_of_two(-e - w.shift);
       }
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
