@@ -245,7 +245,7 @@ cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cu
   int64_t grid = heads_all * p.group * p.new_tokens;
   if (p.weights) {
     const int64_t most = (p.pages.max_length + kFinishThreads - 1) / kFinishThreads;
-    grid += heads_all * std::max<int64_t>(1, std::min(most, 12 * num_sms / heads_all));
+    grid += heads_all * std::max<int64_t>(1, std::min(most, 4 * num_sms / heads_all));
   }
   return launch_after(finish_kernel, dim3((unsigned)grid), kFinishThreads, 0, s, p);
 }

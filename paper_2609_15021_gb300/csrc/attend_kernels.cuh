@@ -45,7 +45,7 @@ namespace kvx {
 namespace {
 
 constexpr int kMaxCtas = 320;  // of a launch
-constexpr int kItemSteps = 6;
+constexpr int kItemSteps = 12;
 // Exponents are relative to 2^10 below the largest score so far (fp16 probabilities stay
 // normal down to 2^-24 of it), and it is raised when a score passes it by more than 2^5.
 constexpr float kBelow = 10.f, kSlack = 15.f;
@@ -63,7 +63,7 @@ struct AttendShape {
   static constexpr int kRowsPerLoad = 32 / kVecs;
   static constexpr int kLoads = kStep / kRowsPerLoad;  // of K, and of V, by a lane
   static constexpr int kRows = 8 * kTiles;
-  // the queries as the products' right factor: [16 dims][tile] x 8 bytes a lane, kept in registers where they fit
+  // the queries as the products' right factor: [32 dims][tile] x 16 bytes a lane, kept in registers where they fit
   static constexpr bool kQueryInRegs = kDim / 16 * kTiles <= 16;
   static constexpr int kQueryBytes = kQueryInRegs ? 0 : kDim / 16 * kTiles * 256;
   // two CTAs an SM, but one where two stages of every ring are more than half its shared memory
@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
           if constexpr (S::kQueryInRegs) {
             qf[ks][tile][0] = f[0], qf[ks][tile][1] = f[1];
           } else {
-            *reinterpret_cast<uint2*>(query_smem + ((ks * kTiles + tile) * 32 + lane) * 8) = make_uint2(f[0], f[1]);
+            *reinterpret_cast<uint2*>(query_smem + ((ks / 2 * kTiles + tile) * 32 + lane) * 16 + ks % 2 * 8) = make_uint2(f[0], f[1]);
           }
         }
       }
@@ -414,35 +414,36 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         for (int t = 0; t < kTiles; ++t)
 #pragma unroll
           for (int e = 0; e < 4; ++e) sc[n][t][e] = 0.f;
-      auto score = [&](int n, int ks, const uint32_t (&a)[4]) {
+#pragma unroll
+      for (int ks = 0; ks < kKs; ks += 2) {  // 32 dims
+        uint4 q[kTiles];
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-          if constexpr (S::kQueryInRegs) {
-            mma<C>(sc[n][t], a, qf[ks][t][0], qf[ks][t][1]);
-          } else {
-            const uint2 b = *reinterpret_cast<const uint2*>(query_smem + ((ks * kTiles + t) * 32 + lane) * 8);
-            mma<C>(sc[n][t], a, b.x, b.y);
-          }
+          if constexpr (S::kQueryInRegs)
+            q[t] = make_uint4(qf[ks][t][0], qf[ks][t][1], qf[ks + 1][t][0], qf[ks + 1][t][1]);
+          else
+            q[t] = *reinterpret_cast<const uint4*>(query_smem + ((ks / 2 * kTiles + t) * 32 + lane) * 16);
         }
-      };
-#pragma unroll
-      for (int ks = 0; ks < kKs; ks += kWide ? 2 : 1) {
 #pragma unroll
         for (int n = 0; n < kBlocks; ++n) {
-          uint32_t b[4];
+          uint32_t b[4], a[4];
           if constexpr (!kWide) {
-            load_matrices(b, at_k + n * 16 * S::kPitch + ks * 32);
-            score(n, ks, b);
+            load_matrices(a, at_k + n * 16 * S::kPitch + ks * 32);
           } else {
             load_matrices(b, at_k + n * 16 * S::kPitch + ks * 16);
-            uint32_t a[4];
             widen4(b[0], a[0], a[2]);
             widen4(b[1], a[1], a[3]);
-            score(n, ks, a);
+          }
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) mma<C>(sc[n][t], a, q[t].x, q[t].y);
+          if constexpr (!kWide) {
+            load_matrices(a, at_k + n * 16 * S::kPitch + ks * 32 + 32);
+          } else {
             widen4(b[2], a[0], a[2]);
             widen4(b[3], a[1], a[3]);
-            score(n, ks + 1, a);
           }
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) mma<C>(sc[n][t], a, q[t].z, q[t].w);
         }
       }
 
