@@ -16,9 +16,10 @@
 // beginning on, into one buffer more and those that a product has done with.
 //
 // Rounding: M and the carried state are rounded to the inputs' type for the product that makes y, one rounding
-// a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into two numbers of that
-// type, whose sum is the weighted x to 16 bits or more, and both are multiplied with B.  In fp16 the state and W are
-// scaled by powers of two into its range; M is not.
+// a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into three bf16 or two fp16
+// numbers, whose sum is the weighted x to 22 bits or more, and all are multiplied with B (two bf16 parts, 16 bits, left
+// the state off by 2.5e-6 where the recurrence in fp32 is by 5e-7).  In fp16 the state and W are scaled by powers of two
+// into its range; M is not.
 //
 // A long sequence is cut into segments, so that every SM has some: a first pass makes each segment's state from
 // nothing (from its last chunk to its first, so that weights need no later decay), a second one carries the states
@@ -59,8 +60,10 @@ struct ScanShape {
   static constexpr int kRows = 2 * kPanel;         // B or C: 128 tokens of up to 128 elements
   static constexpr int kSlice = kP / 64 * kPanel;  // x, its two weighted parts, the rounded state
   // three buffers for B and C of this chunk and the next, three for x and its parts, the state's (the first pass: two
-  // for B, four for x and its parts)
-  static constexpr int kB = 0, kX = 3 * kRows, kShared = kX + 4 * kSlice;
+  // for B, four for x and its parts), and one for the third part in bf16: where slices are as large as rows the third of
+  // the first ones
+  static constexpr int kB = 0, kX = 3 * kRows, kRest = kP == 64 ? kX + 4 * kSlice : kB + 2 * kRows;
+  static constexpr int kShared = kX + (kP == 64 ? 5 : 4) * kSlice;
   static constexpr int kSmem = kShared + 2048 + 1024;  // 1024: what aligns the panels to their swizzle
   static_assert(sizeof(Shared) <= 2048 && kSmem <= 232448, "shared memory of an SM");
 };
@@ -88,6 +91,8 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   constexpr bool kHalf = std::is_same<E, Fp16>::value;
   constexpr int kCols = kP / 2;  // columns of x, Y and H that a thread has
   constexpr bool kAdds = kStateOnly && !kHalf;  // S adds up over the chunks in tensor memory
+  constexpr bool kThree = !kHalf;               // parts of W
+  constexpr bool kSpare = kStateOnly || !kThree || kP == 64;  // a buffer of rows more than a chunk takes
   // The last pass's predecessor is the carrying of the states: it waits for that before it reads them.
   const bool carried = !kStateOnly && p.segment_states;
   if (!carried) wait_for_previous();
@@ -127,7 +132,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   const uint32_t base = smem_at(smem), bar_g = smem_at(&sh.bars[0]), bar_y2 = smem_at(&sh.bars[1]),
                  bar_s = smem_at(&sh.bars[2]), bar_y1 = smem_at(&sh.bars[3]);
   constexpr uint32_t kLast = S::kX + 3 * S::kSlice;  // the rounded state's, or, in the first pass, x's fourth buffer
-  uint32_t b_to = S::kB, c_to = S::kB + S::kRows, spare_to = S::kB + 2 * S::kRows;
+  uint32_t b_to = S::kB, c_to = S::kB + S::kRows, spare_to = kStateOnly ? c_to : S::kB + 2 * S::kRows;
   uint32_t x_to = S::kX, hi_to = S::kX + S::kSlice, lo_to = S::kX + 2 * S::kSlice, next_to = kLast;
 
   // Rows of a chunk, swizzled; those behind the last are zeros.  A thread has one column of vectors of rows that are a
@@ -223,7 +228,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       }
     }
     if (N == 64)  // S's lanes beyond state_dim: their rows of B^T are zeros
-      for (int i = threadIdx.x; i < 3 * kPanel / 16; i += kThreads)
+      for (int i = threadIdx.x; i < (kSpare && !kStateOnly ? 3 : 2) * kPanel / 16; i += kThreads)
         *reinterpret_cast<uint4*>(smem + S::kB + (i / (kPanel / 16) * 2 + 1) * kPanel + i % (kPanel / 16) * 16) =
             make_uint4(0, 0, 0, 0);
   }
@@ -261,7 +266,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
     if (kStateOnly) {
       b_to = spare_to, spare_to = b_was, x_to = next_to, next_to = x_was;
     } else {
-      b_to = c_to, c_to = spare_to, spare_to = b_was;
+      if (kSpare) b_to = c_to, c_to = spare_to, spare_to = b_was;
       x_to = lo_to, lo_to = hi_to, hi_to = x_was;
     }
   };
@@ -295,8 +300,12 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         }
 #pragma unroll
         for (int k = 0; k < kChunk / 16; ++k) {
+          const bool add = k > 0 || (kAdds && n > 0);
+          if (kThree)
+            matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + S::kRest, k),
+                           instruction<E>(true, true, kP), add);
           matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + lo_to, k),
-                         instruction<E>(true, true, kP), k > 0 || (kAdds && n > 0));
+                         instruction<E>(true, true, kP), kThree || add);
           matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + hi_to, k),
                          instruction<E>(true, true, kP), true);
         }
@@ -317,12 +326,12 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       turn();
       continue;
     }
-    if (more) {
+    if (more && kSpare) {
       fetch(kStateOnly ? b_at : c_at, kStateOnly ? p.b_token : p.c_token, t0 + step, spare_to, state_vecs);
       if (kStateOnly) fetch(x_at, p.x_token, t0 + step, next_to, slice_vecs);
     }
 
-    // x weighted, in two parts, vector by vector where it lies
+    // x weighted, in its parts, vector by vector where it lies
     bool odd;
     float back = 1.f;  // fp16: what undoes the scaling of W
     {
@@ -351,20 +360,29 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         const int i = k * kThreads + threadIdx.x, row = i / 8 % kChunk;
         const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
         const float weight = w.weight[row] * scale;
-        uint32_t hi[4], lo[4];
+        uint32_t hi[4], lo[4], rest[4] = {};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           float2 f = unpack2<E>(u[j]);
           f.x *= weight, f.y *= weight;
           hi[j] = pack2<E>(f.x, f.y);
           const float2 r = unpack2<E>(hi[j]);
-          lo[j] = pack2<E>(f.x - r.x, f.y - r.y);
+          f.x -= r.x, f.y -= r.y;
+          lo[j] = pack2<E>(f.x, f.y);
+          if constexpr (kThree) {
+            const float2 q = unpack2<E>(lo[j]);
+            rest[j] = pack2<E>(f.x - q.x, f.y - q.y);
+          }
         }
-        if (odd) {  // inf - inf: an infinite x has no second part
+        if (odd) {  // inf - inf: an infinite x has no other part
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            lo[j] &= (odd2<E>(hi[j] & 0xFFFFu) ? 0 : 0xFFFFu) | (odd2<E>(hi[j] & 0xFFFF0000u) ? 0 : 0xFFFF0000u);
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t fine = (odd2<E>(hi[j] & 0xFFFFu) ? 0 : 0xFFFFu) | (odd2<E>(hi[j] & 0xFFFF0000u) ? 0 : 0xFFFF0000u);
+            lo[j] &= fine, rest[j] &= fine;
+          }
         }
+        if constexpr (kThree)
+          *reinterpret_cast<uint4*>(smem + S::kRest + i * 16) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
         *reinterpret_cast<uint4*>(smem + hi_to + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
         *reinterpret_cast<uint4*>(smem + lo_to + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
@@ -421,7 +439,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       // Y2 decayed, and the tokens' own x
       dead |= !bar_wait(bar_y2, parity, p.wait_cycles);
       tmem_after_sync();
-      if (more) fetch(b_at, p.b_token, t0 + step, c_to, state_vecs);
+      if (more) fetch(kSpare ? b_at : c_at, kSpare ? p.b_token : p.c_token, t0 + step, c_to, state_vecs);
       const float by = ex2(sum_t) * state_scale;
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
@@ -447,7 +465,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
     // The state after the chunk.
     dead |= !bar_wait(bar_s, parity, p.wait_cycles);
     tmem_after_sync();
-    if (!kStateOnly && more) fetch(x_at, p.x_token, t0 + step, lo_to, slice_vecs);
+    if (!kStateOnly && more) {
+      if (!kSpare) fetch(b_at, p.b_token, t0 + step, b_to, state_vecs);
+      fetch(x_at, p.x_token, t0 + step, lo_to, slice_vecs);
+    }
     commit_async();
     if (!kAdds || !more) {
       const float decay = kStateOnly ? 1.f : ex2(chunk_exponent);
