@@ -162,9 +162,10 @@ typedef struct {
   uint32_t flags;             /* KVX_FLAG_*                                     */
   int64_t wait_cycles;        /* limit of every bounded wait inside a kernel, in
                                  SM cycles (the TMA engine's waits for its
-                                 global -> shared copies); 0 = 4e9, about 2 s at
+                                 global -> shared copies, kv_state_scan's for
+                                 the tensor cores); 0 = 4e9, about 2 s at
                                  the maximum SM clock.  When a wait expires, the
-                                 CTA issues no further copy, waits once more
+                                 TMA engine's CTA issues no further copy, waits once more
                                  (same limit) for each copy it has started,
                                  then returns; kv_get_device_error reports
                                  KVX_ETIMEOUT and that call's output is
@@ -746,7 +747,7 @@ typedef struct {
 
 /* Bytes of device workspace that kv_attend needs for these shapes (more with
    attention->weights, whose scores are kept until the softmax sums are known).
-   It must be zero before its first use; every call leaves it fit for the next.
+   It needs no initial contents and keeps nothing from one call for the next.
    One call uses it at a time: calls that may overlap need one each.            */
 kvx_status kv_attend_workspace(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch,
                                const kvx_attention* attention, int64_t* bytes);
@@ -845,7 +846,13 @@ typedef struct {
   int64_t x_token_stride, x_head_stride, dt_token_stride, b_token_stride, b_group_stride, c_token_stride,
       c_group_stride, out_token_stride, out_head_stride;
 } kvx_scan;
-/* Device workspace of kv_state_scan (0 for one token of every sequence).       */
+/* Prompts (starts given, 16 tokens a sequence or more on average, head_dim a
+   multiple of 64, state_dim 64 or 128) are scanned in matrix form on the tensor
+   cores, where the products C.B, decayed and weighted, must stay within the
+   range of `type` (65504 in fp16); others token by token.  A wait for the tensor
+   cores that runs out (kvx_opts.wait_cycles) is reported as KVX_ETIMEOUT by
+   kv_get_device_error, the output then being incomplete.
+   Device workspace (0 for one token of every sequence); as kv_attend's.        */
 kvx_status kv_state_scan_workspace(kvx_ctx* ctx, const kvx_state_batch* batch, const kvx_scan* scan, int64_t* bytes);
 kvx_status kv_state_scan(kvx_ctx* ctx, const kvx_state* state, const kvx_state_batch* batch, const kvx_scan* scan,
                          const void* x, const void* dt, const void* B, const void* C, void* out, void* workspace,

@@ -789,7 +789,7 @@ class KvAttention:
 
 def kv_attend_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttention, weights: bool = False,
                         dtype=None):
-    """A zeroed workspace tensor for kv_attend calls of these shapes (weights: that accumulate the
+    """A workspace tensor for kv_attend calls of these shapes (weights: that accumulate the
     attention weights; dtype: the queries', where the cache's does not tell).  One call uses it at a time."""
     import torch
     c = kvx_attention.from_buffer_copy(attention._c)
@@ -799,7 +799,7 @@ def kv_attend_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttentio
     out = ctypes.c_int64()
     _check(_lib.kv_attend_workspace(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(c),
                                     ctypes.byref(out)), "kv_attend_workspace")
-    return torch.zeros(max(16, out.value), dtype=torch.uint8, device=batch.lengths.device)
+    return torch.empty(max(16, out.value), dtype=torch.uint8, device=batch.lengths.device)
 
 
 def kv_attend(ctx, pool: KvPool, layer: int, batch: KvBatch, attention: KvAttention, query, out, workspace,
