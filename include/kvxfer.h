@@ -632,7 +632,7 @@ const char* kv_last_error_message(void);
  * (those whose warps take their work from a queue: large kv_store / kv_load
  * launches over the host link), "memcpy"
  * (staged-mode copies), "event" (the staged pipeline's ordering event
- * recorded on the caller's stream), "host_alloc" (kv_host_alloc).  Three more
+ * recorded on the caller's stream), "host_alloc" (kv_host_alloc).  Four more
  * points fail differently.  "chunk_map": the (after_calls + 1)-th next
  * kv_store_noalloc whose chunks are mapped takes them as not mapped, and
  * packs and copies.  "tma_wait": the (after_calls + 1)-th next launch
@@ -640,7 +640,10 @@ const char* kv_last_error_message(void);
  * that no copy brings, so that unit's bounded wait runs out (after
  * kvx_opts.wait_cycles) with no copy in flight: the launch leaves that unit
  * unmoved and kv_get_device_error returns KVX_ETIMEOUT; nothing faults or
- * hangs.  "tier_exit" ends the process (_exit(3)) inside
+ * hangs.  "scan_wait": the (after_calls + 1)-th next kv_state_scan in matrix
+ * form does not announce the end of its first chunk's products, so the waits for
+ * it run out: the call's output is incomplete and kv_get_device_error returns
+ * KVX_ETIMEOUT.  "tier_exit" ends the process (_exit(3)) inside
  * kv_tier_reserve, while it holds a shared tier's table lock, right after it
  * has taken a slot for the new key; it tests how the processes left recover
  * the tier from a replica that died mid-update.  One point is armed at a

@@ -1232,7 +1232,7 @@ kvx_status kv_state_load(kvx_ctx* ctx, int32_t num_layers, void* const* layer_ba
 
 kvx_status kv_fault_inject(const char* point, int32_t after_calls) {
   static const char* const points[] = {"launch",    "queue_launch", "memcpy",   "event",
-                                       "host_alloc", "tier_exit",    "tma_wait", "chunk_map"};
+                                       "host_alloc", "tier_exit",    "tma_wait", "chunk_map",    "scan_wait"};
   std::lock_guard<std::mutex> lock(g_fault_mu);
   if (!point || !point[0]) {
     g_fault_point[0] = 0;

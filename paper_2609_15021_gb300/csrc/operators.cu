@@ -127,7 +127,6 @@ kvx_status layer_of(DeviceMemory& mem, const kvx_pool* pool, int32_t layer, cons
 }
 
 kvx_status launched(kvx_ctx* ctx, cudaError_t e, const char* what, int line, int n) {
-  if (fault_point("launch")) e = cudaErrorUnknown;
   if (e != cudaSuccess) {
     record_cuda_error((int)e, what, line);
     return KVX_ECUDA;
@@ -135,7 +134,7 @@ kvx_status launched(kvx_ctx* ctx, cudaError_t e, const char* what, int line, int
   count_launches(ctx, n);
   return KVX_OK;
 }
-#define KVX_LAUNCHED(ctx, call, n) launched(ctx, call, #call, __LINE__, n)
+#define KVX_LAUNCHED(ctx, call, n) launched(ctx, fault_point("launch") ? cudaErrorUnknown : call, #call, __LINE__, n)
 
 kvx_status view_state(const CtxView& ctx, const kvx_state* s, const kvx_state_batch* b, int64_t offset, int64_t bytes,
                       DeviceMemory& mem, StateView* v) {
@@ -548,6 +547,7 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
     p.softplus = a->softplus;
     p.wait_cycles = ctx.wait_cycles;
     p.timeout = ctx.timeout;
+    p.stall = p.segment && fault_point("scan_wait");
     return KVX_LAUNCHED(c, launch_scan(p, a->type, ctx.num_sms, stream), space.bytes > 0 ? 3 : 1);
   });
 }

@@ -134,6 +134,7 @@ struct ScanParams {
   float* segment_exponents;  // [piece][head]
   long long wait_cycles;     // limit of a wait for the tensor cores
   int* timeout;              // set when one ran out
+  bool stall;                // fault point "scan_wait": the first chunk's products are not announced
 };
 // The segment of the matrix form for a batch, 0 where it is not used; *cut: whether a sequence may have several.
 int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut);

@@ -52,7 +52,7 @@ struct Shared {
   float largest[2][kWarps];
   int32_t buf[kWarps + 4];
   uint32_t tmem;
-  uint64_t bars[4];
+  uint64_t bars[5];
 };
 
 template <int kP>
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   const T* x_at = reinterpret_cast<const T*>(p.x) + h * p.x_head + p0;
   const T* dt_at = reinterpret_cast<const T*>(p.dt) + h;
   const uint32_t base = smem_at(smem), bar_g = smem_at(&sh.bars[0]), bar_y2 = smem_at(&sh.bars[1]),
-                 bar_s = smem_at(&sh.bars[2]), bar_y1 = smem_at(&sh.bars[3]);
+                 bar_s = smem_at(&sh.bars[2]), bar_y1 = smem_at(&sh.bars[3]), bar_end = smem_at(&sh.bars[4]);
   constexpr uint32_t kLast = S::kX + 3 * S::kSlice;  // the rounded state's, or, in the first pass, x's fourth buffer
   uint32_t b_to = S::kB, c_to = S::kB + S::kRows, spare_to = kStateOnly ? c_to : S::kB + 2 * S::kRows;
   uint32_t x_to = S::kX, hi_to = S::kX + S::kSlice, lo_to = S::kX + 2 * S::kSlice, next_to = kLast;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   __syncthreads();
   tmem_after_sync();
   const uint32_t tmem = sh.tmem, my_lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-  bool dead = false;  // a wait ran out
+  bool dead = false;  // a wait ran out: the others are not waited for
 
   // The state a segment starts from, and the one after every chunk, rounded to shared memory as Y2's right factor.
   float state_scale = 1.f;  // fp16: what undoes the rounded state's scaling
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
           matrix_product(tmem + kState, operand_rows(base + b_to, k), operand_rows(base + hi_to, k),
                          instruction<E>(true, true, kP), true);
         }
-        products_done(bar_s);
+        if (!p.stall || n > 0) products_done(bar_s);
       }
       if (!kStateOnly) {
         __syncthreads();  // M, and x as the product takes it
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
     // G's columns, 16 of every 32 a side: read by all before M takes their place
     float g[4][16];
     if constexpr (!kStateOnly) {
-      dead |= !bar_wait(bar_g, parity, p.wait_cycles);
+      dead = dead || !bar_wait(bar_g, parity, p.wait_cycles);
       tmem_after_sync();
 #pragma unroll
       for (int q = 0; q < 4; ++q) tmem_load16(g[q], my_lanes + kG + q * 32 + side * 16);
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       __syncthreads();  // M, and x as the product takes it
       tmem_after_sync();
       // Y2 decayed, and the tokens' own x
-      dead |= !bar_wait(bar_y2, parity, p.wait_cycles);
+      dead = dead || !bar_wait(bar_y2, parity, p.wait_cycles);
       tmem_after_sync();
       if (more) fetch(kSpare ? b_at : c_at, kSpare ? p.b_token : p.c_token, t0 + step, c_to, state_vecs);
       const float by = ex2(sum_t) * state_scale;
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       }
     }
     // The state after the chunk.
-    dead |= !bar_wait(bar_s, parity, p.wait_cycles);
+    dead = dead || !bar_wait(bar_s, parity, p.wait_cycles);
     tmem_after_sync();
     if (!kStateOnly && more) {
       if (!kSpare) fetch(b_at, p.b_token, t0 + step, b_to, state_vecs);
@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       if (!kStateOnly && more) round_state(state);
     }
     if constexpr (!kStateOnly) {
-      dead |= !bar_wait(bar_y1, parity, p.wait_cycles);
+      dead = dead || !bar_wait(bar_y1, parity, p.wait_cycles);
       tmem_after_sync();
     }
     if constexpr (!kStateOnly) {
@@ -536,7 +536,11 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   }
   if (dead) *p.timeout = 1;
   tmem_before_sync();
-  __syncthreads();
+  if (__syncthreads_or(dead)) {  // products may still be at work: their end, however short the waits' limit is
+    if (issuer && elected()) products_done(bar_end);
+    bar_wait(bar_end, 0, kDefaultWaitCycles);
+    __syncthreads();
+  }
   tmem_after_sync();
   if (issuer) tmem_free(tmem, kColumns);
 }

@@ -293,6 +293,40 @@ def test_bad_slots_give_zeros_and_are_reported(ctx):
         assert k.kv_get_device_error(ctx) == 1
 
 
+@pytest.mark.parametrize("t,heads", [(100, 2), (3000, 2)])
+def test_wait_for_the_tensor_cores_runs_out_then_recovery(t, heads):
+    """Fault point "scan_wait": the end of the first chunk's products is not announced, so the wait for it (2e6 cycles
+    here) runs out.  The call returns, kv_get_device_error tells, and the next call on the context is right."""
+    k = kvx()
+    p, n = 128, 64
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, BF16)
+    batch, _ = batch_of([t], [0])
+    c2 = k.kv_ctx_create(0, wait_cycles=2_000_000)
+    try:
+        dev = [v.cuda() for v in (x, dt, A, b, c)]
+        outs = []
+        for fault in (True, False):
+            st = Slots(1, heads, p, n)
+            out = torch.zeros((t, heads, p), dtype=BF16, device="cuda")
+            ws = k.kv_state_scan_workspace(c2, batch, heads, p, n)
+            torch.cuda.synchronize()
+            if fault:
+                k.kv_fault_inject("scan_wait")
+            k.kv_state_scan(c2, st.slots, batch, dev[0], dev[1], dev[2], dev[3], dev[4], out, workspace=ws)
+            torch.cuda.synchronize()
+            if fault:
+                with pytest.raises(k.KvxError) as e:
+                    k.kv_get_device_error(c2)
+                assert e.value.status == k.KVX_ETIMEOUT
+            assert k.kv_get_device_error(c2) == -1
+            outs.append(out)
+        y, _, size, _ = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, True, st.state[0].double())
+        assert bool(((outs[1].cpu().double() - y).abs() <= refs.UNIT[BF16] * y.abs() + (3 * refs.UNIT[BF16] + 2.0 ** -13) * size + 1e-7).all())
+    finally:
+        k.kv_fault_inject(None)
+        k.kv_ctx_destroy(c2)
+
+
 def test_captured_step(ctx):
     """A captured convolution and scan of single tokens, replayed: the state moves on in its slot."""
     k = kvx()
