@@ -23,14 +23,18 @@ __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
 }
 
 // A thread keeps 8 neighbouring channels' window of kWidth inputs in registers and walks up to 32 rows of
-// one sequence, the next four rows' loads in flight behind the four it computes.  Bound by its bytes: a row in and a row out, the window's rows
-// read again at the head of a piece (3 of 32, from L2).  The piece at a sequence's head, which alone reads the slot,
-// also writes it, so a slot may be updated in place.
+// one sequence.  Bound by its bytes: a row in and a row out, the window's rows read again at the head of a piece (3
+// of 32, from L2).  Rows come through a ring in shared memory, four groups of four ahead, that a thread
+// fills and empties for itself, so there is no barrier (with the four next rows in registers, half as many bytes were in
+// flight, and 12k x 8192 took 86 us instead of 74).  The piece at a sequence's head, which alone reads the slot, also writes it, so
+// a slot may be updated in place.
+constexpr int kGroup = 4, kAhead = 4;
 template <class E, int kWidth>
-__global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constant__ ConvParams p) {
+__global__ void __launch_bounds__(kConvThreads, 4) conv_kernel(const __grid_constant__ ConvParams p) {
   wait_for_previous();
   constexpr int kPast = kWidth - 1;
   __shared__ int32_t buf[kConvThreads / 32 + 3];
+  __shared__ uint4 ring[kAhead + 1][kGroup][kConvThreads];
   const StateView& v = p.state;
   Piece found;
   if (!find_piece<kConvThreads>(v, blockIdx.x, kConvRows, buf, &found)) return;
@@ -47,7 +51,7 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
     for (int64_t t = begin; t < end; ++t) *out_row(t) = make_uint4(0, 0, 0, 0);
     return;
   }
-  float w[kWidth][8], bias[8] = {}, x[kPast + 4][8];  // the inputs before four rows, and theirs
+  float w[kWidth][8], bias[8] = {}, x[kPast + kGroup][8];  // the inputs before four rows, and theirs
   {
     float flat[8 * kWidth];
 #pragma unroll
@@ -87,35 +91,28 @@ __global__ void __launch_bounds__(kConvThreads) conv_kernel(const __grid_constan
   const uint8_t* from = p.x + (begin * p.x_stride + c) * 2;
   uint8_t* to = p.out + (begin * p.out_stride + c) * 2;
   const int64_t from_step = p.x_stride * 2, to_step = p.out_stride * 2;
-  int32_t left = (int32_t)(end - begin);
-  uint4 next[4];
-  if (left >= 4) {
+  const int32_t rows = (int32_t)(end - begin);
+  auto fetch = [&](int32_t r) {  // rows r .. r + 3
 #pragma unroll
-    for (int u = 0; u < 4; ++u) next[u] = __ldcs(reinterpret_cast<const uint4*>(from + u * from_step));
-  }
-  for (; left >= 4; left -= 4) {
+    for (int u = 0; u < kGroup; ++u)
+      if (r + u < rows) copy_async(smem_at(&ring[r / kGroup % (kAhead + 1)][u][threadIdx.x]), from + (r + u) * from_step);
+    commit_async();
+  };
 #pragma unroll
-    for (int u = 0; u < 4; ++u) unpack8<E>(next[u], x[kPast + u]);
-    from += 4 * from_step;
-    if (left >= 8) {
+  for (int g = 0; g < kAhead; ++g) fetch(g * kGroup);
+#pragma unroll 1
+  for (int32_t r = 0; r < rows; r += kGroup) {
+    fetch(r + kAhead * kGroup);
+    wait_async<kAhead>();
 #pragma unroll
-      for (int u = 0; u < 4; ++u) next[u] = __ldcs(reinterpret_cast<const uint4*>(from + u * from_step));
-    }
+    for (int u = 0; u < kGroup; ++u) unpack8<E>(ring[r / kGroup % (kAhead + 1)][u][threadIdx.x], x[kPast + u]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) row(u, reinterpret_cast<uint4*>(to + u * to_step));
-    to += 4 * to_step;
-#pragma unroll
-    for (int j = 0; j < kPast; ++j)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[j][k] = x[j + 4][k];
-  }
-  for (; left > 0; --left, from += from_step, to += to_step) {
-    unpack8<E>(*reinterpret_cast<const uint4*>(from), x[kPast]);
-    row(0, reinterpret_cast<uint4*>(to));
+    for (int u = 0; u < kGroup; ++u)
+      if (r + u < rows) row(u, reinterpret_cast<uint4*>(to + (r + u) * to_step));
 #pragma unroll
     for (int j = 0; j < kPast; ++j)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[j][k] = x[j + 1][k];
+      for (int k = 0; k < 8; ++k) x[j][k] = x[j + kGroup][k];
   }
   if (piece == 0) {
 #pragma unroll

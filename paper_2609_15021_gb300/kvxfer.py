@@ -717,9 +717,15 @@ def _cache_type(pool: KvPool, given) -> int:
     return _type_of(pool.layers[0].dtype if given is None else given)
 
 
-def _need(x, what: str, dtype, shape=None) -> None:
+_dtypes: dict = {}
+
+
+def _need(x, what: str, dtype: str, shape=None) -> None:
     """A tensor of `dtype` (and shape) whose innermost dimension is contiguous."""
-    if str(x.dtype) != "torch." + dtype:
+    if dtype not in _dtypes:
+        import torch
+        _dtypes[dtype] = getattr(torch, dtype)
+    if x.dtype is not _dtypes[dtype]:
         raise TypeError(f"{what} must be {dtype}, not {x.dtype}")
     if shape is not None and x.shape != shape:
         raise ValueError(f"{what} is {tuple(x.shape)}, not {tuple(shape)}")
