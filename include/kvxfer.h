@@ -727,6 +727,7 @@ kvx_status kv_append(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kv
  * A query that sees no key (a position before 0, an idle place) gets out = 0 and
  * lse = -inf.  A key whose table entry is out of range is left out and reported.
  * Positions count the cache's tokens: after an eviction they are its slots.
+ * num_seqs * new_tokens * q_heads may not pass 2^30 (KVX_ERANGE).
  */
 typedef struct {
   int32_t type;         /* of q and out: KVX_TYPE_BF16 or _FP16                 */
@@ -766,7 +767,8 @@ kvx_status kv_attend(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kv
  * their order to the pages that new_tables names; the old pages are not changed
  * (other sequences may share them) and are the caller's to free.  A sequence of
  * at most `budget` tokens keeps all.  The pages of new_tables must not be among
- * those of the block tables.
+ * those of the block tables.  Layers * sequences * heads * kept tokens / 32 may not
+ * pass 2^30 (KVX_ERANGE).
  */
 typedef struct {
   int32_t budget;          /* >= 1, sinks + recent <= budget                     */

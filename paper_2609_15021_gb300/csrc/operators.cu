@@ -14,6 +14,7 @@ using namespace kvx;
 namespace {
 
 constexpr int32_t kMaxSeqs = 65535, kMaxHeads = 4096;
+constexpr int64_t kMaxRows = 1ll << 30;
 
 kvx_status refuse(kvx_status st, const char* why) {
   set_error_text(why);
@@ -183,7 +184,7 @@ AttendSpace attend_space(const CtxView& ctx, const PagesView& v, const kvx_atten
 }
 
 // Checks of an attention that need no device.
-kvx_status check_attention(const kvx_pool* pool, const kvx_attention* a) {
+kvx_status check_attention(const kvx_pool* pool, const kvx_batch* batch, const kvx_attention* a) {
   if (!check_types(a->type, a->cache_type, pool->elem_bytes)) return refuse(KVX_EINVAL, "type, cache_type or elem_bytes");
   if (a->q_heads < 1 || a->q_heads > kMaxHeads || a->q_heads % pool->num_heads)
     return refuse(KVX_EINVAL, "q_heads is no multiple of the pool's heads");
@@ -191,6 +192,8 @@ kvx_status check_attention(const kvx_pool* pool, const kvx_attention* a) {
   if (!std::isfinite(a->scale) || !(a->softcap >= 0.f) || !std::isfinite(a->softcap) || !std::isfinite(a->k_scale) ||
       !std::isfinite(a->v_scale) || a->window < 0)
     return refuse(KVX_EINVAL, "scale, softcap or window");
+  if ((int64_t)batch->num_seqs * a->new_tokens * a->q_heads > kMaxRows)  // a CTA each where parts are joined
+    return refuse(KVX_ERANGE, "more than 2^30 rows of queries");
   return KVX_OK;
 }
 
@@ -249,7 +252,7 @@ kvx_status kv_attend_workspace(kvx_ctx* c, const kvx_pool* pool, const kvx_batch
     Geometry g;
     PagesView v;
     kvx_status st = view_pages(view_of(c), pool, batch, &g, &v);
-    if (st == KVX_OK) st = check_attention(pool, a);
+    if (st == KVX_OK) st = check_attention(pool, batch, a);
     if (st != KVX_OK) return st;
     *bytes = attend_space(view_of(c), v, a).bytes;
     return KVX_OK;
@@ -264,7 +267,7 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     AttendParams p;
     Geometry g;
     kvx_status st = view_pages(ctx, pool, batch, &g, &p.pages);
-    if (st == KVX_OK) st = check_attention(pool, a);
+    if (st == KVX_OK) st = check_attention(pool, batch, a);
     if (st != KVX_OK) return st;
     CurrentDevice guard(ctx.device);
     if (!guard.ok) return KVX_ECUDA;
@@ -354,6 +357,7 @@ kvx_status kv_evict(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, co
     if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
     const int64_t s = batch->num_seqs, h = pool->num_heads, layers = pool->num_layers;
     if (s == 0) return KVX_OK;
+    if (layers * s * h * ((most + 31) / 32) > kMaxRows) return refuse(KVX_ERANGE, "more than 2^30 groups of 32 kept tokens");
     DeviceMemory mem(ctx.device);
     for (int32_t l = 0; l < layers; ++l)
       if ((st = layer_of(mem, pool, l, g, &p.layer_base[l])) != KVX_OK) return st;

@@ -394,6 +394,36 @@ def test_refusals(ctx):
     assert k.kv_get_device_error(ctx) == -1
 
 
+def test_more_rows_than_a_launch_has(ctx):
+    """65,535 sequences of 64 tokens and 4,096 heads are 1.7e10 rows of queries: refused, not wrapped."""
+    k = kvx()
+    case = Case([3], heads=1)
+    many = k.KvBatch(torch.zeros((65535, 4), dtype=torch.int32, device="cuda"),
+                     torch.zeros(65535, dtype=torch.int32, device="cuda"))
+    with pytest.raises(k.KvxError) as e:
+        k.kv_attend_workspace(ctx, case.pool, many, k.KvAttention(4096, new_tokens=64))
+    assert e.value.status == k.KVX_ERANGE
+
+
+@pytest.mark.parametrize("byte", [0x00, 0xFF, 0x7F])
+def test_workspace_needs_no_initial_contents(ctx, byte):
+    k = kvx()
+    case = Case([500, 1, 0, 37], heads=2)
+    q = normal((4 * 3, 8, 64), BF16, 26).cuda()
+    att = k.KvAttention(8, new_tokens=3)
+
+    def once(fill):
+        ws = k.kv_attend_workspace(ctx, case.pool, case.batch, att, weights=True)
+        ws.view(torch.uint8).fill_(fill)
+        out, weights = torch.full_like(q, 7.0), torch.zeros((4, 2, 500), device="cuda")
+        lse = torch.zeros((12, 8), device="cuda")
+        k.kv_attend(ctx, case.pool, 0, case.batch, att, q, out, ws, lse=lse, weights=weights)
+        return out, weights, lse
+
+    for got, want in zip(once(byte), once(0x3C)):
+        assert same_bits(got, want)
+
+
 def test_nothing_to_do(ctx):
     k = kvx()
     case = Case([3], heads=1)
