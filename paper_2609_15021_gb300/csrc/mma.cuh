@@ -88,6 +88,24 @@ __device__ __forceinline__ uint32_t odd_carry(uint32_t v) {
   return (v & 0x7FFF7FFFu) + (std::is_same<C, Bf16>::value ? 0x00800080u : 0x04000400u);
 }
 __device__ __forceinline__ bool odd_carried(uint32_t carries) { return carries & 0x80008000u; }
+// Two fp32 operations in one instruction, each rounded as by itself.
+__device__ __forceinline__ uint64_t bits_of(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
+__device__ __forceinline__ float2 floats_of(uint64_t v) { return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
+  return floats_of(d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+  return floats_of(d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+  return floats_of(d);
+}
 // Whether one of two numbers is not finite.
 template <class C>
 __device__ __forceinline__ bool odd2(uint32_t v) {

@@ -13,20 +13,17 @@ namespace {
 constexpr int kConvThreads = 128, kConvRows = 32;
 
 template <class E>
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+__device__ __forceinline__ void unpack8(const uint4& v, float2 (&f)[4]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float2 x = unpack2<E>(w[i]);
-    f[2 * i] = x.x, f[2 * i + 1] = x.y;
-  }
+  for (int i = 0; i < 4; ++i) f[i] = unpack2<E>(w[i]);
 }
 
 // A thread keeps 8 neighbouring channels' window of kWidth inputs in registers and walks up to 32 rows of
 // one sequence.  Bound by its bytes: a row in and a row out, the window's rows read again at the head of a piece (3
 // of 32, from L2).  Rows come through a ring in shared memory, four groups of four ahead, that a thread
 // fills and empties for itself, so there is no barrier (with the four next rows in registers, half as many bytes were in
-// flight, and 12k x 8192 took 86 us instead of 74).  The piece at a sequence's head, which alone reads the slot, also writes it, so
+// flight, and 12k x 8192 took 86 us instead of 74).  Two channels go through one fp32 instruction (74 us became 72).  The piece at a sequence's head, which alone reads the slot, also writes it, so
 // a slot may be updated in place.
 constexpr int kGroup = 4, kAhead = 4;
 template <class E, int kWidth>
@@ -51,16 +48,17 @@ __global__ void __launch_bounds__(kConvThreads, 4) conv_kernel(const __grid_cons
     for (int64_t t = begin; t < end; ++t) *out_row(t) = make_uint4(0, 0, 0, 0);
     return;
   }
-  float w[kWidth][8], bias[8] = {}, x[kPast + kGroup][8];  // the inputs before four rows, and theirs
+  float2 w[kWidth][4], bias[4] = {}, x[kPast + kGroup][4];  // the inputs before four rows, and theirs
   {
-    float flat[8 * kWidth];
+    float2 flat[kWidth][4];
 #pragma unroll
     for (int i = 0; i < kWidth; ++i)
-      unpack8<E>(*reinterpret_cast<const uint4*>(p.weight + ((int64_t)c * kWidth + 8 * i) * 2), *reinterpret_cast<float(*)[8]>(flat + 8 * i));
+      unpack8<E>(*reinterpret_cast<const uint4*>(p.weight + ((int64_t)c * kWidth + 8 * i) * 2), flat[i]);
+    auto at = [&](int n) { return n & 1 ? flat[n / 8][n % 8 / 2].y : flat[n / 8][n % 8 / 2].x; };
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int j = 0; j < kWidth; ++j) w[j][k] = flat[k * kWidth + j];
+      for (int j = 0; j < kWidth; ++j) w[j][k] = make_float2(at(2 * k * kWidth + j), at((2 * k + 1) * kWidth + j));
   }
   if (p.bias) unpack8<E>(*reinterpret_cast<const uint4*>(p.bias + (int64_t)c * 2), bias);
   uint4 old[kPast];  // the inputs before the piece
@@ -75,18 +73,22 @@ __global__ void __launch_bounds__(kConvThreads, 4) conv_kernel(const __grid_cons
     unpack8<E>(old[j], x[j]);
   }
   auto row = [&](int u, uint4* to) {  // of the four
-    float y[8];
+    float2 y[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 4; ++k) {
       y[k] = bias[k];
 #pragma unroll
-      for (int j = 0; j < kWidth; ++j) y[k] += w[j][k] * x[u + j][k];
+      for (int j = 0; j < kWidth; ++j) y[k] = fma2(w[j][k], x[u + j][k], y[k]);
     }
     if (p.silu) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) y[k] *= rcp(1.f + ex2(-kLog2e * y[k]));
+      for (int k = 0; k < 4; ++k) {
+        const float2 e = mul2(y[k], make_float2(-kLog2e, -kLog2e));
+        const float2 one = add2(make_float2(ex2(e.x), ex2(e.y)), make_float2(1.f, 1.f));
+        y[k] = mul2(y[k], make_float2(rcp(one.x), rcp(one.y)));
+      }
     }
-    *to = make_uint4(pack2<E>(y[0], y[1]), pack2<E>(y[2], y[3]), pack2<E>(y[4], y[5]), pack2<E>(y[6], y[7]));
+    *to = make_uint4(pack2<E>(y[0].x, y[0].y), pack2<E>(y[1].x, y[1].y), pack2<E>(y[2].x, y[2].y), pack2<E>(y[3].x, y[3].y));
   };
   const uint8_t* from = p.x + (begin * p.x_stride + c) * 2;
   uint8_t* to = p.out + (begin * p.out_stride + c) * 2;
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(kConvThreads, 4) conv_kernel(const __grid_cons
 #pragma unroll
     for (int j = 0; j < kPast; ++j)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[j][k] = x[j + kGroup][k];
+      for (int k = 0; k < 4; ++k) x[j][k] = x[j + kGroup][k];
   }
   if (piece == 0) {
 #pragma unroll
