@@ -33,7 +33,12 @@
 namespace kvx {
 namespace {
 
-constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;  // and a warp more
+constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;  // of the elements
+// And a group of four warps more, of which one issues.  A thread has 168 registers at the launch, and these four warps
+// give up what the eight take (256 * 216 + 128 * 72 = 384 * 168), as spills are dear where shared memory leaves the L1
+// cache little: with one warp more and 168 registers for all, 24k tokens of fp16 took 242 us instead of 230.
+constexpr int kAllThreads = kThreads + 128, kLaunchRegs = 168, kRegs = 216, kIssuerRegs = 72;
+static_assert(kThreads * kRegs + 128 * kIssuerRegs <= kAllThreads * kLaunchRegs, "registers of a CTA");
 
 // Columns of tensor memory.
 constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
@@ -50,7 +55,7 @@ struct Weights {
 struct Shared {
   Weights weights;
   float largest[2][kWarps];
-  int32_t buf[kWarps + 4];
+  int32_t buf[kAllThreads / 32 + 3];
   uint32_t tmem;
   uint64_t bars[5];
 };
@@ -67,6 +72,10 @@ struct ScanShape {
   static constexpr int kSmem = kShared + 2048 + 1024;  // 1024: what aligns the panels to their swizzle
   static_assert(sizeof(Shared) <= 2048 && kSmem <= 232448, "shared memory of an SM");
 };
+
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 at2(const float* p) { return make_float2(p[0], p[1]); }
+__device__ __forceinline__ void put2(float* p, float2 v) { p[0] = v.x, p[1] = v.y; }
 
 // A barrier of the eight warps.
 __device__ __forceinline__ void sync_eight() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -85,7 +94,7 @@ __device__ __forceinline__ int range_of(float top) {
 }
 
 template <class E, int N, int kP, bool kStateOnly>
-__global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_constant__ ScanParams p) {
   using S = ScanShape<kP>;
   using T = typename E::T;
   constexpr bool kHalf = std::is_same<E, Fp16>::value;
@@ -104,11 +113,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   const int lane = threadIdx.x & 31, warp = __shfl_sync(~0u, threadIdx.x >> 5, 0);
   const int line = (warp & 3) * 32 + lane;  // of tensor memory: a token of G and Y, an element of state_dim of H
   const int side = warp >> 2;               // which half of the columns
-  const bool issuer = warp == kWarps;
   const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
   const int32_t h = blockIdx.y, group = h / p.heads_per_group;
   Piece found;
-  if (!find_piece<kThreads + 32>(v, piece, p.segment, sh.buf, &found)) {
+  if (!find_piece<kAllThreads>(v, piece, p.segment, sh.buf, &found)) {
     if (carried) wait_for_previous();  // no kernel may end before the one before it
     return;
   }
@@ -120,7 +128,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   if (!in || !keep) {
     if (carried) wait_for_previous();
     if (!kStateOnly)
-      for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kThreads + 32)
+      for (int64_t i = threadIdx.x; i < (end - begin) * (kP / 2); i += kAllThreads)
         *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.out) + (begin + i / (kP / 2)) * p.out_token + h * p.out_head + p0 +
                                      i % (kP / 2) * 2) = 0;
     return;
@@ -151,115 +159,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   };
   const std::integral_constant<int, N / 8> state_vecs;
   const std::integral_constant<int, kP / 8> slice_vecs;
-  // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
-  // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
-  const float A2 = p.A[h] * kLog2e, D = p.D ? p.D[h] : 0.f;
-  float d[4];
-  auto load_steps = [&](int64_t t0) {
-    T raw[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) raw[k] = t0 + 4 * lane + k < end ? dt_at[(t0 + 4 * lane + k) * p.dt_token] : E::down(0.f);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) d[k] = t0 + 4 * lane + k < end ? step_of(p, E::up(raw[k]), h) : 0.f;
-  };
-  auto weigh = [&](float after) {
-    float a[4], upto = 0.f, behind = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = d[k] * A2;
-    upto = behind = (a[0] + a[1]) + (a[2] + a[3]);
-    for (int m = 1; m < 32; m <<= 1) {
-      const float y = __shfl_up_sync(~0u, upto, m), z = __shfl_down_sync(~0u, behind, m);
-      if (lane >= m) upto += y;
-      if (lane + m < 32) behind += z;
-    }
-    float below = __shfl_up_sync(~0u, upto, 1), above = __shfl_down_sync(~0u, behind, 1);
-    if (lane == 0) below = 0.f;
-    if (lane == 31) above = 0.f, w.exponent = upto;
-    above += after;
-    float top = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      w.d[4 * lane + k] = d[k];
-      w.sum[4 * lane + k] = below += a[k];
-    }
-#pragma unroll
-    for (int k = 3; k >= 0; --k) {
-      const float weight = d[k] * ex2(above);
-      w.weight[4 * lane + k] = weight;
-      above += a[k];
-      top = fmaxf(top, fabsf(weight));
-    }
-    if (kHalf) {
-      for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-      if (lane == 0) w.shift = top > 0.f && top < INFINITY ? max(-60, min(60, -1 - ilogbf(top))) : 0;
-    }
-  };
-
   // ---- set-up: barriers, tensor memory, the first chunk's rows and weights
   const int64_t chunks = (end - begin + kChunk - 1) / kChunk;
   const int64_t step = kStateOnly ? -kChunk : kChunk;
   int64_t t0 = kStateOnly ? begin + (chunks - 1) * kChunk : begin;
-  const int64_t all = (int64_t)p.heads * p.head_dim * N;
-  const int64_t state_at = ((int64_t)h * p.head_dim + p0 + side * kCols) * N + line;  // + column * N
-  float state[kCols];
-#pragma unroll
-  for (int k = 0; k < kCols; ++k) state[k] = 0.f;
-  if (issuer) {
-    if (chunks > 0) load_steps(t0);
-    tmem_alloc(smem_at(&sh.tmem), kColumns);
-    if (lane == 0) {
-      for (uint64_t& bar : sh.bars) bar_init(smem_at(&bar));
-      fence_operands();
-    }
-    if (chunks > 0) weigh(0.f);
-  } else {
-    if (chunks > 0) {
-      fetch(b_at, p.b_token, t0, b_to, state_vecs);
-      fetch(x_at, p.x_token, t0, x_to, slice_vecs);
-      if (!kStateOnly) fetch(c_at, p.c_token, t0, c_to, state_vecs);
-    }
-    commit_async();
-    if (!kStateOnly) {
-      if (carried) wait_for_previous();
-      const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
-      if (line < N && (p.segment_states || !found.fresh)) {
-#pragma unroll
-        for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
-      }
-    }
-    if (N == 64)  // S's lanes beyond state_dim: their rows of B^T are zeros
-      for (int i = threadIdx.x; i < (kSpare && !kStateOnly ? 3 : 2) * kPanel / 16; i += kThreads)
-        *reinterpret_cast<uint4*>(smem + S::kB + (i / (kPanel / 16) * 2 + 1) * kPanel + i % (kPanel / 16) * 16) =
-            make_uint4(0, 0, 0, 0);
-  }
-  tmem_before_sync();
-  __syncthreads();
-  tmem_after_sync();
-  const uint32_t tmem = sh.tmem, my_lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-  bool dead = false;  // a wait ran out: the others are not waited for
-
-  // The state a segment starts from, and the one after every chunk, rounded to shared memory as Y2's right factor.
-  float state_scale = 1.f;  // fp16: what undoes the rounded state's scaling
-  auto round_state = [&](const float (&state)[kCols]) {
-    float scale = 1.f;
-    if constexpr (kHalf) {
-      float top = 0.f;
-#pragma unroll
-      for (int k = 0; k < kCols; ++k) top = fmaxf(top, fabsf(state[k]));
-      const int e = range_of(cta_max(top, sh.largest[0]));
-      scale = power_of_two(e), state_scale = power_of_two(-e);
-    }
-    if (line < N) {
-#pragma unroll
-      for (int k = 0; k < kCols; k += 8)
-        *reinterpret_cast<uint4*>(smem + kLast + panel_at(line, (side * kCols + k) / 8)) =
-            make_uint4(pack2<E>(state[k] * scale, state[k + 1] * scale), pack2<E>(state[k + 2] * scale, state[k + 3] * scale),
-                       pack2<E>(state[k + 4] * scale, state[k + 5] * scale), pack2<E>(state[k + 6] * scale, state[k + 7] * scale));
-    }
-    fence_operands();
-  };
-  if (!kStateOnly && !issuer && chunks > 0) round_state(state);
-
   float exponent = 0.f;  // of the decay over the segment's chunks so far
   auto turn = [&]() {    // the buffers' roles in the next chunk
     const uint32_t b_was = b_to, x_was = x_to;
@@ -270,17 +173,70 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       x_to = lo_to, lo_to = hi_to, hi_to = x_was;
     }
   };
-  for (int64_t n = 0; n < chunks; ++n, t0 += step) {
-    const bool more = n + 1 < chunks;
-    const uint32_t parity = n & 1;
-    wait_async<0>();
-    fence_operands();
+  if (warp >= kWarps) {
+    give_registers<kIssuerRegs>();
+    if (warp > kWarps) return;
+    // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
+    // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
+    const float A2 = p.A[h] * kLog2e;
+    float d[4];
+    auto load_steps = [&](int64_t t0) {
+      T raw[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) raw[k] = t0 + 4 * lane + k < end ? dt_at[(t0 + 4 * lane + k) * p.dt_token] : E::down(0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) d[k] = t0 + 4 * lane + k < end ? step_of(p, E::up(raw[k]), h) : 0.f;
+    };
+    auto weigh = [&](float after) {
+      float a[4], upto = 0.f, behind = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) a[k] = d[k] * A2;
+      upto = behind = (a[0] + a[1]) + (a[2] + a[3]);
+      for (int m = 1; m < 32; m <<= 1) {
+        const float y = __shfl_up_sync(~0u, upto, m), z = __shfl_down_sync(~0u, behind, m);
+        if (lane >= m) upto += y;
+        if (lane + m < 32) behind += z;
+      }
+      float below = __shfl_up_sync(~0u, upto, 1), above = __shfl_down_sync(~0u, behind, 1);
+      if (lane == 0) below = 0.f;
+      if (lane == 31) above = 0.f, w.exponent = upto;
+      above += after;
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        w.d[4 * lane + k] = d[k];
+        w.sum[4 * lane + k] = below += a[k];
+      }
+#pragma unroll
+      for (int k = 3; k >= 0; --k) {
+        const float weight = d[k] * ex2(above);
+        w.weight[4 * lane + k] = weight;
+        above += a[k];
+        top = fmaxf(top, fabsf(weight));
+      }
+      if (kHalf) {
+        for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
+        if (lane == 0) w.shift = top > 0.f && top < INFINITY ? max(-60, min(60, -1 - ilogbf(top))) : 0;
+      }
+    };
+
+    if (chunks > 0) load_steps(t0);
+    tmem_alloc(smem_at(&sh.tmem), kColumns);
+    if (lane == 0) {
+      for (uint64_t& bar : sh.bars) bar_init(smem_at(&bar));
+      fence_operands();
+    }
+    if (chunks > 0) weigh(0.f);
     tmem_before_sync();
-    if (__syncthreads_or(dead)) break;  // the chunk's rows, its weights and the rounded state are there
+    __syncthreads();
     tmem_after_sync();
-    const float chunk_exponent = w.exponent;
-    exponent += chunk_exponent;
-    if (issuer) {
+    const uint32_t tmem = sh.tmem;
+    for (int64_t n = 0; n < chunks; ++n, t0 += step) {
+      const bool more = n + 1 < chunks;
+      tmem_before_sync();
+      if (__syncthreads_or(0)) break;
+      tmem_after_sync();
+      exponent += w.exponent;
       if (!kStateOnly && elected()) {
 #pragma unroll
         for (int k = 0; k < N / 16; ++k)
@@ -324,8 +280,86 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
       __syncwarp();
       if (more) weigh(kStateOnly ? exponent : 0.f);  // the others have read this chunk's
       turn();
-      continue;
     }
+    tmem_before_sync();
+    if (__syncthreads_or(0)) {  // a wait ran out, and products may still be at work
+      if (elected()) products_done(bar_end);
+      __syncwarp();
+      bar_wait(bar_end, 0, kDefaultWaitCycles);
+      __syncthreads();
+    }
+    tmem_after_sync();
+    tmem_free(tmem, kColumns);
+    return;
+  }
+  take_registers<kRegs>();
+  const float D = p.D ? p.D[h] : 0.f;
+  const int64_t all = (int64_t)p.heads * p.head_dim * N;
+  const int64_t state_at = ((int64_t)h * p.head_dim + p0 + side * kCols) * N + line;  // + column * N
+  float state[kCols];
+#pragma unroll
+  for (int k = 0; k < kCols; ++k) state[k] = 0.f;
+  if (chunks > 0) {
+    fetch(b_at, p.b_token, t0, b_to, state_vecs);
+    fetch(x_at, p.x_token, t0, x_to, slice_vecs);
+    if (!kStateOnly) fetch(c_at, p.c_token, t0, c_to, state_vecs);
+  }
+  commit_async();
+  if (!kStateOnly) {
+    if (carried) wait_for_previous();
+    const float* from = p.segment_states ? p.segment_states + piece * all : reinterpret_cast<const float*>(in);
+    if (line < N && (p.segment_states || !found.fresh)) {
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) state[k] = from[state_at + k * N];
+    }
+  }
+  if (N == 64)  // S's lanes beyond state_dim: their rows of B^T are zeros
+    for (int i = threadIdx.x; i < (kSpare && !kStateOnly ? 3 : 2) * kPanel / 16; i += kThreads)
+      *reinterpret_cast<uint4*>(smem + S::kB + (i / (kPanel / 16) * 2 + 1) * kPanel + i % (kPanel / 16) * 16) =
+          make_uint4(0, 0, 0, 0);
+  tmem_before_sync();
+  __syncthreads();
+  tmem_after_sync();
+  const uint32_t tmem = sh.tmem, my_lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+  bool dead = false;  // a wait ran out: the others are not waited for
+
+  // The state a segment starts from, and the one after every chunk, rounded to shared memory as Y2's right factor.
+  float state_scale = 1.f;  // fp16: what undoes the rounded state's scaling
+  auto round_state = [&](const float (&state)[kCols]) {
+    float scale = 1.f;
+    if constexpr (kHalf) {
+      float top = 0.f;
+#pragma unroll
+      for (int k = 0; k < kCols; ++k) top = fmaxf(top, fabsf(state[k]));
+      const int e = range_of(cta_max(top, sh.largest[0]));
+      scale = power_of_two(e), state_scale = power_of_two(-e);
+    }
+    if (line < N) {
+#pragma unroll
+      for (int k = 0; k < kCols; k += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = kHalf ? mul2(at2(state + k + 2 * j), twice(scale)) : at2(state + k + 2 * j);
+          w[j] = pack2<E>(v.x, v.y);
+        }
+        *reinterpret_cast<uint4*>(smem + kLast + panel_at(line, (side * kCols + k) / 8)) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    fence_operands();
+  };
+  if (!kStateOnly && chunks > 0) round_state(state);
+
+  for (int64_t n = 0; n < chunks; ++n, t0 += step) {
+    const bool more = n + 1 < chunks;
+    const uint32_t parity = n & 1;
+    wait_async<0>();
+    fence_operands();
+    tmem_before_sync();
+    if (__syncthreads_or(dead)) break;  // the chunk's rows, its weights and the rounded state are there
+    tmem_after_sync();
+    const float chunk_exponent = w.exponent;
+    exponent += chunk_exponent;
     if (more && kSpare) {
       fetch(kStateOnly ? b_at : c_at, kStateOnly ? p.b_token : p.c_token, t0 + step, spare_to, state_vecs);
       if (kStateOnly) fetch(x_at, p.x_token, t0 + step, next_to, slice_vecs);
@@ -363,15 +397,13 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         uint32_t hi[4], lo[4], rest[4] = {};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          float2 f = unpack2<E>(u[j]);
-          f.x *= weight, f.y *= weight;
+          float2 f = mul2(unpack2<E>(u[j]), twice(weight));
           hi[j] = pack2<E>(f.x, f.y);
-          const float2 r = unpack2<E>(hi[j]);
-          f.x -= r.x, f.y -= r.y;
+          f = fma2(unpack2<E>(hi[j]), twice(-1.f), f);
           lo[j] = pack2<E>(f.x, f.y);
           if constexpr (kThree) {
-            const float2 q = unpack2<E>(lo[j]);
-            rest[j] = pack2<E>(f.x - q.x, f.y - q.y);
+            f = fma2(unpack2<E>(lo[j]), twice(-1.f), f);
+            rest[j] = pack2<E>(f.x, f.y);
           }
         }
         if (odd) {  // inf - inf: an infinite x has no other part
@@ -389,8 +421,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
     }
     fence_operands();
 
-    const int64_t token = t0 + line;
-    float y[kCols];
+      float y[kCols];
     // G's columns, 16 of every 32 a side: read by all before M takes their place
     float g[4][16];
     if constexpr (!kStateOnly) {
@@ -414,9 +445,9 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
           for (int j = 0; j < 8; ++j) {
             const int u = c0 + 2 * j;
             const float2 su = *reinterpret_cast<const float2*>(&w.sum[u]), du = *reinterpret_cast<const float2*>(&w.d[u]);
-            const float a = u <= line ? g[q][2 * j] * (ex2(sum_t - su.x) * du.x) : 0.f;
-            const float b = u + 1 <= line ? g[q][2 * j + 1] * (ex2(sum_t - su.y) * du.y) : 0.f;
-            m[j] = pack2<E>(a, b);
+            const float2 e = fma2(su, twice(-1.f), twice(sum_t));
+            const float2 by = mul2(make_float2(ex2(e.x), ex2(e.y)), du), all = mul2(make_float2(g[q][2 * j], g[q][2 * j + 1]), by);
+            m[j] = pack2<E>(u <= line ? all.x : 0.f, u + 1 <= line ? all.y : 0.f);
           }
         } else {
 #pragma unroll
@@ -447,7 +478,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         tmem_load16(r, my_lanes + kY2 + side * kCols + k);
         tmem_wait_loads();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[k + j] = r[j] * by;
+        for (int j = 0; j < 16; j += 2) put2(y + k + j, mul2(at2(r + j), twice(by)));
       }
       if (p.D) {
 #pragma unroll
@@ -456,8 +487,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
           const uint32_t u[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 f = unpack2<E>(u[j]);
-            y[k + 2 * j] += D * f.x, y[k + 2 * j + 1] += D * f.y;
+            put2(y + k + 2 * j, fma2(unpack2<E>(u[j]), twice(D), at2(y + k + 2 * j)));
           }
         }
       }
@@ -478,7 +508,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         tmem_load16(r, my_lanes + kState + side * kCols + k);
         tmem_wait_loads();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) state[k + j] = state[k + j] * decay + r[j] * back;
+        for (int j = 0; j < 16; j += 2) {
+          const float2 before = at2(state + k + j), made = at2(r + j);
+          put2(state + k + j, kHalf ? fma2(made, twice(back), mul2(before, twice(decay))) : fma2(before, twice(decay), made));
+        }
       }
       if (!kStateOnly && more) round_state(state);
     }
@@ -493,7 +526,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
         tmem_load16(r, my_lanes + kY1 + side * kCols + k);
         tmem_wait_loads();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[k + j] += r[j];
+        for (int j = 0; j < 16; j += 2) put2(y + k + j, add2(at2(y + k + j), at2(r + j)));
       }
       if (odd) {
         for (int u = 0; u < kChunk && t0 + u < end; ++u) {
@@ -528,7 +561,7 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   }
   if (kStateOnly || seg + 1 == segs) {
     float* to = kStateOnly ? p.segment_states + piece * all : reinterpret_cast<float*>(keep);
-    if (!issuer && line < N) {
+    if (line < N) {
 #pragma unroll
       for (int k = 0; k < kCols; ++k) to[state_at + k * N] = state[k];
     }
@@ -537,12 +570,10 @@ __global__ void __launch_bounds__(kThreads + 32, 1) chunk_kernel(const __grid_co
   if (dead) *p.timeout = 1;
   tmem_before_sync();
   if (__syncthreads_or(dead)) {  // products may still be at work: their end, however short the waits' limit is
-    if (issuer && elected()) products_done(bar_end);
     bar_wait(bar_end, 0, kDefaultWaitCycles);
     __syncthreads();
   }
   tmem_after_sync();
-  if (issuer) tmem_free(tmem, kColumns);
 }
 
 // Carries the states through a sequence's segments, four elements a thread: where the first pass left what a
@@ -600,12 +631,12 @@ cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
   const dim3 grid((unsigned)(pieces * (p.head_dim / kP)), p.heads);
   constexpr int kSmem = ScanShape<kP>::kSmem;
   if (p.segment_states) {
-    cudaError_t e = launch_after(chunk_kernel<E, N, kP, true>, grid, kThreads + 32, kSmem, s, p);
+    cudaError_t e = launch_after(chunk_kernel<E, N, kP, true>, grid, kAllThreads, kSmem, s, p);
     if (e != cudaSuccess) return e;
     const dim3 all((p.head_dim * N / 4 + 255) / 256, p.heads, p.state.num_seqs);
     if ((e = launch_after(carry_kernel, all, 256, 0, s, p)) != cudaSuccess) return e;
   }
-  return launch_after(chunk_kernel<E, N, kP, false>, grid, kThreads + 32, kSmem, s, p);
+  return launch_after(chunk_kernel<E, N, kP, false>, grid, kAllThreads, kSmem, s, p);
 }
 
 template <class E>
@@ -614,13 +645,22 @@ cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
   return p.state_dim == 64 ? chunks<E, 64, 64>(p, s) : chunks<E, 128, 64>(p, s);
 }
 
+template <class E, int N, int kP, bool kStateOnly>
+cudaError_t prepare() {
+  auto kernel = chunk_kernel<E, N, kP, kStateOnly>;
+  cudaFuncAttributes a;
+  const cudaError_t e = cudaFuncGetAttributes(&a, kernel);
+  if (e != cudaSuccess) return e;
+  if (a.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration;  // the eight warps would wait for registers
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ScanShape<kP>::kSmem);
+}
+
 template <class E, int N, int kP>
 cudaError_t prepare() {
-  const cudaError_t e = cudaFuncSetAttribute(chunk_kernel<E, N, kP, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             ScanShape<kP>::kSmem);
-  if (e != cudaSuccess) return e;
-  return cudaFuncSetAttribute(chunk_kernel<E, N, kP, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, ScanShape<kP>::kSmem);
+  const cudaError_t e = prepare<E, N, kP, true>();
+  return e == cudaSuccess ? prepare<E, N, kP, false>() : e;
 }
+
 template <class E>
 cudaError_t prepare() {
   cudaError_t e;
