@@ -102,8 +102,9 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
 template <class In, bool kFp8>
 cudaError_t append(const AppendParams& p, int num_sms, cudaStream_t s) {
   constexpr int kWarps = kAppendThreads / 32;
-  // a warp per token where that fills the GPU, four where it does not
-  if (p.tokens >= 16 * num_sms)
+  // a warp per token where that fills the GPU, four where it does not (rows of 4 x 256 to e4m3: 1024 tokens 3.6 us against
+  // 3.2, 2048 tokens 4.3 against 5.1)
+  if (p.tokens >= 10 * num_sms)
     return launch_after(append_kernel<In, kFp8, 1>, dim3((unsigned)((p.tokens + kWarps - 1) / kWarps)), kAppendThreads, 0, s, p);
   return launch_after(append_kernel<In, kFp8, 4>, dim3((unsigned)((p.tokens * 4 + kWarps - 1) / kWarps)), kAppendThreads, 0, s, p);
 }
