@@ -851,10 +851,10 @@ typedef struct {
   int64_t x_token_stride, x_head_stride, dt_token_stride, b_token_stride, b_group_stride, c_token_stride,
       c_group_stride, out_token_stride, out_head_stride;
 } kvx_scan;
-/* Prompts (starts given, 16 tokens a sequence or more on average, head_dim a
-   multiple of 64, state_dim 64 or 128) are scanned in matrix form on the tensor
-   cores, where the products C.B, decayed and weighted, must stay within the
-   range of `type` (65504 in fp16); others token by token.  A wait for the tensor
+/* Sequences of more than 16 tokens, and shorter ones where they are few (starts
+   given, head_dim a multiple of 64, state_dim 64 or 128), are scanned in matrix
+   form on the tensor cores, where the products C.B, decayed and weighted, must
+   stay within the range of `type` (65504 in fp16); others token by token.  A wait for the tensor
    cores that runs out (kvx_opts.wait_cycles) is reported as KVX_ETIMEOUT by
    kv_get_device_error, the output then being incomplete.
    Device workspace (0 for one token of every sequence); as kv_attend's.        */

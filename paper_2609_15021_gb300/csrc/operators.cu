@@ -458,7 +458,7 @@ kvx_status check_scan(const kvx_state_batch* b, const kvx_scan* s) {
 
 // kv_state_scan's workspace: the segments' states and exponents, where sequences are cut.
 struct ScanSpace {
-  int32_t segment;
+  int32_t segment, by_token;
   int64_t exponents, bytes;
 };
 ScanSpace scan_space(const CtxView& ctx, const kvx_state_batch* b, const kvx_scan* a) {
@@ -467,7 +467,8 @@ ScanSpace scan_space(const CtxView& ctx, const kvx_state_batch* b, const kvx_sca
   v.tokens = b->tokens;
   v.num_seqs = b->num_seqs;
   bool cut;
-  ScanSpace w = {scan_segment(v, a->heads, a->head_dim, a->state_dim, ctx.num_sms, &cut), 0, 0};
+  ScanSpace w = {};
+  w.segment = scan_segment(v, a->heads, a->head_dim, a->state_dim, ctx.num_sms, &cut, &w.by_token);
   if (cut) {
     const int64_t pieces = b->tokens / w.segment + b->num_seqs;
     w.exponents = pieces * a->heads * a->head_dim * a->state_dim * 4;
@@ -525,6 +526,7 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
       if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
     }
     p.segment = space.segment;
+    p.by_token = space.by_token;
     p.segment_states = space.bytes > 0 ? (float*)workspace : nullptr;
     p.segment_exponents = space.bytes > 0 ? (float*)((uint8_t*)workspace + space.exponents) : nullptr;
     p.x = (const uint8_t*)x;
@@ -552,6 +554,7 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
     p.wait_cycles = ctx.wait_cycles;
     p.timeout = ctx.timeout;
     p.stall = p.segment && fault_point("scan_wait");
-    return KVX_LAUNCHED(c, launch_scan(p, a->type, ctx.num_sms, stream), space.bytes > 0 ? 3 : 1);
+    return KVX_LAUNCHED(c, launch_scan(p, a->type, ctx.num_sms, stream),
+                        (space.by_token >= 0) + (space.segment ? space.bytes > 0 ? 3 : 1 : 0));
   });
 }

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
   const int32_t slices = p.head_dim / kP, piece = blockIdx.x / slices, p0 = (blockIdx.x - piece * slices) * kP;
   const int32_t h = blockIdx.y, group = h / p.heads_per_group;
   Piece found;
-  if (!find_piece<kAllThreads>(v, piece, p.segment, sh.buf, &found)) {
+  if (!find_piece<kAllThreads>(v, piece, p.segment, p.by_token, sh.buf, &found)) {
     if (carried) wait_for_previous();  // no kernel may end before the one before it
     return;
   }
@@ -589,7 +589,7 @@ __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ Scan
   for (int32_t i = threadIdx.x; i < s; i += 256) {
     int64_t a, b;
     rows_of(v, i, &a, &b);
-    mine += max(1, (int32_t)((b - a + p.segment - 1) / p.segment));
+    mine += pieces_of(a, b, p.segment, p.by_token);
   }
   for (int m = 16; m; m >>= 1) mine += __shfl_xor_sync(~0u, mine, m);
   if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&first_s, mine);
@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ Scan
   if (!in || !slot_of(v, v.slots_out, s)) return;
   int64_t a, b;
   rows_of(v, s, &a, &b);
-  const int32_t segs = max(1, (int32_t)((b - a + p.segment - 1) / p.segment));
+  const int32_t segs = pieces_of(a, b, p.segment, p.by_token);
   const int32_t i = blockIdx.x * 256 + threadIdx.x, vecs = p.head_dim * p.state_dim / 4;
   if (i >= vecs) return;
   float4 state = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -671,11 +671,24 @@ cudaError_t prepare() {
 
 }  // namespace
 
-int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut) {
+int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut,
+                     int32_t* by_token) {
   *cut = false;
+  *by_token = INT32_MAX;
   if (!v.starts || head_dim % 64 || (state_dim != 64 && state_dim != 128)) return 0;
-  if (v.tokens < 16ll * v.num_seqs) return 0;  // mostly short ones: a chunk would be mostly empty
-  const int64_t all = (v.tokens + kChunk - 1) / kChunk * heads * (head_dim / (head_dim % 128 ? 64 : 128));
+  // A CTA of the matrix form takes some 9 us however few tokens a sequence has, a token of the recurrence 0.45 (one
+  // sequence of 16 heads: 16 tokens 8.5 us against 9.8, 32 tokens 14.6 against 9.8).  A batch's short sequences are
+  // left to the recurrence where most are short or there are CTAs for more than a round of the SMs; that is a launch more
+  // and the time of its longest (32 sequences of unlike lengths: 8192 tokens 148 us instead of 174; 4 of them: 64
+  // tokens 19 instead of 10).
+  constexpr int32_t kShort = 16;
+  const int32_t slices = head_dim / (head_dim % 128 ? 64 : 128);
+  if (v.tokens <= kShort) return 0;
+  const bool both = v.tokens <= 8ll * v.num_seqs || (int64_t)v.num_seqs * heads * slices >= 2 * num_sms;
+  *by_token = v.num_seqs > 1 && both ? kShort : -1;
+  // two chunks in a row take less than the three launches below (15 us instead of 20), three as long
+  if (v.tokens <= 2 * kChunk) return 2 * kChunk;
+  const int64_t all = (v.tokens + kChunk - 1) / kChunk * heads * slices;
   const int64_t each = std::max<int64_t>(1, (all + num_sms - 1) / num_sms);
   *cut = v.tokens > each * kChunk;
   return (int32_t)(each * kChunk);

@@ -14,8 +14,8 @@ struct Piece {
   uint8_t* keep;
   bool fresh;
 };
-__device__ __forceinline__ int32_t pieces_of(int64_t first, int64_t last, int32_t length) {
-  return max(1, (int32_t)((last - first + length - 1) / length));
+__device__ __forceinline__ int32_t pieces_of(int64_t first, int64_t last, int32_t length, int32_t none_up_to) {
+  return last - first <= none_up_to ? 0 : max(1, (int32_t)((last - first + length - 1) / length));
 }
 __device__ __forceinline__ uint8_t* slot_at(const StateView& v, int32_t i, int32_t s) {
   if (i < 0 || i >= v.num_slots) {
@@ -25,11 +25,12 @@ __device__ __forceinline__ uint8_t* slot_at(const StateView& v, int32_t i, int32
   return v.base + (int64_t)i * v.slot_bytes + v.offset;
 }
 
-// The piece'th of all sequences' pieces of `length` rows (at least one a sequence), counted in their order:
-// False behind the last.  Up to 32 sequences are looked at by every warp for itself, with one round of loads;
+// The piece'th of all sequences' pieces of `length` rows (at least one of a sequence longer than none_up_to), counted
+// in their order: False behind the last.  Up to 32 sequences are looked at by every warp for itself, with one round of loads;
 // more by the whole CTA.  buf: a word a warp and three more.
 template <int kThreads>
-__device__ __forceinline__ bool find_piece(const StateView& v, int32_t piece, int32_t length, int32_t* buf, Piece* found) {
+__device__ __forceinline__ bool find_piece(const StateView& v, int32_t piece, int32_t length, int32_t none_up_to, int32_t* buf,
+                                           Piece* found) {
   if (v.starts && v.num_seqs <= 32) {
     const int lane = threadIdx.x & 31;
     const bool there = lane < v.num_seqs;
@@ -40,7 +41,7 @@ __device__ __forceinline__ bool find_piece(const StateView& v, int32_t piece, in
       from_slot = v.slots_in[lane], to_slot = v.slots_out[lane];
       if (v.fresh) fresh = v.fresh[lane];
     }
-    const int32_t mine = there ? pieces_of(first, last, length) : 0;
+    const int32_t mine = there ? pieces_of(first, last, length, none_up_to) : 0;
     int32_t upto = mine;
     for (int d = 1; d < 32; d <<= 1) {
       const int32_t y = __shfl_up_sync(~0u, upto, d);
@@ -77,7 +78,7 @@ __device__ __forceinline__ bool find_piece(const StateView& v, int32_t piece, in
     if (s < v.num_seqs) {
       int64_t first, last;
       rows_of(v, s, &first, &last);
-      mine = pieces_of(first, last, length);
+      mine = pieces_of(first, last, length, none_up_to);
     }
     int32_t upto = mine;
     for (int d = 1; d < 32; d <<= 1) {

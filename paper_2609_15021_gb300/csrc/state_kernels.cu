@@ -34,7 +34,7 @@ __global__ void __launch_bounds__(kConvThreads, 4) conv_kernel(const __grid_cons
   __shared__ uint4 ring[kAhead + 1][kGroup][kConvThreads];
   const StateView& v = p.state;
   Piece found;
-  if (!find_piece<kConvThreads>(v, blockIdx.x, kConvRows, buf, &found)) return;
+  if (!find_piece<kConvThreads>(v, blockIdx.x, kConvRows, -1, buf, &found)) return;
   const int32_t c = (blockIdx.y * kConvThreads + threadIdx.x) * 8;
   if (c >= p.channels) return;
   const int32_t piece = found.at;
@@ -140,7 +140,7 @@ cudaError_t conv(const ConvParams& p, cudaStream_t s) {
 
 // ---------------------------------------------------------------- scan, token by token
 
-// The recurrence as it stands, for single tokens and for what the matrix form below does not take.  Bound by the
+// The recurrence as it stands, for sequences of up to by_token tokens and for shapes that the matrix form does not take.  Bound by the
 // state's bytes, read and written once: a row of N elements lies over kLanes lanes, 16 bytes each
 // at least, and a lane has kRows rows, whose loads are all in flight at once; their sums y meet in one
 // reduction that halves the rows at every step.
@@ -157,6 +157,7 @@ __global__ void __launch_bounds__(128) scan_kernel(const __grid_constant__ ScanP
   uint8_t* keep = slot_of(v, v.slots_out, s);
   int64_t first, last;
   rows_of(v, s, &first, &last);
+  if (last - first > p.by_token) return;
   T* out = reinterpret_cast<T*>(p.out) + h * p.out_head;
   if (!in || !keep) {
     for (int64_t t = first; t < last; ++t)
@@ -265,8 +266,11 @@ cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s) {
 }
 
 cudaError_t launch_scan(const ScanParams& p, int type, int num_sms, cudaStream_t s) {
-  if (p.segment) return launch_scan_chunks(p, type, s);
-  return type == KVX_TYPE_BF16 ? scan<Bf16>(p, num_sms, s) : scan<Fp16>(p, num_sms, s);
+  if (p.by_token >= 0) {
+    const cudaError_t e = type == KVX_TYPE_BF16 ? scan<Bf16>(p, num_sms, s) : scan<Fp16>(p, num_sms, s);
+    if (e != cudaSuccess) return e;
+  }
+  return p.segment ? launch_scan_chunks(p, type, s) : cudaSuccess;
 }
 
 }  // namespace kvx

@@ -191,6 +191,21 @@ def test_scan_prompts_of_other_sizes(ctx, p, n):
     check_scan(ctx, [0, 1, 40, 150], 2, p, n, 1, BF16)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_scan_of_short_and_long_sequences_together(ctx, dtype):
+    """Around the 16 tokens up to which a sequence of a batch goes token by token, with more sequences than a warp has lanes."""
+    check_scan(ctx, [17, 16, 15, 0, 400, 1], 2, 128, 128, 1, dtype, fresh=[0, 1, 0, 0, 1, 0])
+    check_scan(ctx, [17, 0, 1, 16, 3, 1, 2, 2], 2, 128, 128, 1, dtype, fresh=[0, 1, 0, 0, 1, 0, 0, 0])
+    check_scan(ctx, [17, 16, 15, 0, 400, 1], 52, 128, 128, 4, dtype)
+    check_scan(ctx, [3, 16, 17, 0, 2] * 7 + [200, 1, 90], 2, 64, 64, 2, dtype, in_place=True)
+    check_scan(ctx, [16, 16, 16], 2, 128, 64, 1, dtype)
+
+
+@pytest.mark.parametrize("t", [1, 16, 17, 384, 385, 520])
+def test_scan_of_one_sequence(ctx, t):
+    check_scan(ctx, [t], 3, 128, 128, 1, BF16)
+
+
 def test_scan_long_prompt(ctx):
     check_scan(ctx, [1500, 700], 2, 128, 128, 1, BF16)
 
