@@ -1,4 +1,5 @@
-"""GB300-native paged-KV <-> pinned-host-chunk transfer (libkvxfer).
+"""GB300-native paged-KV <-> pinned-host-chunk transfer, and the attention, eviction and
+recurrent operators on the same pages and state slots (libkvxfer).
 
 The compute path is ``libkvxfer.so`` (hand-written CUDA for sm_103a behind a C
 ABI, ``include/kvxfer.h``); ``kvxfer`` is its ctypes binding.  Import the

