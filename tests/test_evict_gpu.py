@@ -145,6 +145,24 @@ def test_long_rows(ctx):
         assert torch.equal(data[tables[s][at // 64].long(), :, 0, at % 64], data[tables[2 + s][to // 64].long(), :, 0, to % 64])
 
 
+@pytest.mark.parametrize("width", [0, 1])  # rows of weights on 16 bytes, and off them
+@pytest.mark.parametrize("n", [4096, 12288, 12289, 32768, 32769])
+def test_rows_that_just_fill_a_tile(ctx, n, width):
+    k = kvx()
+    budget = 700
+    w = torch.randn((1, 1, 2, (n + 3) // 4 * 4 + width), generator=torch.Generator().manual_seed(8)).exp()
+    w[0, 0, 1] = torch.randint(0, 30, (w.shape[-1],), generator=torch.Generator().manual_seed(9)).float()
+    tables, blocks = refs.tables_for([n, budget], 64, 6)
+    layer = torch.zeros((blocks, 2, 2, 64, 16), dtype=torch.uint8, device="cuda")
+    pool = k.KvPool.from_tensors([layer], 2, 64)
+    batch = k.KvBatch(tables[:1].cuda(), torch.tensor([n], dtype=torch.int32, device="cuda"), max_length=n)
+    kept = torch.zeros((1, 1, 2, budget), dtype=torch.int32, device="cuda")
+    new_lengths = torch.zeros(1, dtype=torch.int32, device="cuda")
+    k.kv_evict(ctx, pool, batch, w.cuda(), budget, tables[1:].cuda(), kept, new_lengths, sinks=3, recent=5)
+    for h in range(2):
+        assert kept[0, 0, h].tolist() == refs.select(w[0, 0, h].tolist(), n, budget, 3, 5)
+
+
 def test_on_another_stream_after_the_attention_that_weighs(ctx):
     """Attention on a side stream accumulates the weights that the eviction behind it on that stream reads."""
     k = kvx()
