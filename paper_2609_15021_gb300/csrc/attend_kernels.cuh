@@ -38,7 +38,7 @@
 // Measured: bf16, sequences of 21k and 32.8k tokens, 8 heads x 128 with 8 query rows each, weights kept (220 MB of
 // K/V): 45 us; fp16, 45 sequences of up to 16k tokens, 8 heads x 96 with 2 rows, cap and slopes (270 MB): 60 us; both
 // at 63 % of the DRAM's rate, as they wait for their first rows and for the last CTA.  e4m3, four sequences of 99k to 127k
-// tokens, 4 heads x 256 with 24 rows (922 MB): 215 us, 4.3 TB/s: 24 x 256 sums are 192 registers a thread, so there
+// tokens, 4 heads x 256 with 24 rows (922 MB): 209 us, 4.4 TB/s: 24 x 256 sums are 192 registers a thread, so there
 // are two warps a scheduler and little to hide a step's dependent products and conversions behind.
 #pragma once
 
@@ -308,9 +308,13 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         if (lane == 0) masks[warp][to] = mask;
         const uint32_t dst = ring_at + to * S::kStageBytes + at_lane_copy;
         if (mask == kAllKeys) {
+          uint32_t rows_at[S::kLoads];  // in front of the copies where a step has many instructions (211 us, 209.5 so)
+#pragma unroll
+          for (int k = 0; k < S::kLoads; ++k)
+            if (kWide) rows_at[k] = __shfl_sync(~0u, row, k * S::kRowsPerLoad + vec_row);
 #pragma unroll
           for (int k = 0; k < S::kLoads; ++k) {
-            const uint32_t r = __shfl_sync(~0u, row, k * S::kRowsPerLoad + vec_row);
+            const uint32_t r = kWide ? rows_at[k] : __shfl_sync(~0u, row, k * S::kRowsPerLoad + vec_row);
             copy_async(dst + k * S::kRowsPerLoad * S::kPitch, lane_k + (uint64_t)r * row_bytes, vec_bytes);
             copy_async(dst + k * S::kRowsPerLoad * S::kPitch + S::kHalfBytes, lane_v + (uint64_t)r * row_bytes, vec_bytes);
           }
@@ -330,6 +334,14 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
     uint2 ahead[S::kStages];
 #pragma unroll
     for (int k = 0; k < S::kStages; ++k) ahead[k] = look(i0 + warp + k * kWarps);
+
+    // The first rows are under way while long queries are made ready (24 rows x 256: 211 us instead of 217 over 922 MB), and
+    // asked for behind short ones, whose loads would wait for the tables (59.5 us instead of 59 over 270 MB).
+    auto start = [&]() {
+#pragma unroll
+      for (int k = 0; k < S::kStages; ++k) issue(i0 + warp + k * kWarps, ahead[k], k);
+    };
+    if (!S::kQueryInRegs) start();
 
     // What is known of the rows, and the queries as the products' right factor: row quad of a tile, dims
     // 2 sub, 2 sub + 1 and those 8 further on (4 sub .. 4 sub + 3 where the cache is widened).
@@ -389,8 +401,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < S::kStages; ++k) issue(i0 + warp + k * kWarps, ahead[k], k);
+    if (S::kQueryInRegs) start();
     uint2 next = look(i0 + warp + S::kStages * kWarps);
 
     float acc[kKs][kTiles][4];
