@@ -315,7 +315,8 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     p.q_heads = a->q_heads;
     p.group = a->q_heads / pool->num_heads;
     p.new_tokens = a->new_tokens;
-    p.window = a->window;
+    // one that reaches past every key is none; smaller ones leave the kernels' 32-bit positions room
+    p.window = a->window < p.pages.max_length ? a->window : 0;
     p.scale = a->scale ? a->scale : 1.f / std::sqrt((float)d);
     p.softcap = a->softcap;
     const bool e4m3 = a->cache_type == KVX_TYPE_E4M3;

@@ -124,6 +124,22 @@ def test_window(ctx, window, new):
     check_attend(ctx, case, normal((5 * new, 4, 64), BF16, 6), new, with_weights=True, window=window)
 
 
+@pytest.mark.parametrize("window", [261, 2 ** 30, 2 ** 31 - 4, 2 ** 31 - 1])
+def test_window_of_more_than_every_key(ctx, window):
+    """As no window at all, also where a sequence is shorter than its new tokens, and whatever the workspace holds."""
+    k = kvx()
+    case = Case([1, 2, 0, 5, 260], heads=2)
+    q = normal((20, 4, 64), BF16, 27)
+    att = k.KvAttention(4, new_tokens=4, window=window)
+    ws = k.kv_attend_workspace(ctx, case.pool, case.batch, att, weights=True)
+    ws.fill_(0x7F)
+    weights, plain = torch.zeros((5, 2, 260), device="cuda"), torch.zeros((5, 2, 260), device="cuda")
+    got = run_attend(ctx, case, q, 4, weights=weights, workspace=ws, window=window)
+    want = run_attend(ctx, case, q, 4, weights=plain)
+    assert all(same_bits(a, b) for a, b in zip(got + (weights,), want + (plain,)))
+    check_attend(ctx, case, q, 4, with_weights=True, window=window)
+
+
 @pytest.mark.parametrize("softcap,slopes,scale", [(30.0, False, None), (5.0, False, 1.5), (0.0, True, None), (20.0, True, 0.3)])
 def test_cap_bias_and_scale(ctx, softcap, slopes, scale):
     case = Case([1, 90, 513], heads=2, dim=128)
