@@ -809,7 +809,9 @@ typedef struct {
                                slot; another sequence's is a caller error)        */
   const int32_t* fresh;     /* device [num_seqs], nonzero: begin from zeros; or NULL */
   const int32_t* starts;    /* device [num_seqs + 1]: rows [starts[s], starts[s+1])
-                               are sequence s's, or NULL: row s                   */
+                               are sequence s's, or NULL: row s.  Ascending, from
+                               0 to tokens: a pair that is not is cut to the rows
+                               there are and reported as such a slot is           */
   int64_t tokens;           /* rows; num_seqs without starts                     */
 } kvx_state_batch;
 

@@ -471,7 +471,7 @@ ScanSpace scan_space(const CtxView& ctx, const kvx_state_batch* b, const kvx_sca
   ScanSpace w = {};
   w.segment = scan_segment(v, a->heads, a->head_dim, a->state_dim, ctx.num_sms, &cut, &w.by_token);
   if (cut) {
-    const int64_t pieces = b->tokens / w.segment + b->num_seqs;
+    const int64_t pieces = scan_pieces(v, w.segment);
     w.exponents = pieces * a->heads * a->head_dim * a->state_dim * 4;
     w.bytes = w.exponents + pieces * a->heads * 4;
   }

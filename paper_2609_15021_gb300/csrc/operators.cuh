@@ -137,6 +137,8 @@ struct ScanParams {
   int* timeout;              // set when one ran out
   bool stall;                // fault point "scan_wait": the first chunk's products are not announced
 };
+// Pieces that the workspace has room for: as many as sequences whose rows do not overlap can have.
+__host__ __device__ inline int64_t scan_pieces(const StateView& v, int32_t segment) { return v.tokens / segment + v.num_seqs; }
 // The segment of the matrix form for a batch, 0 where it is not used; *cut: whether a sequence may have several;
 // *by_token: up to how many tokens a sequence does not take it.
 int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut,
@@ -234,15 +236,17 @@ __device__ __forceinline__ uint8_t* slot_of(const StateView& v, const int32_t* s
   return v.base + (int64_t)i * v.slot_bytes + v.offset;
 }
 
-// Rows of sequence s, cut to the rows there are.
+// Rows of sequence s, cut to the rows there are (a pair of starts that does not ascend within them is reported).
 __device__ __forceinline__ void rows_of(const StateView& v, int32_t s, int64_t* first, int64_t* last) {
   if (!v.starts) {
     *first = s;
     *last = s + 1;
     return;
   }
-  *first = min((int64_t)max(v.starts[s], 0), v.tokens);
-  *last = max(*first, min((int64_t)v.starts[s + 1], v.tokens));
+  const int32_t from = v.starts[s], to = v.starts[s + 1];
+  if (from < 0 || to < from || to > v.tokens) atomicMin(v.err, (long long)s);
+  *first = min((int64_t)max(from, 0), v.tokens);
+  *last = max(*first, min((int64_t)to, v.tokens));
 }
 
 }  // namespace

@@ -308,6 +308,53 @@ def test_bad_slots_give_zeros_and_are_reported(ctx):
         assert k.kv_get_device_error(ctx) == 1
 
 
+@pytest.mark.parametrize("starts", [[0, 3000, 0, 3000], [3000, 0, 3000, 0, 3000], [0, 3000] * 20])
+def test_starts_that_do_not_ascend_stay_within_the_workspace(ctx, starts):
+    """Rows that overlap make more segments than the workspace holds: nothing behind it is written, and the first
+    sequence whose starts descend is reported."""
+    k = kvx()
+    t, heads, p, n = 3000, 2, 128, 128
+    s = len(starts) - 1
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, BF16)
+    st = Slots(s, heads, p, n)
+    batch = k.StateBatch(ints(list(range(s))), starts=ints(starts), tokens=t)
+    need = k.kv_state_scan_workspace(ctx, batch, heads, p, n).numel()
+    room = torch.full((need + s * 24 * heads * p * n * 4,), 0xA5, dtype=torch.uint8, device="cuda")  # as many as overlapping rows make
+    out = torch.empty((t, heads, p), dtype=BF16, device="cuda")
+    k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out, workspace=room[:need])
+    torch.cuda.synchronize()
+    assert bool((room[need:] == 0xA5).all())
+    assert k.kv_get_device_error(ctx) == next(i for i in range(s) if starts[i + 1] < starts[i])
+    k.kv_state_conv(ctx, st.slots, batch, normal((t, 8), BF16, 8).cuda(), normal((8, 4), BF16, 9).cuda(),
+                    torch.empty((t, 8), dtype=BF16, device="cuda"))
+    torch.cuda.synchronize()
+    assert k.kv_get_device_error(ctx) == next(i for i in range(s) if starts[i + 1] < starts[i])
+
+
+@pytest.mark.parametrize("t", [10, 300, 3000])
+def test_starts_past_the_rows_are_cut_and_reported(ctx, t):
+    k = kvx()
+    heads, p, n = 2, 64, 64
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, BF16)
+    dev = [v.cuda() for v in (x, dt, A, b, c)]
+    xc, w = normal((t, 8), BF16, 8).cuda(), normal((8, 4), BF16, 9).cuda()
+    got = []
+    for starts, bad in (([0, 7, t], -1), ([0, 7, t + 500], 1), ([-3, 7, 2 ** 31 - 1], 0)):
+        st = Slots(2, heads, p, n)
+        batch = k.StateBatch(ints([0, 1]), starts=ints(starts), tokens=t)
+        out, cv = torch.zeros((t, heads, p), dtype=BF16, device="cuda"), torch.zeros((t, 8), dtype=BF16, device="cuda")
+        k.kv_state_scan(ctx, st.slots, batch, dev[0], dev[1], dev[2], dev[3], dev[4], out,
+                        workspace=k.kv_state_scan_workspace(ctx, batch, heads, p, n))
+        torch.cuda.synchronize()
+        assert k.kv_get_device_error(ctx) == bad
+        k.kv_state_conv(ctx, st.slots, batch, xc, w, cv)
+        torch.cuda.synchronize()
+        assert k.kv_get_device_error(ctx) == bad
+        got.append((out, cv, st.dev))
+    for g in got[1:]:
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(g, got[0]))
+
+
 @pytest.mark.parametrize("t,heads", [(100, 2), (3000, 2)])
 def test_wait_for_the_tensor_cores_runs_out_then_recovery(t, heads):
     """Fault point "scan_wait": the end of the first chunk's products is not announced, so the wait for it (2e6 cycles
