@@ -111,8 +111,14 @@ kvx_status view_pages(const CtxView& ctx, const kvx_pool* pool, const kvx_batch*
   return KVX_OK;
 }
 
+kvx_status check_tables(DeviceMemory& mem, const int32_t* p, int64_t n, int64_t stride, int64_t len, const char* what) {
+  int64_t bytes;
+  if (!extent(n, n > 1 ? stride : 0, 1, 0, len, 4, &bytes)) return refuse(KVX_EINVAL, what);
+  return check_words(mem, p, bytes / 4, what);
+}
+
 kvx_status check_batch_memory(DeviceMemory& mem, const kvx_batch* b) {
-  kvx_status st = check_words(mem, b->block_tables, (b->num_seqs - 1) * b->table_stride + b->table_len, "block_tables");
+  kvx_status st = check_tables(mem, b->block_tables, b->num_seqs, b->table_stride, b->table_len, "block_tables");
   return st != KVX_OK ? st : check_words(mem, b->lengths, b->num_seqs, "lengths");
 }
 
@@ -363,7 +369,7 @@ kvx_status kv_evict(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, co
     for (int32_t l = 0; l < layers; ++l)
       if ((st = layer_of(mem, pool, l, g, &p.layer_base[l])) != KVX_OK) return st;
     if ((st = check_batch_memory(mem, batch)) != KVX_OK) return st;
-    if ((st = check_words(mem, e->new_tables, (s - 1) * e->new_table_stride + e->new_table_len, "new_tables")) != KVX_OK ||
+    if ((st = check_tables(mem, e->new_tables, s, e->new_table_stride, e->new_table_len, "new_tables")) != KVX_OK ||
         (st = check_words(mem, e->kept, layers * s * h * e->budget, "kept")) != KVX_OK ||
         (st = check_words(mem, e->new_lengths, s, "new_lengths")) != KVX_OK)
       return st;

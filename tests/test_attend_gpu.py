@@ -410,6 +410,24 @@ def test_refusals(ctx):
     assert k.kv_get_device_error(ctx) == -1
 
 
+@pytest.mark.parametrize("stride", [2 ** 60, 2 ** 61, 2 ** 62, 2 ** 63 - 1])
+def test_table_strides_beyond_64_bits_of_bytes(ctx, stride):
+    """Their products with the sequences must not wrap into a small extent."""
+    k = kvx()
+    case = Case([20, 3, 1, 0, 5], heads=2)
+    case.batch._c.table_stride = stride
+    q = normal((5, 4, 64), BF16, 25).cuda()
+    out, ws = torch.full_like(q, 7.0), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    with pytest.raises(k.KvxError) as e:
+        k.kv_attend(ctx, case.pool, 0, case.batch, k.KvAttention(4), q, out, ws)
+    assert e.value.status == k.KVX_EINVAL
+    with pytest.raises(k.KvxError) as e:
+        k.kv_append(ctx, case.pool, 0, case.batch, q[:, :2], q[:, 2:])
+    assert e.value.status == k.KVX_EINVAL
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all()) and same_bits(case.dev[0], case.pages.data[0])
+
+
 def test_more_rows_than_a_launch_has(ctx):
     """65,535 sequences of 64 tokens and 4,096 heads are 1.7e10 rows of queries: refused, not wrapped."""
     k = kvx()

@@ -208,6 +208,28 @@ def test_missing_pages(ctx):
     assert torch.equal(bits(dev[0]), bits(before))
 
 
+@pytest.mark.parametrize("stride", [2 ** 60, 2 ** 61, 2 ** 62, 2 ** 63 - 1])
+@pytest.mark.parametrize("which", ["block_tables", "new_tables"])
+def test_table_strides_beyond_64_bits_of_bytes(ctx, stride, which):
+    """Their products with the sequences must not wrap into a small extent."""
+    import ctypes
+    k = kvx()
+    lengths = [40, 9, 1, 3, 20]
+    pages, dev, pool, old, new = make(lengths, 8)
+    batch = k.KvBatch(old.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda"), max_length=40)
+    w, t = torch.zeros((2, 5, 2, 40), device="cuda"), new.cuda()
+    kept, out = torch.full((2, 5, 2, 8), 77, dtype=torch.int32, device="cuda"), torch.full((5,), 77, dtype=torch.int32, device="cuda")
+    e = k.kvx_eviction(8, 0, 0, w.data_ptr(), *w.stride()[:3], t.data_ptr(), t.stride(0), t.shape[1], kept.data_ptr(), out.data_ptr())
+    if which == "block_tables":
+        batch._c.table_stride = stride
+    else:
+        e.new_table_stride = stride
+    status = k._lib.kv_evict(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(e), torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert status == k.KVX_EINVAL
+    assert bool((kept == 77).all()) and bool((out == 77).all())
+
+
 def test_refusals(ctx):
     k = kvx()
     pages, dev, pool, old, new = make([40, 9], 8)
