@@ -632,7 +632,7 @@ const char* kv_last_error_message(void);
  * (those whose warps take their work from a queue: large kv_store / kv_load
  * launches over the host link), "memcpy"
  * (staged-mode copies), "event" (the staged pipeline's ordering event
- * recorded on the caller's stream), "host_alloc" (kv_host_alloc).  Four more
+ * recorded on the caller's stream), "host_alloc" (kv_host_alloc).  Five more
  * points fail differently.  "chunk_map": the (after_calls + 1)-th next
  * kv_store_noalloc whose chunks are mapped takes them as not mapped, and
  * packs and copies.  "tma_wait": the (after_calls + 1)-th next launch
@@ -643,7 +643,10 @@ const char* kv_last_error_message(void);
  * hangs.  "scan_wait": the (after_calls + 1)-th next kv_state_scan in matrix
  * form does not announce the end of its first chunk's products, so the waits for
  * it run out: the call's output is incomplete and kv_get_device_error returns
- * KVX_ETIMEOUT.  "tier_exit" ends the process (_exit(3)) inside
+ * KVX_ETIMEOUT.  "scan_setup": the (after_calls + 1)-th next kv_ctx_create makes
+ * a context without the scan's matrix form, as where its kernels were compiled
+ * for fewer registers than it needs: kv_state_scan then goes token by token.
+ * "tier_exit" ends the process (_exit(3)) inside
  * kv_tier_reserve, while it holds a shared tier's table lock, right after it
  * has taken a slot for the new key; it tests how the processes left recover
  * the tier from a replica that died mid-update.  One point is armed at a

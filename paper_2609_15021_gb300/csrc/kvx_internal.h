@@ -146,7 +146,9 @@ cudaError_t launch_move_tma(int dir, int layout, const MoveParams& p, int grid, 
 cudaError_t prepare_tma_kernels();
 // Shared-memory limits of the attention kernels (attend_kernels.cu), likewise.
 cudaError_t prepare_attend_kernels();
-cudaError_t prepare_state_kernels();  // and the scan's (scan_kernels.cu)
+// And the scan's (scan_kernels.cu).  *matrix: whether they were compiled for as many registers as the matrix form's split
+// of them takes; a context without them scans token by token.
+cudaError_t prepare_state_kernels(bool* matrix);
 // Tensor-map variant for HND pools: one TMA box per full page half.
 constexpr int kTensorMapBytes = 128;
 // Encodes one tensor map per layer of P (kTensorMapBytes each) into `out`;
@@ -190,6 +192,7 @@ void record_cuda_error(int e, const char* call, int line);
 // What the operators' translation unit (operators.cu) uses of a context.
 struct CtxView {
   int device, num_sms;
+  bool scan_matrix;       // the scan's matrix form may be used
   long long* err;         // device error word: lowest bad logical block (or sequence)
   int* timeout;           // device flag: a bounded wait inside a kernel ran out
   long long wait_cycles;  // and its limit

@@ -127,6 +127,7 @@ struct kvx_ctx {
   int num_sms = 1;
   int move_occ[2] = {1, 1};  // CTAs per SM of the launches that cross the host link
   int seg_occ = 1;
+  bool scan_matrix = false;
   int link_ctas = 1;  // default CTA cap of launches that cross the host link
   cudaStream_t s_kern = nullptr;  // pack / unpack kernels
   cudaStream_t s_copy = nullptr;  // host-link copies of the staged mode
@@ -782,7 +783,7 @@ void push_job(MoveParams* p, uint8_t* chunk_side, int64_t first_page, int32_t to
 int64_t chunk_bytes(const kvx_pool* P, const Geometry& g, int64_t tokens) { return chunk_bytes_of(P, g, tokens); }
 
 CtxView view_of(const kvx_ctx* ctx) {
-  return {ctx->device, ctx->num_sms, ctx->d_err, ctx->d_timeout,
+  return {ctx->device, ctx->num_sms, ctx->scan_matrix, ctx->d_err, ctx->d_timeout,
           ctx->opts.wait_cycles ? ctx->opts.wait_cycles : kDefaultWaitCycles};
 }
 
@@ -1130,7 +1131,8 @@ kvx_status kv_ctx_create(int device, const kvx_opts* opts, kvx_ctx** out) {
     ctx->seg_occ = segment_ctas_per_sm();
     if ((e = prepare_tma_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_attend_kernels()) != cudaSuccess) return fail(e);
-    if ((e = prepare_state_kernels()) != cudaSuccess) return fail(e);
+    if ((e = prepare_state_kernels(&ctx->scan_matrix)) != cudaSuccess) return fail(e);
+    if (fault_point("scan_setup")) ctx->scan_matrix = false;
     // the host-page touch threads, once per process, at set-up rather than
     // inside a transfer call
     if (!(o.flags & KVX_FLAG_NO_HOST_TOUCH)) start_touch_threads();
@@ -1232,7 +1234,7 @@ kvx_status kv_state_load(kvx_ctx* ctx, int32_t num_layers, void* const* layer_ba
 
 kvx_status kv_fault_inject(const char* point, int32_t after_calls) {
   static const char* const points[] = {"launch",    "queue_launch", "memcpy",   "event",
-                                       "host_alloc", "tier_exit",    "tma_wait", "chunk_map",    "scan_wait"};
+                                       "host_alloc", "tier_exit",    "tma_wait", "chunk_map",    "scan_wait", "scan_setup"};
   std::lock_guard<std::mutex> lock(g_fault_mu);
   if (!point || !point[0]) {
     g_fault_point[0] = 0;

@@ -475,6 +475,8 @@ ScanSpace scan_space(const CtxView& ctx, const kvx_state_batch* b, const kvx_sca
   v.num_seqs = b->num_seqs;
   bool cut;
   ScanSpace w = {};
+  w.by_token = INT32_MAX;
+  if (!ctx.scan_matrix) return w;
   w.segment = scan_segment(v, a->heads, a->head_dim, a->state_dim, ctx.num_sms, &cut, &w.by_token);
   if (cut) {
     const int64_t pieces = scan_pieces(v, w.segment);

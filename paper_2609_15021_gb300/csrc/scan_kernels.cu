@@ -656,27 +656,27 @@ cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
 }
 
 template <class E, int N, int kP, bool kStateOnly>
-cudaError_t prepare() {
+cudaError_t prepare(bool* matrix) {
   auto kernel = chunk_kernel<E, N, kP, kStateOnly>;
   cudaFuncAttributes a;
   const cudaError_t e = cudaFuncGetAttributes(&a, kernel);
   if (e != cudaSuccess) return e;
-  if (a.numRegs != kLaunchRegs) return cudaErrorInvalidConfiguration;  // the eight warps would wait for registers
+  if (a.numRegs < kLaunchRegs) *matrix = false;  // the eight warps would wait for registers
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ScanShape<kP>::kSmem);
 }
 
 template <class E, int N, int kP>
-cudaError_t prepare() {
-  const cudaError_t e = prepare<E, N, kP, true>();
-  return e == cudaSuccess ? prepare<E, N, kP, false>() : e;
+cudaError_t prepare(bool* matrix) {
+  const cudaError_t e = prepare<E, N, kP, true>(matrix);
+  return e == cudaSuccess ? prepare<E, N, kP, false>(matrix) : e;
 }
 
 template <class E>
-cudaError_t prepare() {
+cudaError_t prepare(bool* matrix) {
   cudaError_t e;
-  if ((e = prepare<E, 64, 64>()) != cudaSuccess || (e = prepare<E, 64, 128>()) != cudaSuccess) return e;
-  if ((e = prepare<E, 128, 64>()) != cudaSuccess) return e;
-  return prepare<E, 128, 128>();
+  if ((e = prepare<E, 64, 64>(matrix)) != cudaSuccess || (e = prepare<E, 64, 128>(matrix)) != cudaSuccess) return e;
+  if ((e = prepare<E, 128, 64>(matrix)) != cudaSuccess) return e;
+  return prepare<E, 128, 128>(matrix);
 }
 
 }  // namespace
@@ -708,9 +708,10 @@ cudaError_t launch_scan_chunks(const ScanParams& p, int type, cudaStream_t s) {
   return type == KVX_TYPE_BF16 ? chunks<Bf16>(p, s) : chunks<Fp16>(p, s);
 }
 
-cudaError_t prepare_state_kernels() {
-  const cudaError_t e = prepare<Bf16>();
-  return e == cudaSuccess ? prepare<Fp16>() : e;
+cudaError_t prepare_state_kernels(bool* matrix) {
+  *matrix = true;
+  const cudaError_t e = prepare<Bf16>(matrix);
+  return e == cudaSuccess ? prepare<Fp16>(matrix) : e;
 }
 
 }  // namespace kvx

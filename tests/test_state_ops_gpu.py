@@ -389,6 +389,40 @@ def test_wait_for_the_tensor_cores_runs_out_then_recovery(t, heads):
         k.kv_ctx_destroy(c2)
 
 
+def test_without_the_matrix_form_everything_still_works():
+    """Fault point "scan_setup": a context whose matrix form cannot be used, as with kernels compiled for fewer
+    registers, is made all the same, moves slots and scans prompts token by token."""
+    k = kvx()
+    k.kv_fault_inject("scan_setup")
+    c = k.kv_ctx_create(0)
+    try:
+        check_scan(c, [300, 0, 17, 40], 2, 128, 128, 1, BF16)
+        check_scan(c, [1, 1], 2, 128, 128, 1, FP16, single=True)
+        batch, _ = batch_of([3000], [0])
+        assert k.kv_state_scan_workspace(c, batch, 2, 128, 128).numel() == 16  # the least there is
+        before = k.kv_ctx_stats(c)["kernel_launches"]
+        st = Slots(1, 2, 64, 64)
+        batch, _ = batch_of([500], [0])
+        wide, x, b, cc, dt, A, D, dt_bias = scan_inputs(500, 2, 64, 64, 1, BF16)
+        out = torch.empty((500, 2, 64), dtype=BF16, device="cuda")
+        k.kv_state_scan(c, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), cc.cuda(), out)
+        assert k.kv_ctx_stats(c)["kernel_launches"] == before + 1
+        host = k.HostBuffer(st.bytes)
+        k.kv_state_store(c, [st.dev.view(-1)], 1, st.bytes, 0, host.tensor)
+        torch.cuda.synchronize()
+        assert torch.equal(host.tensor[:st.bytes], st.dev.cpu()[0])
+        host.close()
+    finally:
+        k.kv_fault_inject(None)
+        k.kv_ctx_destroy(c)
+    c = k.kv_ctx_create(0)  # and the next context has it
+    try:
+        batch, _ = batch_of([3000], [0])
+        assert k.kv_state_scan_workspace(c, batch, 2, 128, 128).numel() > 16
+    finally:
+        k.kv_ctx_destroy(c)
+
+
 def test_captured_step(ctx):
     """A captured convolution and scan of single tokens, replayed: the state moves on in its slot."""
     k = kvx()
