@@ -858,8 +858,7 @@ typedef struct {
 } kvx_scan;
 /* Sequences of more than 16 tokens, and shorter ones where they are few (starts
    given, head_dim a multiple of 64, state_dim 64 or 128), are scanned in matrix
-   form on the tensor cores, where the products C.B, decayed and weighted, must
-   stay within the range of `type` (65504 in fp16); others token by token.  A wait for the tensor
+   form on the tensor cores; others token by token.  A wait for the tensor
    cores that runs out (kvx_opts.wait_cycles) is reported as KVX_ETIMEOUT by
    kv_get_device_error, the output then being incomplete.
    Device workspace (0 for one token of every sequence); as kv_attend's.        */

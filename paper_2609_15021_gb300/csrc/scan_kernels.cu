@@ -25,8 +25,8 @@
 // Rounding: M and the carried state are rounded to the inputs' type for the product that makes y, one rounding
 // a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into three bf16 or two fp16
 // numbers, whose sum is the weighted x to 22 bits or more, and all are multiplied with B (two bf16 parts, 16 bits, left
-// the state off by 2.5e-6 where the recurrence in fp32 is by 5e-7).  In fp16 the state and W are scaled by powers of two
-// into its range; M is not.
+// the state off by 2.5e-6 where the recurrence in fp32 is by 5e-7).  In fp16 the state, W and every row of M are scaled by
+// powers of two into its range, so that small or large B, C and steps cost no bits.
 //
 // A long sequence is cut into segments, so that every SM has some: a first pass makes each segment's state from
 // nothing (from its last chunk to its first, so that weights need no later decay), a second one carries the states
@@ -53,7 +53,10 @@ constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
 // What a chunk's tokens weigh.
 struct Weights {
   float sum[kChunk];     // exponents up to a token
-  float weight[kChunk];  // d times the decay behind it
+  union {
+    float weight[kChunk];     // d times the decay behind it
+    uint8_t top[2][kChunk];   // fp16, once W is made: the exponents of M's largest elements, a row's halves
+  };
   float d[kChunk];
   float exponent;        // of the whole chunk
   int shift;             // fp16: the power of two that makes the largest weight less than 1
@@ -95,6 +98,8 @@ __device__ __forceinline__ float cta_max(float v, float* buf) {
   for (int i = 1; i < kWarps; ++i) v = fmaxf(v, buf[i]);
   return v;
 }
+// A barrier of the two warps that have the same lanes of tensor memory.
+__device__ __forceinline__ void sync_sides(int lanes) { asm volatile("bar.sync %0, 64;" ::"r"(2 + lanes) : "memory"); }
 // A power of two that takes values up to `top` below 2^11.
 __device__ __forceinline__ int range_of(float top) {
   return top > 0.f && top < INFINITY ? max(-60, min(60, 10 - ilogbf(top))) : 0;
@@ -428,9 +433,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     }
     fence_operands();
 
-      float y[kCols];
+    float y[kCols];
     // G's columns, 16 of every 32 a side: read by all before M takes their place
     float g[4][16];
+    float m_back = 1.f;  // fp16: what undoes the scaling of M's row
     if constexpr (!kStateOnly) {
       dead = dead || !bar_wait(bar_g, parity, p.wait_cycles);
       tmem_after_sync();
@@ -443,18 +449,42 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     tmem_after_sync();
     if constexpr (!kStateOnly) {
       const float sum_t = w.sum[line];
+      auto weighed = [&](int q, int j) {  // elements 2 j and 2 j + 1 of G's q'th columns as M's
+        const int u = q * 32 + side * 16 + 2 * j;
+        const float2 su = *reinterpret_cast<const float2*>(&w.sum[u]), du = *reinterpret_cast<const float2*>(&w.d[u]);
+        const float2 e = fma2(su, twice(-1.f), twice(sum_t));
+        const float2 by = mul2(make_float2(ex2(e.x), ex2(e.y)), du), all = mul2(make_float2(g[q][2 * j], g[q][2 * j + 1]), by);
+        return make_float2(u <= line ? all.x : 0.f, u + 1 <= line ? all.y : 0.f);
+      };
+      auto seen = [&](int q) { return q * 32 + side * 16 <= (warp & 3) * 32 + 31; };  // some of the warp's tokens see some of these
+      float scale = 1.f;
+      if constexpr (kHalf) {  // a row's largest element to [2^14, 2^15)
+        float top = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          if (!seen(q)) continue;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float2 v = weighed(q, j);
+            put2(g[q] + 2 * j, v);
+            top = fmaxf(top, fmaxf(fabsf(v.x), fabsf(v.y)));
+          }
+        }
+        w.top[side][line] = (uint8_t)(__float_as_uint(top) >> 23);
+        sync_sides(warp & 3);
+        const int e = max(w.top[0][line], w.top[1][line]);
+        const int shift = e == 255 ? 0 : min(100, 14 + 127 - e);
+        scale = power_of_two(shift), m_back = power_of_two(-shift);
+      }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const int c0 = q * 32 + side * 16;
         uint32_t m[8];
-        if (c0 <= (warp & 3) * 32 + 31) {  // some of the warp's tokens see some of these
+        if (seen(q)) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int u = c0 + 2 * j;
-            const float2 su = *reinterpret_cast<const float2*>(&w.sum[u]), du = *reinterpret_cast<const float2*>(&w.d[u]);
-            const float2 e = fma2(su, twice(-1.f), twice(sum_t));
-            const float2 by = mul2(make_float2(ex2(e.x), ex2(e.y)), du), all = mul2(make_float2(g[q][2 * j], g[q][2 * j + 1]), by);
-            m[j] = pack2<E>(u <= line ? all.x : 0.f, u + 1 <= line ? all.y : 0.f);
+            const float2 v = kHalf ? mul2(at2(g[q] + 2 * j), twice(scale)) : weighed(q, j);
+            m[j] = pack2<E>(v.x, v.y);
           }
         } else {
 #pragma unroll
@@ -533,10 +563,11 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         tmem_load16(r, my_lanes + kY1 + side * kCols + k);
         tmem_wait_loads();
 #pragma unroll
-        for (int j = 0; j < 16; j += 2) put2(y + k + j, add2(at2(y + k + j), at2(r + j)));
+        for (int j = 0; j < 16; j += 2)
+          put2(y + k + j, kHalf ? fma2(at2(r + j), twice(m_back), at2(y + k + j)) : add2(at2(y + k + j), at2(r + j)));
       }
       if (odd) {
-        for (int u = 0; u < kChunk && t0 + u < end; ++u) {
+        for (int u = 0; u < kChunk && t0 + u < end; ++u) {  // whatever the row's scaling: M's sign decides
           uint32_t m;
           tmem_load1(m, my_lanes + kG + u / 2);
           tmem_wait_loads();

@@ -266,6 +266,37 @@ def test_scan_of_infinities_and_nan(ctx, dtype, p, skip):
     assert bool(((after - state).abs()[fine] <= (2.0 ** -14 * big + 1e-9)[fine]).all())
 
 
+@pytest.mark.parametrize("bc,size_x,step", [(0.01, 1000.0, 1e-3), (0.03, 100.0, 1e-3), (1.0, 1.0, 2e-6), (1.0, 1.0, 1.0), (64.0, 1e-3, 1.0),
+                                            (250.0, 1e-4, 3.0)])
+@pytest.mark.parametrize("p,n", [(64, 64), (128, 128)])
+def test_scan_of_small_and_large_factors_in_fp16(ctx, bc, size_x, step, p, n):
+    """A chunk of small or large B, C and steps, whose decayed products M = (C . B) e^.. d leave the range in which fp16
+    has its 11 bits, or fp16's altogether, where the results do not."""
+    k = kvx()
+    t, heads = 128, 2
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, FP16, seed=31)
+    x, b, c = (x * size_x).to(FP16), (b * bc).to(FP16), (c * bc).to(FP16)
+    dt = (torch.rand((t, heads), generator=torch.Generator().manual_seed(32)) * step).to(FP16)
+    st = Slots(1, heads, p, n, dtype=FP16)
+    batch, _ = batch_of([t], [0], fresh=[1])
+    out = torch.empty((t, heads, p), dtype=FP16, device="cuda")
+    k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out, softplus=False,
+                    workspace=k.kv_state_scan_workspace(ctx, batch, heads, p, n))
+    torch.cuda.synchronize()
+    y, _, size, _ = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, False,
+                              torch.zeros((heads, p, n), dtype=torch.float64))
+    assert float(y.abs().max()) < 65504
+    exponent = torch.cumsum(dt.double() * A.double(), 0).T  # [head][token]
+    decay = torch.exp((exponent[:, :, None] - exponent[:, None, :]).masked_fill(~torch.ones(t, t, dtype=torch.bool).tril(), -math.inf))
+    m = (c[:, 0].double() @ b[:, 0].double().T) * decay * dt.double().T[:, None, :]
+    rounded = (m.abs() @ x.double().abs().permute(1, 0, 2)).permute(1, 0, 2)  # what one rounding a term is relative to
+    # a rounding of M and of y, exponents of some hundreds and C . B in 32 bits; y's own subnormals
+    unit = refs.UNIT[FP16]
+    bound = unit * y.abs() + (unit + 2.0 ** -13) * rounded + 2.0 ** -19 * size + 2.0 ** -25
+    off = (out.cpu().double() - y).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
+
+
 def test_token_by_token_is_the_prompt(ctx):
     """A prompt in one call and its tokens one by one leave the same state within the bounds of both."""
     k = kvx()
