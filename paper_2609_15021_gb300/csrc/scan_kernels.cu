@@ -50,14 +50,17 @@ static_assert(kThreads * kRegs + 128 * kIssuerRegs <= kAllThreads * kLaunchRegs,
 // Columns of tensor memory.
 constexpr uint32_t kG = 0, kY1 = 128, kY2 = 256, kState = 384, kColumns = 512;
 
+constexpr float kMost = 1024.f;  // of a token's exponent
+
 // What a chunk's tokens weigh.
 struct Weights {
-  float sum[kChunk];     // exponents up to a token
+  float sum[kChunk];     // exponents up to a token, rounded
   union {
     float weight[kChunk];     // d times the decay behind it
     uint8_t top[2][kChunk];   // fp16, once W is made: the exponents of M's largest elements, a row's halves
   };
-  float d[kChunk];
+  float d[kChunk];       // d over 2^low
+  __half low[kChunk];    // what the sum lost
   float exponent;        // of the whole chunk
   int shift;             // fp16: the power of two that makes the largest weight less than 1
 };
@@ -189,7 +192,10 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     give_registers<kIssuerRegs>();
     if (warp > kWarps) return;
     // A chunk's weights, by one warp, four tokens a lane.  Sums behind a token are taken from the end, so that they
-    // are exact where their weight is not small; `after`: the exponent of what follows the chunk.
+    // are exact where their weight is not small; `after`: the exponent of what follows the chunk.  Sums up to a token
+    // are of any size, and their differences count: they are taken in two parts, whole 64ths, which 128 tokens of up to 2^10
+    // (a decay of 2^-1024 is as good as nothing) lose no bit of, and what is left, and kept as a rounded sum and what that
+    // lost, which goes into the factors of a column (d) and of a row of M.
     const float A2 = p.A[h] * kLog2e;
     float d[4];
     auto load_steps = [&](int64_t t0) {
@@ -200,24 +206,34 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       for (int k = 0; k < 4; ++k) d[k] = t0 + 4 * lane + k < end ? step_of(p, E::up(raw[k]), h) : 0.f;
     };
     auto weigh = [&](float after) {
-      float a[4], upto = 0.f, behind = 0.f;
+      float a[4], rest[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) a[k] = d[k] * A2;
-      upto = behind = (a[0] + a[1]) + (a[2] + a[3]);
+      for (int k = 0; k < 4; ++k) {
+        a[k] = d[k] * A2;
+        a[k] = a[k] < -kMost ? -kMost : a[k] > kMost ? kMost : a[k];
+        rest[k] = a[k] - rintf(a[k] * 64.f) * (1.f / 64);
+      }
+      float upto = ((a[0] - rest[0]) + (a[1] - rest[1])) + ((a[2] - rest[2]) + (a[3] - rest[3]));
+      float fine = (rest[0] + rest[1]) + (rest[2] + rest[3]);
+      float behind = (a[0] + a[1]) + (a[2] + a[3]);
       for (int m = 1; m < 32; m <<= 1) {
-        const float y = __shfl_up_sync(~0u, upto, m), z = __shfl_down_sync(~0u, behind, m);
-        if (lane >= m) upto += y;
+        const float y = __shfl_up_sync(~0u, upto, m), f = __shfl_up_sync(~0u, fine, m), z = __shfl_down_sync(~0u, behind, m);
+        if (lane >= m) upto += y, fine += f;
         if (lane + m < 32) behind += z;
       }
-      float below = __shfl_up_sync(~0u, upto, 1), above = __shfl_down_sync(~0u, behind, 1);
-      if (lane == 0) below = 0.f;
-      if (lane == 31) above = 0.f, w.exponent = upto;
+      float below = __shfl_up_sync(~0u, upto, 1), below_fine = __shfl_up_sync(~0u, fine, 1), above = __shfl_down_sync(~0u, behind, 1);
+      if (lane == 0) below = below_fine = 0.f;
+      if (lane == 31) above = 0.f, w.exponent = upto + fine;
       above += after;
       float top = 0.f;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        w.d[4 * lane + k] = d[k];
-        w.sum[4 * lane + k] = below += a[k];
+        below += a[k] - rest[k], below_fine += rest[k];
+        // the sum of both, rounded, and what that lost (Knuth, "The Art of Computer Programming", vol. 2, 4.2.2)
+        const float sum = below + below_fine, back = sum - below, low = (below - (sum - back)) + (below_fine - back);
+        w.sum[4 * lane + k] = sum;
+        w.low[4 * lane + k] = __float2half_rn(low);
+        w.d[4 * lane + k] = d[k] * ex2(-low);
       }
 #pragma unroll
       for (int k = 3; k >= 0; --k) {
@@ -436,7 +452,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     float y[kCols];
     // G's columns, 16 of every 32 a side: read by all before M takes their place
     float g[4][16];
-    float m_back = 1.f;  // fp16: what undoes the scaling of M's row
+    float row_factor = 1.f;  // of M's row
     if constexpr (!kStateOnly) {
       dead = dead || !bar_wait(bar_g, parity, p.wait_cycles);
       tmem_after_sync();
@@ -449,6 +465,8 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
     tmem_after_sync();
     if constexpr (!kStateOnly) {
       const float sum_t = w.sum[line];
+      row_factor = ex2(__half2float(w.low[line]));
+      const float by = ex2(sum_t) * row_factor * state_scale;
       auto weighed = [&](int q, int j) {  // elements 2 j and 2 j + 1 of G's q'th columns as M's
         const int u = q * 32 + side * 16 + 2 * j;
         const float2 su = *reinterpret_cast<const float2*>(&w.sum[u]), du = *reinterpret_cast<const float2*>(&w.d[u]);
@@ -474,7 +492,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         sync_sides(warp & 3);
         const int e = max(w.top[0][line], w.top[1][line]);
         const int shift = e == 255 ? 0 : min(100, 14 + 127 - e);
-        scale = power_of_two(shift), m_back = power_of_two(-shift);
+        scale = power_of_two(shift), row_factor *= power_of_two(-shift);
       }
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
@@ -508,7 +526,6 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
       dead = dead || !bar_wait(bar_y2, parity, p.wait_cycles);
       tmem_after_sync();
       if (more) fetch(kSpare ? b_at : c_at, kSpare ? p.b_token : p.c_token, t0 + step, c_to, state_vecs);
-      const float by = ex2(sum_t) * state_scale;
 #pragma unroll
       for (int k = 0; k < kCols; k += 16) {
         float r[16];
@@ -563,8 +580,7 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
         tmem_load16(r, my_lanes + kY1 + side * kCols + k);
         tmem_wait_loads();
 #pragma unroll
-        for (int j = 0; j < 16; j += 2)
-          put2(y + k + j, kHalf ? fma2(at2(r + j), twice(m_back), at2(y + k + j)) : add2(at2(y + k + j), at2(r + j)));
+        for (int j = 0; j < 16; j += 2) put2(y + k + j, fma2(at2(r + j), twice(row_factor), at2(y + k + j)));
       }
       if (odd) {
         for (int u = 0; u < kChunk && t0 + u < end; ++u) {  // whatever the row's scaling: M's sign decides

@@ -297,6 +297,36 @@ def test_scan_of_small_and_large_factors_in_fp16(ctx, bc, size_x, step, p, n):
     assert bool((off <= bound).all()), float((off / bound).max())
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("p,n", [(64, 64), (128, 128)])
+def test_scan_of_slow_decays_behind_fast_ones(ctx, dtype, p, n):
+    """Tokens that forget everything, then tokens that forget little: a decay is taken of the tokens between two, however
+    large the exponents before them are."""
+    k = kvx()
+    t, heads = 128, 4
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, dtype, seed=33)
+    A = -torch.tensor([8.0, 80.0, 800.0, 8e6])  # exponents of 2e3, 2e4, 2e5 and 2e9 before the slow tokens
+    slow = torch.tensor([1e-5, 5e-6, 5e-6, 1e-7]) * torch.rand((t, heads), generator=torch.Generator().manual_seed(34))
+    dt = torch.where(torch.arange(t)[:, None] < 64, torch.tensor(3.0), slow).to(dtype)
+    st = Slots(1, heads, p, n, dtype=dtype)
+    batch, _ = batch_of([t], [0], fresh=[1])
+    out = torch.empty((t, heads, p), dtype=dtype, device="cuda")
+    k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out, softplus=False,
+                    workspace=k.kv_state_scan_workspace(ctx, batch, heads, p, n))
+    torch.cuda.synchronize()
+    y, _, size, _ = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, False,
+                              torch.zeros((heads, p, n), dtype=torch.float64))
+    exponent = torch.cumsum(dt.double() * A.double(), 0).T  # [head][token]
+    decay = torch.exp((exponent[:, :, None] - exponent[:, None, :]).masked_fill(~torch.ones(t, t, dtype=torch.bool).tril(), -math.inf))
+    m = (c[:, 0].double() @ b[:, 0].double().T) * decay * dt.double().T[:, None, :]
+    rounded = (m.abs() @ x.double().abs().permute(1, 0, 2)).permute(1, 0, 2)
+    # a rounding of M and of y; an exponent of up to 30 (beyond which a term is nothing) in 32 bits, and C . B
+    unit = refs.UNIT[dtype]
+    bound = unit * y.abs() + (unit + 2.0 ** -16) * rounded + 2.0 ** -19 * size + 2.0 ** -25
+    off = (out.cpu().double() - y).abs()
+    assert bool((off <= bound).all()), float((off / bound).max())
+
+
 def test_token_by_token_is_the_prompt(ctx):
     """A prompt in one call and its tokens one by one leave the same state within the bounds of both."""
     k = kvx()
