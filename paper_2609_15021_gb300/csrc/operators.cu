@@ -5,7 +5,9 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <string.h>
+#include <utility>
 
 #include "operators.cuh"
 
@@ -30,12 +32,19 @@ bool extent(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t inner, int64
   return true;
 }
 
-// Rows of `inner` elements that are written must not lie over one another.
-bool disjoint(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t inner) {
-  if (n1 > 1 && s1 < inner) return false;
-  if (n0 > 1 && s0 < inner) return false;
-  if (n0 == 1 || n1 == 1) return true;
-  return s0 >= (n1 - 1) * s1 + inner || s1 >= (n0 - 1) * s0 + inner;
+// Rows of `inner` elements that are written must not lie over one another: every dimension (its size and stride) has to
+// step over all that those of smaller strides take.  At most three; extents are checked before.
+bool disjoint(std::initializer_list<std::pair<int64_t, int64_t>> dims, int64_t inner) {
+  std::pair<int64_t, int64_t> by_stride[3];
+  int n = 0;
+  for (const auto& d : dims)
+    if (d.first > 1) by_stride[n++] = {d.second, d.first};
+  std::sort(by_stride, by_stride + n);
+  for (int i = 0; i < n; ++i) {
+    if (by_stride[i].first < inner) return false;
+    inner += (by_stride[i].second - 1) * by_stride[i].first;
+  }
+  return true;
 }
 
 bool vectors(const void* p, int64_t s0, int64_t s1) {  // 16-byte vectors of 2-byte elements
@@ -53,7 +62,7 @@ kvx_status check_rows(DeviceMemory& mem, const Rows& r, bool written) {
   if (!r.p) return refuse(KVX_EINVAL, r.what);
   if (!extent(r.n0, r.s0, r.n1, r.s1, r.inner, 2, &bytes)) return refuse(KVX_EINVAL, r.what);
   if (!vectors(r.p, r.n0 > 1 ? r.s0 : 0, r.n1 > 1 ? r.s1 : 0)) return refuse(KVX_EALIGN, r.what);
-  if (written && !disjoint(r.n0, r.s0, r.n1, r.s1, r.inner)) return refuse(KVX_EINVAL, r.what);
+  if (written && !disjoint({{r.n0, r.s0}, {r.n1, r.s1}}, r.inner)) return refuse(KVX_EINVAL, r.what);
   const kvx_status st = mem.check(r.p, bytes);
   return st == KVX_OK ? st : refuse(st, r.what);
 }
@@ -292,7 +301,7 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
       int64_t bytes;
       if (!extent(batch->num_seqs, a->weights_seq_stride, pool->num_heads, a->weights_head_stride, p.pages.max_length, 4,
                   &bytes) ||
-          !disjoint(batch->num_seqs, a->weights_seq_stride, pool->num_heads, a->weights_head_stride, p.pages.max_length))
+          !disjoint({{batch->num_seqs, a->weights_seq_stride}, {pool->num_heads, a->weights_head_stride}}, p.pages.max_length))
         return refuse(KVX_EINVAL, "strides of weights");
       if ((st = check_words(mem, a->weights, bytes / 4, "weights")) != KVX_OK) return st;
     }
@@ -383,7 +392,7 @@ kvx_status kv_evict(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, co
     if (e->new_weights) {
       if (!extent(layers, e->new_weights_layer_stride, s, e->new_weights_seq_stride, 0, 4, &upper) ||
           !extent(h, e->new_weights_head_stride, 1, 0, most, 4, &bytes) ||
-          !disjoint(s, e->new_weights_seq_stride, h, e->new_weights_head_stride, most))
+          !disjoint({{layers, e->new_weights_layer_stride}, {s, e->new_weights_seq_stride}, {h, e->new_weights_head_stride}}, most))
         return refuse(KVX_EINVAL, "strides of new_weights");
       if ((st = check_words(mem, e->new_weights, (upper + bytes) / 4, "new_weights")) != KVX_OK) return st;
     }

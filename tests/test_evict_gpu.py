@@ -230,6 +230,28 @@ def test_table_strides_beyond_64_bits_of_bytes(ctx, stride, which):
     assert bool((kept == 77).all()) and bool((out == 77).all())
 
 
+@pytest.mark.parametrize("dim", [0, 1, 2])
+def test_new_weights_that_lie_over_one_another(ctx, dim):
+    """Layers, sequences or heads that share their rows of new weights would be written over one another."""
+    k = kvx()
+    pages, dev, pool, old, new = make([40, 9], 8)
+    batch = k.KvBatch(old.cuda(), torch.tensor([40, 9], dtype=torch.int32, device="cuda"), max_length=40)
+    w = torch.zeros((2, 2, 2, 40), device="cuda")
+    kept, out = torch.full((2, 2, 2, 8), 77, dtype=torch.int32, device="cuda"), torch.full((2,), 77, dtype=torch.int32, device="cuda")
+    shape = [2, 2, 2, 8]
+    shape[dim] = 1
+    shared = torch.full(shape, 77.0, device="cuda").expand(2, 2, 2, 8)
+    with pytest.raises(k.KvxError) as e:
+        k.kv_evict(ctx, pool, batch, w, 8, new.cuda(), kept, out, shared)
+    assert e.value.status == k.KVX_EINVAL
+    torch.cuda.synchronize()
+    assert bool((kept == 77).all()) and bool((out == 77).all()) and bool((shared == 77.0).all())
+    # rows in another order are not shared
+    k.kv_evict(ctx, pool, batch, w, 8, new.cuda(), kept, out, torch.zeros((2, 2, 2, 8), device="cuda").permute(2, 0, 1, 3))
+    torch.cuda.synchronize()
+    assert out.tolist() == [8, 8]
+
+
 def test_refusals(ctx):
     k = kvx()
     pages, dev, pool, old, new = make([40, 9], 8)
