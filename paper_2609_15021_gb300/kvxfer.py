@@ -780,13 +780,15 @@ def kv_append(ctx, pool: KvPool, layer: int, batch: KvBatch, key, value, new_tok
 
 class KvAttention:
     """What an attention computes, marshalled once: query heads, tokens of each sequence that attend,
-    scale (None: 1/sqrt(head_dim)), softcap, window, slopes (device float32 [q_heads]; a bias of
+    scale (None: 1/sqrt(head_dim); not 0), softcap, window, slopes (device float32 [q_heads]; a bias of
     slope * distance) and the scales of an e4m3 cache."""
 
     def __init__(self, q_heads: int, new_tokens: int = 1, scale: float | None = None, softcap: float = 0.0,
                  window: int = 0, slopes=None, k_scale: float = 1.0, v_scale: float = 1.0, cache_dtype=None):
         if slopes is not None:
             _need(slopes, "slopes", "float32", (q_heads,))
+        if scale == 0:
+            raise ValueError("a scale of 0 is the library's mark for 1/sqrt(head_dim): pass None for that")
         self.q_heads, self.new_tokens, self.slopes, self.cache_dtype = q_heads, new_tokens, slopes, cache_dtype
         self._c = kvx_attention(q_heads=q_heads, new_tokens=new_tokens, scale=scale or 0.0, softcap=softcap,
                                 window=window, slopes=None if slopes is None else slopes.data_ptr(),

@@ -61,6 +61,13 @@ def test_binding_refuses_other_types_and_shapes():
         k.StateSlots(torch.zeros(100, dtype=torch.uint8), 2, 64)
 
 
+def test_scale_of_zero_is_not_the_default():
+    """0 is how the C call marks the default, so the binding must not pass a caller's 0 on."""
+    with pytest.raises(ValueError):
+        k.KvAttention(2, scale=0.0)
+    assert k.KvAttention(2)._c.scale == 0.0 and k.KvAttention(2, scale=0.5)._c.scale == 0.5
+
+
 def test_reference_attention_by_hand():
     """Two keys, scores 0 and log 3: probabilities 1/4 and 3/4."""
     pages = refs.Pages(1, 1, 1, 4, 8, torch.bfloat16, fill=0.0)
