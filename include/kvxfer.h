@@ -709,7 +709,8 @@ typedef struct {
                            are sequence s's, or NULL                            */
   int64_t key_token_stride, key_head_stride, value_token_stride, value_head_stride;
   float k_scale, v_scale; /* KVX_TYPE_E4M3: stored = x / scale rounded to nearest
-                             even and clamped to +-448; 0 means 1                */
+                             even and clamped to +-448; 0 means 1, no other one
+                             is below 2^-126                                     */
 } kvx_new_rows;
 
 /*

@@ -228,8 +228,8 @@ kvx_status kv_append(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     if (rows->tokens < 0 || rows->tokens > INT32_MAX) return refuse(KVX_EINVAL, "tokens");
     if (!rows->starts && (rows->new_tokens < 1 || rows->tokens != (int64_t)rows->new_tokens * batch->num_seqs))
       return refuse(KVX_EINVAL, "tokens is not new_tokens of every sequence");
-    if (!std::isfinite(rows->k_scale) || !std::isfinite(rows->v_scale) || rows->k_scale < 0.f || rows->v_scale < 0.f)
-      return refuse(KVX_EINVAL, "k_scale or v_scale");
+    for (float scale : {rows->k_scale, rows->v_scale})  // a subnormal one has no reciprocal: its zeros would be NaN
+      if (!(scale == 0.f || (std::isnormal(scale) && scale > 0.f))) return refuse(KVX_EINVAL, "k_scale or v_scale");
     CurrentDevice guard(ctx.device);
     if (!guard.ok) return KVX_ECUDA;
     if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");

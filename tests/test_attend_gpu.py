@@ -212,6 +212,34 @@ def test_append_of_prompts(ctx, dtype, cache, nhd, dim):
     assert k.kv_get_device_error(ctx) == -1
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** -100, 2.0 ** 120, 3.0e38])
+def test_append_with_scales_at_the_ends_of_the_range(ctx, scale):
+    """Zeros stay zeros and other values are their quotients, or the nearest that 8 bits hold."""
+    k = kvx()
+    case = Case([4], heads=1, dim=64, dtype=E4M3)
+    kv = normal((4, 2, 64), BF16, 28)
+    kv[:, :, :16], kv[:, :, 16:32] = 0.0, (kv[:, :, 16:32].float() * min(scale, 1e37)).to(BF16)
+    k.kv_append(ctx, case.pool, 0, case.batch, kv[:, :1].cuda(), kv[:, 1:].cuda(), new_tokens=4, k_scale=scale, v_scale=scale)
+    torch.cuda.synchronize()
+    for i in range(4):
+        case.pages.put(0, case.tables[0], i, refs.quantise(kv[i].view(2, 1, 64), scale))
+    got, want = case.dev[0].cpu().float(), case.pages.data[0].float()
+    assert torch.equal(torch.nan_to_num(got, nan=1e4), torch.nan_to_num(want, nan=1e4))
+
+
+@pytest.mark.parametrize("scale", [1e-39, 1e-45])
+def test_append_refuses_scales_that_have_no_reciprocal(ctx, scale):
+    k = kvx()
+    case = Case([2], heads=1, dim=64, dtype=E4M3)
+    kv = torch.zeros((2, 1, 64), dtype=BF16, device="cuda")
+    for which in ("k_scale", "v_scale"):
+        with pytest.raises(k.KvxError) as e:
+            k.kv_append(ctx, case.pool, 0, case.batch, kv, kv, new_tokens=2, **{which: scale})
+        assert e.value.status == k.KVX_EINVAL
+    torch.cuda.synchronize()
+    assert same_bits(case.dev[0], case.pages.data[0])
+
+
 def test_append_drops_rows_before_the_first_position(ctx):
     k = kvx()
     case = Case([2, 0], heads=1, dim=64)
