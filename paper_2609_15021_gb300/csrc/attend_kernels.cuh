@@ -51,8 +51,6 @@ namespace kvx {
 namespace {
 
 constexpr int kMaxCtas = 320;  // of a launch
-// What beginning and ending an item takes, in steps: the 45 sequences took 88 us at 6, 68 at 9, 61 at 12 and 63 at 16.
-constexpr int kItemSteps = 12;
 // Exponents are relative to 2^10 below the largest score so far (fp16 probabilities stay
 // normal down to 2^-24 of it), and it is raised when a score passes it by more than 2^5.
 constexpr float kBelow = 10.f, kSlack = 15.f;
@@ -735,7 +733,7 @@ cudaError_t prepare() {
 template <class C, int kDim, int kTiles>
 cudaError_t attend(const AttendParams& p, int num_sms, cudaStream_t s) {
   using S = AttendShape<C, kDim, kTiles>;
-  const int grid = (int)std::min<int64_t>(std::min(num_sms * S::kCtas, kMaxCtas), std::max<int64_t>(1, p.most_steps / p.min_steps));
+  const int grid = (int)std::min<int64_t>(std::min(num_sms * S::kCtas, kMaxCtas), (p.most_steps + p.min_steps - 1) / p.min_steps);
   return launch_after(attend_kernel<C, kDim, kTiles>, dim3(grid), S::kThreads, S::kSmem, s, p);
 }
 
