@@ -110,6 +110,62 @@ def test_groups_of_heads_and_several_new_tokens(ctx, group, new):
     check_attend(ctx, case, normal((len(lengths) * new, 2 * group, 64), BF16, 4), new, with_weights=True)
 
 
+# rows of queries (heads of a group x new tokens) that take two, three or four tiles of eight, and blocks of them
+ROWS = [(5, 2), (6, 4), (8, 4), (11, 4), (40, 1)]
+
+
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (FP16, FP16), (BF16, E4M3), (FP16, E4M3)])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+@pytest.mark.parametrize("group,new", ROWS)
+def test_many_query_rows(ctx, dtype, cache, dim, group, new):
+    lengths = [0, 1, 3, 17, 64, 210]
+    case = Case(lengths, heads=2, dim=dim, dtype=cache, seed=2)
+    scales = {"k_scale": 0.5, "v_scale": 1.75} if cache == E4M3 else {}
+    check_attend(ctx, case, normal((len(lengths) * new, 2 * group, dim), dtype, 29), new, with_weights=True, **scales)
+
+
+@pytest.mark.parametrize("cache", [BF16, FP16, E4M3])
+@pytest.mark.parametrize("dim,group,new", [(64, 6, 4), (128, 3, 4), (128, 8, 4), (256, 4, 4), (256, 6, 4)])
+def test_many_query_rows_of_long_caches_with_cap_bias_and_window(ctx, cache, dim, group, new):
+    """Split over the cache and joined."""
+    case = Case([2500, 700, 9], heads=1, dim=dim, dtype=cache, block=32, seed=3)
+    q = normal((3 * new, group, dim), FP16 if cache == FP16 else BF16, 30)
+    slopes = torch.exp2(-torch.arange(1, group + 1, device="cuda").float())
+    check_attend(ctx, case, q, new, with_weights=True, softcap=20.0, slopes=slopes)
+    check_attend(ctx, case, q, new, with_weights=True, window=600)
+
+
+@pytest.mark.parametrize("cache", [BF16, FP16, E4M3])
+@pytest.mark.parametrize("dim,group", [(64, 1), (64, 4), (64, 8), (128, 1), (128, 4), (128, 8), (256, 1), (256, 4), (256, 6)])
+def test_values_that_are_not_finite_in_every_form(ctx, cache, dim, group):
+    """As test_nan_and_infinity_where_a_row_does_not_look, for each type, head size and number of tiles."""
+    new = 4
+    case = Case([30, 64], heads=1, dim=dim, dtype=cache)
+    for s, n in enumerate(case.lengths):
+        case.pages.put(0, case.tables[s], n - 1, torch.tensor([NAN, math.inf]).to(cache).view(2, 1, 1).expand(2, 1, dim))
+        case.pages.put(0, case.tables[s], n - 12, torch.tensor([math.inf, NAN]).to(cache).view(2, 1, 1).expand(2, 1, dim))
+    case.upload()
+    q = normal((2 * new, group, dim), FP16 if cache == FP16 else BF16, 13)
+    weights = torch.zeros((2, 1, 64), device="cuda")
+    out, lse = run_attend(ctx, case, q, new, weights=weights, window=9)
+    want, l, _, bound, err = refs.attend(case.pages, 0, case.tables, case.lengths, q, new, 1 / math.sqrt(dim), window=9)
+    for s in range(2):
+        for t in range(1, new - 1):  # position n-4+t: sees n-12+t .. n-4+t
+            row = s * new + t
+            assert bool(((out[row].cpu().double() - want[row]).abs() <= bound[row]).all())
+            assert bool(((lse[row].cpu().double() - l[row]).abs() <= err + 1e-6).all())
+        assert bool(torch.isnan(out[s * new + new - 1]).all())
+
+
+def test_scores_beyond_the_range_of_fp16(ctx):
+    """Scores are kept in 32 bits: those of fp16 queries and keys may pass 65,504."""
+    case = Case([1, 50, 400], heads=1, dim=64, dtype=FP16)
+    q = normal((3, 2, 64), FP16, 8, 5000.0)
+    check_attend(ctx, case, q, scale=1.5)
+    _, lse, _, _, _ = refs.attend(case.pages, 0, case.tables, case.lengths, q, 1, 1.5)
+    assert float(lse.max()) > 65504
+
+
 @pytest.mark.parametrize("block,pack,dim,cache", [(1, 1, 64, BF16), (3, 5, 64, BF16), (32, 49, 64, E4M3),
                                                   (8, 1, 72, FP16), (48, 2, 80, BF16), (16, 1, 16, E4M3), (16, 1, 8, BF16)])
 def test_pages_that_end_inside_a_step(ctx, block, pack, dim, cache):

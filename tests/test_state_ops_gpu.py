@@ -327,6 +327,38 @@ def test_scan_of_slow_decays_behind_fast_ones(ctx, dtype, p, n):
     assert bool((off <= bound).all()), float((off / bound).max())
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+@pytest.mark.parametrize("p,n", [(64, 64), (64, 128), (128, 64), (128, 128)])
+@pytest.mark.parametrize("t", [40, 128, 300, 520])
+def test_state_keeps_the_bits_of_the_weighted_inputs(ctx, dtype, p, n, t):
+    """One token a head has an input, so an element of the state is one product, decayed: nothing averages out what a
+    split of the weighted input (three bf16 numbers, two of fp16: 24 and 22 bits) would lose."""
+    k = kvx()
+    heads = 4
+    wide, x, b, c, dt, A, D, dt_bias = scan_inputs(t, heads, p, n, 1, dtype, seed=41)
+    x = x.clone()
+    for h, at in enumerate([3, t // 3, t // 2, t - 1]):
+        x[:at, h], x[at + 1:, h] = 0, 0
+    dt = torch.full((t, heads), 2.0 ** -10).to(dtype)
+    A = -torch.tensor([0.3, 0.5, 0.7, 0.9])
+    st = Slots(1, heads, p, n, dtype=dtype)
+    batch, _ = batch_of([t], [0], fresh=[1])
+    out = torch.empty((t, heads, p), dtype=dtype, device="cuda")
+    k.kv_state_scan(ctx, st.slots, batch, x.cuda(), dt.cuda(), A.cuda(), b.cuda(), c.cuda(), out, softplus=False,
+                    workspace=k.kv_state_scan_workspace(ctx, batch, heads, p, n))
+    torch.cuda.synchronize()
+    _, state, _, _ = refs.scan(x.double(), dt.double(), A.double(), b.double(), c.double(), None, None, False,
+                               torch.zeros((heads, p, n), dtype=torch.float64))
+    got = st.dev.cpu()[0, :st.rec].view(torch.float32).view(heads, p, n).double()
+    # 2^-22 of the split, 2^-22 of each of up to five chunks' powers of two, three sums of products in 32 bits
+    assert bool(((got - state).abs() <= 2.0 ** -19 * state.abs()).all())
+
+
+def test_scan_of_fast_and_slow_decays_in_fp16(ctx):
+    check_scan(ctx, [260, 70], 8, 64, 64, 1, FP16, fast=True, bias=False)
+    check_scan(ctx, [700], 8, 128, 128, 2, FP16, fast=True, bias=False)
+
+
 def test_token_by_token_is_the_prompt(ctx):
     """A prompt in one call and its tokens one by one leave the same state within the bounds of both."""
     k = kvx()
