@@ -34,7 +34,7 @@ struct PagesView {
   int64_t half_bytes;               // K half of a page; the V half follows
   int64_t head_bytes;               // from a head of a page half to the next
   int64_t row_bytes;
-  // A K row's number in its layer's rows is (page * page_rows + slot * token_rows + head * head_rows).
+  // Head 0's K row of a token has, of its layer's rows, the number page * page_rows + slot * token_rows.
   uint32_t page_rows, token_rows;
   Div31 by_block, by_pack;          // tokens per page, pages per logical block
   uint32_t entries;                 // valid table entries are below this
@@ -230,15 +230,15 @@ __device__ __forceinline__ void check_length(const PagesView& v, int32_t s) {
   if (n < 0 || n > v.max_length) atomicMin(v.err, (long long)v.table_len);
 }
 
-// The slot `slots[s]`, or null (and reported) where it is out of range.
-__device__ __forceinline__ uint8_t* slot_of(const StateView& v, const int32_t* slots, int32_t s) {
-  const int32_t i = slots[s];
+// Slot i, sequence s's, or null (and reported) where it is out of range.
+__device__ __forceinline__ uint8_t* slot_at(const StateView& v, int32_t i, int32_t s) {
   if (i < 0 || i >= v.num_slots) {
     atomicMin(v.err, (long long)s);
     return nullptr;
   }
   return v.base + (int64_t)i * v.slot_bytes + v.offset;
 }
+__device__ __forceinline__ uint8_t* slot_of(const StateView& v, const int32_t* slots, int32_t s) { return slot_at(v, slots[s], s); }
 
 // Rows of sequence s, cut to the rows there are (a pair of starts that does not ascend within them is reported).
 __device__ __forceinline__ void rows_of(const StateView& v, int32_t s, int64_t* first, int64_t* last) {

@@ -17,13 +17,6 @@ struct Piece {
 __device__ __forceinline__ int32_t pieces_of(int64_t first, int64_t last, int32_t length, int32_t none_up_to) {
   return last - first <= none_up_to ? 0 : max(1, (int32_t)((last - first + length - 1) / length));
 }
-__device__ __forceinline__ uint8_t* slot_at(const StateView& v, int32_t i, int32_t s) {
-  if (i < 0 || i >= v.num_slots) {
-    atomicMin(v.err, (long long)s);
-    return nullptr;
-  }
-  return v.base + (int64_t)i * v.slot_bytes + v.offset;
-}
 
 // The piece'th of all sequences' pieces of `length` rows (at least one of a sequence longer than none_up_to), counted
 // in their order: False behind the last.  Up to 32 sequences are looked at by every warp for itself, with one round of loads;
