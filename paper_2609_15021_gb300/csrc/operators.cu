@@ -544,6 +544,7 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
       if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
     }
     p.segment = space.segment;
+    p.pieces = space.segment ? (int32_t)scan_pieces(p.state, space.segment) : 0;
     p.by_token = space.by_token;
     p.segment_states = space.bytes > 0 ? (float*)workspace : nullptr;
     p.segment_exponents = space.bytes > 0 ? (float*)((uint8_t*)workspace + space.exponents) : nullptr;

@@ -134,6 +134,7 @@ struct ScanParams {
   int64_t x_token, x_head, dt_token, b_token, b_group, c_token, c_group, out_token, out_head;  // in elements
   int32_t heads, head_dim, state_dim, heads_per_group, softplus;
   int32_t segment;           // tokens of a segment in the matrix form; 0: no sequence takes it
+  int32_t pieces;            // scan_pieces of it
   int32_t by_token;          // sequences of up to so many tokens go token by token; -1: none
   float* segment_states;     // [piece][head][head_dim][state_dim], where sequences are cut into segments
   float* segment_exponents;  // [piece][head]
@@ -141,8 +142,9 @@ struct ScanParams {
   int* timeout;              // set when one ran out
   bool stall;                // fault point "scan_wait": the first chunk's products are not announced
 };
-// Pieces that the workspace has room for: as many as sequences whose rows do not overlap can have.
-__host__ __device__ inline int64_t scan_pieces(const StateView& v, int32_t segment) { return v.tokens / segment + v.num_seqs; }
+// Pieces that the workspace has room for: as many as sequences whose rows do not overlap can have.  No more than there are
+// SMs and sequences, where sequences are cut.
+inline int64_t scan_pieces(const StateView& v, int32_t segment) { return v.tokens / segment + v.num_seqs; }
 // The segment of the matrix form for a batch, 0 where it is not used; *cut: whether a sequence may have several;
 // *by_token: up to how many tokens a sequence does not take it.
 int32_t scan_segment(const StateView& v, int32_t heads, int32_t head_dim, int32_t state_dim, int num_sms, bool* cut,

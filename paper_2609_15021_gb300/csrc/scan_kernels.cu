@@ -635,27 +635,25 @@ __global__ void __launch_bounds__(kAllThreads, 1) chunk_kernel(const __grid_cons
 // segments than there is room for: those are left out here, as they are by the grids of the passes.
 __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ ScanParams p) {
   wait_for_previous();
-  __shared__ unsigned long long first_s;
+  __shared__ int32_t first_s;
   const StateView& v = p.state;
   const int32_t s = blockIdx.z, h = blockIdx.y;
   if (threadIdx.x == 0) first_s = 0;
   __syncthreads();
-  int64_t mine = 0;  // pieces of the sequences before
+  int32_t mine = 0;  // pieces of the sequences before, as far as there is room
   for (int32_t i = threadIdx.x; i < s; i += 256) {
     int64_t a, b;
     rows_of(v, i, &a, &b);
-    mine += pieces_of(a, b, p.segment, p.by_token);
+    mine = min(mine + pieces_of(a, b, p.segment, p.by_token), p.pieces);
   }
   for (int m = 16; m; m >>= 1) mine += __shfl_xor_sync(~0u, mine, m);
-  if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&first_s, (unsigned long long)mine);
+  if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&first_s, mine);
   __syncthreads();
   const uint8_t* in = slot_of(v, v.slots_in, s);
   if (!in || !slot_of(v, v.slots_out, s)) return;
   int64_t a, b;
   rows_of(v, s, &a, &b);
-  const int64_t first_piece = (int64_t)first_s;
-  const int64_t room = max((int64_t)0, scan_pieces(v, p.segment) - first_piece);
-  const int32_t segs = (int32_t)min((int64_t)pieces_of(a, b, p.segment, p.by_token), room);
+  const int32_t segs = min(pieces_of(a, b, p.segment, p.by_token), p.pieces - first_s);
   const int32_t i = blockIdx.x * 256 + threadIdx.x, vecs = p.head_dim * p.state_dim / 4;
   if (i >= vecs) return;
   float4 state = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -665,7 +663,7 @@ __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ Scan
     float decay[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const int64_t at = (first_piece + g0 + k) * p.heads + h;
+      const int64_t at = (int64_t)(first_s + g0 + k) * p.heads + h;
       made[k] = make_float4(0.f, 0.f, 0.f, 0.f), decay[k] = 0.f;
       if (g0 + k + 1 < segs) {
         made[k] = reinterpret_cast<const float4*>(p.segment_states)[at * vecs + i];
@@ -675,7 +673,7 @@ __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ Scan
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       if (g0 + k >= segs) break;
-      reinterpret_cast<float4*>(p.segment_states)[((first_piece + g0 + k) * p.heads + h) * vecs + i] = state;
+      reinterpret_cast<float4*>(p.segment_states)[((int64_t)(first_s + g0 + k) * p.heads + h) * vecs + i] = state;
       state.x = state.x * decay[k] + made[k].x, state.y = state.y * decay[k] + made[k].y;
       state.z = state.z * decay[k] + made[k].z, state.w = state.w * decay[k] + made[k].w;
     }
@@ -684,8 +682,7 @@ __global__ void __launch_bounds__(256) carry_kernel(const __grid_constant__ Scan
 
 template <class E, int N, int kP>
 cudaError_t chunks(const ScanParams& p, cudaStream_t s) {
-  const int64_t pieces = scan_pieces(p.state, p.segment);
-  const dim3 grid((unsigned)(pieces * (p.head_dim / kP)), p.heads);
+  const dim3 grid((unsigned)((int64_t)p.pieces * (p.head_dim / kP)), p.heads);
   constexpr int kSmem = ScanShape<kP>::kSmem;
   if (p.segment_states) {
     cudaError_t e = launch_after(chunk_kernel<E, N, kP, true>, grid, kAllThreads, kSmem, s, p);
