@@ -753,8 +753,10 @@ typedef struct {
 } kvx_attention;
 #define KVX_ATTEND_MAX_NEW_TOKENS 64
 
-/* Bytes of device workspace that kv_attend needs for these shapes (more with
-   attention->weights, whose scores are kept until the softmax sums are known).
+/* Bytes of device workspace that kv_attend needs for these shapes.  With
+   attention->weights the scores are kept until the softmax sums are known: 4 bytes
+   for every key (max_length of them), KV head, head of its group and new token of
+   every sequence, 64 new tokens of 32 heads over 32k keys 268 MB a sequence.
    It needs no initial contents and keeps nothing from one call for the next.
    One call uses it at a time: calls that may overlap need one each.            */
 kvx_status kv_attend_workspace(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch,

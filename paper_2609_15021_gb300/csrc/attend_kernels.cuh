@@ -33,7 +33,9 @@
 // An e4m3 cache is widened to fp16 between shared memory and the product, exactly;
 // the queries then are fp16 too, each row scaled by a power of two, so that no bit of
 // a bf16 value is lost within 2^-24 of the row's largest.  Probabilities are rounded to the
-// cache's type (fp16 for e4m3) for the product with V; the sums they are divided by are not.
+// cache's type (fp16 for e4m3) for the product with V; the sums they are divided by are not.  That is 2^-9 of a term, of
+// either sign: in bf16 an output is off by some 2.1e-3 where its own rounding gives 1.6e-3, and a second part of each
+// probability would take the product twice.
 //
 // Measured: bf16, sequences of 21k and 32.8k tokens, 8 heads x 128 with 8 query rows each, weights kept (220 MB of
 // K/V): 45 us; fp16, 45 sequences of up to 16k tokens, 8 heads x 96 with 2 rows, cap and slopes (270 MB): 60 us; both

@@ -344,7 +344,7 @@ kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     p.part_dim = attend_pad(p.pages.head_dim);
     const int32_t step = 16 * attend_blocks(p.part_dim, pool->elem_bytes, block / 8);
     p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * ((p.pages.max_length + step - 1) / step + kItemSteps);
-    p.min_steps = 6;  // one sequence of 1.8k tokens, 8 heads: 12.6 us, as with 3, and 15.4 with 12
+    p.min_steps = 6;  // one sequence of 1.8k tokens, 8 heads: 12.6 us, as with 3, and 14.5 with 12
     return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), 2);
   });
 }

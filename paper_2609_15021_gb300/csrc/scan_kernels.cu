@@ -15,12 +15,13 @@
 // of k).  The next chunk's rows (96 KB an SM, some 2000 cycles) come in from the chunk's beginning on, into one buffer
 // more and those that a product has done with.
 //
-// 24k tokens of 16 heads of 128 x 128 in fp16 take 230 us: 58 for the segments' states, 10 for carrying them, 165 for
-// the last pass, where a chunk takes some 11,500 cycles: the products 2,600, shared memory 5,400 (what the copies,
+// 24k tokens of 16 heads of 128 x 128 in fp16 take 253 us: 61 for the segments' states, 12 for carrying them, 185 for
+// the last pass, where a chunk takes some 12,900 cycles: the products 2,600, shared memory 5,400 (what the copies,
 // the splits, the products' factors, the state and y write and read of it at 128 bytes a cycle), the threads'
-// instructions 4,400; the rest is waiting from one to the next.  Neither 16 warps (277 us), nor decays
+// instructions 4,500; the rest is waiting from one to the next.  15 us of it are the scaling of M's rows, 5 the sums of
+// exponents in two parts (in 64-bit floats they took 30).  When it took 230 without them, neither 16 warps (277), nor decays
 // taken apart by blocks of 32 tokens, with an eighth of the exponentials (231), nor warps of their own that move y
-// (241) made it faster.  2,048 tokens in bf16 take 33.5 us: two chunks a CTA, and three launches.
+// (241) made it faster.  2,048 tokens in bf16 take 34.4 us: two chunks a CTA, and three launches.
 //
 // Rounding: M and the carried state are rounded to the inputs' type for the product that makes y, one rounding
 // a term, as y is rounded to that type anyway.  The state itself is kept in fp32: W is split into three bf16 or two fp16
@@ -43,7 +44,7 @@ namespace {
 constexpr int kChunk = 128, kThreads = 256, kWarps = kThreads / 32;  // of the elements
 // And a group of four warps more, of which one issues.  A thread has 168 registers at the launch, and these four warps
 // give up what the eight take (256 * 216 + 128 * 72 = 384 * 168), as spills are dear where shared memory leaves the L1
-// cache little: with one warp more and 168 registers for all, 24k tokens of fp16 took 242 us instead of 230.
+// cache little: with one warp more and 168 registers for all, 24k tokens of fp16 took 242 us where this took 230.
 constexpr int kAllThreads = kThreads + 128, kLaunchRegs = 168, kRegs = 216, kIssuerRegs = 72;
 static_assert(kThreads * kRegs + 128 * kIssuerRegs <= kAllThreads * kLaunchRegs, "registers of a CTA");
 
