@@ -766,6 +766,84 @@ kvx_status kv_attend(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kv
                      int64_t workspace_bytes, kvx_stream_t stream);
 
 /*
+ * kv_append for keys that still are to be normed and rotated by their position, and the queries with them.
+ * For every head of q and key, in 32 bits and rounded once:
+ *   x = x / sqrt(mean(x^2) + eps) * (weight + weight_offset)      where there is a weight
+ *   (a, b) = (a cos - b sin, b cos + a sin) * rotary_scale         of the pairs of the first rotary_dim elements,
+ * the i'th pair by the angle position * inv_freq[i], whose full turns are taken off in 64 bits.  q goes to q_out (which may
+ * be q itself), key and value to the pages as kv_append puts them there.  A token that belongs to no sequence
+ * leaves its row of q_out as it was; one before position 0 or of a bad page still gets its row.
+ */
+typedef struct {
+  int32_t q_heads;
+  int32_t rotary_dim;       /* even, 0 .. head_dim                              */
+  int32_t interleaved;      /* pairs (2i, 2i + 1); 0: (i, i + rotary_dim / 2)   */
+  float rotary_scale;       /* 0 means 1                                        */
+  const float* inv_freq;    /* device [rotary_dim / 2]: radians a position      */
+  const int32_t* positions; /* device [tokens], or NULL: places in the cache    */
+  const void *q_weight, *k_weight; /* device [head_dim] of rows->type, or NULL: no norm */
+  float eps;                /* >= 0                                             */
+  float weight_offset;      /* 1 for weights that are stored less 1             */
+  int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+} kvx_rotary;
+kvx_status kv_append_rotary(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch,
+                            const kvx_new_rows* rows, const kvx_rotary* rotary, const void* q, const void* key,
+                            const void* value, void* q_out, kvx_stream_t stream);
+
+/*
+ * Attention over the pages that each query picks by their keys' bounds, for caches too long to be read whole.
+ *
+ * The bounds of one layer's pages: of every page and head the least and the greatest value that each element of
+ * the keys it holds takes, as whole numbers of a size of its own,
+ *   size = max |k| / 127,  low = floor(min k / size),  high = ceil(max k / size),
+ * as stored (an e4m3 cache's scale is left out).  A page head that holds a key that is not finite gets the widest bounds
+ * and the largest finite size, so that it is picked before all others.
+ */
+typedef struct {
+  int8_t* boxes; /* device [num_blocks][num_heads][2 (low, high)][head_dim]         */
+  float* sizes;  /* device [num_blocks][num_heads]                                  */
+} kvx_bounds;
+
+/* Make the bounds of the pages that hold the last new_tokens tokens of every sequence: after an append, or, with as many as
+   the longest has, of all its pages after a restore.  elem type: cache_type, KVX_TYPE_*.  They are made from
+   the keys alone, whatever was there.  A page whose table entry is out of range is left out and reported.   */
+kvx_status kv_bounds(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, int32_t cache_type,
+                     int64_t new_tokens, const kvx_bounds* bounds, kvx_stream_t stream);
+
+/*
+ * Pick pages for each of a sequence's last new_tokens tokens and each KV head.  A query row is rounded to whole numbers
+ * of its own size, w = rint(q / step) with step = max |q| / 127 (a row that is not finite counts as zeros), and a page's score is
+ *   max over the head's query rows of (step * sum_d (w_d high_d where w_d > 0, else w_d low_d)) * size,
+ * the sum in whole numbers, the products each rounded to 32 bits: the same whatever the order.  Of the pages up to the
+ * query's own the first `sinks`, the last `recent` and those of the largest scores are picked, `budget` in all (equal
+ * ones: the lowest page; a page whose table entry is out of range comes last and is reported).
+ */
+typedef struct {
+  int32_t type;       /* of q: KVX_TYPE_BF16 or _FP16                           */
+  int32_t q_heads;    /* a multiple of the pool's heads                         */
+  int32_t new_tokens; /* 1 .. KVX_ATTEND_MAX_NEW_TOKENS                         */
+  int32_t budget;     /* pages, sinks + recent <= budget                        */
+  int32_t sinks, recent; /* recent >= 1                                         */
+  int64_t q_token_stride, q_head_stride;
+} kvx_selection;
+/* selected: device [num_seqs * new_tokens][num_heads][budget]: the picked pages' places in their sequence, ascending, -1
+   behind the last.  Workspace as kv_attend's: 4 bytes for every page, head and new token.                       */
+kvx_status kv_select_workspace(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch, const kvx_selection* selection,
+                               int64_t* bytes);
+kvx_status kv_select(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch, const kvx_bounds* bounds,
+                     const kvx_selection* selection, const void* q, int32_t* selected, void* workspace,
+                     int64_t workspace_bytes, kvx_stream_t stream);
+
+/* kv_attend over the tokens of selected pages alone, up to each query's own position.  attention's window, slopes and
+   weights have to be 0 or NULL.  Of a list as many entries are looked at as there are pages up to the query.  One that is
+   negative, names a page behind the query's or is not above the one before it is left out.                       */
+kvx_status kv_attend_selected_workspace(kvx_ctx* ctx, const kvx_pool* pool, const kvx_batch* batch,
+                                        const kvx_attention* attention, int32_t budget, int64_t* bytes);
+kvx_status kv_attend_selected(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch,
+                              const kvx_attention* attention, int32_t budget, const int32_t* selected, const void* q,
+                              void* out, void* workspace, int64_t workspace_bytes, kvx_stream_t stream);
+
+/*
  * Shrink caches to `budget` tokens: in every layer of the pool, for every
  * sequence and KV head, keep the first `sinks` tokens, the last `recent` and, of
  * the others, those with the largest weights (what kv_attend accumulated; equal
@@ -869,6 +947,35 @@ kvx_status kv_state_scan_workspace(kvx_ctx* ctx, const kvx_state_batch* batch, c
 kvx_status kv_state_scan(kvx_ctx* ctx, const kvx_state* state, const kvx_state_batch* batch, const kvx_scan* scan,
                          const void* x, const void* dt, const void* B, const void* C, void* out, void* workspace,
                          int64_t workspace_bytes, kvx_stream_t stream);
+
+/*
+ * Gated delta rule, one decay and one step per head and token: what the state holds for a key is replaced, in part, by the
+ * value.  With q and k of group h / (heads / groups), q = scale * q, k and q first divided by sqrt(sum(x^2) + eps) if
+ * normalize is set, a_t = exp(A d_t), d_t = dt_t + dt_bias (softplus of it if softplus is set; a_t = 1 without dt) and
+ * b_t = beta_t (1 / (1 + exp(-beta_t)) if sigmoid is set):
+ *   S_t = a_t S_{t-1} + b_t (v_t - a_t S_{t-1} k_t) k_t^T   (head_dim x state_dim, fp32, a slot's as kv_state_scan's)
+ *   out_t = S_t q_t
+ * Keys whose b_t |k_t|^2 is above 2 make the recurrence itself grow.
+ */
+typedef struct {
+  int32_t type;       /* KVX_TYPE_BF16 or _FP16: q, k, v, dt, beta, out           */
+  int32_t heads;      /* of v and the state                                     */
+  int32_t head_dim;   /* of v: a multiple of 8, at most 256                     */
+  int32_t state_dim;  /* of q and k: 16, 32, 64, 128 or 256                     */
+  int32_t groups;     /* heads of q and k; divides heads                        */
+  int32_t softplus, sigmoid, normalize;
+  float scale;        /* 0: 1 / sqrt(state_dim)                                 */
+  float eps;          /* >= 0                                                   */
+  const float* A;       /* device [heads]; NULL without dt                      */
+  const float* dt_bias; /* device [heads], or NULL                              */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride, dt_token_stride,
+      beta_token_stride, out_token_stride, out_head_stride;
+} kvx_delta;
+/* dt: [tokens][heads], or NULL: no decay; beta: [tokens][heads].  Workspace as kv_state_scan's.                 */
+kvx_status kv_state_delta_workspace(kvx_ctx* ctx, const kvx_state_batch* batch, const kvx_delta* delta, int64_t* bytes);
+kvx_status kv_state_delta(kvx_ctx* ctx, const kvx_state* state, const kvx_state_batch* batch, const kvx_delta* delta,
+                          const void* q, const void* k, const void* v, const void* dt, const void* beta, void* out,
+                          void* workspace, int64_t workspace_bytes, kvx_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -4,7 +4,7 @@
 
 namespace kvx {
 
-cudaError_t launch_attend_e4m3(const AttendParams& p, int num_sms, cudaStream_t s) { return attend<E4m3>(p, num_sms, s); }
-cudaError_t prepare_attend_e4m3() { return prepare<E4m3>(); }
+cudaError_t launch_attend_e4m3(const AttendParams& p, int num_sms, cudaStream_t s) { return attend<E4m3, false>(p, num_sms, s); }
+cudaError_t prepare_attend_e4m3() { return prepare<E4m3, false>(); }
 
 }  // namespace kvx

@@ -4,7 +4,7 @@
 
 namespace kvx {
 
-cudaError_t launch_attend_fp16(const AttendParams& p, int num_sms, cudaStream_t s) { return attend<Fp16>(p, num_sms, s); }
-cudaError_t prepare_attend_fp16() { return prepare<Fp16>(); }
+cudaError_t launch_attend_fp16(const AttendParams& p, int num_sms, cudaStream_t s) { return attend<Fp16, false>(p, num_sms, s); }
+cudaError_t prepare_attend_fp16() { return prepare<Fp16, false>(); }
 
 }  // namespace kvx

@@ -11,19 +11,6 @@ namespace {
 
 constexpr int kAppendThreads = 128;
 
-// x / scale to the nearest: a product with the rounded reciprocal, corrected by its residual (Markstein, "Computation
-// of elementary functions on the IBM RISC System/6000 processor", 1990).  Quotients that the 8 bits clamp are left as
-// they are, as their residual may not be finite.
-__device__ __forceinline__ float divided(float x, float scale, float inverse) {
-  const float q = x * inverse;
-  const float r = fmaf(fmaf(-q, scale, x), inverse, q);
-  return fabsf(q) < 512.f ? r : q;
-}
-__device__ __forceinline__ uint32_t to_e4m3(float2 x, float scale, float inverse) {
-  return __nv_cvt_float2_to_fp8x2(make_float2(divided(x.x, scale, inverse), divided(x.y, scale, inverse)), __NV_SATFINITE,
-                                  __NV_E4M3);
-}
-
 // A warp finds one token's sequence and place and moves its rows, or a quarter of them (kParts): bound by
 // the rows' bytes, in and out.  A lane has four vectors in flight; a vector is 16 bytes of the cache's row,
 // twice as much of an input that is narrowed.  16,384 tokens of 4 x 256 bf16 into e4m3 (101 MB): 18.8 us, 5.4 TB/s; with a
@@ -38,22 +25,7 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const __grid_con
   const int part = (int)(unit - token * kParts);
   int32_t s;
   int64_t back;  // rows of this sequence from this one to its last
-  if (p.starts) {
-    int32_t lo = 0, hi = p.num_seqs;  // the last s with starts[s] <= token lies in [lo, hi)
-    while (hi - lo > 1) {
-      const int32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
-      const uint32_t below = __ballot_sync(~0u, at < hi && p.starts[at] <= token);
-      const int32_t n = 31 - __clz(below | 1);
-      hi = min(hi, lo + (n + 1) * step);
-      lo += n * step;
-    }
-    s = lo;
-    back = p.starts[s + 1] - token;
-    if (token < p.starts[s] || back <= 0) return;
-  } else {
-    s = (int32_t)(token / p.new_tokens);
-    back = (int64_t)(s + 1) * p.new_tokens - token;
-  }
+  if (!find_row(p.starts, p.num_seqs, p.new_tokens, token, &s, &back)) return;
   if (lane == 0 && part == 0) check_length(v, s);
   const int64_t pos = length_of(v, s) - back;
   if (pos < 0) return;
@@ -241,9 +213,10 @@ cudaError_t launch_append(const AppendParams& p, int type, int cache_type, int n
 }
 
 cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cudaStream_t s) {
-  const cudaError_t e = cache_type == KVX_TYPE_E4M3   ? launch_attend_e4m3(p, num_sms, s)
-                        : cache_type == KVX_TYPE_BF16 ? launch_attend_bf16(p, num_sms, s)
-                                                      : launch_attend_fp16(p, num_sms, s);
+  const auto launch = cache_type == KVX_TYPE_E4M3   ? (p.selected ? launch_attend_selected_e4m3 : launch_attend_e4m3)
+                      : cache_type == KVX_TYPE_BF16 ? (p.selected ? launch_attend_selected_bf16 : launch_attend_bf16)
+                                                    : (p.selected ? launch_attend_selected_fp16 : launch_attend_fp16);
+  const cudaError_t e = launch(p, num_sms, s);
   if (e != cudaSuccess) return e;
   const int64_t heads_all = (int64_t)p.pages.heads * p.pages.num_seqs;
   int64_t grid = heads_all * p.group * p.new_tokens;
@@ -255,9 +228,12 @@ cudaError_t launch_attend(const AttendParams& p, int cache_type, int num_sms, cu
 }
 
 cudaError_t prepare_attend_kernels() {
-  cudaError_t e = prepare_attend_bf16();
-  if (e == cudaSuccess) e = prepare_attend_fp16();
-  return e == cudaSuccess ? prepare_attend_e4m3() : e;
+  for (auto prepare : {prepare_attend_bf16, prepare_attend_fp16, prepare_attend_e4m3, prepare_attend_selected_bf16,
+                       prepare_attend_selected_fp16, prepare_attend_selected_e4m3}) {
+    const cudaError_t e = prepare();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
 }
 
 }  // namespace kvx

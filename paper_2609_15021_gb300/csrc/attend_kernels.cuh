@@ -154,7 +154,10 @@ struct Runs {
   }
 };
 
-template <class C, int kDim, int kTiles>
+// kSelected: of each query's selected pages alone.  A sequence of the launch then is one query (a sequence's last new_tokens
+// tokens after one another), its keys are counted over its list of pages, and its own page, where there are keys behind it, is
+// the one place where some are left out.
+template <class C, int kDim, int kTiles, bool kSelected>
 __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, AttendShape<C, kDim, kTiles>::kCtas)
     attend_kernel(const __grid_constant__ AttendParams p) {
   using S = AttendShape<C, kDim, kTiles>;
@@ -175,14 +178,30 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
   const int32_t rows = p.group * p.new_tokens;
   const int32_t blocks = (rows + kRows - 1) / kRows;  // of query rows
   const int32_t per_seq = v.heads * blocks;           // items
+  // Keys up to a query, and what the launch takes as its sequence's length.
+  auto keys_upto = [&](int32_t s) {
+    const int32_t of = (int32_t)quotient(p.by_query, (uint32_t)s);
+    return max(0, length_of(v, of) - (int32_t)p.by_query.d + 1 + (s - of * (int32_t)p.by_query.d));
+  };
+  auto keys_of = [&](int32_t s) {
+    if (!kSelected) return length_of(v, s);
+    const int32_t upto = keys_upto(s), block = (int32_t)v.by_block.d;
+    return upto > 0 ? min((int32_t)quotient(v.by_block, (uint32_t)(upto - 1)) + 1, p.budget) * block : 0;
+  };
+  auto check = [&](int32_t s) {
+    if (!kSelected)
+      check_length(v, s);
+    else if (s == (int32_t)(quotient(p.by_query, (uint32_t)s) * p.by_query.d))
+      check_length(v, (int32_t)quotient(p.by_query, (uint32_t)s));
+  };
 
   // All steps, and this CTA's run of them.  Up to 32 sequences are added up by every warp for itself.
   const bool few = v.num_seqs <= 32;
   long long total = 0, upto = 0;  // few: steps of this lane's sequence and those before
   if (few) {
     int32_t first;
-    if (blockIdx.x == 0 && threadIdx.x < v.num_seqs) check_length(v, threadIdx.x);
-    upto = lane < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, length_of(v, lane), &first)) * per_seq : 0;
+    if (blockIdx.x == 0 && threadIdx.x < v.num_seqs) check(threadIdx.x);
+    upto = lane < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, keys_of(lane), &first)) * per_seq : 0;
     for (int d = 1; d < 32; d <<= 1) {
       const long long y = __shfl_up_sync(~0u, upto, d);
       if (lane >= d) upto += y;
@@ -191,13 +210,13 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
   } else {
     for (int32_t s = threadIdx.x; s < v.num_seqs; s += kAttendThreads) {
       int32_t first;
-      if (blockIdx.x == 0) check_length(v, s);
-      total += run_steps(steps_of<kStep>(p, length_of(v, s), &first));
+      if (blockIdx.x == 0) check(s);
+      total += run_steps(steps_of<kStep>(p, keys_of(s), &first));
     }
     total = cta_sum<kWarps>(total, buf) * per_seq;
   }
   for (int32_t s = blockIdx.x; s < v.num_seqs; s += gridDim.x) {  // sequences without a key
-    if (length_of(v, s) > 0) continue;
+    if (keys_of(s) > 0) continue;
     for (int32_t i = threadIdx.x; i < v.heads * rows * (v.head_dim / 4); i += kAttendThreads) {
       const int32_t hr = i / (v.head_dim / 4), col = i % (v.head_dim / 4) * 4;
       write_out(p, s, hr / rows, hr % rows, col, make_float4(0.f, 0.f, 0.f, 0.f));
@@ -220,7 +239,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
   for (int32_t base = 0; base < v.num_seqs && !few; base += kAttendThreads) {
     int32_t first;
     const int32_t s = base + threadIdx.x;
-    const long long mine = s < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, length_of(v, s), &first)) * per_seq : 0;
+    const long long mine = s < v.num_seqs ? (long long)run_steps(steps_of<kStep>(p, keys_of(s), &first)) * per_seq : 0;
     long long before = mine;  // inclusive scan over the warp
     for (int d = 1; d < 32; d <<= 1) {
       const long long y = __shfl_up_sync(~0u, before, d);
@@ -267,7 +286,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
     // The piece: steps [i0, i1) of one item.
     int32_t first_key, length, steps;
     for (;;) {
-      length = length_of(v, seq);
+      length = keys_of(seq);
       steps = steps_of<kStep>(p, length, &first_key);
       if (at < seq_begin + (long long)run_steps(steps) * per_seq) break;
       seq_begin += (long long)run_steps(steps) * per_seq;
@@ -279,14 +298,30 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
     if (i1 <= i0) break;  // the run ends before the item's first step
     const int32_t h = item / blocks, row0 = (item % blocks) * kRows;
     const int32_t here = min(rows - row0, kRows);  // rows of this block
-    const int32_t* table = v.tables + seq * v.table_stride;
+    const int32_t of = kSelected ? (int32_t)quotient(p.by_query, (uint32_t)seq) : seq;
+    const int32_t* table = v.tables + of * v.table_stride;
+    const int32_t last = kSelected ? keys_upto(seq) - 1 : 0;  // the query's position
+    const int32_t* list = kSelected ? p.selected + ((int64_t)seq * v.heads + h) * p.budget : nullptr;
 
+    // The page of the sequence that key `slot` of the list's n'th page is in, or kNoRow where the query does not see it.
+    auto selected = [&](uint32_t n, uint32_t slot) -> uint32_t {
+      const int32_t page = __ldg(list + n), before = n ? __ldg(list + n - 1) : -1;
+      const int32_t own = (int32_t)quotient(v.by_block, (uint32_t)last);
+      const bool seen = page > max(before, -1) && (page < own || (page == own && (int32_t)slot <= last - own * (int32_t)v.by_block.d));
+      return seen ? (uint32_t)page : kNoRow;
+    };
     // Lane r (and, of 16 keys, r + 16) finds key r of a step, in two parts, so that nothing waits for the table: its entry
     // and the place in the block first, the row when it is used.
     auto look = [&](int32_t i) -> uint2 {
       const uint32_t key = first_key + i * kStep + lane % kStep;
-      const bool there = i < i1 && (int32_t)key < length;
-      const uint32_t page = quotient(v.by_block, key), slot = key - page * v.by_block.d;
+      bool there = i < i1 && (int32_t)key < length;
+      uint32_t page = quotient(v.by_block, key);
+      const uint32_t slot = key - page * v.by_block.d;
+      if (kSelected) {
+        page = there ? selected(page, slot) : kNoRow;
+        there = page != kNoRow;
+        page = there ? page : 0;
+      }
       const uint32_t block = quotient(v.by_pack, page), in = page - block * v.by_pack.d;
       const uint32_t entry = there && block < v.table_len ? (uint32_t)__ldg(table + block) : kNoRow;
       return make_uint2(entry, there ? in * v.page_rows + slot * v.token_rows : kNoRow);
@@ -295,7 +330,9 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
       if (l.x < v.entries && l.y != kNoRow) return l.x * (v.by_pack.d * v.page_rows) + l.y;
       if (l.y != kNoRow) {
         const uint32_t key = first_key + i * kStep + lane % kStep;
-        atomicMin(v.err, (long long)quotient(v.by_pack, quotient(v.by_block, key)));
+        uint32_t page = quotient(v.by_block, key);
+        if (kSelected) page = selected(page, key - page * v.by_block.d);
+        atomicMin(v.err, (long long)quotient(v.by_pack, page));
       }
       return kNoRow;
     };
@@ -380,7 +417,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         }
         const float up = power_of_two(shift);
         if (sub == 0 && (!S::kQueryInRegs || warp == 0)) {
-          row_pos[tile * 8 + quad] = there ? length - p.new_tokens + t : -1;
+          row_pos[tile * 8 + quad] = !there ? -1 : kSelected ? INT32_MAX : length - p.new_tokens + t;
           row_slope[tile * 8 + quad] = there && p.slopes ? p.slopes[head] * kLog2e : 0.f;
           row_scale[tile * 8 + quad] = p.scale * p.k_scale * kLog2e * power_of_two(-shift);
         }
@@ -423,7 +460,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
     const bool plain_scores = p.softcap == 0.f && !p.slopes;
     const float cap2 = p.softcap * kLog2e, to_cap = p.softcap > 0.f ? 1.f / cap2 : 0.f;  // scores are in powers of two
     // keys below `all_from` or from `all_to` on are not seen by every row
-    const int32_t all_to = length - p.new_tokens + 1, all_from = p.window > 0 ? length - p.window : INT32_MIN;
+    const int32_t all_to = kSelected ? INT32_MAX : length - p.new_tokens + 1, all_from = p.window > 0 ? length - p.window : INT32_MIN;
     float* scores = p.weights ? p.scores + ((int64_t)seq * v.heads + h) * p.score_stride * p.score_rows : nullptr;
 
     uint32_t stage = 0;
@@ -706,11 +743,11 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
 }
 
 // f(kernel, shape) for every form of the kernel over a cache of type C.
-template <class C, class F>
+template <class C, bool kSelected, class F>
 cudaError_t for_each_attend(F&& f) {
   cudaError_t e;
 #define KVX_EACH(kDim, kTiles) \
-  if ((e = f(attend_kernel<C, kDim, kTiles>, AttendShape<C, kDim, kTiles>())) != cudaSuccess) return e
+  if ((e = f(attend_kernel<C, kDim, kTiles, kSelected>, AttendShape<C, kDim, kTiles>())) != cudaSuccess) return e
   KVX_EACH(64, 1);
   KVX_EACH(64, 2);
   KVX_EACH(64, 4);
@@ -724,34 +761,34 @@ cudaError_t for_each_attend(F&& f) {
   return cudaSuccess;
 }
 
-template <class C>
+template <class C, bool kSelected>
 cudaError_t prepare() {
-  return for_each_attend<C>([](auto kernel, auto shape) {
+  return for_each_attend<C, kSelected>([](auto kernel, auto shape) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, decltype(shape)::kSmem);
   });
 }
 
 // The grid: as many CTAs as are resident, or as many runs of min_steps as there may be.
-template <class C, int kDim, int kTiles>
+template <class C, bool kSelected, int kDim, int kTiles>
 cudaError_t attend(const AttendParams& p, int num_sms, cudaStream_t s) {
   using S = AttendShape<C, kDim, kTiles>;
   const int grid = (int)std::min<int64_t>(std::min(num_sms * S::kCtas, kMaxCtas), (p.most_steps + p.min_steps - 1) / p.min_steps);
-  return launch_after(attend_kernel<C, kDim, kTiles>, dim3(grid), S::kThreads, S::kSmem, s, p);
+  return launch_after(attend_kernel<C, kDim, kTiles, kSelected>, dim3(grid), S::kThreads, S::kSmem, s, p);
 }
 
-template <class C>
+template <class C, bool kSelected>
 cudaError_t attend(const AttendParams& p, int num_sms, cudaStream_t s) {
   const int pad = attend_pad(p.pages.head_dim), tiles = attend_tiles(p.pages.head_dim, p.group * p.new_tokens);
   switch (pad + tiles) {
-    case 65: return attend<C, 64, 1>(p, num_sms, s);
-    case 66: return attend<C, 64, 2>(p, num_sms, s);
-    case 68: return attend<C, 64, 4>(p, num_sms, s);
-    case 129: return attend<C, 128, 1>(p, num_sms, s);
-    case 130: return attend<C, 128, 2>(p, num_sms, s);
-    case 132: return attend<C, 128, 4>(p, num_sms, s);
-    case 257: return attend<C, 256, 1>(p, num_sms, s);
-    case 258: return attend<C, 256, 2>(p, num_sms, s);
-    default: return attend<C, 256, 3>(p, num_sms, s);
+    case 65: return attend<C, kSelected, 64, 1>(p, num_sms, s);
+    case 66: return attend<C, kSelected, 64, 2>(p, num_sms, s);
+    case 68: return attend<C, kSelected, 64, 4>(p, num_sms, s);
+    case 129: return attend<C, kSelected, 128, 1>(p, num_sms, s);
+    case 130: return attend<C, kSelected, 128, 2>(p, num_sms, s);
+    case 132: return attend<C, kSelected, 128, 4>(p, num_sms, s);
+    case 257: return attend<C, kSelected, 256, 1>(p, num_sms, s);
+    case 258: return attend<C, kSelected, 256, 2>(p, num_sms, s);
+    default: return attend<C, kSelected, 256, 3>(p, num_sms, s);
   }
 }
 

@@ -1131,6 +1131,7 @@ kvx_status kv_ctx_create(int device, const kvx_opts* opts, kvx_ctx** out) {
     ctx->seg_occ = segment_ctas_per_sm();
     if ((e = prepare_tma_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_attend_kernels()) != cudaSuccess) return fail(e);
+    if ((e = prepare_select_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_state_kernels(&ctx->scan_matrix)) != cudaSuccess) return fail(e);
     if (fault_point("scan_setup")) ctx->scan_matrix = false;
     // the host-page touch threads, once per process, at set-up rather than

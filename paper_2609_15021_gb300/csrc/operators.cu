@@ -212,6 +212,94 @@ kvx_status check_attention(const kvx_pool* pool, const kvx_batch* batch, const k
   return KVX_OK;
 }
 
+// Over selected pages: what an attention may not have there.
+kvx_status check_selected(const kvx_attention* a, int32_t budget) {
+  if (budget < 1 || budget > kMaxRows) return refuse(KVX_EINVAL, "budget");
+  if (a->window || a->slopes || a->weights) return refuse(KVX_EINVAL, "window, slopes or weights over selected pages");
+  return KVX_OK;
+}
+
+bool check_cache_type(int32_t type, int32_t elem_bytes) {
+  return type == KVX_TYPE_E4M3 ? elem_bytes == 1 : (type == KVX_TYPE_BF16 || type == KVX_TYPE_FP16) && elem_bytes == 2;
+}
+
+int64_t most_pages(const kvx_pool* pool, const PagesView& v) {
+  return ((int64_t)v.max_length + pool->block_tokens - 1) / pool->block_tokens;
+}
+
+kvx_status check_selection(const kvx_pool* pool, const kvx_batch* batch, const PagesView& v, const kvx_selection* s) {
+  if (s->type != KVX_TYPE_BF16 && s->type != KVX_TYPE_FP16) return refuse(KVX_EINVAL, "type");
+  if (s->q_heads < 1 || s->q_heads > kMaxHeads || s->q_heads % pool->num_heads)
+    return refuse(KVX_EINVAL, "q_heads is no multiple of the pool's heads");
+  if (s->q_heads / pool->num_heads > kMaxScoreGroup) return refuse(KVX_EINVAL, "more than 128 query heads a KV head");
+  if (s->new_tokens < 1 || s->new_tokens > KVX_ATTEND_MAX_NEW_TOKENS) return refuse(KVX_EINVAL, "new_tokens");
+  if (s->budget < 1 || s->budget > kMaxRows || s->sinks < 0 || s->recent < 1 || (int64_t)s->sinks + s->recent > s->budget)
+    return refuse(KVX_EINVAL, "budget, sinks or recent");
+  const int64_t tokens = (int64_t)batch->num_seqs * s->new_tokens;
+  if (tokens * s->q_heads > kMaxRows) return refuse(KVX_ERANGE, "more than 2^30 rows of queries");
+  // a CTA a tile of pages and part of the new tokens, whatever its size
+  if ((int64_t)batch->num_seqs * s->new_tokens * ((most_pages(pool, v) + kScorePages - 1) / kScorePages) > kMaxRows)
+    return refuse(KVX_ERANGE, "more than 2^30 tiles of pages");
+  return KVX_OK;
+}
+
+// kv_select's workspace: the scores, where there are more pages than are picked.
+int64_t select_bytes(const kvx_pool* pool, const kvx_batch* batch, const PagesView& v, const kvx_selection* s) {
+  const int64_t pages = most_pages(pool, v);
+  return pages > s->budget ? (int64_t)batch->num_seqs * s->new_tokens * pool->num_heads * pages * 4 : 0;
+}
+
+kvx_status check_bounds(DeviceMemory& mem, const kvx_pool* pool, const kvx_bounds* b) {
+  const int64_t rows = pool->num_blocks * (int64_t)pool->num_heads;
+  if (!b->boxes) return refuse(KVX_EINVAL, "boxes");
+  if ((uintptr_t)b->boxes & 15) return refuse(KVX_EALIGN, "boxes");
+  const kvx_status st = mem.check(b->boxes, rows * 2 * pool->head_dim);
+  return st != KVX_OK ? refuse(st, "boxes") : check_words(mem, b->sizes, rows, "sizes");
+}
+
+// What kv_append and kv_append_rotary check alike, in two parts: what needs no device, and the memory.  `none`: there is
+// nothing to append.
+kvx_status view_append(const CtxView& ctx, const kvx_pool* pool, const kvx_batch* batch, const kvx_new_rows* rows, Geometry* g,
+                       AppendParams* p) {
+  kvx_status st = view_pages(ctx, pool, batch, g, &p->pages);
+  if (st != KVX_OK) return st;
+  if (!check_types(rows->type, rows->cache_type, pool->elem_bytes))
+    return refuse(KVX_EINVAL, "type, cache_type or elem_bytes");
+  if (rows->tokens < 0 || rows->tokens > INT32_MAX) return refuse(KVX_EINVAL, "tokens");
+  if (!rows->starts && (rows->new_tokens < 1 || rows->tokens != (int64_t)rows->new_tokens * batch->num_seqs))
+    return refuse(KVX_EINVAL, "tokens is not new_tokens of every sequence");
+  for (float scale : {rows->k_scale, rows->v_scale})  // a subnormal one has no reciprocal: its zeros would be NaN
+    if (!(scale == 0.f || (std::isnormal(scale) && scale > 0.f))) return refuse(KVX_EINVAL, "k_scale or v_scale");
+  return KVX_OK;
+}
+
+kvx_status fill_append(DeviceMemory& mem, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, const kvx_new_rows* rows,
+                       const void* key, const void* value, const Geometry& g, AppendParams* p) {
+  kvx_status st;
+  if ((st = layer_of(mem, pool, layer, g, &p->pages.base)) != KVX_OK) return st;
+  if ((st = check_batch_memory(mem, batch)) != KVX_OK) return st;
+  if (rows->starts && (st = check_words(mem, rows->starts, batch->num_seqs + 1, "starts")) != KVX_OK) return st;
+  const int64_t h = pool->num_heads, d = pool->head_dim;
+  if ((st = check_rows(mem, {key, rows->tokens, rows->key_token_stride, h, rows->key_head_stride, d, "key"}, false)) != KVX_OK ||
+      (st = check_rows(mem, {value, rows->tokens, rows->value_token_stride, h, rows->value_head_stride, d, "value"},
+                       false)) != KVX_OK)
+    return st;
+  p->key = (const uint8_t*)key;
+  p->value = (const uint8_t*)value;
+  p->starts = rows->starts;
+  p->tokens = rows->tokens;
+  p->key_token = 2 * rows->key_token_stride;
+  p->key_head = 2 * rows->key_head_stride;
+  p->value_token = 2 * rows->value_token_stride;
+  p->value_head = 2 * rows->value_head_stride;
+  p->new_tokens = rows->new_tokens;
+  p->num_seqs = batch->num_seqs;
+  p->row_vecs = div31((uint32_t)(g.row / 16));
+  p->k_scale = rows->k_scale ? rows->k_scale : 1.f;
+  p->v_scale = rows->v_scale ? rows->v_scale : 1.f;
+  return KVX_OK;
+}
+
 }  // namespace
 
 kvx_status kv_append(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, const kvx_new_rows* rows,
@@ -221,42 +309,65 @@ kvx_status kv_append(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     const CtxView ctx = view_of(c);
     AppendParams p;
     Geometry g;
-    kvx_status st = view_pages(ctx, pool, batch, &g, &p.pages);
+    kvx_status st = view_append(ctx, pool, batch, rows, &g, &p);
     if (st != KVX_OK) return st;
-    if (!check_types(rows->type, rows->cache_type, pool->elem_bytes))
-      return refuse(KVX_EINVAL, "type, cache_type or elem_bytes");
-    if (rows->tokens < 0 || rows->tokens > INT32_MAX) return refuse(KVX_EINVAL, "tokens");
-    if (!rows->starts && (rows->new_tokens < 1 || rows->tokens != (int64_t)rows->new_tokens * batch->num_seqs))
-      return refuse(KVX_EINVAL, "tokens is not new_tokens of every sequence");
-    for (float scale : {rows->k_scale, rows->v_scale})  // a subnormal one has no reciprocal: its zeros would be NaN
-      if (!(scale == 0.f || (std::isnormal(scale) && scale > 0.f))) return refuse(KVX_EINVAL, "k_scale or v_scale");
     CurrentDevice guard(ctx.device);
     if (!guard.ok) return KVX_ECUDA;
     if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
     if (rows->tokens == 0 || batch->num_seqs == 0) return KVX_OK;
     DeviceMemory mem(ctx.device);
-    if ((st = layer_of(mem, pool, layer, g, &p.pages.base)) != KVX_OK) return st;
-    if ((st = check_batch_memory(mem, batch)) != KVX_OK) return st;
-    if (rows->starts && (st = check_words(mem, rows->starts, batch->num_seqs + 1, "starts")) != KVX_OK) return st;
-    const int64_t h = pool->num_heads, d = pool->head_dim;
-    if ((st = check_rows(mem, {key, rows->tokens, rows->key_token_stride, h, rows->key_head_stride, d, "key"}, false)) != KVX_OK ||
-        (st = check_rows(mem, {value, rows->tokens, rows->value_token_stride, h, rows->value_head_stride, d, "value"},
-                         false)) != KVX_OK)
-      return st;
-    p.key = (const uint8_t*)key;
-    p.value = (const uint8_t*)value;
-    p.starts = rows->starts;
-    p.tokens = rows->tokens;
-    p.key_token = 2 * rows->key_token_stride;
-    p.key_head = 2 * rows->key_head_stride;
-    p.value_token = 2 * rows->value_token_stride;
-    p.value_head = 2 * rows->value_head_stride;
-    p.new_tokens = rows->new_tokens;
-    p.num_seqs = batch->num_seqs;
-    p.row_vecs = div31((uint32_t)(g.row / 16));
-    p.k_scale = rows->k_scale ? rows->k_scale : 1.f;
-    p.v_scale = rows->v_scale ? rows->v_scale : 1.f;
+    if ((st = fill_append(mem, pool, layer, batch, rows, key, value, g, &p)) != KVX_OK) return st;
     return KVX_LAUNCHED(c, launch_append(p, rows->type, rows->cache_type, ctx.num_sms, stream), 1);
+  });
+}
+
+kvx_status kv_append_rotary(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, const kvx_new_rows* rows,
+                            const kvx_rotary* r, const void* q, const void* key, const void* value, void* q_out,
+                            kvx_stream_t stream) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !pool || !batch || !rows || !r) return KVX_EINVAL;
+    const CtxView ctx = view_of(c);
+    RotaryParams p;
+    Geometry g;
+    kvx_status st = view_append(ctx, pool, batch, rows, &g, &p.append);
+    if (st != KVX_OK) return st;
+    if (r->q_heads < 1 || r->q_heads > kMaxHeads) return refuse(KVX_EINVAL, "q_heads");
+    if (r->rotary_dim < 0 || r->rotary_dim % 2 || r->rotary_dim > pool->head_dim) return refuse(KVX_EINVAL, "rotary_dim");
+    if (!std::isfinite(r->rotary_scale) || !std::isfinite(r->eps) || r->eps < 0.f || !std::isfinite(r->weight_offset))
+      return refuse(KVX_EINVAL, "rotary_scale, eps or weight_offset");
+    CurrentDevice guard(ctx.device);
+    if (!guard.ok) return KVX_ECUDA;
+    if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
+    if (rows->tokens == 0 || batch->num_seqs == 0) return KVX_OK;
+    DeviceMemory mem(ctx.device);
+    if ((st = fill_append(mem, pool, layer, batch, rows, key, value, g, &p.append)) != KVX_OK) return st;
+    const int64_t d = pool->head_dim, n = rows->tokens, hq = r->q_heads;
+    if ((st = check_rows(mem, {q, n, r->q_token_stride, hq, r->q_head_stride, d, "q"}, false)) != KVX_OK ||
+        (st = check_rows(mem, {q_out, n, r->out_token_stride, hq, r->out_head_stride, d, "q_out"}, true)) != KVX_OK)
+      return st;
+    if (q_out == q && ((n > 1 && r->q_token_stride != r->out_token_stride) || (hq > 1 && r->q_head_stride != r->out_head_stride)))
+      return refuse(KVX_EINVAL, "q_out is q, with other strides");
+    if (r->rotary_dim > 0 && (st = check_words(mem, r->inv_freq, r->rotary_dim / 2, "inv_freq")) != KVX_OK) return st;
+    if (r->positions && (st = check_words(mem, r->positions, n, "positions")) != KVX_OK) return st;
+    if (r->q_weight && (st = check_rows(mem, {r->q_weight, 1, 0, 1, 0, d, "q_weight"}, false)) != KVX_OK) return st;
+    if (r->k_weight && (st = check_rows(mem, {r->k_weight, 1, 0, 1, 0, d, "k_weight"}, false)) != KVX_OK) return st;
+    p.q = (const uint8_t*)q;
+    p.q_out = (uint8_t*)q_out;
+    p.q_weight = (const uint8_t*)r->q_weight;
+    p.k_weight = (const uint8_t*)r->k_weight;
+    p.inv_freq = r->inv_freq;
+    p.positions = r->positions;
+    p.q_token = 2 * r->q_token_stride;
+    p.q_head = 2 * r->q_head_stride;
+    p.out_token = 2 * r->out_token_stride;
+    p.out_head = 2 * r->out_head_stride;
+    p.q_heads = r->q_heads;
+    p.rotary_dim = r->rotary_dim;
+    p.interleaved = r->interleaved;
+    p.rotary_scale = r->rotary_scale ? r->rotary_scale : 1.f;
+    p.eps = r->eps;
+    p.weight_offset = r->weight_offset;
+    return KVX_LAUNCHED(c, launch_rotary(p, rows->type, rows->cache_type, ctx.num_sms, stream), 1);
   });
 }
 
@@ -274,78 +385,218 @@ kvx_status kv_attend_workspace(kvx_ctx* c, const kvx_pool* pool, const kvx_batch
   });
 }
 
+namespace {
+
+// Attention over all pages, or over those selected ones alone.
+kvx_status attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, const kvx_attention* a, bool some,
+                  int32_t budget, const int32_t* selected, const void* q, void* out, void* workspace, int64_t workspace_bytes,
+                  kvx_stream_t stream) {
+  const CtxView ctx = view_of(c);
+  AttendParams p;
+  Geometry g;
+  kvx_status st = view_pages(ctx, pool, batch, &g, &p.pages);
+  if (st == KVX_OK) st = check_attention(pool, batch, a);
+  if (st == KVX_OK && some) st = check_selected(a, budget);
+  if (st != KVX_OK) return st;
+  CurrentDevice guard(ctx.device);
+  if (!guard.ok) return KVX_ECUDA;
+  if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
+  if (batch->num_seqs == 0) return KVX_OK;
+  DeviceMemory mem(ctx.device);
+  if ((st = layer_of(mem, pool, layer, g, &p.pages.base)) != KVX_OK) return st;
+  if ((st = check_batch_memory(mem, batch)) != KVX_OK) return st;
+  const int64_t tokens = (int64_t)batch->num_seqs * a->new_tokens, d = pool->head_dim;
+  if ((st = check_rows(mem, {q, tokens, a->q_token_stride, a->q_heads, a->q_head_stride, d, "q"}, false)) != KVX_OK ||
+      (st = check_rows(mem, {out, tokens, a->out_token_stride, a->q_heads, a->out_head_stride, d, "out"}, true)) != KVX_OK)
+    return st;
+  if (a->slopes && (st = check_words(mem, a->slopes, a->q_heads, "slopes")) != KVX_OK) return st;
+  if (a->lse && (st = check_words(mem, a->lse, tokens * a->q_heads, "lse")) != KVX_OK) return st;
+  if (a->weights) {
+    int64_t bytes;
+    if (!extent(batch->num_seqs, a->weights_seq_stride, pool->num_heads, a->weights_head_stride, p.pages.max_length, 4,
+                  &bytes) ||
+        !disjoint({{batch->num_seqs, a->weights_seq_stride}, {pool->num_heads, a->weights_head_stride}}, p.pages.max_length))
+      return refuse(KVX_EINVAL, "strides of weights");
+    if ((st = check_words(mem, a->weights, bytes / 4, "weights")) != KVX_OK) return st;
+  }
+  if (some && (st = check_words(mem, selected, tokens * pool->num_heads * budget, "selected")) != KVX_OK) return st;
+  // over selected pages a query is a sequence of its own
+  kvx_attention each = *a;
+  if (some) p.pages.num_seqs = (int32_t)tokens, each.new_tokens = 1;
+  const AttendSpace space = attend_space(ctx, p.pages, &each);
+  if (workspace_bytes < space.bytes)
+    return refuse(KVX_ERANGE, some ? "workspace is smaller than kv_attend_selected_workspace says"
+                                   : "workspace is smaller than kv_attend_workspace says");
+  if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
+  if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
+  uint8_t* ws = (uint8_t*)workspace;
+  p.items = (int2*)(ws + space.items);
+  p.parts = (float*)(ws + space.parts);
+  p.row_lse2 = (float*)(ws + space.row_lse2);
+  p.scores = (float*)(ws + space.scores);
+  p.score_stride = space.score_stride;
+  p.score_rows = space.score_rows;
+  p.q = (const uint8_t*)q;
+  p.out = (uint8_t*)out;
+  p.lse = a->lse;
+  p.weights = a->weights;
+  p.slopes = a->slopes;
+  p.q_token = 2 * a->q_token_stride;
+  p.q_head = 2 * a->q_head_stride;
+  p.out_token = 2 * a->out_token_stride;
+  p.out_head = 2 * a->out_head_stride;
+  p.weights_seq = a->weights_seq_stride;
+  p.weights_head = a->weights_head_stride;
+  p.q_heads = a->q_heads;
+  p.group = a->q_heads / pool->num_heads;
+  p.new_tokens = each.new_tokens;
+  p.selected = some ? selected : nullptr;
+  p.budget = budget;
+  p.by_query = div31((uint32_t)a->new_tokens);
+  // one that reaches past every key is none; smaller ones leave the kernels' 32-bit positions room
+  p.window = a->window < p.pages.max_length ? a->window : 0;
+  p.scale = a->scale ? a->scale : 1.f / std::sqrt((float)d);
+  p.softcap = a->softcap;
+  const bool e4m3 = a->cache_type == KVX_TYPE_E4M3;
+  p.k_scale = e4m3 && a->k_scale ? a->k_scale : 1.f;
+  p.v_scale = e4m3 && a->v_scale ? a->v_scale : 1.f;
+  p.type = a->type;
+  const int32_t rows = p.group * p.new_tokens, block = 8 * attend_tiles(p.pages.head_dim, rows);
+  const int64_t blocks = (rows + block - 1) / block;
+  p.part_rows = block;
+  p.part_dim = attend_pad(p.pages.head_dim);
+  const int32_t step = 16 * attend_blocks(p.part_dim, pool->elem_bytes, block / 8);
+  int64_t longest = p.pages.max_length;
+  if (some) longest = std::min<int64_t>(longest + pool->block_tokens - 1, (int64_t)budget * pool->block_tokens);
+  p.most_steps = (int64_t)p.pages.num_seqs * p.pages.heads * blocks * ((longest + step - 1) / step + kItemSteps);
+  p.min_steps = 6;  // one sequence of 1.8k tokens, 8 heads: 12.6 us, as with 3, and 14.5 with 12
+  return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), 2);
+}
+
+}  // namespace
+
 kvx_status kv_attend(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, const kvx_attention* a,
                      const void* q, void* out, void* workspace, int64_t workspace_bytes, kvx_stream_t stream) {
   return guarded([&]() -> kvx_status {
     if (!c || !pool || !batch || !a) return KVX_EINVAL;
+    return attend(c, pool, layer, batch, a, false, 0, nullptr, q, out, workspace, workspace_bytes, stream);
+  });
+}
+
+kvx_status kv_attend_selected_workspace(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, const kvx_attention* a,
+                                        int32_t budget, int64_t* bytes) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !pool || !batch || !a || !bytes) return KVX_EINVAL;
+    Geometry g;
+    PagesView v;
+    kvx_status st = view_pages(view_of(c), pool, batch, &g, &v);
+    if (st == KVX_OK) st = check_attention(pool, batch, a);
+    if (st == KVX_OK) st = check_selected(a, budget);
+    if (st != KVX_OK) return st;
+    kvx_attention each = *a;
+    v.num_seqs *= a->new_tokens;
+    each.new_tokens = 1;
+    *bytes = attend_space(view_of(c), v, &each).bytes;
+    return KVX_OK;
+  });
+}
+
+kvx_status kv_attend_selected(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, const kvx_attention* a,
+                              int32_t budget, const int32_t* selected, const void* q, void* out, void* workspace,
+                              int64_t workspace_bytes, kvx_stream_t stream) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !pool || !batch || !a) return KVX_EINVAL;
+    return attend(c, pool, layer, batch, a, true, budget, selected, q, out, workspace, workspace_bytes, stream);
+  });
+}
+
+kvx_status kv_bounds(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, int32_t cache_type,
+                     int64_t new_tokens, const kvx_bounds* bounds, kvx_stream_t stream) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !pool || !batch || !bounds) return KVX_EINVAL;
     const CtxView ctx = view_of(c);
-    AttendParams p;
+    BoundsParams p;
     Geometry g;
     kvx_status st = view_pages(ctx, pool, batch, &g, &p.pages);
-    if (st == KVX_OK) st = check_attention(pool, batch, a);
+    if (st != KVX_OK) return st;
+    if (!check_cache_type(cache_type, pool->elem_bytes)) return refuse(KVX_EINVAL, "cache_type or elem_bytes");
+    if (new_tokens < 1) return refuse(KVX_EINVAL, "new_tokens");
+    CurrentDevice guard(ctx.device);
+    if (!guard.ok) return KVX_ECUDA;
+    if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
+    if (batch->num_seqs == 0) return KVX_OK;
+    p.new_tokens = (int32_t)std::min<int64_t>(new_tokens, p.pages.max_length);
+    const int64_t block = pool->block_tokens, most = (p.pages.max_length + block - 1) / block;
+    p.pages_each = (int32_t)std::min(most, (p.new_tokens + block - 2) / block + 1);
+    if ((int64_t)batch->num_seqs * p.pages_each * pool->num_heads > kMaxRows) return refuse(KVX_ERANGE, "more than 2^30 pages and heads");
+    DeviceMemory mem(ctx.device);
+    if ((st = layer_of(mem, pool, layer, g, &p.pages.base)) != KVX_OK) return st;
+    if ((st = check_batch_memory(mem, batch)) != KVX_OK) return st;
+    if ((st = check_bounds(mem, pool, bounds)) != KVX_OK) return st;
+    p.boxes = bounds->boxes;
+    p.sizes = bounds->sizes;
+    return KVX_LAUNCHED(c, launch_bounds(p, cache_type, stream), 1);
+  });
+}
+
+kvx_status kv_select_workspace(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, const kvx_selection* sel, int64_t* bytes) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !pool || !batch || !sel || !bytes) return KVX_EINVAL;
+    Geometry g;
+    PagesView v;
+    kvx_status st = view_pages(view_of(c), pool, batch, &g, &v);
+    if (st == KVX_OK) st = check_selection(pool, batch, v, sel);
+    if (st != KVX_OK) return st;
+    *bytes = select_bytes(pool, batch, v, sel);
+    return KVX_OK;
+  });
+}
+
+kvx_status kv_select(kvx_ctx* c, const kvx_pool* pool, const kvx_batch* batch, const kvx_bounds* bounds, const kvx_selection* sel,
+                     const void* q, int32_t* selected, void* workspace, int64_t workspace_bytes, kvx_stream_t stream) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !pool || !batch || !bounds || !sel) return KVX_EINVAL;
+    const CtxView ctx = view_of(c);
+    SelectParams p;
+    Geometry g;
+    kvx_status st = view_pages(ctx, pool, batch, &g, &p.pages);
+    if (st == KVX_OK) st = check_selection(pool, batch, p.pages, sel);
     if (st != KVX_OK) return st;
     CurrentDevice guard(ctx.device);
     if (!guard.ok) return KVX_ECUDA;
     if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
     if (batch->num_seqs == 0) return KVX_OK;
     DeviceMemory mem(ctx.device);
-    if ((st = layer_of(mem, pool, layer, g, &p.pages.base)) != KVX_OK) return st;
     if ((st = check_batch_memory(mem, batch)) != KVX_OK) return st;
-    const int64_t tokens = (int64_t)batch->num_seqs * a->new_tokens, d = pool->head_dim;
-    if ((st = check_rows(mem, {q, tokens, a->q_token_stride, a->q_heads, a->q_head_stride, d, "q"}, false)) != KVX_OK ||
-        (st = check_rows(mem, {out, tokens, a->out_token_stride, a->q_heads, a->out_head_stride, d, "out"}, true)) != KVX_OK)
+    if ((st = check_bounds(mem, pool, bounds)) != KVX_OK) return st;
+    const int64_t tokens = (int64_t)batch->num_seqs * sel->new_tokens;
+    if ((st = check_rows(mem, {q, tokens, sel->q_token_stride, sel->q_heads, sel->q_head_stride, pool->head_dim, "q"}, false)) != KVX_OK)
       return st;
-    if (a->slopes && (st = check_words(mem, a->slopes, a->q_heads, "slopes")) != KVX_OK) return st;
-    if (a->lse && (st = check_words(mem, a->lse, tokens * a->q_heads, "lse")) != KVX_OK) return st;
-    if (a->weights) {
-      int64_t bytes;
-      if (!extent(batch->num_seqs, a->weights_seq_stride, pool->num_heads, a->weights_head_stride, p.pages.max_length, 4,
-                  &bytes) ||
-          !disjoint({{batch->num_seqs, a->weights_seq_stride}, {pool->num_heads, a->weights_head_stride}}, p.pages.max_length))
-        return refuse(KVX_EINVAL, "strides of weights");
-      if ((st = check_words(mem, a->weights, bytes / 4, "weights")) != KVX_OK) return st;
+    if ((st = check_words(mem, selected, tokens * pool->num_heads * sel->budget, "selected")) != KVX_OK) return st;
+    const int64_t bytes = select_bytes(pool, batch, p.pages, sel);
+    if (bytes > 0) {
+      if (workspace_bytes < bytes) return refuse(KVX_ERANGE, "workspace is smaller than kv_select_workspace says");
+      if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
+      if ((st = mem.check(workspace, bytes)) != KVX_OK) return refuse(st, "workspace");
     }
-    const AttendSpace space = attend_space(ctx, p.pages, a);
-    if (workspace_bytes < space.bytes) return refuse(KVX_ERANGE, "workspace is smaller than kv_attend_workspace says");
-    if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
-    if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
-    uint8_t* ws = (uint8_t*)workspace;
-    p.items = (int2*)(ws + space.items);
-    p.parts = (float*)(ws + space.parts);
-    p.row_lse2 = (float*)(ws + space.row_lse2);
-    p.scores = (float*)(ws + space.scores);
-    p.score_stride = space.score_stride;
-    p.score_rows = space.score_rows;
+    p.boxes = bounds->boxes;
+    p.sizes = bounds->sizes;
     p.q = (const uint8_t*)q;
-    p.out = (uint8_t*)out;
-    p.lse = a->lse;
-    p.weights = a->weights;
-    p.slopes = a->slopes;
-    p.q_token = 2 * a->q_token_stride;
-    p.q_head = 2 * a->q_head_stride;
-    p.out_token = 2 * a->out_token_stride;
-    p.out_head = 2 * a->out_head_stride;
-    p.weights_seq = a->weights_seq_stride;
-    p.weights_head = a->weights_head_stride;
-    p.q_heads = a->q_heads;
-    p.group = a->q_heads / pool->num_heads;
-    p.new_tokens = a->new_tokens;
-    // one that reaches past every key is none; smaller ones leave the kernels' 32-bit positions room
-    p.window = a->window < p.pages.max_length ? a->window : 0;
-    p.scale = a->scale ? a->scale : 1.f / std::sqrt((float)d);
-    p.softcap = a->softcap;
-    const bool e4m3 = a->cache_type == KVX_TYPE_E4M3;
-    p.k_scale = e4m3 && a->k_scale ? a->k_scale : 1.f;
-    p.v_scale = e4m3 && a->v_scale ? a->v_scale : 1.f;
-    p.type = a->type;
-    const int32_t rows = p.group * p.new_tokens, block = 8 * attend_tiles(p.pages.head_dim, rows);
-    const int64_t blocks = (rows + block - 1) / block;
-    p.part_rows = block;
-    p.part_dim = attend_pad(p.pages.head_dim);
-    const int32_t step = 16 * attend_blocks(p.part_dim, pool->elem_bytes, block / 8);
-    p.most_steps = (int64_t)batch->num_seqs * p.pages.heads * blocks * ((p.pages.max_length + step - 1) / step + kItemSteps);
-    p.min_steps = 6;  // one sequence of 1.8k tokens, 8 heads: 12.6 us, as with 3, and 14.5 with 12
-    return KVX_LAUNCHED(c, launch_attend(p, a->cache_type, ctx.num_sms, stream), 2);
+    p.selected = selected;
+    p.q_token = 2 * sel->q_token_stride;
+    p.q_head = 2 * sel->q_head_stride;
+    p.q_heads = sel->q_heads;
+    p.group = sel->q_heads / pool->num_heads;
+    p.new_tokens = sel->new_tokens;
+    p.budget = sel->budget;
+    p.sinks = sel->sinks;
+    p.recent = sel->recent;
+    p.scores = (float*)workspace;
+    p.score_stride = most_pages(pool, p.pages);
+    p.tokens_each = score_tokens(p.group, p.new_tokens);
+    p.score_tiles = bytes > 0 ? (int32_t)((p.score_stride + kScorePages - 1) / kScorePages) : 0;
+    p.score_parts = (p.new_tokens + p.tokens_each - 1) / p.tokens_each;
+    return KVX_LAUNCHED(c, launch_select(p, sel->type, stream), 1 + (p.score_tiles > 0));
   });
 }
 
@@ -575,5 +826,100 @@ kvx_status kv_state_scan(kvx_ctx* c, const kvx_state* state, const kvx_state_bat
     p.stall = p.segment && fault_point("scan_wait");
     return KVX_LAUNCHED(c, launch_scan(p, a->type, ctx.num_sms, stream),
                         (space.by_token >= 0) + (space.segment ? space.bytes > 0 ? 3 : 1 : 0));
+  });
+}
+
+namespace {
+
+kvx_status check_delta(const kvx_state_batch* b, const kvx_delta* d) {
+  if (d->type != KVX_TYPE_BF16 && d->type != KVX_TYPE_FP16) return refuse(KVX_EINVAL, "type");
+  if (d->heads < 1 || d->heads > kMaxHeads || d->groups < 1 || d->heads % d->groups) return refuse(KVX_EINVAL, "heads or groups");
+  const int32_t n = d->state_dim;
+  if (n != 16 && n != 32 && n != 64 && n != 128 && n != 256) return refuse(KVX_EINVAL, "state_dim");
+  if (d->head_dim < 8 || d->head_dim > 256) return refuse(KVX_EINVAL, "head_dim");
+  if (d->head_dim % 8) return refuse(KVX_EALIGN, "head_dim");
+  if (!std::isfinite(d->scale) || !std::isfinite(d->eps) || d->eps < 0.f) return refuse(KVX_EINVAL, "scale or eps");
+  if (b->num_seqs < 0 || b->num_seqs > kMaxSeqs || b->tokens < 0) return refuse(KVX_EINVAL, "num_seqs or tokens");
+  return KVX_OK;
+}
+
+// A value a token and head, 2 bytes each.
+kvx_status check_gate(DeviceMemory& mem, const void* p, int64_t tokens, int64_t stride, int64_t heads, const char* what) {
+  int64_t bytes;
+  if (!p || !extent(tokens, stride, 1, 0, heads, 2, &bytes)) return refuse(KVX_EINVAL, what);
+  if ((uintptr_t)p & 1) return refuse(KVX_EALIGN, what);
+  const kvx_status st = mem.check(p, bytes);
+  return st == KVX_OK ? st : refuse(st, what);
+}
+
+}  // namespace
+
+kvx_status kv_state_delta_workspace(kvx_ctx* c, const kvx_state_batch* batch, const kvx_delta* d, int64_t* bytes) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !batch || !d || !bytes) return KVX_EINVAL;
+    const kvx_status st = check_delta(batch, d);
+    if (st != KVX_OK) return st;
+    *bytes = 0;
+    return KVX_OK;
+  });
+}
+
+kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_batch* batch, const kvx_delta* a, const void* q,
+                          const void* k, const void* v, const void* dt, const void* beta, void* out, void* workspace,
+                          int64_t workspace_bytes, kvx_stream_t stream) {
+  return guarded([&]() -> kvx_status {
+    if (!c || !state || !batch || !a) return KVX_EINVAL;
+    const CtxView ctx = view_of(c);
+    kvx_status st = check_delta(batch, a);
+    if (st != KVX_OK) return st;
+    CurrentDevice guard(ctx.device);
+    if (!guard.ok) return KVX_ECUDA;
+    if ((st = check_stream(stream, ctx.device)) != KVX_OK) return refuse(st, "stream");
+    if (batch->num_seqs == 0) return KVX_OK;
+    DeviceMemory mem(ctx.device);
+    DeltaParams p;
+    const int64_t h = a->heads, d = a->head_dim, n = a->state_dim, rows = batch->tokens;
+    if ((st = view_state(ctx, state, batch, state->recurrent_offset, h * d * n * 4, mem, &p.state)) != KVX_OK) return st;
+    if (rows > 0) {
+      if ((st = check_rows(mem, {q, rows, a->q_token_stride, a->groups, a->q_head_stride, n, "q"}, false)) != KVX_OK ||
+          (st = check_rows(mem, {k, rows, a->k_token_stride, a->groups, a->k_head_stride, n, "k"}, false)) != KVX_OK ||
+          (st = check_rows(mem, {v, rows, a->v_token_stride, h, a->v_head_stride, d, "v"}, false)) != KVX_OK ||
+          (st = check_rows(mem, {out, rows, a->out_token_stride, h, a->out_head_stride, d, "out"}, true)) != KVX_OK)
+        return st;
+      if (dt && (st = check_gate(mem, dt, rows, a->dt_token_stride, h, "dt")) != KVX_OK) return st;
+      if ((st = check_gate(mem, beta, rows, a->beta_token_stride, h, "beta")) != KVX_OK) return st;
+    }
+    if (dt && (st = check_words(mem, a->A, h, "A")) != KVX_OK) return st;
+    if (dt && a->dt_bias && (st = check_words(mem, a->dt_bias, h, "dt_bias")) != KVX_OK) return st;
+    (void)workspace;
+    (void)workspace_bytes;
+    p.q = (const uint8_t*)q;
+    p.k = (const uint8_t*)k;
+    p.v = (const uint8_t*)v;
+    p.dt = (const uint8_t*)dt;
+    p.beta = (const uint8_t*)beta;
+    p.out = (uint8_t*)out;
+    p.A = a->A;
+    p.dt_bias = a->dt_bias;
+    p.q_token = a->q_token_stride;
+    p.q_head = a->q_head_stride;
+    p.k_token = a->k_token_stride;
+    p.k_head = a->k_head_stride;
+    p.v_token = a->v_token_stride;
+    p.v_head = a->v_head_stride;
+    p.dt_token = a->dt_token_stride;
+    p.beta_token = a->beta_token_stride;
+    p.out_token = a->out_token_stride;
+    p.out_head = a->out_head_stride;
+    p.heads = a->heads;
+    p.head_dim = a->head_dim;
+    p.state_dim = a->state_dim;
+    p.heads_per_group = a->heads / a->groups;
+    p.softplus = a->softplus;
+    p.sigmoid = a->sigmoid;
+    p.normalize = a->normalize;
+    p.scale = a->scale ? a->scale : 1.f / std::sqrt((float)n);
+    p.eps = a->eps;
+    return KVX_LAUNCHED(c, launch_delta(p, a->type, ctx.num_sms, stream), 1);
   });
 }

@@ -54,6 +54,43 @@ struct AppendParams {
   float k_scale, v_scale;
 };
 
+struct RotaryParams {
+  AppendParams append;
+  const uint8_t *q, *q_weight, *k_weight;
+  uint8_t* q_out;
+  const float* inv_freq;
+  const int32_t* positions;
+  int64_t q_token, q_head, out_token, out_head;  // strides in bytes
+  int32_t q_heads, rotary_dim, interleaved;
+  float rotary_scale, eps, weight_offset;
+};
+
+struct BoundsParams {
+  PagesView pages;
+  int8_t* boxes;
+  float* sizes;
+  int32_t new_tokens, pages_each;  // pages_each: that a sequence's new tokens may lie in
+};
+
+struct SelectParams {
+  PagesView pages;  // base is not used
+  const int8_t* boxes;
+  const float* sizes;
+  const uint8_t* q;
+  int32_t* selected;
+  int64_t q_token, q_head;  // strides in bytes
+  int32_t q_heads, group, new_tokens, budget, sinks, recent;
+  float* scores;            // workspace: [query][head][score_stride]
+  int64_t score_stride;
+  int32_t tokens_each;      // new tokens whose rows a CTA scores at once
+  int32_t score_tiles, score_parts;  // of a sequence: of pages, and of new tokens
+};
+// A CTA of the scores has 64 pages and at most so many rows of queries, but always all of a head's group.
+constexpr int32_t kScoreRows = 64, kMaxScoreGroup = 128, kScorePages = 64;
+inline int32_t score_tokens(int32_t group, int32_t new_tokens) {
+  return group >= kScoreRows ? 1 : kScoreRows / group < new_tokens ? kScoreRows / group : new_tokens;
+}
+
 struct AttendParams {
   PagesView pages;
   const uint8_t* q;
@@ -74,6 +111,10 @@ struct AttendParams {
   float* scores;          // [sequence][head][score_stride keys][score_rows], with weights only
   int64_t score_stride;
   int32_t score_rows;     // query rows of a head, made even
+  // attention over selected pages: pages.num_seqs counts queries then, by_query of them a sequence, and new_tokens is 1
+  const int32_t* selected;  // [query][head][budget], or null
+  int32_t budget;
+  Div31 by_query;
 };
 // Elements of a row in shared memory, and tiles of 8 query rows that a warp takes at once: what its
 // registers hold of sums (at most 4, 3 for rows of 256); more rows are blocks of their own.
@@ -142,6 +183,15 @@ struct ScanParams {
   int* timeout;              // set when one ran out
   bool stall;                // fault point "scan_wait": the first chunk's products are not announced
 };
+struct DeltaParams {
+  StateView state;
+  const uint8_t *q, *k, *v, *dt, *beta;
+  uint8_t* out;
+  const float *A, *dt_bias;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, dt_token, beta_token, out_token, out_head;  // in elements
+  int32_t heads, head_dim, state_dim, heads_per_group, softplus, sigmoid, normalize;
+  float scale, eps;
+};
 // Pieces that the workspace has room for: as many as sequences whose rows do not overlap can have.  No more than there are
 // SMs and sequences, where sequences are cut.
 inline int64_t scan_pieces(const StateView& v, int32_t segment) { return v.tokens / segment + v.num_seqs; }
@@ -158,9 +208,19 @@ cudaError_t launch_attend_e4m3(const AttendParams& p, int num_sms, cudaStream_t 
 cudaError_t prepare_attend_bf16();
 cudaError_t prepare_attend_fp16();
 cudaError_t prepare_attend_e4m3();
+cudaError_t launch_attend_selected_bf16(const AttendParams& p, int num_sms, cudaStream_t s);
+cudaError_t launch_attend_selected_fp16(const AttendParams& p, int num_sms, cudaStream_t s);
+cudaError_t launch_attend_selected_e4m3(const AttendParams& p, int num_sms, cudaStream_t s);
+cudaError_t prepare_attend_selected_bf16();
+cudaError_t prepare_attend_selected_fp16();
+cudaError_t prepare_attend_selected_e4m3();
+cudaError_t launch_rotary(const RotaryParams& p, int type, int cache_type, int num_sms, cudaStream_t s);
+cudaError_t launch_bounds(const BoundsParams& p, int cache_type, cudaStream_t s);
+cudaError_t launch_select(const SelectParams& p, int type, cudaStream_t s);
 cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
 cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s);
 cudaError_t launch_scan(const ScanParams& p, int type, int num_sms, cudaStream_t s);
+cudaError_t launch_delta(const DeltaParams& p, int type, int num_sms, cudaStream_t s);
 cudaError_t launch_scan_chunks(const ScanParams& p, int type, cudaStream_t s);
 
 #ifdef __CUDACC__

@@ -1,0 +1,401 @@
+// select_kernels.cu -- the bounds of pages' keys, and the pages that each query picks by them.
+//
+//   score(page) = max over the head's query rows of step * (w+ . high + w- . low), times the page's size
+//
+// with w+ and w- the positive and the negative part of the row rounded to whole numbers of its step, low and high the page's
+// bounds: one product over twice the elements, and no less than the rounded row's product with any key of the page.  Everything in it is whole and below
+// 2^24, so the order of the sums does not show, and the same pages are picked whatever the batch.
+#include <algorithm>
+#include <cfloat>
+#include <type_traits>
+
+#include "mma.cuh"
+
+namespace kvx {
+namespace {
+
+// ---------------------------------------------------------------- bounds
+
+constexpr int kBoundsThreads = 128;
+
+// The least and the greatest of two pairs of keys, and whether there is one that is not finite.
+template <class C>
+struct Pairs {
+  using V = __nv_bfloat162;
+};
+template <>
+struct Pairs<Fp16> {
+  using V = __half2;
+};
+template <class C>
+__device__ __forceinline__ uint32_t least2(uint32_t a, uint32_t b) {
+  using V = typename Pairs<C>::V;
+  const V v = __hmin2(*reinterpret_cast<const V*>(&a), *reinterpret_cast<const V*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <class C>
+__device__ __forceinline__ uint32_t most2(uint32_t a, uint32_t b) {
+  using V = typename Pairs<C>::V;
+  const V v = __hmax2(*reinterpret_cast<const V*>(&a), *reinterpret_cast<const V*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// Two e4m3 values as fp16.
+__device__ __forceinline__ uint32_t widen2(uint32_t v) {
+  uint32_t r;
+  asm("{\n .reg .b16 a;\n cvt.u16.u32 a, %1;\n cvt.rn.f16x2.e4m3x2 %0, a;\n}" : "=r"(r) : "r"(v & 0xFFFFu));
+  return r;
+}
+
+// A warp has one head of one page: its lanes have a row's vectors, some rows at once, and meet at the end.  C: the type
+// that keys are compared in (fp16 for e4m3).  Bound by the keys' bytes.
+template <class C, bool kWide, int kVecs>  // kVecs: vectors of a row, rounded up to a power of two
+__global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsParams p) {
+  wait_for_previous();
+  const PagesView& v = p.pages;
+  constexpr int kPairs = kWide ? 8 : 4;  // of a vector
+  constexpr int kRows = 32 / kVecs;
+  const int lane = threadIdx.x & 31, vec = lane % kVecs, sub = lane / kVecs;
+  const int64_t unit = (int64_t)blockIdx.x * (kBoundsThreads / 32) + (threadIdx.x >> 5);
+  const int64_t sp = unit / v.heads;
+  const int32_t h = (int32_t)(unit - sp * v.heads), s = (int32_t)(sp / p.pages_each), n = (int32_t)(sp - (int64_t)s * p.pages_each);
+  if (s >= v.num_seqs) return;
+  if (n == 0 && h == 0 && lane == 0) check_length(v, s);
+  const int32_t length = length_of(v, s), block = (int32_t)v.by_block.d;
+  const int32_t first = (int32_t)quotient(v.by_block, (uint32_t)max(length - p.new_tokens, 0)), page = first + n;
+  if ((int64_t)page * block >= length) return;
+  const int32_t held = min(block, length - page * block);
+  const uint32_t row = row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)page * block);
+  if (row == kNoRow) return;
+  const uint32_t number = row / v.page_rows;
+  const uint8_t* from = v.base + row * v.row_bytes + h * v.head_bytes + vec * 16;
+  const int64_t step = v.token_rows * v.row_bytes;
+  const bool used = vec * 16 < v.row_bytes;
+  constexpr uint32_t kInf = std::is_same<C, Bf16>::value ? 0x7F807F80u : 0x7C007C00u;
+  uint32_t low[kPairs], high[kPairs], carries = 0;
+#pragma unroll
+  for (int k = 0; k < kPairs; ++k) low[k] = kInf, high[k] = kInf | 0x80008000u;
+#pragma unroll 8
+  for (int32_t t = sub; t < held; t += kRows) {
+    const uint4 x = used ? __ldg(reinterpret_cast<const uint4*>(from + t * step)) : make_uint4(0, 0, 0, 0);
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      const uint32_t u = kWide ? widen2(w[k / 2] >> k % 2 * 16) : w[k];
+      low[k] = least2<C>(low[k], u), high[k] = most2<C>(high[k], u);
+      carries |= odd_carry<C>(u);
+    }
+  }
+#pragma unroll
+  for (int m = kVecs; m < 32; m <<= 1)
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+      low[k] = least2<C>(low[k], __shfl_xor_sync(~0u, low[k], m));
+      high[k] = most2<C>(high[k], __shfl_xor_sync(~0u, high[k], m));
+    }
+  float most = 0.f;
+  float2 lo[kPairs], hi[kPairs];
+#pragma unroll
+  for (int k = 0; k < kPairs; ++k) {
+    lo[k] = unpack2<C>(low[k]), hi[k] = unpack2<C>(high[k]);
+    if (used) most = fmaxf(most, fmaxf(fmaxf(fabsf(lo[k].x), fabsf(lo[k].y)), fmaxf(fabsf(hi[k].x), fabsf(hi[k].y))));
+  }
+  const bool odd = __any_sync(~0u, odd_carried(carries));
+#pragma unroll
+  for (int m = kVecs / 2; m; m >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, m));
+  const float size = odd ? FLT_MAX : __fdiv_rn(most, 127.f);
+  const int64_t at = (int64_t)number * v.heads + h;
+  if (lane == 0) p.sizes[at] = size;
+  if (sub || !used) return;
+  auto whole = [&](float x, bool up) -> uint32_t {
+    float r = size > 0.f ? __fdiv_rn(x, size) : 0.f;
+    r = up ? ceilf(r) : floorf(r);
+    return (uint32_t)(int32_t)fminf(fmaxf(r, -127.f), 127.f) & 0xFFu;
+  };
+  uint32_t out[2][kPairs / 2];
+#pragma unroll
+  for (int k = 0; k < kPairs; k += 2) {
+    out[0][k / 2] = odd ? 0x81818181u : whole(lo[k].x, false) | whole(lo[k].y, false) << 8 | whole(lo[k + 1].x, false) << 16 | whole(lo[k + 1].y, false) << 24;
+    out[1][k / 2] = odd ? 0x7F7F7F7Fu : whole(hi[k].x, true) | whole(hi[k].y, true) << 8 | whole(hi[k + 1].x, true) << 16 | whole(hi[k + 1].y, true) << 24;
+  }
+  int8_t* to = p.boxes + at * 2 * v.head_dim + vec * 2 * kPairs;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    if constexpr (kWide)
+      *reinterpret_cast<uint4*>(to + k * v.head_dim) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
+    else
+      *reinterpret_cast<uint2*>(to + k * v.head_dim) = make_uint2(out[k][0], out[k][1]);
+  }
+}
+
+template <class C, bool kWide>
+cudaError_t bounds(const BoundsParams& p, cudaStream_t s) {
+  const int64_t warps = (int64_t)p.pages.num_seqs * p.pages_each * p.pages.heads;
+  const dim3 grid((unsigned)((warps * 32 + kBoundsThreads - 1) / kBoundsThreads));
+  const int64_t vecs = p.pages.row_bytes / 16;
+  auto kernel = vecs <= 4 ? bounds_kernel<C, kWide, 4> : vecs <= 8 ? bounds_kernel<C, kWide, 8> : vecs <= 16 ? bounds_kernel<C, kWide, 16> : bounds_kernel<C, kWide, 32>;
+  return launch_after(kernel, grid, kBoundsThreads, 0, s, p);
+}
+
+// ---------------------------------------------------------------- scores
+
+constexpr int kScoreThreads = 2 * kScorePages;  // 16 pages a warp
+
+// Elements of a row of whole queries in shared memory: both bounds', padded to 64, and 8 bytes so that eight rows' reads of
+// 8 bytes meet no bank twice.
+__host__ __device__ constexpr int32_t score_pitch(int32_t head_dim) { return (2 * head_dim + 63) / 64 * 64 + 4; }
+__host__ __device__ constexpr int32_t score_smem(int32_t head_dim, int32_t rows) {
+  return (rows + 7) / 8 * 8 * (score_pitch(head_dim) * 2 + 4) + kScorePages * ((rows + 7) / 8 * 8 + 1) * 4;
+}
+constexpr int32_t kScoreMaxSmem = score_smem(256, kMaxScoreGroup);
+static_assert(kScoreMaxSmem <= 232448, "shared memory of an SM");
+
+// Four bytes as whole numbers in fp16: 1024 + (byte ^ 128) put together from bits, less 1152.
+__device__ __forceinline__ void halves_of(uint32_t bytes, uint32_t& a, uint32_t& b) {
+  const uint32_t u = bytes ^ 0x80808080u;
+  const __half2 off = __floats2half2_rn(-1152.f, -1152.f);
+  uint32_t w[2] = {__byte_perm(u, 0x64646464u, 0x4140), __byte_perm(u, 0x64646464u, 0x4342)};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const __half2 h = __hadd2(*reinterpret_cast<const __half2*>(&w[k]), off);
+    w[k] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  a = w[0], b = w[1];
+}
+
+// A CTA scores 64 pages of one sequence for one KV head: its queries are made whole numbers in shared memory, as the
+// right factor of products of 16 pages by 8 query rows with k over the low and the high bounds.  (Bytes are widened to fp16, in
+// which they and all their products are exact, as are the sums in fp32.)  The elements of k are taken in an order that lets
+// a lane load 16 neighbouring bytes of a page's bounds.
+template <class E>
+__global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_constant__ SelectParams p) {
+  wait_for_previous();
+  const PagesView& v = p.pages;
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, c = lane & 3;
+  const int32_t unit = blockIdx.x / p.score_tiles, h = blockIdx.y;
+  const int32_t s = unit / p.score_parts, t0 = (unit - s * p.score_parts) * p.tokens_each;
+  const int32_t tokens = min(p.tokens_each, p.new_tokens - t0);
+  const int32_t length = length_of(v, s), block = (int32_t)v.by_block.d;
+  const int32_t pages = length > 0 ? (int32_t)quotient(v.by_block, (uint32_t)(length - 1)) + 1 : 0;  // up to the last query's
+  const int32_t page0 = (blockIdx.x - unit * p.score_tiles) * kScorePages;
+  if (pages <= p.budget || page0 >= pages) return;  // all are picked
+  const int32_t rows = p.group * tokens, tiles = (rows + 7) / 8;
+  const int32_t k_all = 2 * v.head_dim, k_pad = (k_all + 63) / 64 * 64, pitch = score_pitch(v.head_dim);
+  __half* q_s = reinterpret_cast<__half*>(smem);                       // [8 tiles rows][pitch]
+  float* step_s = reinterpret_cast<float*>(q_s + tiles * 8 * pitch);   // [8 tiles]
+  float* dots = step_s + tiles * 8;                                    // [warp][16 pages][8 tiles + 1]
+
+  // A page's bounds are under way while the queries are made ready.
+  const int32_t* table = v.tables + s * v.table_stride;
+  const uint8_t* box[2];
+  bool there[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int32_t page = page0 + warp * 16 + quad + 8 * k;
+    uint32_t row = kNoRow;
+    if (page < pages) row = row_index(v, table, v.table_len, (uint32_t)page * block);
+    there[k] = row != kNoRow;
+    box[k] = reinterpret_cast<const uint8_t*>(p.boxes) + ((int64_t)(there[k] ? row / v.page_rows : 0) * v.heads + h) * k_all;
+  }
+
+  for (int32_t r = warp; r < tiles * 8; r += kScoreThreads / 32) {
+    const bool real = r < rows;
+    const int32_t t = real ? r / p.group : 0, i = real ? r - t * p.group : 0;
+    const typename E::T* q = reinterpret_cast<const typename E::T*>(p.q + ((int64_t)s * p.new_tokens + t0 + t) * p.q_token + (h * p.group + i) * p.q_head);
+    float top = 0.f;
+    bool fine = true;
+    for (int32_t d = lane; d < v.head_dim; d += 32) {
+      const float x = E::up(q[d]);
+      fine &= isfinite(x);
+      top = fmaxf(top, fabsf(x));
+    }
+    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
+    fine = __all_sync(~0u, fine) && real;
+    const float step = fine ? __fdiv_rn(top, 127.f) : 0.f;
+    if (lane == 0) step_s[r] = step;
+    for (int32_t d = lane; d < k_pad / 2; d += 32) {  // what is behind the last element, zeros
+      const float w = d < v.head_dim && step > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(E::up(q[d]), step)), -127.f), 127.f) : 0.f;
+      if (d < v.head_dim) {
+        q_s[r * pitch + d] = __float2half_rn(fminf(w, 0.f));
+        q_s[r * pitch + v.head_dim + d] = __float2half_rn(fmaxf(w, 0.f));
+      }
+    }
+    for (int32_t d = k_all + lane; d < k_pad; d += 32) q_s[r * pitch + d] = __float2half_rn(0.f);
+  }
+  __syncthreads();
+  const int32_t dot_pitch = tiles * 8 + 1;
+  float* mine = dots + warp * 16 * dot_pitch;
+  for (int32_t tile0 = 0; tile0 < tiles; tile0 += 4) {  // 32 rows at a time
+    float acc[4][4] = {};
+    for (int32_t k0 = 0; k0 < k_pad; k0 += 64) {
+      const int32_t at = k0 + c * 16;  // bytes of a page's bounds, and elements of a row
+      uint4 x[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) x[k] = there[k] && at < k_all ? __ldg(reinterpret_cast<const uint4*>(box[k] + at)) : make_uint4(0, 0, 0, 0);
+      const uint32_t w[2][4] = {{x[0].x, x[0].y, x[0].z, x[0].w}, {x[1].x, x[1].y, x[1].z, x[1].w}};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint32_t a[4];
+        halves_of(w[0][u], a[0], a[2]);
+        halves_of(w[1][u], a[1], a[3]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          if (tile0 + t >= tiles) break;
+          const uint2 b = *reinterpret_cast<const uint2*>(q_s + ((tile0 + t) * 8 + quad) * pitch + at + 4 * u);
+          mma<Fp16>(acc[t], a, b.x, b.y);
+        }
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (tile0 + t >= tiles) break;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int32_t r = (tile0 + t) * 8 + 2 * c + (e & 1);
+        mine[(quad + 8 * (e >> 1)) * dot_pitch + r] = __fmul_rn(acc[t][e], step_s[r]);
+      }
+    }
+  }
+  // the page's size; -inf where no page is named
+  const uint32_t live = __ballot_sync(~0u, there[0] && c == 0), live8 = __ballot_sync(~0u, there[1] && c == 0);
+  __syncwarp();
+  for (int32_t i = lane; i < 16 * tokens; i += 32) {
+    const int32_t t = i / 16, in = i % 16, page = page0 + warp * 16 + in;
+    if (page >= pages) continue;
+    float top = -INFINITY;
+    if ((in < 8 ? live : live8) >> (in % 8 * 4) & 1) {
+      for (int32_t r = t * p.group; r < (t + 1) * p.group; ++r) top = fmaxf(top, mine[in * dot_pitch + r]);
+      const uint32_t row = row_index(v, table, v.table_len, (uint32_t)page * block);
+      top = __fmul_rn(top, p.sizes[(int64_t)(row / v.page_rows) * v.heads + h]);
+    }
+    p.scores[(((int64_t)s * p.new_tokens + t0 + t) * v.heads + h) * p.score_stride + page] = top;
+  }
+}
+
+// ---------------------------------------------------------------- the best
+
+constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
+constexpr int kPickBins = 2048;  // digits of 11, 11 and 10 bits
+
+// Whole numbers in the order of the scores: NaN as -inf, -0 as +0.  None is kAlways.
+constexpr uint32_t kAlwaysPicked = UINT32_MAX;
+__device__ __forceinline__ uint32_t score_rank(float w) {
+  const uint32_t u = __float_as_uint(fmaxf(w, -INFINITY) + 0.f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ uint32_t upto_lane(uint32_t v) {
+  const int lane = threadIdx.x & 31;
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint32_t y = __shfl_up_sync(~0u, v, d);
+    if (lane >= d) v += y;
+  }
+  return v;
+}
+
+// A CTA picks the pages of one query and head: the smallest picked score is the budget'th largest, found 11 bits at a time by
+// counting; of the pages that have just that score the first ones are picked, and a page's place among the picked
+// follows from a scan, so that they come out in their order.
+__global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constant__ SelectParams p) {
+  wait_for_previous();
+  const PagesView& v = p.pages;
+  __shared__ int32_t hist[kPickBins];
+  __shared__ uint32_t warp_counts[kPickWarps];
+  __shared__ uint32_t prefix_s;
+  __shared__ int32_t want_s;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int32_t token = blockIdx.x / v.heads, h = blockIdx.x - token * v.heads;
+  const int32_t s = token / p.new_tokens, t = token - s * p.new_tokens;
+  if (threadIdx.x == 0 && h == 0 && t == 0) check_length(v, s);
+  const int32_t at = length_of(v, s) - p.new_tokens + t;  // the query's position
+  const int32_t n = at < 0 ? 0 : (int32_t)quotient(v.by_block, (uint32_t)at) + 1;
+  int32_t* out = p.selected + ((int64_t)token * v.heads + h) * p.budget;
+  const int32_t keep = min(n, p.budget);
+  for (int32_t i = keep + threadIdx.x; i < p.budget; i += kPickThreads) out[i] = -1;
+  if (n <= p.budget) {
+    for (int32_t i = threadIdx.x; i < n; i += kPickThreads) out[i] = i;
+    return;
+  }
+  const float* scores = p.scores + ((int64_t)token * v.heads + h) * p.score_stride;
+  const int32_t last = n - p.recent;
+  auto rank = [&](int32_t i) { return i < p.sinks || i >= last ? kAlwaysPicked : score_rank(scores[i]); };
+  int32_t want = keep;
+  uint32_t prefix = 0;
+  auto digit = [&](int kAt, int kBits) {
+    for (int32_t i = threadIdx.x; i < kPickBins; i += kPickThreads) hist[i] = 0;
+    __syncthreads();
+    for (int32_t i = threadIdx.x; i < n; i += kPickThreads) {
+      const uint32_t r = rank(i);
+      if (kAt + kBits == 32 || r - prefix < 1u << (kAt + kBits)) atomicAdd(&hist[r >> kAt & ((1u << kBits) - 1)], 1);
+    }
+    __syncthreads();
+    // the digit of the want'th largest: sums from the top, four bins a thread
+    int32_t b[4], sum = 0;
+    const int32_t top_bin = kPickBins - 1 - 4 * (int32_t)threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) b[k] = hist[top_bin - k], sum += b[k];
+    const int32_t upto = (int32_t)upto_lane(sum);
+    if (lane == 31) warp_counts[warp] = upto;
+    __syncthreads();
+    int32_t before = upto - sum;
+    for (int i = 0; i < warp; ++i) before += warp_counts[i];
+    int32_t left = want - before;
+    if (left > 0 && left <= sum) {  // one thread's
+      int k = 0;
+      while (left > b[k]) left -= b[k++];
+      prefix_s = prefix | (uint32_t)(top_bin - k) << kAt;
+      want_s = left;
+    }
+    __syncthreads();
+    prefix = prefix_s;
+    want = want_s;
+  };
+  digit(21, 11);
+  digit(10, 11);
+  digit(0, 10);
+  // want: how many pages of rank `prefix` itself are picked
+  int32_t above_all = 0, equal_all = 0;
+  for (int32_t base = 0; base < n; base += kPickThreads) {
+    const int32_t i = base + threadIdx.x;
+    const uint32_t r = i < n ? rank(i) : 0;
+    const bool above = i < n && r > prefix, equal = i < n && r == prefix;
+    const uint32_t mine = (uint32_t)above | (uint32_t)equal << 16, upto = upto_lane(mine);
+    __syncthreads();
+    if (lane == 31) warp_counts[warp] = upto;
+    __syncthreads();
+    uint32_t before = upto - mine, all = 0;
+    for (int w = 0; w < kPickWarps; ++w) {
+      if (w < warp) before += warp_counts[w];
+      all += warp_counts[w];
+    }
+    const int32_t a = above_all + (int32_t)(before & 0xFFFF), e = equal_all + (int32_t)(before >> 16);
+    if (above || (equal && e < want)) out[a + min(e, want)] = i;
+    above_all += (int32_t)(all & 0xFFFF), equal_all += (int32_t)(all >> 16);
+  }
+}
+
+template <class E>
+cudaError_t scores(const SelectParams& p, cudaStream_t s) {
+  const dim3 grid((unsigned)((int64_t)p.score_tiles * p.score_parts * p.pages.num_seqs), p.pages.heads);
+  return launch_after(score_kernel<E>, grid, kScoreThreads, (size_t)score_smem(p.pages.head_dim, p.group * p.tokens_each), s, p);
+}
+
+}  // namespace
+
+cudaError_t launch_bounds(const BoundsParams& p, int cache_type, cudaStream_t s) {
+  return cache_type == KVX_TYPE_E4M3 ? bounds<Fp16, true>(p, s) : cache_type == KVX_TYPE_BF16 ? bounds<Bf16, false>(p, s) : bounds<Fp16, false>(p, s);
+}
+
+cudaError_t launch_select(const SelectParams& p, int type, cudaStream_t s) {
+  if (p.score_tiles) {
+    const cudaError_t e = type == KVX_TYPE_BF16 ? scores<Bf16>(p, s) : scores<Fp16>(p, s);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_after(pick_kernel, dim3((unsigned)(p.pages.heads * p.pages.num_seqs * p.new_tokens)), kPickThreads, 0, s, p);
+}
+
+cudaError_t prepare_select_kernels() {
+  const cudaError_t e = cudaFuncSetAttribute(score_kernel<Bf16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kScoreMaxSmem);
+  return e == cudaSuccess ? cudaFuncSetAttribute(score_kernel<Fp16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kScoreMaxSmem) : e;
+}
+
+}  // namespace kvx

@@ -43,7 +43,8 @@ EXPORTED = (
     "kv_tier_open_shared", "kv_tier_poll", "kv_tier_reclaim", "kv_host_alloc_numa", "kv_host_alloc_ex",
     "kv_host_pool_info", "kv_host_touch", "kv_tier_wait",
     "kv_append", "kv_attend", "kv_attend_workspace", "kv_evict", "kv_state_conv", "kv_state_scan",
-    "kv_state_scan_workspace",
+    "kv_state_scan_workspace", "kv_append_rotary", "kv_bounds", "kv_select", "kv_select_workspace", "kv_attend_selected",
+    "kv_attend_selected_workspace", "kv_state_delta", "kv_state_delta_workspace",
 )
 KVX_TYPE_BF16, KVX_TYPE_FP16, KVX_TYPE_E4M3 = 0, 1, 2
 KVX_ATTEND_MAX_NEW_TOKENS = 64
@@ -124,6 +125,25 @@ class kvx_eviction(ctypes.Structure):
                 ("new_weights_seq_stride", ctypes.c_int64), ("new_weights_head_stride", ctypes.c_int64)]
 
 
+class kvx_rotary(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("rotary_scale", ctypes.c_float), ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("weight_offset", ctypes.c_float), ("q_token_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("out_token_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64)]
+
+
+class kvx_bounds(ctypes.Structure):
+    _fields_ = [("boxes", ctypes.c_void_p), ("sizes", ctypes.c_void_p)]
+
+
+class kvx_selection(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("new_tokens", ctypes.c_int32),
+                ("budget", ctypes.c_int32), ("sinks", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64)]
+
+
 class kvx_state(ctypes.Structure):
     _fields_ = [("base", ctypes.c_void_p), ("num_slots", ctypes.c_int64), ("slot_bytes", ctypes.c_int64),
                 ("recurrent_offset", ctypes.c_int64), ("conv_offset", ctypes.c_int64)]
@@ -148,6 +168,18 @@ class kvx_scan(ctypes.Structure):
                 ("dt_token_stride", ctypes.c_int64),
                 ("b_token_stride", ctypes.c_int64), ("b_group_stride", ctypes.c_int64),
                 ("c_token_stride", ctypes.c_int64), ("c_group_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
+
+
+class kvx_delta(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("state_dim", ctypes.c_int32), ("groups", ctypes.c_int32), ("softplus", ctypes.c_int32),
+                ("sigmoid", ctypes.c_int32), ("normalize", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("eps", ctypes.c_float), ("A", ctypes.c_void_p), ("dt_bias", ctypes.c_void_p),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64),
+                ("k_token_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+                ("v_token_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+                ("dt_token_stride", ctypes.c_int64), ("beta_token_stride", ctypes.c_int64),
                 ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64)]
 
 
@@ -207,10 +239,18 @@ def _declare(lib):
         "kv_append": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_new_rows), vp, vp, vp]),
         "kv_attend_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_attention), P(i64)]),
         "kv_attend": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_attention), vp, vp, vp, i64, vp]),
+        "kv_append_rotary": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_new_rows), P(kvx_rotary), vp, vp, vp, vp, vp]),
+        "kv_bounds": (st, [vp, P(kvx_pool), i32, P(kvx_batch), i32, i64, P(kvx_bounds), vp]),
+        "kv_select_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_selection), P(i64)]),
+        "kv_select": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_bounds), P(kvx_selection), vp, vp, vp, i64, vp]),
+        "kv_attend_selected_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_attention), i32, P(i64)]),
+        "kv_attend_selected": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_attention), i32, vp, vp, vp, vp, i64, vp]),
         "kv_evict": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_eviction), vp]),
         "kv_state_conv": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_conv), vp, vp, vp]),
         "kv_state_scan_workspace": (st, [vp, P(kvx_state_batch), P(kvx_scan), P(i64)]),
         "kv_state_scan": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_scan), vp, vp, vp, vp, vp, vp, i64, vp]),
+        "kv_state_delta_workspace": (st, [vp, P(kvx_state_batch), P(kvx_delta), P(i64)]),
+        "kv_state_delta": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_delta), vp, vp, vp, vp, vp, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -778,6 +818,62 @@ def kv_append(ctx, pool: KvPool, layer: int, batch: KvBatch, key, value, new_tok
                           key.data_ptr(), value.data_ptr(), _stream_handle(stream)), "kv_append")
 
 
+class KvRotary:
+    """How queries and keys are normed and rotated, marshalled once: inv_freq (device float32 [rotary_dim / 2], radians a
+    position), interleaved (pairs (2i, 2i + 1); else (i, i + rotary_dim / 2)), scale (of cosine and sine; not 0), q_weight
+    and k_weight (device [head_dim] of the rows' type; None: no norm), eps, and weight_offset (1 for weights stored less 1)."""
+
+    def __init__(self, q_heads: int, inv_freq=None, interleaved: bool = False, scale: float = 1.0, q_weight=None,
+                 k_weight=None, eps: float = 1e-6, weight_offset: float = 0.0):
+        if inv_freq is not None:
+            if inv_freq.dim() != 1:
+                raise ValueError("inv_freq must be [rotary_dim / 2]")
+            _need(inv_freq, "inv_freq", "float32")
+        if scale == 0:
+            raise ValueError("a scale of 0 is the library's mark for 1")
+        for w, what in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+            if w is not None:
+                if w.dim() != 1:
+                    raise ValueError(f"{what} must be [head_dim]")
+                _check_tensor(w, what)
+        self.q_heads, self.inv_freq, self.q_weight, self.k_weight = q_heads, inv_freq, q_weight, k_weight
+        self._c = kvx_rotary(q_heads, 0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, scale,
+                             None if inv_freq is None else inv_freq.data_ptr(), None,
+                             None if q_weight is None else q_weight.data_ptr(),
+                             None if k_weight is None else k_weight.data_ptr(), eps, weight_offset)
+
+
+def kv_append_rotary(ctx, pool: KvPool, layer: int, batch: KvBatch, rotary: KvRotary, query, key, value, query_out,
+                     positions=None, new_tokens: int = 1, starts=None, k_scale: float = 1.0, v_scale: float = 1.0,
+                     cache_dtype=None, stream=None) -> None:
+    """kv_append of keys that are normed and rotated on their way, and the queries [tokens][q_heads][head_dim] with them,
+    to query_out (which may be query).  positions: device int32 [tokens], where they are not the tokens' places
+    in the cache (after an eviction)."""
+    tokens = key.shape[0] if starts is not None else batch.num_seqs * new_tokens
+    shape = (tokens, pool.num_heads, pool.head_dim)
+    _need_rows(key, "key", key.dtype, shape)
+    _need_rows(value, "value", key.dtype, shape)
+    _need_rows(query, "query", key.dtype, (tokens, rotary.q_heads, pool.head_dim))
+    _need_rows(query_out, "query_out", key.dtype, query.shape)
+    if starts is not None:
+        _need(starts, "starts", "int32", (batch.num_seqs + 1,))
+    for w, what in ((rotary.q_weight, "q_weight"), (rotary.k_weight, "k_weight")):
+        if w is not None:
+            _need_rows(w, what, key.dtype, (pool.head_dim,))
+    r = kvx_rotary.from_buffer_copy(rotary._c)
+    if positions is not None:
+        _need(positions, "positions", "int32", (tokens,))
+        r.positions = positions.data_ptr()
+    r.q_token_stride, r.q_head_stride, _ = query.stride()
+    r.out_token_stride, r.out_head_stride, _ = query_out.stride()
+    ks, vs = key.stride(), value.stride()
+    rows = kvx_new_rows(_type_of(key.dtype), _cache_type(pool, cache_dtype), tokens, new_tokens,
+                        None if starts is None else starts.data_ptr(), ks[0], ks[1], vs[0], vs[1], k_scale, v_scale)
+    _check(_lib.kv_append_rotary(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(rows),
+                                 ctypes.byref(r), query.data_ptr(), key.data_ptr(), value.data_ptr(), query_out.data_ptr(),
+                                 _stream_handle(stream)), "kv_append_rotary")
+
+
 class KvAttention:
     """What an attention computes, marshalled once: query heads, tokens of each sequence that attend,
     scale (None: 1/sqrt(head_dim); not 0), softcap, window, slopes (device float32 [q_heads]; a bias of
@@ -838,6 +934,115 @@ def kv_attend(ctx, pool: KvPool, layer: int, batch: KvBatch, attention: KvAttent
     _check(_lib.kv_attend(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(c),
                           query.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
                           _stream_handle(stream)), "kv_attend")
+
+
+class KvBounds:
+    """The bounds of one layer's pages: boxes (device int8 [num_blocks][heads][2][head_dim], low and high) and sizes (device
+    float32 [num_blocks][heads]), which kv_bounds makes and kv_select reads."""
+
+    def __init__(self, boxes, sizes):
+        if boxes.dim() != 4 or boxes.shape[2] != 2:
+            raise ValueError("boxes must be [num_blocks][heads][2][head_dim]")
+        _need(boxes, "boxes", "int8")
+        _need(sizes, "sizes", "float32", tuple(boxes.shape[:2]))
+        _check_tensor(boxes, "boxes")
+        _check_tensor(sizes, "sizes")
+        self.boxes, self.sizes = boxes, sizes
+        self._c = kvx_bounds(boxes.data_ptr(), sizes.data_ptr())
+
+    @classmethod
+    def for_pool(cls, pool: KvPool) -> "KvBounds":
+        """New ones for a layer of the pool, on its device."""
+        import torch
+        shape, device = (pool.num_blocks, pool.num_heads), pool.layers[0].device
+        return cls(torch.zeros(shape + (2, pool.head_dim), dtype=torch.int8, device=device),
+                   torch.zeros(shape, dtype=torch.float32, device=device))
+
+    def _of(self, pool: KvPool):
+        want = (pool.num_blocks, pool.num_heads, 2, pool.head_dim)
+        if tuple(self.boxes.shape) != want:
+            raise ValueError(f"boxes are {tuple(self.boxes.shape)}, not {want}")
+        return ctypes.byref(self._c)
+
+
+def kv_bounds(ctx, pool: KvPool, layer: int, batch: KvBatch, bounds: KvBounds, new_tokens: int = 1, cache_dtype=None,
+              stream=None) -> None:
+    """Make the bounds of the pages that hold every sequence's last new_tokens tokens (as many as the longest has: of all
+    its pages)."""
+    _check(_lib.kv_bounds(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), _cache_type(pool, cache_dtype),
+                          new_tokens, bounds._of(pool), _stream_handle(stream)), "kv_bounds")
+
+
+class KvSelection:
+    """How many pages each query picks: budget in all, of them the sequence's first `sinks` and the query's last `recent`
+    whatever their scores."""
+
+    def __init__(self, q_heads: int, budget: int, sinks: int = 1, recent: int = 1, new_tokens: int = 1):
+        self.q_heads, self.budget, self.new_tokens = q_heads, budget, new_tokens
+        self._c = kvx_selection(KVX_TYPE_BF16, q_heads, new_tokens, budget, sinks, recent)
+
+
+def kv_select_workspace(ctx, pool: KvPool, batch: KvBatch, selection: KvSelection):
+    """A workspace tensor for kv_select calls of these shapes; one call uses it at a time."""
+    import torch
+    out = ctypes.c_int64()
+    _check(_lib.kv_select_workspace(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(selection._c),
+                                    ctypes.byref(out)), "kv_select_workspace")
+    return torch.empty(max(16, out.value), dtype=torch.uint8, device=batch.lengths.device)
+
+
+def kv_select(ctx, pool: KvPool, batch: KvBatch, bounds: KvBounds, selection: KvSelection, query, selected, workspace,
+              stream=None) -> None:
+    """Pick pages for every sequence's last new_tokens queries [sequences * new_tokens][q_heads][head_dim] by the bounds
+    of their keys: selected (int32 [sequences * new_tokens][heads][budget]) gets their places in the
+    sequence, ascending, -1 behind the last."""
+    tokens = batch.num_seqs * selection.new_tokens
+    _need_rows(query, "query", query.dtype, (tokens, selection.q_heads, pool.head_dim))
+    _need(selected, "selected", "int32", (tokens, pool.num_heads, selection.budget))
+    _check_tensor(selected, "selected")
+    c = kvx_selection.from_buffer_copy(selection._c)
+    c.type = _type_of(query.dtype)
+    c.q_token_stride, c.q_head_stride, _ = query.stride()
+    _check(_lib.kv_select(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), bounds._of(pool), ctypes.byref(c),
+                          query.data_ptr(), selected.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                          _stream_handle(stream)), "kv_select")
+
+
+def kv_attend_selected_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttention, budget: int, dtype=None):
+    """A workspace tensor for kv_attend_selected calls of these shapes, as kv_attend_workspace's."""
+    import torch
+    c = kvx_attention.from_buffer_copy(attention._c)
+    c.cache_type = _cache_type(pool, attention.cache_dtype)
+    c.type = _type_of(dtype) if dtype is not None else KVX_TYPE_BF16 if c.cache_type == KVX_TYPE_E4M3 else c.cache_type
+    out = ctypes.c_int64()
+    _check(_lib.kv_attend_selected_workspace(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(c), budget,
+                                             ctypes.byref(out)), "kv_attend_selected_workspace")
+    return torch.empty(max(16, out.value), dtype=torch.uint8, device=batch.lengths.device)
+
+
+def kv_attend_selected(ctx, pool: KvPool, layer: int, batch: KvBatch, attention: KvAttention, selected, query, out,
+                       workspace, lse=None, stream=None) -> None:
+    """kv_attend over the tokens of selected pages alone (int32 [sequences * new_tokens][heads][budget], from
+    kv_select), each query up to its own position."""
+    shape = (batch.num_seqs * attention.new_tokens, attention.q_heads, pool.head_dim)
+    _need_rows(query, "query", query.dtype, shape)
+    _need_rows(out, "out", query.dtype, shape)
+    if selected.dim() != 3:
+        raise ValueError("selected must be [sequences * new_tokens][heads][budget]")
+    _need(selected, "selected", "int32", (shape[0], pool.num_heads, selected.shape[2]))
+    _check_tensor(selected, "selected")
+    c = kvx_attention.from_buffer_copy(attention._c)
+    c.type = _type_of(query.dtype)
+    c.cache_type = _cache_type(pool, attention.cache_dtype)
+    c.q_token_stride, c.q_head_stride, _ = query.stride()
+    c.out_token_stride, c.out_head_stride, _ = out.stride()
+    if lse is not None:
+        _need(lse, "lse", "float32", shape[:2])
+        _check_tensor(lse, "lse")
+        c.lse = lse.data_ptr()
+    _check(_lib.kv_attend_selected(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(c),
+                                   selected.shape[2], selected.data_ptr(), query.data_ptr(), out.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_attend_selected")
 
 
 def kv_evict(ctx, pool: KvPool, batch: KvBatch, weights, budget: int, new_tables, kept, new_lengths,
@@ -958,6 +1163,54 @@ def kv_state_scan(ctx, state: StateSlots, batch: StateBatch, x, dt, A, B, C, out
                               None if workspace is None else workspace.data_ptr(),
                               0 if workspace is None else workspace.numel(), _stream_handle(stream)),
            "kv_state_scan")
+
+
+def kv_state_delta_workspace(ctx, batch: StateBatch, heads: int, head_dim: int, state_dim: int):
+    """A workspace tensor for kv_state_delta calls of these shapes; one call uses it at a time."""
+    import torch
+    c = kvx_delta(heads=heads, head_dim=head_dim, state_dim=state_dim, groups=1)
+    out = ctypes.c_int64()
+    _check(_lib.kv_state_delta_workspace(ctx, ctypes.byref(batch._c), ctypes.byref(c), ctypes.byref(out)),
+           "kv_state_delta_workspace")
+    return torch.empty(max(16, out.value), dtype=torch.uint8, device=batch._tensors[0].device)
+
+
+def kv_state_delta(ctx, state: StateSlots, batch: StateBatch, query, key, value, beta, out, dt=None, A=None, dt_bias=None,
+                   softplus: bool = True, sigmoid: bool = True, normalize: bool = True, eps: float = 1e-6,
+                   scale: float | None = None, workspace=None, stream=None) -> None:
+    """Gated delta rule of query and key [tokens][groups][state_dim], value [tokens][heads][head_dim], beta and dt
+    [tokens][heads] (dt None: no decay), A and dt_bias [heads] (float32), on the state in each sequence's slot.
+    softplus, sigmoid: of dt and beta; normalize: query and key to unit length; scale: of the queries (None:
+    1/sqrt(state_dim); not 0).  workspace: from kv_state_delta_workspace (None: none is needed for one token of each)."""
+    t, heads, head_dim = value.shape
+    groups, state_dim = key.shape[1:]
+    if scale == 0:
+        raise ValueError("a scale of 0 is the library's mark for 1/sqrt(state_dim): pass None for that")
+    if dt is not None and A is None:
+        raise ValueError("dt needs A")
+    _need_rows(value, "value", value.dtype, (batch.tokens, heads, head_dim))
+    _need_rows(out, "out", value.dtype, value.shape)
+    _need_rows(key, "key", value.dtype, (t, groups, state_dim))
+    _need_rows(query, "query", value.dtype, key.shape)
+    _need_rows(beta, "beta", value.dtype, (t, heads))
+    c = kvx_delta(_type_of(value.dtype), heads, head_dim, state_dim, groups, softplus, sigmoid, normalize, scale or 0.0, eps)
+    if dt is not None:
+        _need_rows(dt, "dt", value.dtype, (t, heads))
+        c.dt_token_stride = dt.stride(0)
+        _need(A, "A", "float32", (heads,))
+        c.A = A.data_ptr()
+        if dt_bias is not None:
+            _need(dt_bias, "dt_bias", "float32", (heads,))
+            c.dt_bias = dt_bias.data_ptr()
+    c.q_token_stride, c.q_head_stride, _ = query.stride()
+    c.k_token_stride, c.k_head_stride, _ = key.stride()
+    c.v_token_stride, c.v_head_stride, _ = value.stride()
+    c.beta_token_stride = beta.stride(0)
+    c.out_token_stride, c.out_head_stride, _ = out.stride()
+    _check(_lib.kv_state_delta(ctx, ctypes.byref(state._c), ctypes.byref(batch._c), ctypes.byref(c), query.data_ptr(),
+                               key.data_ptr(), value.data_ptr(), None if dt is None else dt.data_ptr(), beta.data_ptr(),
+                               out.data_ptr(), None if workspace is None else workspace.data_ptr(),
+                               0 if workspace is None else workspace.numel(), _stream_handle(stream)), "kv_state_delta")
 
 
 # ---------------------------------------------------------------- convenience

@@ -1,0 +1,153 @@
+"""The rotated append, the choice of pages and the delta rule without a GPU: refusals before any CUDA call, the binding's
+checks and structures, and the plain statements that the GPU tests compare with, held against worked values."""
+import ctypes
+import math
+import os
+import subprocess
+
+import pytest
+import torch
+
+import mixer_refs as refs
+import operator_refs
+from paper_2609_15021_gb300 import kvxfer as k
+
+
+def test_no_context_is_refused_before_any_cuda_call():
+    pool, batch, state, sb = k.kvx_pool(), k.kvx_batch(), k.kvx_state(), k.kvx_state_batch()
+    r, out = ctypes.byref, ctypes.c_int64()
+    assert k._lib.kv_append_rotary(None, r(pool), 0, r(batch), r(k.kvx_new_rows()), r(k.kvx_rotary()), 0, 0, 0, 0, None) == k.KVX_EINVAL
+    assert k._lib.kv_bounds(None, r(pool), 0, r(batch), 0, 1, r(k.kvx_bounds()), None) == k.KVX_EINVAL
+    assert k._lib.kv_select_workspace(None, r(pool), r(batch), r(k.kvx_selection()), r(out)) == k.KVX_EINVAL
+    assert k._lib.kv_select(None, r(pool), r(batch), r(k.kvx_bounds()), r(k.kvx_selection()), 0, 0, 0, 0, None) == k.KVX_EINVAL
+    assert k._lib.kv_attend_selected_workspace(None, r(pool), r(batch), r(k.kvx_attention()), 1, r(out)) == k.KVX_EINVAL
+    assert k._lib.kv_attend_selected(None, r(pool), 0, r(batch), r(k.kvx_attention()), 1, 0, 0, 0, 0, 0, None) == k.KVX_EINVAL
+    assert k._lib.kv_state_delta_workspace(None, r(sb), r(k.kvx_delta()), r(out)) == k.KVX_EINVAL
+    assert k._lib.kv_state_delta(None, r(state), r(sb), r(k.kvx_delta()), 0, 0, 0, 0, 0, 0, 0, 0, None) == k.KVX_EINVAL
+
+
+def test_bindings_structures_match_the_header(tmp_path):
+    """Sizes and offsets of the structures, as a C compiler lays them out."""
+    names = ["kvx_rotary", "kvx_bounds", "kvx_selection", "kvx_delta"]
+    lines = ["#include <stddef.h>", "#include <stdio.h>", '#include "kvxfer.h"', "int main(void) {"]
+    for n in names:
+        lines.append(f'  printf("{n} %zu\\n", sizeof({n}));')
+        for f in getattr(k, n)._fields_:
+            lines.append(f'  printf("{n}.{f[0]} %zu\\n", offsetof({n}, {f[0]}));')
+    src = tmp_path / "layout.c"
+    src.write_text("\n".join(lines + ["  return 0;", "}"]))
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run(["gcc", "-I", include, str(src), "-o", str(tmp_path / "layout")], check=True)
+    said = dict(l.split() for l in subprocess.run([str(tmp_path / "layout")], capture_output=True, text=True, check=True).stdout.splitlines())
+    for n in names:
+        assert int(said[n]) == ctypes.sizeof(getattr(k, n))
+        for f in getattr(k, n)._fields_:
+            assert int(said[f"{n}.{f[0]}"]) == getattr(getattr(k, n), f[0]).offset, (n, f[0])
+
+
+def test_binding_refuses_other_types_and_shapes():
+    freq = torch.ones(4)
+    with pytest.raises(TypeError):
+        k.KvRotary(2, freq.double())
+    with pytest.raises(ValueError):
+        k.KvRotary(2, freq.view(2, 2))
+    with pytest.raises(ValueError):
+        k.KvRotary(2, freq, q_weight=freq.view(2, 2))
+    with pytest.raises(ValueError):
+        k.KvRotary(2, freq, k_weight=torch.ones(8)[::2])
+    with pytest.raises(ValueError):  # the C call's mark for 1
+        k.KvRotary(2, freq, scale=0.0)
+    boxes, sizes = torch.zeros((3, 2, 2, 64), dtype=torch.int8), torch.zeros((3, 2))
+    with pytest.raises(TypeError):
+        k.KvBounds(boxes.int(), sizes)
+    with pytest.raises(TypeError):
+        k.KvBounds(boxes, sizes.double())
+    with pytest.raises(ValueError):
+        k.KvBounds(boxes, sizes[:2])
+    with pytest.raises(ValueError):
+        k.KvBounds(boxes[:, :, :1], sizes)
+    with pytest.raises(ValueError):
+        k.KvBounds(boxes[::2], sizes[::2])
+
+
+def test_rotation_by_hand():
+    """A quarter turn of the first pair, none of the second."""
+    x = torch.tensor([[[1.0, 2.0, 3.0, 4.0, 5.0]]])
+    freq = torch.tensor([math.pi / 6, 0.0])
+    got, size = refs.rotate(x, [3], freq, True, 1.0, None, 0.0, 0.0)
+    assert torch.allclose(got[0, 0], torch.tensor([-2.0, 1.0, 3.0, 4.0, 5.0], dtype=torch.float64), atol=1e-6)
+    assert size[0, 0].tolist() == [3.0, 3.0, 7.0, 7.0, 5.0]
+    got, _ = refs.rotate(x, [3], freq, False, 2.0, None, 0.0, 0.0)
+    assert torch.allclose(got[0, 0], torch.tensor([-6.0, 4.0, 2.0, 8.0, 5.0], dtype=torch.float64), atol=1e-6)
+    got, _ = refs.rotate(x, [0], None, False, 1.0, torch.tensor([0.0, 1.0, 1.0, 1.0, 1.0]), 0.0, 1.0)
+    assert torch.allclose(got[0, 0, :2], torch.tensor([1.0, 4.0], dtype=torch.float64) / math.sqrt(11.0))
+
+
+def test_bounds_hold_every_key_and_scores_every_product():
+    """A page's score is no less than the rounded query's product with any of its keys."""
+    g = torch.Generator().manual_seed(1)
+    keys = torch.randn((16, 2, 64), generator=g).to(torch.bfloat16)
+    box, size = refs.bounds_of(keys)
+    k64 = keys.double()
+    by = size.double()[:, None]
+    assert bool((box[:, 0].double() * by <= k64.amin(0) + 1e-6).all()) and bool((box[:, 1].double() * by >= k64.amax(0) - 1e-6).all())
+    q = torch.randn((4, 64), generator=g)
+    score = refs.scores_of(q, box[None], size[None], 2)
+    step = q.abs().amax(-1, keepdim=True) / 127
+    whole = (torch.round(q / step) * step).double()
+    for h in range(2):
+        most = (whole[2 * h:2 * h + 2] @ k64[:, h].T).max()
+        assert float(score[h, 0]) >= float(most) - 1e-5
+    assert refs.bounds_of(torch.zeros((3, 1, 8)))[1].tolist() == [0.0]
+    odd = keys.clone()
+    odd[3, 1, 5] = math.nan
+    box, size = refs.bounds_of(odd)
+    assert box[1, 0].tolist() == [-127] * 64 and float(size[1]) > 1e38 and float(size[0]) < 1.0
+
+
+def test_pick_by_hand():
+    s = [0.5, 0.1, math.nan, 0.5, 0.9, 0.1, 0.2, 0.0]
+    assert refs.pick(s, 8, 4, 1, 1) == [0, 3, 4, 7]
+    assert refs.pick(s, 8, 3, 0, 1) == [0, 4, 7]
+    assert refs.pick(s, 4, 4, 0, 1) == [0, 1, 2, 3]
+    assert refs.pick(s, 7, 2, 1, 1) == [0, 6]
+    assert refs.pick(s, 7, 6, 0, 1) == [0, 1, 3, 4, 5, 6]
+
+
+def test_selected_attention_over_all_pages_is_the_attention():
+    pages = operator_refs.Pages(1, 6, 2, 16, 32, torch.bfloat16, seed=3)
+    tables = [[3, 1, 5], [0, 2, 4]]
+    q = torch.randn((4, 4, 32), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    want, lse, _, _, _ = operator_refs.attend(pages, 0, tables, [40, 1], q, 2, 0.3, softcap=5.0)
+    every = torch.arange(3, dtype=torch.int32).expand(4, 2, 3)
+    out, l, _, _ = refs.attend_selected(pages, 0, tables, [40, 1], q, 2, every, 0.3, softcap=5.0)
+    assert torch.allclose(out, want) and torch.allclose(l, lse)
+
+
+def test_delta_rule_writes_what_a_key_reads():
+    """Orthonormal keys, full steps, no decay: the state maps each key to its last value."""
+    keys = torch.eye(8, dtype=torch.float64)[[0, 3, 0]].view(3, 1, 8)
+    v = torch.tensor([[1.0, 2.0], [3.0, 4.0], [5.0, 6.0]], dtype=torch.float64).view(3, 1, 2)
+    out, state, _, _, _ = refs.delta(keys, keys, v, torch.ones((3, 1)), torch.zeros((1, 2, 8)), sigmoid=False, normalize=False, scale=1.0)
+    assert torch.allclose(out[:, 0], v[:, 0])
+    want = torch.zeros((2, 8), dtype=torch.float64)
+    want[:, 0], want[:, 3] = v[2, 0], v[1, 0]
+    assert torch.allclose(state[0], want)
+
+
+def test_delta_rule_is_its_product_of_matrices():
+    """S_T = sum over s of b_s v_s k_s^T times the products of a_t (I - b_t k_t k_t^T) behind s."""
+    g = torch.Generator().manual_seed(5)
+    t_n, n, p = 6, 8, 4
+    q, k64 = (torch.randn((t_n, 1, n), generator=g, dtype=torch.float64) for _ in range(2))
+    v = torch.randn((t_n, 1, p), generator=g, dtype=torch.float64)
+    beta, dt = (torch.randn((t_n, 1), generator=g, dtype=torch.float64) for _ in range(2))
+    A, first = torch.tensor([-0.7], dtype=torch.float64), torch.randn((1, p, n), generator=g, dtype=torch.float64)
+    _, state, _, _, _ = refs.delta(q, k64, v, beta, first, dt, A, torch.tensor([0.3]))
+    unit = k64[:, 0] / torch.sqrt((k64[:, 0] ** 2).sum(-1, keepdim=True) + 1e-6)
+    b, a = torch.sigmoid(beta[:, 0]), torch.exp(A * torch.nn.functional.softplus(dt[:, 0] + torch.tensor(0.3, dtype=torch.float32).double()))
+    step = [a[t] * (torch.eye(n, dtype=torch.float64) - b[t] * torch.outer(unit[t], unit[t])) for t in range(t_n)]
+    want = first[0]
+    for t in range(t_n):
+        want = want @ step[t] + b[t] * torch.outer(v[t, 0], unit[t])
+    assert torch.allclose(state[0], want, atol=1e-9)
