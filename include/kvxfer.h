@@ -646,6 +646,10 @@ const char* kv_last_error_message(void);
  * KVX_ETIMEOUT.  "scan_setup": the (after_calls + 1)-th next kv_ctx_create makes
  * a context without the scan's matrix form, as where its kernels were compiled
  * for fewer registers than it needs: kv_state_scan then goes token by token.
+ * "delta_wait": the (after_calls + 1)-th next kv_state_delta that goes by chunks
+ * makes no copies for any sequence's second one, so the wait for them runs out:
+ * that sequence's output is incomplete, its state is not written and
+ * kv_get_device_error returns KVX_ETIMEOUT.
  * "tier_exit" ends the process (_exit(3)) inside
  * kv_tier_reserve, while it holds a shared tier's table lock, right after it
  * has taken a slot for the new key; it tests how the processes left recover

@@ -19,7 +19,7 @@ PROBE_LIB = os.path.join(PKG, "_lib", "libkvxfer_probe.so")
 SOURCES = ["pack_kernels.cu", "segment_kernels.cu", "tma_kernels.cu", "kvxfer.cu", "no_alloc.cu", "operators.cu",
            "attend_kernels.cu", "attend_bf16.cu", "attend_fp16.cu", "attend_e4m3.cu", "attend_selected_bf16.cu", "attend_selected_fp16.cu",
            "attend_selected_e4m3.cu", "rotary_kernels.cu", "select_kernels.cu", "evict_kernels.cu", "state_kernels.cu",
-           "scan_kernels.cu", "delta_kernels.cu", "tier.cpp",
+           "scan_kernels.cu", "delta_kernels.cu", "delta_chunks.cu", "tier.cpp",
            "tier_kernels.cu", "host_alloc.cpp", "host_touch.cpp"]
 PROBE_SOURCES = ["probe.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

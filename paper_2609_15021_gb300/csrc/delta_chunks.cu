@@ -1,0 +1,729 @@
+// delta_chunks.cu -- the gated delta rule of prompts, by chunks of 64 tokens.
+//
+// With c_t the sum of the decays' exponents up to t within a chunk, S the state before it and b, k, q, v a token's,
+//   w_t = b_t (v_t - e^{c_t} S k_t - sum_{s<t} e^{c_t - c_s} (k_t . k_s) w_s)
+// is what token t writes, so that W = T rhs with T = (I + A)^-1, A_ts = b_t (k_t . k_s) e^{c_t - c_s} below the diagonal and
+// rhs_t = b_t (v_t - e^{c_t} S k_t).  Then
+//   y_t = e^{c_t} S q_t + sum_{s<=t} (q_t . k_s) e^{c_t - c_s} w_s,   S' = e^{c_63} S + sum_s e^{c_63 - c_s} w_s k_s^T.
+// T, the decayed products M of queries and keys, and what else knows nothing of the state are made first, a CTA a chunk and
+// head (system_kernel).  Then a CTA walks through the chunks of one sequence with 16 rows of one head's state, an element of
+// v each, that know nothing of the other rows (walk_kernel): five products with 16 rows on one side.
+//
+// Rounding: keys and queries are fp16 numbers times a power of two a row, whose largest is in [2^13, 2^14), so that a bf16
+// number keeps its bits down to 2^-27 of that and is off by 2^-38 of it below.  The state, rhs and W's decayed copy are each
+// two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so is 2^9 T.  M and the W that it is multiplied
+// with are rounded to fp16 once.  Sums are fp32.
+//
+// A chunk with a number that is not finite, a decay above 1 or a T above 64 (keys with b |k|^2 well above 2) goes token
+// by token within the walk.
+#include <algorithm>
+
+#include "state_common.cuh"
+#include "tcgen05.cuh"
+
+namespace kvx {
+namespace {
+
+constexpr int kChunk = kDeltaChunk, kThreads = 128;
+constexpr float kMost = 1024.f;   // of a token's exponent
+constexpr float kLargest = 64.f;  // of T
+constexpr float kUp = 512.f;      // that T is multiplied by, as what a decay leaves of it is small, and rhs divided by
+
+// What the system kernel leaves of a chunk and head (offsets in bytes): a token's factors, then T in its two parts
+// and M as 16 x 16 blocks on and below the diagonal, row by row.
+constexpr int kTriangle = 10 * 512;
+struct Factors {
+  float4 by[kChunk];    // of S k_t in rhs, of v_t less that, of w_t in the state, of S q_t in y
+  float row[kChunk];    // M's row
+  float decay;          // of the whole chunk
+  int odd;              // it goes token by token
+  float pad[30];
+};
+constexpr int kFactors = (int)sizeof(Factors), kHeadBytes = kFactors + 3 * kTriangle;
+static_assert(kFactors == 1408 && kHeadBytes == kDeltaHeadBytes && kHeadBytes % 128 == 0, "bulk copies");
+// And of a chunk and group: keys and queries as panels of 64 elements, rows of 128 bytes with their vectors permuted.
+template <int N>
+constexpr int kRowBytes = kChunk * N * 2;
+
+__device__ __forceinline__ int image_at(int row, int vec) { return (vec >> 3) * (kChunk * 128) + row * 128 + (((vec & 7) ^ (row & 7)) << 4); }
+// A 16-byte half of a row of a 16 x 16 block; rows four apart would meet in the banks otherwise.
+__device__ __forceinline__ int block_at(int i, int j, int row, int half) {
+  return (i * (i + 1) / 2 + j) * 512 + row * 32 + ((half ^ (row >> 2 & 1)) << 4);
+}
+__device__ __forceinline__ float decay_of(const DeltaParams& p, float raw, int32_t h) {  // its logarithm
+  if (p.dt_bias) raw += p.dt_bias[h];
+  return (p.softplus ? (raw > 20.f ? raw : log1pf(expf(raw))) : raw) * p.A[h];
+}
+__device__ __forceinline__ float step_size(const DeltaParams& p, float raw) { return p.sigmoid ? 1.f / (1.f + expf(-raw)) : raw; }
+__device__ __forceinline__ int exponent_of(float v) { return min(max((int)(__float_as_uint(v) >> 23 & 255) - 127, -126), 126); }
+__device__ __forceinline__ uint32_t half2_of(float a, float b) { return pack2<Fp16>(a, b); }
+
+// ---------------------------------------------------------------- what knows nothing of the state
+
+constexpr int kPitch = kChunk + 4;  // of 64 x 64 fp32 numbers in shared memory
+template <int N>
+struct SystemShape {
+  // keys and queries, then, when they have been multiplied, A transposed and M
+  static constexpr int kImages = 2 * kRowBytes<N> > kChunk * kPitch * 4 + kTriangle ? 2 * kRowBytes<N> : kChunk * kPitch * 4 + kTriangle;
+  static constexpr int kT = kImages, kDiagonal = kT + kChunk * kPitch * 4, kSmem = kDiagonal + 4 * 16 * 16 * 4;
+};
+
+template <class E, int N>
+__global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant__ DeltaParams p) {
+  wait_for_previous();
+  using S = SystemShape<N>;
+  using T = typename E::T;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Factors f;
+  __shared__ float sum_s[kChunk], low_s[kChunk], key_s[kChunk], query_s[kChunk], beta_s[kChunk];
+  __shared__ int32_t buf[kThreads / 32 + 3];
+  const StateView& v = p.state;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  const int32_t piece = blockIdx.x, h = blockIdx.y, group = h / p.heads_per_group;
+  Piece found;
+  if (!find_piece<kThreads>(v, piece, kChunk, p.by_token, buf, &found) || !found.in || !found.keep) return;
+  const int64_t t0 = found.first + (int64_t)found.at * kChunk;
+  const int32_t n = (int32_t)min((int64_t)kChunk, found.last - t0);
+  uint8_t* rows_to = p.rows_space + ((int64_t)piece * p.groups + group) * 2 * kRowBytes<N>;
+  uint8_t* head_to = p.head_space + ((int64_t)piece * p.heads + h) * kHeadBytes;
+  const bool writes_rows = h == group * p.heads_per_group;
+  bool odd = false;
+
+  // Keys and queries: lengths, and fp16 numbers with the row's largest in [2^13, 2^14).
+  constexpr int kLanes = N / 8, kAtOnce = 32 / kLanes, kRounds = 16 / kAtOnce;
+  const int vec = lane % kLanes, sub = lane / kLanes;
+  const T* rows[2] = {reinterpret_cast<const T*>(p.k) + group * p.k_head + vec * 8, reinterpret_cast<const T*>(p.q) + group * p.q_head + vec * 8};
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    const int64_t stride = which ? p.q_token : p.k_token;
+    uint4 raw[kRounds];
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int row = warp * 16 + i * kAtOnce + sub;
+      raw[i] = row < n ? *reinterpret_cast<const uint4*>(rows[which] + (t0 + row) * stride) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const int row = warp * 16 + i * kAtOnce + sub;
+      const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+      float2 x[4];
+      float squares = 0.f, top = 0.f;
+      uint32_t carries = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[j] = unpack2<E>(u[j]);
+        carries |= odd_carry<E>(u[j]);
+        squares = fmaf(x[j].x, x[j].x, fmaf(x[j].y, x[j].y, squares));
+        top = fmaxf(top, fmaxf(fabsf(x[j].x), fabsf(x[j].y)));
+      }
+#pragma unroll
+      for (int m = kLanes / 2; m; m >>= 1) {
+        squares += __shfl_xor_sync(~0u, squares, m);
+        top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
+      }
+      const int e = top > 0.f ? max(exponent_of(top) - 13, -126) : 0;
+      const float factor = row < n ? (p.normalize ? rsqrtf(squares + p.eps) : 1.f) * (which ? p.scale : 1.f) * power_of_two(e) : 0.f;
+      const float by = power_of_two(-e);
+      odd |= odd_carried(carries) || !isfinite(factor);
+      if (vec == 0) (which ? query_s : key_s)[row] = top > 0.f ? factor : 0.f;  // of zeros it would only set scales
+      const uint4 w = make_uint4(half2_of(x[0].x * by, x[0].y * by), half2_of(x[1].x * by, x[1].y * by),
+                                 half2_of(x[2].x * by, x[2].y * by), half2_of(x[3].x * by, x[3].y * by));
+      const int at = which * kRowBytes<N> + image_at(row, vec);
+      *reinterpret_cast<uint4*>(smem + at) = w;
+      if (writes_rows) *reinterpret_cast<uint4*>(rows_to + at) = w;
+    }
+  }
+  // Gates, two tokens a lane: sums of exponents up to a token in two parts, whole 64ths (that 64 tokens of up to 2^10 lose no
+  // bit of) and the rest, as differences of them count; sums behind a token from the end.
+  if (warp == 0) {
+    float a[2], rest[2], beta[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int t = 2 * lane + k;
+      const bool there = t < n;
+      beta[k] = there ? step_size(p, E::up(reinterpret_cast<const T*>(p.beta)[(t0 + t) * p.beta_token + h])) : 0.f;
+      a[k] = there && p.dt ? decay_of(p, E::up(reinterpret_cast<const T*>(p.dt)[(t0 + t) * p.dt_token + h]), h) * kLog2e : 0.f;
+      odd |= !isfinite(beta[k]) || !(a[k] <= 0.f);
+      a[k] = fmaxf(a[k], -kMost);
+      rest[k] = a[k] - rintf(a[k] * 64.f) * (1.f / 64);
+    }
+    float upto = (a[0] - rest[0]) + (a[1] - rest[1]), fine = rest[0] + rest[1], behind = a[0] + a[1];
+    for (int m = 1; m < 32; m <<= 1) {
+      const float y = __shfl_up_sync(~0u, upto, m), z = __shfl_up_sync(~0u, fine, m), w = __shfl_down_sync(~0u, behind, m);
+      if (lane >= m) upto += y, fine += z;
+      if (lane + m < 32) behind += w;
+    }
+    float below = __shfl_up_sync(~0u, upto, 1), below_fine = __shfl_up_sync(~0u, fine, 1), above = __shfl_down_sync(~0u, behind, 1);
+    if (lane == 0) below = below_fine = 0.f;
+    if (lane == 31) above = 0.f, f.decay = ex2(upto + fine);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      below += a[k] - rest[k], below_fine += rest[k];
+      // the sum of both, rounded, and what that lost (Knuth, "The Art of Computer Programming", vol. 2, 4.2.2)
+      const float sum = below + below_fine, back = sum - below, low = (below - (sum - back)) + (below_fine - back);
+      const int t = 2 * lane + k;
+      sum_s[t] = sum, low_s[t] = low, beta_s[t] = beta[k];
+      const float decay = ex2(sum) * ex2(low);
+      f.by[t] = make_float4(decay, beta[k] * (1 / kUp), 0.f, decay);
+    }
+#pragma unroll
+    for (int k = 1; k >= 0; --k) {
+      f.by[2 * lane + k].z = 2 * lane + k < n ? ex2(above) : 0.f;
+      above += a[k];
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < kChunk) {
+    float4& by = f.by[threadIdx.x];
+    by.x *= key_s[threadIdx.x], by.z *= key_s[threadIdx.x], by.w *= query_s[threadIdx.x];
+  }
+
+  // Products of keys with keys and of queries with keys, 16 rows a warp, up to the diagonal.
+  const uint32_t base = smem_at(smem);
+  float kk[8][4], qk[8][4];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) kk[j][e] = qk[j][e] = 0.f;
+  const int a_row = warp * 16 + (lane >> 3 & 1) * 8 + (lane & 7), a_vec = lane >> 4;  // of a left factor's matrices
+  const int b_row = (lane >> 4) * 8 + (lane & 7), b_vec = lane >> 3 & 1;              // of a right one's
+#pragma unroll 2
+  for (int s = 0; s < N / 16; ++s) {
+    uint32_t ka[4], qa[4];
+    load_matrices(ka, base + image_at(a_row, 2 * s + a_vec));
+    load_matrices(qa, base + kRowBytes<N> + image_at(a_row, 2 * s + a_vec));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (j > warp) break;
+      uint32_t b[4];
+      load_matrices(b, base + image_at(16 * j + b_row, 2 * s + b_vec));
+      mma<Fp16>(kk[2 * j], ka, b[0], b[1]);
+      mma<Fp16>(kk[2 * j + 1], ka, b[2], b[3]);
+      mma<Fp16>(qk[2 * j], qa, b[0], b[1]);
+      mma<Fp16>(qk[2 * j + 1], qa, b[2], b[3]);
+    }
+  }
+  __syncthreads();  // the images have been read
+  float* a_s = reinterpret_cast<float*>(smem);  // A transposed: [s][t]
+  uint8_t* m_s = smem + kChunk * kPitch * 4;
+  float* x_s = reinterpret_cast<float*>(smem + S::kT);         // T: [t][s]
+  float* d_s = reinterpret_cast<float*>(smem + S::kDiagonal);  // its blocks on the diagonal, transposed: [block][s][t]
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {  // rows g and g + 8 of the warp's
+    const int t = warp * 16 + g + 8 * r;
+    const float sum_t = sum_s[t], low_t = low_s[t], key_t = key_s[t] * beta_s[t], query_t = query_s[t];
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j > 2 * warp + 1) break;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int s = 8 * j + 2 * c + e;
+        const float by = key_s[s] * (s <= t ? ex2((sum_t - sum_s[s]) + (low_t - low_s[s])) : 0.f);
+        if (s < t) a_s[s * kPitch + t] = kk[j][2 * r + e] * by * key_t;
+        qk[j][2 * r + e] *= by * query_t;
+        top = fmaxf(top, fabsf(qk[j][2 * r + e]));
+      }
+    }
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
+    odd |= !(top < INFINITY);
+    const int e = top > 0.f ? 13 - exponent_of(top) : 0;  // the row's largest to [2^13, 2^14)
+    const float up = power_of_two(min(e, 126));
+    if (c == 0) f.row[t] = power_of_two(-min(e, 126));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j > 2 * warp + 1) break;
+      *reinterpret_cast<uint32_t*>(m_s + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c) = half2_of(qk[j][2 * r] * up, qk[j][2 * r + 1] * up);
+    }
+  }
+  __syncwarp();
+  // A block on the diagonal inverted by substitution, a column a lane (both halves of the warp alike).
+  {
+    const int col = lane & 15;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = i == col ? 1.f : 0.f;
+    const float* at = a_s + warp * 16 * kPitch + warp * 16;
+#pragma unroll
+    for (int k = 0; k < 15; ++k)
+#pragma unroll
+      for (int i = (k + 1) / 4 * 4; i < 16; i += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(at + k * kPitch + i);
+        if (i > k) x[i] -= a.x * x[k];
+        if (i + 1 > k) x[i + 1] -= a.y * x[k];
+        if (i + 2 > k) x[i + 2] -= a.z * x[k];
+        if (i + 3 > k) x[i + 3] -= a.w * x[k];
+      }
+    if (lane < 16) {
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<float4*>(d_s + (warp * 16 + col) * 16 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x_s[(warp * 16 + i) * kPitch + warp * 16 + col] = x[i];
+    }
+  }
+  __syncthreads();
+  // The blocks below: T_ij = -T_ii sum_{j<=k<i} A_ik T_kj, a column of blocks a warp, a column and half of the rows a lane.
+  {
+    const int col = warp * 16 + (lane & 15), half = lane >> 4;
+    for (int i = warp + 1; i < 4; ++i) {
+      float acc[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) acc[r] = 0.f;
+#pragma unroll 8
+      for (int k = warp * 16; k < i * 16; ++k) {
+        const float x = x_s[k * kPitch + col];
+        const float4 a = *reinterpret_cast<const float4*>(a_s + k * kPitch + i * 16 + half * 8);
+        const float4 b = *reinterpret_cast<const float4*>(a_s + k * kPitch + i * 16 + half * 8 + 4);
+        acc[0] -= a.x * x, acc[1] -= a.y * x, acc[2] -= a.z * x, acc[3] -= a.w * x;
+        acc[4] -= b.x * x, acc[5] -= b.y * x, acc[6] -= b.z * x, acc[7] -= b.w * x;
+      }
+      float* to = x_s + (i * 16 + half * 8) * kPitch + col;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) to[r * kPitch] = acc[r], acc[r] = 0.f;
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const float x = x_s[(i * 16 + k) * kPitch + col];
+        const float4 a = *reinterpret_cast<const float4*>(d_s + (i * 16 + k) * 16 + half * 8);
+        const float4 b = *reinterpret_cast<const float4*>(d_s + (i * 16 + k) * 16 + half * 8 + 4);
+        acc[0] += a.x * x, acc[1] += a.y * x, acc[2] += a.z * x, acc[3] += a.w * x;
+        acc[4] += b.x * x, acc[5] += b.y * x, acc[6] += b.z * x, acc[7] += b.w * x;
+      }
+      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < 8; ++r) to[r * kPitch] = acc[r];
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+  // T in its two parts, M and the factors.
+  uint8_t* t_to = head_to + kFactors;
+  for (int i = threadIdx.x; i < kTriangle / 16; i += kThreads) {
+    *reinterpret_cast<uint4*>(t_to + 2 * kTriangle + i * 16) = *reinterpret_cast<const uint4*>(m_s + i * 16);
+    const int block = i / 32, row = i / 2 % 16, half = (i & 1) ^ (row >> 2 & 1);
+    const int bi = block < 1 ? 0 : block < 3 ? 1 : block < 6 ? 2 : 3, bj = block - bi * (bi + 1) / 2;
+    const float* from = x_s + (bi * 16 + row) * kPitch + bj * 16 + half * 8;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 x = *reinterpret_cast<const float2*>(from + 2 * k);
+      odd |= !(fmaxf(fabsf(x.x), fabsf(x.y)) <= kLargest) || x.x != x.x || x.y != x.y;
+      hi[k] = half2_of(x.x * kUp, x.y * kUp);
+      const float2 back = unpack2<Fp16>(hi[k]);
+      lo[k] = half2_of(x.x * kUp - back.x, x.y * kUp - back.y);
+    }
+    *reinterpret_cast<uint4*>(t_to + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(t_to + kTriangle + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  }
+  odd = __syncthreads_or(odd);
+  if (threadIdx.x == 0) f.odd = odd;
+  __syncthreads();
+  for (int i = threadIdx.x; i < kFactors / 16; i += kThreads)
+    reinterpret_cast<uint4*>(head_to)[i] = reinterpret_cast<const uint4*>(&f)[i];
+}
+
+// ---------------------------------------------------------------- the walk
+
+__device__ __forceinline__ void bulk_load(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes),
+               "r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+template <int N>
+struct WalkShape {
+  static constexpr int kSteps = N / 16;  // of 16 along the state's columns
+  static constexpr int kT = 2 * kRowBytes<N> + kFactors, kStage = 2 * kRowBytes<N> + kFactors + 2 * kTriangle;
+  // left factors as the matrix instruction takes them, 512 bytes for 16 columns and part, and their powers of two
+  static constexpr int kM = 2 * kStage, kState = kM + kTriangle, kRhs = kState + kSteps * 1024, kWrite = kRhs + 4096, kPlain = kWrite + 4096,
+                       kStateBy = kPlain + 2048, kRhsBy = kStateBy + kSteps * 64, kWriteBy = kRhsBy + 256, kPlainBy = kWriteBy + 256,
+                       kBars = kPlainBy + 256, kSmem = kBars + 64;
+  static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs an SM");
+};
+
+// Two tiles of 16 x 8 sums as 16 columns of a left factor: fp16 parts hi and lo, times powers of two a row.
+__device__ __forceinline__ void left_factor(const float (&x)[4], const float (&y)[4], uint8_t* hi, uint8_t* lo, float2* by, int lane) {
+  float top[2] = {fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(y[0]), fabsf(y[1]))),
+                  fmaxf(fmaxf(fabsf(x[2]), fabsf(x[3])), fmaxf(fabsf(y[2]), fabsf(y[3])))};
+  float up[2];
+  float2 down;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
+    top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
+    const int e = min(max(140 - (int)(__float_as_uint(top[r]) >> 23), -126), 126);  // the largest to [2^13, 2^14)
+    up[r] = power_of_two(e);
+    (r ? down.y : down.x) = power_of_two(-e);
+  }
+  const float2 v[4] = {mul2(make_float2(x[0], x[1]), make_float2(up[0], up[0])), mul2(make_float2(x[2], x[3]), make_float2(up[1], up[1])),
+                       mul2(make_float2(y[0], y[1]), make_float2(up[0], up[0])), mul2(make_float2(y[2], y[3]), make_float2(up[1], up[1]))};
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    h[k] = half2_of(v[k].x, v[k].y);
+    const float2 rest = fma2(unpack2<Fp16>(h[k]), make_float2(-1.f, -1.f), v[k]);
+    l[k] = half2_of(rest.x, rest.y);
+  }
+  *reinterpret_cast<uint4*>(hi + lane * 16) = make_uint4(h[0], h[1], h[2], h[3]);
+  if (lo) *reinterpret_cast<uint4*>(lo + lane * 16) = make_uint4(l[0], l[1], l[2], l[3]);
+  if ((lane & 3) == 0) by[lane >> 2] = down;
+}
+__device__ __forceinline__ void left_load(uint32_t (&a)[4], const uint8_t* at, int lane) {
+  const uint4 v = *reinterpret_cast<const uint4*>(at + lane * 16);
+  a[0] = v.x, a[1] = v.y, a[2] = v.z, a[3] = v.w;
+}
+__device__ __forceinline__ void add_scaled(float (&d)[4], const float (&x)[4], float2 by) {
+  d[0] = fmaf(x[0], by.x, d[0]), d[1] = fmaf(x[1], by.x, d[1]);
+  d[2] = fmaf(x[2], by.y, d[2]), d[3] = fmaf(x[3], by.y, d[3]);
+}
+
+template <class E, int N>
+__global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant__ DeltaParams p) {
+  wait_for_previous();
+  using W = WalkShape<N>;
+  using T = typename E::T;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int32_t first_s;
+  const StateView& v = p.state;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  const int32_t p0 = blockIdx.x * 16, h = blockIdx.y, s = blockIdx.z, group = h / p.heads_per_group;
+  int64_t begin, end;
+  rows_of(v, s, &begin, &end);
+  int32_t chunks = pieces_of(begin, end, kChunk, p.by_token);
+  if (chunks == 0) return;
+  const uint32_t base = smem_at(smem), bars = base + W::kBars;  // of both stages and of M
+  if (threadIdx.x == 0) {
+    first_s = 0;
+    for (int i = 0; i < 3; ++i) bar_init(bars + 8 * i);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async;" ::: "memory");  // what the kernel before has written is read by bulk copies
+  }
+  __syncthreads();
+  int32_t before = 0;  // pieces of the sequences in front, as far as there is room
+  for (int32_t i = threadIdx.x; i < s; i += kThreads) {
+    int64_t a, b;
+    rows_of(v, i, &a, &b);
+    before = min(before + pieces_of(a, b, kChunk, p.by_token), p.pieces);
+  }
+  for (int m = 16; m; m >>= 1) before += __shfl_xor_sync(~0u, before, m);
+  if (lane == 0 && before) atomicAdd(&first_s, before);
+  __syncthreads();
+  const int32_t first = min(first_s, p.pieces);
+  chunks = min(chunks, p.pieces - first);
+  const uint8_t* in = slot_of(v, v.slots_in, s);
+  uint8_t* keep = slot_of(v, v.slots_out, s);
+  T* out = reinterpret_cast<T*>(p.out) + h * p.out_head + p0;
+  if (!in || !keep) {
+    for (int64_t i = threadIdx.x; i < (end - begin) * 16; i += kThreads)
+      if (p0 + i % 16 < p.head_dim) out[(begin + i / 16) * p.out_token + i % 16] = E::down(0.f);
+    return;
+  }
+
+  auto load_stage = [&](int32_t i) {  // by one thread
+    const uint32_t bar = bars + 8 * (i & 1), to = base + (i & 1) * W::kStage;
+    if (p.stall && i == 1) return;
+    bar_expect(bar, W::kStage);
+    bulk_load(to, p.rows_space + ((int64_t)(first + i) * p.groups + group) * 2 * kRowBytes<N>, 2 * kRowBytes<N>, bar);
+    bulk_load(to + 2 * kRowBytes<N>, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes, kFactors + 2 * kTriangle, bar);
+  };
+  auto load_m = [&](int32_t i) {
+    bar_expect(bars + 16, kTriangle);
+    bulk_load(base + W::kM, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes + kFactors + 2 * kTriangle, kTriangle, bars + 16);
+  };
+  if (threadIdx.x == 0 && chunks > 0) load_stage(0);
+
+  // Values of a chunk, as a transposing move takes them: tokens 8 u + lane / 4 of the warp's, elements 2 c and the next
+  // of each eight.
+  const T* v_at = reinterpret_cast<const T*>(p.v) + h * p.v_head + p0 + 2 * c;
+  uint32_t raw[2][2];
+  auto load_values = [&](int32_t i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t t = begin + (int64_t)i * kChunk + warp * 16 + 8 * u + g;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        raw[u][k] = t < end && p0 + 8 * k < p.head_dim ? *reinterpret_cast<const uint32_t*>(v_at + t * p.v_token + 8 * k) : 0;
+    }
+  };
+  load_values(0);
+
+  // The state: tiles of 16 x 8, a row g and g + 8, columns 2 c and the next.
+  constexpr int kTiles = N / 32;  // a warp's
+  float state[kTiles][4];
+  const int64_t state_at = ((int64_t)h * p.head_dim + p0) * N + warp * kTiles * 8 + 2 * c;
+  const bool fresh = v.fresh && v.fresh[s];
+#pragma unroll
+  for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      float2 x = make_float2(0.f, 0.f);
+      if (!fresh && p0 + 8 * r < p.head_dim) x = *reinterpret_cast<const float2*>(in + (state_at + (g + 8 * r) * N + k * 8) * 4);
+      state[k][2 * r] = x.x, state[k][2 * r + 1] = x.y;
+    }
+  float2* state_by = reinterpret_cast<float2*>(smem + W::kStateBy);
+  float2* rhs_by = reinterpret_cast<float2*>(smem + W::kRhsBy);
+  float2* write_by = reinterpret_cast<float2*>(smem + W::kWriteBy);
+  float2* plain_by = reinterpret_cast<float2*>(smem + W::kPlainBy);
+  auto publish = [&]() {
+#pragma unroll
+    for (int k = 0; k < kTiles; k += 2) {
+      const int step = (warp * kTiles + k) / 2;
+      left_factor(state[k], state[k + 1], smem + W::kState + step * 1024, smem + W::kState + step * 1024 + 512, state_by + step * 8, lane);
+    }
+  };
+  publish();
+
+  const int b_row = (lane >> 4) * 8 + (lane & 7), b_vec = lane >> 3 & 1;  // of a right factor's matrices
+  const int t_row = (lane >> 3 & 1) * 8 + (lane & 7), t_vec = lane >> 4;  // of one that is transposed
+  bool dead = false;
+  int32_t i = 0;
+  for (; i < chunks; ++i) {
+    const int64_t t0 = begin + (int64_t)i * kChunk;
+    uint8_t* stage = smem + (i & 1) * W::kStage;
+    const uint32_t rows = base + (i & 1) * W::kStage;
+    const Factors& f = *reinterpret_cast<const Factors*>(stage + 2 * kRowBytes<N>);
+    dead = dead || !bar_wait(bars + 8 * (i & 1), i >> 1 & 1, p.wait_cycles);
+    const uint32_t carries = odd_carry<E>(raw[0][0]) | odd_carry<E>(raw[0][1]) | odd_carry<E>(raw[1][0]) | odd_carry<E>(raw[1][1]);
+    bool odd = odd_carried(carries) || (!dead && f.odd);
+    if (__syncthreads_or(odd || dead)) {  // and the state is there for all
+      if (__syncthreads_or(dead)) break;
+      odd = true;
+    }
+    if (threadIdx.x == 0) {
+      load_m(i);
+      if (i + 1 < chunks) load_stage(i + 1);
+    }
+    if (odd) {
+      // Token by token, a row for eight lanes.
+      float* all = reinterpret_cast<float*>(smem + W::kState);
+      static_assert(W::kSteps * 1024 == 16 * N * 4, "the state's room");
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) all[(g + 8 * (e >> 1)) * N + (warp * kTiles + k) * 8 + 2 * c + (e & 1)] = state[k][e];
+      __syncthreads();
+      const int row = threadIdx.x / 8, part = threadIdx.x % 8;
+      const bool used = p0 + row < p.head_dim;
+      float x[N / 8];
+#pragma unroll
+      for (int k = 0; k < N / 8; ++k) x[k] = all[row * N + k * 8 + part];
+      const int64_t stop = min(end, t0 + kChunk);
+      for (int64_t t = t0; t < stop; ++t) {
+        const T* k_at = reinterpret_cast<const T*>(p.k) + t * p.k_token + group * p.k_head + part;
+        const T* q_at = reinterpret_cast<const T*>(p.q) + t * p.q_token + group * p.q_head + part;
+        float kk = 0.f, qq = 0.f, kq = 0.f, sk = 0.f, sq = 0.f;
+#pragma unroll
+        for (int k = 0; k < N / 8; ++k) {
+          const float a = E::up(k_at[8 * k]), b = E::up(q_at[8 * k]);
+          kk += a * a, qq += b * b, kq += a * b, sk += x[k] * a, sq += x[k] * b;
+        }
+#pragma unroll
+        for (int m = 4; m; m >>= 1) {
+          kk += __shfl_xor_sync(~0u, kk, m), qq += __shfl_xor_sync(~0u, qq, m), kq += __shfl_xor_sync(~0u, kq, m);
+          sk += __shfl_xor_sync(~0u, sk, m), sq += __shfl_xor_sync(~0u, sq, m);
+        }
+        const float k_by = p.normalize ? rsqrtf(kk + p.eps) : 1.f, q_by = p.normalize ? p.scale * rsqrtf(qq + p.eps) : p.scale;
+        const float decay = p.dt ? expf(decay_of(p, E::up(reinterpret_cast<const T*>(p.dt)[t * p.dt_token + h]), h)) : 1.f;
+        const float beta = step_size(p, E::up(reinterpret_cast<const T*>(p.beta)[t * p.beta_token + h]));
+        const float value = used ? E::up(reinterpret_cast<const T*>(p.v)[t * p.v_token + h * p.v_head + p0 + row]) : 0.f;
+        const float d = beta * (value - decay * (sk * k_by));
+        if (used && part == 0) out[t * p.out_token + row] = E::down(decay * (sq * q_by) + d * (kq * k_by * q_by));
+#pragma unroll
+        for (int k = 0; k < N / 8; ++k) x[k] = x[k] * decay + d * (E::up(k_at[8 * k]) * k_by);
+      }
+#pragma unroll
+      for (int k = 0; k < N / 8; ++k) all[row * N + k * 8 + part] = x[k];
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) state[k][e] = all[(g + 8 * (e >> 1)) * N + (warp * kTiles + k) * 8 + 2 * c + (e & 1)];
+      load_values(i + 1);
+      dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+      __syncthreads();
+      publish();
+      continue;
+    }
+
+    // S k and S q of the warp's 16 tokens.
+    float sk[2][4], y[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sk[u][e] = y[u][e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < W::kSteps; ++k) {
+      uint32_t hi[4], lo[4], b[4], q[4];
+      left_load(hi, smem + W::kState + k * 1024, lane);
+      left_load(lo, smem + W::kState + k * 1024 + 512, lane);
+      load_matrices(b, rows + image_at(warp * 16 + b_row, 2 * k + b_vec));
+      load_matrices(q, rows + kRowBytes<N> + image_at(warp * 16 + b_row, 2 * k + b_vec));
+      const float2 by = state_by[k * 8 + g];
+      float x[4][4] = {};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        mma<Fp16>(x[u], hi, b[2 * u], b[2 * u + 1]);
+        mma<Fp16>(x[2 + u], hi, q[2 * u], q[2 * u + 1]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        mma<Fp16>(x[u], lo, b[2 * u], b[2 * u + 1]);
+        mma<Fp16>(x[2 + u], lo, q[2 * u], q[2 * u + 1]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        add_scaled(sk[u], x[u], by);
+        add_scaled(y[u], x[2 + u], by);
+      }
+    }
+    float4 by[2][2];
+    float m_by[2][2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        by[u][e] = f.by[warp * 16 + 8 * u + 2 * c + e];
+        m_by[u][e] = f.row[warp * 16 + 8 * u + 2 * c + e];
+      }
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const float2 value = unpack2<E>(transpose(raw[u][r]));
+        sk[u][2 * r] = by[u][0].y * (value.x - by[u][0].x * sk[u][2 * r]);
+        sk[u][2 * r + 1] = by[u][1].y * (value.y - by[u][1].x * sk[u][2 * r + 1]);
+      }
+    }
+    left_factor(sk[0], sk[1], smem + W::kRhs + warp * 1024, smem + W::kRhs + warp * 1024 + 512, rhs_by + warp * 8, lane);
+    load_values(i + 1);
+    __syncthreads();
+    // W = T rhs
+    float w[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k > warp) break;
+      uint32_t hi[4], lo[4], b[4], b_lo[4];
+      left_load(hi, smem + W::kRhs + k * 1024, lane);
+      left_load(lo, smem + W::kRhs + k * 1024 + 512, lane);
+      load_matrices(b, rows + W::kT + block_at(warp, k, b_row, b_vec));
+      load_matrices(b_lo, rows + W::kT + kTriangle + block_at(warp, k, b_row, b_vec));
+      const float2 by = rhs_by[k * 8 + g];
+      float x[2][4] = {};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        mma<Fp16>(x[u], hi, b[2 * u], b[2 * u + 1]);
+        mma<Fp16>(x[u], lo, b[2 * u], b[2 * u + 1]);
+        mma<Fp16>(x[u], hi, b_lo[2 * u], b_lo[2 * u + 1]);
+        add_scaled(w[u], x[u], by);
+      }
+    }
+    left_factor(w[0], w[1], smem + W::kPlain + warp * 512, nullptr, plain_by + warp * 8, lane);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[u][e] *= by[u][e & 1].z;
+    left_factor(w[0], w[1], smem + W::kWrite + warp * 1024, smem + W::kWrite + warp * 1024 + 512, write_by + warp * 8, lane);
+    __syncthreads();
+    // The state after the chunk.
+    const float decay = f.decay;
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) state[k][e] *= decay;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      uint32_t hi[4], lo[4];
+      left_load(hi, smem + W::kWrite + k * 1024, lane);
+      left_load(lo, smem + W::kWrite + k * 1024 + 512, lane);
+      const float2 by = write_by[k * 8 + g];
+#pragma unroll
+      for (int j = 0; j < kTiles; j += 2) {
+        uint32_t b[4];
+        load_matrices_t(b, rows + image_at(16 * k + t_row, warp * kTiles + j + t_vec));
+        float x[2][4] = {};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          mma<Fp16>(x[u], hi, b[2 * u], b[2 * u + 1]);
+          mma<Fp16>(x[u], lo, b[2 * u], b[2 * u + 1]);
+          add_scaled(state[j + u], x[u], by);
+        }
+      }
+    }
+    publish();
+    // y = e^c S q + M W
+    dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+    float my[2][4] = {};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k > warp) break;
+      uint32_t hi[4], b[4];
+      left_load(hi, smem + W::kPlain + k * 512, lane);
+      load_matrices(b, base + W::kM + block_at(warp, k, b_row, b_vec));
+      const float2 by = plain_by[k * 8 + g];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float x[4] = {};
+        mma<Fp16>(x, hi, b[2 * u], b[2 * u + 1]);
+        add_scaled(my[u], x, by);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t t = t0 + warp * 16 + 8 * u + g;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const uint32_t pair = transpose(pack2<E>(by[u][0].w * y[u][2 * r] + m_by[u][0] * my[u][2 * r],
+                                                 by[u][1].w * y[u][2 * r + 1] + m_by[u][1] * my[u][2 * r + 1]));
+        if (t < end && p0 + 8 * r < p.head_dim) *reinterpret_cast<uint32_t*>(out + t * p.out_token + 8 * r + 2 * c) = pair;
+      }
+    }
+  }
+  if (__syncthreads_or(dead)) {
+    if (threadIdx.x == 0) {
+      *p.timeout = 1;
+      // copies may still be on their way: their end, however short the waits' limit is
+      if (i < chunks && !(p.stall && i == 1)) bar_wait(bars + 8 * (i & 1), i >> 1 & 1, kDefaultWaitCycles);
+      if (i > 0) bar_wait(bars + 16, (i - 1) & 1, kDefaultWaitCycles);
+    }
+    __syncthreads();
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+      if (p0 + 8 * r < p.head_dim)
+        *reinterpret_cast<float2*>(keep + (state_at + (g + 8 * r) * N + k * 8) * 4) = make_float2(state[k][2 * r], state[k][2 * r + 1]);
+}
+
+template <class E, int N>
+cudaError_t chunks(const DeltaParams& p, cudaStream_t s) {
+  const cudaError_t e = launch_after(system_kernel<E, N>, dim3((unsigned)p.pieces, p.heads), kThreads, SystemShape<N>::kSmem, s, p);
+  if (e != cudaSuccess) return e;
+  return launch_after(walk_kernel<E, N>, dim3((p.head_dim + 15) / 16, p.heads, p.state.num_seqs), kThreads, WalkShape<N>::kSmem, s, p);
+}
+
+template <class E, int N>
+cudaError_t prepare() {
+  const cudaError_t e = cudaFuncSetAttribute(system_kernel<E, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, SystemShape<N>::kSmem);
+  return e == cudaSuccess ? cudaFuncSetAttribute(walk_kernel<E, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, WalkShape<N>::kSmem) : e;
+}
+
+}  // namespace
+
+cudaError_t launch_delta_chunks(const DeltaParams& p, int type, cudaStream_t s) {
+  if (type == KVX_TYPE_BF16) return p.state_dim == 64 ? chunks<Bf16, 64>(p, s) : chunks<Bf16, 128>(p, s);
+  return p.state_dim == 64 ? chunks<Fp16, 64>(p, s) : chunks<Fp16, 128>(p, s);
+}
+
+cudaError_t prepare_delta_kernels() {
+  for (auto prepare : {prepare<Bf16, 64>, prepare<Bf16, 128>, prepare<Fp16, 64>, prepare<Fp16, 128>}) {
+    const cudaError_t e = prepare();
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+}  // namespace kvx

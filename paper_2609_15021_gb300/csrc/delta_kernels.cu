@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(128) delta_kernel(const __grid_constant__ Delt
   uint8_t* keep = slot_of(v, v.slots_out, s);
   int64_t first, last;
   rows_of(v, s, &first, &last);
+  if (last - first > p.by_token) return;
   T* out = reinterpret_cast<T*>(p.out) + h * p.out_head;
   if (!in || !keep) {
     for (int64_t t = first; t < last; ++t)
@@ -160,8 +161,20 @@ cudaError_t delta(const DeltaParams& p, int num_sms, cudaStream_t s) {
 
 }  // namespace
 
+bool delta_by_chunks(int64_t tokens, int32_t num_seqs, bool packed, int32_t state_dim, int32_t* by_token) {
+  constexpr int32_t kShort = 8;
+  *by_token = INT32_MAX;
+  if (!packed || (state_dim != 64 && state_dim != 128) || tokens <= kShort) return false;
+  *by_token = num_seqs > 1 ? kShort : -1;
+  return true;
+}
+
 cudaError_t launch_delta(const DeltaParams& p, int type, int num_sms, cudaStream_t s) {
-  return type == KVX_TYPE_BF16 ? delta<Bf16>(p, num_sms, s) : delta<Fp16>(p, num_sms, s);
+  if (p.by_token >= 0) {
+    const cudaError_t e = type == KVX_TYPE_BF16 ? delta<Bf16>(p, num_sms, s) : delta<Fp16>(p, num_sms, s);
+    if (e != cudaSuccess) return e;
+  }
+  return p.pieces ? launch_delta_chunks(p, type, s) : cudaSuccess;
 }
 
 }  // namespace kvx

@@ -146,8 +146,9 @@ cudaError_t launch_move_tma(int dir, int layout, const MoveParams& p, int grid, 
 cudaError_t prepare_tma_kernels();
 // Shared-memory limits of the attention kernels (attend_kernels.cu), likewise.
 cudaError_t prepare_attend_kernels();
-// And those of the selection (select_kernels.cu).
+// And those of the selection (select_kernels.cu) and of the delta rule (delta_chunks.cu).
 cudaError_t prepare_select_kernels();
+cudaError_t prepare_delta_kernels();
 // And the scan's (scan_kernels.cu).  *matrix: whether they were compiled for as many registers as the matrix form's split
 // of them takes; a context without them scans token by token.
 cudaError_t prepare_state_kernels(bool* matrix);

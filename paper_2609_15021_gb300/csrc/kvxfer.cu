@@ -1132,6 +1132,7 @@ kvx_status kv_ctx_create(int device, const kvx_opts* opts, kvx_ctx** out) {
     if ((e = prepare_tma_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_attend_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_select_kernels()) != cudaSuccess) return fail(e);
+    if ((e = prepare_delta_kernels()) != cudaSuccess) return fail(e);
     if ((e = prepare_state_kernels(&ctx->scan_matrix)) != cudaSuccess) return fail(e);
     if (fault_point("scan_setup")) ctx->scan_matrix = false;
     // the host-page touch threads, once per process, at set-up rather than
@@ -1235,7 +1236,8 @@ kvx_status kv_state_load(kvx_ctx* ctx, int32_t num_layers, void* const* layer_ba
 
 kvx_status kv_fault_inject(const char* point, int32_t after_calls) {
   static const char* const points[] = {"launch",    "queue_launch", "memcpy",   "event",
-                                       "host_alloc", "tier_exit",    "tma_wait", "chunk_map",    "scan_wait", "scan_setup"};
+                                       "host_alloc", "tier_exit",    "tma_wait", "chunk_map",    "scan_wait", "scan_setup",
+                                       "delta_wait"};
   std::lock_guard<std::mutex> lock(g_fault_mu);
   if (!point || !point[0]) {
     g_fault_point[0] = 0;

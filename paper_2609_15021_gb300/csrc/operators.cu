@@ -843,6 +843,22 @@ kvx_status check_delta(const kvx_state_batch* b, const kvx_delta* d) {
   return KVX_OK;
 }
 
+// kv_state_delta's workspace: what the chunks of 64 tokens are worked on with, where there are any.
+struct DeltaSpace {
+  int32_t by_token, pieces;
+  int64_t heads, bytes;  // heads: the offset of head_space
+};
+kvx_status delta_space(const kvx_state_batch* b, const kvx_delta* d, DeltaSpace* w) {
+  *w = {};
+  if (!delta_by_chunks(b->tokens, b->num_seqs, b->starts, d->state_dim, &w->by_token)) return KVX_OK;
+  const int64_t pieces = b->tokens / kDeltaChunk + b->num_seqs;
+  if (pieces > kMaxRows / d->heads) return refuse(KVX_ERANGE, "more than 2^30 chunks and heads");
+  w->pieces = (int32_t)pieces;
+  w->heads = pieces * d->groups * 2 * kDeltaChunk * d->state_dim * 2;
+  w->bytes = w->heads + pieces * d->heads * kDeltaHeadBytes;
+  return KVX_OK;
+}
+
 // A value a token and head, 2 bytes each.
 kvx_status check_gate(DeviceMemory& mem, const void* p, int64_t tokens, int64_t stride, int64_t heads, const char* what) {
   int64_t bytes;
@@ -857,9 +873,11 @@ kvx_status check_gate(DeviceMemory& mem, const void* p, int64_t tokens, int64_t 
 kvx_status kv_state_delta_workspace(kvx_ctx* c, const kvx_state_batch* batch, const kvx_delta* d, int64_t* bytes) {
   return guarded([&]() -> kvx_status {
     if (!c || !batch || !d || !bytes) return KVX_EINVAL;
-    const kvx_status st = check_delta(batch, d);
+    DeltaSpace space;
+    kvx_status st = check_delta(batch, d);
+    if (st == KVX_OK) st = delta_space(batch, d, &space);
     if (st != KVX_OK) return st;
-    *bytes = 0;
+    *bytes = space.bytes;
     return KVX_OK;
   });
 }
@@ -870,7 +888,9 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
   return guarded([&]() -> kvx_status {
     if (!c || !state || !batch || !a) return KVX_EINVAL;
     const CtxView ctx = view_of(c);
+    DeltaSpace space;
     kvx_status st = check_delta(batch, a);
+    if (st == KVX_OK) st = delta_space(batch, a, &space);
     if (st != KVX_OK) return st;
     CurrentDevice guard(ctx.device);
     if (!guard.ok) return KVX_ECUDA;
@@ -891,8 +911,18 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
     }
     if (dt && (st = check_words(mem, a->A, h, "A")) != KVX_OK) return st;
     if (dt && a->dt_bias && (st = check_words(mem, a->dt_bias, h, "dt_bias")) != KVX_OK) return st;
-    (void)workspace;
-    (void)workspace_bytes;
+    if (space.bytes > 0) {
+      if (workspace_bytes < space.bytes) return refuse(KVX_ERANGE, "workspace is smaller than kv_state_delta_workspace says");
+      if (!workspace || ((uintptr_t)workspace & 15)) return refuse(workspace ? KVX_EALIGN : KVX_EINVAL, "workspace");
+      if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
+    }
+    p.by_token = space.by_token;
+    p.pieces = space.pieces;
+    p.rows_space = (uint8_t*)workspace;
+    p.head_space = (uint8_t*)workspace + space.heads;
+    p.wait_cycles = ctx.wait_cycles;
+    p.timeout = ctx.timeout;
+    p.stall = p.pieces && fault_point("delta_wait");
     p.q = (const uint8_t*)q;
     p.k = (const uint8_t*)k;
     p.v = (const uint8_t*)v;
@@ -915,11 +945,12 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
     p.head_dim = a->head_dim;
     p.state_dim = a->state_dim;
     p.heads_per_group = a->heads / a->groups;
+    p.groups = a->groups;
     p.softplus = a->softplus;
     p.sigmoid = a->sigmoid;
     p.normalize = a->normalize;
     p.scale = a->scale ? a->scale : 1.f / std::sqrt((float)n);
     p.eps = a->eps;
-    return KVX_LAUNCHED(c, launch_delta(p, a->type, ctx.num_sms, stream), 1);
+    return KVX_LAUNCHED(c, launch_delta(p, a->type, ctx.num_sms, stream), (p.by_token >= 0) + (p.pieces ? 2 : 0));
   });
 }

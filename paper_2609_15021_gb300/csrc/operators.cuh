@@ -189,9 +189,19 @@ struct DeltaParams {
   uint8_t* out;
   const float *A, *dt_bias;
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, dt_token, beta_token, out_token, out_head;  // in elements
-  int32_t heads, head_dim, state_dim, heads_per_group, softplus, sigmoid, normalize;
+  int32_t heads, head_dim, state_dim, heads_per_group, groups, softplus, sigmoid, normalize;
   float scale, eps;
+  int32_t by_token;          // sequences of up to so many tokens go token by token, the others by chunks; -1: none
+  int32_t pieces;            // room for chunks; 0: no sequence goes by chunks
+  uint8_t* rows_space;       // workspace: a chunk's and group's keys and queries
+  uint8_t* head_space;       // and what else a chunk and head has
+  long long wait_cycles;     // limit of a wait for a copy
+  int* timeout;              // set when one ran out
+  bool stall;                // fault point "delta_wait": the second chunk's copies are not made
 };
+constexpr int32_t kDeltaChunk = 64, kDeltaHeadBytes = 16768;  // tokens; bytes of head_space
+// Whether a batch's sequences go by chunks, and which do not (*by_token).
+bool delta_by_chunks(int64_t tokens, int32_t num_seqs, bool packed, int32_t state_dim, int32_t* by_token);
 // Pieces that the workspace has room for: as many as sequences whose rows do not overlap can have.  No more than there are
 // SMs and sequences, where sequences are cut.
 inline int64_t scan_pieces(const StateView& v, int32_t segment) { return v.tokens / segment + v.num_seqs; }
@@ -221,6 +231,7 @@ cudaError_t launch_evict(const EvictParams& p, cudaStream_t s);
 cudaError_t launch_conv(const ConvParams& p, int type, cudaStream_t s);
 cudaError_t launch_scan(const ScanParams& p, int type, int num_sms, cudaStream_t s);
 cudaError_t launch_delta(const DeltaParams& p, int type, int num_sms, cudaStream_t s);
+cudaError_t launch_delta_chunks(const DeltaParams& p, int type, cudaStream_t s);
 cudaError_t launch_scan_chunks(const ScanParams& p, int type, cudaStream_t s);
 
 #ifdef __CUDACC__

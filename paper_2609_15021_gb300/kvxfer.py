@@ -1165,10 +1165,11 @@ def kv_state_scan(ctx, state: StateSlots, batch: StateBatch, x, dt, A, B, C, out
            "kv_state_scan")
 
 
-def kv_state_delta_workspace(ctx, batch: StateBatch, heads: int, head_dim: int, state_dim: int):
-    """A workspace tensor for kv_state_delta calls of these shapes; one call uses it at a time."""
+def kv_state_delta_workspace(ctx, batch: StateBatch, heads: int, head_dim: int, state_dim: int, groups: int | None = None):
+    """A workspace tensor for kv_state_delta calls of these shapes (groups None: of any number of them); one call uses it
+    at a time."""
     import torch
-    c = kvx_delta(heads=heads, head_dim=head_dim, state_dim=state_dim, groups=1)
+    c = kvx_delta(heads=heads, head_dim=head_dim, state_dim=state_dim, groups=groups or heads)
     out = ctypes.c_int64()
     _check(_lib.kv_state_delta_workspace(ctx, ctypes.byref(batch._c), ctypes.byref(c), ctypes.byref(out)),
            "kv_state_delta_workspace")

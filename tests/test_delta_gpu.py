@@ -324,6 +324,36 @@ def test_starts_that_do_not_ascend_stay_within_the_rows(ctx, starts):
     assert (k.kv_get_device_error(ctx) != -1) == bad
 
 
+def test_wait_for_a_copy_runs_out_then_recovery():
+    """The second chunk's copies are left out: the walk gives up after its limit, reports it and writes no state."""
+    k = kvx()
+    c = k.kv_ctx_create(0, wait_cycles=2_000_000)
+    try:
+        t, heads, p, n = 200, 2, 64, 64
+        data = Inputs(t, heads, p, n, 1, BF16)
+        x, A = data.cuda(), data.A.cuda()
+        batch, _ = batch_of([t], [0], [1])
+        outs = []
+        for point in (None, "delta_wait", None):
+            st = Slots(2, heads, p, n)
+            out = torch.zeros((t, heads, p), dtype=BF16, device="cuda")
+            if point:
+                k.kv_fault_inject(point)
+            k.kv_state_delta(c, st.slots, batch, out=out, A=A, workspace=k.kv_state_delta_workspace(c, batch, heads, p, n), **x)
+            torch.cuda.synchronize()
+            if point:
+                assert torch.equal(st.dev.cpu(), st.cpu)
+                with pytest.raises(k.KvxError) as e:
+                    k.kv_get_device_error(c)
+                assert e.value.status == k.KVX_ETIMEOUT
+            else:
+                outs.append((out, st.dev))
+                assert k.kv_get_device_error(c) == -1
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+    finally:
+        k.kv_ctx_destroy(c)
+
+
 def test_captured_step(ctx):
     """Replayed with other slots, starts and freshness, on a workspace that calls in between have used."""
     k = kvx()
