@@ -535,6 +535,7 @@ kvx_status kv_bounds(kvx_ctx* c, const kvx_pool* pool, int32_t layer, const kvx_
     if ((st = check_bounds(mem, pool, bounds)) != KVX_OK) return st;
     p.boxes = bounds->boxes;
     p.sizes = bounds->sizes;
+    p.by_heads = div31((uint32_t)pool->num_heads);
     return KVX_LAUNCHED(c, launch_bounds(p, cache_type, stream), 1);
   });
 }

@@ -63,6 +63,8 @@ struct RotaryParams {
   int64_t q_token, q_head, out_token, out_head;  // strides in bytes
   int32_t q_heads, rotary_dim, interleaved;
   float rotary_scale, eps, weight_offset;
+  float inverse_dim;  // 1 / head_dim
+  int32_t parts;      // warps of a token
 };
 
 struct BoundsParams {
@@ -70,6 +72,7 @@ struct BoundsParams {
   int8_t* boxes;
   float* sizes;
   int32_t new_tokens, pages_each;  // pages_each: that a sequence's new tokens may lie in
+  Div31 by_heads;
 };
 
 struct SelectParams {

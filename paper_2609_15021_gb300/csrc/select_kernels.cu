@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kBoundsThreads = 128;
 
-// The least and the greatest of two pairs of keys, and whether there is one that is not finite.
+// The least and the greatest of two pairs of keys; NaN where there is one.
 template <class C>
 struct Pairs {
   using V = __nv_bfloat162;
@@ -30,13 +30,13 @@ struct Pairs<Fp16> {
 template <class C>
 __device__ __forceinline__ uint32_t least2(uint32_t a, uint32_t b) {
   using V = typename Pairs<C>::V;
-  const V v = __hmin2(*reinterpret_cast<const V*>(&a), *reinterpret_cast<const V*>(&b));
+  const V v = __hmin2_nan(*reinterpret_cast<const V*>(&a), *reinterpret_cast<const V*>(&b));
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 template <class C>
 __device__ __forceinline__ uint32_t most2(uint32_t a, uint32_t b) {
   using V = typename Pairs<C>::V;
-  const V v = __hmax2(*reinterpret_cast<const V*>(&a), *reinterpret_cast<const V*>(&b));
+  const V v = __hmax2_nan(*reinterpret_cast<const V*>(&a), *reinterpret_cast<const V*>(&b));
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 // Two e4m3 values as fp16.
@@ -46,8 +46,22 @@ __device__ __forceinline__ uint32_t widen2(uint32_t v) {
   return r;
 }
 
-// A warp has one head of one page: its lanes have a row's vectors, some rows at once, and meet at the end.  C: the type
-// that keys are compared in (fp16 for e4m3).  Bound by the keys' bytes.
+// Quotients by one number, rounded to the nearest: as `divided` of attend_common.cuh, where the number leaves the residuals their
+// bits, by division elsewhere.
+struct Divisor {
+  float by, inverse;
+  bool plain;
+  __device__ __forceinline__ explicit Divisor(float d) : by(d), inverse(1.f / d), plain(d > 0x1p-80f && d < 0x1p80f) {}
+  __device__ __forceinline__ float operator()(float x) const {
+    if (!plain) return by > 0.f ? __fdiv_rn(x, by) : 0.f;
+    const float q = x * inverse;
+    return fmaf(fmaf(-q, by, x), inverse, q);
+  }
+};
+
+// A warp has one head of one page: its lanes have a row's vectors, some rows at once, and meet at the end, after which, where
+// a row is half a warp, one half makes the low bounds and the other the high ones.  C: the type that keys are compared in
+// (fp16 for e4m3).
 template <class C, bool kWide, int kVecs>  // kVecs: vectors of a row, rounded up to a power of two
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsParams p) {
   wait_for_previous();
@@ -55,11 +69,10 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
   constexpr int kPairs = kWide ? 8 : 4;  // of a vector
   constexpr int kRows = 32 / kVecs;
   const int lane = threadIdx.x & 31, vec = lane % kVecs, sub = lane / kVecs;
-  const int64_t unit = (int64_t)blockIdx.x * (kBoundsThreads / 32) + (threadIdx.x >> 5);
-  const int64_t sp = unit / v.heads;
-  const int32_t h = (int32_t)(unit - sp * v.heads), s = (int32_t)(sp / p.pages_each), n = (int32_t)(sp - (int64_t)s * p.pages_each);
-  if (s >= v.num_seqs) return;
-  if (n == 0 && h == 0 && lane == 0) check_length(v, s);
+  const int32_t s = blockIdx.y, unit = (int32_t)blockIdx.x * (kBoundsThreads / 32) + (threadIdx.x >> 5);
+  const int32_t n = (int32_t)quotient(p.by_heads, (uint32_t)unit), h = unit - n * v.heads;
+  if (n >= p.pages_each) return;
+  if (unit == 0 && lane == 0) check_length(v, s);
   const int32_t length = length_of(v, s), block = (int32_t)v.by_block.d;
   const int32_t first = (int32_t)quotient(v.by_block, (uint32_t)max(length - p.new_tokens, 0)), page = first + n;
   if ((int64_t)page * block >= length) return;
@@ -71,20 +84,21 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
   const int64_t step = v.token_rows * v.row_bytes;
   const bool used = vec * 16 < v.row_bytes;
   constexpr uint32_t kInf = std::is_same<C, Bf16>::value ? 0x7F807F80u : 0x7C007C00u;
-  uint32_t low[kPairs], high[kPairs], carries = 0;
+  uint32_t low[kPairs], high[kPairs];
 #pragma unroll
-  for (int k = 0; k < kPairs; ++k) low[k] = kInf, high[k] = kInf | 0x80008000u;
+  for (int k = 0; k < kPairs; ++k) low[k] = used ? kInf : 0, high[k] = used ? kInf | 0x80008000u : 0;
 #pragma unroll 8
   for (int32_t t = sub; t < held; t += kRows) {
-    const uint4 x = used ? __ldg(reinterpret_cast<const uint4*>(from + t * step)) : make_uint4(0, 0, 0, 0);
+    if (!used) break;
+    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(from + t * step));
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
       const uint32_t u = kWide ? widen2(w[k / 2] >> k % 2 * 16) : w[k];
       low[k] = least2<C>(low[k], u), high[k] = most2<C>(high[k], u);
-      carries |= odd_carry<C>(u);
     }
   }
+  __syncwarp();
 #pragma unroll
   for (int m = kVecs; m < 32; m <<= 1)
 #pragma unroll
@@ -92,45 +106,48 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
       low[k] = least2<C>(low[k], __shfl_xor_sync(~0u, low[k], m));
       high[k] = most2<C>(high[k], __shfl_xor_sync(~0u, high[k], m));
     }
-  float most = 0.f;
-  float2 lo[kPairs], hi[kPairs];
+  uint32_t most = 0, carries = 0;  // of both numbers' magnitudes, as their bits are in order
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) {
-    lo[k] = unpack2<C>(low[k]), hi[k] = unpack2<C>(high[k]);
-    if (used) most = fmaxf(most, fmaxf(fmaxf(fabsf(lo[k].x), fabsf(lo[k].y)), fmaxf(fabsf(hi[k].x), fabsf(hi[k].y))));
+    carries |= odd_carry<C>(low[k]) | odd_carry<C>(high[k]);
+    most = __vmaxu2(most, __vmaxu2(low[k] & 0x7FFF7FFFu, high[k] & 0x7FFF7FFFu));
   }
   const bool odd = __any_sync(~0u, odd_carried(carries));
-#pragma unroll
-  for (int m = kVecs / 2; m; m >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, m));
-  const float size = odd ? FLT_MAX : __fdiv_rn(most, 127.f);
+  most = __reduce_max_sync(~0u, max(most & 0xFFFFu, most >> 16));
+  const float size = odd ? FLT_MAX : __fdiv_rn(unpack2<C>(most).x, 127.f);
   const int64_t at = (int64_t)number * v.heads + h;
   if (lane == 0) p.sizes[at] = size;
-  if (sub || !used) return;
-  auto whole = [&](float x, bool up) -> uint32_t {
-    float r = size > 0.f ? __fdiv_rn(x, size) : 0.f;
-    r = up ? ceilf(r) : floorf(r);
-    return (uint32_t)(int32_t)fminf(fmaxf(r, -127.f), 127.f) & 0xFFu;
-  };
-  uint32_t out[2][kPairs / 2];
+  if (!used || sub > 1) return;
+  const Divisor by(size);
+  const bool both = kRows == 1;
 #pragma unroll
-  for (int k = 0; k < kPairs; k += 2) {
-    out[0][k / 2] = odd ? 0x81818181u : whole(lo[k].x, false) | whole(lo[k].y, false) << 8 | whole(lo[k + 1].x, false) << 16 | whole(lo[k + 1].y, false) << 24;
-    out[1][k / 2] = odd ? 0x7F7F7F7Fu : whole(hi[k].x, true) | whole(hi[k].y, true) << 8 | whole(hi[k + 1].x, true) << 16 | whole(hi[k + 1].y, true) << 24;
-  }
-  int8_t* to = p.boxes + at * 2 * v.head_dim + vec * 2 * kPairs;
+  for (int side = 0; side < 2; ++side) {
+    if (!both && side != sub) continue;
+    uint32_t out[kPairs / 2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < kPairs; ++k) {
+      const float2 x = unpack2<C>(side ? high[k] : low[k]);
+      float2 r = make_float2(by(x.x), by(x.y));
+      r = side ? make_float2(ceilf(r.x), ceilf(r.y)) : make_float2(floorf(r.x), floorf(r.y));
+      const int32_t a = (int32_t)fminf(fmaxf(r.x, -127.f), 127.f), b = (int32_t)fminf(fmaxf(r.y, -127.f), 127.f);
+      const uint32_t pair = (uint32_t)(a & 0xFF) | (uint32_t)(b & 0xFF) << 8;
+      out[k / 2] = k % 2 ? out[k / 2] | pair << 16 : pair;
+    }
+    if (odd)
+#pragma unroll
+      for (int k = 0; k < kPairs / 2; ++k) out[k] = side ? 0x7F7F7F7Fu : 0x81818181u;
+    int8_t* to = p.boxes + at * 2 * v.head_dim + side * v.head_dim + vec * 2 * kPairs;
     if constexpr (kWide)
-      *reinterpret_cast<uint4*>(to + k * v.head_dim) = make_uint4(out[k][0], out[k][1], out[k][2], out[k][3]);
+      *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
     else
-      *reinterpret_cast<uint2*>(to + k * v.head_dim) = make_uint2(out[k][0], out[k][1]);
+      *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
   }
 }
 
 template <class C, bool kWide>
 cudaError_t bounds(const BoundsParams& p, cudaStream_t s) {
-  const int64_t warps = (int64_t)p.pages.num_seqs * p.pages_each * p.pages.heads;
-  const dim3 grid((unsigned)((warps * 32 + kBoundsThreads - 1) / kBoundsThreads));
+  constexpr int kWarps = kBoundsThreads / 32;
+  const dim3 grid((unsigned)(((int64_t)p.pages_each * p.pages.heads + kWarps - 1) / kWarps), p.pages.num_seqs);
   const int64_t vecs = p.pages.row_bytes / 16;
   auto kernel = vecs <= 4 ? bounds_kernel<C, kWide, 4> : vecs <= 8 ? bounds_kernel<C, kWide, 8> : vecs <= 16 ? bounds_kernel<C, kWide, 16> : bounds_kernel<C, kWide, 32>;
   return launch_after(kernel, grid, kBoundsThreads, 0, s, p);
@@ -198,29 +215,49 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
     box[k] = reinterpret_cast<const uint8_t*>(p.boxes) + ((int64_t)(there[k] ? row / v.page_rows : 0) * v.heads + h) * k_all;
   }
 
-  for (int32_t r = warp; r < tiles * 8; r += kScoreThreads / 32) {
-    const bool real = r < rows;
-    const int32_t t = real ? r / p.group : 0, i = real ? r - t * p.group : 0;
-    const typename E::T* q = reinterpret_cast<const typename E::T*>(p.q + ((int64_t)s * p.new_tokens + t0 + t) * p.q_token + (h * p.group + i) * p.q_head);
-    float top = 0.f;
-    bool fine = true;
-    for (int32_t d = lane; d < v.head_dim; d += 32) {
-      const float x = E::up(q[d]);
-      fine &= isfinite(x);
-      top = fmaxf(top, fabsf(x));
+  // Rows of queries, four vectors of 16 bytes in flight: one row a vector, 8 elements a lane.
+  constexpr int kAtOnce = 4, kWarps = kScoreThreads / 32;
+  const bool used = lane * 8 < v.head_dim;
+  for (int32_t r0 = warp; r0 < tiles * 8; r0 += kAtOnce * kWarps) {
+    uint4 raw[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int32_t r = r0 + k * kWarps, t = r / p.group, i = r - t * p.group;
+      raw[k] = make_uint4(0, 0, 0, 0);
+      if (r < rows && used)
+        raw[k] = *(reinterpret_cast<const uint4*>(p.q + ((int64_t)s * p.new_tokens + t0 + t) * p.q_token + (h * p.group + i) * p.q_head) + lane);
     }
-    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-    fine = __all_sync(~0u, fine) && real;
-    const float step = fine ? __fdiv_rn(top, 127.f) : 0.f;
-    if (lane == 0) step_s[r] = step;
-    for (int32_t d = lane; d < k_pad / 2; d += 32) {  // what is behind the last element, zeros
-      const float w = d < v.head_dim && step > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(E::up(q[d]), step)), -127.f), 127.f) : 0.f;
-      if (d < v.head_dim) {
-        q_s[r * pitch + d] = __float2half_rn(fminf(w, 0.f));
-        q_s[r * pitch + v.head_dim + d] = __float2half_rn(fmaxf(w, 0.f));
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int32_t r = r0 + k * kWarps;
+      if (r >= tiles * 8) break;
+      uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w}, most = 0, carries = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) carries |= odd_carry<E>(w[j]), most = __vmaxu2(most, w[j] & 0x7FFF7FFFu);
+      const bool fine = !__any_sync(~0u, odd_carried(carries));
+      most = __reduce_max_sync(~0u, max(most & 0xFFFFu, most >> 16));
+      const float step = fine ? __fdiv_rn(unpack2<E>(most).x, 127.f) : 0.f;
+      if (lane == 0) step_s[r] = step;
+      if (!used) continue;
+      const Divisor by(step);
+      __half2 up[4], down[4];
+      const __half2 zero = __floats2half2_rn(0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 x = unpack2<E>(fine ? w[j] : 0);
+        const __half2 whole = __floats2half2_rn(fminf(fmaxf(rintf(by(x.x)), -127.f), 127.f), fminf(fmaxf(rintf(by(x.y)), -127.f), 127.f));
+        up[j] = __hmax2(whole, zero), down[j] = __hmin2(whole, zero);
       }
+      uint2* to = reinterpret_cast<uint2*>(q_s + r * pitch + lane * 8);
+      to[0] = *reinterpret_cast<const uint2*>(&down[0]), to[1] = *reinterpret_cast<const uint2*>(&down[2]);
+      to = reinterpret_cast<uint2*>(q_s + r * pitch + v.head_dim + lane * 8);
+      to[0] = *reinterpret_cast<const uint2*>(&up[0]), to[1] = *reinterpret_cast<const uint2*>(&up[2]);
     }
-    for (int32_t d = k_all + lane; d < k_pad; d += 32) q_s[r * pitch + d] = __float2half_rn(0.f);
+  }
+  // what is behind the last element, zeros
+  for (int32_t i = threadIdx.x; i < tiles * 8 * (k_pad - k_all); i += kScoreThreads) {
+    const int32_t r = i / (k_pad - k_all);
+    q_s[r * pitch + k_all + i - r * (k_pad - k_all)] = __float2half_rn(0.f);
   }
   __syncthreads();
   const int32_t dot_pitch = tiles * 8 + 1;
@@ -275,10 +312,9 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
 // ---------------------------------------------------------------- the best
 
 constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
-constexpr int kPickBins = 2048;  // digits of 11, 11 and 10 bits
+constexpr int kPickBins = 2048;
 
-// Whole numbers in the order of the scores: NaN as -inf, -0 as +0.  None is kAlways.
-constexpr uint32_t kAlwaysPicked = UINT32_MAX;
+// Whole numbers in the order of the scores: NaN as -inf, -0 as +0.  None is 0.
 __device__ __forceinline__ uint32_t score_rank(float w) {
   const uint32_t u = __float_as_uint(fmaxf(w, -INFINITY) + 0.f);
   return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
@@ -292,16 +328,20 @@ __device__ __forceinline__ uint32_t upto_lane(uint32_t v) {
   return v;
 }
 
-// A CTA picks the pages of one query and head: the smallest picked score is the budget'th largest, found 11 bits at a time by
-// counting; of the pages that have just that score the first ones are picked, and a page's place among the picked
-// follows from a scan, so that they come out in their order.
+// A CTA picks the pages of one query and head: the smallest picked score is the budget'th largest.  It is found by counting
+// pages in 2,048 equal ranges of what their ranks span, then of the range that it falls in, until all pages of that are
+// picked or it is one rank, of whose pages the first are picked (as a rule once or twice, and without many pages in
+// one counter: digits of the ranks themselves, of which a batch's scores share most, took three passes and twice as long).
+// A warp has a stretch of neighbouring pages, so that a page's place among the picked follows from ballots and one sum
+// over the warps.
 __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constant__ SelectParams p) {
   wait_for_previous();
   const PagesView& v = p.pages;
+  constexpr int kKept = 8;  // ranks that a lane keeps: those of up to 4,096 pages are read once
   __shared__ int32_t hist[kPickBins];
-  __shared__ uint32_t warp_counts[kPickWarps];
-  __shared__ uint32_t prefix_s;
-  __shared__ int32_t want_s;
+  __shared__ uint32_t warp_a[kPickWarps], warp_b[kPickWarps];
+  __shared__ uint32_t bin_s;
+  __shared__ int32_t want_s, count_s;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int32_t token = blockIdx.x / v.heads, h = blockIdx.x - token * v.heads;
   const int32_t s = token / p.new_tokens, t = token - s * p.new_tokens;
@@ -317,60 +357,86 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
   }
   const float* scores = p.scores + ((int64_t)token * v.heads + h) * p.score_stride;
   const int32_t last = n - p.recent;
-  auto rank = [&](int32_t i) { return i < p.sinks || i >= last ? kAlwaysPicked : score_rank(scores[i]); };
-  int32_t want = keep;
-  uint32_t prefix = 0;
-  auto digit = [&](int kAt, int kBits) {
-    for (int32_t i = threadIdx.x; i < kPickBins; i += kPickThreads) hist[i] = 0;
-    __syncthreads();
-    for (int32_t i = threadIdx.x; i < n; i += kPickThreads) {
-      const uint32_t r = rank(i);
-      if (kAt + kBits == 32 || r - prefix < 1u << (kAt + kBits)) atomicAdd(&hist[r >> kAt & ((1u << kBits) - 1)], 1);
-    }
-    __syncthreads();
-    // the digit of the want'th largest: sums from the top, four bins a thread
-    int32_t b[4], sum = 0;
-    const int32_t top_bin = kPickBins - 1 - 4 * (int32_t)threadIdx.x;
+  // The ranks of pages that are picked by their scores; 0, which no score has, of the others.
+  const int32_t each = (n + kPickThreads - 1) / kPickThreads * 32, from = min(warp * each, n), to = min(from + each, n);
+  auto always = [&](int32_t i) { return i < p.sinks || i >= last; };
+  auto rank = [&](int32_t i) { return i < to && !always(i) ? score_rank(scores[i]) : 0u; };
+  uint32_t kept[kKept];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) b[k] = hist[top_bin - k], sum += b[k];
-    const int32_t upto = (int32_t)upto_lane(sum);
-    if (lane == 31) warp_counts[warp] = upto;
-    __syncthreads();
-    int32_t before = upto - sum;
-    for (int i = 0; i < warp; ++i) before += warp_counts[i];
-    int32_t left = want - before;
-    if (left > 0 && left <= sum) {  // one thread's
-      int k = 0;
-      while (left > b[k]) left -= b[k++];
-      prefix_s = prefix | (uint32_t)(top_bin - k) << kAt;
-      want_s = left;
-    }
-    __syncthreads();
-    prefix = prefix_s;
-    want = want_s;
+  for (int k = 0; k < kKept; ++k) kept[k] = rank(from + k * 32 + lane);
+  auto for_each = [&](auto&& f) {  // of the warp's pages, 32 at once
+#pragma unroll
+    for (int k = 0; k < kKept; ++k)
+      if (from + k * 32 < to) f(from + k * 32 + lane, kept[k]);
+    for (int32_t i = from + kKept * 32; i < to; i += 32) f(i + lane, rank(i + lane));
   };
-  digit(21, 11);
-  digit(10, 11);
-  digit(0, 10);
-  // want: how many pages of rank `prefix` itself are picked
-  int32_t above_all = 0, equal_all = 0;
-  for (int32_t base = 0; base < n; base += kPickThreads) {
-    const int32_t i = base + threadIdx.x;
-    const uint32_t r = i < n ? rank(i) : 0;
-    const bool above = i < n && r > prefix, equal = i < n && r == prefix;
-    const uint32_t mine = (uint32_t)above | (uint32_t)equal << 16, upto = upto_lane(mine);
-    __syncthreads();
-    if (lane == 31) warp_counts[warp] = upto;
-    __syncthreads();
-    uint32_t before = upto - mine, all = 0;
-    for (int w = 0; w < kPickWarps; ++w) {
-      if (w < warp) before += warp_counts[w];
-      all += warp_counts[w];
+  uint32_t low = UINT32_MAX, high = 0;
+  for_each([&](int32_t, uint32_t r) {
+    if (r) low = min(low, r), high = max(high, r);
+  });
+  low = __reduce_min_sync(~0u, low), high = __reduce_max_sync(~0u, high);
+  if (lane == 0) warp_a[warp] = low, warp_b[warp] = high;
+  for (int32_t i = threadIdx.x; i < kPickBins; i += kPickThreads) hist[i] = 0;
+  __syncthreads();
+  low = __reduce_min_sync(~0u, warp_a[lane % kPickWarps]), high = __reduce_max_sync(~0u, warp_b[lane % kPickWarps]);
+  int32_t want = keep - min(p.sinks + p.recent, n);  // of those picked by their scores, which are more than that
+  uint32_t border = UINT32_MAX;  // ranks above it are picked, and the first `equal` of those that have it
+  int32_t equal = 0;
+  if (want > 0) {
+    for (;;) {
+      const int shift = max(0, 21 - __clz(high - low));  // (high - low) >> shift is below 2^11
+      for_each([&](int32_t, uint32_t r) {
+        if (r >= low && r <= high) atomicAdd(&hist[(r - low) >> shift], 1);
+      });
+      __syncthreads();
+      // the range of the want'th largest: sums from the top, four ranges a thread
+      int32_t b[4], sum = 0;
+      const int32_t top_bin = kPickBins - 1 - 4 * (int32_t)threadIdx.x;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) b[k] = hist[top_bin - k], sum += b[k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) hist[top_bin - k] = 0;
+      const int32_t upto = (int32_t)upto_lane(sum);
+      if (lane == 31) warp_a[warp] = upto;
+      __syncthreads();
+      const uint32_t mine = lane < kPickWarps && lane < warp ? warp_a[lane] : 0;
+      const int32_t before = upto - sum + (int32_t)__reduce_add_sync(~0u, mine);
+      int32_t left = want - before;
+      if (left > 0 && left <= sum) {  // one thread's
+        int k = 0;
+        while (left > b[k]) left -= b[k++];
+        bin_s = (uint32_t)(top_bin - k), want_s = left, count_s = b[k];
+      }
+      __syncthreads();
+      low += bin_s << shift;
+      want = want_s;
+      if (shift == 0 || count_s == want) {
+        border = shift == 0 ? low : low - 1;  // low is above 0: 0 is no score's
+        equal = shift == 0 ? want : 0;
+        break;
+      }
+      high = min(high, low + ((1u << shift) - 1));
     }
-    const int32_t a = above_all + (int32_t)(before & 0xFFFF), e = equal_all + (int32_t)(before >> 16);
-    if (above || (equal && e < want)) out[a + min(e, want)] = i;
-    above_all += (int32_t)(all & 0xFFFF), equal_all += (int32_t)(all >> 16);
   }
+  // A page's place: those picked in front of it.
+  uint32_t above = 0, same = 0;
+  for_each([&](int32_t i, uint32_t r) {
+    above += __popc(__ballot_sync(~0u, i < to && (r > border || always(i))));
+    same += __popc(__ballot_sync(~0u, r == border && r != 0));
+  });
+  __syncthreads();  // warp_a has been read
+  if (lane == 0) warp_a[warp] = above, warp_b[warp] = same;
+  __syncthreads();
+  int32_t a = (int32_t)__reduce_add_sync(~0u, lane < warp ? warp_a[lane % kPickWarps] : 0);
+  int32_t e = (int32_t)__reduce_add_sync(~0u, lane < warp ? warp_b[lane % kPickWarps] : 0);
+  const uint32_t below = (1u << lane) - 1;
+  for_each([&](int32_t i, uint32_t r) {
+    const bool is_above = i < to && (r > border || always(i)), is_equal = r == border && r != 0;
+    const uint32_t a_bits = __ballot_sync(~0u, is_above), e_bits = __ballot_sync(~0u, is_equal);
+    const int32_t my_a = a + __popc(a_bits & below), my_e = e + __popc(e_bits & below);
+    if (is_above || (is_equal && my_e < equal)) out[my_a + min(my_e, equal)] = i;
+    a += __popc(a_bits), e += __popc(e_bits);
+  });
 }
 
 template <class E>
