@@ -758,18 +758,20 @@ def _cache_type(pool: KvPool, given) -> int:
 
 
 _dtypes: dict = {}
+_byref = ctypes.byref
 
 
 def _need(x, what: str, dtype: str, shape=None) -> None:
     """A tensor of `dtype` (and shape) whose innermost dimension is contiguous."""
-    if dtype not in _dtypes:
+    want = _dtypes.get(dtype)
+    if want is None:
         import torch
-        _dtypes[dtype] = getattr(torch, dtype)
-    if x.dtype is not _dtypes[dtype]:
+        want = _dtypes[dtype] = getattr(torch, dtype)
+    if x.dtype is not want:
         raise TypeError(f"{what} must be {dtype}, not {x.dtype}")
     if shape is not None and x.shape != shape:
         raise ValueError(f"{what} is {tuple(x.shape)}, not {tuple(shape)}")
-    if x.dim() and x.shape[-1] > 1 and x.stride(-1) != 1:
+    if not x.is_contiguous() and x.shape[-1] > 1 and x.stride(-1) != 1:
         raise ValueError(f"the last dimension of {what} must be contiguous")
 
 
@@ -780,6 +782,19 @@ def _need_rows(x, what: str, dtype, shape) -> None:
         raise ValueError(f"{what} is {tuple(x.shape)}, not {tuple(shape)}")
     if x.stride(-1) != 1:
         raise ValueError(f"the last dimension of {what} must be contiguous")
+
+
+def _row_strides(x, what: str, dtype, shape) -> tuple:
+    """The strides of a tensor of `dtype` and `shape` whose innermost dimension is contiguous: _need_rows in one look, for
+    calls that are as short as their checks."""
+    if x.dtype is not dtype:
+        raise TypeError(f"{what} must be {dtype}, not {x.dtype}")
+    if x.shape != shape:
+        raise ValueError(f"{what} is {tuple(x.shape)}, not {tuple(shape)}")
+    strides = x.stride()
+    if strides[-1] != 1:
+        raise ValueError(f"the last dimension of {what} must be contiguous")
+    return strides
 
 
 class KvBatch:
@@ -837,10 +852,10 @@ class KvRotary:
                     raise ValueError(f"{what} must be [head_dim]")
                 _check_tensor(w, what)
         self.q_heads, self.inv_freq, self.q_weight, self.k_weight = q_heads, inv_freq, q_weight, k_weight
-        self._c = kvx_rotary(q_heads, 0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, scale,
-                             None if inv_freq is None else inv_freq.data_ptr(), None,
-                             None if q_weight is None else q_weight.data_ptr(),
-                             None if k_weight is None else k_weight.data_ptr(), eps, weight_offset)
+        self._front = (q_heads, 0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, scale,
+                       None if inv_freq is None else inv_freq.data_ptr())
+        self._rear = (None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
+                      weight_offset)
 
 
 def kv_append_rotary(ctx, pool: KvPool, layer: int, batch: KvBatch, rotary: KvRotary, query, key, value, query_out,
@@ -850,28 +865,25 @@ def kv_append_rotary(ctx, pool: KvPool, layer: int, batch: KvBatch, rotary: KvRo
     to query_out (which may be query).  positions: device int32 [tokens], where they are not the tokens' places
     in the cache (after an eviction)."""
     tokens = key.shape[0] if starts is not None else batch.num_seqs * new_tokens
-    shape = (tokens, pool.num_heads, pool.head_dim)
-    _need_rows(key, "key", key.dtype, shape)
-    _need_rows(value, "value", key.dtype, shape)
-    _need_rows(query, "query", key.dtype, (tokens, rotary.q_heads, pool.head_dim))
-    _need_rows(query_out, "query_out", key.dtype, query.shape)
+    dtype, dim = key.dtype, pool.head_dim
+    ks = _row_strides(key, "key", dtype, (tokens, pool.num_heads, dim))
+    vs = _row_strides(value, "value", dtype, (tokens, pool.num_heads, dim))
+    qs = _row_strides(query, "query", dtype, (tokens, rotary.q_heads, dim))
+    outs = _row_strides(query_out, "query_out", dtype, (tokens, rotary.q_heads, dim))
     if starts is not None:
         _need(starts, "starts", "int32", (batch.num_seqs + 1,))
-    for w, what in ((rotary.q_weight, "q_weight"), (rotary.k_weight, "k_weight")):
-        if w is not None:
-            _need_rows(w, what, key.dtype, (pool.head_dim,))
-    r = kvx_rotary.from_buffer_copy(rotary._c)
+    if rotary.q_weight is not None:
+        _row_strides(rotary.q_weight, "q_weight", dtype, (dim,))
+    if rotary.k_weight is not None:
+        _row_strides(rotary.k_weight, "k_weight", dtype, (dim,))
     if positions is not None:
         _need(positions, "positions", "int32", (tokens,))
-        r.positions = positions.data_ptr()
-    r.q_token_stride, r.q_head_stride, _ = query.stride()
-    r.out_token_stride, r.out_head_stride, _ = query_out.stride()
-    ks, vs = key.stride(), value.stride()
-    rows = kvx_new_rows(_type_of(key.dtype), _cache_type(pool, cache_dtype), tokens, new_tokens,
+    r = kvx_rotary(*rotary._front, None if positions is None else positions.data_ptr(), *rotary._rear, qs[0], qs[1], outs[0], outs[1])
+    rows = kvx_new_rows(_type_of(dtype), _cache_type(pool, cache_dtype), tokens, new_tokens,
                         None if starts is None else starts.data_ptr(), ks[0], ks[1], vs[0], vs[1], k_scale, v_scale)
-    _check(_lib.kv_append_rotary(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(rows),
-                                 ctypes.byref(r), query.data_ptr(), key.data_ptr(), value.data_ptr(), query_out.data_ptr(),
-                                 _stream_handle(stream)), "kv_append_rotary")
+    _check(_lib.kv_append_rotary(ctx, _byref(pool._c), layer, _byref(batch._c), _byref(rows), _byref(r), query.data_ptr(),
+                                 key.data_ptr(), value.data_ptr(), query_out.data_ptr(), _stream_handle(stream)),
+           "kv_append_rotary")
 
 
 class KvAttention:
@@ -960,17 +972,17 @@ class KvBounds:
 
     def _of(self, pool: KvPool):
         want = (pool.num_blocks, pool.num_heads, 2, pool.head_dim)
-        if tuple(self.boxes.shape) != want:
+        if self.boxes.shape != want:
             raise ValueError(f"boxes are {tuple(self.boxes.shape)}, not {want}")
-        return ctypes.byref(self._c)
+        return _byref(self._c)
 
 
 def kv_bounds(ctx, pool: KvPool, layer: int, batch: KvBatch, bounds: KvBounds, new_tokens: int = 1, cache_dtype=None,
               stream=None) -> None:
     """Make the bounds of the pages that hold every sequence's last new_tokens tokens (as many as the longest has: of all
     its pages)."""
-    _check(_lib.kv_bounds(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), _cache_type(pool, cache_dtype),
-                          new_tokens, bounds._of(pool), _stream_handle(stream)), "kv_bounds")
+    _check(_lib.kv_bounds(ctx, _byref(pool._c), layer, _byref(batch._c), _cache_type(pool, cache_dtype), new_tokens,
+                          bounds._of(pool), _stream_handle(stream)), "kv_bounds")
 
 
 class KvSelection:
@@ -979,15 +991,15 @@ class KvSelection:
 
     def __init__(self, q_heads: int, budget: int, sinks: int = 1, recent: int = 1, new_tokens: int = 1):
         self.q_heads, self.budget, self.new_tokens = q_heads, budget, new_tokens
-        self._c = kvx_selection(KVX_TYPE_BF16, q_heads, new_tokens, budget, sinks, recent)
+        self._fields = (q_heads, new_tokens, budget, sinks, recent)
 
 
 def kv_select_workspace(ctx, pool: KvPool, batch: KvBatch, selection: KvSelection):
     """A workspace tensor for kv_select calls of these shapes; one call uses it at a time."""
     import torch
     out = ctypes.c_int64()
-    _check(_lib.kv_select_workspace(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), ctypes.byref(selection._c),
-                                    ctypes.byref(out)), "kv_select_workspace")
+    c = kvx_selection(KVX_TYPE_BF16, *selection._fields)
+    _check(_lib.kv_select_workspace(ctx, _byref(pool._c), _byref(batch._c), _byref(c), _byref(out)), "kv_select_workspace")
     return torch.empty(max(16, out.value), dtype=torch.uint8, device=batch.lengths.device)
 
 
@@ -997,15 +1009,12 @@ def kv_select(ctx, pool: KvPool, batch: KvBatch, bounds: KvBounds, selection: Kv
     of their keys: selected (int32 [sequences * new_tokens][heads][budget]) gets their places in the
     sequence, ascending, -1 behind the last."""
     tokens = batch.num_seqs * selection.new_tokens
-    _need_rows(query, "query", query.dtype, (tokens, selection.q_heads, pool.head_dim))
+    qs = _row_strides(query, "query", query.dtype, (tokens, selection.q_heads, pool.head_dim))
     _need(selected, "selected", "int32", (tokens, pool.num_heads, selection.budget))
     _check_tensor(selected, "selected")
-    c = kvx_selection.from_buffer_copy(selection._c)
-    c.type = _type_of(query.dtype)
-    c.q_token_stride, c.q_head_stride, _ = query.stride()
-    _check(_lib.kv_select(ctx, ctypes.byref(pool._c), ctypes.byref(batch._c), bounds._of(pool), ctypes.byref(c),
-                          query.data_ptr(), selected.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                          _stream_handle(stream)), "kv_select")
+    c = kvx_selection(_type_of(query.dtype), *selection._fields, qs[0], qs[1])
+    _check(_lib.kv_select(ctx, _byref(pool._c), _byref(batch._c), bounds._of(pool), _byref(c), query.data_ptr(),
+                          selected.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_select")
 
 
 def kv_attend_selected_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttention, budget: int, dtype=None):
@@ -1024,25 +1033,24 @@ def kv_attend_selected(ctx, pool: KvPool, layer: int, batch: KvBatch, attention:
                        workspace, lse=None, stream=None) -> None:
     """kv_attend over the tokens of selected pages alone (int32 [sequences * new_tokens][heads][budget], from
     kv_select), each query up to its own position."""
-    shape = (batch.num_seqs * attention.new_tokens, attention.q_heads, pool.head_dim)
-    _need_rows(query, "query", query.dtype, shape)
-    _need_rows(out, "out", query.dtype, shape)
+    dtype, tokens = query.dtype, batch.num_seqs * attention.new_tokens
+    qs = _row_strides(query, "query", dtype, (tokens, attention.q_heads, pool.head_dim))
+    outs = _row_strides(out, "out", dtype, (tokens, attention.q_heads, pool.head_dim))
     if selected.dim() != 3:
         raise ValueError("selected must be [sequences * new_tokens][heads][budget]")
-    _need(selected, "selected", "int32", (shape[0], pool.num_heads, selected.shape[2]))
+    budget = selected.shape[2]
+    _need(selected, "selected", "int32", (tokens, pool.num_heads, budget))
     _check_tensor(selected, "selected")
-    c = kvx_attention.from_buffer_copy(attention._c)
-    c.type = _type_of(query.dtype)
-    c.cache_type = _cache_type(pool, attention.cache_dtype)
-    c.q_token_stride, c.q_head_stride, _ = query.stride()
-    c.out_token_stride, c.out_head_stride, _ = out.stride()
     if lse is not None:
-        _need(lse, "lse", "float32", shape[:2])
+        _need(lse, "lse", "float32", (tokens, attention.q_heads))
         _check_tensor(lse, "lse")
-        c.lse = lse.data_ptr()
-    _check(_lib.kv_attend_selected(ctx, ctypes.byref(pool._c), layer, ctypes.byref(batch._c), ctypes.byref(c),
-                                   selected.shape[2], selected.data_ptr(), query.data_ptr(), out.data_ptr(),
-                                   workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_attend_selected")
+    a = attention._c
+    c = kvx_attention(_type_of(dtype), _cache_type(pool, attention.cache_dtype), a.q_heads, a.new_tokens, a.scale, a.softcap,
+                      a.k_scale, a.v_scale, a.window, a.slopes, qs[0], qs[1], outs[0], outs[1],
+                      None if lse is None else lse.data_ptr())
+    _check(_lib.kv_attend_selected(ctx, _byref(pool._c), layer, _byref(batch._c), _byref(c), budget, selected.data_ptr(),
+                                   query.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                                   _stream_handle(stream)), "kv_attend_selected")
 
 
 def kv_evict(ctx, pool: KvPool, batch: KvBatch, weights, budget: int, new_tables, kept, new_lengths,
@@ -1183,34 +1191,31 @@ def kv_state_delta(ctx, state: StateSlots, batch: StateBatch, query, key, value,
     [tokens][heads] (dt None: no decay), A and dt_bias [heads] (float32), on the state in each sequence's slot.
     softplus, sigmoid: of dt and beta; normalize: query and key to unit length; scale: of the queries (None:
     1/sqrt(state_dim); not 0).  workspace: from kv_state_delta_workspace (None: none is needed for one token of each)."""
-    t, heads, head_dim = value.shape
-    groups, state_dim = key.shape[1:]
+    dtype, tokens = value.dtype, batch.tokens
+    _, heads, head_dim = value.shape
+    _, groups, state_dim = key.shape
     if scale == 0:
         raise ValueError("a scale of 0 is the library's mark for 1/sqrt(state_dim): pass None for that")
-    if dt is not None and A is None:
-        raise ValueError("dt needs A")
-    _need_rows(value, "value", value.dtype, (batch.tokens, heads, head_dim))
-    _need_rows(out, "out", value.dtype, value.shape)
-    _need_rows(key, "key", value.dtype, (t, groups, state_dim))
-    _need_rows(query, "query", value.dtype, key.shape)
-    _need_rows(beta, "beta", value.dtype, (t, heads))
-    c = kvx_delta(_type_of(value.dtype), heads, head_dim, state_dim, groups, softplus, sigmoid, normalize, scale or 0.0, eps)
+    vs = _row_strides(value, "value", dtype, (tokens, heads, head_dim))
+    outs = _row_strides(out, "out", dtype, (tokens, heads, head_dim))
+    ks = _row_strides(key, "key", dtype, (tokens, groups, state_dim))
+    qs = _row_strides(query, "query", dtype, (tokens, groups, state_dim))
+    steps = _row_strides(beta, "beta", dtype, (tokens, heads))
+    decays, a, bias = 0, None, None
     if dt is not None:
-        _need_rows(dt, "dt", value.dtype, (t, heads))
-        c.dt_token_stride = dt.stride(0)
+        if A is None:
+            raise ValueError("dt needs A")
+        decays = _row_strides(dt, "dt", dtype, (tokens, heads))[0]
         _need(A, "A", "float32", (heads,))
-        c.A = A.data_ptr()
+        a = A.data_ptr()
         if dt_bias is not None:
             _need(dt_bias, "dt_bias", "float32", (heads,))
-            c.dt_bias = dt_bias.data_ptr()
-    c.q_token_stride, c.q_head_stride, _ = query.stride()
-    c.k_token_stride, c.k_head_stride, _ = key.stride()
-    c.v_token_stride, c.v_head_stride, _ = value.stride()
-    c.beta_token_stride = beta.stride(0)
-    c.out_token_stride, c.out_head_stride, _ = out.stride()
-    _check(_lib.kv_state_delta(ctx, ctypes.byref(state._c), ctypes.byref(batch._c), ctypes.byref(c), query.data_ptr(),
-                               key.data_ptr(), value.data_ptr(), None if dt is None else dt.data_ptr(), beta.data_ptr(),
-                               out.data_ptr(), None if workspace is None else workspace.data_ptr(),
+            bias = dt_bias.data_ptr()
+    c = kvx_delta(_type_of(dtype), heads, head_dim, state_dim, groups, softplus, sigmoid, normalize, scale or 0.0, eps, a, bias,
+                  qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], decays, steps[0], outs[0], outs[1])
+    _check(_lib.kv_state_delta(ctx, _byref(state._c), _byref(batch._c), _byref(c), query.data_ptr(), key.data_ptr(),
+                               value.data_ptr(), None if dt is None else dt.data_ptr(), beta.data_ptr(), out.data_ptr(),
+                               None if workspace is None else workspace.data_ptr(),
                                0 if workspace is None else workspace.numel(), _stream_handle(stream)), "kv_state_delta")
 
 
