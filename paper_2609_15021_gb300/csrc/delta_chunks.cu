@@ -9,8 +9,8 @@
 // head (system_kernel).  Then a CTA walks through the chunks of one sequence with 16 rows of one head's state, an element of
 // v each, that know nothing of the other rows (walk_kernel): five products with 16 rows on one side.
 //
-// Rounding: keys and queries are fp16 numbers times a power of two a row, whose largest is in [2^13, 2^14), so that a bf16
-// number keeps its bits down to 2^-27 of that and is off by 2^-38 of it below.  The state, rhs and W's decayed copy are each
+// Rounding: keys and queries are fp16 numbers times a power of two a row, whose length is below 2^14 and above 2^12, so that a
+// bf16 number keeps its bits down to 2^-27 of that and is off by 2^-37 of it below.  The state, rhs and W's decayed copy are each
 // two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so is 2^9 T.  M and the W that it is multiplied
 // with are rounded to fp16 once.  Sums are fp32.
 //
@@ -37,7 +37,8 @@ struct Factors {
   float row[kChunk];    // M's row
   float decay;          // of the whole chunk
   int odd;              // it goes token by token
-  float pad[30];
+  float into[4];        // powers of two that are taken out of the third factors, 16 tokens each
+  float pad[26];
 };
 constexpr int kFactors = (int)sizeof(Factors), kHeadBytes = kFactors + 3 * kTriangle;
 static_assert(kFactors == 1408 && kHeadBytes == kDeltaHeadBytes && kHeadBytes % 128 == 0, "bulk copies");
@@ -60,22 +61,31 @@ __device__ __forceinline__ uint32_t half2_of(float a, float b) { return pack2<Fp
 
 // ---------------------------------------------------------------- what knows nothing of the state
 
-constexpr int kPitch = kChunk + 4;  // of 64 x 64 fp32 numbers in shared memory
+constexpr int kDiagonalPitch = 20;
 template <int N>
 struct SystemShape {
-  // keys and queries, then, when they have been multiplied, A transposed and M
-  static constexpr int kImages = 2 * kRowBytes<N> > kChunk * kPitch * 4 + kTriangle ? 2 * kRowBytes<N> : kChunk * kPitch * 4 + kTriangle;
-  static constexpr int kT = kImages, kDiagonal = kT + kChunk * kPitch * 4, kSmem = kDiagonal + 4 * 16 * 16 * 4;
+  // keys and queries; when they have been multiplied, in their place: A below the diagonal blocks and T, each in two parts,
+  // M, and A's diagonal blocks transposed in 32 bits
+  static constexpr int kA = 0, kT = 2 * kTriangle, kM = 4 * kTriangle, kDiagonal = 5 * kTriangle, kThen = kDiagonal + 4 * 16 * kDiagonalPitch * 4;
+  static constexpr int kSmem = 2 * kRowBytes<N> > kThen ? 2 * kRowBytes<N> : kThen;
 };
+__device__ __forceinline__ void split2(float2 x, uint32_t& hi, uint32_t& lo) {
+  hi = half2_of(x.x, x.y);
+  const float2 rest = fma2(unpack2<Fp16>(hi), make_float2(-1.f, -1.f), x);
+  lo = half2_of(rest.x, rest.y);
+}
 
+// A chunk and head a CTA, 16 of its tokens a warp.  T is made block by block: on the diagonal by substitution, below it as
+// T_ij = -T_ii sum_{j<=k<i} A_ik T_kj, a column of blocks a warp, by products of numbers in two parts (in 32-bit floats, a column
+// and half of the rows a lane, it took a third of the kernel's time, most of it the first warp's).
 template <class E, int N>
-__global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant__ DeltaParams p) {
+__global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_constant__ DeltaParams p) {
   wait_for_previous();
   using S = SystemShape<N>;
   using T = typename E::T;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Factors f;
-  __shared__ float sum_s[kChunk], low_s[kChunk], key_s[kChunk], query_s[kChunk], beta_s[kChunk];
+  __shared__ float sum_s[kChunk], low_s[kChunk], key_s[kChunk], query_s[kChunk], beta_s[kChunk], squares_s[2][kChunk];
   __shared__ int32_t buf[kThreads / 32 + 3];
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
@@ -89,7 +99,7 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
   const bool writes_rows = h == group * p.heads_per_group;
   bool odd = false;
 
-  // Keys and queries: lengths, and fp16 numbers with the row's largest in [2^13, 2^14).
+  // Keys and queries: lengths, and fp16 numbers that leave the row's below 2^14.
   constexpr int kLanes = N / 8, kAtOnce = 32 / kLanes, kRounds = 16 / kAtOnce;
   const int vec = lane % kLanes, sub = lane / kLanes;
   const T* rows[2] = {reinterpret_cast<const T*>(p.k) + group * p.k_head + vec * 8, reinterpret_cast<const T*>(p.q) + group * p.q_head + vec * 8};
@@ -102,35 +112,65 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
       const int row = warp * 16 + i * kAtOnce + sub;
       raw[i] = row < n ? *reinterpret_cast<const uint4*>(rows[which] + (t0 + row) * stride) : make_uint4(0, 0, 0, 0);
     }
+    // sums of squares of the rounds' rows meet in a reduction that halves the rounds at every step
+    float squares[kRounds];
+    uint32_t carries = 0;
+#pragma unroll
+    for (int i = 0; i < kRounds; ++i) {
+      const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+      float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float2 x = unpack2<E>(u[j]);
+        sum = fma2(x, x, sum);
+        carries |= odd_carry<E>(u[j]);
+      }
+      squares[i] = sum.x + sum.y;
+    }
+    odd |= odd_carried(carries);
+    int m = kLanes / 2, at = 0;
+#pragma unroll
+    for (int left = kRounds; left > 1; left /= 2, m /= 2) {
+      const bool upper = lane & m;
+      at = 2 * at + upper;
+#pragma unroll
+      for (int k = 0; k < left / 2; ++k) {
+        const float send = upper ? squares[k] : squares[k + left / 2], stay = upper ? squares[k + left / 2] : squares[k];
+        squares[k] = stay + __shfl_xor_sync(~0u, send, m);
+      }
+    }
+#pragma unroll
+    for (; m; m >>= 1) squares[0] += __shfl_xor_sync(~0u, squares[0], m);
+    squares_s[which][warp * 16 + at * kAtOnce + sub] = squares[0];
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const int row = warp * 16 + i * kAtOnce + sub;
+      const float all = squares_s[which][row];
+      const int e = all > 0.f ? (((int)(__float_as_uint(all) >> 23) - 127) >> 1) - 13 : 0;  // its root is below 2^(e + 14)
+      const float by = power_of_two(-e);
       const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-      float2 x[4];
-      float squares = 0.f, top = 0.f;
-      uint32_t carries = 0;
+      uint32_t w[4];
+      odd |= all < 0x1p-100f && ((u[0] | u[1] | u[2] | u[3]) & 0x7FFF7FFFu);  // too small for their squares
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        x[j] = unpack2<E>(u[j]);
-        carries |= odd_carry<E>(u[j]);
-        squares = fmaf(x[j].x, x[j].x, fmaf(x[j].y, x[j].y, squares));
-        top = fmaxf(top, fmaxf(fabsf(x[j].x), fabsf(x[j].y)));
+        const float2 x = mul2(unpack2<E>(u[j]), make_float2(by, by));
+        w[j] = half2_of(x.x, x.y);
       }
+      const int to = which * kRowBytes<N> + image_at(row, vec);
+      *reinterpret_cast<uint4*>(smem + to) = make_uint4(w[0], w[1], w[2], w[3]);
+      if (writes_rows) *reinterpret_cast<uint4*>(rows_to + to) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  if (lane < 16) {  // a token's factors
+    const int t = warp * 16 + lane;
 #pragma unroll
-      for (int m = kLanes / 2; m; m >>= 1) {
-        squares += __shfl_xor_sync(~0u, squares, m);
-        top = fmaxf(top, __shfl_xor_sync(~0u, top, m));
-      }
-      const int e = top > 0.f ? max(exponent_of(top) - 13, -126) : 0;
-      const float factor = row < n ? (p.normalize ? rsqrtf(squares + p.eps) : 1.f) * (which ? p.scale : 1.f) * power_of_two(e) : 0.f;
-      const float by = power_of_two(-e);
-      odd |= odd_carried(carries) || !isfinite(factor);
-      if (vec == 0) (which ? query_s : key_s)[row] = top > 0.f ? factor : 0.f;  // of zeros it would only set scales
-      const uint4 w = make_uint4(half2_of(x[0].x * by, x[0].y * by), half2_of(x[1].x * by, x[1].y * by),
-                                 half2_of(x[2].x * by, x[2].y * by), half2_of(x[3].x * by, x[3].y * by));
-      const int at = which * kRowBytes<N> + image_at(row, vec);
-      *reinterpret_cast<uint4*>(smem + at) = w;
-      if (writes_rows) *reinterpret_cast<uint4*>(rows_to + at) = w;
+    for (int which = 0; which < 2; ++which) {
+      const float all = squares_s[which][t];
+      const int e = all > 0.f ? (((int)(__float_as_uint(all) >> 23) - 127) >> 1) - 13 : 0;
+      const float factor = t < n ? (p.normalize ? rsqrtf(all + p.eps) : 1.f) * (which ? p.scale : 1.f) * power_of_two(e) : 0.f;
+      odd |= !isfinite(factor) || !isfinite(all);
+      (which ? query_s : key_s)[t] = all > 0.f ? factor : 0.f;  // of zeros it would only set scales
     }
   }
   // Gates, two tokens a lane: sums of exponents up to a token in two parts, whole 64ths (that 64 tokens of up to 2^10 lose no
@@ -176,6 +216,12 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
   if (threadIdx.x < kChunk) {
     float4& by = f.by[threadIdx.x];
     by.x *= key_s[threadIdx.x], by.z *= key_s[threadIdx.x], by.w *= query_s[threadIdx.x];
+    float most = fabsf(by.z);
+#pragma unroll
+    for (int m = 8; m; m >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, m));
+    const int into = min(exponent_of(most) + 1, 126);
+    by.z *= power_of_two(-into);
+    if (threadIdx.x % 16 == 0) f.into[threadIdx.x / 16] = power_of_two(into);
   }
 
   // Products of keys with keys and of queries with keys, 16 rows a warp, up to the diagonal.
@@ -185,13 +231,13 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int e = 0; e < 4; ++e) kk[j][e] = qk[j][e] = 0.f;
-  const int a_row = warp * 16 + (lane >> 3 & 1) * 8 + (lane & 7), a_vec = lane >> 4;  // of a left factor's matrices
-  const int b_row = (lane >> 4) * 8 + (lane & 7), b_vec = lane >> 3 & 1;              // of a right one's
+  const int a_row = (lane >> 3 & 1) * 8 + (lane & 7), a_vec = lane >> 4;  // of a left factor's matrices, and a right one's transposed
+  const int b_row = (lane >> 4) * 8 + (lane & 7), b_vec = lane >> 3 & 1;  // of a right one's
 #pragma unroll 2
   for (int s = 0; s < N / 16; ++s) {
     uint32_t ka[4], qa[4];
-    load_matrices(ka, base + image_at(a_row, 2 * s + a_vec));
-    load_matrices(qa, base + kRowBytes<N> + image_at(a_row, 2 * s + a_vec));
+    load_matrices(ka, base + image_at(warp * 16 + a_row, 2 * s + a_vec));
+    load_matrices(qa, base + kRowBytes<N> + image_at(warp * 16 + a_row, 2 * s + a_vec));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (j > warp) break;
@@ -204,10 +250,7 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
     }
   }
   __syncthreads();  // the images have been read
-  float* a_s = reinterpret_cast<float*>(smem);  // A transposed: [s][t]
-  uint8_t* m_s = smem + kChunk * kPitch * 4;
-  float* x_s = reinterpret_cast<float*>(smem + S::kT);         // T: [t][s]
-  float* d_s = reinterpret_cast<float*>(smem + S::kDiagonal);  // its blocks on the diagonal, transposed: [block][s][t]
+  float* diagonal = reinterpret_cast<float*>(smem + S::kDiagonal) + warp * 16 * kDiagonalPitch;  // [s][t]
 #pragma unroll
   for (int r = 0; r < 2; ++r) {  // rows g and g + 8 of the warp's
     const int t = warp * 16 + g + 8 * r;
@@ -216,13 +259,22 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j > 2 * warp + 1) break;
+      float2 a;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int s = 8 * j + 2 * c + e;
         const float by = key_s[s] * (s <= t ? ex2((sum_t - sum_s[s]) + (low_t - low_s[s])) : 0.f);
-        if (s < t) a_s[s * kPitch + t] = kk[j][2 * r + e] * by * key_t;
+        (e ? a.y : a.x) = kk[j][2 * r + e] * by * key_t;
         qk[j][2 * r + e] *= by * query_t;
         top = fmaxf(top, fabsf(qk[j][2 * r + e]));
+        if (j >= 2 * warp && s < t) diagonal[(s & 15) * kDiagonalPitch + (t & 15)] = e ? a.y : a.x;
+      }
+      if (j < 2 * warp) {  // with its sign turned
+        uint32_t hi, lo;
+        split2(make_float2(a.x * -kUp, a.y * -kUp), hi, lo);
+        uint8_t* to = smem + S::kA + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c;
+        *reinterpret_cast<uint32_t*>(to) = hi;
+        *reinterpret_cast<uint32_t*>(to + kTriangle) = lo;
       }
     }
     top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
@@ -234,7 +286,7 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j > 2 * warp + 1) break;
-      *reinterpret_cast<uint32_t*>(m_s + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c) = half2_of(qk[j][2 * r] * up, qk[j][2 * r + 1] * up);
+      *reinterpret_cast<uint32_t*>(smem + S::kM + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c) = half2_of(qk[j][2 * r] * up, qk[j][2 * r + 1] * up);
     }
   }
   __syncwarp();
@@ -244,81 +296,79 @@ __global__ void __launch_bounds__(kThreads) system_kernel(const __grid_constant_
     float x[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = i == col ? 1.f : 0.f;
-    const float* at = a_s + warp * 16 * kPitch + warp * 16;
 #pragma unroll
     for (int k = 0; k < 15; ++k)
 #pragma unroll
       for (int i = (k + 1) / 4 * 4; i < 16; i += 4) {
-        const float4 a = *reinterpret_cast<const float4*>(at + k * kPitch + i);
+        const float4 a = *reinterpret_cast<const float4*>(diagonal + k * kDiagonalPitch + i);
         if (i > k) x[i] -= a.x * x[k];
         if (i + 1 > k) x[i + 1] -= a.y * x[k];
         if (i + 2 > k) x[i + 2] -= a.z * x[k];
         if (i + 3 > k) x[i + 3] -= a.w * x[k];
       }
-    if (lane < 16) {
+    // T's block, a half of its rows a half of the warp
+    uint8_t* to = smem + S::kT;
+    const bool upper = lane >= 16;
 #pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(d_s + (warp * 16 + col) * 16 + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x_s[(warp * 16 + i) * kPitch + warp * 16 + col] = x[i];
+    for (int i = 0; i < 8; ++i) {
+      const float y = (upper ? x[i + 8] : x[i]) * kUp;
+      odd |= !(fabsf(y) <= kLargest * kUp);
+      const __half hi = __float2half_rn(y), lo = __float2half_rn(y - __half2float(hi));
+      const int at = block_at(warp, warp, i + (upper ? 8 : 0), col >> 3) + (col & 7) * 2;
+      *reinterpret_cast<__half*>(to + at) = hi;
+      *reinterpret_cast<__half*>(to + kTriangle + at) = lo;
     }
   }
   __syncthreads();
-  // The blocks below: T_ij = -T_ii sum_{j<=k<i} A_ik T_kj, a column of blocks a warp, a column and half of the rows a lane.
-  {
-    const int col = warp * 16 + (lane & 15), half = lane >> 4;
-    for (int i = warp + 1; i < 4; ++i) {
-      float acc[8];
+  for (int i = warp + 1; i < 4; ++i) {
+    float x[2][4] = {};  // 2^18 times the sum, rows g and g + 8, columns 2 c and the next of each eight
+    for (int k = warp; k < i; ++k) {
+      uint32_t a[4], a_lo[4], b[4], b_lo[4];
+      load_matrices(a, base + S::kA + block_at(i, k, a_row, a_vec));
+      load_matrices(a_lo, base + S::kA + kTriangle + block_at(i, k, a_row, a_vec));
+      load_matrices_t(b, base + S::kT + block_at(k, warp, a_row, a_vec));
+      load_matrices_t(b_lo, base + S::kT + kTriangle + block_at(k, warp, a_row, a_vec));
 #pragma unroll
-      for (int r = 0; r < 8; ++r) acc[r] = 0.f;
-#pragma unroll 8
-      for (int k = warp * 16; k < i * 16; ++k) {
-        const float x = x_s[k * kPitch + col];
-        const float4 a = *reinterpret_cast<const float4*>(a_s + k * kPitch + i * 16 + half * 8);
-        const float4 b = *reinterpret_cast<const float4*>(a_s + k * kPitch + i * 16 + half * 8 + 4);
-        acc[0] -= a.x * x, acc[1] -= a.y * x, acc[2] -= a.z * x, acc[3] -= a.w * x;
-        acc[4] -= b.x * x, acc[5] -= b.y * x, acc[6] -= b.z * x, acc[7] -= b.w * x;
+      for (int u = 0; u < 2; ++u) {
+        mma<Fp16>(x[u], a, b[2 * u], b[2 * u + 1]);
+        mma<Fp16>(x[u], a_lo, b[2 * u], b[2 * u + 1]);
+        mma<Fp16>(x[u], a, b_lo[2 * u], b_lo[2 * u + 1]);
       }
-      float* to = x_s + (i * 16 + half * 8) * kPitch + col;
+    }
+    // as a right factor: its columns lie along k
+    uint32_t hi[2][2], lo[2][2], a[4], a_lo[4];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) to[r * kPitch] = acc[r], acc[r] = 0.f;
-      __syncwarp();
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int k = 0; k < 16; ++k) {
-        const float x = x_s[(i * 16 + k) * kPitch + col];
-        const float4 a = *reinterpret_cast<const float4*>(d_s + (i * 16 + k) * 16 + half * 8);
-        const float4 b = *reinterpret_cast<const float4*>(d_s + (i * 16 + k) * 16 + half * 8 + 4);
-        acc[0] += a.x * x, acc[1] += a.y * x, acc[2] += a.z * x, acc[3] += a.w * x;
-        acc[4] += b.x * x, acc[5] += b.y * x, acc[6] += b.z * x, acc[7] += b.w * x;
+      for (int r = 0; r < 2; ++r) {
+        split2(mul2(make_float2(x[u][2 * r], x[u][2 * r + 1]), make_float2(1 / kUp, 1 / kUp)), hi[u][r], lo[u][r]);
+        hi[u][r] = transpose(hi[u][r]), lo[u][r] = transpose(lo[u][r]);
       }
-      __syncwarp();
+    load_matrices(a, base + S::kT + block_at(i, i, a_row, a_vec));
+    load_matrices(a_lo, base + S::kT + kTriangle + block_at(i, i, a_row, a_vec));
 #pragma unroll
-      for (int r = 0; r < 8; ++r) to[r * kPitch] = acc[r];
-      __syncwarp();
-    }
-  }
-  __syncthreads();
-  // T in its two parts, M and the factors.
-  uint8_t* t_to = head_to + kFactors;
-  for (int i = threadIdx.x; i < kTriangle / 16; i += kThreads) {
-    *reinterpret_cast<uint4*>(t_to + 2 * kTriangle + i * 16) = *reinterpret_cast<const uint4*>(m_s + i * 16);
-    const int block = i / 32, row = i / 2 % 16, half = (i & 1) ^ (row >> 2 & 1);
-    const int bi = block < 1 ? 0 : block < 3 ? 1 : block < 6 ? 2 : 3, bj = block - bi * (bi + 1) / 2;
-    const float* from = x_s + (bi * 16 + row) * kPitch + bj * 16 + half * 8;
-    uint32_t hi[4], lo[4];
+    for (int u = 0; u < 2; ++u) {
+      float y[4] = {};
+      mma<Fp16>(y, a, hi[u][0], hi[u][1]);
+      mma<Fp16>(y, a_lo, hi[u][0], hi[u][1]);
+      mma<Fp16>(y, a, lo[u][0], lo[u][1]);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 x = *reinterpret_cast<const float2*>(from + 2 * k);
-      odd |= !(fmaxf(fabsf(x.x), fabsf(x.y)) <= kLargest) || x.x != x.x || x.y != x.y;
-      hi[k] = half2_of(x.x * kUp, x.y * kUp);
-      const float2 back = unpack2<Fp16>(hi[k]);
-      lo[k] = half2_of(x.x * kUp - back.x, x.y * kUp - back.y);
+      for (int r = 0; r < 2; ++r) {
+        const float2 t = mul2(make_float2(y[2 * r], y[2 * r + 1]), make_float2(1 / kUp, 1 / kUp));
+        odd |= !(fabsf(t.x) <= kLargest * kUp) || !(fabsf(t.y) <= kLargest * kUp);
+        uint32_t t_hi, t_lo;
+        split2(t, t_hi, t_lo);
+        uint8_t* to = smem + S::kT + block_at(i, warp, g + 8 * r, u) + 4 * c;
+        *reinterpret_cast<uint32_t*>(to) = t_hi;
+        *reinterpret_cast<uint32_t*>(to + kTriangle) = t_lo;
+      }
     }
-    *reinterpret_cast<uint4*>(t_to + i * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(t_to + kTriangle + i * 16) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    __syncwarp();
   }
   odd = __syncthreads_or(odd);
   if (threadIdx.x == 0) f.odd = odd;
+  for (int i = threadIdx.x; i < 3 * kTriangle / 16; i += kThreads)
+    reinterpret_cast<uint4*>(head_to + kFactors)[i] = reinterpret_cast<const uint4*>(smem + S::kT)[i];
   __syncthreads();
   for (int i = threadIdx.x; i < kFactors / 16; i += kThreads)
     reinterpret_cast<uint4*>(head_to)[i] = reinterpret_cast<const uint4*>(&f)[i];
@@ -340,27 +390,34 @@ struct WalkShape {
   static constexpr int kT = 2 * kRowBytes<N> + kFactors, kStage = 2 * kRowBytes<N> + kFactors + 2 * kTriangle;
   // left factors as the matrix instruction takes them, 512 bytes for 16 columns and part, and their powers of two
   static constexpr int kM = 2 * kStage, kState = kM + kTriangle, kRhs = kState + kSteps * 1024, kWrite = kRhs + 4096, kPlain = kWrite + 4096,
-                       kStateBy = kPlain + 2048, kRhsBy = kStateBy + kSteps * 64, kWriteBy = kRhsBy + 256, kPlainBy = kWriteBy + 256,
+                       kStateBy = kPlain + 2048, kRhsBy = kStateBy + kSteps * 64, kPlainBy = kRhsBy + 256,
                        kBars = kPlainBy + 256, kSmem = kBars + 64;
   static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs an SM");
 };
 
-// Two tiles of 16 x 8 sums as 16 columns of a left factor: fp16 parts hi and lo, times powers of two a row.
-__device__ __forceinline__ void left_factor(const float (&x)[4], const float (&y)[4], uint8_t* hi, uint8_t* lo, float2* by, int lane) {
-  float top[2] = {fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(y[0]), fabsf(y[1]))),
-                  fmaxf(fmaxf(fabsf(x[2]), fabsf(x[3])), fmaxf(fabsf(y[2]), fabsf(y[3])))};
+// Two tiles of 16 x 8 sums as 16 columns of a left factor: fp16 parts hi and lo, times powers of two a row, the largest number
+// to [2^13, 2^14).
+struct Scaled {
   float up[2];
   float2 down;
+};
+__device__ __forceinline__ Scaled scaled_for(const float (&x)[4], const float (&y)[4]) {
+  float top[2] = {fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(y[0]), fabsf(y[1]))),
+                  fmaxf(fmaxf(fabsf(x[2]), fabsf(x[3])), fmaxf(fabsf(y[2]), fabsf(y[3])))};
+#pragma unroll
+  for (int m = 1; m < 4; m <<= 1)
+#pragma unroll
+    for (int r = 0; r < 2; ++r) top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], m));
+  Scaled s;
 #pragma unroll
   for (int r = 0; r < 2; ++r) {
-    top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
-    top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
-    const int e = min(max(140 - (int)(__float_as_uint(top[r]) >> 23), -126), 126);  // the largest to [2^13, 2^14)
-    up[r] = power_of_two(e);
-    (r ? down.y : down.x) = power_of_two(-e);
+    const int e = min(140 - (int)(__float_as_uint(top[r]) >> 23), 126);
+    s.up[r] = power_of_two(e);
+    (r ? s.down.y : s.down.x) = power_of_two(-e);
   }
-  const float2 v[4] = {mul2(make_float2(x[0], x[1]), make_float2(up[0], up[0])), mul2(make_float2(x[2], x[3]), make_float2(up[1], up[1])),
-                       mul2(make_float2(y[0], y[1]), make_float2(up[0], up[0])), mul2(make_float2(y[2], y[3]), make_float2(up[1], up[1]))};
+  return s;
+}
+__device__ __forceinline__ void left_factor(const float2 (&v)[4], uint8_t* hi, uint8_t* lo) {
   uint32_t h[4], l[4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
@@ -368,19 +425,22 @@ __device__ __forceinline__ void left_factor(const float (&x)[4], const float (&y
     const float2 rest = fma2(unpack2<Fp16>(h[k]), make_float2(-1.f, -1.f), v[k]);
     l[k] = half2_of(rest.x, rest.y);
   }
-  *reinterpret_cast<uint4*>(hi + lane * 16) = make_uint4(h[0], h[1], h[2], h[3]);
-  if (lo) *reinterpret_cast<uint4*>(lo + lane * 16) = make_uint4(l[0], l[1], l[2], l[3]);
-  if ((lane & 3) == 0) by[lane >> 2] = down;
+  *reinterpret_cast<uint4*>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
+  if (lo) *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
 }
-__device__ __forceinline__ void left_load(uint32_t (&a)[4], const uint8_t* at, int lane) {
-  const uint4 v = *reinterpret_cast<const uint4*>(at + lane * 16);
+__device__ __forceinline__ void times(float2 (&v)[4], const float (&x)[4], const float (&y)[4], const float (&up)[2]) {
+  v[0] = mul2(make_float2(x[0], x[1]), make_float2(up[0], up[0])), v[1] = mul2(make_float2(x[2], x[3]), make_float2(up[1], up[1]));
+  v[2] = mul2(make_float2(y[0], y[1]), make_float2(up[0], up[0])), v[3] = mul2(make_float2(y[2], y[3]), make_float2(up[1], up[1]));
+}
+__device__ __forceinline__ void left_load(uint32_t (&a)[4], const uint8_t* at) {
+  const uint4 v = *reinterpret_cast<const uint4*>(at);
   a[0] = v.x, a[1] = v.y, a[2] = v.z, a[3] = v.w;
 }
 __device__ __forceinline__ void add_scaled(float (&d)[4], const float (&x)[4], float2 by) {
-  d[0] = fmaf(x[0], by.x, d[0]), d[1] = fmaf(x[1], by.x, d[1]);
-  d[2] = fmaf(x[2], by.y, d[2]), d[3] = fmaf(x[3], by.y, d[3]);
+  const float2 a = fma2(make_float2(x[0], x[1]), make_float2(by.x, by.x), make_float2(d[0], d[1]));
+  const float2 b = fma2(make_float2(x[2], x[3]), make_float2(by.y, by.y), make_float2(d[2], d[3]));
+  d[0] = a.x, d[1] = a.y, d[2] = b.x, d[3] = b.y;
 }
-
 template <class E, int N>
 __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant__ DeltaParams p) {
   wait_for_previous();
@@ -390,7 +450,20 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
   __shared__ int32_t first_s;
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-  const int32_t p0 = blockIdx.x * 16, h = blockIdx.y, s = blockIdx.z, group = h / p.heads_per_group;
+  const int32_t p0 = blockIdx.x * 16, h = blockIdx.y, group = h / p.heads_per_group;
+  // The longest sequences first, as they are walked through longest (of more than a warp can look at, in their order).
+  int32_t s = blockIdx.z;
+  if (v.num_seqs > 1 && v.num_seqs <= 32) {
+    int64_t a = 0, b = 0;
+    if (lane < v.num_seqs) rows_of(v, lane, &a, &b);
+    const int32_t mine = lane < v.num_seqs ? (int32_t)(b - a) : -1;
+    int32_t rank = 0;
+    for (int32_t k = 0; k < v.num_seqs; ++k) {
+      const int32_t other = __shfl_sync(~0u, mine, k);
+      rank += other > mine || (other == mine && k < lane);
+    }
+    s = __ffs(__ballot_sync(~0u, lane < v.num_seqs && rank == (int32_t)blockIdx.z)) - 1;
+  }
   int64_t begin, end;
   rows_of(v, s, &begin, &end);
   int32_t chunks = pieces_of(begin, end, kChunk, p.by_token);
@@ -466,13 +539,16 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
     }
   float2* state_by = reinterpret_cast<float2*>(smem + W::kStateBy);
   float2* rhs_by = reinterpret_cast<float2*>(smem + W::kRhsBy);
-  float2* write_by = reinterpret_cast<float2*>(smem + W::kWriteBy);
   float2* plain_by = reinterpret_cast<float2*>(smem + W::kPlainBy);
   auto publish = [&]() {
 #pragma unroll
     for (int k = 0; k < kTiles; k += 2) {
       const int step = (warp * kTiles + k) / 2;
-      left_factor(state[k], state[k + 1], smem + W::kState + step * 1024, smem + W::kState + step * 1024 + 512, state_by + step * 8, lane);
+      const Scaled by = scaled_for(state[k], state[k + 1]);
+      float2 x[4];
+      times(x, state[k], state[k + 1], by.up);
+      left_factor(x, smem + W::kState + step * 1024 + lane * 16, smem + W::kState + step * 1024 + 512 + lane * 16);
+      if (c == 0) state_by[step * 8 + g] = by.down;
     }
   };
   publish();
@@ -549,36 +625,43 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
       continue;
     }
 
-    // S k and S q of the warp's 16 tokens.
-    float sk[2][4], y[2][4];
+    // S k and S q of the warp's 16 tokens.  Here and below what a product takes is loaded for many of them before the
+    // first, and every step has sums of its own, so that none waits for another.
+    float sk[2][4] = {}, y[2][4] = {};
+    constexpr int kAtOnce = 4;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int k0 = 0; k0 < W::kSteps; k0 += kAtOnce) {
+      uint32_t hi[kAtOnce][4], lo[kAtOnce][4], b[kAtOnce][4], q[kAtOnce][4];
+      float2 by[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sk[u][e] = y[u][e] = 0.f;
-#pragma unroll
-    for (int k = 0; k < W::kSteps; ++k) {
-      uint32_t hi[4], lo[4], b[4], q[4];
-      left_load(hi, smem + W::kState + k * 1024, lane);
-      left_load(lo, smem + W::kState + k * 1024 + 512, lane);
-      load_matrices(b, rows + image_at(warp * 16 + b_row, 2 * k + b_vec));
-      load_matrices(q, rows + kRowBytes<N> + image_at(warp * 16 + b_row, 2 * k + b_vec));
-      const float2 by = state_by[k * 8 + g];
-      float x[4][4] = {};
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        mma<Fp16>(x[u], hi, b[2 * u], b[2 * u + 1]);
-        mma<Fp16>(x[2 + u], hi, q[2 * u], q[2 * u + 1]);
+      for (int k = 0; k < kAtOnce; ++k) {
+        left_load(hi[k], smem + W::kState + (k0 + k) * 1024 + lane * 16);
+        left_load(lo[k], smem + W::kState + (k0 + k) * 1024 + 512 + lane * 16);
+        load_matrices(b[k], rows + image_at(warp * 16 + b_row, 2 * (k0 + k) + b_vec));
+        load_matrices(q[k], rows + kRowBytes<N> + image_at(warp * 16 + b_row, 2 * (k0 + k) + b_vec));
+        by[k] = state_by[(k0 + k) * 8 + g];
       }
+      float x[kAtOnce][4][4] = {};
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        mma<Fp16>(x[u], lo, b[2 * u], b[2 * u + 1]);
-        mma<Fp16>(x[2 + u], lo, q[2 * u], q[2 * u + 1]);
-      }
+      for (int part = 0; part < 2; ++part)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        add_scaled(sk[u], x[u], by);
-        add_scaled(y[u], x[2 + u], by);
-      }
+        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) mma<Fp16>(x[k][u], part ? lo[k] : hi[k], b[k][2 * u], b[k][2 * u + 1]);
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) mma<Fp16>(x[k][2 + u], part ? lo[k] : hi[k], q[k][2 * u], q[k][2 * u + 1]);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) add_scaled(sk[u], x[k][u], by[k]);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) add_scaled(y[u], x[k][2 + u], by[k]);
     }
     float4 by[2][2];
     float m_by[2][2];
@@ -596,59 +679,85 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
         sk[u][2 * r + 1] = by[u][1].y * (value.y - by[u][1].x * sk[u][2 * r + 1]);
       }
     }
-    left_factor(sk[0], sk[1], smem + W::kRhs + warp * 1024, smem + W::kRhs + warp * 1024 + 512, rhs_by + warp * 8, lane);
+    {
+      const Scaled to = scaled_for(sk[0], sk[1]);
+      float2 x[4];
+      times(x, sk[0], sk[1], to.up);
+      left_factor(x, smem + W::kRhs + warp * 1024 + lane * 16, smem + W::kRhs + warp * 1024 + 512 + lane * 16);
+      if (c == 0) rhs_by[warp * 8 + g] = to.down;
+    }
     load_values(i + 1);
     __syncthreads();
-    // W = T rhs
+    // W = T rhs: a warp's rows of T have as many blocks as it is warps from the first
     float w[2][4] = {};
+    auto solve = [&](auto blocks) {
+      constexpr int kBlocks = decltype(blocks)::value;
+      uint32_t hi[kBlocks][4], lo[kBlocks][4], b[kBlocks][4], b_lo[kBlocks][4];
+      float2 undo[kBlocks];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (k > warp) break;
-      uint32_t hi[4], lo[4], b[4], b_lo[4];
-      left_load(hi, smem + W::kRhs + k * 1024, lane);
-      left_load(lo, smem + W::kRhs + k * 1024 + 512, lane);
-      load_matrices(b, rows + W::kT + block_at(warp, k, b_row, b_vec));
-      load_matrices(b_lo, rows + W::kT + kTriangle + block_at(warp, k, b_row, b_vec));
-      const float2 by = rhs_by[k * 8 + g];
-      float x[2][4] = {};
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        mma<Fp16>(x[u], hi, b[2 * u], b[2 * u + 1]);
-        mma<Fp16>(x[u], lo, b[2 * u], b[2 * u + 1]);
-        mma<Fp16>(x[u], hi, b_lo[2 * u], b_lo[2 * u + 1]);
-        add_scaled(w[u], x[u], by);
+      for (int k = 0; k < kBlocks; ++k) {
+        left_load(hi[k], smem + W::kRhs + k * 1024 + lane * 16);
+        left_load(lo[k], smem + W::kRhs + k * 1024 + 512 + lane * 16);
+        load_matrices(b[k], rows + W::kT + block_at(kBlocks - 1, k, b_row, b_vec));
+        load_matrices(b_lo[k], rows + W::kT + kTriangle + block_at(kBlocks - 1, k, b_row, b_vec));
+        undo[k] = rhs_by[k * 8 + g];
       }
+      float x[kBlocks][2][4] = {};
+#pragma unroll
+      for (int part = 0; part < 3; ++part)
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+            mma<Fp16>(x[k][u], part == 1 ? lo[k] : hi[k], part == 2 ? b_lo[k][2 * u] : b[k][2 * u], part == 2 ? b_lo[k][2 * u + 1] : b[k][2 * u + 1]);
+#pragma unroll
+      for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) add_scaled(w[u], x[k][u], undo[k]);
+    };
+    if (warp == 0) solve(std::integral_constant<int, 1>());
+    else if (warp == 1) solve(std::integral_constant<int, 2>());
+    else if (warp == 2) solve(std::integral_constant<int, 3>());
+    else solve(std::integral_constant<int, 4>());
+    {
+      const Scaled to = scaled_for(w[0], w[1]);
+      float2 x[4];
+      times(x, w[0], w[1], to.up);
+      left_factor(x, smem + W::kPlain + warp * 512 + lane * 16, nullptr);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], make_float2(by[k >> 1][0].z, by[k >> 1][1].z));
+      left_factor(x, smem + W::kWrite + warp * 1024 + lane * 16, smem + W::kWrite + warp * 1024 + 512 + lane * 16);
+      if (c == 0) plain_by[warp * 8 + g] = to.down;
     }
-    left_factor(w[0], w[1], smem + W::kPlain + warp * 512, nullptr, plain_by + warp * 8, lane);
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[u][e] *= by[u][e & 1].z;
-    left_factor(w[0], w[1], smem + W::kWrite + warp * 1024, smem + W::kWrite + warp * 1024 + 512, write_by + warp * 8, lane);
     __syncthreads();
     // The state after the chunk.
-    const float decay = f.decay;
+    {
+      uint32_t hi[4][4], lo[4][4], b[4][kTiles / 2][4];
+      float2 undo[4];
 #pragma unroll
-    for (int k = 0; k < kTiles; ++k)
+      for (int k = 0; k < 4; ++k) {
+        left_load(hi[k], smem + W::kWrite + k * 1024 + lane * 16);
+        left_load(lo[k], smem + W::kWrite + k * 1024 + 512 + lane * 16);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) state[k][e] *= decay;
+        for (int j = 0; j < kTiles; j += 2) load_matrices_t(b[k][j / 2], rows + image_at(16 * k + t_row, warp * kTiles + j + t_vec));
+        undo[k] = plain_by[k * 8 + g];
+        const float into = f.into[k];
+        undo[k].x *= into, undo[k].y *= into;
+      }
+      const float decay = f.decay;
+      float x[4][kTiles][4] = {};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      uint32_t hi[4], lo[4];
-      left_load(hi, smem + W::kWrite + k * 1024, lane);
-      left_load(lo, smem + W::kWrite + k * 1024 + 512, lane);
-      const float2 by = write_by[k * 8 + g];
+      for (int part = 0; part < 2; ++part)
 #pragma unroll
-      for (int j = 0; j < kTiles; j += 2) {
-        uint32_t b[4];
-        load_matrices_t(b, rows + image_at(16 * k + t_row, warp * kTiles + j + t_vec));
-        float x[2][4] = {};
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          mma<Fp16>(x[u], hi, b[2 * u], b[2 * u + 1]);
-          mma<Fp16>(x[u], lo, b[2 * u], b[2 * u + 1]);
-          add_scaled(state[j + u], x[u], by);
-        }
+          for (int j = 0; j < kTiles; ++j) mma<Fp16>(x[k][j], part ? lo[k] : hi[k], b[k][j / 2][2 * (j & 1)], b[k][j / 2][2 * (j & 1) + 1]);
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) state[j][e] *= decay;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add_scaled(state[j], x[k][j], undo[k]);
       }
     }
     publish();
@@ -659,14 +768,14 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
     for (int k = 0; k < 4; ++k) {
       if (k > warp) break;
       uint32_t hi[4], b[4];
-      left_load(hi, smem + W::kPlain + k * 512, lane);
+      left_load(hi, smem + W::kPlain + k * 512 + lane * 16);
       load_matrices(b, base + W::kM + block_at(warp, k, b_row, b_vec));
-      const float2 by = plain_by[k * 8 + g];
+      const float2 undo = plain_by[k * 8 + g];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         float x[4] = {};
         mma<Fp16>(x, hi, b[2 * u], b[2 * u + 1]);
-        add_scaled(my[u], x, by);
+        add_scaled(my[u], x, undo);
       }
     }
 #pragma unroll
