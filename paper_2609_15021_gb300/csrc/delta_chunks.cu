@@ -384,15 +384,16 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
+constexpr int kWalkThreads = 288;  // four warps for the state, four for the outputs, one for the copies
+
 template <int N>
 struct WalkShape {
   static constexpr int kSteps = N / 16;  // of 16 along the state's columns
   static constexpr int kT = 2 * kRowBytes<N> + kFactors, kStage = 2 * kRowBytes<N> + kFactors + 2 * kTriangle;
   // left factors as the matrix instruction takes them, 512 bytes for 16 columns and part, and their powers of two
   static constexpr int kM = 2 * kStage, kState = kM + kTriangle, kRhs = kState + kSteps * 1024, kWrite = kRhs + 4096, kPlain = kWrite + 4096,
-                       kStateBy = kPlain + 2048, kRhsBy = kStateBy + kSteps * 64, kPlainBy = kRhsBy + 256,
-                       kBars = kPlainBy + 256, kSmem = kBars + 64;
-  static_assert(2 * (kSmem + 1024) <= 233472, "two CTAs an SM");
+                       kStateBy = kPlain + 2048, kRhsBy = kStateBy + kSteps * 64, kPlainBy = kRhsBy + 256, kSmem = kPlainBy + 256;
+  static_assert(kSmem <= 231424, "shared memory of an SM");
 };
 
 // Two tiles of 16 x 8 sums as 16 columns of a left factor: fp16 parts hi and lo, times powers of two a row, the largest number
@@ -441,15 +442,22 @@ __device__ __forceinline__ void add_scaled(float (&d)[4], const float (&x)[4], f
   const float2 b = fma2(make_float2(x[2], x[3]), make_float2(by.y, by.y), make_float2(d[2], d[3]));
   d[0] = a.x, d[1] = a.y, d[2] = b.x, d[3] = b.y;
 }
+// Barriers: of all at a chunk's beginning, of the first four where rhs is there, of the eight where w is, and otherwise.
+enum { kBegin = 1, kRhsThere, kWThere, kEight };
+template <int kCount>
+__device__ __forceinline__ void meet(int id) { asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(kCount) : "memory"); }
+
 template <class E, int N>
-__global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant__ DeltaParams p) {
+__global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_constant__ DeltaParams p) {
   wait_for_previous();
   using W = WalkShape<N>;
   using T = typename E::T;
   extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars_s[3];  // of both stages and of M
+  __shared__ uint32_t flags_s[2];  // a chunk's: it goes token by token; a wait has run out
   __shared__ int32_t first_s;
   const StateView& v = p.state;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
+  const int lane = threadIdx.x & 31, all_warps = __shfl_sync(~0u, threadIdx.x >> 5, 0), warp = all_warps & 3, g = lane >> 2, c = lane & 3;
   const int32_t p0 = blockIdx.x * 16, h = blockIdx.y, group = h / p.heads_per_group;
   // The longest sequences first, as they are walked through longest (of more than a warp can look at, in their order).
   int32_t s = blockIdx.z;
@@ -468,16 +476,16 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
   rows_of(v, s, &begin, &end);
   int32_t chunks = pieces_of(begin, end, kChunk, p.by_token);
   if (chunks == 0) return;
-  const uint32_t base = smem_at(smem), bars = base + W::kBars;  // of both stages and of M
+  const uint32_t base = smem_at(smem), bars = smem_at(bars_s);
   if (threadIdx.x == 0) {
-    first_s = 0;
+    first_s = 0, flags_s[0] = flags_s[1] = 0;
     for (int i = 0; i < 3; ++i) bar_init(bars + 8 * i);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");  // what the kernel before has written is read by bulk copies
   }
   __syncthreads();
   int32_t before = 0;  // pieces of the sequences in front, as far as there is room
-  for (int32_t i = threadIdx.x; i < s; i += kThreads) {
+  for (int32_t i = threadIdx.x; i < s; i += kWalkThreads) {
     int64_t a, b;
     rows_of(v, i, &a, &b);
     before = min(before + pieces_of(a, b, kChunk, p.by_token), p.pieces);
@@ -491,14 +499,14 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
   uint8_t* keep = slot_of(v, v.slots_out, s);
   T* out = reinterpret_cast<T*>(p.out) + h * p.out_head + p0;
   if (!in || !keep) {
-    for (int64_t i = threadIdx.x; i < (end - begin) * 16; i += kThreads)
+    for (int64_t i = threadIdx.x; i < (end - begin) * 16; i += kWalkThreads)
       if (p0 + i % 16 < p.head_dim) out[(begin + i / 16) * p.out_token + i % 16] = E::down(0.f);
     return;
   }
 
   auto load_stage = [&](int32_t i) {  // by one thread
     const uint32_t bar = bars + 8 * (i & 1), to = base + (i & 1) * W::kStage;
-    if (p.stall && i == 1) return;
+    if (i >= chunks || (p.stall && i == 1)) return;
     bar_expect(bar, W::kStage);
     bulk_load(to, p.rows_space + ((int64_t)(first + i) * p.groups + group) * 2 * kRowBytes<N>, 2 * kRowBytes<N>, bar);
     bulk_load(to + 2 * kRowBytes<N>, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes, kFactors + 2 * kTriangle, bar);
@@ -507,141 +515,31 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
     bar_expect(bars + 16, kTriangle);
     bulk_load(base + W::kM, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes + kFactors + 2 * kTriangle, kTriangle, bars + 16);
   };
-  if (threadIdx.x == 0 && chunks > 0) load_stage(0);
-
-  // Values of a chunk, as a transposing move takes them: tokens 8 u + lane / 4 of the warp's, elements 2 c and the next
-  // of each eight.
-  const T* v_at = reinterpret_cast<const T*>(p.v) + h * p.v_head + p0 + 2 * c;
-  uint32_t raw[2][2];
-  auto load_values = [&](int32_t i) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t t = begin + (int64_t)i * kChunk + warp * 16 + 8 * u + g;
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-        raw[u][k] = t < end && p0 + 8 * k < p.head_dim ? *reinterpret_cast<const uint32_t*>(v_at + t * p.v_token + 8 * k) : 0;
-    }
-  };
-  load_values(0);
-
-  // The state: tiles of 16 x 8, a row g and g + 8, columns 2 c and the next.
-  constexpr int kTiles = N / 32;  // a warp's
-  float state[kTiles][4];
-  const int64_t state_at = ((int64_t)h * p.head_dim + p0) * N + warp * kTiles * 8 + 2 * c;
-  const bool fresh = v.fresh && v.fresh[s];
-#pragma unroll
-  for (int k = 0; k < kTiles; ++k)
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      float2 x = make_float2(0.f, 0.f);
-      if (!fresh && p0 + 8 * r < p.head_dim) x = *reinterpret_cast<const float2*>(in + (state_at + (g + 8 * r) * N + k * 8) * 4);
-      state[k][2 * r] = x.x, state[k][2 * r + 1] = x.y;
-    }
+  auto factors_of = [&](int32_t i) -> const Factors& { return *reinterpret_cast<const Factors*>(smem + (i & 1) * W::kStage + 2 * kRowBytes<N>); };
+  constexpr uint32_t kOdd = 1, kDead = 2;
+  bool dead = false;
   float2* state_by = reinterpret_cast<float2*>(smem + W::kStateBy);
   float2* rhs_by = reinterpret_cast<float2*>(smem + W::kRhsBy);
   float2* plain_by = reinterpret_cast<float2*>(smem + W::kPlainBy);
-  auto publish = [&]() {
-#pragma unroll
-    for (int k = 0; k < kTiles; k += 2) {
-      const int step = (warp * kTiles + k) / 2;
-      const Scaled by = scaled_for(state[k], state[k + 1]);
-      float2 x[4];
-      times(x, state[k], state[k + 1], by.up);
-      left_factor(x, smem + W::kState + step * 1024 + lane * 16, smem + W::kState + step * 1024 + 512 + lane * 16);
-      if (c == 0) state_by[step * 8 + g] = by.down;
-    }
-  };
-  publish();
-
   const int b_row = (lane >> 4) * 8 + (lane & 7), b_vec = lane >> 3 & 1;  // of a right factor's matrices
-  const int t_row = (lane >> 3 & 1) * 8 + (lane & 7), t_vec = lane >> 4;  // of one that is transposed
-  bool dead = false;
   int32_t i = 0;
-  for (; i < chunks; ++i) {
-    const int64_t t0 = begin + (int64_t)i * kChunk;
-    uint8_t* stage = smem + (i & 1) * W::kStage;
-    const uint32_t rows = base + (i & 1) * W::kStage;
-    const Factors& f = *reinterpret_cast<const Factors*>(stage + 2 * kRowBytes<N>);
-    dead = dead || !bar_wait(bars + 8 * (i & 1), i >> 1 & 1, p.wait_cycles);
-    const uint32_t carries = odd_carry<E>(raw[0][0]) | odd_carry<E>(raw[0][1]) | odd_carry<E>(raw[1][0]) | odd_carry<E>(raw[1][1]);
-    bool odd = odd_carried(carries) || (!dead && f.odd);
-    if (__syncthreads_or(odd || dead)) {  // and the state is there for all
-      if (__syncthreads_or(dead)) break;
-      odd = true;
-    }
-    if (threadIdx.x == 0) {
-      load_m(i);
-      if (i + 1 < chunks) load_stage(i + 1);
-    }
-    if (odd) {
-      // Token by token, a row for eight lanes.
-      float* all = reinterpret_cast<float*>(smem + W::kState);
-      static_assert(W::kSteps * 1024 == 16 * N * 4, "the state's room");
-#pragma unroll
-      for (int k = 0; k < kTiles; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) all[(g + 8 * (e >> 1)) * N + (warp * kTiles + k) * 8 + 2 * c + (e & 1)] = state[k][e];
-      __syncthreads();
-      const int row = threadIdx.x / 8, part = threadIdx.x % 8;
-      const bool used = p0 + row < p.head_dim;
-      float x[N / 8];
-#pragma unroll
-      for (int k = 0; k < N / 8; ++k) x[k] = all[row * N + k * 8 + part];
-      const int64_t stop = min(end, t0 + kChunk);
-      for (int64_t t = t0; t < stop; ++t) {
-        const T* k_at = reinterpret_cast<const T*>(p.k) + t * p.k_token + group * p.k_head + part;
-        const T* q_at = reinterpret_cast<const T*>(p.q) + t * p.q_token + group * p.q_head + part;
-        float kk = 0.f, qq = 0.f, kq = 0.f, sk = 0.f, sq = 0.f;
-#pragma unroll
-        for (int k = 0; k < N / 8; ++k) {
-          const float a = E::up(k_at[8 * k]), b = E::up(q_at[8 * k]);
-          kk += a * a, qq += b * b, kq += a * b, sk += x[k] * a, sq += x[k] * b;
-        }
-#pragma unroll
-        for (int m = 4; m; m >>= 1) {
-          kk += __shfl_xor_sync(~0u, kk, m), qq += __shfl_xor_sync(~0u, qq, m), kq += __shfl_xor_sync(~0u, kq, m);
-          sk += __shfl_xor_sync(~0u, sk, m), sq += __shfl_xor_sync(~0u, sq, m);
-        }
-        const float k_by = p.normalize ? rsqrtf(kk + p.eps) : 1.f, q_by = p.normalize ? p.scale * rsqrtf(qq + p.eps) : p.scale;
-        const float decay = p.dt ? expf(decay_of(p, E::up(reinterpret_cast<const T*>(p.dt)[t * p.dt_token + h]), h)) : 1.f;
-        const float beta = step_size(p, E::up(reinterpret_cast<const T*>(p.beta)[t * p.beta_token + h]));
-        const float value = used ? E::up(reinterpret_cast<const T*>(p.v)[t * p.v_token + h * p.v_head + p0 + row]) : 0.f;
-        const float d = beta * (value - decay * (sk * k_by));
-        if (used && part == 0) out[t * p.out_token + row] = E::down(decay * (sq * q_by) + d * (kq * k_by * q_by));
-#pragma unroll
-        for (int k = 0; k < N / 8; ++k) x[k] = x[k] * decay + d * (E::up(k_at[8 * k]) * k_by);
-      }
-#pragma unroll
-      for (int k = 0; k < N / 8; ++k) all[row * N + k * 8 + part] = x[k];
-      __syncthreads();
-#pragma unroll
-      for (int k = 0; k < kTiles; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) state[k][e] = all[(g + 8 * (e >> 1)) * N + (warp * kTiles + k) * 8 + 2 * c + (e & 1)];
-      load_values(i + 1);
-      dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
-      __syncthreads();
-      publish();
-      continue;
-    }
 
-    // S k and S q of the warp's 16 tokens.  Here and below what a product takes is loaded for many of them before the
-    // first, and every step has sums of its own, so that none waits for another.
-    float sk[2][4] = {}, y[2][4] = {};
+  // S times the keys or queries at `image` of the warp's 16 tokens.  Here and below what products take is loaded for many of
+  // them before the first, and every step has sums of its own, so that none waits for another.
+  auto read_state = [&](float (&d)[2][4], uint32_t image) {
     constexpr int kAtOnce = 4;
 #pragma unroll
     for (int k0 = 0; k0 < W::kSteps; k0 += kAtOnce) {
-      uint32_t hi[kAtOnce][4], lo[kAtOnce][4], b[kAtOnce][4], q[kAtOnce][4];
+      uint32_t hi[kAtOnce][4], lo[kAtOnce][4], b[kAtOnce][4];
       float2 by[kAtOnce];
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
         left_load(hi[k], smem + W::kState + (k0 + k) * 1024 + lane * 16);
         left_load(lo[k], smem + W::kState + (k0 + k) * 1024 + 512 + lane * 16);
-        load_matrices(b[k], rows + image_at(warp * 16 + b_row, 2 * (k0 + k) + b_vec));
-        load_matrices(q[k], rows + kRowBytes<N> + image_at(warp * 16 + b_row, 2 * (k0 + k) + b_vec));
+        load_matrices(b[k], image + image_at(warp * 16 + b_row, 2 * (k0 + k) + b_vec));
         by[k] = state_by[(k0 + k) * 8 + g];
       }
-      float x[kAtOnce][4][4] = {};
+      float x[kAtOnce][2][4] = {};
 #pragma unroll
       for (int part = 0; part < 2; ++part)
 #pragma unroll
@@ -649,148 +547,301 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
 #pragma unroll
           for (int u = 0; u < 2; ++u) mma<Fp16>(x[k][u], part ? lo[k] : hi[k], b[k][2 * u], b[k][2 * u + 1]);
 #pragma unroll
-      for (int part = 0; part < 2; ++part)
-#pragma unroll
-        for (int k = 0; k < kAtOnce; ++k)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) mma<Fp16>(x[k][2 + u], part ? lo[k] : hi[k], q[k][2 * u], q[k][2 * u + 1]);
-#pragma unroll
       for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) add_scaled(sk[u], x[k][u], by[k]);
-#pragma unroll
-      for (int k = 0; k < kAtOnce; ++k)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) add_scaled(y[u], x[k][2 + u], by[k]);
+        for (int u = 0; u < 2; ++u) add_scaled(d[u], x[k][u], by[k]);
     }
-    float4 by[2][2];
-    float m_by[2][2];
+  };
+  // A chunk that goes token by token, a row of the state for sixteen lanes; the state in `all`, between two barriers.
+  float* all = reinterpret_cast<float*>(smem + W::kState);
+  static_assert(W::kSteps * 1024 == 16 * N * 4, "the state's room");
+  auto by_tokens = [&](int64_t t0) {
+    constexpr int kCols = N / 16;
+    const int row = threadIdx.x / 16, part = threadIdx.x % 16;
+    const bool used = p0 + row < p.head_dim;
+    float x[kCols];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int k = 0; k < kCols; ++k) x[k] = all[row * N + k * 16 + part];
+    const int64_t stop = min(end, t0 + kChunk);
+    for (int64_t t = t0; t < stop; ++t) {
+      const T* k_at = reinterpret_cast<const T*>(p.k) + t * p.k_token + group * p.k_head + part;
+      const T* q_at = reinterpret_cast<const T*>(p.q) + t * p.q_token + group * p.q_head + part;
+      float kk = 0.f, qq = 0.f, kq = 0.f, sk = 0.f, sq = 0.f;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        by[u][e] = f.by[warp * 16 + 8 * u + 2 * c + e];
-        m_by[u][e] = f.row[warp * 16 + 8 * u + 2 * c + e];
+      for (int k = 0; k < kCols; ++k) {
+        const float a = E::up(k_at[16 * k]), b = E::up(q_at[16 * k]);
+        kk += a * a, qq += b * b, kq += a * b, sk += x[k] * a, sq += x[k] * b;
       }
 #pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float2 value = unpack2<E>(transpose(raw[u][r]));
-        sk[u][2 * r] = by[u][0].y * (value.x - by[u][0].x * sk[u][2 * r]);
-        sk[u][2 * r + 1] = by[u][1].y * (value.y - by[u][1].x * sk[u][2 * r + 1]);
+      for (int m = 8; m; m >>= 1) {
+        kk += __shfl_xor_sync(~0u, kk, m), qq += __shfl_xor_sync(~0u, qq, m), kq += __shfl_xor_sync(~0u, kq, m);
+        sk += __shfl_xor_sync(~0u, sk, m), sq += __shfl_xor_sync(~0u, sq, m);
       }
-    }
-    {
-      const Scaled to = scaled_for(sk[0], sk[1]);
-      float2 x[4];
-      times(x, sk[0], sk[1], to.up);
-      left_factor(x, smem + W::kRhs + warp * 1024 + lane * 16, smem + W::kRhs + warp * 1024 + 512 + lane * 16);
-      if (c == 0) rhs_by[warp * 8 + g] = to.down;
-    }
-    load_values(i + 1);
-    __syncthreads();
-    // W = T rhs: a warp's rows of T have as many blocks as it is warps from the first
-    float w[2][4] = {};
-    auto solve = [&](auto blocks) {
-      constexpr int kBlocks = decltype(blocks)::value;
-      uint32_t hi[kBlocks][4], lo[kBlocks][4], b[kBlocks][4], b_lo[kBlocks][4];
-      float2 undo[kBlocks];
+      const float k_by = p.normalize ? rsqrtf(kk + p.eps) : 1.f, q_by = p.normalize ? p.scale * rsqrtf(qq + p.eps) : p.scale;
+      const float decay = p.dt ? expf(decay_of(p, E::up(reinterpret_cast<const T*>(p.dt)[t * p.dt_token + h]), h)) : 1.f;
+      const float beta = step_size(p, E::up(reinterpret_cast<const T*>(p.beta)[t * p.beta_token + h]));
+      const float value = used ? E::up(reinterpret_cast<const T*>(p.v)[t * p.v_token + h * p.v_head + p0 + row]) : 0.f;
+      const float d = beta * (value - decay * (sk * k_by));
+      if (used && part == 0) out[t * p.out_token + row] = E::down(decay * (sq * q_by) + d * (kq * k_by * q_by));
 #pragma unroll
-      for (int k = 0; k < kBlocks; ++k) {
-        left_load(hi[k], smem + W::kRhs + k * 1024 + lane * 16);
-        left_load(lo[k], smem + W::kRhs + k * 1024 + 512 + lane * 16);
-        load_matrices(b[k], rows + W::kT + block_at(kBlocks - 1, k, b_row, b_vec));
-        load_matrices(b_lo[k], rows + W::kT + kTriangle + block_at(kBlocks - 1, k, b_row, b_vec));
-        undo[k] = rhs_by[k * 8 + g];
+      for (int k = 0; k < kCols; ++k) x[k] = x[k] * decay + d * (E::up(k_at[16 * k]) * k_by);
+    }
+#pragma unroll
+    for (int k = 0; k < kCols; ++k) all[row * N + k * 16 + part] = x[k];
+  };
+
+  if (all_warps == 8) {
+    // The copies: a chunk's before it begins, and whether it goes token by token.
+    if (lane == 0) load_stage(0);
+    for (; i < chunks; ++i) {
+      dead = dead || !bar_wait(bars + 8 * (i & 1), i >> 1 & 1, p.wait_cycles);
+      if (lane == 0 && (dead || factors_of(i).odd)) atomicOr(&flags_s[i & 1], dead ? kDead : kOdd);
+      meet<kWalkThreads>(kBegin);
+      if (flags_s[i & 1] & kDead) break;
+      if (lane == 0) load_m(i), load_stage(i + 1);
+      __syncwarp();
+    }
+  } else if (all_warps >= 4) {
+    for (; i < chunks; ++i) {
+      const int64_t t0 = begin + (int64_t)i * kChunk;
+      const uint32_t rows = base + (i & 1) * W::kStage;
+      const Factors& f = factors_of(i);
+      meet<kWalkThreads>(kBegin);  // the state and the chunk's copies are there
+      const uint32_t flags = flags_s[i & 1];
+      if (flags & kDead) break;
+      if (flags & kOdd) {
+        meet<256>(kEight);
+        if (threadIdx.x == 128) flags_s[i & 1] = 0;
+        by_tokens(t0);
+        dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+        meet<256>(kEight);
+        continue;
       }
-      float x[kBlocks][2][4] = {};
+      // S q of the warp's 16 tokens
+      float y[2][4] = {};
+      read_state(y, rows + kRowBytes<N>);
+      float by[2][2], m_by[2][2];
 #pragma unroll
-      for (int part = 0; part < 3; ++part)
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int k = 0; k < kBlocks; ++k)
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-            mma<Fp16>(x[k][u], part == 1 ? lo[k] : hi[k], part == 2 ? b_lo[k][2 * u] : b[k][2 * u], part == 2 ? b_lo[k][2 * u + 1] : b[k][2 * u + 1]);
-#pragma unroll
-      for (int k = 0; k < kBlocks; ++k)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) add_scaled(w[u], x[k][u], undo[k]);
-    };
-    if (warp == 0) solve(std::integral_constant<int, 1>());
-    else if (warp == 1) solve(std::integral_constant<int, 2>());
-    else if (warp == 2) solve(std::integral_constant<int, 3>());
-    else solve(std::integral_constant<int, 4>());
-    {
-      const Scaled to = scaled_for(w[0], w[1]);
-      float2 x[4];
-      times(x, w[0], w[1], to.up);
-      left_factor(x, smem + W::kPlain + warp * 512 + lane * 16, nullptr);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], make_float2(by[k >> 1][0].z, by[k >> 1][1].z));
-      left_factor(x, smem + W::kWrite + warp * 1024 + lane * 16, smem + W::kWrite + warp * 1024 + 512 + lane * 16);
-      if (c == 0) plain_by[warp * 8 + g] = to.down;
-    }
-    __syncthreads();
-    // The state after the chunk.
-    {
-      uint32_t hi[4][4], lo[4][4], b[4][kTiles / 2][4];
-      float2 undo[4];
+        for (int e = 0; e < 2; ++e) {
+          by[u][e] = f.by[warp * 16 + 8 * u + 2 * c + e].w;
+          m_by[u][e] = f.row[warp * 16 + 8 * u + 2 * c + e];
+        }
+      dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+      meet<256>(kWThere);  // S has been read
+      // y = e^c S q + M w
+      float mw[2][4] = {};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        left_load(hi[k], smem + W::kWrite + k * 1024 + lane * 16);
-        left_load(lo[k], smem + W::kWrite + k * 1024 + 512 + lane * 16);
+        if (k > warp) break;
+        uint32_t hi[4], b[4];
+        left_load(hi, smem + W::kPlain + k * 512 + lane * 16);
+        load_matrices(b, base + W::kM + block_at(warp, k, b_row, b_vec));
+        const float2 undo = plain_by[k * 8 + g];
 #pragma unroll
-        for (int j = 0; j < kTiles; j += 2) load_matrices_t(b[k][j / 2], rows + image_at(16 * k + t_row, warp * kTiles + j + t_vec));
-        undo[k] = plain_by[k * 8 + g];
-        const float into = f.into[k];
-        undo[k].x *= into, undo[k].y *= into;
+        for (int u = 0; u < 2; ++u) {
+          float x[4] = {};
+          mma<Fp16>(x, hi, b[2 * u], b[2 * u + 1]);
+          add_scaled(mw[u], x, undo);
+        }
       }
-      const float decay = f.decay;
-      float x[4][kTiles][4] = {};
-#pragma unroll
-      for (int part = 0; part < 2; ++part)
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-#pragma unroll
-          for (int j = 0; j < kTiles; ++j) mma<Fp16>(x[k][j], part ? lo[k] : hi[k], b[k][j / 2][2 * (j & 1)], b[k][j / 2][2 * (j & 1) + 1]);
-#pragma unroll
-      for (int j = 0; j < kTiles; ++j) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) state[j][e] *= decay;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) add_scaled(state[j], x[k][j], undo[k]);
-      }
-    }
-    publish();
-    // y = e^c S q + M W
-    dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
-    float my[2][4] = {};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (k > warp) break;
-      uint32_t hi[4], b[4];
-      left_load(hi, smem + W::kPlain + k * 512 + lane * 16);
-      load_matrices(b, base + W::kM + block_at(warp, k, b_row, b_vec));
-      const float2 undo = plain_by[k * 8 + g];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        float x[4] = {};
-        mma<Fp16>(x, hi, b[2 * u], b[2 * u + 1]);
-        add_scaled(my[u], x, undo);
-      }
-    }
+        const int64_t t = t0 + warp * 16 + 8 * u + g;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t t = t0 + warp * 16 + 8 * u + g;
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const uint32_t pair = transpose(pack2<E>(by[u][0].w * y[u][2 * r] + m_by[u][0] * my[u][2 * r],
-                                                 by[u][1].w * y[u][2 * r + 1] + m_by[u][1] * my[u][2 * r + 1]));
-        if (t < end && p0 + 8 * r < p.head_dim) *reinterpret_cast<uint32_t*>(out + t * p.out_token + 8 * r + 2 * c) = pair;
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t pair = transpose(pack2<E>(by[u][0] * y[u][2 * r] + m_by[u][0] * mw[u][2 * r],
+                                                   by[u][1] * y[u][2 * r + 1] + m_by[u][1] * mw[u][2 * r + 1]));
+          if (t < end && p0 + 8 * r < p.head_dim) *reinterpret_cast<uint32_t*>(out + t * p.out_token + 8 * r + 2 * c) = pair;
+        }
       }
     }
   }
+
+  // The state: tiles of 16 x 8, rows g and g + 8, columns 2 c and the next.
+  constexpr int kTiles = N / 32;  // a warp's
+  float state[kTiles][4];
+  const int64_t state_at = ((int64_t)h * p.head_dim + p0) * N + warp * kTiles * 8 + 2 * c;
+  if (all_warps < 4) {
+    // Values of a chunk, as a transposing move takes them: tokens 8 u + lane / 4 of the warp's, elements 2 c and the next
+    // of each eight.
+    const T* v_at[2];  // of the chunk that is loaded next
+    int64_t left = end - begin - warp * 16 - g;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) v_at[u] = reinterpret_cast<const T*>(p.v) + (begin + warp * 16 + 8 * u + g) * p.v_token + h * p.v_head + p0 + 2 * c;
+    const int64_t v_step = kChunk * p.v_token;
+    const bool has_row[2] = {true, p0 + 8 < p.head_dim};
+    uint32_t raw[2][2];
+    auto load_values = [&]() {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) raw[u][k] = left > 8 * u && has_row[k] ? *reinterpret_cast<const uint32_t*>(v_at[u] + 8 * k) : 0;
+        v_at[u] += v_step;
+      }
+      left -= kChunk;
+    };
+    auto values_there = [&](int32_t i) {
+      if (odd_carried(odd_carry<E>(raw[0][0]) | odd_carry<E>(raw[0][1]) | odd_carry<E>(raw[1][0]) | odd_carry<E>(raw[1][1]))) atomicOr(&flags_s[i & 1], kOdd);
+    };
+    load_values();
+    const bool fresh = v.fresh && v.fresh[s];
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        float2 x = make_float2(0.f, 0.f);
+        if (!fresh && p0 + 8 * r < p.head_dim) x = *reinterpret_cast<const float2*>(in + (state_at + (g + 8 * r) * N + k * 8) * 4);
+        state[k][2 * r] = x.x, state[k][2 * r + 1] = x.y;
+      }
+    auto publish = [&]() {
+#pragma unroll
+      for (int k = 0; k < kTiles; k += 2) {
+        const int step = (warp * kTiles + k) / 2;
+        const Scaled by = scaled_for(state[k], state[k + 1]);
+        float2 x[4];
+        times(x, state[k], state[k + 1], by.up);
+        left_factor(x, smem + W::kState + step * 1024 + lane * 16, smem + W::kState + step * 1024 + 512 + lane * 16);
+        if (c == 0) state_by[step * 8 + g] = by.down;
+      }
+    };
+    publish();
+    values_there(0);
+    const int t_row = (lane >> 3 & 1) * 8 + (lane & 7), t_vec = lane >> 4;  // of a factor that is transposed
+    for (; i < chunks; ++i) {
+      const uint32_t rows = base + (i & 1) * W::kStage;
+      const Factors& f = factors_of(i);
+      meet<kWalkThreads>(kBegin);  // the state and the chunk's copies are there
+      const uint32_t flags = flags_s[i & 1];
+      if (flags & kDead) break;
+      if (flags & kOdd) {
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) all[(g + 8 * (e >> 1)) * N + (warp * kTiles + k) * 8 + 2 * c + (e & 1)] = state[k][e];
+        meet<256>(kEight);
+        by_tokens(begin + (int64_t)i * kChunk);
+        load_values();
+        values_there(i + 1);
+        meet<256>(kEight);
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) state[k][e] = all[(g + 8 * (e >> 1)) * N + (warp * kTiles + k) * 8 + 2 * c + (e & 1)];
+        meet<128>(kRhsThere);
+        publish();
+        continue;
+      }
+      // S k of the warp's 16 tokens
+      float sk[2][4] = {};
+      read_state(sk, rows);
+      float write[2][2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float4 by[2] = {f.by[warp * 16 + 8 * u + 2 * c], f.by[warp * 16 + 8 * u + 2 * c + 1]};
+        write[u][0] = by[0].z, write[u][1] = by[1].z;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float2 value = unpack2<E>(transpose(raw[u][r]));
+          sk[u][2 * r] = by[0].y * (value.x - by[0].x * sk[u][2 * r]);
+          sk[u][2 * r + 1] = by[1].y * (value.y - by[1].x * sk[u][2 * r + 1]);
+        }
+      }
+      {
+        const Scaled by = scaled_for(sk[0], sk[1]);
+        float2 x[4];
+        times(x, sk[0], sk[1], by.up);
+        left_factor(x, smem + W::kRhs + warp * 1024 + lane * 16, smem + W::kRhs + warp * 1024 + 512 + lane * 16);
+        if (c == 0) rhs_by[warp * 8 + g] = by.down;
+      }
+      load_values();
+      // W = T rhs: a warp's rows of T have as many blocks as it is warps from the first
+      float w[2][4] = {};
+      auto solve = [&](auto blocks) {
+        constexpr int kBlocks = decltype(blocks)::value;
+        uint32_t hi[kBlocks][4], lo[kBlocks][4], b[kBlocks][4], b_lo[kBlocks][4];
+        float2 undo[kBlocks];
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) {
+          load_matrices(b[k], rows + W::kT + block_at(kBlocks - 1, k, b_row, b_vec));
+          load_matrices(b_lo[k], rows + W::kT + kTriangle + block_at(kBlocks - 1, k, b_row, b_vec));
+        }
+        meet<128>(kRhsThere);
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) {
+          left_load(hi[k], smem + W::kRhs + k * 1024 + lane * 16);
+          left_load(lo[k], smem + W::kRhs + k * 1024 + 512 + lane * 16);
+          undo[k] = rhs_by[k * 8 + g];
+        }
+        float x[kBlocks][2][4] = {};
+#pragma unroll
+        for (int part = 0; part < 3; ++part)
+#pragma unroll
+          for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+              mma<Fp16>(x[k][u], part == 1 ? lo[k] : hi[k], part == 2 ? b_lo[k][2 * u] : b[k][2 * u], part == 2 ? b_lo[k][2 * u + 1] : b[k][2 * u + 1]);
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) add_scaled(w[u], x[k][u], undo[k]);
+      };
+      if (warp == 0) solve(std::integral_constant<int, 1>());
+      else if (warp == 1) solve(std::integral_constant<int, 2>());
+      else if (warp == 2) solve(std::integral_constant<int, 3>());
+      else solve(std::integral_constant<int, 4>());
+      {
+        const Scaled by = scaled_for(w[0], w[1]);
+        float2 x[4];
+        times(x, w[0], w[1], by.up);
+        left_factor(x, smem + W::kPlain + warp * 512 + lane * 16, nullptr);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], make_float2(write[k >> 1][0], write[k >> 1][1]));
+        left_factor(x, smem + W::kWrite + warp * 1024 + lane * 16, smem + W::kWrite + warp * 1024 + 512 + lane * 16);
+        if (c == 0) plain_by[warp * 8 + g] = by.down;
+      }
+      // The state after the chunk.
+      {
+        uint32_t hi[4][4], lo[4][4], b[4][kTiles / 2][4];
+        float2 undo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int j = 0; j < kTiles; j += 2) load_matrices_t(b[k][j / 2], rows + image_at(16 * k + t_row, warp * kTiles + j + t_vec));
+        const float decay = f.decay;
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) state[j][e] *= decay;
+        meet<256>(kWThere);  // S has been read
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          left_load(hi[k], smem + W::kWrite + k * 1024 + lane * 16);
+          left_load(lo[k], smem + W::kWrite + k * 1024 + 512 + lane * 16);
+          undo[k] = plain_by[k * 8 + g];
+          const float into = f.into[k];
+          undo[k].x *= into, undo[k].y *= into;
+        }
+        float x[4][kTiles][4] = {};
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) mma<Fp16>(x[k][j], part ? lo[k] : hi[k], b[k][j / 2][2 * (j & 1)], b[k][j / 2][2 * (j & 1) + 1]);
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) add_scaled(state[j], x[k][j], undo[k]);
+        }
+      }
+      publish();
+      values_there(i + 1);
+    }
+  }
   if (__syncthreads_or(dead)) {
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 256) {
       *p.timeout = 1;
       // copies may still be on their way: their end, however short the waits' limit is
       if (i < chunks && !(p.stall && i == 1)) bar_wait(bars + 8 * (i & 1), i >> 1 & 1, kDefaultWaitCycles);
@@ -799,6 +850,7 @@ __global__ void __launch_bounds__(kThreads, 2) walk_kernel(const __grid_constant
     __syncthreads();
     return;
   }
+  if (all_warps >= 4) return;
 #pragma unroll
   for (int k = 0; k < kTiles; ++k)
 #pragma unroll
@@ -811,7 +863,7 @@ template <class E, int N>
 cudaError_t chunks(const DeltaParams& p, cudaStream_t s) {
   const cudaError_t e = launch_after(system_kernel<E, N>, dim3((unsigned)p.pieces, p.heads), kThreads, SystemShape<N>::kSmem, s, p);
   if (e != cudaSuccess) return e;
-  return launch_after(walk_kernel<E, N>, dim3((p.head_dim + 15) / 16, p.heads, p.state.num_seqs), kThreads, WalkShape<N>::kSmem, s, p);
+  return launch_after(walk_kernel<E, N>, dim3((p.head_dim + 15) / 16, p.heads, p.state.num_seqs), kWalkThreads, WalkShape<N>::kSmem, s, p);
 }
 
 template <class E, int N>
