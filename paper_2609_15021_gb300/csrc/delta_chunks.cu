@@ -85,7 +85,8 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
   using T = typename E::T;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ Factors f;
-  __shared__ float sum_s[kChunk], low_s[kChunk], key_s[kChunk], query_s[kChunk], beta_s[kChunk], squares_s[2][kChunk];
+  __shared__ float key_s[kChunk], query_s[kChunk], by_s[2][kChunk];
+  __shared__ float4 token_s[kChunk];  // the exponents' sum up to a token, what it lost, the key's factor, the step
   __shared__ int32_t buf[kThreads / 32 + 3];
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
@@ -114,7 +115,6 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
     }
     // sums of squares of the rounds' rows meet in a reduction that halves the rounds at every step
     float squares[kRounds];
-    uint32_t carries = 0;
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
@@ -123,11 +123,9 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
       for (int j = 0; j < 4; ++j) {
         const float2 x = unpack2<E>(u[j]);
         sum = fma2(x, x, sum);
-        carries |= odd_carry<E>(u[j]);
       }
       squares[i] = sum.x + sum.y;
     }
-    odd |= odd_carried(carries);
     int m = kLanes / 2, at = 0;
 #pragma unroll
     for (int left = kRounds; left > 1; left /= 2, m /= 2) {
@@ -141,17 +139,22 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
     }
 #pragma unroll
     for (; m; m >>= 1) squares[0] += __shfl_xor_sync(~0u, squares[0], m);
-    squares_s[which][warp * 16 + at * kAtOnce + sub] = squares[0];
+    {  // what takes the row's length below 2^14, and a token's factor; a row whose squares vanish counts as zeros
+      const int row = warp * 16 + at * kAtOnce + sub;
+      const float all = squares[0];
+      const int e = all > 0.f ? (((int)(__float_as_uint(all) >> 23) - 127) >> 1) - 13 : 0;  // its root is below 2^(e + 14)
+      const float factor = row < n ? (p.normalize ? rsqrtf(all + p.eps) : 1.f) * (which ? p.scale : 1.f) * power_of_two(e) : 0.f;
+      odd |= !isfinite(factor) || !isfinite(all);
+      by_s[which][row] = power_of_two(-e);
+      (which ? query_s : key_s)[row] = all > 0.f ? factor : 0.f;  // of zeros it would only set scales
+    }
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
       const int row = warp * 16 + i * kAtOnce + sub;
-      const float all = squares_s[which][row];
-      const int e = all > 0.f ? (((int)(__float_as_uint(all) >> 23) - 127) >> 1) - 13 : 0;  // its root is below 2^(e + 14)
-      const float by = power_of_two(-e);
+      const float by = by_s[which][row];
       const uint32_t u[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
       uint32_t w[4];
-      odd |= all < 0x1p-100f && ((u[0] | u[1] | u[2] | u[3]) & 0x7FFF7FFFu);  // too small for their squares
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 x = mul2(unpack2<E>(u[j]), make_float2(by, by));
@@ -160,17 +163,6 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
       const int to = which * kRowBytes<N> + image_at(row, vec);
       *reinterpret_cast<uint4*>(smem + to) = make_uint4(w[0], w[1], w[2], w[3]);
       if (writes_rows) *reinterpret_cast<uint4*>(rows_to + to) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  }
-  if (lane < 16) {  // a token's factors
-    const int t = warp * 16 + lane;
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      const float all = squares_s[which][t];
-      const int e = all > 0.f ? (((int)(__float_as_uint(all) >> 23) - 127) >> 1) - 13 : 0;
-      const float factor = t < n ? (p.normalize ? rsqrtf(all + p.eps) : 1.f) * (which ? p.scale : 1.f) * power_of_two(e) : 0.f;
-      odd |= !isfinite(factor) || !isfinite(all);
-      (which ? query_s : key_s)[t] = all > 0.f ? factor : 0.f;  // of zeros it would only set scales
     }
   }
   // Gates, two tokens a lane: sums of exponents up to a token in two parts, whole 64ths (that 64 tokens of up to 2^10 lose no
@@ -202,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
       // the sum of both, rounded, and what that lost (Knuth, "The Art of Computer Programming", vol. 2, 4.2.2)
       const float sum = below + below_fine, back = sum - below, low = (below - (sum - back)) + (below_fine - back);
       const int t = 2 * lane + k;
-      sum_s[t] = sum, low_s[t] = low, beta_s[t] = beta[k];
+      token_s[t] = make_float4(sum, low, 0.f, beta[k]);
       const float decay = ex2(sum) * ex2(low);
       f.by[t] = make_float4(decay, beta[k] * (1 / kUp), 0.f, decay);
     }
@@ -215,6 +207,7 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
   __syncthreads();
   if (threadIdx.x < kChunk) {
     float4& by = f.by[threadIdx.x];
+    token_s[threadIdx.x].z = key_s[threadIdx.x];
     by.x *= key_s[threadIdx.x], by.z *= key_s[threadIdx.x], by.w *= query_s[threadIdx.x];
     float most = fabsf(by.z);
 #pragma unroll
@@ -251,38 +244,46 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
   }
   __syncthreads();  // the images have been read
   float* diagonal = reinterpret_cast<float*>(smem + S::kDiagonal) + warp * 16 * kDiagonalPitch;  // [s][t]
+  float top[2] = {0.f, 0.f};
+  const float4 row[2] = {token_s[warp * 16 + g], token_s[warp * 16 + g + 8]};  // of the warp's
+  const float query[2] = {query_s[warp * 16 + g], query_s[warp * 16 + g + 8]};
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {  // rows g and g + 8 of the warp's
-    const int t = warp * 16 + g + 8 * r;
-    const float sum_t = sum_s[t], low_t = low_s[t], key_t = key_s[t] * beta_s[t], query_t = query_s[t];
-    float top = 0.f;
+  for (int j = 0; j < 8; ++j) {
+    if (j > 2 * warp + 1) break;
+    const int s = 8 * j + 2 * c;
+    const float4 col[2] = {token_s[s], token_s[s + 1]};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if (j > 2 * warp + 1) break;
-      float2 a;
+    for (int r = 0; r < 2; ++r) {
+      const int t = warp * 16 + g + 8 * r;
+      float a[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int s = 8 * j + 2 * c + e;
-        const float by = key_s[s] * (s <= t ? ex2((sum_t - sum_s[s]) + (low_t - low_s[s])) : 0.f);
-        (e ? a.y : a.x) = kk[j][2 * r + e] * by * key_t;
-        qk[j][2 * r + e] *= by * query_t;
-        top = fmaxf(top, fabsf(qk[j][2 * r + e]));
-        if (j >= 2 * warp && s < t) diagonal[(s & 15) * kDiagonalPitch + (t & 15)] = e ? a.y : a.x;
+        const float decay = ex2((row[r].x - col[e].x) + (row[r].y - col[e].y));
+        const float by = j < 2 * warp || s + e <= t ? col[e].z * decay : 0.f;
+        a[e] = kk[j][2 * r + e] * (by * (row[r].z * row[r].w));
+        qk[j][2 * r + e] *= by * query[r];
+        top[r] = fmaxf(top[r], fabsf(qk[j][2 * r + e]));
       }
       if (j < 2 * warp) {  // with its sign turned
         uint32_t hi, lo;
-        split2(make_float2(a.x * -kUp, a.y * -kUp), hi, lo);
+        split2(make_float2(a[0] * -kUp, a[1] * -kUp), hi, lo);
         uint8_t* to = smem + S::kA + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c;
         *reinterpret_cast<uint32_t*>(to) = hi;
         *reinterpret_cast<uint32_t*>(to + kTriangle) = lo;
+      } else {
+        diagonal[(s & 15) * kDiagonalPitch + (t & 15)] = a[0];  // of which what is below the diagonal is read
+        diagonal[(s + 1 & 15) * kDiagonalPitch + (t & 15)] = a[1];
       }
     }
-    top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-    odd |= !(top < INFINITY);
-    const int e = top > 0.f ? 13 - exponent_of(top) : 0;  // the row's largest to [2^13, 2^14)
-    const float up = power_of_two(min(e, 126));
-    if (c == 0) f.row[t] = power_of_two(-min(e, 126));
+  }
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 1));
+    top[r] = fmaxf(top[r], __shfl_xor_sync(~0u, top[r], 2));
+    odd |= !(top[r] < INFINITY);
+    const int e = top[r] > 0.f ? min(13 - exponent_of(top[r]), 126) : 0;  // the row's largest to [2^13, 2^14)
+    const float up = power_of_two(e);
+    if (c == 0) f.row[warp * 16 + g + 8 * r] = power_of_two(-e);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j > 2 * warp + 1) break;
@@ -459,18 +460,33 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, all_warps = __shfl_sync(~0u, threadIdx.x >> 5, 0), warp = all_warps & 3, g = lane >> 2, c = lane & 3;
   const int32_t p0 = blockIdx.x * 16, h = blockIdx.y, group = h / p.heads_per_group;
-  // The longest sequences first, as they are walked through longest (of more than a warp can look at, in their order).
+  // Of the sequences that go by chunks the longest first, as they are walked through longest (of more than a warp can look
+  // at, in their order).
   int32_t s = blockIdx.z;
-  if (v.num_seqs > 1 && v.num_seqs <= 32) {
-    int64_t a = 0, b = 0;
-    if (lane < v.num_seqs) rows_of(v, lane, &a, &b);
-    const int32_t mine = lane < v.num_seqs ? (int32_t)(b - a) : -1;
-    int32_t rank = 0;
-    for (int32_t k = 0; k < v.num_seqs; ++k) {
-      const int32_t other = __shfl_sync(~0u, mine, k);
-      rank += other > mine || (other == mine && k < lane);
+  if (v.num_seqs > 1) {
+    int32_t found = -1;
+    if (v.num_seqs <= 32) {
+      int64_t a = 0, b = 0;
+      if (lane < v.num_seqs) rows_of(v, lane, &a, &b);
+      const int32_t mine = lane < v.num_seqs ? (int32_t)(b - a) : -1;
+      int32_t rank = 0;
+      for (int32_t k = 0; k < v.num_seqs; ++k) {
+        const int32_t other = __shfl_sync(~0u, mine, k);
+        rank += other > mine || (other == mine && k < lane);
+      }
+      found = __ffs(__ballot_sync(~0u, lane < v.num_seqs && rank == s)) - 1;
+    } else {
+      int32_t before = 0;
+      for (int32_t base = 0; base < v.num_seqs && found < 0; base += 32) {  // every warp for itself
+        int64_t a = 0, b = 0;
+        if (base + lane < v.num_seqs) rows_of(v, base + lane, &a, &b);
+        const uint32_t some = __ballot_sync(~0u, base + lane < v.num_seqs && b - a > p.by_token);
+        if (before + __popc(some) > s) found = base + __fns(some, 0, s - before + 1);
+        before += __popc(some);
+      }
     }
-    s = __ffs(__ballot_sync(~0u, lane < v.num_seqs && rank == (int32_t)blockIdx.z)) - 1;
+    if (found < 0) return;
+    s = found;
   }
   int64_t begin, end;
   rows_of(v, s, &begin, &end);
@@ -863,7 +879,7 @@ template <class E, int N>
 cudaError_t chunks(const DeltaParams& p, cudaStream_t s) {
   const cudaError_t e = launch_after(system_kernel<E, N>, dim3((unsigned)p.pieces, p.heads), kThreads, SystemShape<N>::kSmem, s, p);
   if (e != cudaSuccess) return e;
-  return launch_after(walk_kernel<E, N>, dim3((p.head_dim + 15) / 16, p.heads, p.state.num_seqs), kWalkThreads, WalkShape<N>::kSmem, s, p);
+  return launch_after(walk_kernel<E, N>, dim3((p.head_dim + 15) / 16, p.heads, p.long_seqs), kWalkThreads, WalkShape<N>::kSmem, s, p);
 }
 
 template <class E, int N>

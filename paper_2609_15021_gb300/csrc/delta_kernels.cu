@@ -42,7 +42,7 @@ __device__ __forceinline__ float meet(float (&y)[kRows], int lane, int* mine) {
   return y[0];
 }
 
-template <class E, int N, int kRows>
+template <class E, int N, int kRows, bool kPacked>  // kPacked: sequences have several tokens
 __global__ void __launch_bounds__(128) delta_kernel(const __grid_constant__ DeltaParams p) {
   wait_for_previous();
   using T = typename E::T;
@@ -80,20 +80,39 @@ __global__ void __launch_bounds__(128) delta_kernel(const __grid_constant__ Delt
   const T* q_at = reinterpret_cast<const T*>(p.q) + group * p.q_head + col;
   const T* k_at = reinterpret_cast<const T*>(p.k) + group * p.k_head + col;
   const T* v_at = reinterpret_cast<const T*>(p.v) + h * p.v_head;
-  for (int64_t t = first; t < last; ++t) {
+  // A token's rows, loaded while the one before it is at work.
+  struct Token {
+    uint32_t q[kVec / 2], k[kVec / 2];
+    T v[kRows], dt, beta;
+  };
+  auto load = [&](int64_t t, Token& to) {
+#pragma unroll
+    for (int i = 0; i < kVec / 2; ++i) {
+      to.q[i] = *reinterpret_cast<const uint32_t*>(q_at + t * p.q_token + 2 * i);
+      to.k[i] = *reinterpret_cast<const uint32_t*>(k_at + t * p.k_token + 2 * i);
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      if (row0 + r * kSub < p.head_dim) to.v[r] = v_at[t * p.v_token + row0 + r * kSub];
+    if (p.dt) to.dt = reinterpret_cast<const T*>(p.dt)[t * p.dt_token + h];
+    to.beta = reinterpret_cast<const T*>(p.beta)[t * p.beta_token + h];
+  };
+  Token now, next;
+  if (!kPacked || first < last) load(first, now);
+  for (int64_t t = first; t < (kPacked ? last : first + 1); ++t) {
+    if (kPacked && t + 1 < last) load(t + 1, next);
     float q[kVec], k[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; i += 2) {
-      const float2 a = unpack2<E>(*reinterpret_cast<const uint32_t*>(q_at + t * p.q_token + i));
-      const float2 b = unpack2<E>(*reinterpret_cast<const uint32_t*>(k_at + t * p.k_token + i));
+      const float2 a = unpack2<E>(now.q[i / 2]), b = unpack2<E>(now.k[i / 2]);
       q[i] = a.x, q[i + 1] = a.y, k[i] = b.x, k[i + 1] = b.y;
     }
     float x[kRows];
 #pragma unroll
-    for (int r = 0; r < kRows; ++r)
-      x[r] = row0 + r * kSub < p.head_dim ? E::up(v_at[t * p.v_token + row0 + r * kSub]) : 0.f;
-    const float decay = p.dt ? expf(decay_of(p, E::up(reinterpret_cast<const T*>(p.dt)[t * p.dt_token + h]), h)) : 1.f;
-    const float beta = step_size(p, E::up(reinterpret_cast<const T*>(p.beta)[t * p.beta_token + h]));
+    for (int r = 0; r < kRows; ++r) x[r] = row0 + r * kSub < p.head_dim ? E::up(now.v[r]) : 0.f;
+    const float decay = p.dt ? expf(decay_of(p, E::up(now.dt), h)) : 1.f;
+    const float beta = step_size(p, E::up(now.beta));
+    if (kPacked) now = next;
     float qq = 0.f, kk = 0.f, kq = 0.f;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) qq += q[i] * q[i], kk += k[i] * k[i], kq += k[i] * q[i];
@@ -145,7 +164,9 @@ cudaError_t delta(const DeltaParams& p, int num_sms, cudaStream_t s) {
   const bool many = (int64_t)p.state.num_seqs * p.heads * p.head_dim >= (int64_t)num_sms * 4 * kSub * kMany;
   const int rows = 4 * kSub * (many ? kMany : kFew);
   const dim3 grid((p.head_dim + rows - 1) / rows, p.heads, p.state.num_seqs);
-  return many ? launch_after(delta_kernel<E, N, kMany>, grid, 128, 0, s, p) : launch_after(delta_kernel<E, N, kFew>, grid, 128, 0, s, p);
+  const auto kernel = p.state.starts ? (many ? delta_kernel<E, N, kMany, true> : delta_kernel<E, N, kFew, true>)
+                                     : (many ? delta_kernel<E, N, kMany, false> : delta_kernel<E, N, kFew, false>);
+  return launch_after(kernel, grid, 128, 0, s, p);
 }
 
 template <class E>

@@ -846,13 +846,15 @@ kvx_status check_delta(const kvx_state_batch* b, const kvx_delta* d) {
 
 // kv_state_delta's workspace: what the chunks of 64 tokens are worked on with, where there are any.
 struct DeltaSpace {
-  int32_t by_token, pieces;
+  int32_t by_token, long_seqs, pieces;
   int64_t heads, bytes;  // heads: the offset of head_space
 };
 kvx_status delta_space(const kvx_state_batch* b, const kvx_delta* d, DeltaSpace* w) {
   *w = {};
   if (!delta_by_chunks(b->tokens, b->num_seqs, b->starts, d->state_dim, &w->by_token)) return KVX_OK;
-  const int64_t pieces = b->tokens / kDeltaChunk + b->num_seqs;
+  // as many as sequences whose rows do not overlap can have
+  w->long_seqs = (int32_t)std::min<int64_t>(b->num_seqs, w->by_token < 0 ? b->num_seqs : b->tokens / (w->by_token + 1));
+  const int64_t pieces = b->tokens / kDeltaChunk + w->long_seqs;
   if (pieces > kMaxRows / d->heads) return refuse(KVX_ERANGE, "more than 2^30 chunks and heads");
   w->pieces = (int32_t)pieces;
   w->heads = pieces * d->groups * 2 * kDeltaChunk * d->state_dim * 2;
@@ -918,6 +920,7 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
       if ((st = mem.check(workspace, space.bytes)) != KVX_OK) return refuse(st, "workspace");
     }
     p.by_token = space.by_token;
+    p.long_seqs = space.long_seqs;
     p.pieces = space.pieces;
     p.rows_space = (uint8_t*)workspace;
     p.head_space = (uint8_t*)workspace + space.heads;

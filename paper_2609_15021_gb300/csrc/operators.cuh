@@ -195,6 +195,7 @@ struct DeltaParams {
   int32_t heads, head_dim, state_dim, heads_per_group, groups, softplus, sigmoid, normalize;
   float scale, eps;
   int32_t by_token;          // sequences of up to so many tokens go token by token, the others by chunks; -1: none
+  int32_t long_seqs;         // sequences that may go by chunks
   int32_t pieces;            // room for chunks; 0: no sequence goes by chunks
   uint8_t* rows_space;       // workspace: a chunk's and group's keys and queries
   uint8_t* head_space;       // and what else a chunk and head has
