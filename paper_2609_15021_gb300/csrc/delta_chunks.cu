@@ -18,7 +18,7 @@
 // by token within the walk.
 #include <algorithm>
 
-#include "state_common.cuh"
+#include "delta_common.cuh"
 #include "tcgen05.cuh"
 
 namespace kvx {
@@ -51,15 +51,14 @@ __device__ __forceinline__ int image_at(int row, int vec) { return (vec >> 3) * 
 __device__ __forceinline__ int block_at(int i, int j, int row, int half) {
   return (i * (i + 1) / 2 + j) * 512 + row * 32 + ((half ^ (row >> 2 & 1)) << 4);
 }
-__device__ __forceinline__ float decay_of(const DeltaParams& p, float raw, int32_t h) {  // its logarithm
-  if (p.dt_bias) raw += p.dt_bias[h];
-  return (p.softplus ? (raw > 20.f ? raw : log1pf(expf(raw))) : raw) * p.A[h];
-}
-__device__ __forceinline__ float step_size(const DeltaParams& p, float raw) { return p.sigmoid ? 1.f / (1.f + expf(-raw)) : raw; }
 __device__ __forceinline__ int exponent_of(float v) { return min(max((int)(__float_as_uint(v) >> 23 & 255) - 127, -126), 126); }
 __device__ __forceinline__ uint32_t half2_of(float a, float b) { return pack2<Fp16>(a, b); }
 
 // ---------------------------------------------------------------- what knows nothing of the state
+
+constexpr int kTokenRows = 8;
+template <int N>
+__host__ __device__ constexpr int32_t token_ctas(int32_t head_dim) { return (head_dim + 4 * kTokenRows * kTokenSub<N> - 1) / (4 * kTokenRows * kTokenSub<N>); }
 
 constexpr int kDiagonalPitch = 20;
 template <int N>
@@ -75,7 +74,8 @@ __device__ __forceinline__ void split2(float2 x, uint32_t& hi, uint32_t& lo) {
   lo = half2_of(rest.x, rest.y);
 }
 
-// A chunk and head a CTA, 16 of its tokens a warp.  T is made block by block: on the diagonal by substitution, below it as
+// A chunk and head a CTA, 16 of its tokens a warp; before them the CTAs of the sequences that go token by token, which
+// nothing here waits for (a launch of their own took 6 us more).  T is made block by block: on the diagonal by substitution, below it as
 // T_ij = -T_ii sum_{j<=k<i} A_ik T_kj, a column of blocks a warp, by products of numbers in two parts (in 32-bit floats, a column
 // and half of the rows a lane, it took a third of the kernel's time, most of it the first warp's).
 template <class E, int N>
@@ -90,7 +90,13 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
   __shared__ int32_t buf[kThreads / 32 + 3];
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, c = lane & 3;
-  const int32_t piece = blockIdx.x, h = blockIdx.y, group = h / p.heads_per_group;
+  const int32_t h = blockIdx.y, group = h / p.heads_per_group;
+  if ((int32_t)blockIdx.x < p.token_ctas) {
+    const int32_t each = token_ctas<N>(p.head_dim), s = blockIdx.x / each;
+    by_tokens<E, N, kTokenRows, true>(p, blockIdx.x - s * each, h, s);
+    return;
+  }
+  const int32_t piece = blockIdx.x - p.token_ctas;
   Piece found;
   if (!find_piece<kThreads>(v, piece, kChunk, p.by_token, buf, &found) || !found.in || !found.keep) return;
   const int64_t t0 = found.first + (int64_t)found.at * kChunk;
@@ -456,61 +462,50 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ __align__(8) uint64_t bars_s[3];  // of both stages and of M
   __shared__ uint32_t flags_s[2];  // a chunk's: it goes token by token; a wait has run out
-  __shared__ int32_t first_s;
   const StateView& v = p.state;
   const int lane = threadIdx.x & 31, all_warps = __shfl_sync(~0u, threadIdx.x >> 5, 0), warp = all_warps & 3, g = lane >> 2, c = lane & 3;
   const int32_t p0 = blockIdx.x * 16, h = blockIdx.y, group = h / p.heads_per_group;
   // Of the sequences that go by chunks the longest first, as they are walked through longest (of more than a warp can look
   // at, in their order).
-  int32_t s = blockIdx.z;
-  if (v.num_seqs > 1) {
-    int32_t found = -1;
-    if (v.num_seqs <= 32) {
-      int64_t a = 0, b = 0;
-      if (lane < v.num_seqs) rows_of(v, lane, &a, &b);
-      const int32_t mine = lane < v.num_seqs ? (int32_t)(b - a) : -1;
-      int32_t rank = 0;
-      for (int32_t k = 0; k < v.num_seqs; ++k) {
-        const int32_t other = __shfl_sync(~0u, mine, k);
-        rank += other > mine || (other == mine && k < lane);
-      }
-      found = __ffs(__ballot_sync(~0u, lane < v.num_seqs && rank == s)) - 1;
-    } else {
-      int32_t before = 0;
-      for (int32_t base = 0; base < v.num_seqs && found < 0; base += 32) {  // every warp for itself
-        int64_t a = 0, b = 0;
-        if (base + lane < v.num_seqs) rows_of(v, base + lane, &a, &b);
-        const uint32_t some = __ballot_sync(~0u, base + lane < v.num_seqs && b - a > p.by_token);
-        if (before + __popc(some) > s) found = base + __fns(some, 0, s - before + 1);
-        before += __popc(some);
-      }
+  int32_t s = -1, first = 0;  // its number, and that of its first chunk
+  int64_t begin = 0, end = 0;
+  if (v.num_seqs <= 32) {
+    if (lane < v.num_seqs) rows_of(v, lane, &begin, &end);
+    const int32_t mine = lane < v.num_seqs ? (int32_t)(end - begin) : -1;
+    int32_t rank = 0;
+    for (int32_t k = 0; k < v.num_seqs; ++k) {
+      const int32_t other = __shfl_sync(~0u, mine, k);
+      rank += other > mine || (other == mine && k < lane);
     }
-    if (found < 0) return;
-    s = found;
+    s = __ffs(__ballot_sync(~0u, lane < v.num_seqs && rank == (int32_t)blockIdx.z)) - 1;
+    if (s < 0) return;
+    first = __reduce_add_sync(~0u, lane < s ? min(pieces_of(begin, end, kChunk, p.by_token), (1 << 30) / 32) : 0);
+    begin = __shfl_sync(~0u, begin, s), end = __shfl_sync(~0u, end, s);
+  } else {  // every warp for itself
+    int32_t before = 0;
+    for (int32_t base = 0; base < v.num_seqs && s < 0; base += 32) {
+      int64_t a = 0, b = 0;
+      if (base + lane < v.num_seqs) rows_of(v, base + lane, &a, &b);
+      const int32_t pieces = base + lane < v.num_seqs ? min(pieces_of(a, b, kChunk, p.by_token), (1 << 30) / 32) : 0;
+      const uint32_t some = __ballot_sync(~0u, pieces > 0);
+      const int at = before + __popc(some) > (int32_t)blockIdx.z ? __fns(some, 0, (int32_t)blockIdx.z - before + 1) : 32;
+      first = min(first + (int32_t)__reduce_add_sync(~0u, lane < at ? pieces : 0), p.pieces);
+      if (at < 32) s = base + at, begin = __shfl_sync(~0u, a, at), end = __shfl_sync(~0u, b, at);
+      before += __popc(some);
+    }
+    if (s < 0) return;
   }
-  int64_t begin, end;
-  rows_of(v, s, &begin, &end);
-  int32_t chunks = pieces_of(begin, end, kChunk, p.by_token);
-  if (chunks == 0) return;
+  first = min(first, p.pieces);
+  const int32_t chunks = min(pieces_of(begin, end, kChunk, p.by_token), p.pieces - first);
+  if (pieces_of(begin, end, kChunk, p.by_token) == 0) return;
   const uint32_t base = smem_at(smem), bars = smem_at(bars_s);
   if (threadIdx.x == 0) {
-    first_s = 0, flags_s[0] = flags_s[1] = 0;
+    flags_s[0] = flags_s[1] = 0;
     for (int i = 0; i < 3; ++i) bar_init(bars + 8 * i);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async;" ::: "memory");  // what the kernel before has written is read by bulk copies
   }
   __syncthreads();
-  int32_t before = 0;  // pieces of the sequences in front, as far as there is room
-  for (int32_t i = threadIdx.x; i < s; i += kWalkThreads) {
-    int64_t a, b;
-    rows_of(v, i, &a, &b);
-    before = min(before + pieces_of(a, b, kChunk, p.by_token), p.pieces);
-  }
-  for (int m = 16; m; m >>= 1) before += __shfl_xor_sync(~0u, before, m);
-  if (lane == 0 && before) atomicAdd(&first_s, before);
-  __syncthreads();
-  const int32_t first = min(first_s, p.pieces);
-  chunks = min(chunks, p.pieces - first);
   const uint8_t* in = slot_of(v, v.slots_in, s);
   uint8_t* keep = slot_of(v, v.slots_out, s);
   T* out = reinterpret_cast<T*>(p.out) + h * p.out_head + p0;
@@ -877,7 +872,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
 
 template <class E, int N>
 cudaError_t chunks(const DeltaParams& p, cudaStream_t s) {
-  const cudaError_t e = launch_after(system_kernel<E, N>, dim3((unsigned)p.pieces, p.heads), kThreads, SystemShape<N>::kSmem, s, p);
+  DeltaParams q = p;
+  q.token_ctas = p.by_token >= 0 ? token_ctas<N>(p.head_dim) * p.state.num_seqs : 0;
+  const cudaError_t e = launch_after(system_kernel<E, N>, dim3((unsigned)(q.token_ctas + p.pieces), p.heads), kThreads, SystemShape<N>::kSmem, s, q);
   if (e != cudaSuccess) return e;
   return launch_after(walk_kernel<E, N>, dim3((p.head_dim + 15) / 16, p.heads, p.long_seqs), kWalkThreads, WalkShape<N>::kSmem, s, p);
 }

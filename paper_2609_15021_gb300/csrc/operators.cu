@@ -955,6 +955,6 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
     p.normalize = a->normalize;
     p.scale = a->scale ? a->scale : 1.f / std::sqrt((float)n);
     p.eps = a->eps;
-    return KVX_LAUNCHED(c, launch_delta(p, a->type, ctx.num_sms, stream), (p.by_token >= 0) + (p.pieces ? 2 : 0));
+    return KVX_LAUNCHED(c, launch_delta(p, a->type, ctx.num_sms, stream), p.pieces ? 2 : 1);
   });
 }

@@ -197,6 +197,7 @@ struct DeltaParams {
   int32_t by_token;          // sequences of up to so many tokens go token by token, the others by chunks; -1: none
   int32_t long_seqs;         // sequences that may go by chunks
   int32_t pieces;            // room for chunks; 0: no sequence goes by chunks
+  int32_t token_ctas;        // of the first kernel, of sequences that go token by token
   uint8_t* rows_space;       // workspace: a chunk's and group's keys and queries
   uint8_t* head_space;       // and what else a chunk and head has
   long long wait_cycles;     // limit of a wait for a copy
