@@ -239,18 +239,19 @@ def _declare(lib):
         "kv_append": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_new_rows), vp, vp, vp]),
         "kv_attend_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_attention), P(i64)]),
         "kv_attend": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_attention), vp, vp, vp, i64, vp]),
-        "kv_append_rotary": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_new_rows), P(kvx_rotary), vp, vp, vp, vp, vp]),
+        # structures that are made for a call: bytes (see _packer)
+        "kv_append_rotary": (st, [vp, P(kvx_pool), i32, P(kvx_batch), vp, vp, vp, vp, vp, vp, vp]),
         "kv_bounds": (st, [vp, P(kvx_pool), i32, P(kvx_batch), i32, i64, P(kvx_bounds), vp]),
         "kv_select_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_selection), P(i64)]),
-        "kv_select": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_bounds), P(kvx_selection), vp, vp, vp, i64, vp]),
+        "kv_select": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_bounds), vp, vp, vp, vp, i64, vp]),
         "kv_attend_selected_workspace": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_attention), i32, P(i64)]),
-        "kv_attend_selected": (st, [vp, P(kvx_pool), i32, P(kvx_batch), P(kvx_attention), i32, vp, vp, vp, vp, i64, vp]),
+        "kv_attend_selected": (st, [vp, P(kvx_pool), i32, P(kvx_batch), vp, i32, vp, vp, vp, vp, i64, vp]),
         "kv_evict": (st, [vp, P(kvx_pool), P(kvx_batch), P(kvx_eviction), vp]),
         "kv_state_conv": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_conv), vp, vp, vp]),
         "kv_state_scan_workspace": (st, [vp, P(kvx_state_batch), P(kvx_scan), P(i64)]),
         "kv_state_scan": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_scan), vp, vp, vp, vp, vp, vp, i64, vp]),
         "kv_state_delta_workspace": (st, [vp, P(kvx_state_batch), P(kvx_delta), P(i64)]),
-        "kv_state_delta": (st, [vp, P(kvx_state), P(kvx_state_batch), P(kvx_delta), vp, vp, vp, vp, vp, vp, vp, i64, vp]),
+        "kv_state_delta": (st, [vp, P(kvx_state), P(kvx_state_batch), vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -784,6 +785,20 @@ def _need_rows(x, what: str, dtype, shape) -> None:
         raise ValueError(f"the last dimension of {what} must be contiguous")
 
 
+def _packer(structure):
+    """pack(values of all fields) -> a structure's bytes as a C compiler lays them out, for structures that live for one call:
+    a sixth of the time that a ctypes object of 22 fields takes.  Pointers are whole numbers, 0 for none."""
+    import struct
+    codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_float: "f", ctypes.c_void_p: "P"}
+    s = struct.Struct("@" + "".join(codes[t] for _, t in structure._fields_) + "0q")
+    assert s.size == ctypes.sizeof(structure)
+    return s.pack
+
+
+_pack_new_rows, _pack_rotary, _pack_selection = _packer(kvx_new_rows), _packer(kvx_rotary), _packer(kvx_selection)
+_pack_attention, _pack_delta = _packer(kvx_attention), _packer(kvx_delta)
+
+
 def _row_strides(x, what: str, dtype, shape) -> tuple:
     """The strides of a tensor of `dtype` and `shape` whose innermost dimension is contiguous: _need_rows in one look, for
     calls that are as short as their checks."""
@@ -853,8 +868,8 @@ class KvRotary:
                 _check_tensor(w, what)
         self.q_heads, self.inv_freq, self.q_weight, self.k_weight = q_heads, inv_freq, q_weight, k_weight
         self._front = (q_heads, 0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, scale,
-                       None if inv_freq is None else inv_freq.data_ptr())
-        self._rear = (None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), eps,
+                       0 if inv_freq is None else inv_freq.data_ptr())
+        self._rear = (0 if q_weight is None else q_weight.data_ptr(), 0 if k_weight is None else k_weight.data_ptr(), eps,
                       weight_offset)
 
 
@@ -878,12 +893,11 @@ def kv_append_rotary(ctx, pool: KvPool, layer: int, batch: KvBatch, rotary: KvRo
         _row_strides(rotary.k_weight, "k_weight", dtype, (dim,))
     if positions is not None:
         _need(positions, "positions", "int32", (tokens,))
-    r = kvx_rotary(*rotary._front, None if positions is None else positions.data_ptr(), *rotary._rear, qs[0], qs[1], outs[0], outs[1])
-    rows = kvx_new_rows(_type_of(dtype), _cache_type(pool, cache_dtype), tokens, new_tokens,
-                        None if starts is None else starts.data_ptr(), ks[0], ks[1], vs[0], vs[1], k_scale, v_scale)
-    _check(_lib.kv_append_rotary(ctx, _byref(pool._c), layer, _byref(batch._c), _byref(rows), _byref(r), query.data_ptr(),
-                                 key.data_ptr(), value.data_ptr(), query_out.data_ptr(), _stream_handle(stream)),
-           "kv_append_rotary")
+    r = _pack_rotary(*rotary._front, 0 if positions is None else positions.data_ptr(), *rotary._rear, qs[0], qs[1], outs[0], outs[1])
+    rows = _pack_new_rows(_type_of(dtype), _cache_type(pool, cache_dtype), tokens, new_tokens,
+                          0 if starts is None else starts.data_ptr(), ks[0], ks[1], vs[0], vs[1], k_scale, v_scale)
+    _check(_lib.kv_append_rotary(ctx, _byref(pool._c), layer, _byref(batch._c), rows, r, query.data_ptr(), key.data_ptr(),
+                                 value.data_ptr(), query_out.data_ptr(), _stream_handle(stream)), "kv_append_rotary")
 
 
 class KvAttention:
@@ -1012,9 +1026,8 @@ def kv_select(ctx, pool: KvPool, batch: KvBatch, bounds: KvBounds, selection: Kv
     qs = _row_strides(query, "query", query.dtype, (tokens, selection.q_heads, pool.head_dim))
     _need(selected, "selected", "int32", (tokens, pool.num_heads, selection.budget))
     _check_tensor(selected, "selected")
-    c = kvx_selection(_type_of(query.dtype), *selection._fields, qs[0], qs[1])
-    _check(_lib.kv_select(ctx, _byref(pool._c), _byref(batch._c), bounds._of(pool), _byref(c), query.data_ptr(),
-                          selected.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_select")
+    c = _pack_selection(_type_of(query.dtype), *selection._fields, qs[0], qs[1])
+    _check(_lib.kv_select(ctx, _byref(pool._c), _byref(batch._c), bounds._of(pool), c, query.data_ptr(), selected.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_select")
 
 
 def kv_attend_selected_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttention, budget: int, dtype=None):
@@ -1045,10 +1058,10 @@ def kv_attend_selected(ctx, pool: KvPool, layer: int, batch: KvBatch, attention:
         _need(lse, "lse", "float32", (tokens, attention.q_heads))
         _check_tensor(lse, "lse")
     a = attention._c
-    c = kvx_attention(_type_of(dtype), _cache_type(pool, attention.cache_dtype), a.q_heads, a.new_tokens, a.scale, a.softcap,
-                      a.k_scale, a.v_scale, a.window, a.slopes, qs[0], qs[1], outs[0], outs[1],
-                      None if lse is None else lse.data_ptr())
-    _check(_lib.kv_attend_selected(ctx, _byref(pool._c), layer, _byref(batch._c), _byref(c), budget, selected.data_ptr(),
+    c = _pack_attention(_type_of(dtype), _cache_type(pool, attention.cache_dtype), a.q_heads, a.new_tokens, a.scale, a.softcap,
+                        a.k_scale, a.v_scale, a.window, a.slopes or 0, qs[0], qs[1], outs[0], outs[1],
+                        0 if lse is None else lse.data_ptr(), 0, 0, 0)
+    _check(_lib.kv_attend_selected(ctx, _byref(pool._c), layer, _byref(batch._c), c, budget, selected.data_ptr(),
                                    query.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
                                    _stream_handle(stream)), "kv_attend_selected")
 
@@ -1201,7 +1214,7 @@ def kv_state_delta(ctx, state: StateSlots, batch: StateBatch, query, key, value,
     ks = _row_strides(key, "key", dtype, (tokens, groups, state_dim))
     qs = _row_strides(query, "query", dtype, (tokens, groups, state_dim))
     steps = _row_strides(beta, "beta", dtype, (tokens, heads))
-    decays, a, bias = 0, None, None
+    decays, a, bias = 0, 0, 0
     if dt is not None:
         if A is None:
             raise ValueError("dt needs A")
@@ -1211,10 +1224,10 @@ def kv_state_delta(ctx, state: StateSlots, batch: StateBatch, query, key, value,
         if dt_bias is not None:
             _need(dt_bias, "dt_bias", "float32", (heads,))
             bias = dt_bias.data_ptr()
-    c = kvx_delta(_type_of(dtype), heads, head_dim, state_dim, groups, softplus, sigmoid, normalize, scale or 0.0, eps, a, bias,
-                  qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], decays, steps[0], outs[0], outs[1])
-    _check(_lib.kv_state_delta(ctx, _byref(state._c), _byref(batch._c), _byref(c), query.data_ptr(), key.data_ptr(),
-                               value.data_ptr(), None if dt is None else dt.data_ptr(), beta.data_ptr(), out.data_ptr(),
+    c = _pack_delta(_type_of(dtype), heads, head_dim, state_dim, groups, softplus, sigmoid, normalize, scale or 0.0, eps, a, bias,
+                    qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], decays, steps[0], outs[0], outs[1])
+    _check(_lib.kv_state_delta(ctx, _byref(state._c), _byref(batch._c), c, query.data_ptr(), key.data_ptr(), value.data_ptr(),
+                               None if dt is None else dt.data_ptr(), beta.data_ptr(), out.data_ptr(),
                                None if workspace is None else workspace.data_ptr(),
                                0 if workspace is None else workspace.numel(), _stream_handle(stream)), "kv_state_delta")
 
