@@ -45,13 +45,13 @@ enum { kNoTurn, kNeighbours, kVectors, kElements };  // how elements are paired
 template <class E, int kLanes, bool kFp8, int kPairs>
 __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_constant__ RotaryParams p) {
   wait_for_previous();
-  constexpr int kRows = 32 / kLanes;        // heads' rows that a warp takes at once
+  constexpr int kRows = 32 / kLanes;           // heads' rows that a warp takes at once
   constexpr int kEach = kRows * kRotaryBatch;  // and that are in flight: a unit of work
   __shared__ float2 turns[kRotaryWarps][kMaxPairs];  // cosine and sine
   const AppendParams& a = p.append;
   const PagesView& v = a.pages;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / kLanes, vec = lane % kLanes;
-  const int64_t at = (int64_t)blockIdx.x * kRotaryWarps + warp, token = at / p.parts;
+  const int64_t at = (int64_t)blockIdx.x * kRotaryWarps + warp, token = p.parts == 1 ? at : at / p.parts;
   if (token >= a.tokens) return;
   const int32_t part = (int32_t)(at - token * p.parts);
   int32_t s;
@@ -61,23 +61,26 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
   const int64_t place = length_of(v, s) - back;
   const bool used = vec * 8 < v.head_dim;
 
-  // Units: queries', keys', values'.
+  // Units: queries', keys', values', in that order.
   const int32_t q_units = (p.q_heads + kEach - 1) / kEach, k_units = (v.heads + kEach - 1) / kEach, units = q_units + 2 * k_units;
-  auto set_of = [&](int32_t u) { return u < q_units ? 0 : u < q_units + k_units ? 1 : 2; };
-  auto first_of = [&](int32_t u) { return (u - (u < q_units ? 0 : u < q_units + k_units ? q_units : q_units + k_units)) * kEach + sub; };
-  auto source = [&](int set, int32_t h) {
-    return set == 0 ? p.q + token * p.q_token + h * p.q_head
-                    : set == 1 ? a.key + token * a.key_token + h * a.key_head : a.value + token * a.value_token + h * a.value_head;
-  };
+  const uint8_t* q_at = p.q + token * p.q_token + sub * p.q_head + vec * 16;
+  const uint8_t* k_at = a.key + token * a.key_token + sub * a.key_head + vec * 16;
+  const uint8_t* v_at = a.value + token * a.value_token + sub * a.value_head + vec * 16;
   uint4 raw[kRotaryBatch], next[kRotaryBatch];
   auto load = [&](int32_t u, uint4 (&to)[kRotaryBatch]) {
-    const int set = set_of(u);
-    const int32_t h0 = first_of(u), heads = set ? v.heads : p.q_heads;
+    auto from = [&](const uint8_t* base, int64_t head, int32_t h0, int32_t heads) {
+      const int32_t rest = used ? heads - h0 - sub : 0;
+      const uint8_t* at = base + h0 * head;
 #pragma unroll
-    for (int k = 0; k < kRotaryBatch; ++k) {
-      const int32_t h = h0 + k * kRows;
-      to[k] = h < heads && used ? __ldcs(reinterpret_cast<const uint4*>(source(set, h)) + vec) : make_uint4(0, 0, 0, 0);
-    }
+      for (int k = 0; k < kRotaryBatch; ++k, at += kRows * head)
+        to[k] = k * kRows < rest ? __ldcs(reinterpret_cast<const uint4*>(at)) : make_uint4(0, 0, 0, 0);
+    };
+    if (u < q_units)
+      from(q_at, p.q_head, u * kEach, p.q_heads);
+    else if (u < q_units + k_units)
+      from(k_at, a.key_head, (u - q_units) * kEach, v.heads);
+    else
+      from(v_at, a.value_head, (u - q_units - k_units) * kEach, v.heads);
   };
   int32_t u = part;
   if (u < units) load(u, raw);
@@ -85,7 +88,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
   const int32_t half = p.rotary_dim / 2;
   float2* turn = turns[warp];
   const int64_t position = p.positions ? p.positions[token] : place;
-  if (kPairs != kNoTurn && set_of(u) < 2)
+  if (kPairs != kNoTurn && u < q_units + k_units)
     for (int32_t i = lane; i < half; i += 32) {
       float sine, cosine;
       sincospif(2.f * turn_of(position, p.inv_freq[i]), &sine, &cosine);
@@ -93,20 +96,22 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
     }
   __syncwarp();
 
-  // How an element of this lane is paired.
+  // How an element of this lane is paired, and its factors of x and of y.  A vector that is not turned is its own partner, with
+  // half of the weight in both factors, which is exact and leaves an infinite element infinite.
   const int32_t half_vecs = half / 8;
-  const bool turned = vec * 8 < 2 * half;  // some of the lane's are
-  const int32_t other = kPairs == kVectors && turned ? (vec < half_vecs ? vec + half_vecs : vec - half_vecs) : vec;
+  const bool turned = vec * 8 < 2 * half;
+  const int other = sub * kLanes + (kPairs == kVectors && turned ? (vec < half_vecs ? vec + half_vecs : vec - half_vecs) : vec);
   auto partner = [&](int32_t i) { return kPairs == kNeighbours ? i ^ 1 : i < half ? i + half : i - half; };
-  float2 c[4], y_by[4];  // factors of x and of y
-  auto factors = [&](int set) {
-    const typename E::T* w = reinterpret_cast<const typename E::T*>(set ? p.k_weight : p.q_weight);
+  float2 c[4], y_by[4];
+  auto factors = [&](const uint8_t* weights) {
+    const typename E::T* w = reinterpret_cast<const typename E::T*>(weights);
     auto weight = [&](int32_t i) { return w && i < v.head_dim ? E::up(w[i]) + p.weight_offset : 1.f; };
     float cs[8], ys[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int32_t i = vec * 8 + j;
       cs[j] = weight(i), ys[j] = 0.f;
+      if (kPairs == kVectors && !turned) cs[j] = ys[j] = 0.5f * cs[j];
       if (kPairs != kNoTurn && i < 2 * half) {
         const bool low = kPairs == kNeighbours ? !(i & 1) : i < half;
         const float2 t = turn[kPairs == kNeighbours ? i >> 1 : low ? i : i - half];
@@ -117,87 +122,100 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
     for (int j = 0; j < 4; ++j) c[j] = make_float2(cs[2 * j], cs[2 * j + 1]), y_by[j] = make_float2(ys[2 * j], ys[2 * j + 1]);
   };
   const float k_inverse = 1.f / a.k_scale, v_inverse = 1.f / a.v_scale;
-  int set = -1;
-  for (; u < units; u += p.parts) {
-    const int32_t ahead = u + p.parts;
-    if (ahead < units) load(ahead, next);
-    const int now = set_of(u);
-    if (now != set && now < 2) factors(now);
-    set = now;
-    const bool normed = set == 0 ? p.q_weight != nullptr : set == 1 && p.k_weight;
-    const int32_t h0 = first_of(u), heads = set ? v.heads : p.q_heads;
-    // All rows of the unit step by step, as none waits for another.
-    float2 x[kRotaryBatch][4];
+  auto unpack = [&](const uint4& q, float2 (&x)[4]) { x[0] = unpack2<E>(q.x), x[1] = unpack2<E>(q.y), x[2] = unpack2<E>(q.z), x[3] = unpack2<E>(q.w); };
+  auto packed = [&](const float2 (&x)[4]) {
+    return make_uint4(pack2<E>(x[0].x, x[0].y), pack2<E>(x[1].x, x[1].y), pack2<E>(x[2].x, x[2].y), pack2<E>(x[3].x, x[3].y));
+  };
+  // Rows normed and turned, step by step for all of the unit, as none waits for another.
+  auto turn_rows = [&](float2 (&x)[kRotaryBatch][4], bool normed, const uint8_t* from, int64_t head, int32_t rest) {
+    float by[kRotaryBatch];
+    if (normed) {
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k) {
+        float2 sum = mul2(x[k][0], x[k][0]);
+#pragma unroll
+        for (int j = 1; j < 4; ++j) sum = fma2(x[k][j], x[k][j], sum);
+        by[k] = sum.x + sum.y;
+      }
+#pragma unroll
+      for (int m = kLanes / 2; m; m >>= 1)
+#pragma unroll
+        for (int k = 0; k < kRotaryBatch; ++k) by[k] += __shfl_xor_sync(~0u, by[k], m);
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k) by[k] = rsqrtf(fmaf(by[k], p.inverse_dim, p.eps));
+    }
 #pragma unroll
     for (int k = 0; k < kRotaryBatch; ++k) {
-      const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+      float2 y[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[k][j] = unpack2<E>(w[j]);
-    }
-    if (now < 2) {
-      float by[kRotaryBatch];
-#pragma unroll
-      for (int k = 0; k < kRotaryBatch; ++k) by[k] = 1.f;
-      if (normed) {
-#pragma unroll
-        for (int k = 0; k < kRotaryBatch; ++k) {
-          float2 sum = mul2(x[k][0], x[k][0]);
-#pragma unroll
-          for (int j = 1; j < 4; ++j) sum = fma2(x[k][j], x[k][j], sum);
-          by[k] = sum.x + sum.y;
-        }
-#pragma unroll
-        for (int m = kLanes / 2; m; m >>= 1)
-#pragma unroll
-          for (int k = 0; k < kRotaryBatch; ++k) by[k] += __shfl_xor_sync(~0u, by[k], m);
-#pragma unroll
-        for (int k = 0; k < kRotaryBatch; ++k) by[k] = rsqrtf(by[k] * p.inverse_dim + p.eps);
-      }
-#pragma unroll
-      for (int k = 0; k < kRotaryBatch; ++k) {
-        const uint32_t w[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
-        const int32_t h = h0 + k * kRows;
-        float2 y[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int32_t i = vec * 8 + 2 * j;
-          y[j] = make_float2(0.f, 0.f);
-          if constexpr (kPairs == kNeighbours) {
-            if (i < 2 * half) y[j] = make_float2(x[k][j].y, x[k][j].x);
-          } else if constexpr (kPairs == kVectors) {
-            const uint32_t o = __shfl_sync(~0u, w[j], sub * kLanes + other);
-            y[j] = unpack2<E>(turned ? o : 0);
-          } else if constexpr (kPairs == kElements) {
-            const typename E::T* from = reinterpret_cast<const typename E::T*>(source(now, h < heads ? h : 0));
-            if (i < 2 * half && used) y[j].x = E::up(from[partner(i)]);
-            if (i + 1 < 2 * half && used) y[j].y = E::up(from[partner(i + 1)]);
-          }
-        }
-        if constexpr (kPairs == kElements) __syncwarp();  // q_out may be q: the row's elements have been read
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          x[k][j] = mul2(x[k][j], c[j]);
-          if constexpr (kPairs != kNoTurn) x[k][j] = fma2(y[j], y_by[j], x[k][j]);
-          x[k][j] = mul2(x[k][j], make_float2(by[k], by[k]));
+      for (int j = 0; j < 4; ++j) {
+        const int32_t i = vec * 8 + 2 * j;
+        if constexpr (kPairs == kNeighbours) {
+          y[j] = i < 2 * half ? make_float2(x[k][j].y, x[k][j].x) : make_float2(0.f, 0.f);
+        } else if constexpr (kPairs == kVectors) {
+          y[j].x = __shfl_sync(~0u, x[k][j].x, other), y[j].y = __shfl_sync(~0u, x[k][j].y, other);
+        } else if constexpr (kPairs == kElements) {
+          const typename E::T* at = reinterpret_cast<const typename E::T*>(from + k * kRows * head - vec * 16);
+          const bool there = k * kRows < rest;
+          y[j].x = there && i < 2 * half ? E::up(at[partner(i)]) : 0.f;
+          y[j].y = there && i + 1 < 2 * half ? E::up(at[partner(i + 1)]) : 0.f;
         }
       }
-    }
-    if (used && (now == 0 || row != kNoRow)) {
-      uint8_t* to = now == 0 ? p.q_out + token * p.out_token : v.base + row * v.row_bytes + (now == 2 ? v.half_bytes : 0);
-      const int64_t head = now == 0 ? p.out_head : v.head_bytes;
+      if constexpr (kPairs == kElements) __syncwarp();  // q_out may be q: the row's elements have been read
 #pragma unroll
-      for (int k = 0; k < kRotaryBatch; ++k) {
-        const int32_t h = h0 + k * kRows;
-        if (h >= heads) continue;
-        if (kFp8 && now > 0) {
-          const float scale = now == 2 ? a.v_scale : a.k_scale, inverse = now == 2 ? v_inverse : k_inverse;
-          *(reinterpret_cast<uint2*>(to + h * head) + vec) = make_uint2(to_e4m3(x[k][0], scale, inverse) | to_e4m3(x[k][1], scale, inverse) << 16,
-                                                                       to_e4m3(x[k][2], scale, inverse) | to_e4m3(x[k][3], scale, inverse) << 16);
-        } else if (now == 2) {
-          *(reinterpret_cast<uint4*>(to + h * head) + vec) = raw[k];
+      for (int j = 0; j < 4; ++j) {
+        x[k][j] = mul2(x[k][j], c[j]);
+        if constexpr (kPairs != kNoTurn) x[k][j] = fma2(y[j], y_by[j], x[k][j]);
+        if (normed) x[k][j] = mul2(x[k][j], make_float2(by[k], by[k]));
+      }
+    }
+  };
+  auto put = [&](const float2 (&x)[4], uint8_t* to, float scale, float inverse) {  // into the cache
+    if constexpr (kFp8)
+      *reinterpret_cast<uint2*>(to) = make_uint2(to_e4m3(x[0], scale, inverse) | to_e4m3(x[1], scale, inverse) << 16,
+                                                 to_e4m3(x[2], scale, inverse) | to_e4m3(x[3], scale, inverse) << 16);
+    else
+      *reinterpret_cast<uint4*>(to) = packed(x);
+  };
+  constexpr int kCacheVec = kFp8 ? 8 : 16;  // bytes of a vector's elements in the cache
+  uint8_t* cache = v.base + (row == kNoRow ? 0 : row) * v.row_bytes + sub * v.head_bytes + vec * kCacheVec;
+  bool q_made = false, k_made = false;
+  for (; u < units; u += p.parts) {
+    if (u + p.parts < units) load(u + p.parts, next);
+    if (u < q_units) {
+      if (!q_made) factors(p.q_weight), q_made = true;
+      const int32_t h0 = u * kEach, rest = used ? p.q_heads - h0 - sub : 0;
+      float2 x[kRotaryBatch][4];
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k) unpack(raw[k], x[k]);
+      turn_rows(x, p.q_weight != nullptr, q_at + h0 * p.q_head, p.q_head, rest);
+      uint8_t* to = p.q_out + token * p.out_token + (h0 + sub) * p.out_head + vec * 16;
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k, to += kRows * p.out_head)
+        if (k * kRows < rest) *reinterpret_cast<uint4*>(to) = packed(x[k]);
+    } else if (u < q_units + k_units) {
+      if (!k_made) factors(p.k_weight), k_made = true;
+      const int32_t h0 = (u - q_units) * kEach, rest = used ? v.heads - h0 - sub : 0;
+      float2 x[kRotaryBatch][4];
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k) unpack(raw[k], x[k]);
+      turn_rows(x, p.k_weight != nullptr, k_at + h0 * a.key_head, a.key_head, rest);
+      uint8_t* to = cache + h0 * v.head_bytes;
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k, to += kRows * v.head_bytes)
+        if (k * kRows < rest && row != kNoRow) put(x[k], to, a.k_scale, k_inverse);
+    } else {
+      const int32_t h0 = (u - q_units - k_units) * kEach, rest = used ? v.heads - h0 - sub : 0;
+      uint8_t* to = cache + v.half_bytes + h0 * v.head_bytes;
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k, to += kRows * v.head_bytes) {
+        if (!(k * kRows < rest && row != kNoRow)) continue;
+        if constexpr (kFp8) {
+          float2 x[4];
+          unpack(raw[k], x);
+          put(x, to, a.v_scale, v_inverse);
         } else {
-          *(reinterpret_cast<uint4*>(to + h * head) + vec) = make_uint4(pack2<E>(x[k][0].x, x[k][0].y), pack2<E>(x[k][1].x, x[k][1].y),
-                                                                       pack2<E>(x[k][2].x, x[k][2].y), pack2<E>(x[k][3].x, x[k][3].y));
+          *reinterpret_cast<uint4*>(to) = raw[k];
         }
       }
     }

@@ -87,17 +87,22 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
   uint32_t low[kPairs], high[kPairs];
 #pragma unroll
   for (int k = 0; k < kPairs; ++k) low[k] = used ? kInf : 0, high[k] = used ? kInf | 0x80008000u : 0;
-#pragma unroll 8
-  for (int32_t t = sub; t < held; t += kRows) {
-    if (!used) break;
-    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(from + t * step));
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  constexpr int kAtOnce = 8;  // loads in flight
+  if (used)
+    for (int32_t t0 = sub; t0 < held; t0 += kAtOnce * kRows) {
+      uint4 x[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) {
-      const uint32_t u = kWide ? widen2(w[k / 2] >> k % 2 * 16) : w[k];
-      low[k] = least2<C>(low[k], u), high[k] = most2<C>(high[k], u);
+      for (int i = 0; i < kAtOnce; ++i) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + min(t0 + i * kRows, held - 1) * step));
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int k = 0; k < kPairs; ++k) {
+          const uint32_t u = kWide ? widen2(w[k / 2] >> k % 2 * 16) : w[k];
+          low[k] = least2<C>(low[k], u), high[k] = most2<C>(high[k], u);
+        }
+      }
     }
-  }
   __syncwarp();
 #pragma unroll
   for (int m = kVecs; m < 32; m <<= 1)
