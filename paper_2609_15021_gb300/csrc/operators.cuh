@@ -88,8 +88,8 @@ struct SelectParams {
   int32_t tokens_each;      // new tokens whose rows a CTA scores at once
   int32_t score_tiles, score_parts;  // of a sequence: of pages, and of new tokens
 };
-// A CTA of the scores has 64 pages and at most so many rows of queries, but always all of a head's group.
-constexpr int32_t kScoreRows = 64, kMaxScoreGroup = 128, kScorePages = 64;
+// A CTA of the scores has 128 pages and at most so many rows of queries, but always all of a head's group.
+constexpr int32_t kScoreRows = 64, kMaxScoreGroup = 128, kScorePages = 128;
 inline int32_t score_tokens(int32_t group, int32_t new_tokens) {
   return group >= kScoreRows ? 1 : kScoreRows / group < new_tokens ? kScoreRows / group : new_tokens;
 }

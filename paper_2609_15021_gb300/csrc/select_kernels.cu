@@ -184,7 +184,7 @@ __device__ __forceinline__ void halves_of(uint32_t bytes, uint32_t& a, uint32_t&
   a = w[0], b = w[1];
 }
 
-// A CTA scores 64 pages of one sequence for one KV head: its queries are made whole numbers in shared memory, as the
+// A CTA scores 128 pages of one sequence for one KV head: its queries are made whole numbers in shared memory, as the
 // right factor of products of 16 pages by 8 query rows with k over the low and the high bounds.  (Bytes are widened to fp16, in
 // which they and all their products are exact, as are the sums in fp32.)  The elements of k are taken in an order that lets
 // a lane load 16 neighbouring bytes of a page's bounds.
@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
   // A page's bounds are under way while the queries are made ready.
   const int32_t* table = v.tables + s * v.table_stride;
   const uint8_t* box[2];
+  float size[2] = {0.f, 0.f};
   bool there[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
@@ -217,7 +218,9 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
     uint32_t row = kNoRow;
     if (page < pages) row = row_index(v, table, v.table_len, (uint32_t)page * block);
     there[k] = row != kNoRow;
-    box[k] = reinterpret_cast<const uint8_t*>(p.boxes) + ((int64_t)(there[k] ? row / v.page_rows : 0) * v.heads + h) * k_all;
+    const int64_t at = (int64_t)(there[k] ? row / v.page_rows : 0) * v.heads + h;
+    box[k] = reinterpret_cast<const uint8_t*>(p.boxes) + at * k_all;
+    if (there[k]) size[k] = p.sizes[at];
   }
 
   // Rows of queries, four vectors of 16 bytes in flight: one row a vector, 8 elements a lane.
@@ -250,7 +253,11 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 x = unpack2<E>(fine ? w[j] : 0);
-        const __half2 whole = __floats2half2_rn(fminf(fmaxf(rintf(by(x.x)), -127.f), 127.f), fminf(fmaxf(rintf(by(x.y)), -127.f), 127.f));
+        // to whole numbers by a sum that leaves no fraction; a step that lost bits can leave more than 127
+        constexpr float kWhole = 12582912.f;  // 1.5 2^23
+        const float2 y = make_float2(by(x.x), by(x.y));
+        __half2 whole = __floats2half2_rn((y.x + kWhole) - kWhole, (y.y + kWhole) - kWhole);
+        if (!by.plain) whole = __hmax2(__hmin2(whole, __floats2half2_rn(127.f, 127.f)), __floats2half2_rn(-127.f, -127.f));
         up[j] = __hmax2(whole, zero), down[j] = __hmin2(whole, zero);
       }
       uint2* to = reinterpret_cast<uint2*>(q_s + r * pitch + lane * 8);
@@ -298,17 +305,16 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
       }
     }
   }
-  // the page's size; -inf where no page is named
-  const uint32_t live = __ballot_sync(~0u, there[0] && c == 0), live8 = __ballot_sync(~0u, there[1] && c == 0);
+  // times the page's size; -inf where no page is named
+  const uint32_t live[2] = {__ballot_sync(~0u, there[0]), __ballot_sync(~0u, there[1])};
   __syncwarp();
-  for (int32_t i = lane; i < 16 * tokens; i += 32) {
-    const int32_t t = i / 16, in = i % 16, page = page0 + warp * 16 + in;
-    if (page >= pages) continue;
+  const int32_t in = lane % 16, page = page0 + warp * 16 + in;
+  const float low = __shfl_sync(~0u, size[0], in % 8 * 4), high = __shfl_sync(~0u, size[1], in % 8 * 4);
+  for (int32_t t = lane / 16; t < tokens && page < pages; t += 2) {
     float top = -INFINITY;
-    if ((in < 8 ? live : live8) >> (in % 8 * 4) & 1) {
+    if (live[in / 8] >> (in % 8 * 4) & 1) {
       for (int32_t r = t * p.group; r < (t + 1) * p.group; ++r) top = fmaxf(top, mine[in * dot_pitch + r]);
-      const uint32_t row = row_index(v, table, v.table_len, (uint32_t)page * block);
-      top = __fmul_rn(top, p.sizes[(int64_t)(row / v.page_rows) * v.heads + h]);
+      top = __fmul_rn(top, in < 8 ? low : high);
     }
     p.scores[(((int64_t)s * p.new_tokens + t0 + t) * v.heads + h) * p.score_stride + page] = top;
   }
