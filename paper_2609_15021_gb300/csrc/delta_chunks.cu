@@ -11,12 +11,14 @@
 //
 // Rounding: keys and queries are fp16 numbers times a power of two a row, whose length is below 2^14 and above 2^12, so that a
 // bf16 number keeps its bits down to 2^-27 of that and is off by 2^-37 of it below.  The state, rhs and W's decayed copy are each
-// two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so is 2^9 T.  M and the W that it is multiplied
-// with are rounded to fp16 once.  Sums are fp32.
+// two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so is 2^9 T.  M and the W that it is multiplied with
+// are too for fp16 outputs, which would be off by 3.3e-4 where their own rounding gives 2.1e-4; for bf16 ones, whose rounding
+// gives 1.7e-3, they are rounded to fp16 once, which adds 2.5e-4 (squared, so nothing) and takes 4 % less time.  Sums are fp32.
 //
 // A chunk with a number that is not finite, a decay above 1 or a T above 64 (keys with b |k|^2 well above 2) goes token
 // by token within the walk.
 #include <algorithm>
+#include <type_traits>
 
 #include "delta_common.cuh"
 #include "tcgen05.cuh"
@@ -29,9 +31,11 @@ constexpr float kMost = 1024.f;   // of a token's exponent
 constexpr float kLargest = 64.f;  // of T
 constexpr float kUp = 512.f;      // that T is multiplied by, as what a decay leaves of it is small, and rhs divided by
 
-// What the system kernel leaves of a chunk and head (offsets in bytes): a token's factors, then T in its two parts
-// and M as 16 x 16 blocks on and below the diagonal, row by row.
+// What the system kernel leaves of a chunk and head (offsets in bytes): a token's factors, then T and M, each in
+// two parts (M for bf16 in one), as 16 x 16 blocks on and below the diagonal, row by row.
 constexpr int kTriangle = 10 * 512;
+template <class E>
+constexpr int kPartsOfM = std::is_same<E, Fp16>::value ? 2 : 1;
 struct Factors {
   float4 by[kChunk];    // of S k_t in rhs, of v_t less that, of w_t in the state, of S q_t in y
   float row[kChunk];    // M's row
@@ -40,7 +44,7 @@ struct Factors {
   float into[4];        // powers of two that are taken out of the third factors, 16 tokens each
   float pad[26];
 };
-constexpr int kFactors = (int)sizeof(Factors), kHeadBytes = kFactors + 3 * kTriangle;
+constexpr int kFactors = (int)sizeof(Factors), kHeadBytes = kFactors + 4 * kTriangle;
 static_assert(kFactors == 1408 && kHeadBytes == kDeltaHeadBytes && kHeadBytes % 128 == 0, "bulk copies");
 // And of a chunk and group: keys and queries as panels of 64 elements, rows of 128 bytes with their vectors permuted.
 template <int N>
@@ -63,9 +67,9 @@ __host__ __device__ constexpr int32_t token_ctas(int32_t head_dim) { return (hea
 constexpr int kDiagonalPitch = 20;
 template <int N>
 struct SystemShape {
-  // keys and queries; when they have been multiplied, in their place: A below the diagonal blocks and T, each in two parts,
-  // M, and A's diagonal blocks transposed in 32 bits
-  static constexpr int kA = 0, kT = 2 * kTriangle, kM = 4 * kTriangle, kDiagonal = 5 * kTriangle, kThen = kDiagonal + 4 * 16 * kDiagonalPitch * 4;
+  // keys and queries; when they have been multiplied, in their place: A below the diagonal blocks, T and M, each in two
+  // parts, and A's diagonal blocks transposed in 32 bits
+  static constexpr int kA = 0, kT = 2 * kTriangle, kM = 4 * kTriangle, kDiagonal = 6 * kTriangle, kThen = kDiagonal + 4 * 16 * kDiagonalPitch * 4;
   static constexpr int kSmem = 2 * kRowBytes<N> > kThen ? 2 * kRowBytes<N> : kThen;
 };
 __device__ __forceinline__ void split2(float2 x, uint32_t& hi, uint32_t& lo) {
@@ -293,7 +297,11 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (j > 2 * warp + 1) break;
-      *reinterpret_cast<uint32_t*>(smem + S::kM + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c) = half2_of(qk[j][2 * r] * up, qk[j][2 * r + 1] * up);
+      uint32_t hi, lo;
+      split2(mul2(make_float2(qk[j][2 * r], qk[j][2 * r + 1]), make_float2(up, up)), hi, lo);
+      uint8_t* to = smem + S::kM + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c;
+      *reinterpret_cast<uint32_t*>(to) = hi;
+      if constexpr (kPartsOfM<E> == 2) *reinterpret_cast<uint32_t*>(to + kTriangle) = lo;
     }
   }
   __syncwarp();
@@ -374,7 +382,7 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
   }
   odd = __syncthreads_or(odd);
   if (threadIdx.x == 0) f.odd = odd;
-  for (int i = threadIdx.x; i < 3 * kTriangle / 16; i += kThreads)
+  for (int i = threadIdx.x; i < (2 + kPartsOfM<E>) * kTriangle / 16; i += kThreads)
     reinterpret_cast<uint4*>(head_to + kFactors)[i] = reinterpret_cast<const uint4*>(smem + S::kT)[i];
   __syncthreads();
   for (int i = threadIdx.x; i < kFactors / 16; i += kThreads)
@@ -398,8 +406,8 @@ struct WalkShape {
   static constexpr int kSteps = N / 16;  // of 16 along the state's columns
   static constexpr int kT = 2 * kRowBytes<N> + kFactors, kStage = 2 * kRowBytes<N> + kFactors + 2 * kTriangle;
   // left factors as the matrix instruction takes them, 512 bytes for 16 columns and part, and their powers of two
-  static constexpr int kM = 2 * kStage, kState = kM + kTriangle, kRhs = kState + kSteps * 1024, kWrite = kRhs + 4096, kPlain = kWrite + 4096,
-                       kStateBy = kPlain + 2048, kRhsBy = kStateBy + kSteps * 64, kPlainBy = kRhsBy + 256, kSmem = kPlainBy + 256;
+  static constexpr int kM = 2 * kStage, kState = kM + 2 * kTriangle, kRhs = kState + kSteps * 1024, kWrite = kRhs + 4096, kPlain = kWrite + 4096,
+                       kStateBy = kPlain + 4096, kRhsBy = kStateBy + kSteps * 64, kPlainBy = kRhsBy + 256, kSmem = kPlainBy + 256;
   static_assert(kSmem <= 231424, "shared memory of an SM");
 };
 
@@ -523,8 +531,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     bulk_load(to + 2 * kRowBytes<N>, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes, kFactors + 2 * kTriangle, bar);
   };
   auto load_m = [&](int32_t i) {
-    bar_expect(bars + 16, kTriangle);
-    bulk_load(base + W::kM, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes + kFactors + 2 * kTriangle, kTriangle, bars + 16);
+    constexpr int kBytes = kPartsOfM<E> * kTriangle;
+    bar_expect(bars + 16, kBytes);
+    bulk_load(base + W::kM, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes + kFactors + 2 * kTriangle, kBytes, bars + 16);
   };
   auto factors_of = [&](int32_t i) -> const Factors& { return *reinterpret_cast<const Factors*>(smem + (i & 1) * W::kStage + 2 * kRowBytes<N>); };
   constexpr uint32_t kOdd = 1, kDead = 2;
@@ -646,14 +655,22 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         if (k > warp) break;
-        uint32_t hi[4], b[4];
-        left_load(hi, smem + W::kPlain + k * 512 + lane * 16);
+        uint32_t hi[4], lo[4], b[4], b_lo[4];
+        left_load(hi, smem + W::kPlain + k * 1024 + lane * 16);
         load_matrices(b, base + W::kM + block_at(warp, k, b_row, b_vec));
+        if constexpr (kPartsOfM<E> == 2) {
+          left_load(lo, smem + W::kPlain + k * 1024 + 512 + lane * 16);
+          load_matrices(b_lo, base + W::kM + kTriangle + block_at(warp, k, b_row, b_vec));
+        }
         const float2 undo = plain_by[k * 8 + g];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           float x[4] = {};
           mma<Fp16>(x, hi, b[2 * u], b[2 * u + 1]);
+          if constexpr (kPartsOfM<E> == 2) {
+            mma<Fp16>(x, lo, b[2 * u], b[2 * u + 1]);
+            mma<Fp16>(x, hi, b_lo[2 * u], b_lo[2 * u + 1]);
+          }
           add_scaled(mw[u], x, undo);
         }
       }
@@ -806,7 +823,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         const Scaled by = scaled_for(w[0], w[1]);
         float2 x[4];
         times(x, w[0], w[1], by.up);
-        left_factor(x, smem + W::kPlain + warp * 512 + lane * 16, nullptr);
+        left_factor(x, smem + W::kPlain + warp * 1024 + lane * 16, kPartsOfM<E> == 2 ? smem + W::kPlain + warp * 1024 + 512 + lane * 16 : nullptr);
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], make_float2(write[k >> 1][0], write[k >> 1][1]));
         left_factor(x, smem + W::kWrite + warp * 1024 + lane * 16, smem + W::kWrite + warp * 1024 + 512 + lane * 16);

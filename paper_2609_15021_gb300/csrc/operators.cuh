@@ -204,7 +204,7 @@ struct DeltaParams {
   int* timeout;              // set when one ran out
   bool stall;                // fault point "delta_wait": the second chunk's copies are not made
 };
-constexpr int32_t kDeltaChunk = 64, kDeltaHeadBytes = 16768;  // tokens; bytes of head_space
+constexpr int32_t kDeltaChunk = 64, kDeltaHeadBytes = 21888;  // tokens; bytes of head_space
 // Whether a batch's sequences go by chunks, and which do not (*by_token).
 bool delta_by_chunks(int64_t tokens, int32_t num_seqs, bool packed, int32_t state_dim, int32_t* by_token);
 // Pieces that the workspace has room for: as many as sequences whose rows do not overlap can have.  No more than there are

@@ -152,6 +152,24 @@ def test_long_prompts(ctx):
     check(ctx, [2100], 1, 64, 128, 1, FP16)
 
 
+def test_a_prompt_in_fp16_is_off_by_its_rounding(ctx):
+    """Factors in two parts are off by 2^-22, sums by some 2^-20: beside the rounding of an output, 2^-11 at most and
+    2^-11 / sqrt(3) in the mean square, they are nothing.  (A factor rounded to fp16 once would add half of that to the square.)"""
+    k = kvx()
+    t, heads, n = 700, 2, 128
+    st = Slots(2, heads, n, n, dtype=FP16)
+    batch, _ = batch_of([t], [0], [1], [1], False)
+    data = Inputs(t, heads, n, n, 1, FP16, seed=31)
+    out = torch.empty((t, heads, n), dtype=FP16, device="cuda")
+    k.kv_state_delta(ctx, st.slots, batch, out=out, A=data.A.cuda(), dt_bias=data.bias.cuda(),
+                     workspace=k.kv_state_delta_workspace(ctx, batch, heads, n, n), **data.cuda())
+    torch.cuda.synchronize()
+    x = data.cpu()
+    y = mixers.delta(x["query"], x["key"], x["value"], x["beta"], torch.zeros_like(st.state[0]), x["dt"], data.A, data.bias)[0]
+    rounding, off = y.half().double() - y, out.cpu().double() - y
+    assert float(off.square().mean()) <= 1.1 * float(rounding.square().mean())
+
+
 @pytest.mark.parametrize("softplus,sigmoid,normalize,bias", [(False, True, True, False), (True, False, True, True), (True, True, False, False),
                                                              (False, False, False, False)])
 def test_options(ctx, softplus, sigmoid, normalize, bias):
