@@ -775,8 +775,8 @@ kvx_status kv_attend(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kv
  *   x = x / sqrt(mean(x^2) + eps) * (weight + weight_offset)      where there is a weight
  *   (a, b) = (a cos - b sin, b cos + a sin) * rotary_scale         of the pairs of the first rotary_dim elements,
  * the i'th pair by the angle position * inv_freq[i], whose full turns are taken off in 64 bits.  q goes to q_out (which may
- * be q itself), key and value to the pages as kv_append puts them there.  A token that belongs to no sequence
- * leaves its row of q_out as it was; one before position 0 or of a bad page still gets its row.
+ * be q itself, and else may not lie over q, key or value), key and value to the pages as kv_append puts them there.  A token
+ * that belongs to no sequence leaves its row of q_out as it was; one before position 0 or of a bad page still gets its row.
  */
 typedef struct {
   int32_t q_heads;
@@ -809,8 +809,8 @@ typedef struct {
 } kvx_bounds;
 
 /* Make the bounds of the pages that hold the last new_tokens tokens of every sequence: after an append, or, with as many as
-   the longest has, of all its pages after a restore.  elem type: cache_type, KVX_TYPE_*.  They are made from
-   the keys alone, whatever was there.  A page whose table entry is out of range is left out and reported.   */
+   the longest has, of all its pages after a restore or an eviction into new ones.  elem type: cache_type, KVX_TYPE_*.  They
+   are made from the keys alone, whatever was there.  A page whose table entry is out of range is left out and reported.   */
 kvx_status kv_bounds(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, int32_t cache_type,
                      int64_t new_tokens, const kvx_bounds* bounds, kvx_stream_t stream);
 
@@ -959,7 +959,8 @@ kvx_status kv_state_scan(kvx_ctx* ctx, const kvx_state* state, const kvx_state_b
  * b_t = beta_t (1 / (1 + exp(-beta_t)) if sigmoid is set):
  *   S_t = a_t S_{t-1} + b_t (v_t - a_t S_{t-1} k_t) k_t^T   (head_dim x state_dim, fp32, a slot's as kv_state_scan's)
  *   out_t = S_t q_t
- * Keys whose b_t |k_t|^2 is above 2 make the recurrence itself grow.
+ * Keys whose b_t |k_t|^2 is above 2 make the recurrence itself grow.  out may not lie over q, k or v, whose rows are read for
+ * many of its columns (the same pointer is refused).
  */
 typedef struct {
   int32_t type;       /* KVX_TYPE_BF16 or _FP16: q, k, v, dt, beta, out           */

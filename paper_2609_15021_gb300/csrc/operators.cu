@@ -257,8 +257,7 @@ kvx_status check_bounds(DeviceMemory& mem, const kvx_pool* pool, const kvx_bound
   return st != KVX_OK ? refuse(st, "boxes") : check_words(mem, b->sizes, rows, "sizes");
 }
 
-// What kv_append and kv_append_rotary check alike, in two parts: what needs no device, and the memory.  `none`: there is
-// nothing to append.
+// What kv_append and kv_append_rotary check alike, in two parts: what needs no device, and the memory.
 kvx_status view_append(const CtxView& ctx, const kvx_pool* pool, const kvx_batch* batch, const kvx_new_rows* rows, Geometry* g,
                        AppendParams* p) {
   kvx_status st = view_pages(ctx, pool, batch, g, &p->pages);
@@ -909,6 +908,7 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
           (st = check_rows(mem, {v, rows, a->v_token_stride, h, a->v_head_stride, d, "v"}, false)) != KVX_OK ||
           (st = check_rows(mem, {out, rows, a->out_token_stride, h, a->out_head_stride, d, "out"}, true)) != KVX_OK)
         return st;
+      if (out == q || out == k || out == v) return refuse(KVX_EINVAL, "out is q, k or v");
       if (dt && (st = check_gate(mem, dt, rows, a->dt_token_stride, h, "dt")) != KVX_OK) return st;
       if ((st = check_gate(mem, beta, rows, a->beta_token_stride, h, "beta")) != KVX_OK) return st;
     }

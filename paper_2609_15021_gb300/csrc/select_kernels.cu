@@ -445,7 +445,8 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
     const bool is_above = i < to && (r > border || always(i)), is_equal = r == border && r != 0;
     const uint32_t a_bits = __ballot_sync(~0u, is_above), e_bits = __ballot_sync(~0u, is_equal);
     const int32_t my_a = a + __popc(a_bits & below), my_e = e + __popc(e_bits & below);
-    if (is_above || (is_equal && my_e < equal)) out[my_a + min(my_e, equal)] = i;
+    const int32_t place = my_a + min(my_e, equal);  // below keep, but where another call writes to the same workspace
+    if ((is_above || (is_equal && my_e < equal)) && place < keep) out[place] = i;
     a += __popc(a_bits), e += __popc(e_bits);
   });
 }

@@ -437,6 +437,23 @@ def test_slots_past_four_gib(ctx):
         close(out.cpu().double(), y, after, state, slack, terms, q, BF16, True)
 
 
+def test_an_output_over_an_input_is_refused(ctx):
+    k = kvx()
+    st = Slots(2, 2, 64, 64)
+    for lens in ([100, 3], [1, 1]):
+        batch, starts = batch_of(lens, [0, 1])
+        data = Inputs(starts[-1], 2, 64, 64, 2, BF16)
+        x = data.cuda()
+        before = {name: v.clone() for name, v in x.items()}
+        ws = k.kv_state_delta_workspace(ctx, batch, 2, 64, 64)
+        for name in ("query", "key", "value"):
+            with pytest.raises(k.KvxError) as e:
+                k.kv_state_delta(ctx, st.slots, batch, out=x[name], A=data.A.cuda(), workspace=ws, **x)
+            assert e.value.status == k.KVX_EINVAL
+        torch.cuda.synchronize()
+        assert all(torch.equal(x[name], before[name]) for name in before) and torch.equal(st.dev.cpu(), st.cpu)
+
+
 def test_refusals(ctx):
     """Each returns its status before anything is enqueued and leaves the outputs alone."""
     k = kvx()
