@@ -1,6 +1,10 @@
 // delta_kernels.cu -- the gated delta rule token by token, and which sequences go by chunks.
 //
 //   S_t = a_t S_{t-1} + b_t (v_t - a_t S_{t-1} k_t) k_t^T,   y_t = S_t q_t
+//
+// Rows of the state know nothing of one another, and stay in registers from the first token of a sequence to the last.  One token
+// of each sequence is bound by the state's bytes: 96 sequences of 16 heads x 128 x 128 (201 MB) take 34 us, 88 % of the DRAM's
+// rate; of several tokens a chain of two sums over a row and what the token before wrote, 0.6 us a token.
 #include <algorithm>
 
 #include "delta_common.cuh"
@@ -17,6 +21,9 @@ __global__ void __launch_bounds__(128) delta_kernel(const __grid_constant__ Delt
 template <class E, int N>
 cudaError_t delta(const DeltaParams& p, int num_sms, cudaStream_t s) {
   constexpr int kSub = kTokenSub<N>;
+  // Rows of a warp at once: 8, that many loads are in flight (96 sequences of a token 35 us in a graph, 49 with 2), or 2 where there
+  // are too few rows for all SMs (a sequence of 16 tokens 14.5 us, and 16.4).  A row of 16 has four lanes, which end the sums of
+  // four rows, and eight rows of 256 would take 165 registers a thread.
   constexpr int kMany = N == 16 ? 4 : N == 256 ? 4 : 8, kFew = 2;
   const bool many = (int64_t)p.state.num_seqs * p.heads * p.head_dim >= (int64_t)num_sms * 4 * kSub * kMany;
   const int rows = 4 * kSub * (many ? kMany : kFew);
@@ -40,8 +47,9 @@ cudaError_t delta(const DeltaParams& p, int num_sms, cudaStream_t s) {
 }  // namespace
 
 bool delta_by_chunks(int64_t tokens, int32_t num_seqs, bool packed, int32_t state_dim, int32_t* by_token) {
-  // 16 heads of 128 x 128: a sequence of 16 tokens takes 10 us token by token and 12 by chunks, which take no longer for 64, 24 tokens
-  // 16; sixteen sequences of 16 tokens 47 us and 78, of 32 tokens 117 and 74.
+  // 16 heads of 128 x 128, in a graph: a sequence of 16 tokens takes 14.5 us token by token and 16.5 by chunks, which take no
+  // longer for 64, and one of 24 tokens 20.6; four of 24 tokens 34 and 31, of 16 tokens 23 and 31; sixteen of 16 tokens
+  // 51 and 80, of 24 tokens 74 and 80, of 32 tokens 146 (in launches of their own) and 80.
   const int32_t few = num_seqs > 1 ? 24 : 16;
   *by_token = INT32_MAX;
   if (!packed || (state_dim != 64 && state_dim != 128) || tokens <= few) return false;

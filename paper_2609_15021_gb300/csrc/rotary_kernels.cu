@@ -10,7 +10,11 @@
 //
 // Angles: a position of 2^20 times a frequency has 2^-4 left of a 32-bit product's 24 bits, so turns are taken in 64-bit
 // whole numbers: f / 2 pi in units of 2^-64, times the position, of which the whole turns overflow.  Sine and cosine are
-// taken of the rest in 32 bits.  (In 64-bit floats, of which an SM has two units, they took a third of the time.)
+// taken of the rest in 32 bits.  (An SM has two units for 64-bit floats.)
+//
+// Measured: 16,384 tokens of 24 + 2 x 4 heads x 256, bf16 into e4m3 (503 MB): 103 us, 4.9 TB/s, 72 % of the DRAM's rate: what is
+// left is its 84 million instructions.  With the way of pairing read from the parameters instead of a template's, and rows by
+// indexes instead of pointers, 123 us.
 #include <algorithm>
 
 #include "attend_common.cuh"
@@ -228,7 +232,8 @@ template <class E, int kLanes>
 cudaError_t rotary(const RotaryParams& p, bool fp8, int num_sms, cudaStream_t s) {
   constexpr int kEach = 32 / kLanes * kRotaryBatch;
   const int32_t units = (p.q_heads + kEach - 1) / kEach + 2 * ((p.append.pages.heads + kEach - 1) / kEach);
-  // few tokens: a warp a unit
+  // Few tokens: a warp a unit.  Of 32 + 2 x 8 heads x 128, in a graph: 64 tokens 6.8 us, 12.4 with a warp a token; 608 tokens 12.3
+  // either way; 1,216 tokens 16.4 and 12.5, 4,864 51.4 and 26.8, as every unit of a token makes its sines and factors again.
   RotaryParams q = p;
   q.parts = p.append.tokens >= 8 * num_sms ? 1 : units;
   q.inverse_dim = 1.f / p.append.pages.head_dim;
