@@ -12,9 +12,11 @@
 // whole numbers: f / 2 pi in units of 2^-64, times the position, of which the whole turns overflow.  Sine and cosine are
 // taken of the rest in 32 bits.  (An SM has two units for 64-bit floats.)
 //
-// Measured: 16,384 tokens of 24 + 2 x 4 heads x 256, bf16 into e4m3 (503 MB): 103 us, 4.9 TB/s, 72 % of the DRAM's rate: what is
-// left is its 84 million instructions.  With the way of pairing read from the parameters instead of a template's, and rows by
-// indexes instead of pointers, 123 us.
+// Measured: 16,384 tokens of 24 + 2 x 4 heads x 256, bf16 into e4m3 (503 MB): 96 us, 5.2 TB/s, 77 % of the DRAM's rate: what is
+// left is its 59 million instructions, at 16 warps an SM.  With the way of pairing read from the parameters instead of a
+// template's, and rows by indexes instead of pointers, 123 us; with the next rows in registers of their own, every row's sum made by
+// all lanes and 256 threads a CTA, 103.  Two rows in flight a lane and 28 warps an SM take 95 there and 37 instead of 27 for
+// 4,864 tokens of 32 + 2 x 8 heads x 128.
 #include <algorithm>
 
 #include "attend_common.cuh"
@@ -22,7 +24,7 @@
 namespace kvx {
 namespace {
 
-constexpr int kRotaryThreads = 256, kRotaryWarps = kRotaryThreads / 32;
+constexpr int kRotaryThreads = 128, kRotaryWarps = kRotaryThreads / 32;
 constexpr int kMaxPairs = 128;
 constexpr int kRotaryBatch = 4;  // rows' vectors that a lane has in flight
 
@@ -47,7 +49,7 @@ __device__ __forceinline__ float turn_of(int64_t position, float f) {
 enum { kNoTurn, kNeighbours, kVectors, kElements };  // how elements are paired
 
 template <class E, int kLanes, bool kFp8, int kPairs>
-__global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_constant__ RotaryParams p) {
+__global__ void __launch_bounds__(kRotaryThreads, 4) rotary_kernel(const __grid_constant__ RotaryParams p) {
   wait_for_previous();
   constexpr int kRows = 32 / kLanes;           // heads' rows that a warp takes at once
   constexpr int kEach = kRows * kRotaryBatch;  // and that are in flight: a unit of work
@@ -70,14 +72,15 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
   const uint8_t* q_at = p.q + token * p.q_token + sub * p.q_head + vec * 16;
   const uint8_t* k_at = a.key + token * a.key_token + sub * a.key_head + vec * 16;
   const uint8_t* v_at = a.value + token * a.value_token + sub * a.value_head + vec * 16;
-  uint4 raw[kRotaryBatch], next[kRotaryBatch];
-  auto load = [&](int32_t u, uint4 (&to)[kRotaryBatch]) {
+  uint4 raw[kRotaryBatch];
+  auto load = [&](int32_t u) {
+    if (u >= units) return;
     auto from = [&](const uint8_t* base, int64_t head, int32_t h0, int32_t heads) {
       const int32_t rest = used ? heads - h0 - sub : 0;
       const uint8_t* at = base + h0 * head;
 #pragma unroll
       for (int k = 0; k < kRotaryBatch; ++k, at += kRows * head)
-        to[k] = k * kRows < rest ? __ldcs(reinterpret_cast<const uint4*>(at)) : make_uint4(0, 0, 0, 0);
+        raw[k] = k * kRows < rest ? __ldcs(reinterpret_cast<const uint4*>(at)) : make_uint4(0, 0, 0, 0);
     };
     if (u < q_units)
       from(q_at, p.q_head, u * kEach, p.q_heads);
@@ -87,7 +90,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
       from(v_at, a.value_head, (u - q_units - k_units) * kEach, v.heads);
   };
   int32_t u = part;
-  if (u < units) load(u, raw);
+  load(u);
   const uint32_t row = place < 0 ? kNoRow : row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)place);
   const int32_t half = p.rotary_dim / 2;
   float2* turn = turns[warp];
@@ -142,11 +145,19 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
         by[k] = sum.x + sum.y;
       }
 #pragma unroll
-      for (int m = kLanes / 2; m; m >>= 1)
+      for (int m = kLanes / 2, left = kRotaryBatch / 2; left; left /= 2, m /= 2) {  // a half of the lanes goes on with a half of the rows
+        const bool upper = lane & m;
 #pragma unroll
-        for (int k = 0; k < kRotaryBatch; ++k) by[k] += __shfl_xor_sync(~0u, by[k], m);
+        for (int k = 0; k < left; ++k) {
+          const float send = upper ? by[k] : by[k + left], stay = upper ? by[k + left] : by[k];
+          by[k] = stay + __shfl_xor_sync(~0u, send, m);
+        }
+      }
 #pragma unroll
-      for (int k = 0; k < kRotaryBatch; ++k) by[k] = rsqrtf(fmaf(by[k], p.inverse_dim, p.eps));
+      for (int m = kLanes / (2 * kRotaryBatch); m; m >>= 1) by[0] += __shfl_xor_sync(~0u, by[0], m);
+      const float mine = rsqrtf(fmaf(by[0], p.inverse_dim, p.eps));
+#pragma unroll
+      for (int k = 0; k < kRotaryBatch; ++k) by[k] = __shfl_sync(~0u, mine, sub * kLanes + k * (kLanes / kRotaryBatch));
     }
 #pragma unroll
     for (int k = 0; k < kRotaryBatch; ++k) {
@@ -185,13 +196,13 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
   uint8_t* cache = v.base + (row == kNoRow ? 0 : row) * v.row_bytes + sub * v.head_bytes + vec * kCacheVec;
   bool q_made = false, k_made = false;
   for (; u < units; u += p.parts) {
-    if (u + p.parts < units) load(u + p.parts, next);
     if (u < q_units) {
       if (!q_made) factors(p.q_weight), q_made = true;
       const int32_t h0 = u * kEach, rest = used ? p.q_heads - h0 - sub : 0;
       float2 x[kRotaryBatch][4];
 #pragma unroll
       for (int k = 0; k < kRotaryBatch; ++k) unpack(raw[k], x[k]);
+      load(u + p.parts);
       turn_rows(x, p.q_weight != nullptr, q_at + h0 * p.q_head, p.q_head, rest);
       uint8_t* to = p.q_out + token * p.out_token + (h0 + sub) * p.out_head + vec * 16;
 #pragma unroll
@@ -203,6 +214,7 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
       float2 x[kRotaryBatch][4];
 #pragma unroll
       for (int k = 0; k < kRotaryBatch; ++k) unpack(raw[k], x[k]);
+      load(u + p.parts);
       turn_rows(x, p.k_weight != nullptr, k_at + h0 * a.key_head, a.key_head, rest);
       uint8_t* to = cache + h0 * v.head_bytes;
 #pragma unroll
@@ -222,9 +234,8 @@ __global__ void __launch_bounds__(kRotaryThreads, 2) rotary_kernel(const __grid_
           *reinterpret_cast<uint4*>(to) = raw[k];
         }
       }
+      load(u + p.parts);
     }
-#pragma unroll
-    for (int k = 0; k < kRotaryBatch; ++k) raw[k] = next[k];
   }
 }
 
