@@ -6,7 +6,7 @@
 // row's elements that x is paired with, every element is  by (x c + y s)  with by the row's norm and factors c = w cos t
 // and s = +-w' sin t that all heads of a token share: they are made once for the queries and once for the keys.  y is the
 // neighbour's place in the lane for neighbouring pairs; else another lane's whole vector where half of rotary_dim
-// is a multiple of 8 (four shuffles of raw pairs); elsewhere it is read again, element by element.
+// is a multiple of 8 (eight shuffles); elsewhere it is read again, element by element.
 //
 // Angles: a position of 2^20 times a frequency has 2^-4 left of a 32-bit product's 24 bits, so turns are taken in 64-bit
 // whole numbers: f / 2 pi in units of 2^-64, times the position, of which the whole turns overflow.  Sine and cosine are

@@ -1027,7 +1027,8 @@ def kv_select(ctx, pool: KvPool, batch: KvBatch, bounds: KvBounds, selection: Kv
     _need(selected, "selected", "int32", (tokens, pool.num_heads, selection.budget))
     _check_tensor(selected, "selected")
     c = _pack_selection(_type_of(query.dtype), *selection._fields, qs[0], qs[1])
-    _check(_lib.kv_select(ctx, _byref(pool._c), _byref(batch._c), bounds._of(pool), c, query.data_ptr(), selected.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_select")
+    _check(_lib.kv_select(ctx, _byref(pool._c), _byref(batch._c), bounds._of(pool), c, query.data_ptr(), selected.data_ptr(),
+                          workspace.data_ptr(), workspace.numel(), _stream_handle(stream)), "kv_select")
 
 
 def kv_attend_selected_workspace(ctx, pool: KvPool, batch: KvBatch, attention: KvAttention, budget: int, dtype=None):
