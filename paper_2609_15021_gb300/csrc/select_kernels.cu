@@ -59,11 +59,13 @@ struct Divisor {
   }
 };
 
-// A warp has one head of one page: its lanes have a row's vectors, some rows at once, and meet at the end, after which, where
-// a row is half a warp, one half makes the low bounds and the other the high ones.  C: the type that keys are compared in
-// (fp16 for e4m3).  Bound by the keys' bytes, of which a lane has eight rows' in flight: 2 sequences of 21k and 32.8k tokens, 8 heads x
-// 128, bf16 (117 MB with the bounds): 24 us, 72 % of the DRAM's rate (in a graph 27, and 29 where a page's loads were not all made first).  After a step's append
-// it has a page a sequence, and takes the 5 us that a launch and four loads on end take.
+// A warp has one head of two pages, one after the other, whose places are looked up at once: its lanes have a row's vectors, some
+// rows at once, and meet at the end, the second page's rows under way; then, where a row is half a warp, one half makes the low
+// bounds and the other the high ones.  C: the type that keys are compared in
+// (fp16 for e4m3).  Bound by the keys' bytes, of which a lane has eight rows' in
+// flight: 2 sequences of 21k and 32.8k tokens, 8 heads x 128, bf16 (117 MB with the bounds): 21 us, 83 % of the DRAM's rate (in a graph 23; 27 with one page a
+// warp, 29 where a page's loads were not all made first).  After a step's append it has a page a sequence, and takes the 5 us
+// that a launch and four loads on end take.
 template <class C, bool kWide, int kVecs>  // kVecs: vectors of a row, rounded up to a power of two
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsParams p) {
   wait_for_previous();
@@ -73,88 +75,104 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
   const int lane = threadIdx.x & 31, vec = lane % kVecs, sub = lane / kVecs;
   const int32_t s = blockIdx.y, unit = (int32_t)blockIdx.x * (kBoundsThreads / 32) + (threadIdx.x >> 5);
   const int32_t n = (int32_t)quotient(p.by_heads, (uint32_t)unit), h = unit - n * v.heads;
-  if (n >= p.pages_each) return;
   if (unit == 0 && lane == 0) check_length(v, s);
   const int32_t length = length_of(v, s), block = (int32_t)v.by_block.d;
-  const int32_t first = (int32_t)quotient(v.by_block, (uint32_t)max(length - p.new_tokens, 0)), page = first + n;
-  if ((int64_t)page * block >= length) return;
-  const int32_t held = min(block, length - page * block);
-  const uint32_t row = row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)page * block);
-  if (row == kNoRow) return;
-  const uint32_t number = row / v.page_rows;
-  const uint8_t* from = v.base + row * v.row_bytes + h * v.head_bytes + vec * 16;
+  const int32_t page = (int32_t)quotient(v.by_block, (uint32_t)max(length - p.new_tokens, 0)) + 2 * n;  // and the next
+  uint32_t row[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    row[j] = 2 * n + j < p.pages_each && (int64_t)(page + j) * block < length
+                 ? row_index(v, v.tables + s * v.table_stride, v.table_len, (uint32_t)(page + j) * block)
+                 : kNoRow;
   const int64_t step = v.token_rows * v.row_bytes;
   const bool used = vec * 16 < v.row_bytes;
-  constexpr uint32_t kInf = std::is_same<C, Bf16>::value ? 0x7F807F80u : 0x7C007C00u;
-  uint32_t low[kPairs], high[kPairs];
-#pragma unroll
-  for (int k = 0; k < kPairs; ++k) low[k] = used ? kInf : 0, high[k] = used ? kInf | 0x80008000u : 0;
   constexpr int kAtOnce = 8;  // loads in flight
-  if (used)
-    for (int32_t t0 = sub; t0 < held; t0 += kAtOnce * kRows) {
-      uint4 x[kAtOnce];
+  uint4 x[kAtOnce];
+  auto load = [&](int j, int32_t t0) {
+    const uint32_t at = j ? row[1] : row[0];
+    if (at == kNoRow || !used) return;
+    const uint8_t* from = v.base + at * v.row_bytes + h * v.head_bytes + vec * 16;
+    const int32_t held = min(block, length - (page + j) * block);
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + min(t0 + i * kRows, held - 1) * step));
+    for (int i = 0; i < kAtOnce; ++i) x[i] = __ldcs(reinterpret_cast<const uint4*>(from + min(t0 + i * kRows, held - 1) * step));
+  };
+  load(0, sub);
+  constexpr int kUnrolled = kWide ? 1 : 2;  // (e4m3's code twice took 5 us more where a sequence has one page)
+#pragma unroll kUnrolled
+  for (int j = 0; j < 2; ++j) {
+    const uint32_t here = j ? row[1] : row[0];
+    constexpr uint32_t kInf = std::is_same<C, Bf16>::value ? 0x7F807F80u : 0x7C007C00u;
+    uint32_t low[kPairs], high[kPairs];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    for (int k = 0; k < kPairs; ++k) low[k] = used ? kInf : 0, high[k] = used ? kInf | 0x80008000u : 0;
+    if (here != kNoRow && used)
+      for (int32_t t0 = sub;;) {
 #pragma unroll
-        for (int k = 0; k < kPairs; ++k) {
-          const uint32_t u = kWide ? widen2(w[k / 2] >> k % 2 * 16) : w[k];
-          low[k] = least2<C>(low[k], u), high[k] = most2<C>(high[k], u);
+        for (int i = 0; i < kAtOnce; ++i) {
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+          for (int k = 0; k < kPairs; ++k) {
+            const uint32_t u = kWide ? widen2(w[k / 2] >> k % 2 * 16) : w[k];
+            low[k] = least2<C>(low[k], u), high[k] = most2<C>(high[k], u);
+          }
         }
+        t0 += kAtOnce * kRows;
+        if (t0 >= min(block, length - (page + j) * block)) break;
+        load(j, t0);
       }
-    }
-  __syncwarp();
+    if (j == 0) load(1, sub);
+    if (here == kNoRow) continue;
+    __syncwarp();
 #pragma unroll
-  for (int m = kVecs; m < 32; m <<= 1)
+    for (int m = kVecs; m < 32; m <<= 1)
 #pragma unroll
-    for (int k = 0; k < kPairs; ++k) {
-      low[k] = least2<C>(low[k], __shfl_xor_sync(~0u, low[k], m));
-      high[k] = most2<C>(high[k], __shfl_xor_sync(~0u, high[k], m));
-    }
-  uint32_t most = 0, carries = 0;  // of both numbers' magnitudes, as their bits are in order
-#pragma unroll
-  for (int k = 0; k < kPairs; ++k) {
-    carries |= odd_carry<C>(low[k]) | odd_carry<C>(high[k]);
-    most = __vmaxu2(most, __vmaxu2(low[k] & 0x7FFF7FFFu, high[k] & 0x7FFF7FFFu));
-  }
-  const bool odd = __any_sync(~0u, odd_carried(carries));
-  most = __reduce_max_sync(~0u, max(most & 0xFFFFu, most >> 16));
-  const float size = odd ? FLT_MAX : __fdiv_rn(unpack2<C>(most).x, 127.f);
-  const int64_t at = (int64_t)number * v.heads + h;
-  if (lane == 0) p.sizes[at] = size;
-  if (!used || sub > 1) return;
-  const Divisor by(size);
-  const bool both = kRows == 1;
-#pragma unroll
-  for (int side = 0; side < 2; ++side) {
-    if (!both && side != sub) continue;
-    uint32_t out[kPairs / 2];
+      for (int k = 0; k < kPairs; ++k) {
+        low[k] = least2<C>(low[k], __shfl_xor_sync(~0u, low[k], m));
+        high[k] = most2<C>(high[k], __shfl_xor_sync(~0u, high[k], m));
+      }
+    uint32_t most = 0, carries = 0;  // of both numbers' magnitudes, as their bits are in order
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
-      const float2 x = unpack2<C>(side ? high[k] : low[k]);
-      float2 r = make_float2(by(x.x), by(x.y));
-      r = side ? make_float2(ceilf(r.x), ceilf(r.y)) : make_float2(floorf(r.x), floorf(r.y));
-      const int32_t a = (int32_t)fminf(fmaxf(r.x, -127.f), 127.f), b = (int32_t)fminf(fmaxf(r.y, -127.f), 127.f);
-      const uint32_t pair = (uint32_t)(a & 0xFF) | (uint32_t)(b & 0xFF) << 8;
-      out[k / 2] = k % 2 ? out[k / 2] | pair << 16 : pair;
+      carries |= odd_carry<C>(low[k]) | odd_carry<C>(high[k]);
+      most = __vmaxu2(most, __vmaxu2(low[k] & 0x7FFF7FFFu, high[k] & 0x7FFF7FFFu));
     }
-    if (odd)
+    const bool odd = __any_sync(~0u, odd_carried(carries));
+    most = __reduce_max_sync(~0u, max(most & 0xFFFFu, most >> 16));
+    const float size = odd ? FLT_MAX : __fdiv_rn(unpack2<C>(most).x, 127.f);
+    const int64_t at = (int64_t)(here / v.page_rows) * v.heads + h;
+    if (lane == 0) p.sizes[at] = size;
+    if (!used || sub > 1) continue;
+    const Divisor by(size);
+    const bool both = kRows == 1;
 #pragma unroll
-      for (int k = 0; k < kPairs / 2; ++k) out[k] = side ? 0x7F7F7F7Fu : 0x81818181u;
-    int8_t* to = p.boxes + at * 2 * v.head_dim + side * v.head_dim + vec * 2 * kPairs;
-    if constexpr (kWide)
-      *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
-    else
-      *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
+    for (int side = 0; side < 2; ++side) {
+      if (!both && side != sub) continue;
+      uint32_t out[kPairs / 2];
+#pragma unroll
+      for (int k = 0; k < kPairs; ++k) {
+        const float2 y = unpack2<C>(side ? high[k] : low[k]);
+        float2 r = make_float2(by(y.x), by(y.y));
+        r = side ? make_float2(ceilf(r.x), ceilf(r.y)) : make_float2(floorf(r.x), floorf(r.y));
+        const int32_t a = (int32_t)fminf(fmaxf(r.x, -127.f), 127.f), b = (int32_t)fminf(fmaxf(r.y, -127.f), 127.f);
+        const uint32_t pair = (uint32_t)(a & 0xFF) | (uint32_t)(b & 0xFF) << 8;
+        out[k / 2] = k % 2 ? out[k / 2] | pair << 16 : pair;
+      }
+      if (odd)
+#pragma unroll
+        for (int k = 0; k < kPairs / 2; ++k) out[k] = side ? 0x7F7F7F7Fu : 0x81818181u;
+      int8_t* to = p.boxes + at * 2 * v.head_dim + side * v.head_dim + vec * 2 * kPairs;
+      if constexpr (kWide)
+        *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
+      else
+        *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
+    }
   }
 }
 
 template <class C, bool kWide>
 cudaError_t bounds(const BoundsParams& p, cudaStream_t s) {
   constexpr int kWarps = kBoundsThreads / 32;
-  const dim3 grid((unsigned)(((int64_t)p.pages_each * p.pages.heads + kWarps - 1) / kWarps), p.pages.num_seqs);
+  const dim3 grid((unsigned)((((int64_t)p.pages_each + 1) / 2 * p.pages.heads + kWarps - 1) / kWarps), p.pages.num_seqs);
   const int64_t vecs = p.pages.row_bytes / 16;
   auto kernel = vecs <= 4 ? bounds_kernel<C, kWide, 4> : vecs <= 8 ? bounds_kernel<C, kWide, 8> : vecs <= 16 ? bounds_kernel<C, kWide, 16> : bounds_kernel<C, kWide, 32>;
   return launch_after(kernel, grid, kBoundsThreads, 0, s, p);
