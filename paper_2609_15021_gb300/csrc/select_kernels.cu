@@ -246,8 +246,9 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
     if (there[k]) size[k] = p.sizes[at];
   }
 
-  // Rows of queries, four vectors of 16 bytes in flight: one row a vector, 8 elements a lane.
-  constexpr int kAtOnce = 4, kWarps = kScoreThreads / 32;
+  // Rows of queries, two vectors of 16 bytes in flight: one row a vector, 8 elements a lane (most heads have one or two rows
+  // a warp; four in flight are no faster).
+  constexpr int kAtOnce = 2, kWarps = kScoreThreads / 32;
   const bool used = lane * 8 < v.head_dim;
   for (int32_t r0 = warp; r0 < tiles * 8; r0 += kAtOnce * kWarps) {
     uint4 raw[kAtOnce];
@@ -347,6 +348,7 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
 
 constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
 constexpr int kPickBins = 2048;
+static_assert(kPickBins == 4 * kPickThreads && kPickWarps <= 32, "a thread has four ranges, a lane a warp's sum");
 
 // Whole numbers in the order of the scores: NaN as -inf, -0 as +0.  None is 0.
 __device__ __forceinline__ uint32_t score_rank(float w) {
