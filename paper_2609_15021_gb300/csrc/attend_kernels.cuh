@@ -35,7 +35,9 @@
 // a bf16 value is lost within 2^-24 of the row's largest.  Probabilities are rounded to the
 // cache's type (fp16 for e4m3) for the product with V; the sums they are divided by are not.  That is 2^-9 of a term, of
 // either sign: in bf16 an output is off by some 2.1e-3 where its own rounding gives 1.6e-3, and a second part of each
-// probability would take the product twice.
+// probability would take the product twice.  Over selected pages of 16-bit caches the sums are divided by what the rounded probabilities
+// add up to (a part is scaled by the true sum over that, so that parts join and logarithms stay as they are): a row
+// that one key dominates, as such pages are picked for, then has that key's error cancelled.
 //
 // Measured: bf16, sequences of 21k and 32.8k tokens, 8 heads x 128 with 8 query rows each, weights kept (220 MB of
 // K/V): 45 us; fp16, 45 sequences of up to 16k tokens, 8 heads x 96 with 2 rows, cap and slopes (270 MB): 60 us; both
@@ -165,6 +167,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
     attend_kernel(const __grid_constant__ AttendParams p) {
   using S = AttendShape<C, kDim, kTiles>;
   constexpr bool kWide = S::kElem == 1;  // cache to be widened
+  constexpr bool kExactMean = kSelected && !kWide;
   constexpr int kKs = kDim / 16, kRows = S::kRows, kBlocks = S::kBlocks, kStep = S::kStep;
   constexpr int kWarps = S::kWarps, kAttendThreads = S::kThreads;
   constexpr uint32_t kAllKeys = kStep == 32 ? ~0u : 0xFFFFu;
@@ -453,6 +456,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         for (int e = 0; e < 4; ++e) acc[c][t][e] = 0.f;
     // rows 2 sub and 2 sub + 1 of each tile: what exponents are relative to, and the sums over this lane's keys
     float m[kTiles][2], l[kTiles][2], scale2[kTiles][2];
+    float rounded[kTiles][2] = {};  // kExactMean: what rounding added to the probabilities
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -579,11 +583,13 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
             const float keep = factor(m[t][j], top);
             m[t][j] = top;
             l[t][j] *= keep;
+            if constexpr (kExactMean) rounded[t][j] *= keep;
 #pragma unroll
             for (int c = 0; c < kKs; ++c) acc[c][t][j] *= keep, acc[c][t][2 + j] *= keep;
           }
       }
       uint32_t pf[kBlocks][kTiles][2];
+      float added[kTiles][2] = {};
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
@@ -594,8 +600,15 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
             sc[n][t][e] = ex2(sc[n][t][e] - ref[e & 1]);
             l[t][e & 1] += sc[n][t][e];
           }
-          pf[n][t][0] = transpose(pack2<C>(sc[n][t][0], sc[n][t][1]));
-          pf[n][t][1] = transpose(pack2<C>(sc[n][t][2], sc[n][t][3]));
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t pair = pack2<C>(sc[n][t][2 * k], sc[n][t][2 * k + 1]);
+            if constexpr (kExactMean) {
+              const float2 x = unpack2<C>(pair);
+              added[t][0] += x.x - sc[n][t][2 * k], added[t][1] += x.y - sc[n][t][2 * k + 1];
+            }
+            pf[n][t][k] = transpose(pair);
+          }
         }
       }
 
@@ -618,6 +631,10 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         odd = __any_sync(~0u, odd);
       }
       if (!odd) {
+        if constexpr (kExactMean) {
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) rounded[t][0] += added[t][0], rounded[t][1] += added[t][1];
+        }
 #pragma unroll
         for (int c = 0; c < kKs; c += kWide ? 2 : 1) {
 #pragma unroll
@@ -694,6 +711,11 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
       for (int j = 0; j < 2; ++j) {
         const int r = t * 8 + 2 * sub + j;
         const float sum = column_sum(l[t][j]);
+        if constexpr (kExactMean) {
+          const float taken = sum + column_sum(rounded[t][j]), by = taken > 0.f ? sum / taken : 1.f;
+#pragma unroll
+          for (int c = 0; c < kKs; ++c) acc[c][t][j] *= by, acc[c][t][2 + j] *= by;
+        }
         if (r >= here) continue;
         if (quad == 0) {
           stats[2 * (warp * kRows + r)] = m[t][j];

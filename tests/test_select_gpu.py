@@ -291,6 +291,25 @@ def test_attend_selected(ctx, dtype, cache, nhd, dim):
     check_attend(ctx, case, normal((len(LENGTHS), 6, dim), dtype, 15), some_pages(case, 1, 3, 16), **scales)
 
 
+@pytest.mark.parametrize("dtype", [BF16, FP16])
+def test_a_key_that_dominates_gives_its_value(ctx, dtype):
+    """Its probability's rounding cancels: the mean is its value, of the type already, but for the others' weights, of
+    1e-7 at most, and what 32 bits leave of 64 values below 5: 2^-21 of these."""
+    case = Case([64, 64, 64], dtype=dtype, seed=23)
+    keys = torch.stack([case.pages.rows(0, case.tables[s], range(64)) for s in range(3)]).double()  # [seq][2][token][head][dim]
+    at = torch.tensor([5, 31, 62])
+    chosen = keys[torch.arange(3), :, at]  # [seq][2][head][dim]
+    q = (chosen[:, 0].repeat_interleave(3, 1) * torch.tensor([7.0, 8.1, 9.7, 7.3, 11.0, 8.9])[:, None]).to(dtype)
+    scores = torch.einsum("shd,sthd->sht", q.double(), keys[:, 0].repeat_interleave(3, 2)) / 8
+    weights = scores.softmax(-1)
+    assert bool((weights.gather(-1, at[:, None, None].expand(3, 6, 1)) > 1 - 1e-7).all())
+    selected = torch.arange(4, dtype=torch.int32).expand(3, 2, 4).contiguous()
+    out, _ = attend(ctx, case, q, selected, 1)
+    want = chosen[:, 1].repeat_interleave(3, 1)
+    assert float(want.abs().max()) < 5
+    assert bool(((out.cpu().double() - want).abs() <= 5e-7 + 5 * 2.0 ** -21).all())
+
+
 @pytest.mark.parametrize("cache", [BF16, FP16, E4M3])
 @pytest.mark.parametrize("dim,group,new", [(64, 1, 5), (64, 9, 2), (128, 8, 3), (128, 17, 1), (128, 40, 2), (256, 6, 4), (256, 20, 1), (96, 33, 1)])
 def test_many_query_rows_and_new_tokens(ctx, cache, dim, group, new):
