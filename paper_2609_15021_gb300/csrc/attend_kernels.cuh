@@ -35,7 +35,7 @@
 // a bf16 value is lost within 2^-24 of the row's largest.  Probabilities are rounded to the
 // cache's type (fp16 for e4m3) for the product with V; the sums they are divided by are not.  That is 2^-9 of a term, of
 // either sign: in bf16 an output is off by some 2.1e-3 where its own rounding gives 1.6e-3, and a second part of each
-// probability would take the product twice.  Over selected pages of 16-bit caches the sums are divided by what the rounded probabilities
+// probability would take the product twice.  Over selected pages the sums are divided by what the rounded probabilities
 // add up to (a part is scaled by the true sum over that, so that parts join and logarithms stay as they are): a row
 // that one key dominates, as such pages are picked for, then has that key's error cancelled.
 //
@@ -167,7 +167,6 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
     attend_kernel(const __grid_constant__ AttendParams p) {
   using S = AttendShape<C, kDim, kTiles>;
   constexpr bool kWide = S::kElem == 1;  // cache to be widened
-  constexpr bool kExactMean = kSelected && !kWide;
   constexpr int kKs = kDim / 16, kRows = S::kRows, kBlocks = S::kBlocks, kStep = S::kStep;
   constexpr int kWarps = S::kWarps, kAttendThreads = S::kThreads;
   constexpr uint32_t kAllKeys = kStep == 32 ? ~0u : 0xFFFFu;
@@ -456,7 +455,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         for (int e = 0; e < 4; ++e) acc[c][t][e] = 0.f;
     // rows 2 sub and 2 sub + 1 of each tile: what exponents are relative to, and the sums over this lane's keys
     float m[kTiles][2], l[kTiles][2], scale2[kTiles][2];
-    float rounded[kTiles][2] = {};  // kExactMean: what rounding added to the probabilities
+    float rounded[kTiles][2] = {};  // kSelected: what rounding added to the probabilities
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -583,7 +582,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
             const float keep = factor(m[t][j], top);
             m[t][j] = top;
             l[t][j] *= keep;
-            if constexpr (kExactMean) rounded[t][j] *= keep;
+            if constexpr (kSelected) rounded[t][j] *= keep;
 #pragma unroll
             for (int c = 0; c < kKs; ++c) acc[c][t][j] *= keep, acc[c][t][2 + j] *= keep;
           }
@@ -603,7 +602,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const uint32_t pair = pack2<C>(sc[n][t][2 * k], sc[n][t][2 * k + 1]);
-            if constexpr (kExactMean) {
+            if constexpr (kSelected) {
               const float2 x = unpack2<C>(pair);
               added[t][0] += x.x - sc[n][t][2 * k], added[t][1] += x.y - sc[n][t][2 * k + 1];
             }
@@ -631,7 +630,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         odd = __any_sync(~0u, odd);
       }
       if (!odd) {
-        if constexpr (kExactMean) {
+        if constexpr (kSelected) {
 #pragma unroll
           for (int t = 0; t < kTiles; ++t) rounded[t][0] += added[t][0], rounded[t][1] += added[t][1];
         }
@@ -711,7 +710,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
       for (int j = 0; j < 2; ++j) {
         const int r = t * 8 + 2 * sub + j;
         const float sum = column_sum(l[t][j]);
-        if constexpr (kExactMean) {
+        if constexpr (kSelected) {
           const float taken = sum + column_sum(rounded[t][j]), by = taken > 0.f ? sum / taken : 1.f;
 #pragma unroll
           for (int c = 0; c < kKs; ++c) acc[c][t][j] *= by, acc[c][t][2 + j] *= by;

@@ -291,12 +291,12 @@ def test_attend_selected(ctx, dtype, cache, nhd, dim):
     check_attend(ctx, case, normal((len(LENGTHS), 6, dim), dtype, 15), some_pages(case, 1, 3, 16), **scales)
 
 
-@pytest.mark.parametrize("dtype", [BF16, FP16])
-def test_a_key_that_dominates_gives_its_value(ctx, dtype):
+@pytest.mark.parametrize("dtype,cache", [(BF16, BF16), (FP16, FP16), (BF16, E4M3), (FP16, E4M3)])
+def test_a_key_that_dominates_gives_its_value(ctx, dtype, cache):
     """Its probability's rounding cancels: the mean is its value, of the type already, but for the others' weights, of
     1e-7 at most, and what 32 bits leave of 64 values below 5: 2^-21 of these."""
-    case = Case([64, 64, 64], dtype=dtype, seed=23)
-    keys = torch.stack([case.pages.rows(0, case.tables[s], range(64)) for s in range(3)]).double()  # [seq][2][token][head][dim]
+    case = Case([64, 64, 64], dtype=cache, seed=23)
+    keys = torch.stack([case.pages.rows(0, case.tables[s], range(64)).float() for s in range(3)]).double()  # [seq][2][token][head][dim]
     at = torch.tensor([5, 31, 62])
     chosen = keys[torch.arange(3), :, at]  # [seq][2][head][dim]
     q = (chosen[:, 0].repeat_interleave(3, 1) * torch.tensor([7.0, 8.1, 9.7, 7.3, 11.0, 8.9])[:, None]).to(dtype)
