@@ -649,7 +649,8 @@ const char* kv_last_error_message(void);
  * "delta_wait": the (after_calls + 1)-th next kv_state_delta that goes by chunks
  * makes no copies for any sequence's second one, so the wait for them runs out:
  * that sequence's output is incomplete, its state is not written and
- * kv_get_device_error returns KVX_ETIMEOUT.
+ * kv_get_device_error returns KVX_ETIMEOUT.  "delta_wait_m": the same with what the
+ * first chunk's outputs alone wait for.
  * "tier_exit" ends the process (_exit(3)) inside
  * kv_tier_reserve, while it holds a shared tier's table lock, right after it
  * has taken a slot for the new key; it tests how the processes left recover

@@ -538,19 +538,26 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
 
   auto load_stage = [&](int32_t i) {  // by one thread
     const uint32_t bar = bars + 8 * (i & 1), to = base + (i & 1) * W::kStage;
-    if (i >= chunks || (p.stall && i == 1)) return;
+    if (i >= chunks || (p.stall == 1 && i == 1)) return;
     bar_expect(bar, W::kStage);
     bulk_load(to, p.rows_space + ((int64_t)(first + i) * p.groups + group) * 2 * kRowBytes<N>, 2 * kRowBytes<N>, bar);
     bulk_load(to + 2 * kRowBytes<N>, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes, kFactors + 2 * kTriangle, bar);
   };
   auto load_m = [&](int32_t i) {
     constexpr int kBytes = kPartsOfM<E> * kTriangle;
+    if (p.stall == 2 && i == 0) return;
     bar_expect(bars + 16, kBytes);
     bulk_load(base + W::kM, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes + kFactors + 2 * kTriangle, kBytes, bars + 16);
   };
   auto factors_of = [&](int32_t i) -> const Factors& { return *reinterpret_cast<const Factors*>(smem + (i & 1) * W::kStage + 2 * kRowBytes<N>); };
   constexpr uint32_t kOdd = 1, kDead = 2;
   bool dead = false;
+  // M's wait, by the warps of the outputs: where it runs out all warps end before the next chunk, as no copy may follow one that is
+  // on its way.
+  auto wait_for_m = [&](int32_t i) {
+    dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+    if (dead) atomicOr(&flags_s[(i + 1) & 1], kDead);
+  };
   float2* state_by = reinterpret_cast<float2*>(smem + W::kStateBy);
   float2* rhs_by = reinterpret_cast<float2*>(smem + W::kRhsBy);
   float2* plain_by = reinterpret_cast<float2*>(smem + W::kPlainBy);
@@ -646,7 +653,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         meet<256>(kEight);
         if (threadIdx.x == 128) flags_s[i & 1] = 0;
         by_tokens(t0);
-        dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+        wait_for_m(i);
         meet<256>(kEight);
         continue;
       }
@@ -661,7 +668,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
           by[u][e] = f.by[warp * 16 + 8 * u + 2 * c + e].w;
           m_by[u][e] = f.row[warp * 16 + 8 * u + 2 * c + e];
         }
-      dead = dead || !bar_wait(bars + 16, i & 1, p.wait_cycles);
+      wait_for_m(i);
       meet<256>(kWThere);  // S has been read
       // y = e^c S q + M w
       float mw[2][4] = {};
@@ -885,8 +892,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     if (threadIdx.x == 256) {
       *p.timeout = 1;
       // copies may still be on their way: their end, however short the waits' limit is
-      if (i < chunks && !(p.stall && i == 1)) bar_wait(bars + 8 * (i & 1), i >> 1 & 1, kDefaultWaitCycles);
-      if (i > 0) bar_wait(bars + 16, (i - 1) & 1, kDefaultWaitCycles);
+      if (i < chunks && !(p.stall == 1 && i == 1)) bar_wait(bars + 8 * (i & 1), i >> 1 & 1, kDefaultWaitCycles);
+      if (i > 0 && !(p.stall == 2 && i == 1)) bar_wait(bars + 16, (i - 1) & 1, kDefaultWaitCycles);
     }
     __syncthreads();
     return;

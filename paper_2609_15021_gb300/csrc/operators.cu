@@ -926,7 +926,7 @@ kvx_status kv_state_delta(kvx_ctx* c, const kvx_state* state, const kvx_state_ba
     p.head_space = (uint8_t*)workspace + space.heads;
     p.wait_cycles = ctx.wait_cycles;
     p.timeout = ctx.timeout;
-    p.stall = p.pieces && fault_point("delta_wait");
+    p.stall = !p.pieces ? 0 : fault_point("delta_wait") ? 1 : fault_point("delta_wait_m") ? 2 : 0;
     p.q = (const uint8_t*)q;
     p.k = (const uint8_t*)k;
     p.v = (const uint8_t*)v;

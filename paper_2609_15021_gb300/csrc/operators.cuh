@@ -202,7 +202,7 @@ struct DeltaParams {
   uint8_t* head_space;       // and what else a chunk and head has
   long long wait_cycles;     // limit of a wait for a copy
   int* timeout;              // set when one ran out
-  bool stall;                // fault point "delta_wait": the second chunk's copies are not made
+  int32_t stall;             // fault points: 1, "delta_wait", the second chunk's copies are not made; 2, "delta_wait_m", the first one's M is not
 };
 constexpr int32_t kDeltaChunk = 64, kDeltaHeadBytes = 21888;  // tokens; bytes of head_space
 // Whether a batch's sequences go by chunks, and which do not (*by_token).

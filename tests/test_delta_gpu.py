@@ -372,6 +372,41 @@ def test_wait_for_a_copy_runs_out_then_recovery():
         k.kv_ctx_destroy(c)
 
 
+@pytest.mark.parametrize("t, odd", [(200, False), (50, False), (200, True)])
+def test_wait_for_what_the_outputs_take_runs_out_then_recovery(t, odd):
+    """The first chunk's factors of the outputs are left out, by chunks and token by token, of several chunks and of one: every
+    warp ends before the next chunk's are asked for, no state is written, and the next call gives what the first gave."""
+    k = kvx()
+    c = k.kv_ctx_create(0, wait_cycles=2_000_000)
+    try:
+        heads, p, n = 2, 64, 64
+        data = Inputs(t, heads, p, n, 1, BF16)
+        x, A = data.cuda(), data.A.cuda()
+        if odd:
+            x["value"][5, 0, 3] = math.inf
+        batch, _ = batch_of([t], [0], [1])
+        outs = []
+        for point in (None, "delta_wait_m", None):
+            st = Slots(2, heads, p, n)
+            out = torch.zeros((t, heads, p), dtype=BF16, device="cuda")
+            if point:
+                k.kv_fault_inject(point)
+            k.kv_state_delta(c, st.slots, batch, out=out, A=A, workspace=k.kv_state_delta_workspace(c, batch, heads, p, n), **x)
+            torch.cuda.synchronize()
+            if point:
+                assert torch.equal(st.dev.cpu(), st.cpu)
+                assert not bool(out[64:].any())  # chunks that were not begun
+                with pytest.raises(k.KvxError) as e:
+                    k.kv_get_device_error(c)
+                assert e.value.status == k.KVX_ETIMEOUT
+            else:
+                outs.append((out.view(torch.int16), st.dev))
+                assert k.kv_get_device_error(c) == -1
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+    finally:
+        k.kv_ctx_destroy(c)
+
+
 def test_captured_step(ctx):
     """Replayed with other slots, starts and freshness, on a workspace that calls in between have used."""
     k = kvx()
