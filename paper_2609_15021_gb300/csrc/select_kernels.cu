@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "mma.cuh"
+#include "pick_border.cuh"
 
 namespace kvx {
 namespace {
@@ -347,7 +348,6 @@ __global__ void __launch_bounds__(kScoreThreads) score_kernel(const __grid_const
 // ---------------------------------------------------------------- the best
 
 constexpr int kPickThreads = 512, kPickWarps = kPickThreads / 32;
-constexpr int kPickBins = 2048;
 static_assert(kPickBins == 4 * kPickThreads && kPickWarps <= 32, "a thread has four ranges, a lane a warp's sum");
 
 // Whole numbers in the order of the scores: NaN as -inf, -0 as +0.  None is 0.
@@ -416,12 +416,11 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
   for (int32_t i = threadIdx.x; i < kPickBins; i += kPickThreads) hist[i] = 0;
   __syncthreads();
   low = __reduce_min_sync(~0u, warp_a[lane % kPickWarps]), high = __reduce_max_sync(~0u, warp_b[lane % kPickWarps]);
-  int32_t want = keep - min(p.sinks + p.recent, n);  // of those picked by their scores, which are more than that
-  uint32_t border = UINT32_MAX;  // ranks above it are picked, and the first `equal` of those that have it
-  int32_t equal = 0;
-  if (want > 0) {
-    for (;;) {
-      const int shift = max(0, 21 - __clz(high - low));  // (high - low) >> shift is below 2^11
+  Border search = {low, high, keep - min(p.sinks + p.recent, n)};  // of those picked by their scores, which are more than that
+  if (search.want > 0) {
+    for (int pass = 0; pass < kPickPasses; ++pass) {
+      const int shift = search.shift();
+      low = search.low, high = search.high;
       for_each([&](int32_t, uint32_t r) {
         if (r >= low && r <= high) atomicAdd(&hist[(r - low) >> shift], 1);
       });
@@ -435,26 +434,22 @@ __global__ void __launch_bounds__(kPickThreads) pick_kernel(const __grid_constan
       for (int k = 0; k < 4; ++k) hist[top_bin - k] = 0;
       const int32_t upto = (int32_t)upto_lane(sum);
       if (lane == 31) warp_a[warp] = upto;
+      if (threadIdx.x == 0) want_s = 0;  // of the range that one thread names, if any does
       __syncthreads();
       const uint32_t mine = lane < kPickWarps && lane < warp ? warp_a[lane] : 0;
       const int32_t before = upto - sum + (int32_t)__reduce_add_sync(~0u, mine);
-      int32_t left = want - before;
+      int32_t left = search.want - before;
       if (left > 0 && left <= sum) {  // one thread's
         int k = 0;
         while (left > b[k]) left -= b[k++];
         bin_s = (uint32_t)(top_bin - k), want_s = left, count_s = b[k];
       }
       __syncthreads();
-      low += bin_s << shift;
-      want = want_s;
-      if (shift == 0 || count_s == want) {
-        border = shift == 0 ? low : low - 1;  // low is above 0: 0 is no score's
-        equal = shift == 0 ? want : 0;
-        break;
-      }
-      high = min(high, low + ((1u << shift) - 1));
+      if (!search.narrow(shift, bin_s, want_s, count_s)) break;
     }
   }
+  const uint32_t border = search.rank;
+  const int32_t equal = search.equal;
   // A page's place: those picked in front of it.
   uint32_t above = 0, same = 0;
   for_each([&](int32_t i, uint32_t r) {

@@ -151,3 +151,77 @@ def test_delta_rule_is_its_product_of_matrices():
     for t in range(t_n):
         want = want @ step[t] + b[t] * torch.outer(v[t, 0], unit[t])
     assert torch.allclose(state[0], want, atol=1e-9)
+
+
+SEARCH = r"""
+#include <algorithm>
+#include <cstdio>
+#include <vector>
+#include "pick_border.cuh"
+using namespace kvx;
+static uint64_t state = 12345;
+static uint32_t any() { return (uint32_t)((state = state * 6364136223846793005ull + 1442695040888963407ull) >> 32); }
+#define NEED(x) do { if (!(x)) { printf("line %d: %s\n", __LINE__, #x); return 1; } } while (0)
+
+// The kernel's search; `change` makes other ranks between passes.
+template <class F>
+static int search(std::vector<uint32_t>& ranks, Border& b, F change, int* passes) {
+  bool ended = false;
+  for (*passes = 0; *passes < kPickPasses && !ended; ++*passes) {
+    std::vector<int> counts(kPickBins);
+    const int shift = b.shift();
+    NEED(b.low <= b.high && shift <= 32 - kPickBits);
+    for (uint32_t r : ranks)
+      if (r >= b.low && r <= b.high) {
+        NEED((r - b.low) >> shift < (uint32_t)kPickBins);
+        ++counts[(r - b.low) >> shift];
+      }
+    int bin = kPickBins - 1, left = b.want;
+    while (bin >= 0 && left > counts[bin]) left -= counts[bin--];
+    ended = !b.narrow(shift, bin < 0 ? 0xDEADBEEFu : (uint32_t)bin, bin < 0 ? 0 : left, bin < 0 ? 0x7FFFFFFF : counts[bin]);
+    change();
+  }
+  NEED(ended);
+  return 0;
+}
+
+int main() {
+  const int sizes[] = {1, 2, 5, 100, 4097, 9000};
+  for (int n : sizes)
+    for (uint32_t span : {0u, 1u, 2046u, 2047u, 2048u, 1u << 21, 0xFFFFFFFEu})
+      for (int k = 0; k < 20; ++k) {
+        std::vector<uint32_t> ranks(n);
+        auto make = [&] { const uint32_t base = 1 + any() % (0xFFFFFFFFu - span); for (uint32_t& r : ranks) r = base + (uint32_t)(any() * (uint64_t)span >> 32); };
+        make();
+        std::vector<uint32_t> sorted = ranks;
+        std::sort(sorted.begin(), sorted.end());
+        const int32_t want = 1 + any() % n;
+        int passes;
+        Border b = {sorted.front(), sorted.back(), want};
+        if (search(ranks, b, [] {}, &passes)) return 1;
+        // those above the border and the first `equal` at it are the want largest
+        const uint32_t last = sorted[n - want];
+        const long above = sorted.end() - std::upper_bound(sorted.begin(), sorted.end(), b.rank);
+        NEED(above + b.equal == want && (b.equal ? b.rank == last : b.rank < last));
+        // ranks of other calls between the passes, among them none within what is searched
+        Border other = {sorted.front(), sorted.back(), want};
+        if (search(ranks, other, make, &passes)) return 1;
+        make();
+        Border none = {sorted.front(), sorted.back(), want};
+        if (search(ranks, none, [&] { std::fill(ranks.begin(), ranks.end(), 0u); }, &passes)) return 1;
+        NEED(passes <= kPickPasses);
+      }
+  printf("ok\n");
+}
+"""
+
+
+def test_search_for_the_last_picked_page_ends(tmp_path):
+    """The search's arithmetic as the kernel has it: three passes at most, with the right border where the ranks stay, and an end
+    where another call writes to the workspace between two passes."""
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_15021_gb300", "csrc")
+    src = tmp_path / "search.cpp"
+    src.write_text(SEARCH)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", csrc, str(src), "-o", str(tmp_path / "search")], check=True)
+    done = subprocess.run([str(tmp_path / "search")], capture_output=True, text=True, timeout=60)
+    assert done.returncode == 0 and done.stdout == "ok\n", done.stdout

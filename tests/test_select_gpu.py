@@ -420,6 +420,37 @@ def test_captured_run_follows_lengths_and_tables(ctx):
         assert same_bits(out, got[0]) and torch.equal(picked, got[1])
 
 
+def test_a_workspace_that_another_stream_writes_to(ctx):
+    """Not allowed, and the picked pages are none in particular, but every call ends, writes its lists alone and nothing but places of
+    pages to them; the call that has its workspace to itself again is right.  More pages than a warp's lanes keep."""
+    k = kvx()
+    pages, budget = 20000, 70
+    layer = torch.zeros((pages, 2, 2, 1, 32), dtype=BF16, device="cuda")
+    pool = k.KvPool.from_tensors([layer], 2, 1)
+    bounds = k.KvBounds.for_pool(pool)
+    g = torch.Generator().manual_seed(41)
+    bounds.boxes.copy_(torch.randint(-127, 128, tuple(bounds.boxes.shape), generator=g).to(torch.int8).sort(2).values)
+    bounds.sizes.copy_(torch.rand(tuple(bounds.sizes.shape), generator=g))
+    batch = k.KvBatch(torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1), ints([pages]))
+    sel, q = k.KvSelection(4, budget), normal((1, 4, 32), BF16, 42)
+    dev, space = q.cuda(), k.kv_select_workspace(ctx, pool, batch, sel)
+    room = torch.full((3, 2, budget), -5, dtype=torch.int32, device="cuda")
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(40):
+        with torch.cuda.stream(other):
+            for _ in range(6):
+                space.random_(0, 256)
+        k.kv_select(ctx, pool, batch, bounds, sel, dev, room[1:2], space)
+    torch.cuda.synchronize()
+    assert bool((room[::2] == -5).all()) and bool(((room[1] >= -5) & (room[1] < pages)).all())
+    k.kv_select(ctx, pool, batch, bounds, sel, dev, room[1:2], space)
+    torch.cuda.synchronize()
+    scores = mixers.scores_of(q[0], bounds.boxes.cpu(), bounds.sizes.cpu(), 2)
+    for h in range(2):
+        assert room[1, h].tolist() == mixers.pick(scores[h], pages, budget, 1, 1)
+
+
 def test_same_bits_every_time(ctx):
     case = Case([3000, 1, 900], heads=2)
     q = normal((3, 4, 64), BF16, 32)
