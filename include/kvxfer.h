@@ -811,7 +811,9 @@ typedef struct {
 
 /* Make the bounds of the pages that hold the last new_tokens tokens of every sequence: after an append, or, with as many as
    the longest has, of all its pages after a restore or an eviction into new ones.  elem type: cache_type, KVX_TYPE_*.  They
-   are made from the keys alone, whatever was there.  A page whose table entry is out of range is left out and reported.   */
+   are made from the keys alone, whatever was there: a page that several sequences of the batch hold, at the same
+   place in each, gets those of all keys that any of them holds there; a sequence that holds more of it in another batch, or
+   has it at another place, is not looked at.  A page whose table entry is out of range is left out and reported.   */
 kvx_status kv_bounds(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kvx_batch* batch, int32_t cache_type,
                      int64_t new_tokens, const kvx_bounds* bounds, kvx_stream_t stream);
 

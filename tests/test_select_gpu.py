@@ -128,6 +128,34 @@ def test_bounds_of_odd_keys(ctx, dtype):
     check_bounds(ctx, case, 160)
 
 
+@pytest.mark.parametrize("lengths", [(21, 30, 17, 26), (30, 21, 26, 17), (18, 200, 18, 31), (32, 17, 0, 19)])
+@pytest.mark.parametrize("new,pack,many", [(1, 1, False), (40, 3, False), (1, 1, True)])
+@pytest.mark.parametrize("dtype", [BF16, E4M3])
+def test_bounds_of_a_page_that_sequences_hold_to_other_lengths(ctx, lengths, new, pack, many, dtype):
+    """Sequences that share their first two pages, the second held to different lengths by each, also by one whose new tokens lie
+    further on, and among more sequences than a warp has lanes: bounds of all keys that any of them holds, every time."""
+    k = kvx()
+    rest = [5] * 70 if many else []
+    case = Case([max(lengths)] + rest, block=16, pack=pack, dtype=dtype)
+    own = case.tables[:1].repeat(4, 1)
+    case.tables = torch.cat([own[:2], case.tables[1:], own[2:]])
+    case.lengths = list(lengths[:2]) + rest + list(lengths[2:])
+    case.upload()
+    boxes, sizes = case.bounds.boxes.cpu().clone(), case.bounds.sizes.cpu().clone()
+    case.want_bounds(boxes, sizes, new)
+    most = min(32, max(lengths)) - 16
+    i = case.number(0, 1)
+    boxes[i], sizes[i] = mixers.bounds_of(mixers.keys_of(case.pages, 0, case.tables[0], 1, most))
+    if max(lengths) > 32 and new < max(lengths):  # whose first pages are not made for its own sake
+        assert any(16 < n <= 32 for n in lengths)
+    for _ in range(5):
+        case.bounds.boxes.fill_(99)
+        case.bounds.sizes.fill_(9.0)
+        k.kv_bounds(ctx, case.pool, 0, case.batch, case.bounds, new_tokens=new)
+        torch.cuda.synchronize()
+        assert torch.equal(case.bounds.boxes.cpu(), boxes) and torch.equal(case.bounds.sizes.cpu(), sizes)
+
+
 def check_select(ctx, case, q, budget, sinks=1, recent=1, new=1, made=None, stream=None):
     """made: bounds (boxes, sizes) in place of the keys'."""
     k = kvx()
