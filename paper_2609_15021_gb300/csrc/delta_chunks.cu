@@ -11,9 +11,9 @@
 //
 // Rounding: keys and queries are fp16 numbers times a power of two a row, whose length is below 2^14 and above 2^12, so that a
 // bf16 number keeps its bits down to 2^-27 of that and is off by 2^-37 of it below.  The state, rhs and W's decayed copy are each
-// two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so is 2^9 T.  M and the W that it is multiplied with
-// are too for fp16 outputs, which would be off by 3.3e-4 where their own rounding gives 2.1e-4; for bf16 ones, whose rounding
-// gives 1.7e-3, they are rounded to fp16 once, which adds 2.5e-4 (squared, so nothing) and takes 4 % less time.  Sums are fp32.
+// two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so are 2^9 T, M and the W that M is multiplied with.
+// (Those two rounded to fp16 once put fp16 outputs off by 3.3e-4 where their own rounding gives 2.1e-4, and bf16 ones by 1.68e-3 instead
+// of 1.66e-3; 2,048 tokens then take 72 us instead of 74.)  Sums are fp32.
 //
 // What bounds it is the walk: chunks of a sequence follow on one another, and each is three products on end (S k, T rhs, the state's
 // update) with sums, scales and a barrier between, 3,200 to 3,900 cycles, with no unit near busy.  24k tokens in
@@ -38,10 +38,8 @@ constexpr float kLargest = 64.f;  // of T
 constexpr float kUp = 512.f;      // that T is multiplied by, as what a decay leaves of it is small, and rhs divided by
 
 // What the system kernel leaves of a chunk and head (offsets in bytes): a token's factors, then T and M, each in
-// two parts (M for bf16 in one), as 16 x 16 blocks on and below the diagonal, row by row.
+// two parts, as 16 x 16 blocks on and below the diagonal, row by row.
 constexpr int kTriangle = 10 * 512;
-template <class E>
-constexpr int kPartsOfM = std::is_same<E, Fp16>::value ? 2 : 1;
 struct Factors {
   float4 by[kChunk];    // of S k_t in rhs, of v_t less that, of w_t in the state, of S q_t in y
   float row[kChunk];    // M's row
@@ -308,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
       split2(mul2(make_float2(qk[j][2 * r], qk[j][2 * r + 1]), make_float2(up, up)), hi, lo);
       uint8_t* to = smem + S::kM + block_at(warp, j >> 1, g + 8 * r, j & 1) + 4 * c;
       *reinterpret_cast<uint32_t*>(to) = hi;
-      if constexpr (kPartsOfM<E> == 2) *reinterpret_cast<uint32_t*>(to + kTriangle) = lo;
+      *reinterpret_cast<uint32_t*>(to + kTriangle) = lo;
     }
   }
   __syncwarp();
@@ -389,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_consta
   }
   odd = __syncthreads_or(odd);
   if (threadIdx.x == 0) f.odd = odd;
-  for (int i = threadIdx.x; i < (2 + kPartsOfM<E>) * kTriangle / 16; i += kThreads)
+  for (int i = threadIdx.x; i < 4 * kTriangle / 16; i += kThreads)
     reinterpret_cast<uint4*>(head_to + kFactors)[i] = reinterpret_cast<const uint4*>(smem + S::kT)[i];
   __syncthreads();
   for (int i = threadIdx.x; i < kFactors / 16; i += kThreads)
@@ -449,7 +447,7 @@ __device__ __forceinline__ void left_factor(const float2 (&v)[4], uint8_t* hi, u
     l[k] = half2_of(rest.x, rest.y);
   }
   *reinterpret_cast<uint4*>(hi) = make_uint4(h[0], h[1], h[2], h[3]);
-  if (lo) *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
+  *reinterpret_cast<uint4*>(lo) = make_uint4(l[0], l[1], l[2], l[3]);
 }
 __device__ __forceinline__ void times(float2 (&v)[4], const float (&x)[4], const float (&y)[4], const float (&up)[2]) {
   v[0] = mul2(make_float2(x[0], x[1]), make_float2(up[0], up[0])), v[1] = mul2(make_float2(x[2], x[3]), make_float2(up[1], up[1]));
@@ -544,7 +542,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     bulk_load(to + 2 * kRowBytes<N>, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes, kFactors + 2 * kTriangle, bar);
   };
   auto load_m = [&](int32_t i) {
-    constexpr int kBytes = kPartsOfM<E> * kTriangle;
+    constexpr int kBytes = 2 * kTriangle;
     if (p.stall == 2 && i == 0) return;
     bar_expect(bars + 16, kBytes);
     bulk_load(base + W::kM, p.head_space + ((int64_t)(first + i) * p.heads + h) * kHeadBytes + kFactors + 2 * kTriangle, kBytes, bars + 16);
@@ -678,19 +676,15 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         uint32_t hi[4], lo[4], b[4], b_lo[4];
         left_load(hi, smem + W::kPlain + k * 1024 + lane * 16);
         load_matrices(b, base + W::kM + block_at(warp, k, b_row, b_vec));
-        if constexpr (kPartsOfM<E> == 2) {
-          left_load(lo, smem + W::kPlain + k * 1024 + 512 + lane * 16);
-          load_matrices(b_lo, base + W::kM + kTriangle + block_at(warp, k, b_row, b_vec));
-        }
+        left_load(lo, smem + W::kPlain + k * 1024 + 512 + lane * 16);
+        load_matrices(b_lo, base + W::kM + kTriangle + block_at(warp, k, b_row, b_vec));
         const float2 undo = plain_by[k * 8 + g];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           float x[4] = {};
           mma<Fp16>(x, hi, b[2 * u], b[2 * u + 1]);
-          if constexpr (kPartsOfM<E> == 2) {
-            mma<Fp16>(x, lo, b[2 * u], b[2 * u + 1]);
-            mma<Fp16>(x, hi, b_lo[2 * u], b_lo[2 * u + 1]);
-          }
+          mma<Fp16>(x, lo, b[2 * u], b[2 * u + 1]);
+          mma<Fp16>(x, hi, b_lo[2 * u], b_lo[2 * u + 1]);
           add_scaled(mw[u], x, undo);
         }
       }
@@ -843,7 +837,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         const Scaled by = scaled_for(w[0], w[1]);
         float2 x[4];
         times(x, w[0], w[1], by.up);
-        left_factor(x, smem + W::kPlain + warp * 1024 + lane * 16, kPartsOfM<E> == 2 ? smem + W::kPlain + warp * 1024 + 512 + lane * 16 : nullptr);
+        left_factor(x, smem + W::kPlain + warp * 1024 + lane * 16, smem + W::kPlain + warp * 1024 + 512 + lane * 16);
 #pragma unroll
         for (int k = 0; k < 4; ++k) x[k] = mul2(x[k], make_float2(write[k >> 1][0], write[k >> 1][1]));
         left_factor(x, smem + W::kWrite + warp * 1024 + lane * 16, smem + W::kWrite + warp * 1024 + 512 + lane * 16);

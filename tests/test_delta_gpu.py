@@ -170,6 +170,26 @@ def test_a_prompt_in_fp16_is_off_by_its_rounding(ctx):
     assert float(off.square().mean()) <= 1.1 * float(rounding.square().mean())
 
 
+@pytest.mark.parametrize("t,n", [(700, 128), (60, 64)])
+def test_a_prompt_in_bf16_is_off_by_its_rounding(ctx, t, n):
+    """As in fp16: what the factors' 2^-22 and the sums' 2^-20 or so of an output's terms add to the square of its rounding, 2^-9 to 2^-8
+    of it, is below 2^-20 of that even where the terms are 2^3 times the output.  (Factors rounded to fp16 once, 2^-11 at most
+    and half of that in the root mean square for either, would add some 2 % to the square.)"""
+    k = kvx()
+    heads = 2
+    st = Slots(2, heads, n, n, dtype=BF16)
+    batch, _ = batch_of([t], [0], [1], [1], False)
+    data = Inputs(t, heads, n, n, 1, BF16, seed=32)
+    out = torch.empty((t, heads, n), dtype=BF16, device="cuda")
+    k.kv_state_delta(ctx, st.slots, batch, out=out, A=data.A.cuda(), dt_bias=data.bias.cuda(),
+                     workspace=k.kv_state_delta_workspace(ctx, batch, heads, n, n), **data.cuda())
+    torch.cuda.synchronize()
+    x = data.cpu()
+    y = mixers.delta(x["query"], x["key"], x["value"], x["beta"], torch.zeros_like(st.state[0]), x["dt"], data.A, data.bias)[0]
+    rounding, off = y.bfloat16().double() - y, out.cpu().double() - y
+    assert float(off.square().mean()) <= 1.002 * float(rounding.square().mean())
+
+
 @pytest.mark.parametrize("softplus,sigmoid,normalize,bias", [(False, True, True, False), (True, False, True, True), (True, True, False, False),
                                                              (False, False, False, False)])
 def test_options(ctx, softplus, sigmoid, normalize, bias):
