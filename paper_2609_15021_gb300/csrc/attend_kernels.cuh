@@ -35,9 +35,9 @@
 // a bf16 value is lost within 2^-24 of the row's largest.  Probabilities are rounded to the
 // cache's type (fp16 for e4m3) for the product with V; the sums they are divided by are not.  That is 2^-9 of a term, of
 // either sign: in bf16 an output is off by some 2.1e-3 where its own rounding gives 1.6e-3, and a second part of each
-// probability would take the product twice.  Over selected pages the sums are divided by what the rounded probabilities
-// add up to (a part is scaled by the true sum over that, so that parts join and logarithms stay as they are): a row
-// that one key dominates, as such pages are picked for, then has that key's error cancelled.
+// probability would take the product twice.  Over selected pages, of which there are few, it does: what rounding takes
+// of a probability is a second factor of V in the same type, and an output is off by its own rounding alone (1.6e-3 in bf16,
+// where one part gives 1.9e-3 even if sums are those of the rounded probabilities; times are the same within 2 %).
 //
 // Measured: bf16, sequences of 21k and 32.8k tokens, 8 heads x 128 with 8 query rows each, weights kept (220 MB of
 // K/V): 45 us; fp16, 45 sequences of up to 16k tokens, 8 heads x 96 with 2 rows, cap and slopes (270 MB): 60 us; both
@@ -455,7 +455,6 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         for (int e = 0; e < 4; ++e) acc[c][t][e] = 0.f;
     // rows 2 sub and 2 sub + 1 of each tile: what exponents are relative to, and the sums over this lane's keys
     float m[kTiles][2], l[kTiles][2], scale2[kTiles][2];
-    float rounded[kTiles][2] = {};  // kSelected: what rounding added to the probabilities
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -582,13 +581,12 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
             const float keep = factor(m[t][j], top);
             m[t][j] = top;
             l[t][j] *= keep;
-            if constexpr (kSelected) rounded[t][j] *= keep;
 #pragma unroll
             for (int c = 0; c < kKs; ++c) acc[c][t][j] *= keep, acc[c][t][2 + j] *= keep;
           }
       }
       uint32_t pf[kBlocks][kTiles][2];
-      float added[kTiles][2] = {};
+      [[maybe_unused]] uint32_t pf_rest[kBlocks][kTiles][2];  // kSelected: what rounding took
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         const float ref[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
@@ -603,8 +601,8 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
           for (int k = 0; k < 2; ++k) {
             const uint32_t pair = pack2<C>(sc[n][t][2 * k], sc[n][t][2 * k + 1]);
             if constexpr (kSelected) {
-              const float2 x = unpack2<C>(pair);
-              added[t][0] += x.x - sc[n][t][2 * k], added[t][1] += x.y - sc[n][t][2 * k + 1];
+              const float2 x = fma2(unpack2<C>(pair), make_float2(-1.f, -1.f), make_float2(sc[n][t][2 * k], sc[n][t][2 * k + 1]));
+              pf_rest[n][t][k] = transpose(pack2<C>(x.x, x.y));
             }
             pf[n][t][k] = transpose(pair);
           }
@@ -630,10 +628,13 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
         odd = __any_sync(~0u, odd);
       }
       if (!odd) {
-        if constexpr (kSelected) {
+        auto add = [&](int n, int c, const uint32_t (&a)[4]) {
 #pragma unroll
-          for (int t = 0; t < kTiles; ++t) rounded[t][0] += added[t][0], rounded[t][1] += added[t][1];
-        }
+          for (int t = 0; t < kTiles; ++t) {
+            mma<C>(acc[c][t], a, pf[n][t][0], pf[n][t][1]);
+            if constexpr (kSelected) mma<C>(acc[c][t], a, pf_rest[n][t][0], pf_rest[n][t][1]);
+          }
+        };
 #pragma unroll
         for (int c = 0; c < kKs; c += kWide ? 2 : 1) {
 #pragma unroll
@@ -641,8 +642,7 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
             uint32_t b[4];
             if constexpr (!kWide) {
               load_matrices_t(b, at_v + n * 16 * S::kPitch + c * 32);
-#pragma unroll
-              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c][t], b, pf[n][t][0], pf[n][t][1]);
+              add(n, c, b);
             } else {
               // a transposed pair of bytes is two neighbouring dims of a key: the even ones are the product's
               // first eight rows, the odd ones the others
@@ -652,12 +652,10 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
               uint32_t a[4];
               widen4(b[0], a[0], a[1]);
               widen4(b[1], a[2], a[3]);
-#pragma unroll
-              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c][t], a, pf[n][t][0], pf[n][t][1]);
+              add(n, c, a);
               widen4(b[2], a[0], a[1]);
               widen4(b[3], a[2], a[3]);
-#pragma unroll
-              for (int t = 0; t < kTiles; ++t) mma<C>(acc[c + 1][t], a, pf[n][t][0], pf[n][t][1]);
+              add(n, c + 1, a);
             }
           }
         }
@@ -710,11 +708,6 @@ __global__ void __launch_bounds__(AttendShape<C, kDim, kTiles>::kThreads, Attend
       for (int j = 0; j < 2; ++j) {
         const int r = t * 8 + 2 * sub + j;
         const float sum = column_sum(l[t][j]);
-        if constexpr (kSelected) {
-          const float taken = sum + column_sum(rounded[t][j]), by = taken > 0.f ? sum / taken : 1.f;
-#pragma unroll
-          for (int c = 0; c < kKs; ++c) acc[c][t][j] *= by, acc[c][t][2 + j] *= by;
-        }
         if (r >= here) continue;
         if (quad == 0) {
           stats[2 * (warp * kRows + r)] = m[t][j];

@@ -338,6 +338,21 @@ def test_a_key_that_dominates_gives_its_value(ctx, dtype, cache):
     assert bool(((out.cpu().double() - want).abs() <= 5e-7 + 5 * 2.0 ** -21).all())
 
 
+@pytest.mark.parametrize("dtype,cache,dim,group", [(BF16, BF16, 128, 4), (FP16, FP16, 96, 2), (BF16, E4M3, 256, 6), (FP16, E4M3, 128, 4),
+                                                   (BF16, BF16, 256, 20)])
+def test_selected_attention_is_off_by_its_rounding(ctx, dtype, cache, dim, group):
+    """Probabilities in two parts are off by 2^-17 of themselves in bf16 and 2^-22 in fp16, scores and sums by some 2^-20: against an
+    output's own rounding, 2^-9 / sqrt(3) or 2^-12 / sqrt(3) of it and more in the root mean square, less than 2^-6 of
+    that, and 2^-12 of its square.  (Rounded once, a probability is off by as much as an output.)"""
+    case = Case([3000, 700, 90], dim=dim, dtype=cache, seed=43)
+    q = normal((3, 2 * group, dim), dtype, 44)
+    sel = some_pages(case, 1, 60, 45)
+    out, _ = attend(ctx, case, q, sel)
+    want = mixers.attend_selected(case.pages, 0, case.tables, case.lengths, q, 1, sel, 1 / math.sqrt(dim))[0]
+    rounding, off = want.to(dtype).double() - want, out.cpu().double() - want
+    assert float(off.square().mean()) <= 1.002 * float(rounding.square().mean())
+
+
 @pytest.mark.parametrize("cache", [BF16, FP16, E4M3])
 @pytest.mark.parametrize("dim,group,new", [(64, 1, 5), (64, 9, 2), (128, 8, 3), (128, 17, 1), (128, 40, 2), (256, 6, 4), (256, 20, 1), (96, 33, 1)])
 def test_many_query_rows_and_new_tokens(ctx, cache, dim, group, new):
