@@ -801,8 +801,10 @@ kvx_status kv_append_rotary(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, c
  * The bounds of one layer's pages: of every page and head the least and the greatest value that each element of
  * the keys it holds takes, as whole numbers of a size of its own,
  *   size = max |k| / 127,  low = floor(min k / size),  high = ceil(max k / size),
- * as stored (an e4m3 cache's scale is left out).  A page head that holds a key that is not finite gets the widest bounds
- * and the largest finite size, so that it is picked before all others.
+ * as stored (an e4m3 cache's scale is left out), the quotients in 32 bits to the nearest: low * size and high * size miss a
+ * key by at most 2^-24 of max |k| (and 2^-143).  A page head that holds a key that is not finite gets the widest bounds
+ * and the largest finite size, so that no page's score is above its own.  (Where all of a head's query rows are zeros or not
+ * finite every page's score is 0, and the lowest pages are picked.)
  */
 typedef struct {
   int8_t* boxes; /* device [num_blocks][num_heads][2 (low, high)][head_dim]         */

@@ -3,8 +3,9 @@
 //   score(page) = max over the head's query rows of step * (w+ . high + w- . low), times the page's size
 //
 // with w+ and w- the positive and the negative part of the row rounded to whole numbers of its step, low and high the page's
-// bounds: one product over twice the elements, and no less than the rounded row's product with any key of the page.  Everything
-// in it is whole and below 2^24, so the order of the sums does not show, and the same pages are picked whatever the batch.
+// bounds: one product over twice the elements, and no less than the rounded row's product with any key of the page but for what rounding
+// sizes and quotients to the nearest leaves a bound short by, 2^-24 of the page's largest element (a whole number of a
+// size is 2^-7 of it).  Everything in the sum is whole and below 2^24, so its order does not show, and the same pages are picked whatever the batch.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>

@@ -225,3 +225,36 @@ def test_search_for_the_last_picked_page_ends(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-I", csrc, str(src), "-o", str(tmp_path / "search")], check=True)
     done = subprocess.run([str(tmp_path / "search")], capture_output=True, text=True, timeout=60)
     assert done.returncode == 0 and done.stdout == "ok\n", done.stdout
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_bounds_miss_a_key_by_no_more_than_they_say(dtype):
+    """A size and a quotient are each off by 2^-24 of themselves at most, so bounds times sizes miss a key by 2^-24 of the largest,
+    and a score the rounded rows' largest product by as much of its terms for each of the bounds and its two products; some do
+    miss.  A page with a key that is not finite has the largest score, and no query but zeros or odd ones gives every page 0."""
+    g = torch.Generator().manual_seed(2)
+    unit, missed = 2.0 ** -24, 0
+    for scale in (1.0, 3e-3, 700.0, 1e-38 if dtype is torch.bfloat16 else 1e-6):
+        keys = (torch.randn((40, 16, 2, 64), generator=g) * scale).to(dtype)
+        boxes, sizes = (torch.stack(x) for x in zip(*(refs.bounds_of(k_) for k_ in keys)))
+        by, k64 = sizes.double()[:, :, None], keys.double()
+        low, high = boxes[:, :, 0].double() * by, boxes[:, :, 1].double() * by
+        slack = unit * k64.abs().amax((1, 3))[:, :, None] + 2.0 ** -143
+        assert bool((low <= k64.amin(1) + slack).all()) and bool((high >= k64.amax(1) - slack).all())
+        missed += int((low > k64.amin(1)).sum()) + int((high < k64.amax(1)).sum())
+        q = torch.randn((4, 64), generator=g)
+        score = refs.scores_of(q, boxes, sizes, 2).double()
+        step = (q.abs().amax(-1, keepdim=True) / 127).double()
+        rows = torch.round(q / step.float()).double() * step
+        for h in range(2):
+            most = torch.einsum("rd,ptd->prt", rows[2 * h:2 * h + 2], k64[:, :, h]).amax((1, 2))
+            terms = rows[2 * h:2 * h + 2].abs().sum(-1).max() * k64[:, :, h].abs().amax((1, 2))
+            assert bool((score[h] >= most - 4 * unit * terms - 2.0 ** -130).all())
+    assert missed > 0
+    odd = keys.clone()
+    odd[7, 3, 0, 9] = math.nan
+    boxes, sizes = (torch.stack(x) for x in zip(*(refs.bounds_of(k_) for k_ in odd)))
+    assert int(refs.scores_of(torch.randn((2, 64), generator=g), boxes, sizes, 2)[0].argmax()) == 7
+    for q in (torch.zeros((2, 64)), torch.full((2, 64), math.nan)):
+        scores = refs.scores_of(q, boxes, sizes, 2)
+        assert not bool(scores.any()) and refs.pick(scores[0], 40, 3, 0, 1) == [0, 1, 39]
