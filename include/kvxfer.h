@@ -775,7 +775,8 @@ kvx_status kv_attend(kvx_ctx* ctx, const kvx_pool* pool, int32_t layer, const kv
  * For every head of q and key, in 32 bits and rounded once:
  *   x = x / sqrt(mean(x^2) + eps) * (weight + weight_offset)      where there is a weight
  *   (a, b) = (a cos - b sin, b cos + a sin) * rotary_scale         of the pairs of the first rotary_dim elements,
- * the i'th pair by the angle position * inv_freq[i], whose full turns are taken off in 64 bits.  q goes to q_out (which may
+ * the i'th pair by the angle position * inv_freq[i], whose full turns are taken off in 64 bits, to within
+ * |position| (1 + |inv_freq[i]|) 2^-64 turns before its rounding to 32 (NaN where inv_freq[i] is not finite).  q goes to q_out (which may
  * be q itself, and else may not lie over q, key or value), key and value to the pages as kv_append puts them there.  A token
  * that belongs to no sequence leaves its row of q_out as it was; one before position 0 or of a bad page still gets its row.
  */

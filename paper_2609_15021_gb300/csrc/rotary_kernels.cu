@@ -28,7 +28,7 @@ constexpr int kRotaryThreads = 128, kRotaryWarps = kRotaryThreads / 32;
 constexpr int kMaxPairs = 128;
 constexpr int kRotaryBatch = 4;  // rows' vectors that a lane has in flight
 
-// position * f / 2 pi less its whole part, from -1/2 to 1/2.
+// position * f / 2 pi less its whole part, from -1/2 to 1/2; NaN for an f that is not finite.
 __device__ __forceinline__ float turn_of(int64_t position, float f) {
   const uint32_t bits = __float_as_uint(f);
   const int s = 150 - (int)(bits >> 23 & 255);  // f = m 2^-s
@@ -43,7 +43,7 @@ __device__ __forceinline__ float turn_of(int64_t position, float f) {
     turns = s < 128 ? hi >> (s - 64) : 0;
   turns *= (uint64_t)position;
   const float t = __ll2float_rn((int64_t)turns) * 0x1p-64f;
-  return f < 0.f ? -t : t;
+  return (bits & 0x7F800000u) == 0x7F800000u ? NAN : f < 0.f ? -t : t;
 }
 
 enum { kNoTurn, kNeighbours, kVectors, kElements };  // how elements are paired

@@ -211,6 +211,34 @@ def test_infinities_and_nan_stay_in_their_rows(ctx):
         assert odd.tolist() == [[False, row == 7], [False, False]]
 
 
+def test_frequencies_that_are_not_finite_or_reach_around_many_times(ctx):
+    """Pairs of a frequency that is no number are none; the others are as without it.  Angles of whole turns' many, at places of up to
+    2^31, against whole-number arithmetic: within (1 + f) 2^-33 turns and what 32 bits leave of a turn and of its sine, 2^-21 in all."""
+    k = kvx()
+    pi = 31415926535897932384626433832795028841971693993751058209749445923  # over 10^64
+    freq = torch.tensor([1.0, math.nan, 100.0, math.inf, 3e-7, -math.inf, 0.7, 977.25], dtype=torch.float32)
+    places = [0, 1, 2 ** 20 + 1, 2 ** 31 - 1]
+    st = Step([4], [4], dim=16, dtype=FP16)
+    st.qkv[:, :4, :8], st.qkv[:, :4, 8:] = 1.0, 0.0  # rows that become cosines and sines
+    out = torch.zeros((4, 4, 16), dtype=FP16, device="cuda")
+    qkv = st.qkv.cuda()
+    k.kv_append_rotary(ctx, st.pool, 0, st.batch, k.KvRotary(4, freq.cuda()), qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], out, positions=ints(places),
+                       new_tokens=4)
+    got = out.cpu().double()
+    for i, f in enumerate(freq.tolist()):
+        for t, place in enumerate(places):
+            pair = got[t, 0, [i, i + 8]]
+            if not math.isfinite(f):
+                assert bool(torch.isnan(pair).all()), (i, t)
+                continue
+            over, under = f.as_integer_ratio()
+            top, bottom = over * place * 10 ** 64, under * 2 * pi  # turns
+            angle = 2 * math.pi * ((top % bottom) / bottom)
+            off = 2 * math.pi * (1 + f) * 2.0 ** -33 + 2.0 ** -21
+            for have, want in zip(pair.tolist(), (math.cos(angle), math.sin(angle))):
+                assert abs(have - want) <= off + 2.0 ** -11 * abs(want) + 2.0 ** -25, (f, place)
+
+
 def test_missing_pages_are_left_out_and_reported(ctx):
     k = kvx()
     st = Step([40, 20], [30, 4])
