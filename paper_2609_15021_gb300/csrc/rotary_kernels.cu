@@ -243,10 +243,12 @@ template <class E, int kLanes>
 cudaError_t rotary(const RotaryParams& p, bool fp8, int num_sms, cudaStream_t s) {
   constexpr int kEach = 32 / kLanes * kRotaryBatch;
   const int32_t units = (p.q_heads + kEach - 1) / kEach + 2 * ((p.append.pages.heads + kEach - 1) / kEach);
-  // Few tokens: a warp a unit.  Of 32 + 2 x 8 heads x 128, in a graph: 64 tokens 6.8 us, 12.4 with a warp a token; 608 tokens 12.3
-  // either way; 1,216 tokens 16.4 and 12.5, 4,864 51.4 and 26.8, as every unit of a token makes its sines and factors again.
+  // Few tokens: a warp a unit, as one a token leaves SMs idle; many: a warp a token, as every unit makes its sines and factors
+  // again.  With a warp a unit and a warp a token, in a graph, us, of 2, 4, 6 and 8 tokens an SM: 32 + 2 x 8 heads x 128 5.2 8.5 11.5 12.5 and
+  // 8.0 8.1 8.8 8.9; 16 + 2 x 8 x 96 4.9 5.3 9.1 9.6 and 7.4 7.4 7.8 7.9; 24 + 2 x 4 x 256 into e4m3 6.5 11.5 15.9 20.1 and 10.5 10.6 11.6
+  // 11.6; 4 + 2 x 2 x 64 4.1 4.6 7.5 7.6 and 5.6 5.5 5.9 5.9; 64 + 2 x 8 x 128 8.2 11.8 15.6 19.7 and 10.6 10.6 11.7 11.8.
   RotaryParams q = p;
-  q.parts = p.append.tokens >= 8 * num_sms ? 1 : units;
+  q.parts = p.append.tokens > 4 * num_sms ? 1 : units;
   q.inverse_dim = 1.f / p.append.pages.head_dim;
   const dim3 grid((unsigned)((p.append.tokens * q.parts + kRotaryWarps - 1) / kRotaryWarps));
   auto launch = [&](auto pairs) {

@@ -152,6 +152,25 @@ def test_heads_and_many_tokens(ctx, heads, q_heads, tokens):
     check(ctx, st, frequencies(32), False, [normal((64,), FP16, 3, 0.1) + 1] * 2)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_a_warp_a_token_and_a_warp_a_unit_give_the_same_bits(ctx, interleaved):
+    """A call of few tokens an SM and one of many share their rows: what becomes of a row does not depend on the others."""
+    k = kvx()
+    few = 4 * torch.cuda.get_device_properties(0).multi_processor_count
+    rotary = k.KvRotary(4, frequencies(32).cuda(), interleaved=interleaved, q_weight=normal((64,), BF16, 6, 0.1).cuda(),
+                        k_weight=normal((64,), BF16, 7, 0.1).cuda())
+    for dtype, cache in ((BF16, BF16), (BF16, E4M3)):
+        got = []
+        for rows in (few, few + 1):
+            st = Step([few + 1], [few + 1], dtype=dtype, cache=cache)
+            batch = k.KvBatch(st.tables.cuda(), ints([rows]), max_length=few + 1)
+            qkv, out = st.qkv.cuda()[:rows], torch.zeros((rows, 4, 64), dtype=dtype, device="cuda")
+            k.kv_append_rotary(ctx, st.pool, 0, batch, rotary, qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], out, new_tokens=rows)
+            st.pages.data = st.dev.cpu()[None]
+            got.append((out[:few].view(torch.int16).cpu(), st.pages.rows(0, st.tables[0], range(few)).view(torch.uint8)))
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
 def test_more_sequences_than_a_warp_has_lanes(ctx):
     new = [i % 4 for i in range(75)]
     st = Step([n + 7 * i for i, n in enumerate(new)], new, spare=2)
