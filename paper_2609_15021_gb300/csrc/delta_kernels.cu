@@ -47,9 +47,11 @@ cudaError_t delta(const DeltaParams& p, int num_sms, cudaStream_t s) {
 }  // namespace
 
 bool delta_by_chunks(int64_t tokens, int32_t num_seqs, bool packed, int32_t state_dim, int32_t* by_token) {
-  // 16 heads of 128 x 128, in a graph: a sequence of 16 tokens takes 14.5 us token by token and 16.5 by chunks, which take no
-  // longer for 64, and one of 24 tokens 20.6; four of 24 tokens 34 and 31, of 16 tokens 23 and 31; sixteen of 16 tokens
-  // 51 and 80, of 24 tokens 74 and 80, of 32 tokens 146 (in launches of their own) and 80.
+  // A chunk takes the same for 8 tokens as for 64, so both meet at some number of tokens: at 20 of one sequence and 22 of two (16
+  // heads of 128 x 128), at 34 to 38 of four to sixteen; of 8 heads at 22 for up to four sequences, of 16 of 64 x 64 at 18, 22, 27, 32 and 42 for one
+  // to sixteen.  In a graph, us token by token and by chunks, of 16 heads of 128 x 128: one of 16 tokens 11.9 and 14.2, of 24 16.6 and
+  // 14.2; two of 24 20.9 and 19.5; four of 24 21.8 and 29.4, of 32 27.9 and 29.6; sixteen of 24 52 and 79, of 32 68 and 79.  24 is near
+  // where few sequences meet; that many of 25 to 34 tokens go by chunks costs them up to a third.
   const int32_t few = num_seqs > 1 ? 24 : 16;
   *by_token = INT32_MAX;
   if (!packed || (state_dim != 64 && state_dim != 128) || tokens <= few) return false;
