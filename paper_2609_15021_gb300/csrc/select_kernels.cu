@@ -81,28 +81,22 @@ __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_con
   const int32_t length = length_of(v, s), block = (int32_t)v.by_block.d;
   const int32_t page = (int32_t)quotient(v.by_block, (uint32_t)max(length - p.new_tokens, 0)) + 2 * n;  // and the next
   // The sequence's last page may be another's too, which holds more of it: its bounds are those of all keys that any
-  // sequence of the batch holds there, so that all warps that make them write the same.  The CTA that has that page looks for it
-  // (a token of each of 48 sequences 3.1 us in a graph, 2.4 without; of 512 5.3 and 4.0, of 2,000 23 and 13).
+  // sequence of the batch holds there, so that all warps that make them write the same.  (A token of each of 48 sequences
+  // takes 3.2 us in a graph, 2.4 without the search; of 512 6.8 and 4.0, of 2,000 38 and 13.  A search by the CTA, whose barrier the compiler orders
+  // all loads around, takes 5.2 of 512, and two long caches 22.5 instead of 21.2.)
   int32_t reach = length;
   const int32_t last = (int32_t)quotient(v.by_block, (uint32_t)max(length - 1, 0));
-  const int32_t unit0 = (int32_t)blockIdx.x * kWarps, first = page - 2 * n;
-  if (v.num_seqs > 1 && length > 0 && length - last * block < block && last >= first + 2 * (int32_t)quotient(p.by_heads, (uint32_t)unit0) &&
-      last <= first + 2 * (int32_t)quotient(p.by_heads, (uint32_t)(unit0 + kWarps - 1)) + 1) {
-    __shared__ int32_t reach_s[kWarps];
+  if (v.num_seqs > 1 && length > 0 && length - last * block < block && (page == last || page + 1 == last)) {
     const uint32_t at = quotient(v.by_pack, (uint32_t)last);
     if (at < v.table_len) {
       const int32_t entry = __ldg(v.tables + s * v.table_stride + at);
 #pragma unroll 4
-      for (int32_t other = threadIdx.x; other < v.num_seqs; other += kBoundsThreads) {
+      for (int32_t other = lane; other < v.num_seqs; other += 32) {
         const int32_t held = length_of(v, other);
         if (held > length && __ldg(v.tables + other * v.table_stride + at) == entry) reach = max(reach, held);
       }
     }
     reach = __reduce_max_sync(~0u, reach);
-    if (lane == 0) reach_s[threadIdx.x >> 5] = reach;
-    __syncthreads();
-    reach = __reduce_max_sync(~0u, reach_s[lane % kWarps]);
-    if (page != last && page + 1 != last) reach = length;
   }
   uint32_t row[2];
 #pragma unroll
