@@ -37,7 +37,7 @@
 // either sign: in bf16 an output is off by some 2.1e-3 where its own rounding gives 1.6e-3, and a second part of each
 // probability would take the product twice.  Over selected pages, of which there are few, it does: what rounding takes
 // of a probability is a second factor of V in the same type, and an output is off by its own rounding alone (1.6e-3 in bf16,
-// where one part gives 1.9e-3 even if sums are those of the rounded probabilities; times are the same within 2 %).
+// where one part gives 1.9e-3 even if sums are those of the rounded probabilities; times are the same within 3 %).
 //
 // Measured: bf16, sequences of 21k and 32.8k tokens, 8 heads x 128 with 8 query rows each, weights kept (220 MB of
 // K/V): 45 us; fp16, 45 sequences of up to 16k tokens, 8 heads x 96 with 2 rows, cap and slopes (270 MB): 60 us; both
@@ -46,7 +46,7 @@
 // are two warps a scheduler and little to hide a step's dependent products and conversions behind.
 //
 // Over selected pages: four sequences of 99k to 127k tokens, 4 heads x 256 in e4m3, four queries of 6 rows a head with 128 pages
-// of 32 tokens each (134 MB): 35 us, 3.9 TB/s; one query of 8 x 128 in bf16 over 64 pages of 16 (4 MB): 9.4 us.
+// of 32 tokens each (134 MB): 36 us, 3.7 TB/s; one query of 8 x 128 in bf16 over 64 pages of 16 (4 MB): 9.4 us.
 #pragma once
 
 #include <algorithm>

@@ -13,12 +13,12 @@
 // bf16 number keeps its bits down to 2^-27 of that and is off by 2^-37 of it below.  The state, rhs and W's decayed copy are each
 // two fp16 numbers, 22 bits, times a power of two a row and 16 columns, and so are 2^9 T, M and the W that M is multiplied with.
 // (Those two rounded to fp16 once put fp16 outputs off by 3.3e-4 where their own rounding gives 2.1e-4, and bf16 ones by 1.68e-3 instead
-// of 1.66e-3; 2,048 tokens then take 72 us instead of 74.)  Sums are fp32.
+// of 1.66e-3, for 3 % less time.)  Sums are fp32.
 //
 // What bounds it is the walk: chunks of a sequence follow on one another, and each is three products on end (S k, T rhs, the state's
 // update) with sums, scales and a barrier between, 3,200 to 3,900 cycles, with no unit near busy.  24k tokens in
-// six sequences, 16 heads of 128 x 128, fp16: 731 us, of which the systems are 148 and the walk 589, 282 chunks on end; 2,048 tokens in
-// one, bf16: 73 us, 16 and 57.  16 rows of the state a CTA, as a matrix instruction has 16, make 128 CTAs of a sequence of 16 heads of
+// six sequences, 16 heads of 128 x 128, fp16: 728 us (under the profiler the systems are 150 and the walk 589, 282 chunks on end); 2,048 tokens in
+// one, bf16: 75 us (18 and 60).  16 rows of the state a CTA, as a matrix instruction has 16, make 128 CTAs of a sequence of 16 heads of
 // 128.  (Token by token it is 0.6 us a token.)
 //
 // A chunk with a number that is not finite, a decay above 1 or a T above 64 (keys with b |k|^2 well above 2) goes token
@@ -84,9 +84,9 @@ __device__ __forceinline__ void split2(float2 x, uint32_t& hi, uint32_t& lo) {
 
 // A chunk and head a CTA, 16 of its tokens a warp; before them the CTAs of the sequences that go token by token, which
 // nothing here waits for (a launch of their own took 6 us more).  T is made block by block: on the diagonal by substitution, below it as
-// T_ij = -T_ii sum_{j<=k<i} A_ik T_kj, a column of blocks a warp, by products of numbers in two parts (24k tokens of 16 heads 141 us;
-// 184 with columns by substitution in 32-bit floats, whose longest is the first warp's).  Bound by instructions, 3,400 a warp, and
-// by what it reads and writes, which is 81 us of those 141 at the DRAM's rate.
+// T_ij = -T_ii sum_{j<=k<i} A_ik T_kj, a column of blocks a warp, by products of numbers in two parts (24k tokens of 16 heads 150 us under
+// the profiler, and 30 % more with columns by substitution in 32-bit floats, whose longest is the first warp's).  Bound by instructions,
+// 3,400 a warp, and by what it reads and writes, which is 81 us of those 150 at the DRAM's rate.
 template <class E, int N>
 __global__ void __launch_bounds__(kThreads, 5) system_kernel(const __grid_constant__ DeltaParams p) {
   wait_for_previous();
@@ -470,8 +470,9 @@ __device__ __forceinline__ void meet(int id) { asm volatile("bar.sync %0, %1;" :
 // A CTA walks with 16 rows of one head's state: four warps have the state in registers, a quarter of its columns each, and make rhs
 // and W, 16 tokens each; four make the outputs beside the next chunk's first product; one copies chunks, a chunk ahead.  (With
 // four warps for all of it, and what does not wait loaded behind the barriers, a chunk took 3,900 cycles instead of 3,200; a thread
-// of the chain that issues the copies costs 300 of these.  Not taken: eight warps for the state with 8 tokens each, 146 us for 2,048 tokens instead of 70, as
-// all read the state's fragments and shared memory is the bound; the products on tcgen05, 97 us, as one takes 680 cycles from
+// of the chain that issues the copies costs 300 of these.  Not taken, and measured against 70 us for 2,048 tokens, before bf16 outputs' products had two parts:
+// eight warps for the state with 8 tokens each, 146, as all read the state's fragments and shared memory is the bound; the products on
+// tcgen05, 97, as one takes 680 cycles from
 // its issue to the warps that wait for it, three times a chunk, where mma.sync's steps take 20.)
 template <class E, int N>
 __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_constant__ DeltaParams p) {

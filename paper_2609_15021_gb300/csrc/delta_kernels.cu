@@ -3,7 +3,7 @@
 //   S_t = a_t S_{t-1} + b_t (v_t - a_t S_{t-1} k_t) k_t^T,   y_t = S_t q_t
 //
 // Rows of the state know nothing of one another, and stay in registers from the first token of a sequence to the last.  One token
-// of each sequence is bound by the state's bytes: 96 sequences of 16 heads x 128 x 128 (201 MB) take 34 us, 88 % of the DRAM's
+// of each sequence is bound by the state's bytes: 96 sequences of 16 heads x 128 x 128 (201 MB) take 34 us, 89 % of the DRAM's
 // rate; of several tokens a chain of two sums over a row and what the token before wrote, 0.6 us a token.
 #include <algorithm>
 

@@ -65,9 +65,10 @@ struct Divisor {
 // rows at once, and meet at the end, the second page's rows under way; then, where a row is half a warp, one half makes the low
 // bounds and the other the high ones.  C: the type that keys are compared in
 // (fp16 for e4m3).  Bound by the keys' bytes, of which a lane has eight rows' in
-// flight: 2 sequences of 21k and 32.8k tokens, 8 heads x 128, bf16 (117 MB with the bounds): 21 us, 83 % of the DRAM's rate (in a graph 23; 27 with one page a
-// warp, 29 where a page's loads were not all made first).  After a step's append it has a page a sequence, and takes the 5 us
-// that a launch and four loads on end take.
+// flight: 2 sequences of 21k and 32.8k tokens, 8 heads x 128, bf16 (117 MB with the bounds): 21 us among other
+// calls, 81 % of the DRAM's rate (alone in a graph, whose beginning nothing hides, 25; two pages a warp took 4 less than one, and all of a page's
+// loads made first 2 less).  After a step's append it has a page a sequence, and is a launch and four loads on end, 2.3 us in a graph of
+// such calls.
 template <class C, bool kWide, int kVecs>  // kVecs: vectors of a row, rounded up to a power of two
 __global__ void __launch_bounds__(kBoundsThreads) bounds_kernel(const __grid_constant__ BoundsParams p) {
   wait_for_previous();
